@@ -511,6 +511,111 @@ int nvq_precision_from_scores(const double *scores, int L, double tau, double ep
                               int32_t *out);
 
 /*
+ * Microscaled 4-bit floating point (the MXFP4 format of the OCP Microscaling
+ * Formats specification 1.0): blocks of 32 values that lie next to each other in
+ * K share a scale 2^(byte - 127) kept as that byte; a value is code * scale, the
+ * code one of 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives (sign bit, two bits
+ * of exponent, one of mantissa: codes 0..7 in this order, 8..15 negative).
+ *   q[m][k/2]        low nibble = element k, high nibble = element k + 1 (k even)
+ *   scales[m][k/32]  one byte; 255 stands for no number (NaN)
+ * 17 bytes per 32 values = 4.25 bits per value.  The same layout holds weights
+ * ([N][K]) and activations ([M][K]).  q, x and bf16 outputs are 16-byte aligned;
+ * scales have no alignment beyond what an entry point states.
+ *
+ * nvq_quant_mxfp4 -- byte = max(floor(log2(absmax)) + 125, 0) of a block, code =
+ * the value nearest to x / scale, ties to the even code, magnitudes beyond 6 become 6
+ * (the specification's conversion); a block that holds an infinity or a NaN gets
+ * byte 255 and zero codes.  The sign of zero is kept.  x [M][K] fp32 or bf16
+ * (x_dtype, the y_dtype constants); scales 4-byte aligned.
+ * nvq_dequant_mxfp4 -- out[m][k] = code * scale as bf16, exact (blocks of byte 255:
+ * NaN; values of byte 253 and 254 beyond the type's range: infinite).
+ * K % 32 == 0, any M.  Errors as for the other entry points.
+ */
+int nvq_quant_mxfp4(const void *x, int x_dtype, int64_t M, int64_t K, uint8_t *q, uint8_t *scales,
+                    void *stream);
+int nvq_dequant_mxfp4(const uint8_t *q, const uint8_t *scales, int64_t M, int64_t K,
+                      uint16_t *out_bf16, void *stream);
+
+/*
+ * nvq_gemv_mxfp4 -- y[m][n] = sum_k w[n][k] * x[m][k] for microscaled weights and
+ * bf16 activations of 1 <= M <= NVQ_MAX_M tokens; neither is rounded (the
+ * counterpart of nvq_gemv_w4a16), sums in fp32.
+ *   qweight [N][K/2], scales [N][K/32], x_bf16 [M][K], y [M][N] (y_dtype)
+ *
+ * nvq_gemm_mxfp4 -- the same product with both operands microscaled, for any M
+ * (prompts; the activations come from nvq_quant_mxfp4): y[m][n] = sum_k w[n][k] *
+ * xv[m][k], xv the values that xq and xscale stand for, on the scaled matrix
+ * instructions, sums in fp32.
+ *   xq [M][K/2], xscale [M][K/32]
+ * A result depends neither on the other tokens of the call nor on their number in
+ * the first one's two kernels (up to 16 tokens and beyond) taken each by itself; both
+ * may add in another order at other sizes.
+ */
+int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int N, int K,
+                   const uint16_t *x_bf16, int M, void *y, int y_dtype, void *stream);
+int nvq_gemm_mxfp4(const uint8_t *qweight, const uint8_t *scales, int64_t N, int64_t K,
+                   const uint8_t *xq, const uint8_t *xscale, int64_t M, void *y, int y_dtype,
+                   void *stream);
+
+/*
+ * A mixture-of-experts feed-forward layer for 1 <= M <= NVQ_MAX_M tokens: the
+ * router in one launch, the experts in two.
+ *
+ * nvq_moe_route -- logit[m][e] = sum_k x[m][k] * router[e][k] (bf16 operands, fp32
+ * sums); ids[m][0 .. top_k) = the experts of the top_k largest logits, in
+ * descending order, the lowest index first among equal ones; weights[m][s] =
+ * exp(logit of ids[m][s]) / sum of exp(logit) over the chosen experts (renormalise =
+ * 1) or over all E (renormalise = 0).  A NaN logit counts as the smallest; the ids of
+ * a token are distinct and in [0, E) whatever the inputs.
+ *   x_bf16 [M][K], router_bf16 [E][K], 16-byte aligned; ids, weights [M][top_k]
+ *   workspace  nvq_moe_route_workspace_bytes(M, E) bytes, 256-byte aligned.  Its
+ *              first 256 bytes must be zero before the first call and are zero
+ *              again after every call: clear it once, then use it for any number of
+ *              calls of these or smaller M and E, one after the other (not by two that overlap).
+ * nvq_moe_route_workspace_bytes returns 0 for an M or E out of range.
+ */
+#define NVQ_MOE_MAX_EXPERTS 512
+#define NVQ_MOE_MAX_TOP_K 16
+size_t nvq_moe_route_workspace_bytes(int M, int E);
+int nvq_moe_route(const uint16_t *x_bf16, const uint16_t *router_bf16, int M, int E, int K,
+                  int top_k, int renormalise, int32_t *ids, float *weights, void *workspace,
+                  size_t workspace_bytes, void *stream);
+
+/*
+ * nvq_moe_experts -- y[m] = sum over the slots s of weights[m][s] * D_e h,
+ * h = bf16(silu(G_e x[m]) * (U_e x[m])), e = ids[m][s].  The weights are 4-bit, in
+ * either format, and not rounded; all sums in fp32, h is rounded to bf16 once
+ * (nvq_silu_mul_bf16's output type), y once.  No atomic additions: the same call
+ * gives the same bits.
+ * A slot whose id is outside [0, E) is not used (padding: a token without any used slot
+ * gets zeros); the weights of an expert that stands in several slots of one token add up.
+ * A token's result does not change by a value of another token or of an expert that it
+ * did not choose.
+ *   gate_up  [E][2 F][K/2] codes, rows 0 .. F-1 of an expert the gate G_e, F .. 2 F - 1
+ *            U_e; gate_up_scales [E][2 F][K/32]
+ *   down     [E][K][F/2] codes, down_scales [E][K][F/32]
+ *   format   NVQ_FMT_INT4: as nvq_pack_int4 writes them, scales fp16 bits;
+ *            NVQ_FMT_MXFP4: as nvq_quant_mxfp4 writes them
+ *   x_bf16 [M][K], ids, weights [M][top_k], y [M][K] (y_dtype); K % 32 == 0, F % 32 == 0
+ *   workspace  nvq_moe_workspace_bytes(...) bytes, 256-byte aligned, scratch (whatever it
+ *              holds); y may overlap neither it nor any input.
+ * nvq_moe_workspace_bytes looks at the sizes alone and returns 0 where they are invalid.
+ */
+enum { NVQ_FMT_INT4 = 0, NVQ_FMT_MXFP4 = 1 };
+typedef struct nvq_experts {
+    const uint8_t *gate_up;
+    const void *gate_up_scales;
+    const uint8_t *down;
+    const void *down_scales;
+    int32_t format;  /* NVQ_FMT_* */
+    int32_t E, K, F;
+} nvq_experts;
+size_t nvq_moe_workspace_bytes(const nvq_experts *experts, int M, int top_k);
+int nvq_moe_experts(const nvq_experts *experts, const uint16_t *x_bf16, const int32_t *ids,
+                    const float *weights, int M, int top_k, void *y, int y_dtype, void *workspace,
+                    size_t workspace_bytes, void *stream);
+
+/*
  * Measurement helpers (not part of the method): a streaming read that sums a
  * buffer into `out` (8 bytes) and a plain copy, used to find the HBM ceiling
  * of the machine and to calibrate profiler byte counters.  bytes % 16 == 0.

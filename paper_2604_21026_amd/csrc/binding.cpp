@@ -21,6 +21,12 @@ decltype(&nvq_gemv_w4a16) g_gemv_w4a16;
 decltype(&nvq_gemv_w4a8) g_gemv_w4a8;
 decltype(&nvq_quant_act_i8) g_quant_act_i8;
 decltype(&nvq_gemm_w4a16) g_gemm_w4a16;
+decltype(&nvq_quant_mxfp4) g_quant_mxfp4;
+decltype(&nvq_dequant_mxfp4) g_dequant_mxfp4;
+decltype(&nvq_gemv_mxfp4) g_gemv_mxfp4;
+decltype(&nvq_gemm_mxfp4) g_gemm_mxfp4;
+decltype(&nvq_moe_route) g_moe_route;
+decltype(&nvq_moe_experts) g_moe_experts;
 
 // A contiguous device tensor of that type; dims < 0: any shape.
 const at::Tensor *device_tensor(PyObject *o, at::ScalarType type, int64_t dims) {
@@ -160,15 +166,146 @@ PyObject *quant_act_i8(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// The addresses of gemv_w4a16, gemv_w4a8, quant_act_i8, gemm_w4a16 in the library.
+// A microscaled matrix: codes [rows][K / 2], scale bytes [rows][K / 32].
+struct Scaled {
+    const uint8_t *q, *s;
+    int64_t rows, K;
+};
+bool scaled(PyObject *codes, PyObject *scales, Scaled *w) {
+    const at::Tensor *q = device_tensor(codes, at::kByte, 2), *s = device_tensor(scales, at::kByte, 2);
+    if (!q || !s) return false;
+    w->rows = q->size(0);
+    w->K = q->size(1) * 2;
+    if (s->size(0) != w->rows || s->size(1) != w->K / 32 || w->rows > INT32_MAX || w->K > INT32_MAX) return false;
+    w->q = static_cast<const uint8_t *>(q->data_ptr());
+    w->s = static_cast<const uint8_t *>(s->data_ptr());
+    return true;
+}
+
+// (x, q, scales)
+PyObject *quant_mxfp4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 3) return none();
+    int dtype = NVQ_BF16;
+    const at::Tensor *x = device_tensor(a[0], at::kBFloat16, 2);
+    if (!x) {
+        dtype = NVQ_F32;
+        x = device_tensor(a[0], at::kFloat, 2);
+    }
+    if (!x || x->size(0) > INT32_MAX || x->size(1) > INT32_MAX) return none();
+    const int64_t M = x->size(0), K = x->size(1);
+    const at::Tensor *const q = device_room(a[1], at::kByte, M * (K / 2)), *const s = device_room(a[2], at::kByte, M * (K / 32));
+    if (!q || !s) return none();
+    const void *const xp = x->data_ptr();
+    uint8_t *const qp = static_cast<uint8_t *>(q->data_ptr()), *const sp = static_cast<uint8_t *>(s->data_ptr());
+    void *const st = current_stream();
+    return status_of([&] { return g_quant_mxfp4(xp, dtype, M, K, qp, sp, st); });
+    END_HANDLE_TH_ERRORS
+}
+
+// (q, scales, out)
+PyObject *dequant_mxfp4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Scaled w;
+    if (n != 3 || !scaled(a[0], a[1], &w)) return none();
+    const at::Tensor *const out = device_tensor(a[2], at::kBFloat16, 2);
+    if (!out || out->size(0) != w.rows || out->size(1) != w.K) return none();
+    uint16_t *const p = static_cast<uint16_t *>(out->data_ptr());
+    void *const st = current_stream();
+    return status_of([&] { return g_dequant_mxfp4(w.q, w.s, w.rows, w.K, p, st); });
+    END_HANDLE_TH_ERRORS
+}
+
+// (qweight, scales, x, y)
+PyObject *gemv_mxfp4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Scaled w;
+    int y_dtype;
+    if (n != 4 || !scaled(a[0], a[1], &w)) return none();
+    const at::Tensor *const x = device_tensor(a[2], at::kBFloat16, 2);
+    if (!x || x->size(1) != w.K || x->size(0) > INT32_MAX) return none();
+    const int M = (int)x->size(0);
+    const at::Tensor *const y = output_tensor(a[3], M * w.rows, &y_dtype);
+    if (!y) return none();
+    const uint16_t *const xp = static_cast<const uint16_t *>(x->data_ptr());
+    void *const yp = y->data_ptr(), *const st = current_stream();
+    return status_of([&] { return g_gemv_mxfp4(w.q, w.s, (int)w.rows, (int)w.K, xp, M, yp, y_dtype, st); });
+    END_HANDLE_TH_ERRORS
+}
+
+// (qweight, scales, xq, xscale, y)
+PyObject *gemm_mxfp4(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    Scaled w, x;
+    int y_dtype;
+    if (n != 5 || !scaled(a[0], a[1], &w) || !scaled(a[2], a[3], &x) || x.K != w.K) return none();
+    const at::Tensor *const y = output_tensor(a[4], x.rows * w.rows, &y_dtype);
+    if (!y) return none();
+    void *const yp = y->data_ptr(), *const st = current_stream();
+    return status_of([&] { return g_gemm_mxfp4(w.q, w.s, w.rows, w.K, x.q, x.s, x.rows, yp, y_dtype, st); });
+    END_HANDLE_TH_ERRORS
+}
+
+// (x, router, top_k, renormalise, ids, weights, workspace)
+PyObject *moe_route(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int top_k, renormalise;
+    if (n != 7 || !small_int(a[2], &top_k) || !small_int(a[3], &renormalise) || top_k < 1) return none();
+    const at::Tensor *const x = device_tensor(a[0], at::kBFloat16, 2), *const r = device_tensor(a[1], at::kBFloat16, 2);
+    if (!x || !r || x->size(1) != r->size(1) || x->size(0) > INT32_MAX || r->size(0) > INT32_MAX || x->size(1) > INT32_MAX)
+        return none();
+    const int M = (int)x->size(0), E = (int)r->size(0), K = (int)x->size(1);
+    const at::Tensor *const ids = device_room(a[4], at::kInt, (int64_t)M * top_k),
+                     *const wt = device_room(a[5], at::kFloat, (int64_t)M * top_k),
+                     *const ws = device_tensor(a[6], at::kByte, -1);
+    if (!ids || !wt || !ws) return none();
+    const uint16_t *const xp = static_cast<const uint16_t *>(x->data_ptr()), *const rp = static_cast<const uint16_t *>(r->data_ptr());
+    int32_t *const ip = static_cast<int32_t *>(ids->data_ptr());
+    float *const wp = static_cast<float *>(wt->data_ptr());
+    void *const sp = ws->data_ptr(), *const st = current_stream();
+    const size_t bytes = (size_t)ws->numel();
+    return status_of([&] { return g_moe_route(xp, rp, M, E, K, top_k, renormalise, ip, wp, sp, bytes, st); });
+    END_HANDLE_TH_ERRORS
+}
+
+// (address of an nvq_experts, its K, x, ids, weights, y, workspace)
+PyObject *moe_experts(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    int K, y_dtype;
+    if (n != 7 || !PyLong_CheckExact(a[0]) || !small_int(a[1], &K)) return none();
+    const nvq_experts *const e = static_cast<const nvq_experts *>(PyLong_AsVoidPtr(a[0]));
+    if (!e) {
+        PyErr_Clear();
+        return none();
+    }
+    const at::Tensor *const x = device_tensor(a[2], at::kBFloat16, 2), *const ids = device_tensor(a[3], at::kInt, 2),
+                     *const wt = device_tensor(a[4], at::kFloat, 2), *const ws = device_tensor(a[6], at::kByte, -1);
+    if (!x || !ids || !wt || !ws || x->size(1) != K || x->size(0) != ids->size(0) || wt->size(0) != ids->size(0) ||
+        wt->size(1) != ids->size(1) || ids->size(0) > INT32_MAX || ids->size(1) > INT32_MAX)
+        return none();
+    const at::Tensor *const y = output_tensor(a[5], x->size(0) * K, &y_dtype);
+    if (!y) return none();
+    const uint16_t *const xp = static_cast<const uint16_t *>(x->data_ptr());
+    const int32_t *const ip = static_cast<const int32_t *>(ids->data_ptr());
+    const float *const wp = static_cast<const float *>(wt->data_ptr());
+    const int M = (int)ids->size(0), top_k = (int)ids->size(1);
+    void *const yp = y->data_ptr(), *const sp = ws->data_ptr(), *const st = current_stream();
+    const size_t bytes = (size_t)ws->numel();
+    return status_of([&] { return g_moe_experts(e, xp, ip, wp, M, top_k, yp, y_dtype, sp, bytes, st); });
+    END_HANDLE_TH_ERRORS
+}
+
+// The addresses of gemv_w4a16, gemv_w4a8, quant_act_i8, gemm_w4a16, quant_mxfp4, dequant_mxfp4, gemv_mxfp4, gemm_mxfp4,
+// moe_route, moe_experts in the library.
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    void *p[4];
-    if (n != 4) {
-        PyErr_SetString(PyExc_TypeError, "four addresses");
+    constexpr int kCalls = 10;
+    void *p[kCalls];
+    if (n != kCalls) {
+        PyErr_SetString(PyExc_TypeError, "ten addresses");
         return nullptr;
     }
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < kCalls; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (!p[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address");
@@ -179,6 +316,12 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
     g_gemv_w4a8 = reinterpret_cast<decltype(g_gemv_w4a8)>(p[1]);
     g_quant_act_i8 = reinterpret_cast<decltype(g_quant_act_i8)>(p[2]);
     g_gemm_w4a16 = reinterpret_cast<decltype(g_gemm_w4a16)>(p[3]);
+    g_quant_mxfp4 = reinterpret_cast<decltype(g_quant_mxfp4)>(p[4]);
+    g_dequant_mxfp4 = reinterpret_cast<decltype(g_dequant_mxfp4)>(p[5]);
+    g_gemv_mxfp4 = reinterpret_cast<decltype(g_gemv_mxfp4)>(p[6]);
+    g_gemm_mxfp4 = reinterpret_cast<decltype(g_gemm_mxfp4)>(p[7]);
+    g_moe_route = reinterpret_cast<decltype(g_moe_route)>(p[8]);
+    g_moe_experts = reinterpret_cast<decltype(g_moe_experts)>(p[9]);
     return none();
     END_HANDLE_TH_ERRORS
 }
@@ -196,6 +339,12 @@ PyMethodDef methods[] = {{"bind", NVQ_FAST(bind)},
                          {"gemv_w4a8", NVQ_FAST(gemv_w4a8)},
                          {"quant_act_i8", NVQ_FAST(quant_act_i8)},
                          {"gemm_w4a16", NVQ_FAST(gemm_w4a16)},
+                         {"quant_mxfp4", NVQ_FAST(quant_mxfp4)},
+                         {"dequant_mxfp4", NVQ_FAST(dequant_mxfp4)},
+                         {"gemv_mxfp4", NVQ_FAST(gemv_mxfp4)},
+                         {"gemm_mxfp4", NVQ_FAST(gemm_mxfp4)},
+                         {"moe_route", NVQ_FAST(moe_route)},
+                         {"moe_experts", NVQ_FAST(moe_experts)},
                          {"stream_handle", stream_handle, METH_NOARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

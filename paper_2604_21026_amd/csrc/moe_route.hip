@@ -1,0 +1,220 @@
+// nvq_moe_route: the router of a mixture of experts for 1 to 32 tokens, in one launch: logits = x R^T (bf16 operands,
+// fp32 sums), the top_k largest of each token in descending order (the lowest index first among equals) and their
+// softmax weights.
+//
+// A few tokens' router is latency, not bytes: the grid is tiles of 16 experts times parts of K, so that a few
+// hundred waves ask for everything at once; each leaves its partial logits in the workspace, and the workgroup that
+// arrives last (a counter that wraps to zero by itself) adds them in the order of the parts and chooses.
+#include "mfma_act.h"
+
+namespace nvq {
+
+namespace {
+
+constexpr int kRouteThreads = 512, kRouteWaves = kRouteThreads / 64;
+constexpr int kRouteMaxParts = 16;
+
+struct RouteArgs {
+    const uint16_t *x, *router;
+    int M, E, K, top_k, renormalise;
+    int32_t *ids;
+    float *weights;
+    uint32_t *arrived;  // workspace
+    float *partial;     // [parts][M][E]
+    int tiles, parts, cols;  // columns of 32 inputs per part
+};
+
+// Logits as words whose unsigned order is theirs; equal numbers (both zeros) give equal words, NaN the lowest.
+__device__ __forceinline__ uint32_t order_word(float f) {
+    if (f != f) return 1u;
+    const uint32_t u = __float_as_uint(f + 0.0f);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+struct MaxWord {
+    __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
+};
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+    v = with_lane_xor<32>(v, MaxWord());
+    v = with_lane_xor<16>(v, MaxWord());
+    v = with_lane_xor<8>(v, MaxWord());
+    v = with_lane_xor<4>(v, MaxWord());
+    v = with_lane_xor<2>(v, MaxWord());
+    return with_lane_xor<1>(v, MaxWord());
+}
+
+// The chosen experts of one token, by one wave.  PER: experts per lane (E <= 64 * PER).
+template <int PER>
+__device__ __forceinline__ void choose(const RouteArgs &a, int m) {
+    const int lane = threadIdx.x & 63;
+    float l[PER];
+    uint32_t key[PER];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int e = 64 * j + lane;
+        l[j] = 0.0f;
+        if (e < a.E) {
+            for (int p = 0; p < a.parts; ++p)
+                l[j] += __hip_atomic_load(a.partial + ((int64_t)p * a.M + m) * a.E + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        key[j] = e < a.E ? order_word(l[j]) : 0u;
+    }
+    float all = 0.0f, top = 0.0f, chosen = 0.0f, mine = 0.0f;
+    int my_id = 0;
+    for (int k = 0; k < a.top_k; ++k) {
+        uint32_t best = key[0];
+#pragma unroll
+        for (int j = 1; j < PER; ++j) best = key[j] > best ? key[j] : best;
+        best = wave_max(best);
+        int id = -1;
+        float value = 0.0f;
+#pragma unroll
+        for (int j = 0; j < PER; ++j) {
+            const uint64_t at = __ballot(key[j] == best);
+            if (id < 0 && at) {  // (uniform)
+                const int owner = __builtin_ctzll(at);
+                id = 64 * j + owner;
+                value = __shfl(l[j], owner, 64);
+                if (lane == owner) key[j] = 0u;
+            }
+        }
+        if (k == 0) {
+            top = value;
+            if (!a.renormalise) {
+#pragma unroll
+                for (int j = 0; j < PER; ++j) all += 64 * j + lane < a.E ? expf(l[j] - top) : 0.0f;
+                all = group_sum<64>(all);
+            }
+        }
+        const float w = expf(value - top);
+        chosen += w;
+        if (lane == k) {
+            my_id = id;
+            mine = w;
+        }
+    }
+    if (lane < a.top_k) {
+        a.ids[m * a.top_k + lane] = my_id;
+        a.weights[m * a.top_k + lane] = mine / (a.renormalise ? chosen : all);
+    }
+}
+
+template <int T>
+__global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(RouteArgs a) {
+    __shared__ float red[kRouteWaves][T * 4][64];
+    __shared__ uint32_t last;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int n = lane & 15, kb = lane >> 4;
+    const int tile = blockIdx.x % a.tiles, part = blockIdx.x / a.tiles;
+    const int e0 = 16 * tile;
+    const int all_cols = a.K / 32, col0 = part * a.cols;
+    const int col1 = col0 + a.cols < all_cols ? col0 + a.cols : all_cols;
+
+    const char *const r = reinterpret_cast<const char *>(a.router) + (int64_t)(e0 + n < a.E ? e0 + n : a.E - 1) * a.K * 2 + kb * 16;
+    const char *x[T];
+    float4v sum[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        const int m = 16 * t + n;
+        x[t] = reinterpret_cast<const char *>(a.x) + (int64_t)(m < a.M ? m : 0) * a.K * 2 + kb * 16;
+        sum[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+    for (int c = col0 + w; c < col1; c += kRouteWaves) {
+        const bf16x8 b = __builtin_bit_cast(bf16x8, load_stream(reinterpret_cast<const uint4 *>(r + (int64_t)c * 64)));
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            const bf16x8 v = __builtin_bit_cast(bf16x8, load_stream(reinterpret_cast<const uint4 *>(x[t] + (int64_t)c * 64)));
+            sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, b, sum[t], 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        wait_written(sum[t]);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) red[w][4 * t + j][lane] = sum[t][j];
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < T * 4 * 64; i += kRouteThreads) {
+        const int reg = i >> 6, l = i & 63;
+        const int m = 16 * (reg >> 2) + 4 * (l >> 4) + (reg & 3), e = e0 + (l & 15);
+        float v = red[0][reg][l];
+#pragma unroll
+        for (int k = 1; k < kRouteWaves; ++k) v += red[k][reg][l];
+        if (m < a.M && e < a.E)
+            __hip_atomic_store(a.partial + ((int64_t)part * a.M + m) * a.E + e, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's partial logits are written
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        // all partial logits of the workgroup before its arrival, those of the others after the last one's
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+        const uint32_t before = __hip_atomic_fetch_add(a.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        last = before == gridDim.x - 1;
+        if (last) __hip_atomic_store(a.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    }
+    __syncthreads();
+    if (!last) return;
+    for (int m = w; m < a.M; m += kRouteWaves) {
+        if (a.E <= 64)
+            choose<1>(a, m);
+        else if (a.E <= 128)
+            choose<2>(a, m);
+        else if (a.E <= 256)
+            choose<4>(a, m);
+        else
+            choose<8>(a, m);
+    }
+}
+
+constexpr size_t kRouteCounterBytes = 256;
+
+bool route_shape(int M, int E) { return M >= 1 && M <= NVQ_MAX_M && E >= 1 && E <= NVQ_MOE_MAX_EXPERTS; }
+
+}  // namespace
+
+}  // namespace nvq
+
+extern "C" size_t nvq_moe_route_workspace_bytes(int M, int E) {
+    using namespace nvq;
+    if (!route_shape(M, E)) return 0;
+    return kRouteCounterBytes + sizeof(float) * kRouteMaxParts * (size_t)M * E;
+}
+
+extern "C" int nvq_moe_route(const uint16_t *x_bf16, const uint16_t *router_bf16, int M, int E, int K, int top_k,
+                             int renormalise, int32_t *ids, float *weights, void *workspace, size_t workspace_bytes,
+                             void *stream) {
+    using namespace nvq;
+    if (!x_bf16 || !router_bf16 || !ids || !weights || (renormalise != 0 && renormalise != 1)) return NVQ_ERR_INVALID_ARG;
+    if (!route_shape(M, E) || top_k < 1 || top_k > NVQ_MOE_MAX_TOP_K || top_k > E || K <= 0 || K % 32 || K > NVQ_MAX_K)
+        return NVQ_ERR_SHAPE;
+    if (!aligned(x_bf16, 16) || !aligned(router_bf16, 16) || !aligned(ids, 4) || !aligned(weights, 4)) return NVQ_ERR_ALIGN;
+    if (!workspace || !aligned(workspace, 256) || workspace_bytes < nvq_moe_route_workspace_bytes(M, E))
+        return NVQ_ERR_WORKSPACE;
+    RouteArgs a;
+    a.x = x_bf16;
+    a.router = router_bf16;
+    a.M = M;
+    a.E = E;
+    a.K = K;
+    a.top_k = top_k;
+    a.renormalise = renormalise;
+    a.ids = ids;
+    a.weights = weights;
+    a.arrived = static_cast<uint32_t *>(workspace);
+    a.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + kRouteCounterBytes);
+    a.tiles = (E + 15) / 16;
+    // a part: two columns per wave or more
+    const int cols = K / 32;
+    int parts = (cols + 2 * kRouteWaves - 1) / (2 * kRouteWaves);
+    parts = parts < kRouteMaxParts ? parts : kRouteMaxParts;
+    a.cols = (cols + parts - 1) / parts;
+    a.parts = (cols + a.cols - 1) / a.cols;
+    const dim3 grid((unsigned)(a.tiles * a.parts)), block(kRouteThreads);
+    if (M <= 16)
+        hipLaunchKernelGGL(moe_route_kernel<1>, grid, block, 0, (hipStream_t)stream, a);
+    else
+        hipLaunchKernelGGL(moe_route_kernel<2>, grid, block, 0, (hipStream_t)stream, a);
+    NVQ_HIP_TRY(hipGetLastError());
+    return NVQ_OK;
+}

@@ -22,6 +22,7 @@ W4A8, W4A16 = 0, 1
 MAX_M = 32
 PLAN_ORDERED = 1
 IN_PLAIN, IN_RMSNORM, IN_SILU_MUL = 0, 1, 2
+FMT_INT4, FMT_MXFP4 = 0, 1
 
 EXPORTS = (
     "nvq_status_string", "nvq_last_hip_error", "nvq_pack_int4", "nvq_quant_act_i8",
@@ -31,6 +32,8 @@ EXPORTS = (
     "nvq_plan_destroy", "nvq_plan_describe", "nvq_plan_describe_batches",
     "nvq_plan_describe_skips", "nvq_plan_describe_kernels", "nvq_plan_describe_steps",
     "nvq_dequant_bf16", "nvq_gemm_w4a16", "nvq_gemm_describe", "nvq_rms_norm_bf16", "nvq_silu_mul_bf16", "nvq_precision_from_scores", "nvq_token_norms", "nvq_mcap_scores", "nvq_stream_read", "nvq_stream_copy",
+    "nvq_quant_mxfp4", "nvq_dequant_mxfp4", "nvq_gemv_mxfp4", "nvq_gemm_mxfp4",
+    "nvq_moe_route_workspace_bytes", "nvq_moe_route", "nvq_moe_workspace_bytes", "nvq_moe_experts",
 )
 
 
@@ -50,6 +53,13 @@ class Linear(C.Structure):
                 ("h_out_bf16", C.c_void_p)]
 
 
+class ExpertsStruct(C.Structure):
+    """Mirror of `nvq_experts`."""
+    _fields_ = [("gate_up", C.c_void_p), ("gate_up_scales", C.c_void_p), ("down", C.c_void_p),
+                ("down_scales", C.c_void_p), ("format", C.c_int32), ("E", C.c_int32), ("K", C.c_int32),
+                ("F", C.c_int32)]
+
+
 _lib = None
 _calls = None  # csrc/binding.cpp, once the library is loaded, or None
 
@@ -66,7 +76,8 @@ def _load_calls(L):
                       "build it with `python -m paper_2604_21026_amd.build`" % (CALLS_PATH, e))
         return None
     calls.bind(*(C.cast(f, C.c_void_p).value for f in
-                 (L.nvq_gemv_w4a16, L.nvq_gemv_w4a8, L.nvq_quant_act_i8, L.nvq_gemm_w4a16)))
+                 (L.nvq_gemv_w4a16, L.nvq_gemv_w4a8, L.nvq_quant_act_i8, L.nvq_gemm_w4a16, L.nvq_quant_mxfp4,
+                  L.nvq_dequant_mxfp4, L.nvq_gemv_mxfp4, L.nvq_gemm_mxfp4, L.nvq_moe_route, L.nvq_moe_experts)))
     return calls
 
 
@@ -115,7 +126,19 @@ def lib() -> C.CDLL:
     L.nvq_mcap_scores.argtypes = [vp, vp, vp, ci, ci, vp]
     L.nvq_stream_read.argtypes = [vp, sz, vp, vp]
     L.nvq_stream_copy.argtypes = [vp, vp, sz, vp]
+    L.nvq_quant_mxfp4.argtypes = [vp, ci, i64, i64, vp, vp, vp]
+    L.nvq_dequant_mxfp4.argtypes = [vp, vp, i64, i64, vp, vp]
+    L.nvq_gemv_mxfp4.argtypes = [vp, vp, ci, ci, vp, ci, vp, ci, vp]
+    L.nvq_gemm_mxfp4.argtypes = [vp, vp, i64, i64, vp, vp, i64, vp, ci, vp]
+    L.nvq_moe_route_workspace_bytes.argtypes = [ci, ci]
+    L.nvq_moe_route_workspace_bytes.restype = sz
+    L.nvq_moe_route.argtypes = [vp, vp, ci, ci, ci, ci, ci, vp, vp, vp, sz, vp]
+    L.nvq_moe_workspace_bytes.argtypes = [vp, ci, ci]
+    L.nvq_moe_workspace_bytes.restype = sz
+    L.nvq_moe_experts.argtypes = [vp, vp, vp, vp, ci, ci, vp, ci, vp, sz, vp]
     for f in ("nvq_pack_int4", "nvq_quant_act_i8", "nvq_gemv_w4a16", "nvq_gemv_w4a8",
+              "nvq_quant_mxfp4", "nvq_dequant_mxfp4", "nvq_gemv_mxfp4", "nvq_gemm_mxfp4", "nvq_moe_route",
+              "nvq_moe_experts",
               "nvq_decode_linears", "nvq_decode_status", "nvq_decode_linears_static",
               "nvq_precision_from_scores", "nvq_stream_read",
               "nvq_stream_copy", "nvq_plan_create", "nvq_plan_run", "nvq_plan_info",
@@ -515,6 +538,173 @@ def decode_linears(entries: Sequence[dict], M: int, act_group: int = 0) -> Decod
     dl = DecodeList(entries, M, act_group)
     dl.run()
     return dl
+
+
+def quant_mxfp4(x: torch.Tensor, out=None):
+    """x f32 or bf16 [M,K] -> microscaled 4-bit codes q u8 [M,K/2], scale bytes u8 [M,K/32]
+    (`out`: the two tensors to write into, as returned by an earlier call)."""
+    if out is not None:
+        q, s = out
+        if _calls is not None:
+            status = _calls.quant_mxfp4(x, q, s)
+            if status is not None:  # (None: not the ordinary case)
+                if status:
+                    _check(status, "nvq_quant_mxfp4")
+                return q, s
+    M, K = x.shape
+    if out is None:
+        q = torch.empty((M, K // 2), dtype=torch.uint8, device=x.device)
+        s = torch.empty((M, K // 32), dtype=torch.uint8, device=x.device)
+    _check(lib().nvq_quant_mxfp4(_dev(x, x.dtype, "x"), _y_dtype(x.dtype), M, K,
+                                 _dev(q, torch.uint8, "q", M * (K // 2)), _dev(s, torch.uint8, "scales", M * (K // 32)),
+                                 _stream()), "nvq_quant_mxfp4")
+    return q, s
+
+
+def dequant_mxfp4(q: torch.Tensor, scales: torch.Tensor, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """q u8 [M,K/2], scales u8 [M,K/32] -> the values they stand for, bf16 [M,K]."""
+    if out is not None and _calls is not None:
+        status = _calls.dequant_mxfp4(q, scales, out)
+        if status is not None:  # (None: not the ordinary case)
+            if status:
+                _check(status, "nvq_dequant_mxfp4")
+            return out
+    M, K = q.shape[0], q.shape[1] * 2
+    if out is None:
+        out = torch.empty((M, K), dtype=torch.bfloat16, device=q.device)
+    if tuple(out.shape) != (M, K) or tuple(scales.shape) != (M, K // 32):
+        raise ValueError("shape mismatch")
+    _check(lib().nvq_dequant_mxfp4(_dev(q, torch.uint8, "q"), _dev(scales, torch.uint8, "scales"), M, K,
+                                   _dev(out, torch.bfloat16, "out"), _stream()), "nvq_dequant_mxfp4")
+    return out
+
+
+def gemv_mxfp4(qweight, scales, x, out_dtype=torch.float32, out: Optional[torch.Tensor] = None):
+    """Microscaled weights (u8 [N,K/2], scales u8 [N,K/32]) times x bf16 [M,K], up to 32 tokens -> y [M,N]."""
+    if out is not None and _calls is not None:
+        status = _calls.gemv_mxfp4(qweight, scales, x, out)
+        if status is not None:  # (None: not the ordinary case)
+            if status:
+                _check(status, "nvq_gemv_mxfp4")
+            return out
+    N, K = qweight.shape[0], qweight.shape[1] * 2
+    M = x.shape[0]
+    if x.shape[1] != K or tuple(scales.shape) != (N, K // 32):
+        raise ValueError("shape mismatch")
+    y = out if out is not None else torch.empty((M, N), dtype=out_dtype, device=x.device)
+    _check(lib().nvq_gemv_mxfp4(_dev(qweight, torch.uint8, "qweight"), _dev(scales, torch.uint8, "scales"), N, K,
+                                _dev(x, torch.bfloat16, "x"), M, _dev(y, y.dtype, "y", M * N),
+                                _y_dtype(y.dtype), _stream()), "nvq_gemv_mxfp4")
+    return y
+
+
+def gemm_mxfp4(qweight, scales, xq, xscale, out_dtype=torch.float32, out: Optional[torch.Tensor] = None):
+    """Microscaled weights (u8 [N,K/2], scales u8 [N,K/32]) times microscaled activations (the same of
+    [M,K], from quant_mxfp4), any number of tokens -> y [M,N]."""
+    if out is not None and _calls is not None:
+        status = _calls.gemm_mxfp4(qweight, scales, xq, xscale, out)
+        if status is not None:  # (None: not the ordinary case)
+            if status:
+                _check(status, "nvq_gemm_mxfp4")
+            return out
+    N, K = qweight.shape[0], qweight.shape[1] * 2
+    M = xq.shape[0]
+    if xq.shape[1] * 2 != K or tuple(scales.shape) != (N, K // 32) or tuple(xscale.shape) != (M, K // 32):
+        raise ValueError("shape mismatch")
+    y = out if out is not None else torch.empty((M, N), dtype=out_dtype, device=xq.device)
+    _check(lib().nvq_gemm_mxfp4(_dev(qweight, torch.uint8, "qweight"), _dev(scales, torch.uint8, "scales"), N, K,
+                                _dev(xq, torch.uint8, "xq"), _dev(xscale, torch.uint8, "xscale"), M,
+                                _dev(y, y.dtype, "y", M * N), _y_dtype(y.dtype), _stream()), "nvq_gemm_mxfp4")
+    return y
+
+
+def moe_route_workspace(M: int, E: int, device="cuda") -> torch.Tensor:
+    """The workspace of moe_route for up to M tokens and E experts: cleared here, and by every call after its use."""
+    need = lib().nvq_moe_route_workspace_bytes(M, E)
+    if need == 0:
+        raise NvqError(2, "nvq_moe_route_workspace_bytes")
+    return torch.zeros(need, dtype=torch.uint8, device=device)
+
+
+def moe_route(x: torch.Tensor, router: torch.Tensor, top_k: int, renormalise: bool = True, out=None,
+              workspace: Optional[torch.Tensor] = None):
+    """x bf16 [M,K], router bf16 [E,K] -> ids i32 [M,top_k], weights f32 [M,top_k] (`out`: the two tensors to
+    write into; `workspace`: from moe_route_workspace, for calls one after the other)."""
+    if out is not None and workspace is not None and _calls is not None:
+        status = _calls.moe_route(x, router, top_k, int(renormalise), out[0], out[1], workspace)
+        if status is not None:  # (None: not the ordinary case)
+            if status:
+                _check(status, "nvq_moe_route")
+            return out[0], out[1]
+    M, K = x.shape
+    E = router.shape[0]
+    if router.shape[1] != K:
+        raise ValueError("shape mismatch")
+    if out is None:
+        out = (torch.empty((M, max(top_k, 0)), dtype=torch.int32, device=x.device),
+               torch.empty((M, max(top_k, 0)), dtype=torch.float32, device=x.device))
+    if workspace is None:
+        workspace = moe_route_workspace(M, E, x.device)
+    _check(lib().nvq_moe_route(_dev(x, torch.bfloat16, "x"), _dev(router, torch.bfloat16, "router"), M, E, K, top_k,
+                               int(renormalise), _dev(out[0], torch.int32, "ids", M * top_k),
+                               _dev(out[1], torch.float32, "weights", M * top_k), _dev(workspace, torch.uint8, "workspace"),
+                               workspace.numel(), _stream()), "nvq_moe_route")
+    return out[0], out[1]
+
+
+class Experts:
+    """The weights of a mixture's experts (`nvq_experts` plus the tensors it points to): gate_up u8 [E,2F,K/2] (the
+    gate's rows first), down u8 [E,K,F/2] and their scales [E,2F,K/32], [E,K,F/32], int16 (fp16 bits, as pack_int4
+    returns them) or u8 (as quant_mxfp4 does)."""
+
+    def __init__(self, gate_up, gate_up_scales, down, down_scales):
+        E, rows, K = gate_up.shape[0], gate_up.shape[1], gate_up.shape[2] * 2
+        F = rows // 2
+        dtype = gate_up_scales.dtype
+        if dtype not in (torch.int16, torch.uint8):
+            raise ValueError("scales must be int16 (fp16 bits) or uint8, got %s" % dtype)
+        if (rows % 2 or F % 32 or K % 32 or tuple(gate_up_scales.shape) != (E, rows, K // 32)
+                or tuple(down.shape) != (E, K, F // 2) or tuple(down_scales.shape) != (E, K, F // 32)):
+            raise ValueError("shape mismatch")
+        self.keep = (gate_up, gate_up_scales, down, down_scales)
+        if any(t.device != gate_up.device for t in self.keep):
+            raise ValueError("tensors on different devices")
+        self.E, self.K, self.F, self.device = E, K, F, gate_up.device
+        self.struct = ExpertsStruct(_dev(gate_up, torch.uint8, "gate_up"), _dev(gate_up_scales, dtype, "gate_up_scales"),
+                                    _dev(down, torch.uint8, "down"), _dev(down_scales, dtype, "down_scales"),
+                                    FMT_INT4 if dtype == torch.int16 else FMT_MXFP4, E, K, F)
+        self.address = C.addressof(self.struct)
+
+    def workspace(self, M: int, top_k: int) -> torch.Tensor:
+        """Scratch memory of moe_experts for up to M tokens of top_k slots."""
+        need = lib().nvq_moe_workspace_bytes(self.address, M, top_k)
+        if need == 0:
+            raise NvqError(2, "nvq_moe_workspace_bytes")
+        return torch.empty(need, dtype=torch.uint8, device=self.device)
+
+
+def moe_experts(experts: Experts, x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor,
+                out_dtype=torch.bfloat16, out: Optional[torch.Tensor] = None,
+                workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x bf16 [M,K], ids i32 [M,top_k] (outside [0,E): not used), weights f32 [M,top_k] -> y [M,K], the weighted sum
+    of the chosen experts' outputs (`workspace`: from experts.workspace, for calls one after the other)."""
+    if out is not None and workspace is not None and _calls is not None:
+        status = _calls.moe_experts(experts.address, experts.K, x, ids, weights, out, workspace)
+        if status is not None:  # (None: not the ordinary case)
+            if status:
+                _check(status, "nvq_moe_experts")
+            return out
+    M, top_k = ids.shape
+    if tuple(x.shape) != (M, experts.K) or tuple(weights.shape) != (M, top_k):
+        raise ValueError("shape mismatch")
+    y = out if out is not None else torch.empty((M, experts.K), dtype=out_dtype, device=x.device)
+    if workspace is None:
+        workspace = experts.workspace(M, top_k)
+    _check(lib().nvq_moe_experts(experts.address, _dev(x, torch.bfloat16, "x"), _dev(ids, torch.int32, "ids"),
+                                 _dev(weights, torch.float32, "weights"), M, top_k, _dev(y, y.dtype, "y", M * experts.K),
+                                 _y_dtype(y.dtype), _dev(workspace, torch.uint8, "workspace"), workspace.numel(),
+                                 _stream()), "nvq_moe_experts")
+    return y
 
 
 def token_norms(a: torch.Tensor, b: Optional[torch.Tensor] = None) -> torch.Tensor:
