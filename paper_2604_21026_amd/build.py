@@ -30,9 +30,9 @@ FLAGS = [
     "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,
 ]
 # MFMA results go to ordinary vector registers (no accumulator-register copies), except in the
-# prefill GEMM, whose accumulators alone fill the 256 ordinary registers of a wave
+# prompt GEMMs, whose accumulators alone fill the 256 ordinary registers of a wave
 VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
-NO_VGPR_FORM = {"gemm_w4a16.hip"}
+NO_VGPR_FORM = {"gemm_w4a16.hip", "gemm_mxfp4.hip"}
 
 
 def sources():
