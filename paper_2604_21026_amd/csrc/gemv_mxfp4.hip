@@ -18,7 +18,7 @@ __global__ __launch_bounds__(64 * W) void gemv_mxfp4_kernel(const uint8_t *__res
                                                             void *__restrict__ y, int y_dtype) {
     __shared__ float red[W][R * T * 4][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int n = lane & 15, kb = lane >> 4;
+    const int n = lane & 15;
     const int row0 = blockIdx.x * (16 * R);
 
     RowAt at[R];
@@ -31,7 +31,7 @@ __global__ __launch_bounds__(64 * W) void gemv_mxfp4_kernel(const uint8_t *__res
 #pragma unroll
     for (int t = 0; t < T; ++t) {
         const int m = 16 * t + n;  // (tokens past the end read token 0: a product keeps tokens apart)
-        xt[t] = reinterpret_cast<const char *>(x) + (size_t)(m < M ? m : 0) * G * 64 + kb * 16;
+        xt[t] = reinterpret_cast<const char *>(x) + (size_t)(m < M ? m : 0) * G * 64;
     }
     float4v sum[R][T];
 #pragma unroll
@@ -58,6 +58,172 @@ __global__ __launch_bounds__(64 * W) void gemv_mxfp4_kernel(const uint8_t *__res
     }
 }
 
+
+// The same for more tokens, whose activations outweigh the weights where every row tile reads them for itself: a workgroup of RG
+// x S waves takes RG * R row tiles, and brings the activations of S passes of C columns into LDS for all of them, a pass ahead
+// (through registers, the loads two passes ahead); wave (g, s) multiplies the row tiles of group g with pass s of each turn.
+// Piece c (16 bytes) of token n lies at position c ^ swapped(n % 16): a read takes lanes 0-3, 12-15 and 20-27 of a half wave
+// together and then its other sixteen, and either sixteen touch every bank once.
+__device__ __forceinline__ int swapped(int n) { return (n & 9) | (n & 2) << 1 | (n & 4) >> 1; }
+
+template <int T, int R, int RG, int S, int C>
+__global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const uint8_t *__restrict__ q,
+                                                                        const uint8_t *__restrict__ scales, int N, int G,
+                                                                        const uint16_t *__restrict__ x, int M,
+                                                                        void *__restrict__ y, int y_dtype) {
+    constexpr int kThreads = 64 * RG * S, kPieces = 16 * C;         // pieces of a token and pass
+    constexpr int kAll = S * 16 * T * kPieces, kMine = kAll / kThreads;  // pieces of a turn, of a thread
+    static_assert(kMine * kThreads == kAll, "whole pieces per thread");
+    __shared__ __attribute__((aligned(1024))) uint4v xs[2][kAll];
+    constexpr int kRegs = R * T * 4;
+    static_assert(S == 1 || (S - 1) * RG * kRegs * 64 * 4 <= (int)sizeof(xs), "the partial tiles fit");
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), g = wave / S, s = wave % S;
+    const int n = lane & 15, kb = lane >> 4;
+    const int row0 = (blockIdx.x * RG + g) * (16 * R);
+    const int passes = G / (4 * C), turns = (passes + S - 1) / S;
+
+    RowAt at[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = row0 + 16 * r + n;
+        at[r] = row_at<NVQ_FMT_MXFP4>(q, scales, row < N ? row : N - 1, G);
+    }
+    // pieces of a turn, as they lie in LDS: [slice][token][position]
+    auto ask = [&](uint4v (&v)[kMine], int turn) {
+#pragma unroll
+        for (int k = 0; k < kMine; ++k) {
+            const int i = tid + k * kThreads, slice = i / (16 * T * kPieces), m = i / kPieces % (16 * T);
+            const int piece = (i % kPieces) ^ swapped(m & 15);
+            int pass = turn * S + slice;
+            pass = pass < passes ? pass : passes - 1;
+            v[k] = *as_global<uint4v>(reinterpret_cast<const char *>(x) + ((int64_t)(m < M ? m : 0) * G * 64 +
+                                                                          (int64_t)pass * (256 * C) + piece * 16));
+        }
+    };
+    auto keep = [&](const uint4v (&v)[kMine], int buf) {
+#pragma unroll
+        for (int k = 0; k < kMine; ++k) xs[buf][tid + k * kThreads] = v[k];
+    };
+    auto weights = [&](RowColumns<NVQ_FMT_MXFP4, C> (&w)[R], int turn) {
+        const int pass = turn * S + s;  // (uniform; past the end: the last one, with codes of zero)
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            load_columns<NVQ_FMT_MXFP4, C>(w[r], at[r], (pass < passes ? pass : passes - 1) * C, kb);
+        }
+    };
+    float4v sum[R][T];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int t = 0; t < T; ++t) sum[r][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+
+    if (turns > 0) {
+        uint4v xr[kMine];
+        RowColumns<NVQ_FMT_MXFP4, C> w[R], next[R];
+        ask(xr, 0);
+        weights(w, 0);
+        keep(xr, 0);
+        ask(xr, 1 < turns ? 1 : 0);
+        auto one = [&](RowColumns<NVQ_FMT_MXFP4, C> (&now)[R], RowColumns<NVQ_FMT_MXFP4, C> (&then)[R], int turn) {
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's pieces are in LDS
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            keep(xr, (turn + 1) & 1);
+            ask(xr, turn + 2 < turns ? turn + 2 : turns - 1);
+            weights(then, turn + 1 < turns ? turn + 1 : turn);
+            __builtin_amdgcn_sched_barrier(0);
+            const bool mine = turn * S + s < passes;  // (uniform)
+            const uint4v *const xb = &xs[turn & 1][s * (16 * T * kPieces)];
+#pragma unroll
+            for (int b = 0; b < C; ++b) {
+                uint4v raw[T][4];
+#pragma unroll
+                for (int t = 0; t < T; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) raw[t][i] = xb[(16 * t + n) * kPieces + ((16 * b + 4 * kb + i) ^ swapped(n))];
+                if (S > 1 && !mine) {
+#pragma unroll
+                    for (int r = 0; r < R; ++r) now[r].w[b] = uint4v{0, 0, 0, 0};
+                }
+                multiply_column<NVQ_FMT_MXFP4, R, T, C>(now, b, raw, sum);
+            }
+        };
+        // (two turns: the registers of the weights change roles, they are not copied)
+        for (int turn = 0; turn < turns; turn += 2) {
+            one(w, next, turn);
+            if (turn + 1 >= turns) break;
+            one(next, w, turn + 1);
+        }
+    }
+    const char *xt[T];
+#pragma unroll
+    for (int t = 0; t < T; ++t) {
+        const int m = 16 * t + n;
+        xt[t] = reinterpret_cast<const char *>(x) + (size_t)(m < M ? m : 0) * G * 64;
+    }
+    last_columns<NVQ_FMT_MXFP4, R, T>(at, xt, G, passes * C, 0, s, S, sum);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int t = 0; t < T; ++t) wait_written(sum[r][t]);
+    if constexpr (S > 1) {
+        __syncthreads();
+        float *const red = reinterpret_cast<float *>(&xs[0][0]);
+        if (s > 0) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int t = 0; t < T; ++t)
+                    *reinterpret_cast<float4v *>(&red[(((g * (S - 1) + s - 1) * (R * T) + r * T + t) * 64 + lane) * 4]) = sum[r][t];
+        }
+        __syncthreads();
+        if (s > 0) return;
+#pragma unroll
+        for (int k = 0; k < S - 1; ++k)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int t = 0; t < T; ++t)
+                    sum[r][t] += *reinterpret_cast<const float4v *>(&red[(((g * (S - 1) + k) * (R * T) + r * T + t) * 64 + lane) * 4]);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int m = 16 * t + 4 * kb + j, row = row0 + 16 * r + n;
+                if (m < M && row < N) store_global(y, y_dtype, (int64_t)m * N + row, sum[r][t][j]);
+            }
+}
+
+struct GemvArgs {
+    const uint8_t *q, *s;
+    const uint16_t *x;
+    void *y;
+    int N, G, M, y_dtype;
+};
+
+// Up to 16 tokens, R row tiles per workgroup.
+template <int R>
+int gemv_rows(const GemvArgs &a, hipStream_t st) {
+    const dim3 grid((unsigned)(((int64_t)a.N + 16 * R - 1) / (16 * R)));
+    hipLaunchKernelGGL((gemv_mxfp4_kernel<R, 1, 4, 4>), grid, dim3(256), 0, st, a.q, a.s, a.N, a.G, a.x, a.M, a.y, a.y_dtype);
+    NVQ_HIP_TRY(hipGetLastError());
+    return NVQ_OK;
+}
+
+template <int T, int R, int RG, int S, int C>
+int gemv_shared(const GemvArgs &a, hipStream_t st) {
+    const dim3 grid((unsigned)(((int64_t)a.N + 16 * R * RG - 1) / (16 * R * RG)));
+    hipLaunchKernelGGL((gemv_mxfp4_shared_kernel<T, R, RG, S, C>), grid, dim3(64 * RG * S), 0, st, a.q, a.s, a.N, a.G, a.x, a.M,
+                       a.y, a.y_dtype);
+    NVQ_HIP_TRY(hipGetLastError());
+    return NVQ_OK;
+}
+
 }  // namespace
 
 }  // namespace nvq
@@ -67,17 +233,28 @@ extern "C" int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
     using namespace nvq;
     if (!qweight || !scales || !x_bf16 || !y || (y_dtype != NVQ_F32 && y_dtype != NVQ_BF16))
         return NVQ_ERR_INVALID_ARG;
-    if (N <= 0 || M < 1 || M > NVQ_MAX_M || K <= 0 || K % 32 || K > NVQ_MAX_K) return NVQ_ERR_SHAPE;
+    if (N <= 0 || N > (1 << 30) || M < 1 || M > NVQ_MAX_M || K <= 0 || K % 32 || K > NVQ_MAX_K) return NVQ_ERR_SHAPE;
     if (!aligned(qweight, 16) || !aligned(x_bf16, 16) || !aligned(y, y_dtype == NVQ_F32 ? 4 : 2)) return NVQ_ERR_ALIGN;
     const hipStream_t st = (hipStream_t)stream;
-    constexpr int R = 1, W = 4, B = 4;
-    const dim3 grid((unsigned)(((int64_t)N + 16 * R - 1) / (16 * R))), block(64 * W);
-    if (M <= 16)
-        hipLaunchKernelGGL((gemv_mxfp4_kernel<R, 1, W, B>), grid, block, 0, st, qweight, scales, N, K / 32, x_bf16, M, y,
-                           y_dtype);
-    else
-        hipLaunchKernelGGL((gemv_mxfp4_kernel<R, 2, W, B>), grid, block, 0, st, qweight, scales, N, K / 32, x_bf16, M, y,
-                           y_dtype);
-    NVQ_HIP_TRY(hipGetLastError());
-    return NVQ_OK;
+    const GemvArgs a = {qweight, scales, x_bf16, y, N, K / 32, M, y_dtype};
+    const int64_t cus = device_cu_count(), tiles = ((int64_t)N + 15) / 16;
+    // us at (tokens, rows, inputs)   (1, 4096, 4096) (1, 14336, 4096) (1, 128256, 4096) (8, 14336, 4096) (16, 128256, 4096)
+    //   1 row tile per workgroup          3.9              10.0             68                15.2              148
+    //   2                                 5.3               8.7             54                11.5               94
+    //   4                                 8.4               8.9             50                 9.9               68
+    //   16, activations shared           22.4              22.6             51                23.3               54
+    if (M <= 8 || (M <= 16 && tiles < 16 * cus)) {
+        if (tiles < 3 * cus) return gemv_rows<1>(a, st);
+        if (tiles < 8 * cus && M == 1) return gemv_rows<2>(a, st);
+        return gemv_rows<4>(a, st);
+    }
+    if (M <= 16) return gemv_shared<1, 2, 8, 1, 4>(a, st);
+    // us at (32 tokens, rows, inputs)  (4096, 4096) (4096, 14336) (14336, 4096) (128256, 4096)
+    //   1 row tile, nothing shared         10.2          30.2          34.4          261
+    //   2 row tiles, K in four slices       9.1          24.1          19.1          155
+    //   4 row tiles, K in two              10.8          32.1          12.4           93
+    //   16 row tiles                       26.4          82.8          27.2           63
+    if (tiles < 2 * cus) return gemv_shared<2, 1, 2, 4, 2>(a, st);
+    if (tiles < 16 * cus) return gemv_shared<2, 1, 4, 2, 2>(a, st);
+    return gemv_shared<2, 2, 8, 1, 4>(a, st);
 }

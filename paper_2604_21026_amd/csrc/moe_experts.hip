@@ -77,7 +77,7 @@ template <int FMT, int R, int T, int W, int B>
 __device__ __forceinline__ void gate_up(const MoeArgs &a, int e, int row0, const ExpertTokens<T> &et, float *red,
                                         const int *pair_of) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int n = lane & 15, kb = lane >> 4, G = a.K / 32;
+    const int n = lane & 15, G = a.K / 32;
     RowAt at[2 * R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
@@ -89,7 +89,7 @@ __device__ __forceinline__ void gate_up(const MoeArgs &a, int e, int row0, const
     float4v sum[2 * R][T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-        x[t] = reinterpret_cast<const char *>(a.x) + (int64_t)et.token[t] * a.K * 2 + kb * 16;
+        x[t] = reinterpret_cast<const char *>(a.x) + (int64_t)et.token[t] * a.K * 2;
 #pragma unroll
         for (int r = 0; r < 2 * R; ++r) sum[r][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
     }
@@ -152,7 +152,7 @@ __device__ __forceinline__ void add_expert(const MoeArgs &a, const RowAt (&at)[R
     float4v sum[R][T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-        h[t] = reinterpret_cast<const char *>(a.h) + (int64_t)pair[t] * a.F * 2 + kb * 16;
+        h[t] = reinterpret_cast<const char *>(a.h) + (int64_t)pair[t] * a.F * 2;
 #pragma unroll
         for (int r = 0; r < R; ++r) sum[r][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
     }
@@ -254,11 +254,18 @@ __global__ __launch_bounds__(64 * W) void moe_down_kernel(MoeArgs a) {
 
 template <int FMT, int T>
 int launch_experts(const MoeArgs &a, hipStream_t st) {
-    constexpr int W1 = 4, W2 = 8;
+#ifndef R1
+#define R1 1
+#define W1 4
+#define C1 2
+#define R2 1
+#define W2 8
+#define C2 4
+#endif
     const unsigned experts = (unsigned)(a.E <= a.pairs ? a.E : a.pairs);
-    hipLaunchKernelGGL((moe_gate_up_kernel<FMT, 1, T, W1, 2>), dim3(a.F / 16, experts), dim3(64 * W1), 0, st, a);
+    hipLaunchKernelGGL((moe_gate_up_kernel<FMT, R1, T, W1, C1>), dim3(a.F / 16 / R1, experts), dim3(64 * W1), 0, st, a);
     NVQ_HIP_TRY(hipGetLastError());
-    hipLaunchKernelGGL((moe_down_kernel<FMT, 1, T, W2, 4>), dim3(a.K / 16), dim3(64 * W2), 0, st, a);
+    hipLaunchKernelGGL((moe_down_kernel<FMT, R2, T, W2, C2>), dim3(a.K / 16 / R2), dim3(64 * W2), 0, st, a);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
 }

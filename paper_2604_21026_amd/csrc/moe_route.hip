@@ -11,8 +11,8 @@ namespace nvq {
 
 namespace {
 
-constexpr int kRouteThreads = 512, kRouteWaves = kRouteThreads / 64;
-constexpr int kRouteMaxParts = 16;
+constexpr int kRouteThreads = 1024, kRouteWaves = kRouteThreads / 64;
+constexpr int kRouteMaxParts = 4;
 
 struct RouteArgs {
     const uint16_t *x, *router;
@@ -20,7 +20,7 @@ struct RouteArgs {
     int32_t *ids;
     float *weights;
     uint32_t *arrived;  // workspace
-    float *partial;     // [parts][M][E]
+    float *partial;     // [tiles][parts][M][16]: a workgroup's in one piece
     int tiles, parts, cols;  // columns of 32 inputs per part
 };
 
@@ -30,6 +30,9 @@ __device__ __forceinline__ uint32_t order_word(float f) {
     const uint32_t u = __float_as_uint(f + 0.0f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
+
+// The logit of such a word (minus zero: zero).
+__device__ __forceinline__ float of_order_word(uint32_t w) { return __uint_as_float(w & 0x80000000u ? w & 0x7fffffffu : ~w); }
 
 struct MaxWord {
     __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
@@ -43,21 +46,34 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
     return with_lane_xor<1>(v, MaxWord());
 }
 
+// The logits of a token from their parts, all requested at once (one after the other they were 14 of the 25 us that
+// 32 tokens and 128 experts took).
+template <int PER>
+__device__ __forceinline__ void ask_parts(const RouteArgs &a, int m, float (&v)[PER][kRouteMaxParts]) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+        const int e = 64 * j + lane;
+        const int in = e < a.E ? e : a.E - 1;
+        const float *const at = a.partial + ((int64_t)(in >> 4) * a.parts * a.M + m) * 16 + (in & 15);
+#pragma unroll
+        for (int p = 0; p < kRouteMaxParts; ++p)
+            v[j][p] = __hip_atomic_load(at + (int64_t)(p < a.parts ? p : 0) * a.M * 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+}
+
 // The chosen experts of one token, by one wave.  PER: experts per lane (E <= 64 * PER).
 template <int PER>
-__device__ __forceinline__ void choose(const RouteArgs &a, int m) {
+__device__ __forceinline__ void choose(const RouteArgs &a, int m, const float (&v)[PER][kRouteMaxParts]) {
     const int lane = threadIdx.x & 63;
     float l[PER];
     uint32_t key[PER];
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-        const int e = 64 * j + lane;
         l[j] = 0.0f;
-        if (e < a.E) {
-            for (int p = 0; p < a.parts; ++p)
-                l[j] += __hip_atomic_load(a.partial + ((int64_t)p * a.M + m) * a.E + e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        key[j] = e < a.E ? order_word(l[j]) : 0u;
+#pragma unroll
+        for (int p = 0; p < kRouteMaxParts; ++p) l[j] += p < a.parts ? v[j][p] : 0.0f;
+        key[j] = 64 * j + lane < a.E ? order_word(l[j]) : 0u;
     }
     float all = 0.0f, top = 0.0f, chosen = 0.0f, mine = 0.0f;
     int my_id = 0;
@@ -67,15 +83,13 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int m) {
         for (int j = 1; j < PER; ++j) best = key[j] > best ? key[j] : best;
         best = wave_max(best);
         int id = -1;
-        float value = 0.0f;
+        const float value = of_order_word(best);
 #pragma unroll
         for (int j = 0; j < PER; ++j) {
             const uint64_t at = __ballot(key[j] == best);
             if (id < 0 && at) {  // (uniform)
-                const int owner = __builtin_ctzll(at);
-                id = 64 * j + owner;
-                value = __shfl(l[j], owner, 64);
-                if (lane == owner) key[j] = 0u;
+                id = 64 * j + __builtin_ctzll(at);
+                if (lane == (id & 63)) key[j] = 0u;
             }
         }
         if (k == 0) {
@@ -99,13 +113,14 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int m) {
     }
 }
 
-template <int T>
+// T token tiles, PER experts per lane in the choice.
+template <int T, int PER>
 __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(RouteArgs a) {
     __shared__ float red[kRouteWaves][T * 4][64];
     __shared__ uint32_t last;
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int n = lane & 15, kb = lane >> 4;
-    const int tile = blockIdx.x % a.tiles, part = blockIdx.x / a.tiles;
+    const int tile = blockIdx.x / a.parts, part = blockIdx.x % a.parts;
     const int e0 = 16 * tile;
     const int all_cols = a.K / 32, col0 = part * a.cols;
     const int col1 = col0 + a.cols < all_cols ? col0 + a.cols : all_cols;
@@ -119,13 +134,23 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(RouteArgs a) {
         x[t] = reinterpret_cast<const char *>(a.x) + (int64_t)(m < a.M ? m : 0) * a.K * 2 + kb * 16;
         sum[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    for (int c = col0 + w; c < col1; c += kRouteWaves) {
-        const bf16x8 b = __builtin_bit_cast(bf16x8, load_stream(reinterpret_cast<const uint4 *>(r + (int64_t)c * 64)));
+    // Two columns at a time, a line of 128 bytes of every row.  (K of an odd number of columns: the last one by itself.)
+    for (int c = col0 + 2 * w; c < col1; c += 2 * kRouteWaves) {
+        const bool both = c + 1 < col1;  // (uniform)
+        uint4v b[2] = {}, v[2][T] = {};
 #pragma unroll
-        for (int t = 0; t < T; ++t) {
-            const bf16x8 v = __builtin_bit_cast(bf16x8, load_stream(reinterpret_cast<const uint4 *>(x[t] + (int64_t)c * 64)));
-            sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, b, sum[t], 0, 0, 0);
+        for (int k = 0; k < 2; ++k) {
+            if (k == 1 && !both) break;
+            b[k] = load_stream(reinterpret_cast<const uint4 *>(r + (int64_t)(c + k) * 64));
+#pragma unroll
+            for (int t = 0; t < T; ++t) v[k][t] = load_stream(reinterpret_cast<const uint4 *>(x[t] + (int64_t)(c + k) * 64));
         }
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int t = 0; t < T; ++t)
+                sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v[k][t]),
+                                                                __builtin_bit_cast(bf16x8, b[k]), sum[t], 0, 0, 0);
     }
 #pragma unroll
     for (int t = 0; t < T; ++t) {
@@ -141,30 +166,41 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(RouteArgs a) {
 #pragma unroll
         for (int k = 1; k < kRouteWaves; ++k) v += red[k][reg][l];
         if (m < a.M && e < a.E)
-            __hip_atomic_store(a.partial + ((int64_t)part * a.M + m) * a.E + e, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(a.partial + ((int64_t)blockIdx.x * a.M + m) * 16 + (l & 15), v, __ATOMIC_RELAXED,
+                               __HIP_MEMORY_SCOPE_AGENT);
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's partial logits are written
     __syncthreads();
     if (threadIdx.x == 0) {
-        // all partial logits of the workgroup before its arrival, those of the others after the last one's
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "agent");
+        // The workgroup's partial logits are written through to where all XCDs see them (agent-scope stores, waited for)
+        // before it arrives; the last one's loads are of that scope too and pass its caches by.  So no cache has to be written
+        // back or emptied here, as a fence of that scope would.
         const uint32_t before = __hip_atomic_fetch_add(a.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         last = before == gridDim.x - 1;
         if (last) __hip_atomic_store(a.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
     }
     __syncthreads();
     if (!last) return;
     for (int m = w; m < a.M; m += kRouteWaves) {
-        if (a.E <= 64)
-            choose<1>(a, m);
-        else if (a.E <= 128)
-            choose<2>(a, m);
-        else if (a.E <= 256)
-            choose<4>(a, m);
-        else
-            choose<8>(a, m);
+        float v[PER][kRouteMaxParts];
+        ask_parts<PER>(a, m, v);
+        choose<PER>(a, m, v);
     }
+}
+
+template <int T>
+int launch_route(const RouteArgs &a, hipStream_t st) {
+    const dim3 grid((unsigned)(a.tiles * a.parts)), block(kRouteThreads);
+    if (a.E <= 64)
+        hipLaunchKernelGGL((moe_route_kernel<T, 1>), grid, block, 0, st, a);
+    else if (a.E <= 128)
+        hipLaunchKernelGGL((moe_route_kernel<T, 2>), grid, block, 0, st, a);
+    else if (a.E <= 256)
+        hipLaunchKernelGGL((moe_route_kernel<T, 4>), grid, block, 0, st, a);
+    else
+        hipLaunchKernelGGL((moe_route_kernel<T, 8>), grid, block, 0, st, a);
+    NVQ_HIP_TRY(hipGetLastError());
+    return NVQ_OK;
 }
 
 constexpr size_t kRouteCounterBytes = 256;
@@ -178,7 +214,7 @@ bool route_shape(int M, int E) { return M >= 1 && M <= NVQ_MAX_M && E >= 1 && E 
 extern "C" size_t nvq_moe_route_workspace_bytes(int M, int E) {
     using namespace nvq;
     if (!route_shape(M, E)) return 0;
-    return kRouteCounterBytes + sizeof(float) * kRouteMaxParts * (size_t)M * E;
+    return kRouteCounterBytes + sizeof(float) * kRouteMaxParts * (size_t)M * ((E + 15) / 16 * 16);
 }
 
 extern "C" int nvq_moe_route(const uint16_t *x_bf16, const uint16_t *router_bf16, int M, int E, int K, int top_k,
@@ -208,13 +244,7 @@ extern "C" int nvq_moe_route(const uint16_t *x_bf16, const uint16_t *router_bf16
     const int cols = K / 32;
     int parts = (cols + 2 * kRouteWaves - 1) / (2 * kRouteWaves);
     parts = parts < kRouteMaxParts ? parts : kRouteMaxParts;
-    a.cols = (cols + parts - 1) / parts;
+    a.cols = ((cols + parts - 1) / parts + 1) / 2 * 2;  // (whole lines)
     a.parts = (cols + a.cols - 1) / a.cols;
-    const dim3 grid((unsigned)(a.tiles * a.parts)), block(kRouteThreads);
-    if (M <= 16)
-        hipLaunchKernelGGL(moe_route_kernel<1>, grid, block, 0, (hipStream_t)stream, a);
-    else
-        hipLaunchKernelGGL(moe_route_kernel<2>, grid, block, 0, (hipStream_t)stream, a);
-    NVQ_HIP_TRY(hipGetLastError());
-    return NVQ_OK;
+    return M <= 16 ? launch_route<1>(a, (hipStream_t)stream) : launch_route<2>(a, (hipStream_t)stream);
 }

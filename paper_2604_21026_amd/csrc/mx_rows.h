@@ -1,12 +1,13 @@
 // Products of 16-row tiles of 4-bit weights with bf16 activations of 16-token tiles on the matrix cores, for
 // both weight formats (nvq_gemv_mxfp4, nvq_moe_experts).
 //
-// A wave takes columns of 128 inputs: lane (n, kb) = (lane % 16, lane / 16) loads the 16 bytes of block 4c + kb of
-// row n and, after a 4x4 transpose across the lane-rows, has dword kb of the blocks 4c .. 4c + 3, eight inputs of
-// each.  One 16x16x32 MFMA multiplies one block of 16 rows with 16 tokens.  Microscaled codes become bf16 values,
-// scale and all, in one instruction per two (exact: two bits of significand and a power of two), and all blocks
-// add up in the accumulators; int4 codes enter as in the small-batch kernels of the int4 layers (mfma_act.h), and each
-// block's product is scaled on its way to the sum.
+// A wave takes columns of 128 inputs: lane (n, kb) = (lane % 16, lane / 16) loads the 16 bytes of block 4c + kb of row n.
+// Microscaled: MFMA i (16x16x32) takes dword i of every lane's block, eight codes, which become bf16 values, scale
+// and all, in one instruction per two (exact: two bits of significand and a power of two); the four MFMAs add into the
+// same sums.  Which inputs stand at which place of a product is free: the activations follow (lane (m, kb) supplies inputs
+// 32 kb + 8 i .. + 7 of its column), and a lane needs its own block's scale alone.
+// int4: each block's product is scaled on its way to the sum, so an MFMA is one block: a 4x4 transpose across the lane-rows
+// gives the lane dword kb of the blocks 4c .. 4c + 3 (mfma_act.h, as in the small-batch kernels of the int4 layers).
 #pragma once
 
 #include "mfma_act.h"
@@ -15,20 +16,11 @@ namespace nvq {
 
 #if defined(__HIPCC__)
 
-// One column of a row tile: a lane's 16 bytes of codes and its row's scales of the four blocks.
-template <int FMT>
-struct RowColumn;
-
-template <>
-struct RowColumn<NVQ_FMT_MXFP4> {
-    uint4v w;
-    uint32_t s;  // four scale bytes
-};
-
-template <>
-struct RowColumn<NVQ_FMT_INT4> {
-    uint4v w;
-    uint2v s;  // four fp16
+// C neighbouring columns of a row tile: a lane's 16 bytes of codes of each, and its row's scales of their 4 C blocks.
+template <int FMT, int C>
+struct RowColumns {
+    uint4v w[C];
+    uint32_t s[FMT == NVQ_FMT_MXFP4 ? C : 2 * C];  // four scale bytes, or fp16, per column
 };
 
 template <int FMT>
@@ -48,43 +40,46 @@ __device__ __forceinline__ RowAt row_at(const uint8_t *q, const void *s, int64_t
                  reinterpret_cast<const char *>(s) + row * G * scale_bytes<FMT>()};
 }
 
-template <int FMT>
-__device__ __forceinline__ void load_column(RowColumn<FMT> &c, const RowAt &at, int col, int kb) {
-    typedef uint32_t u32_any __attribute__((aligned(1)));
-    typedef uint2v u32x2_any __attribute__((aligned(2)));
-    c.w = load_stream(at.q + 4 * col + kb);
-    if constexpr (FMT == NVQ_FMT_MXFP4)
-        c.s = *(const __attribute__((address_space(1))) u32_any *)(at.s + 4 * col);
-    else
-        c.s = *(const __attribute__((address_space(1))) u32x2_any *)(at.s + 8 * col);
+// Columns col .. col + C - 1.  (A row's line of 128 bytes of codes is two columns: asked for together it is fetched once.  Scales
+// column by column, four bytes of a row at a time, fetched their line once per column.)
+template <int FMT, int C>
+__device__ __forceinline__ void load_columns(RowColumns<FMT, C> &c, const RowAt &at, int col, int kb) {
+    typedef uint32_t words __attribute__((ext_vector_type(FMT == NVQ_FMT_MXFP4 ? C : 2 * C)));
+    typedef words words_any __attribute__((aligned(1)));
+#pragma unroll
+    for (int b = 0; b < C; ++b) c.w[b] = load_stream(at.q + 4 * (col + b) + kb);
+    const words v = *(const __attribute__((address_space(1))) words_any *)(at.s + 4 * scale_bytes<FMT>() * col);
+#pragma unroll
+    for (int b = 0; b < (FMT == NVQ_FMT_MXFP4 ? C : 2 * C); ++b) c.s[b] = v[b];
 }
 
-// The last column, with `blocks` (1 to 3) of its four blocks: the others are zero.
+// Column col, with `blocks` (1 to 4) of its four blocks in the row: the others are zero.
 template <int FMT>
-__device__ __forceinline__ void load_last(RowColumn<FMT> &c, const RowAt &at, int col, int kb, int blocks) {
-    c.w = uint4v{0, 0, 0, 0};
-    if (kb < blocks) c.w = load_stream(at.q + 4 * col + kb);
+__device__ __forceinline__ void load_last(RowColumns<FMT, 1> &c, const RowAt &at, int col, int kb, int blocks) {
+    c.w[0] = uint4v{0, 0, 0, 0};
+    if (kb < blocks) c.w[0] = load_stream(at.q + 4 * col + kb);
     uint32_t s[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 3; ++i)
+    for (int i = 0; i < 4; ++i)
         if (i < blocks)
             s[i] = FMT == NVQ_FMT_MXFP4 ? as_global<uint8_t>(at.s)[4 * col + i] : as_global<uint16_t>(at.s)[4 * col + i];
-    if constexpr (FMT == NVQ_FMT_MXFP4)
-        c.s = s[0] | s[1] << 8 | s[2] << 16;
-    else
-        c.s = uint2v{s[0] | s[1] << 16, s[2]};
+    if constexpr (FMT == NVQ_FMT_MXFP4) {
+        c.s[0] = s[0] | s[1] << 8 | s[2] << 16 | s[3] << 24;
+    } else {
+        c.s[0] = s[0] | s[1] << 16;
+        c.s[1] = s[2] | s[3] << 16;
+    }
 }
 
-__device__ __forceinline__ void clear_column(RowColumn<NVQ_FMT_MXFP4> &c) { c.w = uint4v{0, 0, 0, 0}; }
-__device__ __forceinline__ void clear_column(RowColumn<NVQ_FMT_INT4> &c) { c.s = uint2v{0, 0}; }
+// 2^(byte - 127) of byte kb of the word, as the conversions take it (they look at the exponent alone, 0 standing for 2^-127).
+__device__ __forceinline__ float mx_scale_of(uint32_t four, int kb) {
+    return __uint_as_float(__builtin_amdgcn_ubfe(four, 8 * kb, 8) << 23);
+}
 
-// 2^(byte - 127) as the conversions take it (they look at the exponent alone, 0 standing for 2^-127).
-template <int I>
-__device__ __forceinline__ float mx_scale_of(uint32_t four) {
-    return __uint_as_float(I == 0   ? (four & 0xffu) << 23
-                           : I == 1 ? (four & 0xff00u) << 15
-                           : I == 2 ? (four & 0xff0000u) << 7
-                                    : four >> 24 << 23);
+// Where piece i of the lane's activations of a column begins (bytes from the token's first one of the column).
+template <int FMT>
+__device__ __forceinline__ int piece_at(int i, int kb) {
+    return FMT == NVQ_FMT_MXFP4 ? 64 * kb + 16 * i : 64 * i + 16 * kb;
 }
 
 // Eight codes as bf16 values with their block's scale.
@@ -96,21 +91,19 @@ __device__ __forceinline__ bf16x8 mx_values(uint32_t codes, float s) {
     return __builtin_bit_cast(bf16x8, v);
 }
 
-// sum[r][t] += tile r times token tile t over one column.  raw: the lane's pieces of its token's 128 inputs.
-template <int FMT, int R, int T>
-__device__ __forceinline__ void multiply_column(const RowColumn<FMT> (&col)[R], const uint4v (&raw)[T][4],
+// sum[r][t] += tile r times token tile t over column b of those loaded.  raw: the lane's pieces of its token's 128 inputs.
+template <int FMT, int R, int T, int C>
+__device__ __forceinline__ void multiply_column(const RowColumns<FMT, C> (&col)[R], int b, const uint4v (&raw)[T][4],
                                                 float4v (&sum)[R][T]) {
     typedef Act<NVQ_W4A16> A;
     if constexpr (FMT == NVQ_FMT_MXFP4) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            uint32_t q[4] = {col[r].w.x, col[r].w.y, col[r].w.z, col[r].w.w};
-            transpose_rows(q);
-            const float s[4] = {mx_scale_of<0>(col[r].s), mx_scale_of<1>(col[r].s), mx_scale_of<2>(col[r].s),
-                                mx_scale_of<3>(col[r].s)};
+            const uint32_t q[4] = {col[r].w[b].x, col[r].w[b].y, col[r].w[b].z, col[r].w[b].w};
+            const float s = mx_scale_of(col[r].s[b], (threadIdx.x & 63) >> 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const bf16x8 w = mx_values(q[i], s[i]);
+                const bf16x8 w = mx_values(q[i], s);
 #pragma unroll
                 for (int t = 0; t < T; ++t)
                     sum[r][t] = A::multiply(__builtin_bit_cast(bf16x8, raw[t][i]), w, sum[r][t]);
@@ -124,15 +117,14 @@ __device__ __forceinline__ void multiply_column(const RowColumn<FMT> (&col)[R], 
         float s[R][4];
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            q[r][0] = col[r].w.x;
-            q[r][1] = col[r].w.y;
-            q[r][2] = col[r].w.z;
-            q[r][3] = col[r].w.w;
+            q[r][0] = col[r].w[b].x;
+            q[r][1] = col[r].w[b].y;
+            q[r][2] = col[r].w[b].z;
+            q[r][3] = col[r].w[b].w;
             transpose_rows(q[r]);
-            s[r][0] = half_bits_to_float((uint16_t)(col[r].s.x & 0xffffu));
-            s[r][1] = half_bits_to_float((uint16_t)(col[r].s.x >> 16));
-            s[r][2] = half_bits_to_float((uint16_t)(col[r].s.y & 0xffffu));
-            s[r][3] = half_bits_to_float((uint16_t)(col[r].s.y >> 16));
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                s[r][i] = half_bits_to_float((uint16_t)(col[r].s[2 * b + (i >> 1)] >> (16 * (i & 1))));
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -153,49 +145,54 @@ __device__ __forceinline__ void multiply_column(const RowColumn<FMT> (&col)[R], 
     }
 }
 
-// sum[r][t] += R row tiles times T token tiles over the columns first, first + step, ... of K = 32 G inputs, B
-// columns requested at a time.  x[t]: the lane's token of tile t (bf16, at input 8 * kb).  Every lane of the
-// wave calls it.
-template <int FMT, int R, int T, int B>
-__device__ __forceinline__ void rows_times_tokens(const RowAt (&at)[R], const char *const (&x)[T], int G, int first,
-                                                  int step, float4v (&sum)[R][T]) {
-    typedef Act<NVQ_W4A16> A;
+// ... over the columns from `column` on, one by one, the waves in turn (`turn`: whose it is at the first).
+template <int FMT, int R, int T>
+__device__ __forceinline__ void last_columns(const RowAt (&at)[R], const char *const (&x)[T], int G, int column, int turn,
+                                             int first, int step, float4v (&sum)[R][T]) {
     const int kb = (threadIdx.x & 63) >> 4;
-    const int full = G >> 2;
-    for (int c0 = first; c0 < full; c0 += step * B) {
-        RowColumn<FMT> col[B][R];
-        uint4v raw[B][T][4];
-#pragma unroll
-        for (int b = 0; b < B; ++b) {
-            const int c = c0 + b * step;
-            const int cc = c < full ? c : full - 1;  // (wave-uniform)
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                load_column<FMT>(col[b][r], at[r], cc, kb);
-                if (c >= full) clear_column(col[b][r]);
-            }
-#pragma unroll
-            for (int t = 0; t < T; ++t) A::load(x[t] + (size_t)cc * 256, raw[b][t]);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int b = 0; b < B; ++b) multiply_column<FMT, R, T>(col[b], raw[b], sum);
-    }
-    const int blocks = G & 3;
-    if (blocks && full % step == first) {  // (wave-uniform)
-        RowColumn<FMT> col[R];
+    const int columns = (G + 3) >> 2;
+    for (int c = column; c < columns; ++c, ++turn) {
+        if (turn % step != first) continue;  // (wave-uniform)
+        const int blocks = G - 4 * c < 4 ? G - 4 * c : 4;
+        RowColumns<FMT, 1> col[R];
         uint4v raw[T][4];
 #pragma unroll
-        for (int r = 0; r < R; ++r) load_last<FMT>(col[r], at[r], full, kb, blocks);
+        for (int r = 0; r < R; ++r) load_last<FMT>(col[r], at[r], c, kb, blocks);
 #pragma unroll
         for (int t = 0; t < T; ++t)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 raw[t][i] = uint4v{0, 0, 0, 0};
-                if (i < blocks) raw[t][i] = *as_global<uint4v>(x[t] + (size_t)full * 256 + 64 * i);
+                if ((FMT == NVQ_FMT_MXFP4 ? kb : i) < blocks) raw[t][i] = *as_global<uint4v>(x[t] + (size_t)c * 256 + piece_at<FMT>(i, kb));
             }
-        multiply_column<FMT, R, T>(col, raw, sum);
+        multiply_column<FMT, R, T, 1>(col, 0, raw, sum);
     }
+}
+
+// sum[r][t] += R row tiles times T token tiles over K = 32 G inputs, shared out over `step` waves (this one: number `first`)
+// in passes of C columns, all of a pass requested before its first product.  x[t]: the lane's token of tile t (bf16).  Every lane of the wave calls it.
+template <int FMT, int R, int T, int C>
+__device__ __forceinline__ void rows_times_tokens(const RowAt (&at)[R], const char *const (&x)[T], int G, int first,
+                                                  int step, float4v (&sum)[R][T]) {
+    const int kb = (threadIdx.x & 63) >> 4;
+    const int passes = G / (4 * C);
+    for (int p = first; p < passes; p += step) {
+        RowColumns<FMT, C> col[R];
+        uint4v raw[C][T][4];
+#pragma unroll
+        for (int r = 0; r < R; ++r) load_columns<FMT, C>(col[r], at[r], p * C, kb);
+#pragma unroll
+        for (int b = 0; b < C; ++b)
+#pragma unroll
+            for (int t = 0; t < T; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    raw[b][t][i] = *as_global<uint4v>(x[t] + (size_t)(p * C + b) * 256 + piece_at<FMT>(i, kb));
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int b = 0; b < C; ++b) multiply_column<FMT, R, T, C>(col, b, raw[b], sum);
+    }
+    last_columns<FMT, R, T>(at, x, G, passes * C, passes, first, step, sum);
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
