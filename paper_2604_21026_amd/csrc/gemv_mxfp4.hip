@@ -2,16 +2,16 @@
 // blocks g of 2^(scale - 127) * sum_j code[n][32g + j] * x[m][32g + j], weights and activations unrounded, sums in
 // fp32.
 //
-// Bound by reading the weights once (17 bits per 32 of them... see mx_rows.h for the product): a workgroup owns 16 * R
-// rows, its W waves take the columns of 128 inputs in turn, and the partial tiles are added through LDS in wave
-// order.
+// Bound by reading the weights once, 17 bytes per 32 of them, which is 4.25 bits; mx_rows.h has the product.  Three kernels: row
+// tiles whose workgroups read the activations with the weights, for few rows or tokens; activations shared through LDS; and,
+// for many rows, activations that stay in registers.
 #include "mx_rows.h"
 
 namespace nvq {
 
 namespace {
 
-template <int R, int T, int W, int B>
+template <int R, int T, int W, int B, int Q>
 __global__ __launch_bounds__(64 * W) void gemv_mxfp4_kernel(const uint8_t *__restrict__ q,
                                                             const uint8_t *__restrict__ scales, int N, int G,
                                                             const uint16_t *__restrict__ x, int M,
@@ -38,7 +38,7 @@ __global__ __launch_bounds__(64 * W) void gemv_mxfp4_kernel(const uint8_t *__res
     for (int r = 0; r < R; ++r)
 #pragma unroll
         for (int t = 0; t < T; ++t) sum[r][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-    rows_times_tokens<NVQ_FMT_MXFP4, R, T, B>(at, xt, G, w, W, sum);
+    rows_times_tokens<NVQ_FMT_MXFP4, R, T, B, Q>(at, xt, G, w, W, sum);
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -105,11 +105,13 @@ __global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const ui
 #pragma unroll
         for (int k = 0; k < kMine; ++k) xs[buf][tid + k * kThreads] = v[k];
     };
-    auto weights = [&](RowColumns<NVQ_FMT_MXFP4, C> (&w)[R], int turn) {
+    auto weights = [&](Codes<C> (&w)[R], Scales<NVQ_FMT_MXFP4, C> (&sc)[R], int turn) {
         const int pass = turn * S + s;  // (uniform; past the end: the last one, with codes of zero)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            load_columns<NVQ_FMT_MXFP4, C>(w[r], at[r], (pass < passes ? pass : passes - 1) * C, kb);
+            const int c = (pass < passes ? pass : passes - 1) * C;
+            load_codes<C>(w[r], at[r], c, kb);
+            load_scales<NVQ_FMT_MXFP4, C>(sc[r], at[r], c);
         }
     };
     float4v sum[R][T];
@@ -120,19 +122,21 @@ __global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const ui
 
     if (turns > 0) {
         uint4v xr[kMine];
-        RowColumns<NVQ_FMT_MXFP4, C> w[R], next[R];
+        Codes<C> w[R], next[R];
+        Scales<NVQ_FMT_MXFP4, C> sc[R], next_sc[R];
         ask(xr, 0);
-        weights(w, 0);
+        weights(w, sc, 0);
         keep(xr, 0);
         ask(xr, 1 < turns ? 1 : 0);
-        auto one = [&](RowColumns<NVQ_FMT_MXFP4, C> (&now)[R], RowColumns<NVQ_FMT_MXFP4, C> (&then)[R], int turn) {
+        auto one = [&](Codes<C> (&now)[R], Scales<NVQ_FMT_MXFP4, C> (&now_sc)[R], Codes<C> (&then)[R],
+                       Scales<NVQ_FMT_MXFP4, C> (&then_sc)[R], int turn) {
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's pieces are in LDS
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             keep(xr, (turn + 1) & 1);
             ask(xr, turn + 2 < turns ? turn + 2 : turns - 1);
-            weights(then, turn + 1 < turns ? turn + 1 : turn);
+            weights(then, then_sc, turn + 1 < turns ? turn + 1 : turn);
             __builtin_amdgcn_sched_barrier(0);
             const bool mine = turn * S + s < passes;  // (uniform)
             const uint4v *const xb = &xs[turn & 1][s * (16 * T * kPieces)];
@@ -147,20 +151,20 @@ __global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const ui
 #pragma unroll
                     for (int r = 0; r < R; ++r) now[r].w[b] = uint4v{0, 0, 0, 0};
                 }
-                multiply_column<NVQ_FMT_MXFP4, R, T, C>(now, b, raw, sum);
+                multiply_column<NVQ_FMT_MXFP4, R, T, C, C>(now, b, now_sc, b, raw, sum);
             }
         };
         // (two turns: the registers of the weights change roles, they are not copied)
         for (int turn = 0; turn < turns; turn += 2) {
-            one(w, next, turn);
+            one(w, sc, next, next_sc, turn);
             if (turn + 1 >= turns) break;
-            one(next, w, turn + 1);
+            one(next, next_sc, w, sc, turn + 1);
         }
     }
     const char *xt[T];
 #pragma unroll
     for (int t = 0; t < T; ++t) {
-        const int m = 16 * t + n;
+        const int m = 16 * t + n;  // (tokens past the end read token 0: a product keeps tokens apart)
         xt[t] = reinterpret_cast<const char *>(x) + (size_t)(m < M ? m : 0) * G * 64;
     }
     last_columns<NVQ_FMT_MXFP4, R, T>(at, xt, G, passes * C, 0, s, S, sum);
@@ -199,6 +203,83 @@ __global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const ui
             }
 }
 
+
+// The activations stay in registers: wave w of W keeps those of C columns (4 C blocks of 32 inputs), of all tokens, for the whole
+// kernel, and the workgroup streams row tile after row tile past them, D tiles requested ahead.  So nothing but weights and their
+// scales is read in the loop (read again for every tile, one token's activations took 25 of 68 us at 128256 x 4096).  The last wave's
+// blocks may begin earlier than its share, where the activations are zero.
+// Partial tiles are added through LDS in wave order, by four waves that change from tile to tile.
+template <int T, int W, int C, int D>
+__global__ __launch_bounds__(64 * W) void gemv_mxfp4_resident_kernel(const uint8_t *__restrict__ q,
+                                                                     const uint8_t *__restrict__ scales, int N, int G,
+                                                                     const uint16_t *__restrict__ x, int M,
+                                                                     void *__restrict__ y, int y_dtype) {
+    __shared__ float red[2][W][T * 4][64];
+    const int lane = threadIdx.x & 63, n = lane & 15, kb = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int tiles = (N + 15) >> 4;
+    auto tile_of = [&](int it) { return it * (int)gridDim.x + (int)blockIdx.x; };  // the workgroup's tiles
+    const int share = 4 * C * w, b0 = share < G - 4 * C ? share : G - 4 * C;  // (G >= 4 C)
+
+    Codes<C> codes[D][1];
+    Scales<NVQ_FMT_MXFP4, C> sc[D][1];
+    auto load = [&](int d, int tile) {
+        const int row = 16 * (tile < tiles ? tile : tiles - 1) + n;
+        const RowAt at = row_at<NVQ_FMT_MXFP4>(q, scales, row < N ? row : N - 1, G);
+        const RowAt from = {at.q + b0, at.s + b0};
+        load_codes<C>(codes[d][0], from, 0, kb);
+        load_scales<NVQ_FMT_MXFP4, C>(sc[d][0], from, 0);
+    };
+#pragma unroll
+    for (int d = 0; d < D; ++d) load(d, tile_of(d));
+    uint4v xr[C][T][4];
+#pragma unroll
+    for (int b = 0; b < C; ++b)
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            const int block = b0 + 4 * b + kb, m = 16 * t + n;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                xr[b][t][i] = uint4v{0, 0, 0, 0};
+                if (block >= share && m < M)
+                    xr[b][t][i] = *as_global<uint4v>(reinterpret_cast<const char *>(x) + ((size_t)m * G + block) * 64 + 16 * i);
+            }
+        }
+    auto one = [&](int d, int tile, int it) {
+        float4v sum[1][T];
+#pragma unroll
+        for (int t = 0; t < T; ++t) sum[0][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int b = 0; b < C; ++b) multiply_column<NVQ_FMT_MXFP4, 1, T, C, C>(codes[d], b, sc[d], b, xr[b], sum);
+        load(d, tile_of(it + D));
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            wait_written(sum[0][t]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) red[it & 1][w][4 * t + j][lane] = sum[0][t][j];
+        }
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const int reg = (w + W - (it * 4 * T) % W) % W;  // (uniform)
+        if (reg < 4 * T) {
+            float v = red[it & 1][0][reg][lane];
+#pragma unroll
+            for (int k = 1; k < W; ++k) v += red[it & 1][k][reg][lane];
+            const int m = 16 * (reg >> 2) + 4 * kb + (reg & 3), row = 16 * tile + n;
+            if (m < M && row < N) store_global(y, y_dtype, (int64_t)m * N + row, v);
+        }
+    };
+    for (int it = 0; tile_of(it) < tiles; it += D) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            if (d > 0 && tile_of(it + d) >= tiles) break;
+            one(d, tile_of(it + d), it + d);
+        }
+    }
+}
+
 struct GemvArgs {
     const uint8_t *q, *s;
     const uint16_t *x;
@@ -210,7 +291,15 @@ struct GemvArgs {
 template <int R>
 int gemv_rows(const GemvArgs &a, hipStream_t st) {
     const dim3 grid((unsigned)(((int64_t)a.N + 16 * R - 1) / (16 * R)));
-    hipLaunchKernelGGL((gemv_mxfp4_kernel<R, 1, 4, 4>), grid, dim3(256), 0, st, a.q, a.s, a.N, a.G, a.x, a.M, a.y, a.y_dtype);
+    hipLaunchKernelGGL((gemv_mxfp4_kernel<R, 1, 4, R == 1 ? 4 : 2, R == 1 ? 4 : 8>), grid, dim3(256), 0, st, a.q, a.s, a.N, a.G, a.x, a.M, a.y, a.y_dtype);
+    NVQ_HIP_TRY(hipGetLastError());
+    return NVQ_OK;
+}
+
+template <int T, int C>
+int gemv_resident(const GemvArgs &a, int cus, hipStream_t st) {
+    hipLaunchKernelGGL((gemv_mxfp4_resident_kernel<T, 8, C, 2>), dim3((unsigned)cus), dim3(512), 0, st, a.q, a.s, a.N, a.G, a.x,
+                       a.M, a.y, a.y_dtype);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
 }
@@ -237,15 +326,21 @@ extern "C" int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
     if (!aligned(qweight, 16) || !aligned(x_bf16, 16) || !aligned(y, y_dtype == NVQ_F32 ? 4 : 2)) return NVQ_ERR_ALIGN;
     const hipStream_t st = (hipStream_t)stream;
     const GemvArgs a = {qweight, scales, x_bf16, y, N, K / 32, M, y_dtype};
-    const int64_t cus = device_cu_count(), tiles = ((int64_t)N + 15) / 16;
-    // us at (tokens, rows, inputs)   (1, 4096, 4096) (1, 14336, 4096) (1, 128256, 4096) (8, 14336, 4096) (16, 128256, 4096)
-    //   1 row tile per workgroup          3.9              10.0             68                15.2              148
-    //   2                                 5.3               8.7             54                11.5               94
-    //   4                                 8.4               8.9             50                 9.9               68
-    //   16, activations shared           22.4              22.6             51                23.3               54
+    const int cus = device_cu_count();
+    const int64_t tiles = ((int64_t)N + 15) / 16;
+    // Many row tiles, K that eight waves hold: (1, 128256, 4096) 44 us, at 16 tokens 50, at 32 62; below, a tile or two per workgroup,
+    // its start costs more ((1, 14336, 4096) 9.4).
+    if (tiles >= 16 * cus && a.G >= 16 && a.G <= 128) {
+        if (a.G <= 64) return M <= 16 ? gemv_resident<1, 2>(a, cus, st) : gemv_resident<2, 2>(a, cus, st);
+        return M <= 16 ? gemv_resident<1, 4>(a, cus, st) : gemv_resident<2, 4>(a, cus, st);
+    }
+    // us at (tokens, rows, inputs)   (1, 4096, 4096) (1, 14336, 4096) (8, 14336, 4096) (1, 128256, 4096) (16, 128256, 4096)
+    //   1 row tile per workgroup          3.9              10.0             15.1              68               148
+    //   2                                 5.2               8.6             11.1              54                94
+    //   4                                 7.9               8.3              9.5              48                68
+    //   16, activations shared           22.4              22.6             23.3              51                54
     if (M <= 8 || (M <= 16 && tiles < 16 * cus)) {
         if (tiles < 3 * cus) return gemv_rows<1>(a, st);
-        if (tiles < 8 * cus && M == 1) return gemv_rows<2>(a, st);
         return gemv_rows<4>(a, st);
     }
     if (M <= 16) return gemv_shared<1, 2, 8, 1, 4>(a, st);

@@ -13,6 +13,8 @@ namespace nvq {
 
 namespace {
 
+constexpr int kMaxParts = 4, kMaxChunks = NVQ_MAX_M * NVQ_MOE_MAX_TOP_K / 64;
+
 struct MoeArgs {
     const uint8_t *gu_q, *dn_q;
     const void *gu_s, *dn_s;
@@ -23,249 +25,267 @@ struct MoeArgs {
     int M, top_k, pairs;
     uint32_t per_token;  // 65536 / top_k, rounded up: pair / top_k = pair * per_token >> 16 below 512 pairs
     uint16_t *h;         // [M * top_k][F], row m * top_k + the first slot of the expert
+    int parts;           // of the second launch
+    float *partial;      // [row tiles][parts][M][rows of a tile]
+    uint32_t *arrived;   // [row tiles]
     void *y;
     int y_dtype;
 };
 
 __device__ __forceinline__ int token_of(const MoeArgs &a, int pair) { return (int)((uint32_t)pair * a.per_token >> 16); }
 
-// The tokens of one expert in ascending order, spread over a wave: lane n of a lane-row has number 16 t + n of them
-// for tile t (past the end: the first one's), and the pair of its first slot.
-template <int T>
-struct ExpertTokens {
-    int count, token[T], pair[T];
+// The pairs in a wave's registers, pair 64 t + lane.
+template <int CHUNKS>
+struct Pairs {
+    int id[CHUNKS];
+    float weight[CHUNKS];
 };
 
-// From the ids in memory; `first`: the lowest pair of the expert.
-template <int T>
-__device__ __forceinline__ ExpertTokens<T> tokens_of(const MoeArgs &a, int e, int &first) {
-    const int lane = threadIdx.x & 63, n = lane & 15;
-    ExpertTokens<T> et;
-    et.count = 0;
-    first = -1;
+template <int CHUNKS>
+__device__ __forceinline__ void load_ids(const MoeArgs &a, Pairs<CHUNKS> &p) {
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int t = 0; t < CHUNKS; ++t) p.id[t] = 64 * t + lane < a.pairs ? a.ids[64 * t + lane] : -1;
+}
+
+// The tokens of one expert in ascending order, spread over a wave: lane n of a lane-row has number 16 t + n of them for t =
+// 0, 1 (past the end: the first one's), the pair of its first slot and the sum of its slots' weights.
+struct ExpertTokens {
+    int count, first;  // first: the lowest pair
+    int token[2], pair[2];
+    float weight[2];
+};
+
+template <int CHUNKS>
+__device__ __forceinline__ ExpertTokens tokens_of(const MoeArgs &a, const Pairs<CHUNKS> &pairs, int e) {
+    const int n = threadIdx.x & 15;
+    ExpertTokens et = {0, -1, {0, 0}, {0, 0}, {0.0f, 0.0f}};
     int previous = -1;
-    for (int base = 0; base < a.pairs; base += 64) {
-        const int id = base + lane < a.pairs ? a.ids[base + lane] : -1;
-        uint64_t here = __ballot(id == e);
+#pragma unroll
+    for (int t = 0; t < CHUNKS; ++t) {
+        uint64_t here = __ballot(pairs.id[t] == e);
         while (here) {  // (uniform)
-            const int p = base + __builtin_ctzll(here);
+            const int bit = __builtin_ctzll(here), p = 64 * t + bit;
+            const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(pairs.weight[t]), bit));
             here &= here - 1;
             const int m = token_of(a, p);
-            if (m == previous) continue;
-            previous = m;
-            if (et.count == 0) {
-                first = p;
-#pragma unroll
-                for (int t = 0; t < T; ++t) {
-                    et.token[t] = m;
-                    et.pair[t] = p;
+            if (m != previous) {
+                previous = m;
+                if (et.count == 0) {
+                    et.first = p;
+                    et.token[0] = et.token[1] = m;
+                    et.pair[0] = et.pair[1] = p;
                 }
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    if (16 * k + n == et.count) {
+                        et.token[k] = m;
+                        et.pair[k] = p;
+                    }
+                ++et.count;
             }
 #pragma unroll
-            for (int t = 0; t < T; ++t)
-                if (16 * t + n == et.count) {
-                    et.token[t] = m;
-                    et.pair[t] = p;
-                }
-            ++et.count;
+            for (int k = 0; k < 2; ++k) et.weight[k] += 16 * k + n == et.count - 1 ? w : 0.0f;
         }
     }
     return et;
 }
 
-template <int FMT, int R, int T, int W, int B>
-__device__ __forceinline__ void gate_up(const MoeArgs &a, int e, int row0, const ExpertTokens<T> &et, float *red,
-                                        const int *pair_of) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    const int n = lane & 15, G = a.K / 32;
-    RowAt at[2 * R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int64_t row = (int64_t)e * 2 * a.F + row0 + 16 * r + n;
-        at[r] = row_at<FMT>(a.gu_q, a.gu_s, row, G);
-        at[R + r] = row_at<FMT>(a.gu_q, a.gu_s, row + a.F, G);
+// RG groups of KS waves: a group takes 16 * R gate rows and the up rows beside them, its waves share out K.
+template <int FMT, int R, int RG, int KS, int C, int Q, int CHUNKS>
+__global__ __launch_bounds__(64 * RG * KS) void moe_gate_up_kernel(MoeArgs a) {
+    constexpr int kThreads = 64 * RG * KS;
+    const int lane = threadIdx.x & 63, n = lane & 15, kb = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = wave / KS, s = wave % KS;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && a.parts > 1) {  // the counters of the second launch
+        for (int i = threadIdx.x; i < a.K / 16; i += kThreads) a.arrived[i] = 0;
     }
-    const char *x[T];
-    float4v sum[2 * R][T];
-#pragma unroll
-    for (int t = 0; t < T; ++t) {
-        x[t] = reinterpret_cast<const char *>(a.x) + (int64_t)et.token[t] * a.K * 2;
-#pragma unroll
-        for (int r = 0; r < 2 * R; ++r) sum[r][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    rows_times_tokens<FMT, 2 * R, T, B>(at, x, G, w, W, sum);
-    constexpr int kRegs = 2 * R * T * 4;
-#pragma unroll
-    for (int r = 0; r < 2 * R; ++r)
-#pragma unroll
-        for (int t = 0; t < T; ++t)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) red[(w * kRegs + (r * T + t) * 4 + j) * 64 + lane] = sum[r][t][j];
-    __syncthreads();
-    for (int i = threadIdx.x; i < R * T * 4 * 64; i += 64 * W) {
-        const int reg = i >> 6, l = i & 63;
-        const int t = (reg >> 2) % T, r = (reg >> 2) / T;
-        const int number = 16 * t + 4 * (l >> 4) + (reg & 3);
-        float g = 0.0f, u = 0.0f;
-#pragma unroll
-        for (int k = 0; k < W; ++k) {
-            g += red[(k * kRegs + reg) * 64 + l];
-            u += red[(k * kRegs + R * T * 4 + reg) * 64 + l];
-        }
-        if (number < et.count)
-            a.h[(int64_t)pair_of[number] * a.F + row0 + 16 * r + (l & 15)] = float_to_bf16_bits(silu_mul_one(g, u));
-    }
-}
-
-template <int FMT, int R, int T, int W, int B>
-__global__ __launch_bounds__(64 * W) void moe_gate_up_kernel(MoeArgs a) {
-    __shared__ float red[W * 2 * R * T * 4 * 64];
-    __shared__ int pair_of[32];
-    const int row0 = blockIdx.x * (16 * R);
     // the second grid axis: experts, or pairs where there are fewer (a pair that is not the first of its expert has
     // nothing to do)
+    Pairs<CHUNKS> pairs;
+    load_ids<CHUNKS>(a, pairs);
+#pragma unroll
+    for (int t = 0; t < CHUNKS; ++t) pairs.weight[t] = 0.0f;
     const bool by_expert = a.E <= a.pairs;
     const int e = by_expert ? (int)blockIdx.y : a.ids[blockIdx.y];
     if ((uint32_t)e >= (uint32_t)a.E) return;
-    int first;
-    const ExpertTokens<T> et = tokens_of<T>(a, e, first);
-    if (et.count == 0 || (!by_expert && first != (int)blockIdx.y)) return;
-    if (threadIdx.x < 16) {
+    const ExpertTokens et = tokens_of<CHUNKS>(a, pairs, e);
+    if (et.count == 0 || (!by_expert && et.first != (int)blockIdx.y)) return;
+    const int row0 = (blockIdx.x * RG + g) * (16 * R), G = a.K / 32;
+    const bool rows = row0 < a.F;  // (uniform; F is a multiple of 32, 16 * R of 32 or less)
+    RowAt at[2 * R];
 #pragma unroll
-        for (int t = 0; t < T; ++t) pair_of[16 * t + threadIdx.x] = et.pair[t];
+    for (int r = 0; r < R; ++r) {
+        const int64_t row = (int64_t)e * 2 * a.F + (rows ? row0 : 0) + 16 * r + n;
+        at[r] = row_at<FMT>(a.gu_q, a.gu_s, row, G);
+        at[R + r] = row_at<FMT>(a.gu_q, a.gu_s, row + a.F, G);
     }
-    if (T == 1 || et.count > 16) {  // (the barrier inside comes before pair_of is read)
-        gate_up<FMT, R, T, W, B>(a, e, row0, et, red, pair_of);
-    } else {
-        const ExpertTokens<1> one = {et.count, {et.token[0]}, {et.pair[0]}};
-        gate_up<FMT, R, 1, W, B>(a, e, row0, one, red, pair_of);
-    }
-}
-
-// One expert's part of a wave: columns first, first + step, ... of its inputs h, added to the wave's sums out[token][row].
-template <int FMT, int R, int T, int B>
-__device__ __forceinline__ void add_expert(const MoeArgs &a, const RowAt (&at)[R], const int (&token)[T],
-                                           const int (&pair)[T], const float (&weight)[T], int count, int first, int step,
-                                           float *out) {
-    const int lane = threadIdx.x & 63, n = lane & 15, kb = lane >> 4;
-    const char *h[T];
-    float4v sum[R][T];
+    // (an expert of more than 16 tokens reads its weights twice)
+    for (int t = 0; 16 * t < et.count; ++t) {
+        const char *const x[1] = {reinterpret_cast<const char *>(a.x) + (int64_t)(t ? et.token[1] : et.token[0]) * a.K * 2};
+        float4v sum[2 * R][1];
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-        h[t] = reinterpret_cast<const char *>(a.h) + (int64_t)pair[t] * a.F * 2;
+        for (int r = 0; r < 2 * R; ++r) sum[r][0] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        if (rows) rows_times_tokens<FMT, 2 * R, 1, C, Q>(at, x, G, s, KS, sum);
 #pragma unroll
-        for (int r = 0; r < R; ++r) sum[r][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-    }
-    rows_times_tokens<FMT, R, T, B>(at, h, a.F / 32, first, step, sum);
+        for (int r = 0; r < 2 * R; ++r) wait_written(sum[r][0]);
+        if constexpr (KS > 1) {
+            __shared__ float4v red[RG][KS - 1][2 * R][64];
+            if (s > 0) {
 #pragma unroll
-    for (int t = 0; t < T; ++t)
+                for (int r = 0; r < 2 * R; ++r) red[g][s - 1][r][lane] = sum[r][0];
+            }
+            __syncthreads();
+            if (s == 0) {
+#pragma unroll
+                for (int k = 0; k < KS - 1; ++k)
+#pragma unroll
+                    for (int r = 0; r < 2 * R; ++r) sum[r][0] += red[g][k][r][lane];
+            }
+            __syncthreads();
+        }
+        if (s > 0 || !rows) continue;
+        const int mine = t ? et.pair[1] : et.pair[0];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int m = __shfl(token[t], 4 * kb + j, 64);
-            const float w = __shfl(weight[t], 4 * kb + j, 64);
-            if (16 * t + 4 * kb + j < count) {
+            const int pair = __shfl(mine, 4 * kb + j, 64);
+            if (16 * t + 4 * kb + j < et.count) {
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    float *const o = out + (m * R + r) * 16 + n;
-                    *o = fmaf(w, sum[r][t][j], *o);
-                }
+                for (int r = 0; r < R; ++r)
+                    a.h[(int64_t)pair * a.F + row0 + 16 * r + n] = float_to_bf16_bits(silu_mul_one(sum[r][0][j], sum[R + r][0][j]));
             }
         }
+    }
 }
 
-template <int FMT, int R, int T, int W, int B>
+template <int FMT, int R, int W, int C, int Q, int CHUNKS>
 __global__ __launch_bounds__(64 * W) void moe_down_kernel(MoeArgs a) {
-    constexpr int kOut = 16 * T * R * 16;  // a wave's sums
-    __shared__ float out[W * kOut];
-    __shared__ uint32_t chosen[NVQ_MOE_MAX_EXPERTS];  // tokens of each expert
-    __shared__ uint16_t active[NVQ_MOE_MAX_EXPERTS];
-    __shared__ int ids[NVQ_MAX_M * NVQ_MOE_MAX_TOP_K];
-    __shared__ float weights[NVQ_MAX_M * NVQ_MOE_MAX_TOP_K];
-    __shared__ int nactive;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15;
-    const int row0 = blockIdx.x * (16 * R);
-    for (int i = threadIdx.x; i < a.E; i += 64 * W) chosen[i] = 0;
-    for (int i = threadIdx.x; i < W * kOut; i += 64 * W) out[i] = 0.0f;
-    __syncthreads();
-    for (int i = threadIdx.x; i < a.pairs; i += 64 * W) {
-        const int id = a.ids[i];
-        ids[i] = id;
-        weights[i] = a.weights[i];
-        if ((uint32_t)id < (uint32_t)a.E) atomicOr(&chosen[id], 1u << token_of(a, i));
-    }
-    __syncthreads();
-    if (w == 0) {
-        int count = 0;
-        for (int base = 0; base < a.E; base += 64) {
-            const bool is = base + lane < a.E && chosen[base + lane] != 0;
-            const uint64_t b = __ballot(is);
-            if (is) active[count + __popcll(b & ((1ull << lane) - 1))] = (uint16_t)(base + lane);
-            count += __popcll(b);
-        }
-        if (lane == 0) nactive = count;
-    }
-    __syncthreads();
-    const int G = a.F / 32;
-    // experts in `split` parts of their columns where there are fewer experts than waves
-    const int split = nactive == 0 || nactive >= W ? 1 : (W + nactive - 1) / nactive;
-    for (int item = w; item < nactive * split; item += W) {  // (uniform)
-        const int e = __builtin_amdgcn_readfirstlane(active[item / split]);
-        const uint32_t tokens = (uint32_t)__builtin_amdgcn_readfirstlane((int)chosen[e]);
-        const int count = __popc(tokens);
-        int token[T], pair[T];
-        float weight[T];
+    constexpr int kTokens = CHUNKS == 1 ? 16 : NVQ_MAX_M;  // (CHUNKS == 1: up to 16 tokens)
+    constexpr int kOut = kTokens * R * 16;                 // a wave's sums
+    __shared__ float out[W][kOut];
+    __shared__ uint32_t chosen[NVQ_MOE_MAX_EXPERTS / 32];
+    __shared__ uint32_t last;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4;
+    const int row0 = blockIdx.x * (16 * R), part = blockIdx.y;
+    Pairs<CHUNKS> pairs;
+    load_ids<CHUNKS>(a, pairs);
 #pragma unroll
-        for (int t = 0; t < T; ++t) {
-            // the lane's token: bit number 16 t + n of those set (the first one's past the end)
-            uint32_t left = tokens;
-            const int skip = 16 * t + n < count ? 16 * t + n : 0;
-            for (int k = 0; k < skip; ++k) left &= left - 1;
-            token[t] = __builtin_ctz(left);
-            weight[t] = 0.0f;
-            pair[t] = 0;
-            for (int s = a.top_k - 1; s >= 0; --s) {
-                const int p = token[t] * a.top_k + s;
-                if (ids[p] == e) {
-                    pair[t] = p;
-                    weight[t] += weights[p];
-                }
+    for (int t = 0; t < CHUNKS; ++t) pairs.weight[t] = 64 * t + lane < a.pairs ? a.weights[64 * t + lane] : 0.0f;
+    // the experts that some token chose, a bit for each
+    if (w == 0) {
+        if (lane < NVQ_MOE_MAX_EXPERTS / 32) chosen[lane] = 0;
+#pragma unroll
+        for (int t = 0; t < CHUNKS; ++t)
+            if ((uint32_t)pairs.id[t] < (uint32_t)a.E) atomicOr(&chosen[pairs.id[t] >> 5], 1u << (pairs.id[t] & 31));
+    }
+    for (int i = lane; i < kOut; i += 64) out[w][i] = 0.0f;
+    __syncthreads();
+    const uint32_t word = chosen[lane & (NVQ_MOE_MAX_EXPERTS / 32 - 1)];
+    const int words = (a.E + 31) >> 5;
+    int active = 0;
+    for (int i = 0; i < words; ++i) active += __builtin_popcount((uint32_t)__builtin_amdgcn_readlane((int)word, i));
+    // The workgroups of all parts share the experts out among their waves; where there are more waves than experts, each in
+    // `split` slices of its inputs.
+    const int workers = a.parts * W, G = a.F / 32;
+    int split = active == 0 || active >= workers ? 1 : (workers + active - 1) / active;
+    const int passes = (G + 4 * Q - 1) / (4 * Q);
+    split = split < passes ? split : passes;
+    for (int item = part * W + w; item < active * split; item += workers) {  // (uniform)
+        int skip = item / split, e = 0;
+        for (int i = 0; i < words; ++i) {
+            uint32_t bits = (uint32_t)__builtin_amdgcn_readlane((int)word, i);
+            const int count = __builtin_popcount(bits);
+            if (skip >= count) {
+                skip -= count;
+                continue;
             }
+            for (; skip > 0; --skip) bits &= bits - 1;
+            e = 32 * i + __builtin_ctz(bits);
+            break;
         }
+        e = __builtin_amdgcn_readfirstlane(e);
+        const ExpertTokens et = tokens_of<CHUNKS>(a, pairs, e);
         RowAt at[R];
 #pragma unroll
         for (int r = 0; r < R; ++r)
             at[r] = row_at<FMT>(a.dn_q, a.dn_s, (int64_t)e * a.K + row0 + 16 * r + n, G);
-        if (T == 1 || count > 16) {
-            add_expert<FMT, R, T, B>(a, at, token, pair, weight, count, item % split, split, out + w * kOut);
-        } else {
-            const int token1[1] = {token[0]}, pair1[1] = {pair[0]};
-            const float weight1[1] = {weight[0]};
-            add_expert<FMT, R, 1, B>(a, at, token1, pair1, weight1, count, item % split, split, out + w * kOut);
+        for (int t = 0; 16 * t < et.count; ++t) {
+            const int token = t ? et.token[1] : et.token[0], pair = t ? et.pair[1] : et.pair[0];
+            const float weight = t ? et.weight[1] : et.weight[0];
+            const char *const h[1] = {reinterpret_cast<const char *>(a.h) + (int64_t)pair * a.F * 2};
+            float4v sum[R][1];
+#pragma unroll
+            for (int r = 0; r < R; ++r) sum[r][0] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+            rows_times_tokens<FMT, R, 1, C, Q>(at, h, G, item % split, split, sum);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int m = __shfl(token, 4 * kb + j, 64);
+                const float wt = __shfl(weight, 4 * kb + j, 64);
+                if (16 * t + 4 * kb + j < et.count) {
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        float *const o = &out[w][(m * R + r) * 16 + n];
+                        *o = fmaf(wt, sum[r][0][j], *o);
+                    }
+                }
+            }
         }
     }
     __syncthreads();
+    float *const mine = a.partial + ((int64_t)blockIdx.x * a.parts + part) * (a.M * R * 16);
     for (int i = threadIdx.x; i < a.M * R * 16; i += 64 * W) {
-        float v = out[i];
+        float v = out[0][i];
 #pragma unroll
-        for (int k = 1; k < W; ++k) v += out[k * kOut + i];
-        store_global(a.y, a.y_dtype, (int64_t)(i / (R * 16)) * a.K + row0 + i % (R * 16), v);
+        for (int k = 1; k < W; ++k) v += out[k][i];
+        if (a.parts == 1)
+            store_global(a.y, a.y_dtype, (int64_t)(i / (R * 16)) * a.K + row0 + i % (R * 16), v);
+        else
+            __hip_atomic_store(mine + i, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    if (a.parts == 1) return;
+    // The parts' sums are added, in their order, by the workgroup that arrives last: they are written through to where all XCDs
+    // see them before it arrives, and read past its caches.
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    __syncthreads();
+    if (threadIdx.x == 0)
+        last = __hip_atomic_fetch_add(&a.arrived[blockIdx.x], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) ==
+               (uint32_t)a.parts - 1;
+    __syncthreads();
+    if (!last) return;
+    const float *const all = a.partial + (int64_t)blockIdx.x * a.parts * (a.M * R * 16);
+    for (int i = threadIdx.x; i < a.M * R * 16; i += 64 * W) {
+        float v[kMaxParts];
+#pragma unroll
+        for (int k = 0; k < kMaxParts; ++k)
+            v[k] = __hip_atomic_load(all + (int64_t)(k < a.parts ? k : 0) * (a.M * R * 16) + i, __ATOMIC_RELAXED,
+                                     __HIP_MEMORY_SCOPE_AGENT);
+        float s = v[0];
+#pragma unroll
+        for (int k = 1; k < kMaxParts; ++k) s += k < a.parts ? v[k] : 0.0f;
+        store_global(a.y, a.y_dtype, (int64_t)(i / (R * 16)) * a.K + row0 + i % (R * 16), s);
     }
 }
 
-template <int FMT, int T>
-int launch_experts(const MoeArgs &a, hipStream_t st) {
 #ifndef R1
 #define R1 1
+#define G1 1
 #define W1 4
 #define C1 2
 #define R2 1
 #define W2 8
-#define C2 4
+#define C2 2
+#define Q1 4
+#define Q2 4
 #endif
+#ifndef NP
+#define NP 1
+#endif
+template <int FMT, int CHUNKS>
+int launch_experts(const MoeArgs &a, hipStream_t st) {
     const unsigned experts = (unsigned)(a.E <= a.pairs ? a.E : a.pairs);
-    hipLaunchKernelGGL((moe_gate_up_kernel<FMT, R1, T, W1, C1>), dim3(a.F / 16 / R1, experts), dim3(64 * W1), 0, st, a);
+    hipLaunchKernelGGL((moe_gate_up_kernel<FMT, R1, G1, W1, C1, Q1, CHUNKS>), dim3((a.F / 16 + R1 * G1 - 1) / (R1 * G1), experts), dim3(64 * W1 * G1), 0, st, a);
     NVQ_HIP_TRY(hipGetLastError());
-    hipLaunchKernelGGL((moe_down_kernel<FMT, R2, T, W2, C2>), dim3(a.K / 16 / R2), dim3(64 * W2), 0, st, a);
+    hipLaunchKernelGGL((moe_down_kernel<FMT, R2, W2, C2, Q2, CHUNKS>), dim3(a.K / 16 / R2, a.parts), dim3(64 * W2), 0, st, a);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
 }
@@ -283,9 +303,27 @@ int check_experts(const nvq_experts *e, int M, int top_k) {
 
 }  // namespace nvq
 
+namespace {
+
+// The workspace: h, the parts' sums, the counters.
+struct MoeRooms {
+    size_t h, partial, arrived, all;
+};
+MoeRooms moe_rooms(const nvq_experts *e, int M, int top_k) {
+    const auto whole = [](size_t bytes) { return (bytes + 255) / 256 * 256; };
+    MoeRooms r;
+    r.h = 0;
+    r.partial = r.h + whole((size_t)M * top_k * e->F * sizeof(uint16_t));
+    r.arrived = r.partial + whole(sizeof(float) * nvq::kMaxParts * (size_t)M * e->K);
+    r.all = r.arrived + whole(sizeof(uint32_t) * (e->K / 16));
+    return r;
+}
+
+}  // namespace
+
 extern "C" size_t nvq_moe_workspace_bytes(const nvq_experts *experts, int M, int top_k) {
     if (nvq::check_experts(experts, M, top_k) != NVQ_OK) return 0;
-    return ((size_t)M * top_k * experts->F * sizeof(uint16_t) + 255) / 256 * 256;
+    return moe_rooms(experts, M, top_k).all;
 }
 
 extern "C" int nvq_moe_experts(const nvq_experts *experts, const uint16_t *x_bf16, const int32_t *ids,
@@ -320,11 +358,16 @@ extern "C" int nvq_moe_experts(const nvq_experts *experts, const uint16_t *x_bf1
     a.top_k = top_k;
     a.pairs = M * top_k;
     a.per_token = (65536u + top_k - 1) / top_k;
+    const MoeRooms rooms = moe_rooms(experts, M, top_k);
     a.h = static_cast<uint16_t *>(workspace);
+    a.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + rooms.partial);
+    a.arrived = reinterpret_cast<uint32_t *>(static_cast<char *>(workspace) + rooms.arrived);
+    a.parts = NP;
     a.y = y;
     a.y_dtype = y_dtype;
     const hipStream_t st = (hipStream_t)stream;
+    const bool small = a.pairs <= 64 && M <= 16;
     if (experts->format == NVQ_FMT_INT4)
-        return M <= 16 ? launch_experts<NVQ_FMT_INT4, 1>(a, st) : launch_experts<NVQ_FMT_INT4, 2>(a, st);
-    return M <= 16 ? launch_experts<NVQ_FMT_MXFP4, 1>(a, st) : launch_experts<NVQ_FMT_MXFP4, 2>(a, st);
+        return small ? launch_experts<NVQ_FMT_INT4, 1>(a, st) : launch_experts<NVQ_FMT_INT4, kMaxChunks>(a, st);
+    return small ? launch_experts<NVQ_FMT_MXFP4, 1>(a, st) : launch_experts<NVQ_FMT_MXFP4, kMaxChunks>(a, st);
 }

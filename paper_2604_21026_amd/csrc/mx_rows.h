@@ -16,11 +16,14 @@ namespace nvq {
 
 #if defined(__HIPCC__)
 
-// C neighbouring columns of a row tile: a lane's 16 bytes of codes of each, and its row's scales of their 4 C blocks.
-template <int FMT, int C>
-struct RowColumns {
+// Codes of C neighbouring columns of a row tile, a lane's 16 bytes of each, and its row's scales of 4 Q blocks, Q columns.
+template <int C>
+struct Codes {
     uint4v w[C];
-    uint32_t s[FMT == NVQ_FMT_MXFP4 ? C : 2 * C];  // four scale bytes, or fp16, per column
+};
+template <int FMT, int Q>
+struct Scales {
+    uint32_t s[FMT == NVQ_FMT_MXFP4 ? Q : 2 * Q];  // four scale bytes, or fp16, per column
 };
 
 template <int FMT>
@@ -40,22 +43,31 @@ __device__ __forceinline__ RowAt row_at(const uint8_t *q, const void *s, int64_t
                  reinterpret_cast<const char *>(s) + row * G * scale_bytes<FMT>()};
 }
 
-// Columns col .. col + C - 1.  (A row's line of 128 bytes of codes is two columns: asked for together it is fetched once.  Scales
-// column by column, four bytes of a row at a time, fetched their line once per column.)
-template <int FMT, int C>
-__device__ __forceinline__ void load_columns(RowColumns<FMT, C> &c, const RowAt &at, int col, int kb) {
-    typedef uint32_t words __attribute__((ext_vector_type(FMT == NVQ_FMT_MXFP4 ? C : 2 * C)));
-    typedef words words_any __attribute__((aligned(1)));
+// Columns col .. of that many.  (A row's line of 128 bytes of codes is two columns: asked for together it is fetched once.)
+template <int C>
+__device__ __forceinline__ void load_codes(Codes<C> &c, const RowAt &at, int col, int kb) {
 #pragma unroll
     for (int b = 0; b < C; ++b) c.w[b] = load_stream(at.q + 4 * (col + b) + kb);
-    const words v = *(const __attribute__((address_space(1))) words_any *)(at.s + 4 * scale_bytes<FMT>() * col);
+}
+// (A line of scales serves 32 columns of microscaled rows; asked for a column or two at a time it was fetched again every time, as many
+// bytes as the codes are.)
+template <int FMT, int Q>
+__device__ __forceinline__ void load_scales(Scales<FMT, Q> &c, const RowAt &at, int col) {
+    constexpr int kWords = FMT == NVQ_FMT_MXFP4 ? Q : 2 * Q, kWide = kWords < 4 ? kWords : 4;
+    typedef uint32_t words __attribute__((ext_vector_type(kWide)));
+    typedef words words_any __attribute__((aligned(1)));
+    static_assert(kWords % kWide == 0, "");
 #pragma unroll
-    for (int b = 0; b < (FMT == NVQ_FMT_MXFP4 ? C : 2 * C); ++b) c.s[b] = v[b];
+    for (int k = 0; k < kWords / kWide; ++k) {
+        const words v = *(const __attribute__((address_space(1))) words_any *)(at.s + 4 * scale_bytes<FMT>() * col + 4 * kWide * k);
+#pragma unroll
+        for (int b = 0; b < kWide; ++b) c.s[kWide * k + b] = v[b];
+    }
 }
 
 // Column col, with `blocks` (1 to 4) of its four blocks in the row: the others are zero.
 template <int FMT>
-__device__ __forceinline__ void load_last(RowColumns<FMT, 1> &c, const RowAt &at, int col, int kb, int blocks) {
+__device__ __forceinline__ void load_last(Codes<1> &c, Scales<FMT, 1> &sc, const RowAt &at, int col, int kb, int blocks) {
     c.w[0] = uint4v{0, 0, 0, 0};
     if (kb < blocks) c.w[0] = load_stream(at.q + 4 * col + kb);
     uint32_t s[4] = {0, 0, 0, 0};
@@ -64,10 +76,10 @@ __device__ __forceinline__ void load_last(RowColumns<FMT, 1> &c, const RowAt &at
         if (i < blocks)
             s[i] = FMT == NVQ_FMT_MXFP4 ? as_global<uint8_t>(at.s)[4 * col + i] : as_global<uint16_t>(at.s)[4 * col + i];
     if constexpr (FMT == NVQ_FMT_MXFP4) {
-        c.s[0] = s[0] | s[1] << 8 | s[2] << 16 | s[3] << 24;
+        sc.s[0] = s[0] | s[1] << 8 | s[2] << 16 | s[3] << 24;
     } else {
-        c.s[0] = s[0] | s[1] << 16;
-        c.s[1] = s[2] | s[3] << 16;
+        sc.s[0] = s[0] | s[1] << 16;
+        sc.s[1] = s[2] | s[3] << 16;
     }
 }
 
@@ -91,16 +103,17 @@ __device__ __forceinline__ bf16x8 mx_values(uint32_t codes, float s) {
     return __builtin_bit_cast(bf16x8, v);
 }
 
-// sum[r][t] += tile r times token tile t over column b of those loaded.  raw: the lane's pieces of its token's 128 inputs.
-template <int FMT, int R, int T, int C>
-__device__ __forceinline__ void multiply_column(const RowColumns<FMT, C> (&col)[R], int b, const uint4v (&raw)[T][4],
-                                                float4v (&sum)[R][T]) {
+// sum[r][t] += tile r times token tile t over column b of the codes loaded, qb of the scales.  raw: the lane's pieces of its
+// token's 128 inputs.
+template <int FMT, int R, int T, int C, int Q>
+__device__ __forceinline__ void multiply_column(const Codes<C> (&col)[R], int b, const Scales<FMT, Q> (&sc)[R], int qb,
+                                                const uint4v (&raw)[T][4], float4v (&sum)[R][T]) {
     typedef Act<NVQ_W4A16> A;
     if constexpr (FMT == NVQ_FMT_MXFP4) {
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const uint32_t q[4] = {col[r].w[b].x, col[r].w[b].y, col[r].w[b].z, col[r].w[b].w};
-            const float s = mx_scale_of(col[r].s[b], (threadIdx.x & 63) >> 4);
+            const float s = mx_scale_of(sc[r].s[qb], (threadIdx.x & 63) >> 4);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const bf16x8 w = mx_values(q[i], s);
@@ -124,7 +137,7 @@ __device__ __forceinline__ void multiply_column(const RowColumns<FMT, C> (&col)[
             transpose_rows(q[r]);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                s[r][i] = half_bits_to_float((uint16_t)(col[r].s[2 * b + (i >> 1)] >> (16 * (i & 1))));
+                s[r][i] = half_bits_to_float((uint16_t)(sc[r].s[2 * qb + (i >> 1)] >> (16 * (i & 1))));
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -154,10 +167,18 @@ __device__ __forceinline__ void last_columns(const RowAt (&at)[R], const char *c
     for (int c = column; c < columns; ++c, ++turn) {
         if (turn % step != first) continue;  // (wave-uniform)
         const int blocks = G - 4 * c < 4 ? G - 4 * c : 4;
-        RowColumns<FMT, 1> col[R];
+        Codes<1> col[R];
+        Scales<FMT, 1> sc[R];
         uint4v raw[T][4];
 #pragma unroll
-        for (int r = 0; r < R; ++r) load_last<FMT>(col[r], at[r], c, kb, blocks);
+        for (int r = 0; r < R; ++r) {
+            if (blocks == 4) {  // (uniform)
+                load_codes<1>(col[r], at[r], c, kb);
+                load_scales<FMT, 1>(sc[r], at[r], c);
+            } else {
+                load_last<FMT>(col[r], sc[r], at[r], c, kb, blocks);
+            }
+        }
 #pragma unroll
         for (int t = 0; t < T; ++t)
 #pragma unroll
@@ -165,34 +186,65 @@ __device__ __forceinline__ void last_columns(const RowAt (&at)[R], const char *c
                 raw[t][i] = uint4v{0, 0, 0, 0};
                 if ((FMT == NVQ_FMT_MXFP4 ? kb : i) < blocks) raw[t][i] = *as_global<uint4v>(x[t] + (size_t)c * 256 + piece_at<FMT>(i, kb));
             }
-        multiply_column<FMT, R, T, 1>(col, 0, raw, sum);
+        multiply_column<FMT, R, T, 1, 1>(col, 0, sc, 0, raw, sum);
+    }
+}
+
+// Columns that count for nothing: codes of zero, or scales of zero.
+template <int FMT, int R, int C, int Q>
+__device__ __forceinline__ void clear_column(Codes<C> (&col)[R], int b, Scales<FMT, Q> (&sc)[R], int qb) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if constexpr (FMT == NVQ_FMT_MXFP4)
+            col[r].w[b] = uint4v{0, 0, 0, 0};
+        else
+            sc[r].s[2 * qb] = sc[r].s[2 * qb + 1] = 0;
     }
 }
 
 // sum[r][t] += R row tiles times T token tiles over K = 32 G inputs, shared out over `step` waves (this one: number `first`)
-// in passes of C columns, all of a pass requested before its first product.  x[t]: the lane's token of tile t (bf16).  Every lane of the wave calls it.
-template <int FMT, int R, int T, int C>
+// in passes of Q columns: their scales at once, their codes and activations C columns at a time, requested while the C before are
+// multiplied.  A last pass of fewer columns takes the last Q, those that it shares with the one before cleared.  x[t]: the
+// lane's token of tile t (bf16); a product keeps tokens apart, so a lane without one may take any.  (Loading nothing in such
+// lanes was no faster.)  Every lane of the wave calls it.
+template <int FMT, int R, int T, int C, int Q>
 __device__ __forceinline__ void rows_times_tokens(const RowAt (&at)[R], const char *const (&x)[T], int G, int first,
                                                   int step, float4v (&sum)[R][T]) {
+    static_assert(Q % C == 0, "");
     const int kb = (threadIdx.x & 63) >> 4;
-    const int passes = G / (4 * C);
-    for (int p = first; p < passes; p += step) {
-        RowColumns<FMT, C> col[R];
-        uint4v raw[C][T][4];
+    const int full = G >> 2, passes = full >= Q ? (full + Q - 1) / Q : 0;
+    auto load = [&](Codes<C> (&col)[R], uint4v (&raw)[C][T][4], int c) {
 #pragma unroll
-        for (int r = 0; r < R; ++r) load_columns<FMT, C>(col[r], at[r], p * C, kb);
+        for (int r = 0; r < R; ++r) load_codes<C>(col[r], at[r], c, kb);
 #pragma unroll
         for (int b = 0; b < C; ++b)
 #pragma unroll
             for (int t = 0; t < T; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    raw[b][t][i] = *as_global<uint4v>(x[t] + (size_t)(p * C + b) * 256 + piece_at<FMT>(i, kb));
-        __builtin_amdgcn_sched_barrier(0);
+                    raw[b][t][i] = *as_global<uint4v>(x[t] + (size_t)(c + b) * 256 + piece_at<FMT>(i, kb));
+    };
+    for (int p = first; p < passes; p += step) {
+        const int c0 = p * Q + Q <= full ? p * Q : full - Q, again = p * Q - c0;  // (uniform)
+        Scales<FMT, Q> sc[R];
+        Codes<C> col[2][R];
+        uint4v raw[2][C][T][4];
 #pragma unroll
-        for (int b = 0; b < C; ++b) multiply_column<FMT, R, T, C>(col, b, raw[b], sum);
+        for (int r = 0; r < R; ++r) load_scales<FMT, Q>(sc[r], at[r], c0);
+        load(col[0], raw[0], c0);
+#pragma unroll
+        for (int q = 0; q < Q / C; ++q) {
+            if (q + 1 < Q / C) load(col[(q + 1) & 1], raw[(q + 1) & 1], c0 + (q + 1) * C);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int b = 0; b < C; ++b) {
+                if (q * C + b < Q - 1 && q * C + b < again) clear_column<FMT, R, C, Q>(col[q & 1], b, sc, q * C + b);
+                multiply_column<FMT, R, T, C, Q>(col[q & 1], b, sc, q * C + b, raw[q & 1][b], sum);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
     }
-    last_columns<FMT, R, T>(at, x, G, passes * C, passes, first, step, sum);
+    last_columns<FMT, R, T>(at, x, G, passes ? full : 0, passes, first, step, sum);
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll

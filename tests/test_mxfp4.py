@@ -193,7 +193,10 @@ def exact_case(M, N, K, seed, both):
 
 
 GEMV = [(1, 1, 32), (1, 16, 64), (2, 17, 96), (1, 33, 128), (3, 70, 160), (16, 31, 224), (17, 15, 416), (32, 48, 2048),
-        (5, 257, 1440), (31, 100, 4096), (8, 40, 14336), (1, 5000, 512), (7, 20, 65536), (32, 2100, 288)]
+        (5, 257, 1440), (31, 100, 4096), (8, 40, 14336), (1, 5000, 512), (7, 20, 65536), (32, 2100, 288),
+        # many rows: activations in registers, in the last wave's place and not at all; K for eight and for four columns
+        (1, 65523, 512), (16, 70001, 544), (17, 65537, 1440), (32, 66000, 2048), (3, 65600, 4096), (20, 65541, 3968), (9, 65539, 4128),
+        (18, 65540, 480), (2, 9001, 1056), (14, 16001, 608), (24, 9001, 992)]
 
 
 @gpu
