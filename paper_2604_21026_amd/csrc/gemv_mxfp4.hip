@@ -151,7 +151,10 @@ __global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const ui
 #pragma unroll
                     for (int r = 0; r < R; ++r) now[r].w[b] = uint4v{0, 0, 0, 0};
                 }
-                multiply_column<NVQ_FMT_MXFP4, R, T, C, C>(now, b, now_sc, b, raw, sum);
+                bf16x8 a[T][4];
+#pragma unroll
+                for (int t = 0; t < T; ++t) to_operands<NVQ_FMT_MXFP4>(raw[t], a[t]);
+                multiply_column<NVQ_FMT_MXFP4, R, T, C, C>(now, b, now_sc, b, a, sum);
             }
         };
         // (two turns: the registers of the weights change roles, they are not copied)
@@ -232,7 +235,7 @@ __global__ __launch_bounds__(64 * W) void gemv_mxfp4_resident_kernel(const uint8
     };
 #pragma unroll
     for (int d = 0; d < D; ++d) load(d, tile_of(d));
-    uint4v xr[C][T][4];
+    bf16x8 xr[C][T][4];
 #pragma unroll
     for (int b = 0; b < C; ++b)
 #pragma unroll
@@ -240,9 +243,10 @@ __global__ __launch_bounds__(64 * W) void gemv_mxfp4_resident_kernel(const uint8
             const int block = b0 + 4 * b + kb, m = 16 * t + n;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                xr[b][t][i] = uint4v{0, 0, 0, 0};
+                uint4v v = {0, 0, 0, 0};
                 if (block >= share && m < M)
-                    xr[b][t][i] = *as_global<uint4v>(reinterpret_cast<const char *>(x) + ((size_t)m * G + block) * 64 + 16 * i);
+                    v = *as_global<uint4v>(reinterpret_cast<const char *>(x) + ((size_t)m * G + block) * 64 + 16 * i);
+                xr[b][t][i] = __builtin_bit_cast(bf16x8, v);
             }
         }
     auto one = [&](int d, int tile, int it) {

@@ -103,11 +103,21 @@ __device__ __forceinline__ bf16x8 mx_values(uint32_t codes, float s) {
     return __builtin_bit_cast(bf16x8, v);
 }
 
-// sum[r][t] += tile r times token tile t over column b of the codes loaded, qb of the scales.  raw: the lane's pieces of its
-// token's 128 inputs.
+// The operands of a column from the lane's pieces of its token's 128 inputs.
+template <int FMT>
+__device__ __forceinline__ void to_operands(const uint4v (&raw)[4], bf16x8 (&a)[4]) {
+    if constexpr (FMT == NVQ_FMT_MXFP4) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = __builtin_bit_cast(bf16x8, raw[i]);
+    } else {
+        Act<NVQ_W4A16>::operands(raw, a);
+    }
+}
+
+// sum[r][t] += tile r times token tile t over column b of the codes loaded, qb of the scales.
 template <int FMT, int R, int T, int C, int Q>
 __device__ __forceinline__ void multiply_column(const Codes<C> (&col)[R], int b, const Scales<FMT, Q> (&sc)[R], int qb,
-                                                const uint4v (&raw)[T][4], float4v (&sum)[R][T]) {
+                                                const bf16x8 (&a)[T][4], float4v (&sum)[R][T]) {
     typedef Act<NVQ_W4A16> A;
     if constexpr (FMT == NVQ_FMT_MXFP4) {
 #pragma unroll
@@ -119,13 +129,10 @@ __device__ __forceinline__ void multiply_column(const Codes<C> (&col)[R], int b,
                 const bf16x8 w = mx_values(q[i], s);
 #pragma unroll
                 for (int t = 0; t < T; ++t)
-                    sum[r][t] = A::multiply(__builtin_bit_cast(bf16x8, raw[t][i]), w, sum[r][t]);
+                    sum[r][t] = A::multiply(a[t][i], w, sum[r][t]);
             }
         }
     } else {
-        bf16x8 a[T][4];
-#pragma unroll
-        for (int t = 0; t < T; ++t) A::operands(raw[t], a[t]);
         uint32_t q[R][4];
         float s[R][4];
 #pragma unroll
@@ -186,7 +193,10 @@ __device__ __forceinline__ void last_columns(const RowAt (&at)[R], const char *c
                 raw[t][i] = uint4v{0, 0, 0, 0};
                 if ((FMT == NVQ_FMT_MXFP4 ? kb : i) < blocks) raw[t][i] = *as_global<uint4v>(x[t] + (size_t)c * 256 + piece_at<FMT>(i, kb));
             }
-        multiply_column<FMT, R, T, 1, 1>(col, 0, sc, 0, raw, sum);
+        bf16x8 a[T][4];
+#pragma unroll
+        for (int t = 0; t < T; ++t) to_operands<FMT>(raw[t], a[t]);
+        multiply_column<FMT, R, T, 1, 1>(col, 0, sc, 0, a, sum);
     }
 }
 
@@ -239,7 +249,10 @@ __device__ __forceinline__ void rows_times_tokens(const RowAt (&at)[R], const ch
 #pragma unroll
             for (int b = 0; b < C; ++b) {
                 if (q * C + b < Q - 1 && q * C + b < again) clear_column<FMT, R, C, Q>(col[q & 1], b, sc, q * C + b);
-                multiply_column<FMT, R, T, C, Q>(col[q & 1], b, sc, q * C + b, raw[q & 1][b], sum);
+                bf16x8 a[T][4];
+#pragma unroll
+                for (int t = 0; t < T; ++t) to_operands<FMT>(raw[q & 1][b][t], a[t]);
+                multiply_column<FMT, R, T, C, Q>(col[q & 1], b, sc, q * C + b, a, sum);
             }
             __builtin_amdgcn_sched_barrier(0);
         }

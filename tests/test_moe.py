@@ -168,7 +168,11 @@ def check(y, x, values, ids, w):
 
 EXPERTS = [(1, 1, 1, 32, 32), (1, 2, 2, 64, 96), (1, 64, 8, 512, 256), (2, 4, 3, 160, 64), (5, 40, 3, 1440, 224),
            (16, 8, 2, 256, 128), (17, 3, 2, 128, 416), (32, 2, 1, 96, 32), (32, 16, 4, 512, 512), (32, 1, 1, 288, 64),
-           (7, 300, 4, 64, 32), (32, 20, 16, 128, 160), (3, 2, 5, 64, 64)]
+           (7, 300, 4, 64, 32), (32, 20, 16, 128, 160), (3, 2, 5, 64, 64),
+           # the second launch: tiles of 64 outputs, several workgroups to a tile, experts in slices
+           (16, 64, 4, 4096, 32), (32, 64, 2, 4096, 96), (9, 6, 6, 4160, 1056), (4, 70, 16, 2048, 160),
+           # the first one with the activations in registers: a short last wave, 128 inputs to a lane-row in all
+           (7, 8, 4, 2080, 4096), (3, 3, 3, 4096, 11008)]
 
 
 @gpu
@@ -186,6 +190,21 @@ def test_experts_match_the_plain_form(M, E, k, K, F, fmt):
         first = y if first is None else first
     assert torch.equal(first.bfloat16(), y)
     assert torch.equal(first, nvq.moe_experts(ex, x, dev(ids), dev(w), out_dtype=torch.float32))
+
+
+@gpu
+@pytest.mark.parametrize("fmt", ["int4", "mxfp4"])
+def test_many_tokens_of_one_expert_of_many_rows(fmt):
+    """Two tiles of tokens past the same weights, the second one of two tokens; an expert without any."""
+    rng = np.random.default_rng(2)
+    ex, values = make(fmt, 4, 2144, 8192, 5)
+    ids = np.array([[0]] * 18 + [[3], [2], [-1], [3]], np.int32)[rng.permutation(22)]
+    w = rng.random(ids.shape).astype(np.float32)
+    x = torch.randn((22, 2144), generator=torch.Generator().manual_seed(2)).bfloat16().to(DEV)
+    y = nvq.moe_experts(ex, x, dev(ids), dev(w), out_dtype=torch.float32)
+    check(y, x, values, ids, w)
+    for _ in range(3):
+        assert torch.equal(y, nvq.moe_experts(ex, x, dev(ids), dev(w), out_dtype=torch.float32))
 
 
 @gpu
