@@ -122,46 +122,43 @@ __global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const ui
 
     if (turns > 0) {
         uint4v xr[kMine];
-        Codes<C> w[R], next[R];
-        Scales<NVQ_FMT_MXFP4, C> sc[R], next_sc[R];
+        Codes<C> w[2][R];
+        Scales<NVQ_FMT_MXFP4, C> sc[2][R];
         ask(xr, 0);
-        weights(w, sc, 0);
+        weights(w[0], sc[0], 0);
         keep(xr, 0);
-        ask(xr, 1 < turns ? 1 : 0);
-        auto one = [&](Codes<C> (&now)[R], Scales<NVQ_FMT_MXFP4, C> (&now_sc)[R], Codes<C> (&then)[R],
-                       Scales<NVQ_FMT_MXFP4, C> (&then_sc)[R], int turn) {
+        ask(xr, 1);
+        auto one = [&](int d, int turn) {
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's pieces are in LDS
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             keep(xr, (turn + 1) & 1);
-            ask(xr, turn + 2 < turns ? turn + 2 : turns - 1);
-            weights(then, then_sc, turn + 1 < turns ? turn + 1 : turn);
+            ask(xr, turn + 2);
+            weights(w[d ^ 1], sc[d ^ 1], turn + 1);
             __builtin_amdgcn_sched_barrier(0);
             const bool mine = turn * S + s < passes;  // (uniform)
             const uint4v *const xb = &xs[turn & 1][s * (16 * T * kPieces)];
 #pragma unroll
             for (int b = 0; b < C; ++b) {
-                uint4v raw[T][4];
+                bf16x8 a[T][4];
 #pragma unroll
                 for (int t = 0; t < T; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) raw[t][i] = xb[(16 * t + n) * kPieces + ((16 * b + 4 * kb + i) ^ swapped(n))];
+                    for (int i = 0; i < 4; ++i)
+                        a[t][i] = __builtin_bit_cast(bf16x8, xb[(16 * t + n) * kPieces + ((16 * b + 4 * kb + i) ^ swapped(n))]);
                 if (S > 1 && !mine) {
 #pragma unroll
-                    for (int r = 0; r < R; ++r) now[r].w[b] = uint4v{0, 0, 0, 0};
+                    for (int r = 0; r < R; ++r) w[d][r].w[b] = uint4v{0, 0, 0, 0};
                 }
-                bf16x8 a[T][4];
-#pragma unroll
-                for (int t = 0; t < T; ++t) to_operands<NVQ_FMT_MXFP4>(raw[t], a[t]);
-                multiply_column<NVQ_FMT_MXFP4, R, T, C, C>(now, b, now_sc, b, a, sum);
+                multiply_column<NVQ_FMT_MXFP4, R, T, C, C>(w[d], b, sc[d], b, a, sum);
             }
         };
-        // (two turns: the registers of the weights change roles, they are not copied)
+        // (the registers of the weights change roles from turn to turn, they are not copied)
         for (int turn = 0; turn < turns; turn += 2) {
-            one(w, sc, next, next_sc, turn);
+            one(0, turn);
             if (turn + 1 >= turns) break;
-            one(next, next_sc, w, sc, turn + 1);
+            one(1, turn + 1);
         }
     }
     const char *xt[T];
@@ -295,7 +292,8 @@ struct GemvArgs {
 template <int R>
 int gemv_rows(const GemvArgs &a, hipStream_t st) {
     const dim3 grid((unsigned)(((int64_t)a.N + 16 * R - 1) / (16 * R)));
-    hipLaunchKernelGGL((gemv_mxfp4_kernel<R, 1, 4, R == 1 ? 4 : 2, R == 1 ? 4 : 8>), grid, dim3(256), 0, st, a.q, a.s, a.N, a.G, a.x, a.M, a.y, a.y_dtype);
+    hipLaunchKernelGGL((gemv_mxfp4_kernel<R, 1, 4, R == 1 ? 4 : 2, R == 1 ? 4 : 8>), grid, dim3(256), 0, st, a.q, a.s, a.N, a.G,
+                       a.x, a.M, a.y, a.y_dtype);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
 }
@@ -338,22 +336,33 @@ extern "C" int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
         if (a.G <= 64) return M <= 16 ? gemv_resident<1, 2>(a, cus, st) : gemv_resident<2, 2>(a, cus, st);
         return M <= 16 ? gemv_resident<1, 4>(a, cus, st) : gemv_resident<2, 4>(a, cus, st);
     }
-    // us at (tokens, rows, inputs)   (1, 4096, 4096) (1, 14336, 4096) (8, 14336, 4096) (1, 128256, 4096) (16, 128256, 4096)
-    //   1 row tile per workgroup          3.9              10.0             15.1              68               148
-    //   2                                 5.2               8.6             11.1              54                94
-    //   4                                 7.9               8.3              9.5              48                68
-    //   16, activations shared           22.4              22.6             23.3              51                54
-    if (M <= 8 || (M <= 16 && tiles < 16 * cus)) {
-        if (tiles < 3 * cus) return gemv_rows<1>(a, st);
-        return gemv_rows<4>(a, st);
+    // Up to 16 tokens.  us at (tokens, rows, inputs), R row tiles per workgroup with each wave reading its activations, or activations
+    // shared by the RG groups of S waves; a workgroup to each compute unit where row tiles allow:
+    //                       rows 1  rows 4  shared 1, 8  shared 2, 4  shared 4, 2
+    //   (1, 4096, 4096)       4.0     7.9        5.9         6.6         8.8
+    //   (16, 4096, 4096)      6.6    10.4        6.1         6.7         8.8
+    //   (8, 4096, 14336)     13.5    24.4       12.4        16.2        23.5
+    //   (4, 4096, 14336)     11.3    22.6       11.7        15.5        23.4
+    //   (2, 8192, 4096)       6.5     8.4       10.2         7.1         9.3
+    //   (8, 8192, 4096)       8.6     9.3       10.6         7.4         9.5
+    //   (8, 14336, 4096)     15.3     9.5       19.7        11.8        10.0
+    //   (16, 14336, 4096)    20.6    10.7       20.6        12.0         9.9
+    // and at (16, 128256, 14336), too many inputs for registers, 16 row tiles 193 against 242 with 4 row tiles of 4.
+    if (M <= 16) {
+        if (tiles <= cus) return M * a.G >= 2048 ? gemv_shared<1, 1, 1, 8, 2>(a, st) : gemv_rows<1>(a, st);
+        if (tiles <= 2 * cus) return M > 4 ? gemv_shared<1, 1, 2, 4, 2>(a, st) : gemv_rows<1>(a, st);
+        if (M <= 8) return gemv_rows<4>(a, st);
+        return tiles < 16 * cus ? gemv_shared<1, 1, 4, 2, 2>(a, st) : gemv_shared<1, 2, 8, 1, 4>(a, st);
     }
-    if (M <= 16) return gemv_shared<1, 2, 8, 1, 4>(a, st);
-    // us at (32 tokens, rows, inputs)  (4096, 4096) (4096, 14336) (14336, 4096) (128256, 4096)
-    //   1 row tile, nothing shared         10.2          30.2          34.4          261
-    //   2 row tiles, K in four slices       9.1          24.1          19.1          155
-    //   4 row tiles, K in two              10.8          32.1          12.4           93
-    //   16 row tiles                       26.4          82.8          27.2           63
-    if (tiles < 2 * cus) return gemv_shared<2, 1, 2, 4, 2>(a, st);
+    // us at (32 tokens, rows, inputs)    (4096, 4096) (4096, 14336) (8192, 4096) (14336, 4096) (128256, 4096)
+    //   a row tile, K in eight slices         8.6         21.4         15.8         30.3
+    //   2 row tiles, K in four                9.0         23.9         10.5         18.3          155
+    //   4 row tiles, K in two                10.8         32.1         12.0         12.3           93
+    //   16 row tiles                         26.4         82.8                      27.2           63
+    // (Up to 2 row tiles the activations bound it: every compute unit reads all of them, 0.9 MB at 14336 inputs.  Asked for two turns
+    // ahead, each workgroup beginning at another place of K, or with more weights in flight it took as long.)
+    if (tiles <= cus && a.G >= 128) return gemv_shared<2, 1, 1, 8, 1>(a, st);
+    if (tiles <= 2 * cus) return gemv_shared<2, 1, 2, 4, 2>(a, st);
     if (tiles < 16 * cus) return gemv_shared<2, 1, 4, 2, 2>(a, st);
     return gemv_shared<2, 2, 8, 1, 4>(a, st);
 }
