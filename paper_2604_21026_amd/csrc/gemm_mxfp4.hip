@@ -368,29 +368,27 @@ __global__ __launch_bounds__(256 * S) __attribute__((amdgpu_waves_per_eu(W, W)))
 #pragma unroll
         for (int t = 0; t < T; ++t) asm volatile("s_nop 0" : "+a"(sum[p][t]));  // (the last product was written long ago)
     if constexpr (S > 1) {
-        // slices 1 .. of S hand over their results, a tile of 64 lanes after the other
-        constexpr int kTiles = P * T;
-        static_assert(4 * kTiles * 1024 <= kBoth * 128, "a slice's results in its part of a stage");
+        // slices 1 .. of S hand over their results, a tile of 64 lanes after the other, half of them in either stage's place
+        constexpr int kTiles = P / 2 * T;
+        static_assert(4 * kTiles * 1024 <= kBoth * 128, "a slice's results in its part of the stages");
+        auto place = [&](int from, int p, int t) -> float4v & {
+            unsigned char *const half = p < P / 2 ? stage0 : stage1;
+            return reinterpret_cast<float4v *>(half + from * kBoth * 128)[(wave * kTiles + p % (P / 2) * T + t) * 64 + lane];
+        };
+        if (group) {
 #pragma unroll
-        for (int from = 1; from < S; ++from) {
-            float4v *const at = reinterpret_cast<float4v *>(stage0 + from * kBoth * 128) + wave * (kTiles * 64) + lane;
-            if (group == from) {
+            for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int p = 0; p < P; ++p)
-#pragma unroll
-                    for (int t = 0; t < T; ++t) at[(p * T + t) * 64] = sum[p][t];
-            }
+                for (int t = 0; t < T; ++t) place(group, p, t) = sum[p][t];
         }
         __syncthreads();
         if (group) return;
 #pragma unroll
-        for (int from = 1; from < S; ++from) {
-            const float4v *const at = reinterpret_cast<const float4v *>(stage0 + from * kBoth * 128) + wave * (kTiles * 64) + lane;
+        for (int from = 1; from < S; ++from)
 #pragma unroll
             for (int p = 0; p < P; ++p)
 #pragma unroll
-                for (int t = 0; t < T; ++t) sum[p][t] += at[(p * T + t) * 64];
-        }
+                for (int t = 0; t < T; ++t) sum[p][t] += place(from, p, t);
     }
     static_assert(2 * 16 * (16 * P * 4 + 16) <= kBoth * 128, "two waves' rows of results per stage");
     unsigned char *const out = (wave >> 1 ? stage1 : stage0) + (wave & 1) * (16 * (16 * P * 4 + 16));
@@ -441,22 +439,25 @@ extern "C" int nvq_gemm_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
     const GemmArgs a = {qweight, scales, xq, xscale, y, (int)N, (int)M, (int)(K / 32), y_dtype};
     const hipStream_t st = (hipStream_t)stream;
     if (K < 512) return gemm_small_k(a, st);
-    // The largest tile of which there are enough for the compute units (measured in us, tile rows x tokens):
-    //   M x N x K            256x256  128x128  128x64  64x64 in two slices of K  64x32 in two
-    //   4096 x 4096 x 4096        42       49      70            -                  -
-    //   2048 x 4096 x 4096        35       26      36            -                  -
-    //   1024 x 6144 x 4096        34       24      30           50                 63
-    //   512 x 4096 x 14336        80       40      35           50                 67
-    //   128 x 14336 x 4096        31       15      12           16                 19
-    //   256 x 4096 x 4096         29       13      10.4        9.2                 12
-    //   300 x 2048 x 8192         49       22      19           14                 18
-    //   64 x 4096 x 14336         76       37      27           20                 16
-    //   77 x 1003 x 2080          32       13     9.7          7.6                6.2
+    // The largest tile of which there are enough for the compute units (us; tile rows x tokens, in slices of K):
+    //   M x N x K            256x256  128x128  128x64 in 2  64x64 in 2  64x32 in 2  in 4
+    //   4096 x 4096 x 4096      42       49         70
+    //   2048 x 4096 x 4096      35       26         45          63
+    //   1024 x 6144 x 4096      34       23         34          49                   78
+    //   512 x 4096 x 14336      80       40         32          49                   66
+    //   128 x 14336 x 4096      31       15         12          17                   27
+    //   256 x 4096 x 4096       29       13        10.3         8.6                  13.5
+    //   96 x 6144 x 4096                            9.9         8.0         9.4      12.8
+    //   128 x 4096 x 4096                           9.7         7.8         7.2       7.3
+    //   128 x 2048 x 14336                         21.7        17.0        15.3      13.6
+    //   16 x 4096 x 14336                          24.5        19.7        17.7      14.8
+    //   48 x 4096 x 4096                            9.4         7.5         6.7       6.9
+    //   77 x 1003 x 2080                           10.5         7.7         6.4       7.3
     const int64_t cus = device_cu_count();
     const auto tiles = [&](int rows, int tokens) { return ((N + rows - 1) / rows) * ((M + tokens - 1) / tokens); };
     if (tiles(256, 256) >= cus * 7 / 8) return gemm_tiles<8, 8, 1, 1>(a, st);
     if (tiles(128, 128) >= cus * 5 / 4) return gemm_tiles<4, 4, 1, 2>(a, st);
-    if (tiles(128, 64) >= cus * 3 / 4) return gemm_tiles<4, 2, 1, 2>(a, st);
-    if (M > 64 && tiles(64, 64) >= cus * 3 / 8) return gemm_tiles<2, 2, 2, 2>(a, st);
-    return gemm_tiles<2, 1, 2, 4>(a, st);
+    if (tiles(128, 64) >= cus * 3 / 4) return gemm_tiles<4, 2, 2, 2>(a, st);
+    if (tiles(64, 32) > cus) return gemm_tiles<2, 2, 2, 2>(a, st);
+    return K >= 8192 ? gemm_tiles<2, 1, 4, 4>(a, st) : gemm_tiles<2, 1, 2, 4>(a, st);
 }

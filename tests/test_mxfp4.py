@@ -213,7 +213,10 @@ def test_gemv_exact_sums(M, N, K, dtype):
 
 
 GEMM = [(1, 1, 32), (1, 64, 128), (2, 17, 96), (64, 64, 256), (65, 63, 160), (77, 130, 416), (300, 257, 2080),
-        (128, 513, 4096), (256, 256, 1024), (257, 1, 65536), (3, 1000, 14336), (33, 4100, 224), (1030, 70, 512), (512, 768, 1536)]
+        (128, 513, 4096), (256, 256, 1024), (257, 1, 65536), (3, 1000, 14336), (33, 4100, 224), (1030, 70, 512), (512, 768, 1536),
+        # every tile, with ragged edges and stages, some of its slices of K past the end
+        (3585, 4001, 544), (4097, 3590, 1824), (2001, 2500, 800), (2304, 2305, 1312), (1000, 3001, 608), (129, 14001, 1056),
+        (200, 2700, 992), (65, 8209, 544), (50, 700, 8224), (31, 2050, 8704), (10, 300, 12320)]
 
 
 @gpu
