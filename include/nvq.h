@@ -529,7 +529,7 @@ int nvq_precision_from_scores(const double *scores, int L, double tau, double ep
  * (x_dtype, the y_dtype constants); scales 4-byte aligned.
  * nvq_dequant_mxfp4 -- out[m][k] = code * scale as bf16, exact (blocks of byte 255:
  * NaN; values of byte 253 and 254 beyond the type's range: infinite).
- * K % 32 == 0, any M.  Errors as for the other entry points.
+ * K % 32 == 0, K <= NVQ_MAX_K, any M with M * K <= 2^34.  Errors as for the other entry points.
  */
 int nvq_quant_mxfp4(const void *x, int x_dtype, int64_t M, int64_t K, uint8_t *q, uint8_t *scales,
                     void *stream);
@@ -547,9 +547,11 @@ int nvq_dequant_mxfp4(const uint8_t *q, const uint8_t *scales, int64_t M, int64_
  * xv[m][k], xv the values that xq and xscale stand for, on the scaled matrix
  * instructions, sums in fp32.
  *   xq [M][K/2], xscale [M][K/32]
- * A result depends neither on the other tokens of the call nor on their number in
- * the first one's two kernels (up to 16 tokens and beyond) taken each by itself; both
- * may add in another order at other sizes.
+ * K % 32 == 0, K <= NVQ_MAX_K; N <= 2^29 for the first, N, M <= 2^30 for the second.  A
+ * weight or activation block of byte 255 makes every result that it enters NaN.  A
+ * result does not depend on the values of other rows and tokens; the order in which its
+ * products are added does depend on M, N and K (and not on timing: the same call gives the
+ * same bits).  y may not overlap an input.
  */
 int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int N, int K,
                    const uint16_t *x_bf16, int M, void *y, int y_dtype, void *stream);
@@ -568,6 +570,8 @@ int nvq_gemm_mxfp4(const uint8_t *qweight, const uint8_t *scales, int64_t N, int
  * 1) or over all E (renormalise = 0).  A NaN logit counts as the smallest; the ids of
  * a token are distinct and in [0, E) whatever the inputs.
  *   x_bf16 [M][K], router_bf16 [E][K], 16-byte aligned; ids, weights [M][top_k]
+ * K % 32 == 0, K <= NVQ_MAX_K, 1 <= E <= NVQ_MOE_MAX_EXPERTS, 1 <= top_k <= E and
+ * NVQ_MOE_MAX_TOP_K.  Where a chosen logit is infinite or NaN so may the token's weights be NaN.
  *   workspace  nvq_moe_route_workspace_bytes(M, E) bytes, 256-byte aligned.  Its
  *              first 256 bytes must be zero before the first call and are zero
  *              again after every call: clear it once, then use it for any number of
@@ -596,9 +600,10 @@ int nvq_moe_route(const uint16_t *x_bf16, const uint16_t *router_bf16, int M, in
  *   down     [E][K][F/2] codes, down_scales [E][K][F/32]
  *   format   NVQ_FMT_INT4: as nvq_pack_int4 writes them, scales fp16 bits;
  *            NVQ_FMT_MXFP4: as nvq_quant_mxfp4 writes them
- *   x_bf16 [M][K], ids, weights [M][top_k], y [M][K] (y_dtype); K % 32 == 0, F % 32 == 0
+ *   x_bf16 [M][K], ids, weights [M][top_k], y [M][K] (y_dtype); K % 32 == 0, F % 32 == 0,
+ *   both <= NVQ_MAX_K, 1 <= E <= NVQ_MOE_MAX_EXPERTS, 1 <= top_k <= NVQ_MOE_MAX_TOP_K
  *   workspace  nvq_moe_workspace_bytes(...) bytes, 256-byte aligned, scratch (whatever it
- *              holds); y may overlap neither it nor any input.
+ *              holds), for one call at a time; y may overlap neither it nor any input.
  * nvq_moe_workspace_bytes looks at the sizes alone and returns 0 where they are invalid.
  */
 enum { NVQ_FMT_INT4 = 0, NVQ_FMT_MXFP4 = 1 };

@@ -3,12 +3,13 @@
 // token: 6.4 us a call, of which the launch takes 3.6 and the kernel 2.7).
 //
 // Only the ordinary case is served here: tensors (no subclasses, which may say themselves where their
-// data is) of the expected types on a device, contiguous, with fitting shapes and room for what is
+// data is) of the expected types on the current device, contiguous, with fitting shapes and room for what is
 // written and read.  For everything else a function returns None and the caller takes its own way, which
 // names what is wrong.  The library's entry points are handed over by address (bind); a call returns their
 // status.
 #include <Python.h>
 
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -28,12 +29,13 @@ decltype(&nvq_gemm_mxfp4) g_gemm_mxfp4;
 decltype(&nvq_moe_route) g_moe_route;
 decltype(&nvq_moe_experts) g_moe_experts;
 
-// A contiguous device tensor of that type; dims < 0: any shape.
+// A contiguous tensor of that type on the current device; dims < 0: any shape.
 const at::Tensor *device_tensor(PyObject *o, at::ScalarType type, int64_t dims) {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
     if (!t.defined() || !t.is_cuda() || t.scalar_type() != type || !t.is_contiguous()) return nullptr;
     if (dims >= 0 && t.dim() != dims) return nullptr;
+    if (t.get_device() != c10::hip::current_device()) return nullptr;
     return &t;
 }
 
@@ -268,22 +270,22 @@ PyObject *moe_route(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// (address of an nvq_experts, its K, x, ids, weights, y, workspace)
+// (address of an nvq_experts, its K, its device, x, ids, weights, y, workspace)
 PyObject *moe_experts(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    int K, y_dtype;
-    if (n != 7 || !PyLong_CheckExact(a[0]) || !small_int(a[1], &K)) return none();
+    int K, device, y_dtype;
+    if (n != 8 || !PyLong_CheckExact(a[0]) || !small_int(a[1], &K) || !small_int(a[2], &device)) return none();
     const nvq_experts *const e = static_cast<const nvq_experts *>(PyLong_AsVoidPtr(a[0]));
     if (!e) {
         PyErr_Clear();
         return none();
     }
-    const at::Tensor *const x = device_tensor(a[2], at::kBFloat16, 2), *const ids = device_tensor(a[3], at::kInt, 2),
-                     *const wt = device_tensor(a[4], at::kFloat, 2), *const ws = device_tensor(a[6], at::kByte, -1);
-    if (!x || !ids || !wt || !ws || x->size(1) != K || x->size(0) != ids->size(0) || wt->size(0) != ids->size(0) ||
+    const at::Tensor *const x = device_tensor(a[3], at::kBFloat16, 2), *const ids = device_tensor(a[4], at::kInt, 2),
+                     *const wt = device_tensor(a[5], at::kFloat, 2), *const ws = device_tensor(a[7], at::kByte, -1);
+    if (!x || !ids || !wt || !ws || x->get_device() != device || x->size(1) != K || x->size(0) != ids->size(0) || wt->size(0) != ids->size(0) ||
         wt->size(1) != ids->size(1) || ids->size(0) > INT32_MAX || ids->size(1) > INT32_MAX)
         return none();
-    const at::Tensor *const y = output_tensor(a[5], x->size(0) * K, &y_dtype);
+    const at::Tensor *const y = output_tensor(a[6], x->size(0) * K, &y_dtype);
     if (!y) return none();
     const uint16_t *const xp = static_cast<const uint16_t *>(x->data_ptr());
     const int32_t *const ip = static_cast<const int32_t *>(ids->data_ptr());

@@ -408,7 +408,7 @@ struct GemmArgs {
 template <int P, int T, int S, int W>
 int gemm_tiles(const GemmArgs &a, hipStream_t st) {
     const int64_t tn = ((int64_t)a.N + 32 * P - 1) / (32 * P), tm = ((int64_t)a.M + 32 * T - 1) / (32 * T);
-    if (tn * tm > 0x7fffffffLL) return NVQ_ERR_SHAPE;
+    if (tn * tm * (256 * S) > 0xffffffffLL) return NVQ_ERR_SHAPE;  // (a launch's work items)
     hipLaunchKernelGGL((gemm_mxfp4_kernel<P, T, S, W>), dim3((unsigned)(tn * tm)), dim3(256 * S), 0, st, a.wq, a.ws, a.N,
                        a.G, a.xq, a.xs, a.M, a.y, a.y_dtype, (int)tn);
     NVQ_HIP_TRY(hipGetLastError());
@@ -417,7 +417,7 @@ int gemm_tiles(const GemmArgs &a, hipStream_t st) {
 
 int gemm_small_k(const GemmArgs &a, hipStream_t st) {
     const int64_t tn = ((int64_t)a.N + 63) / 64, tm = ((int64_t)a.M + 63) / 64;
-    if (tn * tm > 0x7fffffffLL) return NVQ_ERR_SHAPE;
+    if (tn * tm * 64 > 0xffffffffLL) return NVQ_ERR_SHAPE;  // (a launch's work items)
     hipLaunchKernelGGL(gemm_mxfp4_small_k_kernel, dim3((unsigned)(tn * tm)), dim3(64), 0, st,
                        reinterpret_cast<const uint4 *>(a.wq), a.ws, (int64_t)a.N, a.G, reinterpret_cast<const uint4 *>(a.xq),
                        a.xs, (int64_t)a.M, a.y, a.y_dtype, (int)tn);

@@ -324,7 +324,7 @@ extern "C" int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
     using namespace nvq;
     if (!qweight || !scales || !x_bf16 || !y || (y_dtype != NVQ_F32 && y_dtype != NVQ_BF16))
         return NVQ_ERR_INVALID_ARG;
-    if (N <= 0 || N > (1 << 30) || M < 1 || M > NVQ_MAX_M || K <= 0 || K % 32 || K > NVQ_MAX_K) return NVQ_ERR_SHAPE;
+    if (N <= 0 || N > (1 << 29) || M < 1 || M > NVQ_MAX_M || K <= 0 || K % 32 || K > NVQ_MAX_K) return NVQ_ERR_SHAPE;
     if (!aligned(qweight, 16) || !aligned(x_bf16, 16) || !aligned(y, y_dtype == NVQ_F32 ? 4 : 2)) return NVQ_ERR_ALIGN;
     const hipStream_t st = (hipStream_t)stream;
     const GemvArgs a = {qweight, scales, x_bf16, y, N, K / 32, M, y_dtype};

@@ -150,12 +150,11 @@ __global__ __launch_bounds__(256) void dequant_mxfp4_kernel(const uint32_t *__re
 extern "C" int nvq_quant_mxfp4(const void *x, int x_dtype, int64_t M, int64_t K, uint8_t *q, uint8_t *scales,
                                void *stream) {
     if (!x || !q || !scales || (x_dtype != NVQ_F32 && x_dtype != NVQ_BF16)) return NVQ_ERR_INVALID_ARG;
-    if (M <= 0 || K <= 0 || K % 32 || K > NVQ_MAX_K || M > (INT64_C(1) << 40) / K) return NVQ_ERR_SHAPE;
+    if (M <= 0 || K <= 0 || K % 32 || K > NVQ_MAX_K || M > (INT64_C(1) << 34) / K) return NVQ_ERR_SHAPE;
     if (!nvq::aligned(x, 16) || !nvq::aligned(q, 16) || !nvq::aligned(scales, 4)) return NVQ_ERR_ALIGN;
     const int64_t blocks = M * (K / 32);
     constexpr int U = 2;
     const int64_t per = x_dtype == NVQ_BF16 ? U * 64 : U * 32, grid = (blocks + per - 1) / per;
-    if (grid > 0x7fffffffLL) return NVQ_ERR_SHAPE;
     if (x_dtype == NVQ_BF16)
         hipLaunchKernelGGL((nvq::quant_mxfp4_kernel<true, U>), dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream,
                            reinterpret_cast<const uint4 *>(x), blocks, reinterpret_cast<uint32_t *>(q), scales);
@@ -169,11 +168,10 @@ extern "C" int nvq_quant_mxfp4(const void *x, int x_dtype, int64_t M, int64_t K,
 extern "C" int nvq_dequant_mxfp4(const uint8_t *q, const uint8_t *scales, int64_t M, int64_t K, uint16_t *out_bf16,
                                  void *stream) {
     if (!q || !scales || !out_bf16) return NVQ_ERR_INVALID_ARG;
-    if (M <= 0 || K <= 0 || K % 32 || K > NVQ_MAX_K || M > (INT64_C(1) << 40) / K) return NVQ_ERR_SHAPE;
+    if (M <= 0 || K <= 0 || K % 32 || K > NVQ_MAX_K || M > (INT64_C(1) << 34) / K) return NVQ_ERR_SHAPE;
     if (!nvq::aligned(q, 16) || !nvq::aligned(out_bf16, 16)) return NVQ_ERR_ALIGN;
     constexpr int U = 4;
     const int64_t words = M * (K / 8), grid = (words + 256 * U - 1) / (256 * U);
-    if (grid > 0x7fffffffLL) return NVQ_ERR_SHAPE;
     hipLaunchKernelGGL((nvq::dequant_mxfp4_kernel<U>), dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream,
                        reinterpret_cast<const uint32_t *>(q), scales, words, reinterpret_cast<uint4 *>(out_bf16));
     NVQ_HIP_TRY(hipGetLastError());

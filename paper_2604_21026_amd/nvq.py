@@ -183,6 +183,14 @@ def _dev(t: torch.Tensor, dtype, name: str, n: int = 0) -> int:
     return t.data_ptr()
 
 
+def _here(t: torch.Tensor, dtype, name: str, n: int = 0) -> int:
+    """The same on the current device, on whose stream the call runs."""
+    at = _dev(t, dtype, name, n)
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError("%s is on device %d, the current device is %d" % (name, t.get_device(), torch.cuda.current_device()))
+    return at
+
+
 def _space(t: torch.Tensor, nbytes: int, name: str) -> int:
     """The address of a contiguous device tensor of any type with room for that many bytes."""
     return _dev(t, t.dtype, name, -(-nbytes // t.element_size()))
@@ -555,8 +563,8 @@ def quant_mxfp4(x: torch.Tensor, out=None):
     if out is None:
         q = torch.empty((M, K // 2), dtype=torch.uint8, device=x.device)
         s = torch.empty((M, K // 32), dtype=torch.uint8, device=x.device)
-    _check(lib().nvq_quant_mxfp4(_dev(x, x.dtype, "x"), _y_dtype(x.dtype), M, K,
-                                 _dev(q, torch.uint8, "q", M * (K // 2)), _dev(s, torch.uint8, "scales", M * (K // 32)),
+    _check(lib().nvq_quant_mxfp4(_here(x, x.dtype, "x"), _y_dtype(x.dtype), M, K,
+                                 _here(q, torch.uint8, "q", M * (K // 2)), _here(s, torch.uint8, "scales", M * (K // 32)),
                                  _stream()), "nvq_quant_mxfp4")
     return q, s
 
@@ -574,8 +582,8 @@ def dequant_mxfp4(q: torch.Tensor, scales: torch.Tensor, out: Optional[torch.Ten
         out = torch.empty((M, K), dtype=torch.bfloat16, device=q.device)
     if tuple(out.shape) != (M, K) or tuple(scales.shape) != (M, K // 32):
         raise ValueError("shape mismatch")
-    _check(lib().nvq_dequant_mxfp4(_dev(q, torch.uint8, "q"), _dev(scales, torch.uint8, "scales"), M, K,
-                                   _dev(out, torch.bfloat16, "out"), _stream()), "nvq_dequant_mxfp4")
+    _check(lib().nvq_dequant_mxfp4(_here(q, torch.uint8, "q"), _here(scales, torch.uint8, "scales"), M, K,
+                                   _here(out, torch.bfloat16, "out"), _stream()), "nvq_dequant_mxfp4")
     return out
 
 
@@ -592,8 +600,8 @@ def gemv_mxfp4(qweight, scales, x, out_dtype=torch.float32, out: Optional[torch.
     if x.shape[1] != K or tuple(scales.shape) != (N, K // 32):
         raise ValueError("shape mismatch")
     y = out if out is not None else torch.empty((M, N), dtype=out_dtype, device=x.device)
-    _check(lib().nvq_gemv_mxfp4(_dev(qweight, torch.uint8, "qweight"), _dev(scales, torch.uint8, "scales"), N, K,
-                                _dev(x, torch.bfloat16, "x"), M, _dev(y, y.dtype, "y", M * N),
+    _check(lib().nvq_gemv_mxfp4(_here(qweight, torch.uint8, "qweight"), _here(scales, torch.uint8, "scales"), N, K,
+                                _here(x, torch.bfloat16, "x"), M, _here(y, y.dtype, "y", M * N),
                                 _y_dtype(y.dtype), _stream()), "nvq_gemv_mxfp4")
     return y
 
@@ -612,9 +620,9 @@ def gemm_mxfp4(qweight, scales, xq, xscale, out_dtype=torch.float32, out: Option
     if xq.shape[1] * 2 != K or tuple(scales.shape) != (N, K // 32) or tuple(xscale.shape) != (M, K // 32):
         raise ValueError("shape mismatch")
     y = out if out is not None else torch.empty((M, N), dtype=out_dtype, device=xq.device)
-    _check(lib().nvq_gemm_mxfp4(_dev(qweight, torch.uint8, "qweight"), _dev(scales, torch.uint8, "scales"), N, K,
-                                _dev(xq, torch.uint8, "xq"), _dev(xscale, torch.uint8, "xscale"), M,
-                                _dev(y, y.dtype, "y", M * N), _y_dtype(y.dtype), _stream()), "nvq_gemm_mxfp4")
+    _check(lib().nvq_gemm_mxfp4(_here(qweight, torch.uint8, "qweight"), _here(scales, torch.uint8, "scales"), N, K,
+                                _here(xq, torch.uint8, "xq"), _here(xscale, torch.uint8, "xscale"), M,
+                                _here(y, y.dtype, "y", M * N), _y_dtype(y.dtype), _stream()), "nvq_gemm_mxfp4")
     return y
 
 
@@ -645,9 +653,9 @@ def moe_route(x: torch.Tensor, router: torch.Tensor, top_k: int, renormalise: bo
                torch.empty((M, max(top_k, 0)), dtype=torch.float32, device=x.device))
     if workspace is None:
         workspace = moe_route_workspace(M, E, x.device)
-    _check(lib().nvq_moe_route(_dev(x, torch.bfloat16, "x"), _dev(router, torch.bfloat16, "router"), M, E, K, top_k,
-                               int(renormalise), _dev(out[0], torch.int32, "ids", M * top_k),
-                               _dev(out[1], torch.float32, "weights", M * top_k), _dev(workspace, torch.uint8, "workspace"),
+    _check(lib().nvq_moe_route(_here(x, torch.bfloat16, "x"), _here(router, torch.bfloat16, "router"), M, E, K, top_k,
+                               int(renormalise), _here(out[0], torch.int32, "ids", M * top_k),
+                               _here(out[1], torch.float32, "weights", M * top_k), _here(workspace, torch.uint8, "workspace"),
                                workspace.numel(), _stream()), "nvq_moe_route")
     return out[0], out[1]
 
@@ -689,7 +697,7 @@ def moe_experts(experts: Experts, x: torch.Tensor, ids: torch.Tensor, weights: t
     """x bf16 [M,K], ids i32 [M,top_k] (outside [0,E): not used), weights f32 [M,top_k] -> y [M,K], the weighted sum
     of the chosen experts' outputs (`workspace`: from experts.workspace, for calls one after the other)."""
     if out is not None and workspace is not None and _calls is not None:
-        status = _calls.moe_experts(experts.address, experts.K, x, ids, weights, out, workspace)
+        status = _calls.moe_experts(experts.address, experts.K, experts.device.index, x, ids, weights, out, workspace)
         if status is not None:  # (None: not the ordinary case)
             if status:
                 _check(status, "nvq_moe_experts")
@@ -697,12 +705,14 @@ def moe_experts(experts: Experts, x: torch.Tensor, ids: torch.Tensor, weights: t
     M, top_k = ids.shape
     if tuple(x.shape) != (M, experts.K) or tuple(weights.shape) != (M, top_k):
         raise ValueError("shape mismatch")
+    if x.device != experts.device:
+        raise ValueError("x is on %s, the experts on %s" % (x.device, experts.device))
     y = out if out is not None else torch.empty((M, experts.K), dtype=out_dtype, device=x.device)
     if workspace is None:
         workspace = experts.workspace(M, top_k)
-    _check(lib().nvq_moe_experts(experts.address, _dev(x, torch.bfloat16, "x"), _dev(ids, torch.int32, "ids"),
-                                 _dev(weights, torch.float32, "weights"), M, top_k, _dev(y, y.dtype, "y", M * experts.K),
-                                 _y_dtype(y.dtype), _dev(workspace, torch.uint8, "workspace"), workspace.numel(),
+    _check(lib().nvq_moe_experts(experts.address, _here(x, torch.bfloat16, "x"), _here(ids, torch.int32, "ids"),
+                                 _here(weights, torch.float32, "weights"), M, top_k, _here(y, y.dtype, "y", M * experts.K),
+                                 _y_dtype(y.dtype), _here(workspace, torch.uint8, "workspace"), workspace.numel(),
                                  _stream()), "nvq_moe_experts")
     return y
 

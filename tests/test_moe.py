@@ -346,3 +346,21 @@ def test_the_binding_refuses_what_does_not_fit(monkeypatch):
                 call()
         monkeypatch.setattr(nvq, "_calls", None)
     assert not good.any()
+
+
+@gpu
+def test_tensors_of_another_device_than_the_current_one(monkeypatch):
+    ex, _ = make("mxfp4", 4, 64, 32, 1)
+    x, router = torch.zeros((3, 64), dtype=torch.bfloat16, device=DEV), torch.zeros((4, 64), dtype=torch.bfloat16, device=DEV)
+    ids, w = torch.zeros((3, 2), dtype=torch.int32, device=DEV), torch.zeros((3, 2), device=DEV)
+    y, ws, rws = torch.empty_like(x), ex.workspace(3, 2), nvq.moe_route_workspace(3, 4, DEV)
+    monkeypatch.setattr(ex, "device", torch.device("cuda", 1))
+    with pytest.raises(ValueError, match="the experts on"):
+        nvq.moe_experts(ex, x, ids, w, out=y, workspace=ws)
+    monkeypatch.undo()
+    monkeypatch.setattr(nvq, "_calls", None)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in (lambda: nvq.moe_experts(ex, x, ids, w, out=y, workspace=ws),
+                 lambda: nvq.moe_route(x, router, 2, out=(ids, w), workspace=rws)):
+        with pytest.raises(ValueError, match="current device"):
+            call()

@@ -43,6 +43,11 @@ def test_refusals_before_any_launch():
     assert L.nvq_quant_mxfp4(a, 0, 4, 48, a, a, None) == 2
     assert L.nvq_quant_mxfp4(a, 0, 0, 64, a, a, None) == 2
     assert L.nvq_quant_mxfp4(a, 0, 1 << 62, 64, a, a, None) == 2
+    assert L.nvq_quant_mxfp4(a, 1, (1 << 28) + 1, 64, a, a, None) == 2
+    assert L.nvq_dequant_mxfp4(a, a, (1 << 28) + 1, 64, a, None) == 2
+    assert L.nvq_gemv_mxfp4(a, a, (1 << 29) + 1, 32, a, 1, a, 0, None) == 2
+    assert L.nvq_gemm_mxfp4(a, a, 1 << 30, 64, a, a, 1 << 20, a, 0, None) == 2  # (more results than a launch has lanes)
+    assert L.nvq_gemm_mxfp4(a, a, 1 << 30, 512, a, a, 1 << 20, a, 0, None) == 2
     assert L.nvq_quant_mxfp4(a, 0, 4, 65568, a, a, None) == 2
     assert L.nvq_quant_mxfp4(a + 8, 0, 4, 64, a, a, None) == 3
     assert L.nvq_quant_mxfp4(a, 1, 4, 64, a, a + 2, None) == 3
@@ -89,6 +94,19 @@ def test_the_binding_refuses_what_does_not_fit():
             call()
     with pytest.raises(nvq.NvqError):
         nvq.gemv_mxfp4(q, s, torch.zeros((33, 64), dtype=torch.bfloat16, device=DEV))
+
+
+@gpu
+def test_tensors_of_another_device_than_the_current_one(monkeypatch):
+    q, s = torch.zeros((8, 32), dtype=torch.uint8, device=DEV), torch.zeros((8, 2), dtype=torch.uint8, device=DEV)
+    x, y = torch.zeros((3, 64), dtype=torch.bfloat16, device=DEV), torch.zeros((3, 8), device=DEV)
+    nvq.lib()
+    monkeypatch.setattr(nvq, "_calls", None)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for call in (lambda: nvq.quant_mxfp4(x, out=(q, s)), lambda: nvq.dequant_mxfp4(q[:3], s[:3], out=x),
+                 lambda: nvq.gemv_mxfp4(q, s, x, out=y), lambda: nvq.gemm_mxfp4(q, s, q, s, out=y)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
 
 
 # ---- quantisation ----
@@ -282,6 +300,63 @@ def test_a_block_without_a_number_reaches_its_row_and_token_alone():
     x[20, 200] = np.nan
     y = f64(nvq.gemv_mxfp4(dev(q), dev(s), dev(x).bfloat16()))
     assert np.isnan(y[20]).all() and np.isnan(y[:20]).sum() == 40
+
+
+@gpu
+def test_quantised_nan_reaches_the_products():
+    """A block that held an infinity has zero codes: its byte alone makes the results NaN."""
+    g = torch.Generator().manual_seed(12)
+    w, x = torch.randn((40, 288), generator=g), torch.randn((5, 288), generator=g).bfloat16()
+    w[3, 100], w[33, 287] = float("inf"), float("nan")
+    q, s = nvq.quant_mxfp4(w.to(DEV))
+    y = nvq.gemv_mxfp4(q, s, x.to(DEV))
+    z = nvq.gemm_mxfp4(q, s, *nvq.quant_mxfp4(x.to(DEV)))
+    for got in (y, z):
+        nan = torch.isnan(got).cpu()
+        assert nan[:, [3, 33]].all() and int(nan.sum()) == 10
+
+
+@gpu
+def test_beyond_the_32_bit_offsets():
+    """More than 4 GiB of values, codes and results: the last ones are where they belong."""
+    N, K = 2 ** 21 + 5, 4160
+    tail = slice(N - 37, N)
+    x = torch.zeros((N, K), dtype=torch.bfloat16, device=DEV)
+    ends = torch.randn((42, K), generator=torch.Generator().manual_seed(4)).bfloat16()
+    x[tail], x[:5] = ends[5:].to(DEV), ends[:5].to(DEV)
+    q, s = nvq.quant_mxfp4(x)
+    rq, rs = np_mx.quant(f64(ends))
+    assert q.numel() > 2 ** 32
+    assert np.array_equal(q[tail].cpu().numpy(), rq[5:]) and np.array_equal(s[tail].cpu().numpy(), rs[5:])
+    assert np.array_equal(q[:5].cpu().numpy(), rq[:5]) and not bool(q[5:N - 37].any())
+    x.fill_(1)
+    nvq.dequant_mxfp4(q, s, out=x)
+    v = np_mx.dequant(rq, rs)
+    assert bits_equal(f64(x[tail]), v[5:]) and bits_equal(f64(x[:5]), v[:5]) and not bool(x[5:N - 37].any())
+    del x
+    t = torch.randint(-3, 4, (32, K), generator=torch.Generator().manual_seed(5)).to(DEV).bfloat16()
+    tq, ts = nvq.quant_mxfp4(t)
+    tv = np_mx.dequant(*np_mx.quant(f64(t)))
+    for M in (1, 32):  # (2 GiB of codes beyond the first 4)
+        y = nvq.gemv_mxfp4(q, s, t[:M], out_dtype=torch.bfloat16)
+        want, size = f64(t[:M]) @ v.T, np.abs(f64(t[:M])) @ np.abs(v).T
+        err = np.abs(np.concatenate([f64(y[:, :5]), f64(y[:, tail])], 1) - want)
+        assert (err <= (K + 40) * np_mx.EPS32 * size + np_mx.EPS16 * 1.01 * (np.abs(want) + 1e-3 * size)).all()
+        assert not bool(y[:, 5:N - 37].any())
+        z = nvq.gemm_mxfp4(q, s, tq[:M], ts[:M], out_dtype=torch.bfloat16)
+        want, size = tv[:M] @ v.T, np.abs(tv[:M]) @ np.abs(v).T
+        err = np.abs(np.concatenate([f64(z[:, :5]), f64(z[:, tail])], 1) - want)
+        assert (err <= (K + 40) * np_mx.EPS32 * size + np_mx.EPS16 * 1.01 * (np.abs(want) + 1e-3 * size)).all()
+        del y, z
+    # as activations: rows of y beyond 4 GiB of results
+    wq, ws = nvq.quant_mxfp4(torch.randn((1040, K), generator=torch.Generator().manual_seed(6)).to(DEV))
+    wv = np_mx.dequant(wq.cpu().numpy(), ws.cpu().numpy())
+    z = nvq.gemm_mxfp4(wq, ws, q, s, out_dtype=torch.bfloat16)
+    assert z.numel() * 2 > 2 ** 32
+    got = np.concatenate([f64(z[:5]), f64(z[tail])])
+    want, size = v @ wv.T, np.abs(v) @ np.abs(wv).T
+    assert (np.abs(got - want) <= (K + 40) * np_mx.EPS32 * size + np_mx.EPS16 * 1.01 * (np.abs(want) + 1e-3 * size)).all()
+    assert not bool(z[5:N - 37].any())
 
 
 @gpu
