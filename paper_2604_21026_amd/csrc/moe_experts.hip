@@ -19,7 +19,7 @@ namespace nvq {
 
 namespace {
 
-constexpr int kMaxParts = 4, kMaxChunks = NVQ_MAX_M * NVQ_MOE_MAX_TOP_K / 64;
+constexpr int kMaxParts = 4, kMaxPairs = NVQ_MAX_M * NVQ_MOE_MAX_TOP_K, kMaxChunks = kMaxPairs / 64;
 
 struct MoeArgs {
     const uint8_t *gu_q, *dn_q;
@@ -40,20 +40,6 @@ struct MoeArgs {
 
 __device__ __forceinline__ int token_of(const MoeArgs &a, int pair) { return (int)((uint32_t)pair * a.per_token >> 16); }
 
-// The pairs in a wave's registers, pair 64 t + lane.
-template <int CHUNKS>
-struct Pairs {
-    int id[CHUNKS];
-    float weight[CHUNKS];
-};
-
-template <int CHUNKS>
-__device__ __forceinline__ void load_ids(const MoeArgs &a, Pairs<CHUNKS> &p) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int t = 0; t < CHUNKS; ++t) p.id[t] = 64 * t + lane < a.pairs ? a.ids[64 * t + lane] : -1;
-}
-
 // The tokens of one expert in ascending order, spread over a wave: lane n of a lane-row has number 16 t + n of them for t =
 // 0, 1 (past the end: the first one's), the pair of its first slot and the sum of its slots' weights.
 struct ExpertTokens {
@@ -62,39 +48,95 @@ struct ExpertTokens {
     float weight[2];
 };
 
-template <int CHUNKS>
-__device__ __forceinline__ ExpertTokens tokens_of(const MoeArgs &a, const Pairs<CHUNKS> &pairs, int e) {
+// Up to 64 pairs, one in each lane: those of the expert one after the other.
+__device__ __forceinline__ ExpertTokens tokens_of(const MoeArgs &a, int id, float weight, int e) {
     const int n = threadIdx.x & 15;
     ExpertTokens et = {0, -1, {0, 0}, {0, 0}, {0.0f, 0.0f}};
     int previous = -1;
-#pragma unroll
-    for (int t = 0; t < CHUNKS; ++t) {
-        uint64_t here = __ballot(pairs.id[t] == e);
-        while (here) {  // (uniform)
-            const int bit = __builtin_ctzll(here), p = 64 * t + bit;
-            const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(pairs.weight[t]), bit));
-            here &= here - 1;
-            const int m = token_of(a, p);
-            if (m != previous) {
-                previous = m;
-                if (et.count == 0) {
-                    et.first = p;
-                    et.token[0] = et.token[1] = m;
-                    et.pair[0] = et.pair[1] = p;
-                }
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    if (16 * k + n == et.count) {
-                        et.token[k] = m;
-                        et.pair[k] = p;
-                    }
-                ++et.count;
+    for (uint64_t here = __ballot(id == e); here; here &= here - 1) {  // (uniform)
+        const int p = __builtin_ctzll(here), m = token_of(a, p);
+        const float w = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(weight), p));
+        if (m != previous) {
+            previous = m;
+            if (et.count == 0) {
+                et.first = p;
+                et.token[0] = et.token[1] = m;
+                et.pair[0] = et.pair[1] = p;
             }
 #pragma unroll
-            for (int k = 0; k < 2; ++k) et.weight[k] += 16 * k + n == et.count - 1 ? w : 0.0f;
+            for (int k = 0; k < 2; ++k)
+                if (16 * k + n == et.count) {
+                    et.token[k] = m;
+                    et.pair[k] = p;
+                }
+            ++et.count;
         }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) et.weight[k] += 16 * k + n == et.count - 1 ? w : 0.0f;
     }
     return et;
+}
+
+// More pairs, id_of(t) and weight_of(t) giving the lane's of chunk t: each that is its token's first with the expert finds its
+// number by counting those below, and sends itself to the lane of that number.  (One after the other, 25 tokens' 200 pairs of
+// twelve experts took a seventh of 29 us.)
+template <typename IDS, typename WEIGHTS>
+__device__ __forceinline__ ExpertTokens tokens_of(const MoeArgs &a, int e, IDS id_of, WEIGHTS weight_of) {
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));  // (what follows from it is not kept in registers from expert to expert)
+    const int n = lane & 15;
+    const uint64_t lower = ((uint64_t)1 << lane) - 1;
+    int count = 0, listed = 0;  // listed: in lane i the i-th token's pair, plus one
+    float weight = 0.0f;
+    uint64_t previous = 0;
+#pragma unroll
+    for (int t = 0; t < kMaxChunks; ++t) {
+        if (64 * t >= a.pairs) break;  // (uniform)
+        const uint64_t here = __ballot(id_of(t, lane) == e);
+        if (here) {  // (uniform)
+            const int p = 64 * t + lane, start = token_of(a, p) * a.top_k - 64 * t;  // the lane of the token's first slot
+            const bool again = (here & lower & (start > 0 ? ~(uint64_t)0 << start : ~(uint64_t)0)) != 0 ||
+                               (start < 0 && previous >> (64 + start) != 0);
+            const bool first = (here >> lane & 1) && !again;
+            const uint64_t firsts = __ballot(first);
+            const float w = weight_of(t, lane);
+            const int to = first ? count + __builtin_popcountll(firsts & lower) : 63;  // (63: none; there are 32 tokens)
+            listed |= __builtin_amdgcn_ds_permute(4 * to, p + 1);
+            weight = __uint_as_float(__float_as_uint(weight) | (uint32_t)__builtin_amdgcn_ds_permute(4 * to, (int)__float_as_uint(w)));
+            for (uint64_t more = here & ~firsts; more; more &= more - 1) {  // (an expert in several slots of a token)
+                const int bit = __builtin_ctzll(more);
+                const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), bit));
+                if (lane == count + __builtin_popcountll(firsts & (((uint64_t)1 << bit) - 1)) - 1) weight += other;
+            }
+            count += __builtin_popcountll(firsts);
+        }
+        previous = here;
+    }
+    ExpertTokens et;
+    et.count = count;
+    et.first = __builtin_amdgcn_readfirstlane(listed) - 1;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int from = 16 * k + n < count ? 16 * k + n : 0;
+        et.pair[k] = __shfl(listed, from, 64) - 1;
+        et.token[k] = token_of(a, et.pair[k]);
+        et.weight[k] = __shfl(weight, from, 64);
+    }
+    return et;
+}
+
+// The tokens of a first launch's expert.
+template <bool SMALL>
+__device__ __forceinline__ ExpertTokens own_tokens(const MoeArgs &a, int e) {
+    const int lane = threadIdx.x & 63;
+    if constexpr (SMALL) {
+        return tokens_of(a, lane < a.pairs ? a.ids[lane] : -1, 0.0f, e);
+    } else {
+        int id[kMaxChunks];
+#pragma unroll
+        for (int t = 0; t < kMaxChunks; ++t) id[t] = 64 * t + lane < a.pairs ? a.ids[64 * t + lane] : -1;
+        return tokens_of(a, e, [&](int t, int) { return id[t]; }, [](int, int) { return 0.0f; });
+    }
 }
 
 // The second launch's arrival counters, zero before it begins.
@@ -103,49 +145,56 @@ __device__ __forceinline__ void clear_arrivals(const MoeArgs &a) {
         for (int i = threadIdx.x; i < a.K / 16; i += blockDim.x) a.arrived[i] = 0;
 }
 
-// A workgroup takes 16 gate rows and the up rows beside them, its KS waves share out K.
-template <int FMT, int KS, int C, int CHUNKS>
+// A workgroup takes 16 gate rows and the up rows beside them, its KS waves share out K, T token tiles at a time.
+template <int FMT, int T, int KS, int C, bool SMALL>
 __global__ __launch_bounds__(64 * KS) void moe_gate_up_kernel(MoeArgs a) {
     const int lane = threadIdx.x & 63, n = lane & 15, kb = lane >> 4;
     const int s = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     clear_arrivals(a);
-    Pairs<CHUNKS> pairs;
-    load_ids<CHUNKS>(a, pairs);
-#pragma unroll
-    for (int t = 0; t < CHUNKS; ++t) pairs.weight[t] = 0.0f;
     // the second grid axis: experts, or pairs where there are fewer (a pair that is not the first of its expert has
     // nothing to do)
     const bool by_expert = a.E <= a.pairs;
     const int e = by_expert ? (int)blockIdx.y : a.ids[blockIdx.y];
     if ((uint32_t)e >= (uint32_t)a.E) return;
-    const ExpertTokens et = tokens_of<CHUNKS>(a, pairs, e);
+    const ExpertTokens et = own_tokens<SMALL>(a, e);
     if (et.count == 0 || (!by_expert && et.first != (int)blockIdx.y)) return;
     const int row0 = blockIdx.x * 16, G = a.K / 32;
     const int64_t row = (int64_t)e * 2 * a.F + row0 + n;
     const RowAt at[2] = {row_at<FMT>(a.gu_q, a.gu_s, row, G), row_at<FMT>(a.gu_q, a.gu_s, row + a.F, G)};
-    // (an expert of more than 16 tokens reads its weights twice)
-    for (int t = 0; 16 * t < et.count; ++t) {
-        const char *const x[1] = {reinterpret_cast<const char *>(a.x) + (int64_t)(t ? et.token[1] : et.token[0]) * a.K * 2};
-        float4v sum[2][1] = {{float4v{0.0f, 0.0f, 0.0f, 0.0f}}, {float4v{0.0f, 0.0f, 0.0f, 0.0f}}};
-        rows_times_tokens<FMT, 2, 1, C, C>(at, x, G, s, KS, sum);
-        __shared__ float4v red[KS - 1][2][64];
+    // (T == 1: an expert of more than 16 tokens reads its weights twice)
+    for (int t0 = 0; 16 * t0 < et.count; t0 += T) {
+        const char *x[T];
+        float4v sum[2][T];
+#pragma unroll
+        for (int t = 0; t < T; ++t) {
+            x[t] = reinterpret_cast<const char *>(a.x) + (int64_t)(t0 + t ? et.token[1] : et.token[0]) * a.K * 2;
+            sum[0][t] = sum[1][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        rows_times_tokens<FMT, 2, T, C, C>(at, x, G, s, KS, sum);
+        __shared__ float4v red[KS - 1][2][T][64];
         if (s > 0) {
-            red[s - 1][0][lane] = sum[0][0];
-            red[s - 1][1][lane] = sum[1][0];
+#pragma unroll
+            for (int t = 0; t < T; ++t) {
+                red[s - 1][0][t][lane] = sum[0][t];
+                red[s - 1][1][t][lane] = sum[1][t];
+            }
         }
         __syncthreads();
         if (s == 0) {
 #pragma unroll
-            for (int k = 0; k < KS - 1; ++k) {
-                sum[0][0] += red[k][0][lane];
-                sum[1][0] += red[k][1][lane];
-            }
-            const int mine = t ? et.pair[1] : et.pair[0];
+            for (int t = 0; t < T; ++t) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int pair = __shfl(mine, 4 * kb + j, 64);
-                if (16 * t + 4 * kb + j < et.count)
-                    a.h[(int64_t)pair * a.F + row0 + n] = float_to_bf16_bits(silu_mul_one(sum[0][0][j], sum[1][0][j]));
+                for (int k = 0; k < KS - 1; ++k) {
+                    sum[0][t] += red[k][0][t][lane];
+                    sum[1][t] += red[k][1][t][lane];
+                }
+                const int mine = t0 + t ? et.pair[1] : et.pair[0];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int pair = __shfl(mine, 4 * kb + j, 64);
+                    if (16 * (t0 + t) + 4 * kb + j < et.count)
+                        a.h[(int64_t)pair * a.F + row0 + n] = float_to_bf16_bits(silu_mul_one(sum[0][t][j], sum[1][t][j]));
+                }
             }
         }
         __syncthreads();
@@ -155,7 +204,7 @@ __global__ __launch_bounds__(64 * KS) void moe_gate_up_kernel(MoeArgs a) {
 // The same for experts of many rows: wave w of W keeps the activations of C columns of the expert's tokens in registers and
 // the workgroup streams tiles of gate and up rows past them, two turns of both requested ahead; the grid's first axis shares
 // out an expert's tiles.  The waves' sums meet in LDS, one barrier a turn; four waves add them, the other four in the next turn.
-template <int FMT, int W, int C, int CHUNKS>
+template <int FMT, int W, int C, bool SMALL>
 __global__ __launch_bounds__(64 * W) void moe_gate_up_resident_kernel(MoeArgs a) {
     constexpr int D = 2;
     __shared__ float red[2][W][8][64];
@@ -163,14 +212,10 @@ __global__ __launch_bounds__(64 * W) void moe_gate_up_resident_kernel(MoeArgs a)
     const int lane = threadIdx.x & 63, n = lane & 15, kb = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     clear_arrivals(a);
-    Pairs<CHUNKS> pairs;
-    load_ids<CHUNKS>(a, pairs);
-#pragma unroll
-    for (int t = 0; t < CHUNKS; ++t) pairs.weight[t] = 0.0f;
     const bool by_expert = a.E <= a.pairs;
     const int e = by_expert ? (int)blockIdx.y : a.ids[blockIdx.y];
     if ((uint32_t)e >= (uint32_t)a.E) return;
-    const ExpertTokens et = tokens_of<CHUNKS>(a, pairs, e);
+    const ExpertTokens et = own_tokens<SMALL>(a, e);
     if (et.count == 0 || (!by_expert && et.first != (int)blockIdx.y)) return;
     if (threadIdx.x < 16) {
         pair_of[threadIdx.x] = et.pair[0];
@@ -247,28 +292,40 @@ __global__ __launch_bounds__(64 * W) void moe_gate_up_resident_kernel(MoeArgs a)
 }
 
 // A workgroup takes 16 R rows of the outputs; the row tiles' experts, or slices of them, are shared out among the waves of
-// a.parts workgroups.
-template <int FMT, int R, int W, int C, int CHUNKS>
-__global__ __launch_bounds__(64 * W) void moe_down_kernel(MoeArgs a) {
-    constexpr int kTokens = CHUNKS == 1 ? 16 : NVQ_MAX_M;  // (CHUNKS == 1: up to 16 tokens)
-    constexpr int kOut = kTokens * R * 16;                 // a wave's sums
+// a.parts workgroups.  (R = T = 1: within 128 registers, so that two workgroups run on a compute unit; with 129 one token's eight
+// experts took 17.4 us for 14.6.)
+template <int FMT, int R, int T, int W, int C, bool SMALL>
+__global__ __launch_bounds__(64 * W, R * T == 1 ? 4 : 1) void moe_down_kernel(MoeArgs a) {
+    constexpr int kTokens = SMALL ? 16 : NVQ_MAX_M;
+    constexpr int kOut = kTokens * R * 16;  // a wave's sums
     __shared__ float out[W][kOut];
     __shared__ uint32_t chosen[NVQ_MOE_MAX_EXPERTS / 32];
     __shared__ uint32_t last;
+    constexpr int kListed = SMALL ? 1 : kMaxPairs;
+    __shared__ int ids[kListed];
+    __shared__ float weights[kListed];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4;
     const int row0 = blockIdx.x * (16 * R), part = blockIdx.y;
-    Pairs<CHUNKS> pairs;
-    load_ids<CHUNKS>(a, pairs);
-#pragma unroll
-    for (int t = 0; t < CHUNKS; ++t) pairs.weight[t] = 64 * t + lane < a.pairs ? a.weights[64 * t + lane] : 0.0f;
-    // the experts that some token chose, a bit for each
-    if (w == 0) {
-        if (lane < NVQ_MOE_MAX_EXPERTS / 32) chosen[lane] = 0;
-#pragma unroll
-        for (int t = 0; t < CHUNKS; ++t)
-            if ((uint32_t)pairs.id[t] < (uint32_t)a.E) atomicOr(&chosen[pairs.id[t] >> 5], 1u << (pairs.id[t] & 31));
+    int my_id = -1;  // SMALL: the lane's pair
+    float my_weight = 0.0f;
+    if (SMALL && lane < a.pairs) {
+        my_id = a.ids[lane];
+        my_weight = a.weights[lane];
     }
+    // the experts that some token chose, a bit for each
+    if (threadIdx.x < NVQ_MOE_MAX_EXPERTS / 32) chosen[threadIdx.x] = 0;
     for (int i = lane; i < kOut; i += 64) out[w][i] = 0.0f;
+    __syncthreads();
+    if constexpr (SMALL) {
+        if (w == 0 && (uint32_t)my_id < (uint32_t)a.E) atomicOr(&chosen[my_id >> 5], 1u << (my_id & 31));
+    } else {
+        for (int p = threadIdx.x; p < kMaxPairs; p += 64 * W) {
+            const int e = p < a.pairs ? a.ids[p] : -1;
+            ids[p] = e;
+            weights[p] = p < a.pairs ? a.weights[p] : 0.0f;
+            if ((uint32_t)e < (uint32_t)a.E) atomicOr(&chosen[e >> 5], 1u << (e & 31));
+        }
+    }
     __syncthreads();
     const uint32_t word = chosen[lane & (NVQ_MOE_MAX_EXPERTS / 32 - 1)];
     const int words = (a.E + 31) >> 5;
@@ -294,31 +351,39 @@ __global__ __launch_bounds__(64 * W) void moe_down_kernel(MoeArgs a) {
             break;
         }
         e = __builtin_amdgcn_readfirstlane(e);
-        const ExpertTokens et = tokens_of<CHUNKS>(a, pairs, e);
+        ExpertTokens et;
+        if constexpr (SMALL)
+            et = tokens_of(a, my_id, my_weight, e);
+        else
+            et = tokens_of(a, e, [&](int t, int l) { return ids[64 * t + l]; }, [&](int t, int l) { return weights[64 * t + l]; });
         RowAt at[R];
 #pragma unroll
         for (int r = 0; r < R; ++r)
             at[r] = row_at<FMT>(a.dn_q, a.dn_s, (int64_t)e * a.K + row0 + 16 * r + n, G);
-        for (int t = 0; 16 * t < et.count; ++t) {
-            const int token = t ? et.token[1] : et.token[0], pair = t ? et.pair[1] : et.pair[0];
-            const float weight = t ? et.weight[1] : et.weight[0];
-            const char *const h[1] = {reinterpret_cast<const char *>(a.h) + (int64_t)pair * a.F * 2};
-            float4v sum[R][1];
+        for (int t0 = 0; 16 * t0 < et.count; t0 += T) {
+            const char *h[T];
+            float4v sum[R][T];
 #pragma unroll
-            for (int r = 0; r < R; ++r) sum[r][0] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-            rows_times_tokens<FMT, R, 1, C, C>(at, h, G, item % split, split, sum);
+            for (int t = 0; t < T; ++t) {
+                h[t] = reinterpret_cast<const char *>(a.h) + (int64_t)(t0 + t ? et.pair[1] : et.pair[0]) * a.F * 2;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int m = __shfl(token, 4 * kb + j, 64);
-                const float wt = __shfl(weight, 4 * kb + j, 64);
-                if (16 * t + 4 * kb + j < et.count) {
+                for (int r = 0; r < R; ++r) sum[r][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+            }
+            rows_times_tokens<FMT, R, T, C, C>(at, h, G, item % split, split, sum);
 #pragma unroll
-                    for (int r = 0; r < R; ++r) {
-                        float *const o = &out[w][(m * R + r) * 16 + n];
-                        *o = fmaf(wt, sum[r][0][j], *o);
+            for (int t = 0; t < T; ++t)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int m = __shfl(t0 + t ? et.token[1] : et.token[0], 4 * kb + j, 64);
+                    const float wt = __shfl(t0 + t ? et.weight[1] : et.weight[0], 4 * kb + j, 64);
+                    if (16 * (t0 + t) + 4 * kb + j < et.count) {
+#pragma unroll
+                        for (int r = 0; r < R; ++r) {
+                            float *const o = &out[w][(m * R + r) * 16 + n];
+                            *o = fmaf(wt, sum[r][t][j], *o);
+                        }
                     }
                 }
-            }
         }
     }
     __syncthreads();
@@ -359,16 +424,28 @@ __global__ __launch_bounds__(64 * W) void moe_down_kernel(MoeArgs a) {
 constexpr int kColumns = 2;    // of a pass (rows_times_tokens)
 constexpr int kDownWaves = 8;  // of a workgroup of the second launch
 
-// Workgroups that share a row tile of the second launch: as many as leave each wave two passes (over the experts that the tokens
-// can choose).  Two experts, 14 passes: 5.1 us with one, 6.2 with two, 7.7 with four; eight experts, 32 passes: 7.2 against 6.7 and
-// 6.7; 43 of 64 experts, 172 passes: 26.5, 18.3, 16.9 (all microscaled).
-int parts_of(const MoeArgs &a) {
-    const int experts = a.E <= a.pairs ? a.E : a.pairs, passes = (a.F + 128 * kColumns - 1) / (128 * kColumns);
-    const int parts = experts * passes / (2 * kDownWaves);
-    return parts < 1 ? 1 : parts < kMaxParts ? parts : kMaxParts;
+// The second launch in tiles of 64 outputs (32 with two token tiles), four row tiles reading a token's h at once, where that leaves a
+// workgroup to each compute unit: 4096 outputs of 32 experts 32 us against 44 microscaled, 38 against 47 int4; 2048 outputs, half
+// the workgroups: 26 against 17.
+bool wide_down(const MoeArgs &a, int parts) {
+    return a.K / 16 % 4 == 0 && (int64_t)(a.K / 64) * parts >= device_cu_count();
 }
 
-template <int FMT, int CHUNKS>
+// Workgroups that share a row tile of the second launch: as many as leave each wave a pass (over the experts that the tokens can
+// choose), or two passes where a pass would be more than two workgroups to each compute unit.  Two experts of 4096 outputs, 14
+// passes: 5.1 us with one, 6.2 with two, 7.7 with four; 23 of 28 experts of 992 outputs, 23 passes: both launches 18.2 with one,
+// 13.5 with two; 43 of 64 experts of 2048, 172 passes: 26.5 with one, 18.3 with two, 16.9 with four.
+int parts_of(const MoeArgs &a) {
+    const int experts = a.E <= a.pairs ? a.E : a.pairs, passes = (a.F + 128 * kColumns - 1) / (128 * kColumns);
+    const auto within = [](int v) { return v < 1 ? 1 : v < kMaxParts ? v : kMaxParts; };
+    const int most = within(experts * passes / kDownWaves), least = within(experts * passes / (2 * kDownWaves));
+    if (wide_down(a, most)) return most;
+    const int room = 2 * device_cu_count() / (a.K / 16);
+    return room < least ? least : room < most ? room : most;
+}
+
+// SMALL: up to 64 pairs and 16 tokens.  T: token tiles at a time.
+template <int FMT, int T, bool SMALL>
 int launch_experts(const MoeArgs &a, hipStream_t st) {
     const int experts = a.E <= a.pairs ? a.E : a.pairs, tiles = a.F / 16, out_tiles = a.K / 16;
     const int cus = device_cu_count();
@@ -376,23 +453,33 @@ int launch_experts(const MoeArgs &a, hipStream_t st) {
     // workgroups that are launched (three choices for each on the average leave one in twenty without); eight tiles for each
     // compute unit.  32 experts of 4096 x 1792, 32 tokens: 53 us against 68 microscaled, 65 against 73 int4.  Not for fewer
     // inputs: 64 experts of 2048 x 1024 with half the columns to a wave took 24 us against 20.
-    if (a.K > 2048 && a.K <= 4096 && 3 * a.E <= a.pairs && (int64_t)a.E * tiles >= 8 * cus) {
+    bool resident = false;
+    if constexpr (T == 1) {
+        resident = a.K > 2048 && a.K <= 4096 && 3 * a.E <= a.pairs && (int64_t)a.E * tiles >= 8 * cus;
         const unsigned slices = (unsigned)(a.E < cus ? cus / a.E : 1);
-        hipLaunchKernelGGL((moe_gate_up_resident_kernel<FMT, 8, 4, CHUNKS>), dim3(slices, a.E), dim3(512), 0, st, a);
-    } else {
-        hipLaunchKernelGGL((moe_gate_up_kernel<FMT, 4, kColumns, CHUNKS>), dim3(tiles, experts), dim3(256), 0, st, a);
+        if (resident)
+            hipLaunchKernelGGL((moe_gate_up_resident_kernel<FMT, 8, 4, SMALL>), dim3(slices, a.E), dim3(512), 0, st, a);
     }
+    if (!resident)
+        hipLaunchKernelGGL((moe_gate_up_kernel<FMT, T, 4, kColumns, SMALL>), dim3(tiles, experts), dim3(256), 0, st, a);
     NVQ_HIP_TRY(hipGetLastError());
-    // 64 outputs to a workgroup read a token's h for four row tiles at once, where that leaves a workgroup to each compute unit:
-    // 4096 outputs of 32 experts 32 us against 44 microscaled, 38 against 47 int4; 2048 outputs, half the workgroups: 26 against 17.
-    if (out_tiles % 4 == 0 && (int64_t)(out_tiles / 4) * a.parts >= cus)
-        hipLaunchKernelGGL((moe_down_kernel<FMT, 4, kDownWaves, kColumns, CHUNKS>), dim3(out_tiles / 4, a.parts),
-                           dim3(64 * kDownWaves), 0, st, a);
+    constexpr int kWide = T == 1 ? 4 : 2;
+    const dim3 block(64 * kDownWaves);
+    if (wide_down(a, a.parts))
+        hipLaunchKernelGGL((moe_down_kernel<FMT, kWide, T, kDownWaves, kColumns, SMALL>), dim3(out_tiles / kWide, a.parts), block,
+                           0, st, a);
     else
-        hipLaunchKernelGGL((moe_down_kernel<FMT, 1, kDownWaves, kColumns, CHUNKS>), dim3(out_tiles, a.parts),
-                           dim3(64 * kDownWaves), 0, st, a);
+        hipLaunchKernelGGL((moe_down_kernel<FMT, 1, T, kDownWaves, kColumns, SMALL>), dim3(out_tiles, a.parts), block, 0, st, a);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
+}
+
+template <int FMT>
+int launch_experts(const MoeArgs &a, hipStream_t st) {
+    if (a.pairs <= 64 && a.M <= 16) return launch_experts<FMT, 1, true>(a, st);
+    // Two token tiles at once where most experts have more than 16 tokens: 16 experts of 4096 x 1792 microscaled, 16 tokens each on
+    // the average, 90 us against 101; with twelve 78 against 65.
+    return a.pairs >= 14 * a.E ? launch_experts<FMT, 2, false>(a, st) : launch_experts<FMT, 1, false>(a, st);
 }
 
 // NVQ_OK, or what is wrong with the sizes.
@@ -471,8 +558,5 @@ extern "C" int nvq_moe_experts(const nvq_experts *experts, const uint16_t *x_bf1
     a.y = y;
     a.y_dtype = y_dtype;
     const hipStream_t st = (hipStream_t)stream;
-    const bool small = a.pairs <= 64 && M <= 16;
-    if (experts->format == NVQ_FMT_INT4)
-        return small ? launch_experts<NVQ_FMT_INT4, 1>(a, st) : launch_experts<NVQ_FMT_INT4, kMaxChunks>(a, st);
-    return small ? launch_experts<NVQ_FMT_MXFP4, 1>(a, st) : launch_experts<NVQ_FMT_MXFP4, kMaxChunks>(a, st);
+    return experts->format == NVQ_FMT_INT4 ? launch_experts<NVQ_FMT_INT4>(a, st) : launch_experts<NVQ_FMT_MXFP4>(a, st);
 }

@@ -170,7 +170,7 @@ EXPERTS = [(1, 1, 1, 32, 32), (1, 2, 2, 64, 96), (1, 64, 8, 512, 256), (2, 4, 3,
            (16, 8, 2, 256, 128), (17, 3, 2, 128, 416), (32, 2, 1, 96, 32), (32, 16, 4, 512, 512), (32, 1, 1, 288, 64),
            (7, 300, 4, 64, 32), (32, 20, 16, 128, 160), (3, 2, 5, 64, 64),
            # the second launch: tiles of 64 outputs, several workgroups to a tile, experts in slices
-           (16, 64, 4, 4096, 32), (32, 64, 2, 4096, 96), (9, 6, 6, 4160, 1056), (4, 70, 16, 2048, 160),
+           (16, 64, 4, 4096, 32), (32, 16, 8, 4096, 288), (32, 8, 5, 4128, 288), (29, 2, 2, 160, 800), (32, 64, 2, 4096, 96), (9, 6, 6, 4160, 1056), (4, 70, 16, 2048, 160),
            # the first one with the activations in registers: a short last wave, 128 inputs to a lane-row in all
            (7, 8, 4, 2080, 4096), (3, 3, 3, 4096, 11008)]
 
@@ -225,6 +225,22 @@ def test_unused_slots_padding_and_an_expert_twice(fmt, M, E, k):
         assert not y[2].any() and not y[M - 2].any()
     none = nvq.moe_experts(ex, x, dev(np.full_like(ids, -1)), dev(w))
     assert not none.any()
+
+
+@gpu
+@pytest.mark.parametrize("fmt", ["int4", "mxfp4"])
+@pytest.mark.parametrize("M,E,k", [(30, 9, 3), (32, 4, 11), (32, 7, 16)])
+def test_an_expert_in_several_slots_of_tokens_anywhere_in_the_list(fmt, M, E, k):
+    """Slots next to each other and apart, tokens whose slots lie on both sides of a multiple of 64 pairs, all of them equal."""
+    rng = np.random.default_rng(k)
+    ex, values = make(fmt, E, 96, 64, 9)
+    ids = rng.integers(-1, E, (M, k)).astype(np.int32)
+    ids[64 // k] = ids[128 // k if 128 // k < M else 0] = [E - 1] * k
+    ids[64 // k - 1] = [(i % 2) for i in range(k)]
+    w = rng.random((M, k)).astype(np.float32)
+    x = torch.randn((M, 96), generator=torch.Generator().manual_seed(M)).bfloat16().to(DEV)
+    y = nvq.moe_experts(ex, x, dev(ids), dev(w), out_dtype=torch.float32)
+    check(y, x, values, ids, w)
 
 
 @gpu
