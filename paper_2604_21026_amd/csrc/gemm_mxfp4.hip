@@ -14,62 +14,6 @@ __device__ __forceinline__ int8v fp4_operand(const uint4v &c) {
     return int8v{(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0};
 }
 
-// A wave of 64 x 64 results: weights are the first operand, so that a lane's four registers of a 16x16 tile are
-// four neighbouring rows (columns of y) of one token.
-__global__ __launch_bounds__(64) void gemm_mxfp4_small_k_kernel(const uint4 *__restrict__ wq,
-                                                               const uint8_t *__restrict__ ws, int64_t N, int G,
-                                                               const uint4 *__restrict__ xq,
-                                                               const uint8_t *__restrict__ xs, int64_t M,
-                                                               void *__restrict__ y, int y_dtype, int tiles_n) {
-    const int lane = threadIdx.x, i = lane & 15, kb = lane >> 4;
-    const int64_t n0 = (int64_t)(blockIdx.x % tiles_n) * 64, m0 = (int64_t)(blockIdx.x / tiles_n) * 64;
-    float4v sum[4][4] = {};
-    int64_t wr[4], xr[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        const int64_t n = n0 + 16 * t + i, m = m0 + 16 * t + i;
-        wr[t] = (n < N ? n : N - 1) * G;
-        xr[t] = (m < M ? m : M - 1) * G;
-    }
-    for (int g0 = 0; g0 < G; g0 += 4) {
-        const int g = g0 + kb;
-        const bool in = g < G;
-        uint4v a[4], b[4];
-        int sa[4], sb[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const int64_t at = in ? g : G - 1;
-            a[t] = load_stream(wq + wr[t] + at);
-            b[t] = load_stream(xq + xr[t] + at);
-            sa[t] = ws[wr[t] + at];
-            sb[t] = xs[xr[t] + at];
-            if (!in) {
-                a[t] = b[t] = uint4v{0, 0, 0, 0};
-                sa[t] = sb[t] = 127;
-            }
-        }
-#pragma unroll
-        for (int p = 0; p < 4; ++p)
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                sum[p][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(a[p]), fp4_operand(b[t]), sum[p][t],
-                                                                             4, 4, 0, sa[p], 0, sb[t]);
-    }
-#pragma unroll
-    for (int p = 0; p < 4; ++p)
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            asm volatile("s_nop 7\n\ts_nop 7" : "+v"(sum[p][t]));
-            const int64_t m = m0 + 16 * t + i;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int64_t n = n0 + 16 * p + 4 * kb + j;
-                if (m < M && n < N) store_global(y, y_dtype, m * N + n, sum[p][t][j]);
-            }
-        }
-}
-
-
 // ---- tiles through LDS ----
 typedef __attribute__((address_space(3))) void *lds_void_ptr;
 
@@ -116,41 +60,50 @@ __device__ __forceinline__ GemmTile gemm_tile_of(int block, int tiles, int tiles
     return GemmTile{in / high, first + in % high};
 }
 
-// A wave's results: 16 tokens at a time through LDS (`out`: 16 rows of 16 P results and 16 bytes), so that they leave as
-// whole runs of 16 P results, 16 bytes per lane where the rows of y allow it.  BYTES: of a result.
-template <int P, int T, int BYTES>
+// A wave's results: 16 A tokens at a time through LDS (`out`: 16 A rows of 16 P results and 16 bytes), so that they leave as
+// whole runs of 16 P results, 16 bytes per lane at any
+// alignment (4095 x 28669 x 4096: 281 us, by single results 390).  BYTES: of a result.
+template <int P, int T, int A, int BYTES>
 __device__ __forceinline__ void store_tile(unsigned char *out, float4v (&sum)[P][T], int n0, int N, int m0, int M, void *y) {
     constexpr int kRow = 16 * P * BYTES, kPitch = kRow + 16;
     const int lane = threadIdx.x & 63, i = lane & 15, kb = lane >> 4;
-    const bool whole = n0 + 16 * P <= N && ((int64_t)N * BYTES & 15) == 0 && ((uintptr_t)y & 15) == 0;  // (uniform)
+    typedef uint4v uint4v_any __attribute__((aligned(2)));  // (rows of y begin anywhere)
+    const bool whole = n0 + 16 * P <= N;  // (uniform)
 #pragma unroll
-    for (int t = 0; t < T; ++t) {
-        if (m0 + 16 * t >= M) break;  // (uniform)
+    for (int t0 = 0; t0 < T; t0 += A) {
+        const int first = m0 + 16 * t0;
+        if (first >= M) break;  // (uniform)
 #pragma unroll
-        for (int p = 0; p < P; ++p) {
-            unsigned char *const at = out + i * kPitch + (16 * p + 4 * kb) * BYTES;
-            if (BYTES == 2)
-                *reinterpret_cast<uint2v *>(at) = uint2v{pack_bf16x2(sum[p][t][0], sum[p][t][1]), pack_bf16x2(sum[p][t][2], sum[p][t][3])};
-            else
-                *reinterpret_cast<float4v *>(at) = sum[p][t];
-        }
+        for (int t = 0; t < A; ++t)
+#pragma unroll
+            for (int p = 0; p < P; ++p) {
+                unsigned char *const at = out + (16 * t + i) * kPitch + (16 * p + 4 * kb) * BYTES;
+                const float4v v = sum[p][t0 + t];
+                if (BYTES == 2)
+                    *reinterpret_cast<uint2v *>(at) = uint2v{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                else
+                    *reinterpret_cast<float4v *>(at) = v;
+            }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        const int tokens = M - (m0 + 16 * t) < 16 ? M - (m0 + 16 * t) : 16;
+        const int tokens = M - first < 16 * A ? M - first : 16 * A;
         if (whole) {
             constexpr int kLanes = kRow / 16;  // of a row
 #pragma unroll
-            for (int c = 0; c < 16 * kLanes / 64; ++c) {
+            for (int c = 0; c < 16 * A * kLanes / 64; ++c) {
                 const int r = (64 * c + lane) / kLanes, b = (64 * c + lane) % kLanes * 16;
                 const uint4v v = *reinterpret_cast<const uint4v *>(out + r * kPitch + b);
                 if (r < tokens)
-                    *(__attribute__((address_space(1))) uint4v *)(static_cast<char *>(y) +
-                                                                  ((int64_t)(m0 + 16 * t + r) * N + n0) * BYTES + b) = v;
+                    *(__attribute__((address_space(1))) uint4v_any *)(static_cast<char *>(y) +
+                                                                      ((int64_t)(first + r) * N + n0) * BYTES + b) = v;
             }
         } else {
+            // (one by one, a read of LDS and its store took 2 us more; unrolled in the largest tile, which fills the registers, they
+            // cost its whole rows 4 %)
+#pragma unroll(P == 8 ? 1 : 8)
             for (int c = lane; c < tokens * 16 * P; c += 64) {
                 const int r = c / (16 * P), n = c % (16 * P);
                 if (n0 + n >= N) continue;
-                const int64_t to = (int64_t)(m0 + 16 * t + r) * N + n0 + n;
+                const int64_t to = (int64_t)(first + r) * N + n0 + n;
                 if (BYTES == 2)
                     ((__attribute__((address_space(1))) uint16_t *)y)[to] = *reinterpret_cast<const uint16_t *>(out + r * kPitch + n * 2);
                 else
@@ -159,6 +112,60 @@ __device__ __forceinline__ void store_tile(unsigned char *out, float4v (&sum)[P]
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
+}
+
+// A wave of 64 x 64 results: weights are the first operand, so that a lane's four registers of a 16x16 tile are
+// four neighbouring rows (columns of y) of one token.  For short K, where the results are the work: 658 x 9765 x 448 took 20 us
+// with a store from each lane for each result, 12 in whole runs; 4096 x 4096 x 256 40 and 17.
+__global__ __launch_bounds__(64) void gemm_mxfp4_small_k_kernel(const uint4 *__restrict__ wq,
+                                                               const uint8_t *__restrict__ ws, int N, int G,
+                                                               const uint4 *__restrict__ xq,
+                                                               const uint8_t *__restrict__ xs, int M,
+                                                               void *__restrict__ y, int y_dtype, int tiles_n) {
+    const int lane = threadIdx.x, i = lane & 15, kb = lane >> 4;
+    __shared__ __attribute__((aligned(16))) unsigned char out[64 * (64 * 4 + 16)];
+    const GemmTile tile = gemm_tile_of(blockIdx.x, gridDim.x, tiles_n);
+    const int n0 = tile.n * 64, m0 = tile.m * 64;
+    float4v sum[4][4] = {};
+    int64_t wr[4], xr[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        const int n = n0 + 16 * t + i, m = m0 + 16 * t + i;
+        wr[t] = (int64_t)(n < N ? n : N - 1) * G;
+        xr[t] = (int64_t)(m < M ? m : M - 1) * G;
+    }
+    for (int g0 = 0; g0 < G; g0 += 4) {
+        const int g = g0 + kb;
+        const bool in = g < G;
+        uint4v a[4], b[4];
+        int sa[4], sb[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const int64_t at = in ? g : G - 1;
+            a[t] = load_stream(wq + wr[t] + at);
+            b[t] = load_stream(xq + xr[t] + at);
+            sa[t] = ws[wr[t] + at];
+            sb[t] = xs[xr[t] + at];
+            if (!in) {
+                a[t] = b[t] = uint4v{0, 0, 0, 0};
+                sa[t] = sb[t] = 127;
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < 4; ++p)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                sum[p][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fp4_operand(a[p]), fp4_operand(b[t]), sum[p][t],
+                                                                             4, 4, 0, sa[p], 0, sb[t]);
+    }
+#pragma unroll
+    for (int p = 0; p < 4; ++p)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) asm volatile("s_nop 7\n\ts_nop 7" : "+v"(sum[p][t]));
+    if (y_dtype == NVQ_BF16)
+        store_tile<4, 4, 4, 2>(out, sum, n0, N, m0, M, y);
+    else
+        store_tile<4, 4, 4, 4>(out, sum, n0, N, m0, M, y);
 }
 
 // 4 x 4 bytes transposed: word k of the result holds byte k of the four words.
@@ -394,9 +401,9 @@ __global__ __launch_bounds__(256 * S) __attribute__((amdgpu_waves_per_eu(W, W)))
     unsigned char *const out = (wave >> 1 ? stage1 : stage0) + (wave & 1) * (16 * (16 * P * 4 + 16));
     const int first_n = n0 + wa * (16 * P), first_m = m0 + wb * (16 * T);
     if (y_dtype == NVQ_BF16)
-        store_tile<P, T, 2>(out, sum, first_n, N, first_m, M, y);
+        store_tile<P, T, 1, 2>(out, sum, first_n, N, first_m, M, y);
     else
-        store_tile<P, T, 4>(out, sum, first_n, N, first_m, M, y);
+        store_tile<P, T, 1, 4>(out, sum, first_n, N, first_m, M, y);
 }
 
 struct GemmArgs {
@@ -419,8 +426,8 @@ int gemm_small_k(const GemmArgs &a, hipStream_t st) {
     const int64_t tn = ((int64_t)a.N + 63) / 64, tm = ((int64_t)a.M + 63) / 64;
     if (tn * tm * 64 > 0xffffffffLL) return NVQ_ERR_SHAPE;  // (a launch's work items)
     hipLaunchKernelGGL(gemm_mxfp4_small_k_kernel, dim3((unsigned)(tn * tm)), dim3(64), 0, st,
-                       reinterpret_cast<const uint4 *>(a.wq), a.ws, (int64_t)a.N, a.G, reinterpret_cast<const uint4 *>(a.xq),
-                       a.xs, (int64_t)a.M, a.y, a.y_dtype, (int)tn);
+                       reinterpret_cast<const uint4 *>(a.wq), a.ws, a.N, a.G, reinterpret_cast<const uint4 *>(a.xq),
+                       a.xs, a.M, a.y, a.y_dtype, (int)tn);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
 }
@@ -444,6 +451,9 @@ extern "C" int nvq_gemm_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
     //   4096 x 4096 x 4096      42       49         70
     //   2048 x 4096 x 4096      35       26         45          63
     //   1024 x 6144 x 4096      34       23         34          49                   78
+    //   2048 x 2048 x 4096      31       16         23          33         35        53
+    //   768 x 4096 x 4096       30       16         22          24         27        40
+    //   1500 x 3000 x 2048      36       16         22          25         25        41
     //   512 x 4096 x 14336      80       40         32          49                   66
     //   128 x 14336 x 4096      31       15         12          17                   27
     //   256 x 4096 x 4096       29       13        10.3         8.6                  13.5
@@ -456,7 +466,7 @@ extern "C" int nvq_gemm_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
     const int64_t cus = device_cu_count();
     const auto tiles = [&](int rows, int tokens) { return ((N + rows - 1) / rows) * ((M + tokens - 1) / tokens); };
     if (tiles(256, 256) >= cus * 7 / 8) return gemm_tiles<8, 8, 1, 1>(a, st);
-    if (tiles(128, 128) >= cus * 5 / 4) return gemm_tiles<4, 4, 1, 2>(a, st);
+    if (tiles(128, 64) > cus) return gemm_tiles<4, 4, 1, 2>(a, st);
     if (tiles(128, 64) >= cus * 3 / 4) return gemm_tiles<4, 2, 2, 2>(a, st);
     if (tiles(64, 32) > cus) return gemm_tiles<2, 2, 2, 2>(a, st);
     return K >= 8192 ? gemm_tiles<2, 1, 4, 4>(a, st) : gemm_tiles<2, 1, 2, 4>(a, st);
