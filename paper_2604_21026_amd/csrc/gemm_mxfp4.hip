@@ -61,8 +61,8 @@ __device__ __forceinline__ GemmTile gemm_tile_of(int block, int tiles, int tiles
 }
 
 // A wave's results: 16 A tokens at a time through LDS (`out`: 16 A rows of 16 P results and 16 bytes), so that they leave as
-// whole runs of 16 P results, 16 bytes per lane at any
-// alignment (4095 x 28669 x 4096: 281 us, by single results 390).  BYTES: of a result.
+// whole runs of 16 P results, 16 bytes per lane at any alignment (4095 x 28669 x 4096: 281 us, by single results 390).
+// BYTES: of a result.
 template <int P, int T, int A, int BYTES>
 __device__ __forceinline__ void store_tile(unsigned char *out, float4v (&sum)[P][T], int n0, int N, int m0, int M, void *y) {
     constexpr int kRow = 16 * P * BYTES, kPitch = kRow + 16;
@@ -97,9 +97,10 @@ __device__ __forceinline__ void store_tile(unsigned char *out, float4v (&sum)[P]
                                                                       ((int64_t)(first + r) * N + n0) * BYTES + b) = v;
             }
         } else {
+            constexpr int kAtOnce = P == 8 ? 1 : 8;
             // (one by one, a read of LDS and its store took 2 us more; unrolled in the largest tile, which fills the registers, they
             // cost its whole rows 4 %)
-#pragma unroll(P == 8 ? 1 : 8)
+#pragma unroll kAtOnce
             for (int c = lane; c < tokens * 16 * P; c += 64) {
                 const int r = c / (16 * P), n = c % (16 * P);
                 if (n0 + n >= N) continue;

@@ -5,6 +5,8 @@
 // A few tokens' router is latency, not bytes: the grid is tiles of 16 experts times parts of K, so that a few
 // hundred waves ask for everything at once; each leaves its partial logits in the workspace, and the workgroup that
 // arrives last (a counter that wraps to zero by itself) adds them in the order of the parts and chooses.
+//
+// Measured: one token of 64 experts, 2048 inputs 5.2 us (an empty launch 2.4); 32 tokens of 128 experts, 4096 inputs 7.8 us.
 #include "mfma_act.h"
 
 namespace nvq {
@@ -37,84 +39,92 @@ __device__ __forceinline__ float of_order_word(uint32_t w) { return __uint_as_fl
 struct MaxWord {
     __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
 };
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-    v = with_lane_xor<32>(v, MaxWord());
-    v = with_lane_xor<16>(v, MaxWord());
-    v = with_lane_xor<8>(v, MaxWord());
-    v = with_lane_xor<4>(v, MaxWord());
-    v = with_lane_xor<2>(v, MaxWord());
-    return with_lane_xor<1>(v, MaxWord());
-}
-
-// The logits of a token from their parts, all requested at once (one after the other they were 14 of the 25 us that
-// 32 tokens and 128 experts took).
-template <int PER>
-__device__ __forceinline__ void ask_parts(const RouteArgs &a, int m, float (&v)[PER][kRouteMaxParts]) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        const int e = 64 * j + lane;
-        const int in = e < a.E ? e : a.E - 1;
-        const float *const at = a.partial + ((int64_t)(in >> 4) * a.parts * a.M + m) * 16 + (in & 15);
-#pragma unroll
-        for (int p = 0; p < kRouteMaxParts; ++p)
-            v[j][p] = __hip_atomic_load(at + (int64_t)(p < a.parts ? p : 0) * a.M * 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+struct MinWord {
+    __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return a < b ? a : b; }
+};
+// Over groups of L lanes.
+template <int L, typename T, typename OP>
+__device__ __forceinline__ T over_group(T v, OP op) {
+    if (L == 64) {
+        v = with_lane_xor<32>(v, op);
+        v = with_lane_xor<16>(v, op);
     }
+    v = with_lane_xor<8>(v, op);
+    v = with_lane_xor<4>(v, op);
+    v = with_lane_xor<2>(v, op);
+    return with_lane_xor<1>(v, op);
 }
 
-// The chosen experts of one token, by one wave.  PER: experts per lane (E <= 64 * PER).
-template <int PER>
-__device__ __forceinline__ void choose(const RouteArgs &a, int m, const float (&v)[PER][kRouteMaxParts]) {
-    const int lane = threadIdx.x & 63;
-    float l[PER];
-    uint32_t key[PER];
+// The chosen experts of token m, by L lanes: lane i of them holds the logits of experts i, L + i .., P in all.  Their parts are
+// requested up to eight experts at once (one after the other they were 14 of the 25 us that 32 tokens and 128 experts took).
+// A choice is instructions on one compute unit, not bytes.
+template <int L, int P>
+__device__ __forceinline__ void choose(const RouteArgs &a, int m) {
+    const int i = threadIdx.x & (L - 1);
+    const bool here = m < a.M;
+    const float *const own = a.partial + (here ? m : a.M - 1) * 16;
+    uint32_t key[P];
+    constexpr int kAtOnce = P < 8 ? P : 8;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        l[j] = 0.0f;
+    for (int j0 = 0; j0 < P; j0 += kAtOnce) {
+        float v[kAtOnce][kRouteMaxParts];
 #pragma unroll
-        for (int p = 0; p < kRouteMaxParts; ++p) l[j] += p < a.parts ? v[j][p] : 0.0f;
-        key[j] = 64 * j + lane < a.E ? order_word(l[j]) : 0u;
+        for (int j = 0; j < kAtOnce; ++j) {
+            const int e = L * (j0 + j) + i, in = e < a.E ? e : a.E - 1;
+            const float *const at = own + (int64_t)(in >> 4) * a.parts * a.M * 16 + (in & 15);
+#pragma unroll
+            for (int p = 0; p < kRouteMaxParts; ++p)
+                v[j][p] = __hip_atomic_load(at + (int64_t)(p < a.parts ? p : 0) * a.M * 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            float l = 0.0f;
+#pragma unroll
+            for (int p = 0; p < kRouteMaxParts; ++p) l += p < a.parts ? v[j][p] : 0.0f;
+            key[j0 + j] = L * (j0 + j) + i < a.E ? order_word(l) : 0u;
+        }
     }
     float all = 0.0f, top = 0.0f, chosen = 0.0f, mine = 0.0f;
     int my_id = 0;
     for (int k = 0; k < a.top_k; ++k) {
         uint32_t best = key[0];
+        int at = i;  // the expert (of equal ones the lowest)
 #pragma unroll
-        for (int j = 1; j < PER; ++j) best = key[j] > best ? key[j] : best;
-        best = wave_max(best);
-        int id = -1;
-        const float value = of_order_word(best);
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const uint64_t at = __ballot(key[j] == best);
-            if (id < 0 && at) {  // (uniform)
-                id = 64 * j + __builtin_ctzll(at);
-                if (lane == (id & 63)) key[j] = 0u;
-            }
+        for (int j = 1; j < P; ++j) {
+            const bool more = key[j] > best;
+            best = more ? key[j] : best;
+            at = more ? L * j + i : at;
         }
+        const uint32_t most = over_group<L>(best, MaxWord());
+        const uint32_t id = P == 1 && L == 64 ? (uint32_t)__builtin_ctzll(__ballot(best == most))
+                                              : over_group<L>(best == most ? (uint32_t)at : ~0u, MinWord());
+        const float value = of_order_word(most);
         if (k == 0) {
             top = value;
             if (!a.renormalise) {
 #pragma unroll
-                for (int j = 0; j < PER; ++j) all += 64 * j + lane < a.E ? expf(l[j] - top) : 0.0f;
-                all = group_sum<64>(all);
+                for (int j = 0; j < P; ++j) all += L * j + i < a.E ? expf(of_order_word(key[j]) - top) : 0.0f;
+                all = over_group<L>(all, AddOp());
             }
         }
+#pragma unroll
+        for (int j = 0; j < P; ++j)
+            if ((uint32_t)(L * j + i) == id) key[j] = 0u;
         const float w = expf(value - top);
         chosen += w;
-        if (lane == k) {
-            my_id = id;
+        if (i == k) {
+            my_id = (int)id;
             mine = w;
         }
     }
-    if (lane < a.top_k) {
-        a.ids[m * a.top_k + lane] = my_id;
-        a.weights[m * a.top_k + lane] = mine / (a.renormalise ? chosen : all);
+    if (here && i < a.top_k) {
+        a.ids[m * a.top_k + i] = my_id;
+        a.weights[m * a.top_k + i] = mine / (a.renormalise ? chosen : all);
     }
 }
 
-// T token tiles, PER experts per lane in the choice.
-template <int T, int PER>
+// T token tiles; L lanes per token and P experts per lane in the choice.
+template <int T, int L, int P>
 __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(RouteArgs a) {
     __shared__ float red[kRouteWaves][T * 4][64];
     __shared__ uint32_t last;
@@ -181,24 +191,21 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(RouteArgs a) {
     }
     __syncthreads();
     if (!last) return;
-    for (int m = w; m < a.M; m += kRouteWaves) {
-        float v[PER][kRouteMaxParts];
-        ask_parts<PER>(a, m, v);
-        choose<PER>(a, m, v);
-    }
+    const int m = threadIdx.x / L;
+    if (m - m % (64 / L) < a.M) choose<L, P>(a, m);  // (whole waves)
 }
 
-template <int T>
+template <int T, int L>
 int launch_route(const RouteArgs &a, hipStream_t st) {
     const dim3 grid((unsigned)(a.tiles * a.parts)), block(kRouteThreads);
     if (a.E <= 64)
-        hipLaunchKernelGGL((moe_route_kernel<T, 1>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((moe_route_kernel<T, L, 64 / L>), grid, block, 0, st, a);
     else if (a.E <= 128)
-        hipLaunchKernelGGL((moe_route_kernel<T, 2>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((moe_route_kernel<T, L, 128 / L>), grid, block, 0, st, a);
     else if (a.E <= 256)
-        hipLaunchKernelGGL((moe_route_kernel<T, 4>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((moe_route_kernel<T, L, 256 / L>), grid, block, 0, st, a);
     else
-        hipLaunchKernelGGL((moe_route_kernel<T, 8>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((moe_route_kernel<T, L, 512 / L>), grid, block, 0, st, a);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
 }
@@ -246,5 +253,9 @@ extern "C" int nvq_moe_route(const uint16_t *x_bf16, const uint16_t *router_bf16
     parts = parts < kRouteMaxParts ? parts : kRouteMaxParts;
     a.cols = ((cols + parts - 1) / parts + 1) / 2 * 2;  // (whole lines)
     a.parts = (cols + a.cols - 1) / a.cols;
-    return M <= 16 ? launch_route<1>(a, (hipStream_t)stream) : launch_route<2>(a, (hipStream_t)stream);
+    const hipStream_t st = (hipStream_t)stream;
+    // Lanes per token in the choice: of many tokens four share a wave, sixteen lanes each (32 tokens of 128 experts 7.8 us against 9.4,
+    // of 6 experts 5.5 against 7.7); few tokens have a wave each (one of 256 experts 6.6 against 8.5, of 64 5.2 against 5.9).
+    if (M <= 8) return launch_route<1, 64>(a, st);
+    return M <= 16 ? launch_route<1, 16>(a, st) : launch_route<2, 16>(a, st);
 }

@@ -79,7 +79,7 @@ def test_the_binding_refuses_experts_that_do_not_fit():
 
 # ---- the router ----
 ROUTE = [(1, 1, 32, 1), (1, 8, 64, 8), (3, 5, 96, 2), (1, 64, 2048, 8), (16, 17, 160, 16), (17, 64, 512, 1),
-         (32, 128, 4096, 4), (5, 200, 1440, 6), (32, 256, 288, 8), (9, 512, 2048, 16), (2, 300, 65536, 3)]
+         (32, 128, 4096, 4), (8, 64, 320, 8), (9, 65, 320, 9), (13, 300, 256, 16), (31, 511, 64, 7), (6, 129, 4128, 5), (5, 200, 1440, 6), (32, 256, 288, 8), (9, 512, 2048, 16), (2, 300, 65536, 3)]
 
 
 @gpu
