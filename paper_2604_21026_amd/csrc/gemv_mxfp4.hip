@@ -2,9 +2,9 @@
 // blocks g of 2^(scale - 127) * sum_j code[n][32g + j] * x[m][32g + j], weights and activations unrounded, sums in
 // fp32.
 //
-// Bound by reading the weights once, 17 bytes per 32 of them, which is 4.25 bits; mx_rows.h has the product.  Three kernels: row
-// tiles whose workgroups read the activations with the weights, for few rows or tokens; activations shared through LDS; and,
-// for many rows, activations that stay in registers.
+// Bound by reading the weights once, 17 bytes per 32 of them, which is 4.25 bits; mx_rows.h has the product.  Four kernels: row
+// tiles whose workgroups read the activations with the weights, for few inputs or rows; all activations of a few tokens in LDS;
+// activations shared through LDS step by step; and, for many rows, activations that stay in registers.
 #include "mx_rows.h"
 
 namespace nvq {
@@ -281,6 +281,128 @@ __global__ __launch_bounds__(64 * W) void gemv_mxfp4_resident_kernel(const uint8
     }
 }
 
+// Up to four tokens, whose activations fit in LDS: a workgroup keeps them there for all its row tiles, its W waves share out a
+// tile's columns, four at a time, and four times two are on their way, from tile to tile without a pause.  (Nothing is requested
+// past the last one: that cost a quarter at 4096 x 4096.)
+constexpr int kLdsTokens = 4, kLdsBytes = 56 * 1024;  // (two workgroups to a compute unit)
+__device__ __host__ constexpr int lds_pitch(int G) { return ((G + 3) / 4 + 1) * 256 + 16; }
+
+template <int W>
+__global__ __launch_bounds__(64 * W, 4) void gemv_mxfp4_lds_kernel(const uint8_t *__restrict__ q, const uint8_t *__restrict__ scales,
+                                                                   int N, int G, const uint16_t *__restrict__ x, int M,
+                                                                   void *__restrict__ y, int y_dtype) {
+    constexpr int C = 4;  // 16 scales, in one load
+    __shared__ __attribute__((aligned(16))) unsigned char xs[kLdsBytes];
+    __shared__ float red[2][W][4][64];
+    const int lane = threadIdx.x & 63, n = lane & 15, kb = lane >> 4;
+    const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int tiles = (N + 15) >> 4, cols = (G + 3) >> 2, per = (cols + W * C - 1) / (W * C);
+    const int pitch = lds_pitch(G);  // of a token: its columns, one of zeros, 16 bytes that set the tokens' banks apart
+    Codes<C> codes[2][1];
+    uint4v sc[2];
+    auto load = [&](int d, int tile, int part) {
+        const int row = 16 * tile + n, c0 = (part * W + w) * C;
+        const RowAt at = row_at<NVQ_FMT_MXFP4>(q, scales, row < N ? row : N - 1, G);
+#pragma unroll
+        for (int b = 0; b < C; ++b) {
+            const int block = 4 * (c0 + b) + kb;
+            codes[d][0].w[b] = load_stream(at.q + (block < G ? block : G - 1));
+        }
+        typedef uint4v uint4v_any __attribute__((aligned(1)));
+        sc[d] = *(const __attribute__((address_space(1))) uint4v_any *)(at.s + (4 * c0 < G - 16 ? 4 * c0 : G - 16));
+    };
+    // (the loads' place runs ahead of the products')
+    const int items = ((tiles - 1 - (int)blockIdx.x) / (int)gridDim.x + 1) * per;
+    int lt = blockIdx.x, lp = 0;
+    auto ahead = [&](int d) {
+        load(d, lt, lp);
+        if (++lp == per) {
+            lp = 0;
+            lt += gridDim.x;
+        }
+    };
+    ahead(0);
+    if (items > 1) ahead(1);
+    for (int i = threadIdx.x; i < M * (cols + 1) * 16; i += 64 * W) {
+        const int m = i / ((cols + 1) * 16), p = i - m * (cols + 1) * 16;
+        uint4v v = {0, 0, 0, 0};
+        if (p < 4 * G) v = *as_global<uint4v>(reinterpret_cast<const char *>(x) + ((size_t)m * G * 4 + p) * 16);
+        *reinterpret_cast<uint4v *>(&xs[m * pitch + p * 16]) = v;
+    }
+    __syncthreads();
+    const unsigned char *const mine = xs + (n < M ? n : 0) * pitch + 64 * kb;
+    int ct = blockIdx.x, cp = 0, done = 0;
+    float4v sum[1][1] = {{float4v{0.0f, 0.0f, 0.0f, 0.0f}}};
+    auto one = [&](int d, bool more) {
+        const int c0 = (cp * W + w) * C;
+        const int past = 4 * c0 - (G - 16);  // bytes of the scales before the column's (uniform; past the end: zeros)
+        uint4v v = sc[d];
+        if (past > 0) {
+            if (past >= 16) {
+                v = uint4v{0, 0, 0, 0};
+            } else {
+                uint64_t lo = v.x | (uint64_t)v.y << 32, hi = v.z | (uint64_t)v.w << 32;
+                if (past & 8) {
+                    lo = hi;
+                    hi = 0;
+                }
+                const int bits = 8 * (past & 7);
+                if (bits) {
+                    lo = lo >> bits | hi << (64 - bits);
+                    hi >>= bits;
+                }
+                v = uint4v{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+            }
+        }
+        Scales<NVQ_FMT_MXFP4, C> s[1];
+#pragma unroll
+        for (int b = 0; b < C; ++b) s[0].s[b] = v[b];
+#pragma unroll
+        for (int b = 0; b < C; ++b) {
+            const int c = c0 + b < cols ? c0 + b : cols;
+            bf16x8 a[1][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[0][i] = *reinterpret_cast<const bf16x8 *>(mine + c * 256 + 16 * i);
+            multiply_column<NVQ_FMT_MXFP4, 1, 1, C, C>(codes[d], b, s, b, a, sum);
+        }
+        if (more) ahead(d);
+        if (++cp < per) return;
+        wait_written(sum[0][0]);
+        float(&to)[W][4][64] = red[done & 1];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[w][j][lane] = sum[0][0][j];
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        const int j = (w + W - (done * 4) % W) % W;  // (uniform)
+        if (j < 4) {
+            float r = to[0][j][lane];
+#pragma unroll
+            for (int k = 1; k < W; ++k) r += to[k][j][lane];
+            const int m = 4 * kb + j, row = 16 * ct + n;
+            if (m < M && row < N) store_global(y, y_dtype, (int64_t)m * N + row, r);
+        }
+        ++done;
+        cp = 0;
+        ct += gridDim.x;
+        sum[0][0] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    };
+    int left = items;
+    for (; left >= 4; left -= 2) {
+        one(0, true);
+        one(1, true);
+    }
+    if (left == 3) {
+        one(0, true);
+        one(1, false);
+        one(0, false);
+    } else {
+        one(0, false);
+        if (left == 2) one(1, false);
+    }
+}
+
 struct GemvArgs {
     const uint8_t *q, *s;
     const uint16_t *x;
@@ -302,6 +424,13 @@ template <int T, int C>
 int gemv_resident(const GemvArgs &a, int cus, hipStream_t st) {
     hipLaunchKernelGGL((gemv_mxfp4_resident_kernel<T, 8, C, 2>), dim3((unsigned)cus), dim3(512), 0, st, a.q, a.s, a.N, a.G, a.x,
                        a.M, a.y, a.y_dtype);
+    NVQ_HIP_TRY(hipGetLastError());
+    return NVQ_OK;
+}
+
+int gemv_lds(const GemvArgs &a, int grid, hipStream_t st) {
+    hipLaunchKernelGGL((gemv_mxfp4_lds_kernel<8>), dim3((unsigned)grid), dim3(512), 0, st, a.q, a.s, a.N, a.G, a.x, a.M, a.y,
+                       a.y_dtype);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
 }
@@ -336,6 +465,11 @@ extern "C" int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
         if (a.G <= 64) return M <= 16 ? gemv_resident<1, 2>(a, cus, st) : gemv_resident<2, 2>(a, cus, st);
         return M <= 16 ? gemv_resident<1, 4>(a, cus, st) : gemv_resident<2, 4>(a, cus, st);
     }
+    // Few tokens, K of more than half of what eight waves take in a step: (1, 4096, 4096) 3.7 us against 4.0 of what follows, (1,
+    // 14336, 4096) 7.9 against 8.3, (1, 4096, 14336) 8.3 against 9.2, (3, 18830, 6624) 17.4 against 24.9; (8, 8192, 2048) 5.9
+    // against 4.9, (5, 95675, 4800) 54 against 53.
+    if (M <= kLdsTokens && a.G > 64 && M * lds_pitch(a.G) <= kLdsBytes)
+        return gemv_lds(a, (int)(tiles < 2 * cus ? tiles : 2 * cus), st);
     // Up to 16 tokens.  us at (tokens, rows, inputs), R row tiles per workgroup with each wave reading its activations, or activations
     // shared by the RG groups of S waves; a workgroup to each compute unit where row tiles allow:
     //                       rows 1  rows 4  shared 1, 8  shared 2, 4  shared 4, 2
