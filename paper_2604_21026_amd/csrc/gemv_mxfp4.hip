@@ -281,10 +281,10 @@ __global__ __launch_bounds__(64 * W) void gemv_mxfp4_resident_kernel(const uint8
     }
 }
 
-// Up to four tokens, whose activations fit in LDS: a workgroup keeps them there for all its row tiles, its W waves share out a
+// Up to three tokens, whose activations fit in LDS: a workgroup keeps them there for all its row tiles, its W waves share out a
 // tile's columns, four at a time, and four times two are on their way, from tile to tile without a pause.  (Nothing is requested
 // past the last one: that cost a quarter at 4096 x 4096.)
-constexpr int kLdsTokens = 4, kLdsBytes = 56 * 1024;  // (two workgroups to a compute unit)
+constexpr int kLdsTokens = 3, kLdsBytes = 56 * 1024;  // (two workgroups to a compute unit)
 __device__ __host__ constexpr int lds_pitch(int G) { return ((G + 3) / 4 + 1) * 256 + 16; }
 
 template <int W>
@@ -466,8 +466,8 @@ extern "C" int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
         return M <= 16 ? gemv_resident<1, 4>(a, cus, st) : gemv_resident<2, 4>(a, cus, st);
     }
     // Few tokens, K of more than half of what eight waves take in a step: (1, 4096, 4096) 3.7 us against 4.0 of what follows, (1,
-    // 14336, 4096) 7.9 against 8.3, (1, 4096, 14336) 8.3 against 9.2, (3, 18830, 6624) 17.4 against 24.9; (8, 8192, 2048) 5.9
-    // against 4.9, (5, 95675, 4800) 54 against 53.
+    // 10240, 8192) 11.9 against 13.6, (3, 18830, 6624) 16.9 against 25.1, (1, 4096, 14336) with weights from HBM 9.6 against 9.2; (4,
+    // 14336, 4096) 9.8 against 8.8, (8, 8192, 2048) 5.9 against 4.9.
     if (M <= kLdsTokens && a.G > 64 && M * lds_pitch(a.G) <= kLdsBytes)
         return gemv_lds(a, (int)(tiles < 2 * cus ? tiles : 2 * cus), st);
     // Up to 16 tokens.  us at (tokens, rows, inputs), R row tiles per workgroup with each wave reading its activations, or activations

@@ -216,8 +216,8 @@ GEMV = [(1, 1, 32), (1, 16, 64), (2, 17, 96), (1, 33, 128), (3, 70, 160), (16, 3
         (1, 65523, 512), (16, 70001, 544), (17, 65537, 1440), (32, 66000, 2048), (3, 65600, 4096), (20, 65541, 3968), (9, 65539, 4128),
         (18, 65540, 480), (2, 9001, 1056), (14, 16001, 608), (24, 9001, 992),
         # all activations of a few tokens in LDS: one turn to a workgroup, two, three and more; ragged rows, columns and steps
-        (1, 40, 2080), (2, 8193, 2112), (3, 24601, 2272), (4, 17000, 4128), (1, 41000, 5152), (4, 33, 6752), (1, 9000, 28448),
-        (1, 8200, 28576), (4, 100, 6784), (2, 30, 2944),
+        (1, 40, 2080), (2, 8193, 2112), (3, 24601, 2272), (3, 17000, 4128), (1, 41000, 5152), (3, 33, 9152), (2, 40, 13856), (1, 9000, 28448),
+        (1, 8200, 28576), (3, 100, 9184), (2, 30, 2944),
         # a workgroup to each row tile, to two, to four: K that ends inside a turn, and inside a column
         (16, 1003, 4128), (5, 37, 16416), (13, 4090, 6176), (12, 5001, 1568), (6, 8192, 288), (3, 8000, 320), (23, 4001, 4192),
         (19, 3900, 5152), (32, 5009, 2080), (30, 8209, 1312), (11, 8300, 1184), (8, 12003, 2272), (4, 4097, 7200)]
