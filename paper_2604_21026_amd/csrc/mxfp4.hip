@@ -7,6 +7,9 @@
 // input: eight lanes of four fp32 values or four lanes of eight bf16 values make a block and find its
 // maximum with two or three data-parallel moves; the codes leave as whole words, the scales of four blocks
 // as one.
+//
+// Measured at 14336 x 4096: fp32 to codes 42.7 us (6.2 TB/s; 49.8 with one load in flight per lane, 43.8 with two or eight),
+// codes to bf16 22.4 (6.6 TB/s); 8 x 2048 2.4 us each, an empty launch.
 #include "mfma_act.h"
 
 namespace nvq {
@@ -153,7 +156,7 @@ extern "C" int nvq_quant_mxfp4(const void *x, int x_dtype, int64_t M, int64_t K,
     if (M <= 0 || K <= 0 || K % 32 || K > NVQ_MAX_K || M > (INT64_C(1) << 34) / K) return NVQ_ERR_SHAPE;
     if (!nvq::aligned(x, 16) || !nvq::aligned(q, 16) || !nvq::aligned(scales, 4)) return NVQ_ERR_ALIGN;
     const int64_t blocks = M * (K / 32);
-    constexpr int U = 2;
+    constexpr int U = 4;
     const int64_t per = x_dtype == NVQ_BF16 ? U * 64 : U * 32, grid = (blocks + per - 1) / per;
     if (x_dtype == NVQ_BF16)
         hipLaunchKernelGGL((nvq::quant_mxfp4_kernel<true, U>), dim3((unsigned)grid), dim3(256), 0, (hipStream_t)stream,
