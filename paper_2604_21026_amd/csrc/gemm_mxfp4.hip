@@ -3,8 +3,8 @@
 // (i, kb) = (lane % 16, lane / 16) holding the 16 bytes of codes of one block of row or token i and that block's scale
 // byte.  Sums in fp32.
 //
-// Bound by the matrix units where there is enough to multiply, by the L2's rate into LDS in smaller tiles.  Measured: 4096 x 28672 x 4096 (M, N,
-// K) 265 us = 3.6 PFLOP/s (the products alone, in a loop: 158), 512 x 4096 x 14336 31 us, 77 x 1003 x 2080 6 us.
+// Bound by the matrix units where there is enough to multiply, by the L2's rate into LDS in smaller tiles.  Measured (M x N x K): 4096 x
+// 28672 x 4096 265 us = 3.6 PFLOP/s (the products alone, in a loop: 158), 512 x 4096 x 14336 31 us, 77 x 1003 x 2080 6 us.
 #include "mfma_act.h"
 
 namespace nvq {

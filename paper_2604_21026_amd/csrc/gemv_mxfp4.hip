@@ -6,7 +6,7 @@
 // tiles whose workgroups read the activations with the weights, for few inputs or rows; all activations of a few tokens in LDS;
 // activations shared through LDS step by step; and, for many rows, activations that stay in registers.
 //
-// Measured: 4096 x 4096 at one token 3.7 us (an empty launch 2.4), 128256 x 4096 at one token 44 us (6.3 TB/s), at 32 tokens 64 (4.4),
+// Measured: 4096 x 4096 at one token 3.7 us (an empty launch 2.4), 128256 x 4096 at one token 45 us (6.2 TB/s), at 32 tokens 56 (5.0),
 // 128256 x 14336 at one token 160 (6.1); the choices at the end have more.
 #include "mx_rows.h"
 
@@ -209,33 +209,38 @@ __global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const ui
 
 
 // The activations stay in registers: wave w of W keeps those of C columns (4 C blocks of 32 inputs), of all tokens, for the whole
-// kernel, and the workgroup streams row tile after row tile past them, D tiles requested ahead.  So nothing but weights and their
-// scales is read in the loop (read again for every tile, one token's activations took 25 of 68 us at 128256 x 4096).  The last wave's
-// blocks may begin earlier than its share, where the activations are zero.
-// Partial tiles are added through LDS in wave order, by four waves that change from tile to tile.
+// kernel, and the workgroup streams its row tiles past them, one after the other, D of them requested ahead.  So nothing but weights and
+// their scales is read in the loop (read again for every tile, one token's activations took 25 of 68 us at 128256 x 4096).  The
+// last wave's blocks may begin earlier than its share, where the activations are zero.
+// Partial tiles are added through LDS in wave order, by waves that change from tile to tile, and wait there (`out`) until kGroup
+// tiles' results leave as runs of 16 kGroup rows: stored tile by tile, 32 bytes here and there among the loads, 32 tokens' took 64
+// us for 56.
 template <int T, int W, int C, int D>
 __global__ __launch_bounds__(64 * W) void gemv_mxfp4_resident_kernel(const uint8_t *__restrict__ q,
                                                                      const uint8_t *__restrict__ scales, int N, int G,
                                                                      const uint16_t *__restrict__ x, int M,
                                                                      void *__restrict__ y, int y_dtype) {
+    constexpr int kGroup = 16, kRows = 16 * kGroup, kPitch = kRows + 4;
     __shared__ float red[2][W][T * 4][64];
+    __shared__ __attribute__((aligned(16))) float out[2][16 * T][kPitch];
     const int lane = threadIdx.x & 63, n = lane & 15, kb = lane >> 4;
     const int w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int tiles = (N + 15) >> 4;
-    auto tile_of = [&](int it) { return it * (int)gridDim.x + (int)blockIdx.x; };  // the workgroup's tiles
+    // the workgroup's tiles (there are more than workgroups)
+    const int64_t tiles = (N + 15) >> 4;
+    const int begin = (int)(tiles * blockIdx.x / gridDim.x), mine = (int)(tiles * (blockIdx.x + 1) / gridDim.x) - begin;
     const int share = 4 * C * w, b0 = share < G - 4 * C ? share : G - 4 * C;  // (G >= 4 C)
 
     Codes<C> codes[D][1];
     Scales<NVQ_FMT_MXFP4, C> sc[D][1];
-    auto load = [&](int d, int tile) {
-        const int row = 16 * (tile < tiles ? tile : tiles - 1) + n;
+    auto load = [&](int d, int it) {
+        const int row = 16 * (begin + (it < mine ? it : mine - 1)) + n;
         const RowAt at = row_at<NVQ_FMT_MXFP4>(q, scales, row < N ? row : N - 1, G);
         const RowAt from = {at.q + b0, at.s + b0};
         load_codes<C>(codes[d][0], from, 0, kb);
         load_scales<NVQ_FMT_MXFP4, C>(sc[d][0], from, 0);
     };
 #pragma unroll
-    for (int d = 0; d < D; ++d) load(d, tile_of(d));
+    for (int d = 0; d < D; ++d) load(d, d);
     bf16x8 xr[C][T][4];
 #pragma unroll
     for (int b = 0; b < C; ++b)
@@ -250,13 +255,34 @@ __global__ __launch_bounds__(64 * W) void gemv_mxfp4_resident_kernel(const uint8
                 xr[b][t][i] = __builtin_bit_cast(bf16x8, v);
             }
         }
-    auto one = [&](int d, int tile, int it) {
+    // rows of tiles first .. of the group that lies in out[half], four to a lane
+    auto leave = [&](int half, int first, int count) {
+        typedef uint2v uint2v_any __attribute__((aligned(2)));
+        typedef float4v float4v_any __attribute__((aligned(4)));
+        const int row0 = 16 * (begin + first), rows = 16 * count < N - row0 ? 16 * count : N - row0;
+        for (int i = threadIdx.x; i < M * (kRows / 4); i += 64 * W) {
+            const int m = i / (kRows / 4), r = i % (kRows / 4) * 4;
+            if (r >= rows) continue;
+            const float4v v = *reinterpret_cast<const float4v *>(&out[half][m][r]);
+            const int64_t to = (int64_t)m * N + row0 + r;
+            if (r + 4 <= rows) {
+                if (y_dtype == NVQ_BF16)
+                    *(__attribute__((address_space(1))) uint2v_any *)(static_cast<uint16_t *>(y) + to) =
+                        uint2v{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                else
+                    *(__attribute__((address_space(1))) float4v_any *)(static_cast<float *>(y) + to) = v;
+            } else {
+                for (int j = 0; r + j < rows; ++j) store_global(y, y_dtype, to + j, out[half][m][r + j]);
+            }
+        }
+    };
+    auto one = [&](int d, int it) {
         float4v sum[1][T];
 #pragma unroll
         for (int t = 0; t < T; ++t) sum[0][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int b = 0; b < C; ++b) multiply_column<NVQ_FMT_MXFP4, 1, T, C, C>(codes[d], b, sc[d], b, xr[b], sum);
-        load(d, tile_of(it + D));
+        load(d, it + D);
 #pragma unroll
         for (int t = 0; t < T; ++t) {
             wait_written(sum[0][t]);
@@ -267,22 +293,26 @@ __global__ __launch_bounds__(64 * W) void gemv_mxfp4_resident_kernel(const uint8
         __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+        // (the group before is whole since this barrier, its half is written again a group later)
+        if (it % kGroup == 0 && it > 0) leave((it / kGroup - 1) & 1, it - kGroup, kGroup);
         const int reg = (w + W - (it * 4 * T) % W) % W;  // (uniform)
         if (reg < 4 * T) {
             float v = red[it & 1][0][reg][lane];
 #pragma unroll
             for (int k = 1; k < W; ++k) v += red[it & 1][k][reg][lane];
-            const int m = 16 * (reg >> 2) + 4 * kb + (reg & 3), row = 16 * tile + n;
-            if (m < M && row < N) store_global(y, y_dtype, (int64_t)m * N + row, v);
+            out[it / kGroup & 1][16 * (reg >> 2) + 4 * kb + (reg & 3)][16 * (it % kGroup) + n] = v;
         }
     };
-    for (int it = 0; tile_of(it) < tiles; it += D) {
+    for (int it = 0; it < mine; it += D) {
 #pragma unroll
         for (int d = 0; d < D; ++d) {
-            if (d > 0 && tile_of(it + d) >= tiles) break;
-            one(d, tile_of(it + d), it + d);
+            if (d > 0 && it + d >= mine) break;
+            one(d, it + d);
         }
     }
+    __syncthreads();
+    const int last = (mine - 1) / kGroup;
+    leave(last & 1, last * kGroup, mine - last * kGroup);
 }
 
 // Up to three tokens, whose activations fit in LDS: a workgroup keeps them there for all its row tiles, its W waves share out a
@@ -465,7 +495,7 @@ extern "C" int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
     const GemvArgs a = {qweight, scales, x_bf16, y, N, K / 32, M, y_dtype};
     const int cus = device_cu_count();
     const int64_t tiles = ((int64_t)N + 15) / 16;
-    // Many row tiles, K that eight waves hold: (1, 128256, 4096) 44 us, at 16 tokens 50, at 32 62; below, a tile or two per workgroup,
+    // Many row tiles, K that eight waves hold: (1, 128256, 4096) 45 us, at 16 tokens 50, at 32 56; below, a tile or two per workgroup,
     // its start costs more ((1, 14336, 4096) 9.4).
     if (tiles >= 16 * cus && a.G >= 16 && a.G <= 128) {
         if (a.G <= 64) return M <= 16 ? gemv_resident<1, 2>(a, cus, st) : gemv_resident<2, 2>(a, cus, st);

@@ -215,6 +215,8 @@ GEMV = [(1, 1, 32), (1, 16, 64), (2, 17, 96), (1, 33, 128), (3, 70, 160), (16, 3
         # many rows: activations in registers, in the last wave's place and not at all; K for eight and for four columns
         (1, 65523, 512), (16, 70001, 544), (17, 65537, 1440), (32, 66000, 2048), (3, 65600, 4096), (20, 65541, 3968), (9, 65539, 4128),
         (18, 65540, 480), (2, 9001, 1056), (14, 16001, 608), (24, 9001, 992),
+        # ... whose results leave in groups of 256 rows, whole, short and ragged
+        (32, 65536, 1024), (29, 131077, 544), (4, 135171, 512), (32, 69632, 4064),
         # all activations of a few tokens in LDS: one turn to a workgroup, two, three and more; ragged rows, columns and steps
         (1, 40, 2080), (2, 8193, 2112), (3, 24601, 2272), (3, 17000, 4128), (1, 41000, 5152), (3, 33, 9152), (2, 40, 13856), (1, 9000, 28448),
         (1, 8200, 28576), (3, 100, 9184), (2, 30, 2944),
