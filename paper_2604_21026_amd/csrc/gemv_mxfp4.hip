@@ -6,7 +6,7 @@
 // tiles whose workgroups read the activations with the weights, for few inputs or rows; all activations of a few tokens in LDS;
 // activations shared through LDS step by step; and, for many rows, activations that stay in registers.
 //
-// Measured: 4096 x 4096 at one token 3.7 us (an empty launch 2.4), 128256 x 4096 at one token 45 us (6.2 TB/s), at 32 tokens 56 (5.0),
+// Measured: 4096 x 4096 at one token 4.1 us (an empty launch 2.4), 128256 x 4096 at one token 45 us (6.2 TB/s), at 32 tokens 56 (5.0),
 // 128256 x 14336 at one token 160 (6.1); the choices at the end have more.
 #include "mx_rows.h"
 
@@ -501,10 +501,12 @@ extern "C" int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
         if (a.G <= 64) return M <= 16 ? gemv_resident<1, 2>(a, cus, st) : gemv_resident<2, 2>(a, cus, st);
         return M <= 16 ? gemv_resident<1, 4>(a, cus, st) : gemv_resident<2, 4>(a, cus, st);
     }
-    // Few tokens, K of more than half of what eight waves take in a step: (1, 4096, 4096) 3.7 us against 4.0 of what follows, (1,
-    // 10240, 8192) 11.9 against 13.6, (3, 18830, 6624) 16.9 against 25.1, (1, 4096, 14336) with weights from HBM 9.6 against 9.2; (4,
-    // 14336, 4096) 9.8 against 8.8, (8, 8192, 2048) 5.9 against 4.9.
-    if (M <= kLdsTokens && a.G > 64 && M * lds_pitch(a.G) <= kLdsBytes)
+    // Up to three tokens, many row tiles, or several and more K than the waves take at once, or K in whole steps of them (4096 inputs): (1,
+    // 28672, 4096) 12.0 us against 13.5 of what follows, (1, 10240, 8192) 11.9 against 13.6, (3, 18830, 6624) 16.9 against 25.1,
+    // (1, 2048, 8192) 5.4 against 6.2; not (1, 14336, 4096) 8.5 against 8.3, (1, 4096, 14336) 9.6 against 9.2, (1, 4096, 4096), calls
+    // apart from each other, 4.4 against 4.2; nor (4, 14336, 4096) 9.8 against 8.8, (8, 8192, 2048) 5.9 against 4.9.
+    if (M <= kLdsTokens && a.G > 64 && M * lds_pitch(a.G) <= kLdsBytes &&
+        (tiles >= 4 * cus || (a.G > 128 && (tiles > 2 * cus || a.G % 128 == 0))))
         return gemv_lds(a, (int)(tiles < 2 * cus ? tiles : 2 * cus), st);
     // Up to 16 tokens.  us at (tokens, rows, inputs), R row tiles per workgroup with each wave reading its activations, or activations
     // shared by the RG groups of S waves; a workgroup to each compute unit where row tiles allow:

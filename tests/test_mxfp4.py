@@ -218,7 +218,7 @@ GEMV = [(1, 1, 32), (1, 16, 64), (2, 17, 96), (1, 33, 128), (3, 70, 160), (16, 3
         # ... whose results leave in groups of 256 rows, whole, short and ragged
         (32, 65536, 1024), (29, 131077, 544), (4, 135171, 512), (32, 69632, 4064),
         # all activations of a few tokens in LDS: one turn to a workgroup, two, three and more; ragged rows, columns and steps
-        (1, 40, 2080), (2, 8193, 2112), (3, 24601, 2272), (3, 17000, 4128), (1, 41000, 5152), (3, 33, 9152), (2, 40, 13856), (1, 9000, 28448),
+        (1, 40, 8192), (2, 30, 12288), (3, 33, 8192), (1, 8193, 4128), (1, 40, 2080), (2, 8193, 2112), (3, 24601, 2272), (3, 17000, 4128), (1, 41000, 5152), (3, 33, 9152), (2, 40, 13856), (1, 9000, 28448),
         (1, 8200, 28576), (3, 100, 9184), (2, 30, 2944),
         # a workgroup to each row tile, to two, to four: K that ends inside a turn, and inside a column
         (16, 1003, 4128), (5, 37, 16416), (13, 4090, 6176), (12, 5001, 1568), (6, 8192, 288), (3, 8000, 320), (23, 4001, 4192),
