@@ -2,11 +2,11 @@
 // blocks g of 2^(scale - 127) * sum_j code[n][32g + j] * x[m][32g + j], weights and activations unrounded, sums in
 // fp32.
 //
-// Bound by reading the weights once, 17 bytes per 32 of them, which is 4.25 bits; mx_rows.h has the product.  Four kernels: row
-// tiles whose workgroups read the activations with the weights, for few inputs or rows; all activations of a few tokens in LDS;
+// Bound by reading the weights once, 17 bytes per 32 of them, which is 4.25 bits; mx_rows.h has the product on the matrix cores.  Five
+// kernels: one token by dot products; row tiles whose workgroups read the activations with the weights, for few inputs or rows; all activations of a few tokens in LDS;
 // activations shared through LDS step by step; and, for many rows, activations that stay in registers.
 //
-// Measured: 4096 x 4096 at one token 4.1 us (an empty launch 2.4), 128256 x 4096 at one token 45 us (6.2 TB/s), at 32 tokens 56 (5.0),
+// Measured: 4096 x 4096 at one token 3.1 us (an empty launch 2.4), 128256 x 4096 at one token 43 us (6.5 TB/s), at 32 tokens 56 (5.0),
 // 128256 x 14336 at one token 160 (6.1); the choices at the end have more.
 #include "mx_rows.h"
 
@@ -62,6 +62,103 @@ __global__ __launch_bounds__(64 * W) void gemv_mxfp4_kernel(const uint8_t *__res
     }
 }
 
+
+// One token.  KS waves take R rows at a time, a lane of theirs the blocks l, 64 + l, .. (B in all), whose activations it keeps for
+// all its rows, and ask for the next rows meanwhile.  A block's codes become bf16 values, scale and all, eight in four
+// conversions, and go through the dot product of bf16 pairs.  (The matrix cores' way reads the activations for sixteen tokens: four
+// loads for each one of weights, as much of the address path's time; two tokens this way were no faster.)
+template <int B, int R, int KS>
+__global__ __launch_bounds__(256) void gemv_mxfp4_dot_kernel(const uint8_t *__restrict__ q, const uint8_t *__restrict__ scales, int N,
+                                                             int G, const uint16_t *__restrict__ x, void *__restrict__ y,
+                                                             int y_dtype) {
+    static_assert(KS == 1 || KS == 4, "a wave or the workgroup");
+    constexpr int kTeams = 4 / KS;
+    __shared__ float red[2][KS][R];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int team = blockIdx.x * kTeams + w / KS, teams = gridDim.x * kTeams, l0 = w % KS * (64 * B) + lane;
+    const int groups = (N + R - 1) / R;
+    if (team >= groups) return;  // (KS == 4: the whole workgroup)
+    uint4v c[2][R][B];
+    uint32_t sc[2][R][B];
+    auto load = [&](int d, int group) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int64_t row = group * R + r < N ? group * R + r : N - 1;
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                const int block = l0 + 64 * b < G ? l0 + 64 * b : G - 1;  // (past the end: activations of zero)
+                c[d][r][b] = load_stream(reinterpret_cast<const uint4 *>(q) + row * G + block);
+                sc[d][r][b] = as_global<uint8_t>(scales)[row * G + block];
+            }
+        }
+    };
+    load(0, team);
+    uint4v xr[B][4];
+#pragma unroll
+    for (int b = 0; b < B; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            xr[b][i] = uint4v{0, 0, 0, 0};
+            if (l0 + 64 * b < G) xr[b][i] = as_global<uint4v>(x)[(l0 + 64 * b) * 4 + i];
+        }
+    int turn = 0;
+    auto one = [&](int d, int group) {
+        float mine = 0.0f;  // lane r: the result of row r
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int b = 0; b < B; ++b) {
+                const float s = __uint_as_float(sc[d][r][b] << 23);  // (the conversions look at the exponent alone)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint4v v = __builtin_bit_cast(uint4v, mx_values(c[d][r][b][i], s));
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint32_t w2 = v[k], x2 = xr[b][i][k];
+                        sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(nvq_bf16x2, w2), __builtin_bit_cast(nvq_bf16x2, x2),
+                                                              sum, false);
+                    }
+                }
+            }
+            sum = group_sum<64>(sum);
+            mine = lane == r ? sum : mine;
+        }
+        if constexpr (KS > 1) {
+            if (lane < R) red[turn & 1][w][lane] = mine;
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (w == 0 && lane < R) {
+                mine = red[turn & 1][0][lane];
+#pragma unroll
+                for (int k = 1; k < KS; ++k) mine += red[turn & 1][k][lane];
+            }
+            ++turn;
+        }
+        const int64_t row = (int64_t)group * R + lane;
+        if (w % KS == 0 && lane < R && row < N) store_global(y, y_dtype, row, mine);
+    };
+    // (the registers change roles, nothing is requested past the last rows)
+    int g = team;
+    while (true) {
+        if (g + teams >= groups) {
+            one(0, g);
+            return;
+        }
+        load(1, g + teams);
+        one(0, g);
+        g += teams;
+        if (g + teams >= groups) {
+            one(1, g);
+            return;
+        }
+        load(0, g + teams);
+        one(1, g);
+        g += teams;
+    }
+}
 
 // The same for more tokens, whose activations outweigh the weights where every row tile reads them for itself: a workgroup of RG
 // x S waves takes RG * R row tiles, and brings the activations of S passes of C columns into LDS for all of them, a pass ahead
@@ -464,6 +561,15 @@ int gemv_resident(const GemvArgs &a, int cus, hipStream_t st) {
     return NVQ_OK;
 }
 
+template <int B, int R, int KS>
+int gemv_dot(const GemvArgs &a, int cus, hipStream_t st) {
+    const int64_t wanted = ((int64_t)a.N * KS + 4 * R - 1) / (4 * R);
+    hipLaunchKernelGGL((gemv_mxfp4_dot_kernel<B, R, KS>), dim3((unsigned)(wanted < 2 * cus ? wanted : 2 * cus)), dim3(256), 0, st,
+                       a.q, a.s, a.N, a.G, a.x, a.y, a.y_dtype);
+    NVQ_HIP_TRY(hipGetLastError());
+    return NVQ_OK;
+}
+
 int gemv_lds(const GemvArgs &a, int grid, hipStream_t st) {
     hipLaunchKernelGGL((gemv_mxfp4_lds_kernel<8>), dim3((unsigned)grid), dim3(512), 0, st, a.q, a.s, a.N, a.G, a.x, a.M, a.y,
                        a.y_dtype);
@@ -495,16 +601,26 @@ extern "C" int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
     const GemvArgs a = {qweight, scales, x_bf16, y, N, K / 32, M, y_dtype};
     const int cus = device_cu_count();
     const int64_t tiles = ((int64_t)N + 15) / 16;
-    // Many row tiles, K that eight waves hold: (1, 128256, 4096) 45 us, at 16 tokens 50, at 32 56; below, a tile or two per workgroup,
+    // One token, us against what follows: 4096 x 4096 3.1 (4.0), 14336 x 4096 5.5 (8.3), 1024 x 4096 2.7 (3.9), 4096 x 14336 6.7 (9.2),
+    // 2048 x 8192 3.5 (5.4), 10240 x 8192 9.2 (11.4), 128256 x 4096 43 (45), 14336 x 1024 4.0 (4.9); not 32768 x 512 6.0 (4.3), 4096 x 1024 3.0
+    // (2.5).  Two rows at a time, or four where that is one turn of one workgroup to each compute unit (4096 x 4096 3.2 against 3.5, 14336
+    // x 4096 6.6 against 6.0); from 4096 inputs on the four waves share them, four rows at a time (10240 x 8192 9.5 against 10.6).
+    if (M == 1) {
+        if (a.G >= 32 && a.G <= 64 && (int64_t)N * a.G >= 1024 * cus) return gemv_dot<1, 4, 1>(a, cus, st);
+        if (a.G > 64 && a.G <= 128) return N > 8 * cus && N <= 16 * cus ? gemv_dot<2, 4, 1>(a, cus, st) : gemv_dot<2, 2, 1>(a, cus, st);
+        if (a.G > 128 && a.G <= 256) return gemv_dot<1, 4, 4>(a, cus, st);
+        if (a.G > 256 && a.G <= 512) return gemv_dot<2, 4, 4>(a, cus, st);
+    }
+    // Many row tiles, K that eight waves hold: (2, 128256, 4096) 46 us, at 16 tokens 50, at 32 56; below, a tile or two per workgroup,
     // its start costs more ((1, 14336, 4096) 9.4).
     if (tiles >= 16 * cus && a.G >= 16 && a.G <= 128) {
         if (a.G <= 64) return M <= 16 ? gemv_resident<1, 2>(a, cus, st) : gemv_resident<2, 2>(a, cus, st);
         return M <= 16 ? gemv_resident<1, 4>(a, cus, st) : gemv_resident<2, 4>(a, cus, st);
     }
-    // Up to three tokens, many row tiles, or several and more K than the waves take at once, or K in whole steps of them (4096 inputs): (1,
-    // 28672, 4096) 12.0 us against 13.5 of what follows, (1, 10240, 8192) 11.9 against 13.6, (3, 18830, 6624) 16.9 against 25.1,
-    // (1, 2048, 8192) 5.4 against 6.2; not (1, 14336, 4096) 8.5 against 8.3, (1, 4096, 14336) 9.6 against 9.2, (1, 4096, 4096), calls
-    // apart from each other, 4.4 against 4.2; nor (4, 14336, 4096) 9.8 against 8.8, (8, 8192, 2048) 5.9 against 4.9.
+    // Up to three tokens, many row tiles, or several and more K than the waves take at once, or K in whole steps of them (4096 inputs):
+    // (3, 18830, 6624) 16.9 us against 25.1 of what follows; of one token (28672, 4096) 12.0 against 13.5, (10240, 8192) 11.9 against
+    // 13.6, (2048, 8192) 5.4 against 6.2; not (14336, 4096) 8.5 against 8.3, (4096, 14336) 9.6 against 9.2; nor (4, 14336, 4096) 9.8
+    // against 8.8, (8, 8192, 2048) 5.9 against 4.9.
     if (M <= kLdsTokens && a.G > 64 && M * lds_pitch(a.G) <= kLdsBytes &&
         (tiles >= 4 * cus || (a.G > 128 && (tiles > 2 * cus || a.G % 128 == 0))))
         return gemv_lds(a, (int)(tiles < 2 * cus ? tiles : 2 * cus), st);

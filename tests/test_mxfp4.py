@@ -217,6 +217,9 @@ GEMV = [(1, 1, 32), (1, 16, 64), (2, 17, 96), (1, 33, 128), (3, 70, 160), (16, 3
         (18, 65540, 480), (2, 9001, 1056), (14, 16001, 608), (24, 9001, 992),
         # ... whose results leave in groups of 256 rows, whole, short and ragged
         (32, 65536, 1024), (29, 131077, 544), (4, 135171, 512), (32, 69632, 4064),
+        # one token, a lane to a block: one to two blocks of a row, a wave to it or four, ragged rows and blocks, one turn and several
+        (1, 4100, 2048), (1, 9001, 2016), (1, 3, 2080), (1, 2049, 4096), (1, 4097, 4064), (1, 30000, 3968), (1, 5, 4128), (1, 1003, 8192),
+        (1, 9002, 6624), (1, 6, 8224), (1, 4099, 14336), (1, 20001, 16384), (1, 50, 16416),
         # all activations of a few tokens in LDS: one turn to a workgroup, two, three and more; ragged rows, columns and steps
         (1, 40, 8192), (2, 30, 12288), (3, 33, 8192), (1, 8193, 4128), (1, 40, 2080), (2, 8193, 2112), (3, 24601, 2272), (3, 17000, 4128), (1, 41000, 5152), (3, 33, 9152), (2, 40, 13856), (1, 9000, 28448),
         (1, 8200, 28576), (3, 100, 9184), (2, 30, 2944),
@@ -270,6 +273,26 @@ def test_products_of_ordinary_values(M, N, K):
     xv = np_mx.dequant(*np_mx.quant(f64(x)))
     err = np.abs(f64(nvq.gemm_mxfp4(q, s, xq, xs)) - xv @ wv.T)
     assert (err <= (K + 40) * np_mx.EPS32 * (np.abs(xv) @ np.abs(wv).T)).all()
+
+
+@gpu
+@pytest.mark.parametrize("K", [2080, 4160, 8224])
+@pytest.mark.parametrize("byte", [0, 1, 2, 60, 200, 252])
+def test_one_token_at_the_ends_of_the_scales(byte, K):
+    """Weights at an extreme scale, some activations that bring the result back into fp32's range, the rest zero."""
+    rng = np.random.default_rng(byte)
+    q = rng.integers(0, 256, (20, K // 2), dtype=np.uint8)
+    s = np.full((20, K // 32), byte, np.uint8)
+    x = rng.integers(-3, 4, (1, K)) * 2.0 ** min(max(127 - byte, -120), 120) * (rng.random((1, K)) < 0.05)
+    want = x @ np_mx.dequant(q, s).T
+    y = nvq.gemv_mxfp4(dev(q), dev(s), dev(x).bfloat16())
+    assert np.array_equal(f64(y), want.astype(np.float32).astype(np.float64))
+    # and the other way round: activations below bf16's normal numbers
+    x = rng.integers(-3, 4, (1, K)) * 2.0 ** -131
+    s[:] = 240
+    want = x @ np_mx.dequant(q, s).T
+    y = nvq.gemv_mxfp4(dev(q), dev(s), dev(x).bfloat16())
+    assert np.array_equal(f64(y), want.astype(np.float32).astype(np.float64))
 
 
 @gpu
