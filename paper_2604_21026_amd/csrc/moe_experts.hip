@@ -6,12 +6,12 @@
 // workgroup takes 16 or 64 output rows, its waves the experts in turn, or slices of one where there are fewer experts than
 // waves; the sums over experts stay in LDS, one copy per wave, and are added in wave order.  Where a row tile's experts are more
 // than its waves can do with little in flight, up to four workgroups share them: they leave their sums in the workspace, and
-// the last to arrive adds them in their order.  No sum's order depends on timing.  Products: mx_rows.h.
+// the last to arrive adds them in their order.  No sum's order depends on timing.  Products: mx_rows.h.  A token or a few that
+// share few experts take another way, by dot products (below).
 //
 // Bound: the chosen experts' weights, each read once.  Microscaled, 32 experts of 4096 x 1792, 32 tokens, four experts each: 373
 // MB in 84.5 us (first launch 53, second 32), 4.4 TB/s; int4 (396 MB) 99.6 us.  One token, eight experts of 2048 x 1024: 28 MB in
-// 14.6 us (int4) and 27 MB in 12.9 (microscaled), two launches of 6 to 7 us each, of which the chain ids -> tokens -> activations ->
-// products -> sums is most.
+// 11.4 us (int4) and 27 MB in 8.9 (microscaled), two launches (an empty one 2.4), each a chain of ids -> weights -> sums.
 #include "mx_rows.h"
 #include "transform.h"
 
@@ -421,6 +421,152 @@ __global__ __launch_bounds__(64 * W, R * T == 1 ? 4 : 1) void moe_down_kernel(Mo
     }
 }
 
+// ---- few pairs: by dot products ----
+//
+// With a token or two the matrix cores' way reads activations for sixteen, four loads for each one of weights.  Here a lane keeps the
+// activations of its blocks in registers and takes its blocks of R rows, so that nothing but weights is asked for.  Every pair of a
+// token and a slot is worked off by itself (an expert that two tokens chose is read twice).
+
+// The dot product of a block's 32 weights with the lane's activations, x[k] inputs 2 k and 2 k + 1, added to `sum`.  int4: a nibble n
+// stands for n - 8 and goes in as bf16 128 + n (exact); `offset`, -136 times the sum of the activations, takes the rest away.
+template <int FMT>
+__device__ __forceinline__ float block_dot(const uint4v &codes, uint32_t scale, const uint32_t (&x)[16], float offset, float sum) {
+    auto dot = [](uint32_t a, uint32_t b, float c) {
+        return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(nvq_bf16x2, a), __builtin_bit_cast(nvq_bf16x2, b), c, false);
+    };
+    if constexpr (FMT == NVQ_FMT_MXFP4) {
+        const float s = __uint_as_float(scale << 23);  // (the conversions look at the exponent alone)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4v v = __builtin_bit_cast(uint4v, mx_values(codes[i], s));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t two = v[k];
+                sum = dot(two, x[4 * i + k], sum);
+            }
+        }
+        return sum;
+    } else {
+        float v = offset;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t lo = codes[i] & 0x0f0f0f0fu, hi = (codes[i] >> 4) & 0x0f0f0f0fu;  // inputs 4 i .., 16 + 4 i ..
+            v = dot(__builtin_amdgcn_perm(0x43434343u, lo, 0x04010400u), x[2 * i], v);
+            v = dot(__builtin_amdgcn_perm(0x43434343u, lo, 0x04030402u), x[2 * i + 1], v);
+            v = dot(__builtin_amdgcn_perm(0x43434343u, hi, 0x04010400u), x[8 + 2 * i], v);
+            v = dot(__builtin_amdgcn_perm(0x43434343u, hi, 0x04030402u), x[9 + 2 * i], v);
+        }
+        return fmaf(half_bits_to_float((uint16_t)scale), v, sum);
+    }
+}
+template <int FMT>
+__device__ __forceinline__ float block_offset(const uint32_t (&x)[16]) {
+    float s = 0.0f;
+    if constexpr (FMT == NVQ_FMT_INT4) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k)
+            s = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(nvq_bf16x2, 0x3f803f80u), __builtin_bit_cast(nvq_bf16x2, x[k]),
+                                                s, false);
+        s *= -136.0f;
+    }
+    return s;
+}
+// A block's activations (64 bytes), or zeros.
+__device__ __forceinline__ void load_block(const uint16_t *from, bool there, uint32_t (&x)[16]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint4v v = {0, 0, 0, 0};
+        if (there) v = as_global<uint4v>(from)[i];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[4 * i + k] = v[k];
+    }
+}
+// ... and a block's codes and scale, or zeros (which stand for zero, whatever the place holds).
+template <int FMT>
+__device__ __forceinline__ void load_weights(const uint8_t *q, const void *s, int64_t at, bool there, uint4v &codes, uint32_t &scale) {
+    codes = uint4v{0, 0, 0, 0};
+    scale = 0;
+    if (there) {
+        codes = load_stream(reinterpret_cast<const uint4 *>(q) + at);
+        scale = FMT == NVQ_FMT_MXFP4 ? as_global<uint8_t>(s)[at] : as_global<uint16_t>(s)[at];
+    }
+}
+
+// h of pair blockIdx.y: a wave takes R gate rows and the up rows beside them, a lane the blocks l, 64 + l ..
+template <int FMT, int B, int R>
+__global__ __launch_bounds__(256) void moe_gate_up_dot_kernel(MoeArgs a) {
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int pair = blockIdx.y, e = a.ids[pair], f0 = ((int)blockIdx.x * 4 + w) * R, G = a.K / 32;
+    if ((uint32_t)e >= (uint32_t)a.E) return;
+    uint4v c[2 * R][B];
+    uint32_t sc[2 * R][B];
+#pragma unroll
+    for (int r = 0; r < 2 * R; ++r) {
+        const int64_t row = (int64_t)e * 2 * a.F + (r & 1 ? a.F : 0) + f0 + (r >> 1);  // (F is a multiple of 4 R)
+#pragma unroll
+        for (int b = 0; b < B; ++b)
+            load_weights<FMT>(a.gu_q, a.gu_s, row * G + 64 * b + lane, 64 * b + lane < G, c[r][b], sc[r][b]);
+    }
+    uint32_t x[B][16];
+    float offset[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+        load_block(a.x + ((int64_t)token_of(a, pair) * G + 64 * b + lane) * 32, 64 * b + lane < G, x[b]);
+        offset[b] = block_offset<FMT>(x[b]);
+    }
+    float g = 0.0f, u = 0.0f;  // of row f0 + lane
+#pragma unroll
+    for (int r = 0; r < 2 * R; ++r) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int b = 0; b < B; ++b) sum = block_dot<FMT>(c[r][b], sc[r][b], x[b], offset[b], sum);
+        sum = group_sum<64>(sum);
+        if (r & 1)
+            u = lane == r >> 1 ? sum : u;
+        else
+            g = lane == r >> 1 ? sum : g;
+    }
+    if (lane < R) a.h[(int64_t)pair * a.F + f0 + lane] = float_to_bf16_bits(silu_mul_one(g, u));
+}
+
+// y of token blockIdx.y: the token's pairs as one product, whose blocks are those of h of all its slots, 256 B of them, shared out among
+// the lanes of four waves.  Each block's product is weighted with its pair's weight on its way into the row's sum.
+template <int FMT, int B, int R>
+__global__ __launch_bounds__(256) void moe_down_dot_kernel(MoeArgs a) {
+    __shared__ float red[4][R];
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int m = blockIdx.y, row0 = blockIdx.x * R, G = a.F / 32;
+    uint4v c[R][B];
+    uint32_t sc[R][B], h[B][16];
+    float weight[B], offset[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) {
+        const int unit = 256 * b + (int)threadIdx.x, slot = unit / G, block = unit - slot * G;
+        const int pair = m * a.top_k + (slot < a.top_k ? slot : 0);
+        const int e = a.ids[pair];
+        const bool there = slot < a.top_k && (uint32_t)e < (uint32_t)a.E;
+        weight[b] = there ? a.weights[pair] : 0.0f;
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+            load_weights<FMT>(a.dn_q, a.dn_s, ((int64_t)e * a.K + row0 + r) * G + block, there, c[r][b], sc[r][b]);
+        load_block(a.h + ((int64_t)pair * G + block) * 32, there, h[b]);
+        offset[b] = block_offset<FMT>(h[b]);
+    }
+    float mine = 0.0f;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int b = 0; b < B; ++b) sum = fmaf(weight[b], block_dot<FMT>(c[r][b], sc[r][b], h[b], offset[b], 0.0f), sum);
+        sum = group_sum<64>(sum);
+        mine = lane == r ? sum : mine;
+    }
+    if (lane < R) red[w][lane] = mine;
+    __syncthreads();
+    if (w == 0 && lane < R)
+        store_global(a.y, a.y_dtype, (int64_t)m * a.K + row0 + lane, red[0][lane] + red[1][lane] + red[2][lane] + red[3][lane]);
+}
+
 constexpr int kColumns = 2;    // of a pass (rows_times_tokens)
 constexpr int kDownWaves = 8;  // of a workgroup of the second launch
 
@@ -474,8 +620,37 @@ int launch_experts(const MoeArgs &a, hipStream_t st) {
     return NVQ_OK;
 }
 
+// Where dot products are worked off: a few tokens, few of whose experts are shared; K and a token's slots (blocks of h) that fit the
+// lanes.  us, by dot products and on the matrix cores: one token, eight of 64 experts of 2048 x 1024, int4 11.4 and 14.5, microscaled 8.9
+// and 12.8; two tokens 17.5 and 23.5, 12.6 and 18.4; seven tokens, three of 40 experts of 1440 x 992 16.6 and 18.5; not eight tokens,
+// two of eight 16.1 and 13.1, nor six, four of 16 22.1 and 19.9, nor seven with 128 of 256 lanes' blocks and fewer, 12.5 and 9.7.
+bool by_dot_products(const MoeArgs &a) {
+    const int blocks = a.top_k * (a.F / 32);
+    return a.K <= 4096 && blocks >= 64 && blocks <= 512 &&
+           ((a.M <= 4 && a.pairs <= a.E) || (a.M <= 8 && 8 * a.pairs <= 5 * a.E));
+}
+
+template <int FMT>
+int launch_experts_dot(const MoeArgs &a, hipStream_t st) {
+    // gate rows to a wave, outputs to a workgroup (one and two, or four and eight: 2 to 12 % more)
+    constexpr int kRows = 2, kOut = 4;
+    const dim3 grid(a.F / (4 * kRows), a.pairs), out(a.K / kOut, a.M), block(256);
+    if (a.K <= 2048)
+        hipLaunchKernelGGL((moe_gate_up_dot_kernel<FMT, 1, kRows>), grid, block, 0, st, a);
+    else
+        hipLaunchKernelGGL((moe_gate_up_dot_kernel<FMT, 2, kRows>), grid, block, 0, st, a);
+    NVQ_HIP_TRY(hipGetLastError());
+    if (a.top_k * (a.F / 32) <= 256)
+        hipLaunchKernelGGL((moe_down_dot_kernel<FMT, 1, kOut>), out, block, 0, st, a);
+    else
+        hipLaunchKernelGGL((moe_down_dot_kernel<FMT, 2, kOut>), out, block, 0, st, a);
+    NVQ_HIP_TRY(hipGetLastError());
+    return NVQ_OK;
+}
+
 template <int FMT>
 int launch_experts(const MoeArgs &a, hipStream_t st) {
+    if (by_dot_products(a)) return launch_experts_dot<FMT>(a, st);
     if (a.pairs <= 64 && a.M <= 16) return launch_experts<FMT, 1, true>(a, st);
     // Two token tiles at once where most experts have more than 16 tokens: 16 experts of 4096 x 1792 microscaled, 16 tokens each on
     // the average, 90 us against 101; with twelve 78 against 65.

@@ -171,6 +171,9 @@ EXPERTS = [(1, 1, 1, 32, 32), (1, 2, 2, 64, 96), (1, 64, 8, 512, 256), (2, 4, 3,
            (7, 300, 4, 64, 32), (32, 20, 16, 128, 160), (3, 2, 5, 64, 64),
            # the second launch: tiles of 64 outputs, several workgroups to a tile, experts in slices
            (16, 64, 4, 4096, 32), (32, 16, 8, 4096, 288), (32, 8, 5, 4128, 288), (29, 2, 2, 160, 800), (32, 64, 2, 4096, 96), (9, 6, 6, 4160, 1056), (4, 70, 16, 2048, 160),
+           # a few tokens by dot products: one block to a lane and two, in both launches, lanes without
+           (1, 8, 2, 4096, 1792), (7, 40, 3, 1440, 992), (4, 8, 2, 2080, 1056), (2, 64, 8, 1056, 2048), (3, 16, 2, 768, 2048), (1, 1, 1, 96, 2048),
+           (8, 64, 5, 160, 448), (1, 20, 16, 32, 1024), (4, 4, 1, 64, 16384), (1, 8, 2, 4128, 1792),
            # the first one with the activations in registers: a short last wave, 128 inputs to a lane-row in all
            (7, 8, 4, 2080, 4096), (3, 3, 3, 4096, 11008)]
 
@@ -225,6 +228,33 @@ def test_unused_slots_padding_and_an_expert_twice(fmt, M, E, k):
         assert not y[2].any() and not y[M - 2].any()
     none = nvq.moe_experts(ex, x, dev(np.full_like(ids, -1)), dev(w))
     assert not none.any()
+
+
+@gpu
+@pytest.mark.parametrize("fmt", ["int4", "mxfp4"])
+@pytest.mark.parametrize("M,E,k,K,F", [(1, 20, 6, 96, 352), (3, 20, 6, 96, 352), (2, 24, 8, 2144, 1056), (7, 70, 6, 160, 384)])
+def test_few_tokens_with_unused_slots_and_whatever_the_workspace_holds(fmt, M, E, k, K, F):
+    """Slots out of range, an expert twice, a token without any; a workspace of NaN, and no number in an expert that is not chosen."""
+    rng = np.random.default_rng(M + k)
+    ex, values = make(fmt, E, K, F, 11)
+    ids = np.stack([1 + rng.permutation(E - 1)[:k] for _ in range(M)]).astype(np.int32)
+    w = rng.random((M, k)).astype(np.float32)
+    ids[0, 1], ids[0, 3], ids[0, 4], ids[M - 1, k - 1] = -1, ids[0, 0], E, 2 ** 31 - 1
+    w[0, 1], w[0, 4] = np.nan, np.inf
+    if M > 2:
+        ids[1] = -7
+    for s in (ex.keep[1], ex.keep[3]):
+        s[0] = 0x7e00 if fmt == "int4" else 255
+    x = torch.randn((M, K), generator=torch.Generator().manual_seed(M)).bfloat16().to(DEV)
+    ws = ex.workspace(M, k)
+    ws.fill_(255)
+    y = nvq.moe_experts(ex, x, dev(ids), dev(w), out_dtype=torch.float32, workspace=ws)
+    check(y, x, values, ids, np.nan_to_num(w, posinf=0.0))
+    if M > 2:
+        assert not y[1].any()
+    assert torch.equal(y, nvq.moe_experts(ex, x, dev(ids), dev(w), out_dtype=torch.float32, workspace=ws))
+    one = nvq.moe_experts(ex, x[:1].contiguous(), dev(ids[:1]), dev(w[:1]), out_dtype=torch.float32)
+    check(one, x[:1], values, ids[:1], np.nan_to_num(w[:1], posinf=0.0))
 
 
 @gpu
