@@ -3,7 +3,7 @@
 // fp32.
 //
 // Bound by reading the weights once, 17 bytes per 32 of them, which is 4.25 bits; mx_rows.h has the product on the matrix cores.  Five
-// kernels: one token by dot products; row tiles whose workgroups read the activations with the weights, for few inputs or rows; all activations of a few tokens in LDS;
+// kernels: one or two tokens by dot products; row tiles whose workgroups read the activations with the weights, for few inputs or rows; all activations of a few tokens in LDS;
 // activations shared through LDS step by step; and, for many rows, activations that stay in registers.
 //
 // Measured: 4096 x 4096 at one token 3.1 us (an empty launch 2.4), 128256 x 4096 at one token 43 us (6.5 TB/s), at 32 tokens 56 (5.0),
@@ -63,17 +63,17 @@ __global__ __launch_bounds__(64 * W) void gemv_mxfp4_kernel(const uint8_t *__res
 }
 
 
-// One token.  KS waves take R rows at a time, a lane of theirs the blocks l, 64 + l, .. (B in all), whose activations it keeps for
+// One or two tokens (M).  KS waves take R rows at a time, a lane of theirs the blocks l, 64 + l, .. (B in all), whose activations it keeps for
 // all its rows, and ask for the next rows meanwhile.  A block's codes become bf16 values, scale and all, eight in four
 // conversions, and go through the dot product of bf16 pairs.  (The matrix cores' way reads the activations for sixteen tokens: four
-// loads for each one of weights, as much of the address path's time; two tokens this way were no faster.)
-template <int B, int R, int KS>
+// loads for each one of weights, as much of the address path's time.  Of three tokens on the products themselves cost more.)
+template <int M, int B, int R, int KS>
 __global__ __launch_bounds__(256) void gemv_mxfp4_dot_kernel(const uint8_t *__restrict__ q, const uint8_t *__restrict__ scales, int N,
                                                              int G, const uint16_t *__restrict__ x, void *__restrict__ y,
                                                              int y_dtype) {
     static_assert(KS == 1 || KS == 4, "a wave or the workgroup");
     constexpr int kTeams = 4 / KS;
-    __shared__ float red[2][KS][R];
+    __shared__ float red[2][KS][M * R];
     const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int team = blockIdx.x * kTeams + w / KS, teams = gridDim.x * kTeams, l0 = w % KS * (64 * B) + lane;
     const int groups = (N + R - 1) / R;
@@ -93,20 +93,22 @@ __global__ __launch_bounds__(256) void gemv_mxfp4_dot_kernel(const uint8_t *__re
         }
     };
     load(0, team);
-    uint4v xr[B][4];
+    uint4v xr[M][B][4];
 #pragma unroll
-    for (int b = 0; b < B; ++b)
+    for (int m = 0; m < M; ++m)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            xr[b][i] = uint4v{0, 0, 0, 0};
-            if (l0 + 64 * b < G) xr[b][i] = as_global<uint4v>(x)[(l0 + 64 * b) * 4 + i];
-        }
+        for (int b = 0; b < B; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                xr[m][b][i] = uint4v{0, 0, 0, 0};
+                if (l0 + 64 * b < G) xr[m][b][i] = as_global<uint4v>(x)[((int64_t)m * G + l0 + 64 * b) * 4 + i];
+            }
     int turn = 0;
     auto one = [&](int d, int group) {
-        float mine = 0.0f;  // lane r: the result of row r
+        float mine = 0.0f;  // lane m R + r: the result of row r, token m
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            float sum = 0.0f;
+            float sum[M] = {};
 #pragma unroll
             for (int b = 0; b < B; ++b) {
                 const float s = __uint_as_float(sc[d][r][b] << 23);  // (the conversions look at the exponent alone)
@@ -115,30 +117,37 @@ __global__ __launch_bounds__(256) void gemv_mxfp4_dot_kernel(const uint8_t *__re
                     const uint4v v = __builtin_bit_cast(uint4v, mx_values(c[d][r][b][i], s));
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const uint32_t w2 = v[k], x2 = xr[b][i][k];
-                        sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(nvq_bf16x2, w2), __builtin_bit_cast(nvq_bf16x2, x2),
-                                                              sum, false);
+                        const uint32_t w2 = v[k];
+#pragma unroll
+                        for (int m = 0; m < M; ++m) {
+                            const uint32_t x2 = xr[m][b][i][k];
+                            sum[m] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(nvq_bf16x2, w2),
+                                                                     __builtin_bit_cast(nvq_bf16x2, x2), sum[m], false);
+                        }
                     }
                 }
             }
-            sum = group_sum<64>(sum);
-            mine = lane == r ? sum : mine;
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                const float all = group_sum<64>(sum[m]);
+                mine = lane == m * R + r ? all : mine;
+            }
         }
         if constexpr (KS > 1) {
-            if (lane < R) red[turn & 1][w][lane] = mine;
+            if (lane < M * R) red[turn & 1][w][lane] = mine;
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            if (w == 0 && lane < R) {
+            if (w == 0 && lane < M * R) {
                 mine = red[turn & 1][0][lane];
 #pragma unroll
                 for (int k = 1; k < KS; ++k) mine += red[turn & 1][k][lane];
             }
             ++turn;
         }
-        const int64_t row = (int64_t)group * R + lane;
-        if (w % KS == 0 && lane < R && row < N) store_global(y, y_dtype, row, mine);
+        const int row = group * R + lane % R;
+        if (w % KS == 0 && lane < M * R && row < N) store_global(y, y_dtype, (int64_t)(lane / R) * N + row, mine);
     };
     // (the registers change roles, nothing is requested past the last rows)
     int g = team;
@@ -561,10 +570,10 @@ int gemv_resident(const GemvArgs &a, int cus, hipStream_t st) {
     return NVQ_OK;
 }
 
-template <int B, int R, int KS>
+template <int M, int B, int R, int KS>
 int gemv_dot(const GemvArgs &a, int cus, hipStream_t st) {
     const int64_t wanted = ((int64_t)a.N * KS + 4 * R - 1) / (4 * R);
-    hipLaunchKernelGGL((gemv_mxfp4_dot_kernel<B, R, KS>), dim3((unsigned)(wanted < 2 * cus ? wanted : 2 * cus)), dim3(256), 0, st,
+    hipLaunchKernelGGL((gemv_mxfp4_dot_kernel<M, B, R, KS>), dim3((unsigned)(wanted < 2 * cus ? wanted : 2 * cus)), dim3(256), 0, st,
                        a.q, a.s, a.N, a.G, a.x, a.y, a.y_dtype);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
@@ -606,10 +615,17 @@ extern "C" int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
     // (2.5).  Two rows at a time, or four where that is one turn of one workgroup to each compute unit (4096 x 4096 3.2 against 3.5, 14336
     // x 4096 6.6 against 6.0); from 4096 inputs on the four waves share them, four rows at a time (10240 x 8192 9.5 against 10.6).
     if (M == 1) {
-        if (a.G >= 32 && a.G <= 64 && (int64_t)N * a.G >= 1024 * cus) return gemv_dot<1, 4, 1>(a, cus, st);
-        if (a.G > 64 && a.G <= 128) return N > 8 * cus && N <= 16 * cus ? gemv_dot<2, 4, 1>(a, cus, st) : gemv_dot<2, 2, 1>(a, cus, st);
-        if (a.G > 128 && a.G <= 256) return gemv_dot<1, 4, 4>(a, cus, st);
-        if (a.G > 256 && a.G <= 512) return gemv_dot<2, 4, 4>(a, cus, st);
+        if (a.G >= 32 && a.G <= 64 && (int64_t)N * a.G >= 1024 * cus) return gemv_dot<1, 1, 4, 1>(a, cus, st);
+        if (a.G > 64 && a.G <= 128) return N > 8 * cus && N <= 16 * cus ? gemv_dot<1, 2, 4, 1>(a, cus, st) : gemv_dot<1, 2, 2, 1>(a, cus, st);
+        if (a.G > 128 && a.G <= 256) return gemv_dot<1, 1, 4, 4>(a, cus, st);
+        if (a.G > 256 && a.G <= 512) return gemv_dot<1, 2, 4, 4>(a, cus, st);
+    }
+    // Two: 4096 x 4096 4.0 (4.3), 14336 x 4096 7.5 (8.5), 1024 x 4096 3.2 (4.1), 4096 x 14336 9.1 (9.8); not 28672 x 4096 13.4 (12.5).
+    if (M == 2 && tiles < 4 * cus) {
+        if (a.G > 64 && a.G <= 128)
+            return N > 8 * cus && N <= 16 * cus ? gemv_dot<2, 2, 4, 1>(a, cus, st) : gemv_dot<2, 2, 2, 1>(a, cus, st);
+        if (a.G > 128 && a.G <= 256) return gemv_dot<2, 1, 4, 4>(a, cus, st);
+        if (a.G > 256 && a.G <= 512) return gemv_dot<2, 2, 4, 4>(a, cus, st);
     }
     // Many row tiles, K that eight waves hold: (2, 128256, 4096) 46 us, at 16 tokens 50, at 32 56; below, a tile or two per workgroup,
     // its start costs more ((1, 14336, 4096) 9.4).
