@@ -3,7 +3,8 @@
 // fp32.
 //
 // Bound by reading the weights once, 17 bytes per 32 of them, which is 4.25 bits; mx_rows.h has the product on the matrix cores.  Five
-// kernels: one or two tokens by dot products; row tiles whose workgroups read the activations with the weights, for few inputs or rows; all activations of a few tokens in LDS;
+// kernels: one or two tokens by dot products; row tiles whose workgroups read the activations with the weights, for few inputs or
+// rows; all activations of a few tokens in LDS;
 // activations shared through LDS step by step; and, for many rows, activations that stay in registers.
 //
 // Measured: 4096 x 4096 at one token 3.1 us (an empty launch 2.4), 128256 x 4096 at one token 43 us (6.5 TB/s), at 32 tokens 56 (5.0),
@@ -562,6 +563,14 @@ int gemv_rows(const GemvArgs &a, hipStream_t st) {
     return NVQ_OK;
 }
 
+// 17 to 32 tokens, a row tile per workgroup.
+int gemv_two_tiles(const GemvArgs &a, hipStream_t st) {
+    hipLaunchKernelGGL((gemv_mxfp4_kernel<1, 2, 8, 2, 2>), dim3((unsigned)(((int64_t)a.N + 15) / 16)), dim3(512), 0, st, a.q, a.s, a.N,
+                       a.G, a.x, a.M, a.y, a.y_dtype);
+    NVQ_HIP_TRY(hipGetLastError());
+    return NVQ_OK;
+}
+
 template <int T, int C>
 int gemv_resident(const GemvArgs &a, int cus, hipStream_t st) {
     hipLaunchKernelGGL((gemv_mxfp4_resident_kernel<T, 8, C, 2>), dim3((unsigned)cus), dim3(512), 0, st, a.q, a.s, a.N, a.G, a.x,
@@ -665,6 +674,9 @@ extern "C" int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
     //   16 row tiles                         26.4         82.8                      27.2           63
     // (Up to 2 row tiles the activations bound it: every compute unit reads all of them, 0.9 MB at 14336 inputs.  Asked for two turns
     // ahead, each workgroup beginning at another place of K, or with more weights in flight it took as long.)
+    // and with few inputs, each wave reading its activations: (25, 1236, 1760) 4.4 against 6.9 of two row tiles, (20, 300, 3520) 7.1 against
+    // 9.3, (32, 4096, 1024) 4.1 against 4.5, (32, 2048, 2560) 7.0 against 6.8; not (32, 1024, 4096) 10.2 against 7.7.
+    if (tiles <= cus && a.G < 128) return gemv_two_tiles(a, st);
     if (tiles <= cus && a.G >= 128) return gemv_shared<2, 1, 1, 8, 1>(a, st);
     if (tiles <= 2 * cus) return gemv_shared<2, 1, 2, 4, 2>(a, st);
     if (tiles < 16 * cus) return gemv_shared<2, 1, 4, 2, 2>(a, st);

@@ -220,6 +220,8 @@ GEMV = [(1, 1, 32), (1, 16, 64), (2, 17, 96), (1, 33, 128), (3, 70, 160), (16, 3
         # one token, a lane to a block: one to two blocks of a row, a wave to it or four, ragged rows and blocks, one turn and several
         (1, 4100, 2048), (1, 9001, 2016), (1, 3, 2080), (1, 2049, 4096), (1, 4097, 4064), (1, 30000, 3968), (1, 5, 4128), (1, 1003, 8192),
         (1, 9002, 6624), (1, 6, 8224), (1, 4099, 14336), (1, 20001, 16384), (1, 50, 16416),
+        # 17 to 32 tokens of few inputs and rows
+        (20, 99, 2368), (25, 1236, 1760), (17, 956, 384), (32, 4090, 4064),
         # two tokens the same way, and their other ways
         (2, 3, 2080), (2, 2049, 4096), (2, 4097, 4064), (2, 9001, 3968), (2, 1003, 8192), (2, 4099, 14336), (2, 5, 4128), (2, 6, 16384),
         (2, 16400, 2112), (2, 16399, 2112),
