@@ -410,3 +410,59 @@ def test_tensors_of_another_device_than_the_current_one(monkeypatch):
                  lambda: nvq.moe_route(x, router, 2, out=(ids, w), workspace=rws)):
         with pytest.raises(ValueError, match="current device"):
             call()
+
+
+@gpu
+@pytest.mark.parametrize("M", [1, 3, 16, 32])
+def test_two_streams_at_once_and_replays(M):
+    """Two layers on two streams, each with workspaces of its own; then both captured and replayed together."""
+    E, K, F, k = 32, 512, 1024, 4
+    g = torch.Generator().manual_seed(M)
+    sides = []
+    for fmt, seed in (("mxfp4", 21), ("int4", 22)):
+        ex, values = make(fmt, E, K, F, seed)
+        router = (torch.randn((E, K), generator=g) * 0.05).bfloat16().to(DEV)
+        q, s = nvq.quant_mxfp4((torch.randn((200, K), generator=g) * 0.02).to(DEV))
+        x = torch.randn((M, K), generator=g).bfloat16().to(DEV)
+        out = (torch.empty((M, k), dtype=torch.int32, device=DEV), torch.empty((M, k), device=DEV))
+        buf = dict(y=torch.empty((M, K), dtype=torch.bfloat16, device=DEV), z=torch.empty((M, 200), device=DEV))
+        sides.append((ex, values, router, q, s, x, out, buf, nvq.moe_route_workspace(M, E, DEV), ex.workspace(M, k), torch.cuda.Stream()))
+
+    def layer(side):
+        ex, _, router, q, s, x, out, buf, rws, ews, _ = side
+        nvq.moe_route(x, router, k, out=out, workspace=rws)
+        nvq.moe_experts(ex, x, *out, out=buf["y"], workspace=ews)
+        nvq.gemv_mxfp4(q, s, buf["y"], out=buf["z"])
+
+    want = []
+    for side in sides:
+        layer(side)
+        check(side[7]["y"], side[5], side[1], side[6][0].cpu().numpy(), side[6][1].cpu().numpy())
+        want.append([t.clone() for t in (*side[6], side[7]["y"], side[7]["z"])])
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for side in sides:
+            with torch.cuda.stream(side[10]):
+                side[7]["z"].zero_()
+                layer(side)
+    torch.cuda.synchronize()
+    for side, w in zip(sides, want):
+        assert all(torch.equal(a, b) for a, b in zip((*side[6], side[7]["y"], side[7]["z"]), w))
+    graphs = []
+    for side in sides:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            layer(side)
+        graphs.append(graph)
+    for _ in range(3):
+        for side in sides:
+            side[5].copy_(torch.randn((M, K), generator=g).bfloat16())
+        torch.cuda.synchronize()
+        for side, graph in zip(sides, graphs):
+            with torch.cuda.stream(side[10]):
+                graph.replay()
+        torch.cuda.synchronize()
+        for side in sides:
+            got = [t.clone() for t in (*side[6], side[7]["y"], side[7]["z"])]
+            layer(side)
+            assert all(torch.equal(a, b) for a, b in zip(got, (*side[6], side[7]["y"], side[7]["z"])))
