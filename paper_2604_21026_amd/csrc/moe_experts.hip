@@ -620,14 +620,16 @@ int launch_experts(const MoeArgs &a, hipStream_t st) {
     return NVQ_OK;
 }
 
-// Where dot products are worked off: a few tokens, few of whose experts are shared; K and a token's slots (blocks of h) that fit the
-// lanes.  us, by dot products and on the matrix cores: one token, eight of 64 experts of 2048 x 1024, int4 11.4 and 14.5, microscaled 8.9
-// and 12.8; two tokens 17.5 and 23.5, 12.6 and 18.4; seven tokens, three of 40 experts of 1440 x 992 16.6 and 18.5; not eight tokens,
-// two of eight 16.1 and 13.1, nor six, four of 16 22.1 and 19.9, nor seven with 128 of 256 lanes' blocks and fewer, 12.5 and 9.7.
+// Where dot products are worked off: up to eight tokens, few of whose experts are shared; K and a token's slots (blocks of h) that fit
+// the lanes.  us, by dot products and on the matrix cores: one token, eight of 64 experts of 2048 x 1024, int4 11.0 and 14.5,
+// microscaled 8.9 and 12.8; two tokens 17.5 and 23.5, 12.6 and 18.4; seven tokens, three of 40 experts of 1440 x 992 16.4 and 18.5;
+// eight tokens, eight of 64 experts of 2048 x 1024 microscaled 34.6 and 39.9, int4 54.3 and 47.4; eight tokens, four of 32 of 4096 x 1792
+// 70.6 and 64.5; eight tokens, two of eight 16.1 and 13.1; seven tokens whose slots are four blocks 12.5 and 9.7.
+template <int FMT>
 bool by_dot_products(const MoeArgs &a) {
     const int blocks = a.top_k * (a.F / 32);
-    return a.K <= 4096 && blocks >= 64 && blocks <= 512 &&
-           ((a.M <= 4 && a.pairs <= a.E) || (a.M <= 8 && 8 * a.pairs <= 5 * a.E));
+    if (a.M > 8 || a.pairs > a.E || a.K > 4096 || blocks < 64 || blocks > 512) return false;
+    return a.M <= 3 || 8 * a.pairs <= 5 * a.E || (a.K <= 2048 && (a.M == 4 || FMT == NVQ_FMT_MXFP4));
 }
 
 template <int FMT>
@@ -650,7 +652,7 @@ int launch_experts_dot(const MoeArgs &a, hipStream_t st) {
 
 template <int FMT>
 int launch_experts(const MoeArgs &a, hipStream_t st) {
-    if (by_dot_products(a)) return launch_experts_dot<FMT>(a, st);
+    if (by_dot_products<FMT>(a)) return launch_experts_dot<FMT>(a, st);
     if (a.pairs <= 64 && a.M <= 16) return launch_experts<FMT, 1, true>(a, st);
     // Two token tiles at once where most experts have more than 16 tokens: 16 experts of 4096 x 1792 microscaled, 16 tokens each on
     // the average, 90 us against 101; with twelve 78 against 65.

@@ -173,7 +173,7 @@ EXPERTS = [(1, 1, 1, 32, 32), (1, 2, 2, 64, 96), (1, 64, 8, 512, 256), (2, 4, 3,
            (16, 64, 4, 4096, 32), (32, 16, 8, 4096, 288), (32, 8, 5, 4128, 288), (29, 2, 2, 160, 800), (32, 64, 2, 4096, 96), (9, 6, 6, 4160, 1056), (4, 70, 16, 2048, 160),
            # a few tokens by dot products: one block to a lane and two, in both launches, lanes without
            (1, 8, 2, 4096, 1792), (7, 40, 3, 1440, 992), (4, 8, 2, 2080, 1056), (2, 64, 8, 1056, 2048), (3, 16, 2, 768, 2048), (1, 1, 1, 96, 2048),
-           (8, 64, 5, 160, 448), (1, 20, 16, 32, 1024), (4, 4, 1, 64, 16384), (1, 8, 2, 4128, 1792),
+           (8, 64, 5, 160, 448), (8, 64, 8, 160, 416), (4, 16, 4, 96, 512), (3, 8, 2, 4096, 1056), (1, 20, 16, 32, 1024), (4, 4, 1, 64, 16384), (1, 8, 2, 4128, 1792),
            # the first one with the activations in registers: a short last wave, 128 inputs to a lane-row in all
            (7, 8, 4, 2080, 4096), (3, 3, 3, 4096, 11008)]
 
