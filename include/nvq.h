@@ -567,8 +567,8 @@ int nvq_gemm_mxfp4(const uint8_t *qweight, const uint8_t *scales, int64_t N, int
  * sums); ids[m][0 .. top_k) = the experts of the top_k largest logits, in
  * descending order, the lowest index first among equal ones; weights[m][s] =
  * exp(logit of ids[m][s]) / sum of exp(logit) over the chosen experts (renormalise =
- * 1) or over all E (renormalise = 0).  A NaN logit counts as the smallest; the ids of
- * a token are distinct and in [0, E) whatever the inputs.
+ * 1) or over all E (renormalise = 0).  A NaN logit counts as the smallest and adds nothing
+ * to the sum over all E; the ids of a token are distinct and in [0, E) whatever the inputs.
  *   x_bf16 [M][K], router_bf16 [E][K], 16-byte aligned; ids, weights [M][top_k]
  * K % 32 == 0, K <= NVQ_MAX_K, 1 <= E <= NVQ_MOE_MAX_EXPERTS, 1 <= top_k <= E and
  * NVQ_MOE_MAX_TOP_K.  Where a chosen logit is infinite or NaN so may the token's weights be NaN.

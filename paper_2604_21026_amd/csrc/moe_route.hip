@@ -27,8 +27,9 @@ struct RouteArgs {
 };
 
 // Logits as words whose unsigned order is theirs; equal numbers (both zeros) give equal words, NaN the lowest.
+constexpr uint32_t kNanWord = 1u;
 __device__ __forceinline__ uint32_t order_word(float f) {
-    if (f != f) return 1u;
+    if (f != f) return kNanWord;
     const uint32_t u = __float_as_uint(f + 0.0f);
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
@@ -102,8 +103,9 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int m) {
         if (k == 0) {
             top = value;
             if (!a.renormalise) {
+                // (experts past the last have words of zero; a NaN, the smallest, adds nothing)
 #pragma unroll
-                for (int j = 0; j < P; ++j) all += L * j + i < a.E ? expf(of_order_word(key[j]) - top) : 0.0f;
+                for (int j = 0; j < P; ++j) all += key[j] > kNanWord ? expf(of_order_word(key[j]) - top) : 0.0f;
                 all = over_group<L>(all, AddOp());
             }
         }

@@ -466,3 +466,42 @@ def test_two_streams_at_once_and_replays(M):
             got = [t.clone() for t in (*side[6], side[7]["y"], side[7]["z"])]
             layer(side)
             assert all(torch.equal(a, b) for a, b in zip(got, (*side[6], side[7]["y"], side[7]["z"])))
+
+
+# ---- logits that are no number ----
+@gpu
+@pytest.mark.parametrize("M,E,k", [(5, 20, 6), (1, 64, 8), (32, 130, 4), (3, 300, 2)])
+def test_route_over_all_experts_leaves_out_logits_that_are_no_number(M, E, k):
+    """A NaN logit counts as the smallest: of an expert that was not chosen it does not reach the weights."""
+    g = torch.Generator().manual_seed(E)
+    x, r = torch.randn((M, 64), generator=g).bfloat16(), torch.randn((E, 64), generator=g).bfloat16()
+    r[7, 5] = r[E - 1, 63] = float("nan")
+    logits = f64(x) @ f64(r).T
+    logits[:, [7, E - 1]] = -np.inf
+    d = 2 * (64 + 40) * np_mx.EPS32 * (np.abs(f64(x)) @ np.abs(np.nan_to_num(f64(r))).T).max(1)  # two logits' error
+    for renorm in (True, False):
+        ids, w = nvq.moe_route(x.to(DEV), r.to(DEV), k, renorm)
+        got = ids.cpu().numpy()
+        assert not np.isin(got, [7, E - 1]).any() and all(len(set(row)) == k for row in got.tolist())
+        top = logits.max(1, keepdims=True)
+        p = np.exp(np.take_along_axis(logits, got, 1) - top)
+        p /= (p if renorm else np.exp(logits - top)).sum(1, keepdims=True)
+        # as test_route_of_exact_logits_with_ties: the exponentials, their arguments (here up to 512 units), the sum
+        assert (np.abs(f64(w) - p) <= p * (2 * d[:, None] + 2 * (4 + 512 + E / 64 + 22) * np_mx.EPS32)).all()
+
+
+@gpu
+@pytest.mark.parametrize("renorm", [True, False])
+def test_route_of_fewer_numbers_than_choices(renorm):
+    """Every number comes before what is none; ids stay distinct and in range."""
+    r = torch.zeros((9, 32)).bfloat16()
+    r[:, 0] = torch.tensor([float("nan"), 1, float("nan"), 3, float("-inf"), float("nan"), 2, float("nan"), float("nan")])
+    x = torch.zeros((2, 32)).bfloat16()
+    x[:, 0] = torch.tensor([1.0, 2.0])
+    ids, w = nvq.moe_route(x.to(DEV), r.to(DEV), 6, renorm)
+    assert ids.cpu().tolist() == [[3, 6, 1, 4, 0, 2]] * 2
+    if not renorm:
+        p = np.exp(np.array([[3.0, 2, 1, -np.inf], [6.0, 4, 2, -np.inf]]))
+        p /= p.sum(1, keepdims=True)
+        assert (np.abs(f64(w)[:, :4] - p) <= p * (2 * (4 + 8 + 22) * np_mx.EPS32)).all()
+        assert bool(torch.isnan(w[:, 4:]).all())
