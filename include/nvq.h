@@ -548,7 +548,8 @@ int nvq_dequant_mxfp4(const uint8_t *q, const uint8_t *scales, int64_t M, int64_
  * instructions, sums in fp32.
  *   xq [M][K/2], xscale [M][K/32]
  * K % 32 == 0, K <= NVQ_MAX_K; N <= 2^29 for the first, N, M <= 2^30 for the second.  A
- * weight or activation block of byte 255 makes every result that it enters NaN.  A
+ * weight or activation block of byte 255 makes every result that it enters NaN; an infinite
+ * or NaN x of the first counts as in the plain sum, in its own token's results alone.  A
  * result does not depend on the values of other rows and tokens; the order in which its
  * products are added does depend on M, N and K (and not on timing: the same call gives the
  * same bits).  y may not overlap an input.
@@ -594,7 +595,8 @@ int nvq_moe_route(const uint16_t *x_bf16, const uint16_t *router_bf16, int M, in
  * A slot whose id is outside [0, E) is not used (padding: a token without any used slot
  * gets zeros); the weights of an expert that stands in several slots of one token add up.
  * A token's result does not change by a value of another token or of an expert that it
- * did not choose.
+ * did not choose.  An infinite x or h counts as in the plain sum with NVQ_FMT_MXFP4; with
+ * NVQ_FMT_INT4, whose products subtract an offset, it makes the results that it enters NaN.
  *   gate_up  [E][2 F][K/2] codes, rows 0 .. F-1 of an expert the gate G_e, F .. 2 F - 1
  *            U_e; gate_up_scales [E][2 F][K/32]
  *   down     [E][K][F/2] codes, down_scales [E][K][F/32]

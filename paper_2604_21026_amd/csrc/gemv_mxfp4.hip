@@ -217,7 +217,7 @@ __global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const ui
         for (int k = 0; k < kMine; ++k) xs[buf][tid + k * kThreads] = v[k];
     };
     auto weights = [&](Codes<C> (&w)[R], Scales<NVQ_FMT_MXFP4, C> (&sc)[R], int turn) {
-        const int pass = turn * S + s;  // (uniform; past the end: the last one, with codes of zero)
+        const int pass = turn * S + s;  // (uniform; past the end: the last one, for nothing)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             const int c = (pass < passes ? pass : passes - 1) * C;
@@ -239,16 +239,18 @@ __global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const ui
         weights(w[0], sc[0], 0);
         keep(xr, 0);
         ask(xr, 1);
-        auto one = [&](int d, int turn) {
+        auto arrive = [&]() {
             asm volatile("" ::: "memory");
             __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's pieces are in LDS
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
+        };
+        auto one = [&](int d, int turn) {
+            arrive();
             keep(xr, (turn + 1) & 1);
             ask(xr, turn + 2);
             weights(w[d ^ 1], sc[d ^ 1], turn + 1);
             __builtin_amdgcn_sched_barrier(0);
-            const bool mine = turn * S + s < passes;  // (uniform)
             const uint4v *const xb = &xs[turn & 1][s * (16 * T * kPieces)];
 #pragma unroll
             for (int b = 0; b < C; ++b) {
@@ -258,19 +260,17 @@ __global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const ui
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         a[t][i] = __builtin_bit_cast(bf16x8, xb[(16 * t + n) * kPieces + ((16 * b + 4 * kb + i) ^ swapped(n))]);
-                if (S > 1 && !mine) {
-#pragma unroll
-                    for (int r = 0; r < R; ++r) w[d][r].w[b] = uint4v{0, 0, 0, 0};
-                }
                 multiply_column<NVQ_FMT_MXFP4, R, T, C, C>(w[d], b, sc[d], b, a, sum);
             }
         };
         // (the registers of the weights change roles from turn to turn, they are not copied)
-        for (int turn = 0; turn < turns; turn += 2) {
+        const int mine = (passes - s + S - 1) / S;  // (uniform) all turns, or all but the last one
+        for (int turn = 0; turn < mine; turn += 2) {
             one(0, turn);
-            if (turn + 1 >= turns) break;
+            if (turn + 1 >= mine) break;
             one(1, turn + 1);
         }
+        if (mine < turns) arrive();
     }
     const char *xt[T];
 #pragma unroll

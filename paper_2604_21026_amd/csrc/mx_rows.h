@@ -200,9 +200,9 @@ __device__ __forceinline__ void last_columns(const RowAt (&at)[R], const char *c
     }
 }
 
-// Columns that count for nothing: codes of zero, or scales of zero.
-template <int FMT, int R, int C, int Q>
-__device__ __forceinline__ void clear_column(Codes<C> (&col)[R], int b, Scales<FMT, Q> (&sc)[R], int qb) {
+// A column that counts for nothing: codes of zero, or scales of zero, and activations of zero (an infinite one would make them NaN).
+template <int FMT, int R, int T, int C, int Q>
+__device__ __forceinline__ void clear_column(Codes<C> (&col)[R], uint4v (&raw)[C][T][4], int b, Scales<FMT, Q> (&sc)[R], int qb) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         if constexpr (FMT == NVQ_FMT_MXFP4)
@@ -210,17 +210,23 @@ __device__ __forceinline__ void clear_column(Codes<C> (&col)[R], int b, Scales<F
         else
             sc[r].s[2 * qb] = sc[r].s[2 * qb + 1] = 0;
     }
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) raw[b][t][i] = uint4v{0, 0, 0, 0};
 }
 
 // sum[r][t] += R row tiles times T token tiles over K = 32 G inputs, shared out over `step` waves (this one: number `first`)
 // in passes of Q columns: their scales at once, their codes and activations C columns at a time, requested while the C before are
-// multiplied.  A last pass of fewer columns takes the last Q, those that it shares with the one before cleared.  x[t]: the
-// lane's token of tile t (bf16); a product keeps tokens apart, so a lane without one may take any.  (Loading nothing in such
-// lanes was no faster.)  Every lane of the wave calls it.
+// multiplied.  A last pass of fewer columns takes the last Q, and those that it shares with the one before count for nothing: they
+// are left out (kSkip) or cleared.  (Left out in tiles of two steps or two token tiles, the branches cost up to a tenth, 8 tokens of
+// 14336 x 4096 10.0 and 11.0 us; cleared in the others, up to 7 %.)  x[t]: the lane's token of tile t (bf16); a product keeps tokens
+// apart, so a lane without one may take any.  (Loading nothing in such lanes was no faster.)  Every lane of the wave calls it.
 template <int FMT, int R, int T, int C, int Q>
 __device__ __forceinline__ void rows_times_tokens(const RowAt (&at)[R], const char *const (&x)[T], int G, int first,
                                                   int step, float4v (&sum)[R][T]) {
     static_assert(Q % C == 0, "");
+    constexpr bool kSkip = Q == C && T == 1;
     const int kb = (threadIdx.x & 63) >> 4;
     const int full = G >> 2, passes = full >= Q ? (full + Q - 1) / Q : 0;
     auto load = [&](Codes<C> (&col)[R], uint4v (&raw)[C][T][4], int c) {
@@ -246,13 +252,23 @@ __device__ __forceinline__ void rows_times_tokens(const RowAt (&at)[R], const ch
         for (int q = 0; q < Q / C; ++q) {
             if (q + 1 < Q / C) load(col[(q + 1) & 1], raw[(q + 1) & 1], c0 + (q + 1) * C);
             __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int b = 0; b < C; ++b) {
-                if (q * C + b < Q - 1 && q * C + b < again) clear_column<FMT, R, C, Q>(col[q & 1], b, sc, q * C + b);
+            auto one = [&](int b) {
                 bf16x8 a[T][4];
 #pragma unroll
                 for (int t = 0; t < T; ++t) to_operands<FMT>(raw[q & 1][b][t], a[t]);
                 multiply_column<FMT, R, T, C, Q>(col[q & 1], b, sc, q * C + b, a, sum);
+            };
+            if (kSkip && again > 0) {  // (uniform)
+#pragma unroll
+                for (int b = 0; b < C; ++b)
+                    if (b >= again) one(b);
+            } else {
+#pragma unroll
+                for (int b = 0; b < C; ++b) {
+                    if (!kSkip && q * C + b < Q - 1 && q * C + b < again)
+                        clear_column<FMT, R, T, C, Q>(col[q & 1], raw[q & 1], b, sc, q * C + b);
+                    one(b);
+                }
             }
             __builtin_amdgcn_sched_barrier(0);
         }

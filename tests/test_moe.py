@@ -505,3 +505,48 @@ def test_route_of_fewer_numbers_than_choices(renorm):
         p /= p.sum(1, keepdims=True)
         assert (np.abs(f64(w)[:, :4] - p) <= p * (2 * (4 + 8 + 22) * np_mx.EPS32)).all()
         assert bool(torch.isnan(w[:, 4:]).all())
+
+
+# ---- operands that are not finite ----
+def positive(fmt, rows, K, rng):
+    """Weights above zero: their codes, scales and values."""
+    q = rng.integers(0, 256, (rows, K // 2), dtype=np.uint8)
+    if fmt == "int4":
+        q |= 0x88
+        q |= ((q & 0x0f) == 8).astype(np.uint8) | ((q & 0xf0) == 0x80).astype(np.uint8) << 4
+        s = (2.0 ** -rng.integers(8, 11, (rows, K // 32)).astype(np.float64)).astype(np.float16).view(np.int16)
+    else:
+        q &= 0x77
+        q |= ((q & 0x07) == 0).astype(np.uint8) | ((q & 0x70) == 0).astype(np.uint8) << 4
+        s = rng.integers(115, 118, (rows, K // 32), dtype=np.uint8)
+    return q, s
+
+
+NOT_FINITE = [
+    # products of tiles: both launches' last pass meets a column again; in the second one also with several workgroups to a tile, wide tiles
+    (5, 2, 2, 416, 416), (20, 4, 2, 416, 672), (32, 16, 8, 4096, 288), (9, 6, 6, 4160, 1056), (20, 60, 2, 416, 416),
+    # the first launch with the activations in registers, whose last waves' blocks begin before their share
+    (5, 3, 3, 2144, 11008), (22, 4, 1, 2144, 8192),
+    # dot products
+    (1, 8, 4, 160, 544), (2, 20, 4, 2144, 1056)]
+
+
+@gpu
+@pytest.mark.parametrize("M,E,k,K,F", NOT_FINITE)
+def test_experts_of_infinite_activations(M, E, k, K, F):
+    """Microscaled: an infinite activation beside positive weights makes its token's outputs infinite, wherever it stands."""
+    rng = np.random.default_rng(K * F)
+    (q, s), (dq, ds) = positive("mxfp4", E * 2 * F, K, rng), positive("mxfp4", E * K, F, rng)
+    ex = nvq.Experts(dev(q.reshape(E, 2 * F, K // 2)), dev(s.reshape(E, 2 * F, K // 32)), dev(dq.reshape(E, K, F // 2)),
+                     dev(ds.reshape(E, K, F // 32)))
+    x = rng.integers(1, 4, (M, K)).astype(np.float32) / 64
+    ids = np.stack([rng.permutation(E)[:k] for _ in range(M)]).astype(np.int32)
+    w = dev(rng.random((M, k)).astype(np.float32) + 0.1)
+    plain = nvq.moe_experts(ex, dev(x).bfloat16(), dev(ids), w, out_dtype=torch.float32)
+    assert bool(torch.isfinite(plain).all())
+    for at in (slice(None), slice(0, 1), slice(K // 2, K // 2 + 1), slice(K - 140, K - 139), slice(K - 1, K)):
+        bad = x.copy()
+        bad[M - 1, at] = np.inf
+        y = nvq.moe_experts(ex, dev(bad).bfloat16(), dev(ids), w, out_dtype=torch.float32)
+        assert bool((y[M - 1] == float("inf")).all()), at
+        assert torch.equal(y[:M - 1], plain[:M - 1])

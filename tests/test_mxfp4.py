@@ -469,3 +469,44 @@ def test_calls_without_ctypes_equal_those_through_it(monkeypatch):
     monkeypatch.setattr(nvq, "_calls", None)
     for a, b in zip(fast, all_calls()):
         assert torch.equal(a, b)
+
+
+# ---- operands that are not finite, at sizes that reach every kernel and whose last pass meets columns a second time ----
+BEYOND = [
+    # dot products: blocks past the end of the row, one wave to a row and four, one token and two
+    (1, 20, 2080), (1, 3000, 2080), (1, 8200, 1056), (1, 20, 4128), (1, 20, 8224), (2, 20, 2080), (2, 20, 4128), (2, 20, 8224),
+    # activations read with the weights: a row tile to a workgroup, four, and one of two token tiles
+    (3, 40, 2176), (5, 8209, 2176), (20, 40, 2176),
+    # all activations in LDS
+    (1, 8209, 16672), (2, 17000, 4128), (3, 8209, 4224),
+    # activations shared through LDS: surplus slices in the last turn, and none
+    (16, 40, 4352), (6, 4100, 1440), (9, 8200, 1376), (20, 40, 4224), (20, 4100, 1440), (20, 8200, 1376), (9, 65539, 4128), (20, 65539, 4128),
+    # activations in registers: a last wave whose blocks begin before its share
+    (3, 65523, 544), (20, 65523, 544), (3, 65523, 2080), (20, 65523, 2080)]
+
+
+def positive_weights(N, K, seed):
+    """Random codes 0.5 .. 6 at scale bytes 121 .. 124, and the rows that a test looks at: the first and last forty."""
+    rng = np.random.default_rng(seed)
+    q = rng.integers(0, 256, (N, K // 2), dtype=np.uint8) & 0x77
+    q |= ((q & 0x07) == 0).astype(np.uint8) | ((q & 0x70) == 0).astype(np.uint8) << 4
+    s = rng.integers(121, 125, (N, K // 32), dtype=np.uint8)
+    return q, s, np.unique(np.concatenate([np.arange(min(N, 40)), np.arange(max(0, N - 40), N)])), rng
+
+
+@gpu
+@pytest.mark.parametrize("M,N,K", BEYOND)
+def test_gemv_of_infinite_activations(M, N, K):
+    """Positive weights: a token of infinities gives infinities in every row, one at the end of another token its sign, and
+    the tokens beside them their exact sums."""
+    q, s, rows, rng = positive_weights(N, K, M + N + K)
+    x = rng.integers(1, 4, (M, K)).astype(np.float64)
+    want = x @ np_mx.dequant(q[rows], s[rows]).T
+    qd, sd = dev(q), dev(s)
+    for what in (np.inf, -np.inf):
+        for at in (slice(None), slice(K - 1, K), slice(K // 2, K // 2 + 1), slice(0, 1), slice(max(0, K - 200), max(0, K - 200) + 1)):
+            bad = x.copy()
+            bad[M - 1, at] = what
+            y = f64(nvq.gemv_mxfp4(qd, sd, dev(bad).bfloat16()))[:, rows]
+            assert (y[M - 1] == what).all(), at
+            assert np.array_equal(y[:M - 1], want[:M - 1])
