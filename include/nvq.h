@@ -539,13 +539,15 @@ int nvq_dequant_mxfp4(const uint8_t *q, const uint8_t *scales, int64_t M, int64_
 /*
  * nvq_gemv_mxfp4 -- y[m][n] = sum_k w[n][k] * x[m][k] for microscaled weights and
  * bf16 activations of 1 <= M <= NVQ_MAX_M tokens; neither is rounded (the
- * counterpart of nvq_gemv_w4a16), sums in fp32.
+ * counterpart of nvq_gemv_w4a16), sums in fp32.  The weights are multiplied as bf16
+ * values, which hold all but those of bytes 253 and 254 beyond 2^128: these count as
+ * infinite, as nvq_dequant_mxfp4 gives them (nvq_quant_mxfp4 writes no byte above 252).
  *   qweight [N][K/2], scales [N][K/32], x_bf16 [M][K], y [M][N] (y_dtype)
  *
  * nvq_gemm_mxfp4 -- the same product with both operands microscaled, for any M
  * (prompts; the activations come from nvq_quant_mxfp4): y[m][n] = sum_k w[n][k] *
  * xv[m][k], xv the values that xq and xscale stand for, on the scaled matrix
- * instructions, sums in fp32.
+ * instructions, sums in fp32 (bytes 253 and 254: the products themselves).
  *   xq [M][K/2], xscale [M][K/32]
  * K % 32 == 0, K <= NVQ_MAX_K; N <= 2^29 for the first, N, M <= 2^30 for the second.  A
  * weight or activation block of byte 255 makes every result that it enters NaN; an infinite
@@ -601,7 +603,7 @@ int nvq_moe_route(const uint16_t *x_bf16, const uint16_t *router_bf16, int M, in
  *            U_e; gate_up_scales [E][2 F][K/32]
  *   down     [E][K][F/2] codes, down_scales [E][K][F/32]
  *   format   NVQ_FMT_INT4: as nvq_pack_int4 writes them, scales fp16 bits;
- *            NVQ_FMT_MXFP4: as nvq_quant_mxfp4 writes them
+ *            NVQ_FMT_MXFP4: as nvq_quant_mxfp4 writes them (bytes 253 to 255 as in nvq_gemv_mxfp4)
  *   x_bf16 [M][K], ids, weights [M][top_k], y [M][K] (y_dtype); K % 32 == 0, F % 32 == 0,
  *   both <= NVQ_MAX_K, 1 <= E <= NVQ_MOE_MAX_EXPERTS, 1 <= top_k <= NVQ_MOE_MAX_TOP_K
  *   workspace  nvq_moe_workspace_bytes(...) bytes, 256-byte aligned, scratch (whatever it

@@ -87,7 +87,7 @@ __global__ __launch_bounds__(256) void gemv_mxfp4_dot_kernel(const uint8_t *__re
             const int64_t row = group * R + r < N ? group * R + r : N - 1;
 #pragma unroll
             for (int b = 0; b < B; ++b) {
-                const int block = l0 + 64 * b < G ? l0 + 64 * b : G - 1;  // (past the end: activations of zero)
+                const int block = l0 + 64 * b < G ? l0 + 64 * b : G - 1;
                 c[d][r][b] = load_stream(reinterpret_cast<const uint4 *>(q) + row * G + block);
                 sc[d][r][b] = as_global<uint8_t>(scales)[row * G + block];
             }
@@ -104,6 +104,12 @@ __global__ __launch_bounds__(256) void gemv_mxfp4_dot_kernel(const uint8_t *__re
                 xr[m][b][i] = uint4v{0, 0, 0, 0};
                 if (l0 + 64 * b < G) xr[m][b][i] = as_global<uint4v>(x)[((int64_t)m * G + l0 + 64 * b) * 4 + i];
             }
+    // Scales become exponents (the conversions look at nothing else); past the end, where activations are zero, the smallest one, since
+    // values beyond bf16 would make them NaN.  (4096 x 14336 6.4 us for 6.25, others equal; loads or products left out instead cost
+    // up to 10 %.)
+    int up[B];
+#pragma unroll
+    for (int b = 0; b < B; ++b) up[b] = l0 + 64 * b < G ? 23 : 31;
     int turn = 0;
     auto one = [&](int d, int group) {
         float mine = 0.0f;  // lane m R + r: the result of row r, token m
@@ -112,7 +118,7 @@ __global__ __launch_bounds__(256) void gemv_mxfp4_dot_kernel(const uint8_t *__re
             float sum[M] = {};
 #pragma unroll
             for (int b = 0; b < B; ++b) {
-                const float s = __uint_as_float(sc[d][r][b] << 23);  // (the conversions look at the exponent alone)
+                const float s = __uint_as_float(sc[d][r][b] << up[b]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const uint4v v = __builtin_bit_cast(uint4v, mx_values(c[d][r][b][i], s));
@@ -318,7 +324,7 @@ __global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const ui
 // The activations stay in registers: wave w of W keeps those of C columns (4 C blocks of 32 inputs), of all tokens, for the whole
 // kernel, and the workgroup streams its row tiles past them, one after the other, D of them requested ahead.  So nothing but weights and
 // their scales is read in the loop (read again for every tile, one token's activations took 25 of 68 us at 128256 x 4096).  The
-// last wave's blocks may begin earlier than its share, where the activations are zero.
+// last wave's blocks may begin earlier than its share, where activations and scales are zero.
 // Partial tiles are added through LDS in wave order, by waves that change from tile to tile, and wait there (`out`) until kGroup
 // tiles' results leave as runs of 16 kGroup rows: stored tile by tile, 32 bytes here and there among the loads, 32 tokens' took 64
 // us for 56.
@@ -387,6 +393,7 @@ __global__ __launch_bounds__(64 * W) void gemv_mxfp4_resident_kernel(const uint8
         float4v sum[1][T];
 #pragma unroll
         for (int t = 0; t < T; ++t) sum[0][t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        if (b0 < share) clear_scales<NVQ_FMT_MXFP4, C>(sc[d][0], share - b0);  // (uniform)
 #pragma unroll
         for (int b = 0; b < C; ++b) multiply_column<NVQ_FMT_MXFP4, 1, T, C, C>(codes[d], b, sc[d], b, xr[b], sum);
         load(d, it + D);

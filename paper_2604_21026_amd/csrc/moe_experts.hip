@@ -255,6 +255,10 @@ __global__ __launch_bounds__(64 * W) void moe_gate_up_resident_kernel(MoeArgs a)
         }
         auto one = [&](int d, int it) {
             float4v sum[2][1] = {{float4v{0.0f, 0.0f, 0.0f, 0.0f}}, {float4v{0.0f, 0.0f, 0.0f, 0.0f}}};
+            if (b0 < share) {  // (uniform)
+                clear_scales<FMT, C>(sc[d][0], share - b0);
+                clear_scales<FMT, C>(sc[d][1], share - b0);
+            }
 #pragma unroll
             for (int b = 0; b < C; ++b) multiply_column<FMT, 2, 1, C, C>(codes[d], b, sc[d], b, x[b], sum);
             load(d, it + D);

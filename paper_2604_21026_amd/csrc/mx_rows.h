@@ -65,6 +65,17 @@ __device__ __forceinline__ void load_scales(Scales<FMT, Q> &c, const RowAt &at, 
     }
 }
 
+// Scales of zero for the first `blocks` blocks (uniform), whose activations are zero: values beyond bf16 would make them NaN.
+template <int FMT, int Q>
+__device__ __forceinline__ void clear_scales(Scales<FMT, Q> &c, int blocks) {
+    constexpr int kWords = FMT == NVQ_FMT_MXFP4 ? Q : 2 * Q;
+#pragma unroll
+    for (int k = 0; k < kWords; ++k) {
+        const int bytes = blocks * scale_bytes<FMT>() - 4 * k;
+        c.s[k] &= bytes <= 0 ? ~0u : bytes >= 4 ? 0u : ~0u << (8 * bytes);
+    }
+}
+
 // Column col, with `blocks` (1 to 4) of its four blocks in the row: the others are zero.
 template <int FMT>
 __device__ __forceinline__ void load_last(Codes<1> &c, Scales<FMT, 1> &sc, const RowAt &at, int col, int kb, int blocks) {

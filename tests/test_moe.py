@@ -550,3 +550,47 @@ def test_experts_of_infinite_activations(M, E, k, K, F):
         y = nvq.moe_experts(ex, dev(bad).bfloat16(), dev(ids), w, out_dtype=torch.float32)
         assert bool((y[M - 1] == float("inf")).all()), at
         assert torch.equal(y[:M - 1], plain[:M - 1])
+
+
+@gpu
+@pytest.mark.parametrize("M,E,k,K,F", NOT_FINITE)
+@pytest.mark.parametrize("fmt", ["int4", "mxfp4"])
+def test_experts_with_weights_beyond_the_range(fmt, M, E, k, K, F):
+    """Positive weights and activations: an infinite scale (int4) or values beyond bf16 (scale byte 253) make what they enter
+    infinite, not NaN, wherever in a row the block lies (int4: an infinite h makes its outputs NaN); a scale that is no number
+    makes it NaN."""
+    rng = np.random.default_rng(K + F)
+    up, down = positive(fmt, E * 2 * F, K, rng), positive(fmt, E * K, F, rng)
+    inf, nan = (0x7c00, 0x7e00) if fmt == "int4" else (253, 255)
+    x = dev(rng.integers(1, 4, (M, K)).astype(np.float32) / 64).bfloat16()
+    ids = np.stack([rng.permutation(E)[:k] for _ in range(M)]).astype(np.int32)
+    w = dev(rng.random((M, k)).astype(np.float32) + 0.1)
+    met = np.isin(ids, [E - 1]).any(1)
+    ids[~met, 0] = E - 1  # (every token has the last expert)
+
+    def y_of(rows, at, byte, which):
+        parts = []
+        for (q, s), n, cols, mine in ((up, 2 * F, K, which == "up"), (down, K, F, which == "down")):
+            q, s = q.reshape(E, n, cols // 2), s.reshape(E, n, cols // 32)
+            if mine:
+                q, s = q.copy(), s.copy()
+                for r in rows:
+                    s[E - 1, r, at] = byte
+                    q[E - 1, r, 16 * at:16 * at + 16] = 0xff if fmt == "int4" else 0x77
+            parts += [dev(q), dev(s)]
+        return nvq.moe_experts(nvq.Experts(*parts), x, dev(ids), w, out_dtype=torch.float32)
+
+    plain = y_of([], 0, 0, "")
+    assert bool(torch.isfinite(plain).all())
+    for at in {0, K // 64, K // 32 - 5, K // 32 - 1}:
+        # one gate row, or one up row: h is infinite there, and so are all outputs
+        for row in (5, F - 1, F, 2 * F - 3):
+            y = y_of([row], at, inf, "up")
+            assert bool((torch.isnan(y) if fmt == "int4" else y == float("inf")).all()), (at, row)
+        assert bool(torch.isnan(y_of([F + 1], at, nan, "up")).all())
+    for at in {0, F // 64, F // 32 - 1}:
+        y = y_of([0, 7, K - 1], at, inf, "down")
+        assert bool((y[:, [0, 7, K - 1]] == float("inf")).all()), at
+        others = [i for i in range(K) if i not in (0, 7, K - 1)]
+        assert torch.equal(y[:, others], plain[:, others])
+        assert bool(torch.isnan(y_of([7], at, nan, "down")[:, 7]).all())

@@ -510,3 +510,48 @@ def test_gemv_of_infinite_activations(M, N, K):
             y = f64(nvq.gemv_mxfp4(qd, sd, dev(bad).bfloat16()))[:, rows]
             assert (y[M - 1] == what).all(), at
             assert np.array_equal(y[:M - 1], want[:M - 1])
+
+
+@gpu
+@pytest.mark.parametrize("M,N,K", BEYOND)
+def test_gemv_of_weights_at_and_beyond_the_last_scales(M, N, K):
+    """Scale bytes 253 and 254: values that bf16 holds are themselves, those beyond it infinite (as dequant_mxfp4 gives them);
+    byte 255: no number.  Each in the first, the last or every block of a row."""
+    q, s, rows, rng = positive_weights(N, K, M + N + K)
+    last = N - 1
+    s[3], q[3] = 254, 0x77                              # 6 * 2^127, every block
+    s[5, -1], q[5, -16:] = 253, 0x77                    # 6 * 2^126, the last block
+    s[6, 0], q[6, :16] = 254, 0x44                      # 2 * 2^127, the first block
+    q[7], s[7, -1], q[7, -16:] = 0, 254, 0x21           # 0.5 and 1 times 2^127, the last block of a row of zeros
+    q[8], s[8, 0], q[8, :16] = 0, 253, 0x53             # 1.5 and 3 times 2^126, the first one
+    s[9, -1] = 255
+    s[10, 0], q[10, :16] = 255, 0
+    s[last, -1], q[last, -16:] = 253, 0xff              # -6 * 2^126, the last block of the last row
+    x = rng.integers(1, 4, (M, K)) * 2.0 ** -30
+    w = np_mx.dequant(q[rows], s[rows])
+    w[np.abs(w) >= 2.0 ** 128] = np.inf * np.sign(w[np.abs(w) >= 2.0 ** 128])
+    assert np.isinf(w[[3, 5, 6, -1]]).any(1).all() and np.isfinite(w[[7, 8]]).all()
+    with np.errstate(invalid="ignore"):
+        want = x @ np.nan_to_num(w, posinf=0.0, neginf=0.0).T
+    want[:, [3, 5, 6]], want[:, [9, 10]], want[:, -1] = np.inf, np.nan, -np.inf
+    y = f64(nvq.gemv_mxfp4(dev(q), dev(s), dev(x).bfloat16()))[:, rows]
+    assert np.array_equal(y, want, equal_nan=True)
+
+
+@gpu
+@pytest.mark.parametrize("M,N,K", [(3, 20, 96), (40, 70, 288), (12, 40, 2080), (90, 370, 1056), (300, 300, 544), (700, 9000, 544),
+                                   (3585, 4001, 544)])
+def test_gemm_of_the_last_scales(M, N, K):
+    """Scale bytes 253 and 254 on either side, small values on the other: the product itself, also of values beyond bf16."""
+    rng = np.random.default_rng(M + K)
+    q, s = np_mx.random_mx(rng, N, K)
+    xq, xs = np_mx.random_mx(rng, M, K, 1, 96)
+    # blocks of 253 and 254 alone in their rows: sums of whole multiples of 2^94 * 2^-32, below 2^24 of them
+    for r, (at, byte) in enumerate(((-1, 254), (0, 253), (K // 64, 254))):
+        q[r], s[r, at] = 0, byte
+        q[r, 16 * (at % (K // 32)):16 * (at % (K // 32)) + 16] = rng.integers(0, 256, 16, dtype=np.uint8)
+    want = np_mx.dequant(xq, xs) @ np_mx.dequant(q, s).T
+    y = f64(nvq.gemm_mxfp4(dev(q), dev(s), dev(xq), dev(xs)))
+    assert np.array_equal(y + 0.0, want.astype(np.float32).astype(np.float64) + 0.0)
+    y = f64(nvq.gemm_mxfp4(dev(xq), dev(xs), dev(q), dev(s)))
+    assert np.array_equal(y + 0.0, want.T.astype(np.float32).astype(np.float64) + 0.0)
