@@ -459,7 +459,7 @@ __global__ __launch_bounds__(64 * W, 4) void gemv_mxfp4_lds_kernel(const uint8_t
         typedef uint4v uint4v_any __attribute__((aligned(1)));
         sc[d] = *(const __attribute__((address_space(1))) uint4v_any *)(at.s + (4 * c0 < G - 16 ? 4 * c0 : G - 16));
     };
-    // (the loads' place runs ahead of the products')
+    // (the loads' place runs ahead of the products'; a workgroup has two items or more, of two tiles or of one tile's parts)
     const int items = ((tiles - 1 - (int)blockIdx.x) / (int)gridDim.x + 1) * per;
     int lt = blockIdx.x, lp = 0;
     auto ahead = [&](int d) {
@@ -470,7 +470,7 @@ __global__ __launch_bounds__(64 * W, 4) void gemv_mxfp4_lds_kernel(const uint8_t
         }
     };
     ahead(0);
-    if (items > 1) ahead(1);
+    ahead(1);
     for (int i = threadIdx.x; i < M * (cols + 1) * 16; i += 64 * W) {
         const int m = i / ((cols + 1) * 16), p = i - m * (cols + 1) * 16;
         uint4v v = {0, 0, 0, 0};
@@ -547,7 +547,7 @@ __global__ __launch_bounds__(64 * W, 4) void gemv_mxfp4_lds_kernel(const uint8_t
         one(0, false);
     } else {
         one(0, false);
-        if (left == 2) one(1, false);
+        one(1, false);
     }
 }
 
@@ -649,10 +649,11 @@ extern "C" int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
         if (a.G <= 64) return M <= 16 ? gemv_resident<1, 2>(a, cus, st) : gemv_resident<2, 2>(a, cus, st);
         return M <= 16 ? gemv_resident<1, 4>(a, cus, st) : gemv_resident<2, 4>(a, cus, st);
     }
-    // Up to three tokens, many row tiles, or several and more K than the waves take at once, or K in whole steps of them (4096 inputs):
-    // (3, 18830, 6624) 16.9 us against 25.1 of what follows; of one token (28672, 4096) 12.0 against 13.5, (10240, 8192) 11.9 against
-    // 13.6, (2048, 8192) 5.4 against 6.2; not (14336, 4096) 8.5 against 8.3, (4096, 14336) 9.6 against 9.2; nor (4, 14336, 4096) 9.8
-    // against 8.8, (8, 8192, 2048) 5.9 against 4.9.
+    // Up to three tokens, many row tiles, or several and more K than the waves take at once, or K in whole steps of them (4096 inputs).
+    // us against what follows, of three tokens (18830, 6624) 16.6 and 24.3, (28672, 4096) 13.3 and 14.1, (10240, 8192) 12.4 and
+    // 14.2, (8209, 4224) 7.8 and 9.6, (2048, 8192) 6.1 and 6.6, (33000, 2080) 11.0 and 11.4; of two (28672, 4096) 12.3 and 13.8; of one
+    // (8209, 16672) 19.4 and 27.2, (4096, 24576) 12.4 and 14.4; not of three (4096, 9152) 7.3 and 7.0, of four (14336, 4096) 9.8
+    // and 8.8.
     if (M <= kLdsTokens && a.G > 64 && M * lds_pitch(a.G) <= kLdsBytes &&
         (tiles >= 4 * cus || (a.G > 128 && (tiles > 2 * cus || a.G % 128 == 0))))
         return gemv_lds(a, (int)(tiles < 2 * cus ? tiles : 2 * cus), st);

@@ -555,3 +555,17 @@ def test_gemm_of_the_last_scales(M, N, K):
     assert np.array_equal(y + 0.0, want.astype(np.float32).astype(np.float64) + 0.0)
     y = f64(nvq.gemm_mxfp4(dev(xq), dev(xs), dev(q), dev(s)))
     assert np.array_equal(y + 0.0, want.T.astype(np.float32).astype(np.float64) + 0.0)
+
+
+# all activations of a few tokens in LDS: one token of more inputs than dot products take (three to seven steps to a row tile, the largest
+# K that fits), two and three tokens; many row tiles and few
+@gpu
+@pytest.mark.parametrize("M,N,K", [(1, 40, 20480), (1, 17, 24576), (1, 8209, 16672), (1, 8200, 28416),
+                                   (2, 17000, 4128), (2, 16400, 2112), (2, 16500, 8224),
+                                   (3, 8193, 4128), (3, 8209, 9152), (3, 40, 8192), (3, 33000, 2080)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gemv_exact_sums_of_activations_in_lds(M, N, K, dtype):
+    q, s, x, _, xv = exact_case(M, N, K, M + N + K, False)
+    want = xv @ np_mx.dequant(q, s).T
+    y = nvq.gemv_mxfp4(dev(q), dev(s), dev(x).bfloat16(), out_dtype=dtype)
+    assert bits_equal(f64(y) + 0.0, f64(torch.from_numpy(want).float().to(dtype)) + 0.0)
