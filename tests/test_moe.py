@@ -594,3 +594,29 @@ def test_experts_with_weights_beyond_the_range(fmt, M, E, k, K, F):
         others = [i for i in range(K) if i not in (0, 7, K - 1)]
         assert torch.equal(y[:, others], plain[:, others])
         assert bool(torch.isnan(y_of([7], at, nan, "down")[:, 7]).all())
+
+
+# ---- the general lookup of tokens (more than 16 tokens or 64 pairs) where the first launch's grid is pairs, not experts ----
+@gpu
+@pytest.mark.parametrize("M,E,k,K,F", [(20, 100, 3, 160, 96), (32, 300, 8, 96, 64), (17, 40, 2, 128, 64), (32, 512, 15, 64, 96), (25, 130, 5, 288, 32),
+                                       (9, 160, 16, 96, 32)])
+@pytest.mark.parametrize("fmt", ["int4", "mxfp4"])
+def test_many_tokens_of_more_experts_than_pairs(M, E, k, K, F, fmt):
+    """Few experts of many, shared by tokens in different groups of 64 pairs; slots out of range, an expert twice, tokens without any; a
+    workspace of NaN."""
+    assert M * k < E and (M > 16 or M * k > 64)
+    rng = np.random.default_rng(E)
+    ex, values = make(fmt, E, K, F, E)
+    x = torch.randn((M, K), generator=torch.Generator().manual_seed(M)).bfloat16().to(DEV)
+    for pool in (E, 3, 1, 40):
+        # (E: hardly any shared; 1: one expert for all, in every slot)
+        ids = rng.permutation(E)[:pool][rng.integers(0, pool, (M, k))].astype(np.int32)
+        w = rng.random((M, k)).astype(np.float32)
+        if pool != 1:
+            ids[3, 0], ids[M - 1, k - 1], ids[M // 2, 0] = -1, E, ids[M // 2, k - 1]
+            ids[5] = -2
+        ws = ex.workspace(M, k)
+        ws.fill_(255)
+        y = nvq.moe_experts(ex, x, dev(ids), dev(w), out_dtype=torch.float32, workspace=ws)
+        check(y, x, values, ids, w)
+        assert torch.equal(y, nvq.moe_experts(ex, x, dev(ids), dev(w), out_dtype=torch.float32, workspace=ws))
