@@ -3,10 +3,10 @@
 // token: 6.4 us a call, of which the launch takes 3.6 and the kernel 2.7).
 //
 // Only the ordinary case is served here: tensors (no subclasses, which may say themselves where their
-// data is) of the expected types on the current device, contiguous, with fitting shapes and room for what is
-// written and read.  For everything else a function returns None and the caller takes its own way, which
-// names what is wrong.  The library's entry points are handed over by address (bind); a call returns their
-// status.
+// data is) of the expected types on a device (the microscaled products, the router and the experts: on the
+// current one), contiguous, with fitting shapes and room for what is written and read.  For everything else a
+// function returns None and the caller takes its own way, which names what is wrong.  The library's entry
+// points are handed over by address (bind); a call returns their status.
 #include <Python.h>
 
 #include <c10/hip/HIPFunctions.h>
@@ -29,30 +29,40 @@ decltype(&nvq_gemm_mxfp4) g_gemm_mxfp4;
 decltype(&nvq_moe_route) g_moe_route;
 decltype(&nvq_moe_experts) g_moe_experts;
 
-// A contiguous tensor of that type on the current device; dims < 0: any shape.
-const at::Tensor *device_tensor(PyObject *o, at::ScalarType type, int64_t dims) {
+constexpr int kAny = -1, kNone = -2;  // for a device's number: any, one that no tensor is on
+
+// A contiguous tensor of that type on device `device`; dims < 0: any shape.
+const at::Tensor *device_tensor(PyObject *o, at::ScalarType type, int64_t dims, int device = kAny) {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
     if (!t.defined() || !t.is_cuda() || t.scalar_type() != type || !t.is_contiguous()) return nullptr;
     if (dims >= 0 && t.dim() != dims) return nullptr;
-    if (t.get_device() != c10::hip::current_device()) return nullptr;
+    if (device != kAny && t.get_device() != device) return nullptr;
     return &t;
 }
 
 // The same with room for n values.
-const at::Tensor *device_room(PyObject *o, at::ScalarType type, int64_t n) {
-    const at::Tensor *const t = device_tensor(o, type, -1);
+const at::Tensor *device_room(PyObject *o, at::ScalarType type, int64_t n, int device = kAny) {
+    const at::Tensor *const t = device_tensor(o, type, -1, device);
     return t && t->numel() >= n ? t : nullptr;
 }
 
 // The output of a product (n results), and its type for the library.
-const at::Tensor *output_tensor(PyObject *o, int64_t n, int *y_dtype) {
-    if (const at::Tensor *t = device_room(o, at::kFloat, n)) {
+const at::Tensor *output_tensor(PyObject *o, int64_t n, int *y_dtype, int device = kAny) {
+    if (const at::Tensor *t = device_room(o, at::kFloat, n, device)) {
         *y_dtype = NVQ_F32;
         return t;
     }
     *y_dtype = NVQ_BF16;
-    return device_room(o, at::kBFloat16, n);
+    return device_room(o, at::kBFloat16, n, device);
+}
+
+// The number of the current device, if that tensor is on it, or kNone.  (Asked for once a call: 60 ns.)
+int device_of(PyObject *o) {
+    if (!THPVariable_CheckExact(o)) return kNone;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.defined() || !t.is_cuda()) return kNone;
+    return t.get_device() == c10::hip::current_device() ? t.get_device() : kNone;
 }
 
 struct Weights {
@@ -173,8 +183,8 @@ struct Scaled {
     const uint8_t *q, *s;
     int64_t rows, K;
 };
-bool scaled(PyObject *codes, PyObject *scales, Scaled *w) {
-    const at::Tensor *q = device_tensor(codes, at::kByte, 2), *s = device_tensor(scales, at::kByte, 2);
+bool scaled(PyObject *codes, PyObject *scales, int device, Scaled *w) {
+    const at::Tensor *q = device_tensor(codes, at::kByte, 2, device), *s = device_tensor(scales, at::kByte, 2, device);
     if (!q || !s) return false;
     w->rows = q->size(0);
     w->K = q->size(1) * 2;
@@ -188,15 +198,17 @@ bool scaled(PyObject *codes, PyObject *scales, Scaled *w) {
 PyObject *quant_mxfp4(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     if (n != 3) return none();
+    const int here = device_of(a[0]);
     int dtype = NVQ_BF16;
-    const at::Tensor *x = device_tensor(a[0], at::kBFloat16, 2);
+    const at::Tensor *x = device_tensor(a[0], at::kBFloat16, 2, here);
     if (!x) {
         dtype = NVQ_F32;
-        x = device_tensor(a[0], at::kFloat, 2);
+        x = device_tensor(a[0], at::kFloat, 2, here);
     }
     if (!x || x->size(0) > INT32_MAX || x->size(1) > INT32_MAX) return none();
     const int64_t M = x->size(0), K = x->size(1);
-    const at::Tensor *const q = device_room(a[1], at::kByte, M * (K / 2)), *const s = device_room(a[2], at::kByte, M * (K / 32));
+    const at::Tensor *const q = device_room(a[1], at::kByte, M * (K / 2), here),
+                     *const s = device_room(a[2], at::kByte, M * (K / 32), here);
     if (!q || !s) return none();
     const void *const xp = x->data_ptr();
     uint8_t *const qp = static_cast<uint8_t *>(q->data_ptr()), *const sp = static_cast<uint8_t *>(s->data_ptr());
@@ -208,9 +220,11 @@ PyObject *quant_mxfp4(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // (q, scales, out)
 PyObject *dequant_mxfp4(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
+    if (n != 3) return none();
+    const int here = device_of(a[0]);
     Scaled w;
-    if (n != 3 || !scaled(a[0], a[1], &w)) return none();
-    const at::Tensor *const out = device_tensor(a[2], at::kBFloat16, 2);
+    if (!scaled(a[0], a[1], here, &w)) return none();
+    const at::Tensor *const out = device_tensor(a[2], at::kBFloat16, 2, here);
     if (!out || out->size(0) != w.rows || out->size(1) != w.K) return none();
     uint16_t *const p = static_cast<uint16_t *>(out->data_ptr());
     void *const st = current_stream();
@@ -221,13 +235,15 @@ PyObject *dequant_mxfp4(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // (qweight, scales, x, y)
 PyObject *gemv_mxfp4(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
+    if (n != 4) return none();
+    const int here = device_of(a[0]);
     Scaled w;
     int y_dtype;
-    if (n != 4 || !scaled(a[0], a[1], &w)) return none();
-    const at::Tensor *const x = device_tensor(a[2], at::kBFloat16, 2);
+    if (!scaled(a[0], a[1], here, &w)) return none();
+    const at::Tensor *const x = device_tensor(a[2], at::kBFloat16, 2, here);
     if (!x || x->size(1) != w.K || x->size(0) > INT32_MAX) return none();
     const int M = (int)x->size(0);
-    const at::Tensor *const y = output_tensor(a[3], M * w.rows, &y_dtype);
+    const at::Tensor *const y = output_tensor(a[3], M * w.rows, &y_dtype, here);
     if (!y) return none();
     const uint16_t *const xp = static_cast<const uint16_t *>(x->data_ptr());
     void *const yp = y->data_ptr(), *const st = current_stream();
@@ -238,10 +254,12 @@ PyObject *gemv_mxfp4(PyObject *, PyObject *const *a, Py_ssize_t n) {
 // (qweight, scales, xq, xscale, y)
 PyObject *gemm_mxfp4(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
+    if (n != 5) return none();
+    const int here = device_of(a[0]);
     Scaled w, x;
     int y_dtype;
-    if (n != 5 || !scaled(a[0], a[1], &w) || !scaled(a[2], a[3], &x) || x.K != w.K) return none();
-    const at::Tensor *const y = output_tensor(a[4], x.rows * w.rows, &y_dtype);
+    if (!scaled(a[0], a[1], here, &w) || !scaled(a[2], a[3], here, &x) || x.K != w.K) return none();
+    const at::Tensor *const y = output_tensor(a[4], x.rows * w.rows, &y_dtype, here);
     if (!y) return none();
     void *const yp = y->data_ptr(), *const st = current_stream();
     return status_of([&] { return g_gemm_mxfp4(w.q, w.s, w.rows, w.K, x.q, x.s, x.rows, yp, y_dtype, st); });
@@ -253,15 +271,18 @@ PyObject *moe_route(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     int top_k, renormalise;
     if (n != 7 || !small_int(a[2], &top_k) || !small_int(a[3], &renormalise) || top_k < 1) return none();
-    const at::Tensor *const x = device_tensor(a[0], at::kBFloat16, 2), *const r = device_tensor(a[1], at::kBFloat16, 2);
+    const int here = device_of(a[0]);
+    const at::Tensor *const x = device_tensor(a[0], at::kBFloat16, 2, here),
+                     *const r = device_tensor(a[1], at::kBFloat16, 2, here);
     if (!x || !r || x->size(1) != r->size(1) || x->size(0) > INT32_MAX || r->size(0) > INT32_MAX || x->size(1) > INT32_MAX)
         return none();
     const int M = (int)x->size(0), E = (int)r->size(0), K = (int)x->size(1);
-    const at::Tensor *const ids = device_room(a[4], at::kInt, (int64_t)M * top_k),
-                     *const wt = device_room(a[5], at::kFloat, (int64_t)M * top_k),
-                     *const ws = device_tensor(a[6], at::kByte, -1);
+    const at::Tensor *const ids = device_room(a[4], at::kInt, (int64_t)M * top_k, here),
+                     *const wt = device_room(a[5], at::kFloat, (int64_t)M * top_k, here),
+                     *const ws = device_tensor(a[6], at::kByte, -1, here);
     if (!ids || !wt || !ws) return none();
-    const uint16_t *const xp = static_cast<const uint16_t *>(x->data_ptr()), *const rp = static_cast<const uint16_t *>(r->data_ptr());
+    const uint16_t *const xp = static_cast<const uint16_t *>(x->data_ptr());
+    const uint16_t *const rp = static_cast<const uint16_t *>(r->data_ptr());
     int32_t *const ip = static_cast<int32_t *>(ids->data_ptr());
     float *const wp = static_cast<float *>(wt->data_ptr());
     void *const sp = ws->data_ptr(), *const st = current_stream();
@@ -280,12 +301,16 @@ PyObject *moe_experts(PyObject *, PyObject *const *a, Py_ssize_t n) {
         PyErr_Clear();
         return none();
     }
-    const at::Tensor *const x = device_tensor(a[3], at::kBFloat16, 2), *const ids = device_tensor(a[4], at::kInt, 2),
-                     *const wt = device_tensor(a[5], at::kFloat, 2), *const ws = device_tensor(a[7], at::kByte, -1);
-    if (!x || !ids || !wt || !ws || x->get_device() != device || x->size(1) != K || x->size(0) != ids->size(0) || wt->size(0) != ids->size(0) ||
+    const int here = device_of(a[3]);
+    if (here != device) return none();
+    const at::Tensor *const x = device_tensor(a[3], at::kBFloat16, 2, here),
+                     *const ids = device_tensor(a[4], at::kInt, 2, here),
+                     *const wt = device_tensor(a[5], at::kFloat, 2, here),
+                     *const ws = device_tensor(a[7], at::kByte, -1, here);
+    if (!x || !ids || !wt || !ws || x->size(1) != K || x->size(0) != ids->size(0) || wt->size(0) != ids->size(0) ||
         wt->size(1) != ids->size(1) || ids->size(0) > INT32_MAX || ids->size(1) > INT32_MAX)
         return none();
-    const at::Tensor *const y = output_tensor(a[6], x->size(0) * K, &y_dtype);
+    const at::Tensor *const y = output_tensor(a[6], x->size(0) * K, &y_dtype, here);
     if (!y) return none();
     const uint16_t *const xp = static_cast<const uint16_t *>(x->data_ptr());
     const int32_t *const ip = static_cast<const int32_t *>(ids->data_ptr());
