@@ -620,3 +620,11 @@ def test_many_tokens_of_more_experts_than_pairs(M, E, k, K, F, fmt):
         y = nvq.moe_experts(ex, x, dev(ids), dev(w), out_dtype=torch.float32, workspace=ws)
         check(y, x, values, ids, w)
         assert torch.equal(y, nvq.moe_experts(ex, x, dev(ids), dev(w), out_dtype=torch.float32, workspace=ws))
+
+
+# few tokens of 65 to 128 experts, nine to sixteen of 129 to 256
+@gpu
+@pytest.mark.parametrize("M,E,K,k", [(1, 128, 4096, 8), (3, 100, 320, 7), (8, 65, 96, 16), (9, 256, 288, 8), (16, 140, 2048, 16), (13, 129, 64, 1)])
+@pytest.mark.parametrize("renorm", [True, False])
+def test_route_of_exact_logits_with_ties_at_other_sizes(M, E, K, k, renorm):
+    test_route_of_exact_logits_with_ties(M, E, K, k, renorm)

@@ -569,3 +569,15 @@ def test_gemv_exact_sums_of_activations_in_lds(M, N, K, dtype):
     want = xv @ np_mx.dequant(q, s).T
     y = nvq.gemv_mxfp4(dev(q), dev(s), dev(x).bfloat16(), out_dtype=dtype)
     assert bits_equal(f64(y) + 0.0, f64(torch.from_numpy(want).float().to(dtype)) + 0.0)
+
+
+# tiles of 128 x 64 in two slices of K: whole and ragged rows and tokens, windows of sixteen blocks whole, short and past the end
+@gpu
+@pytest.mark.parametrize("M,N,K", [(512, 4096, 1024), (129, 9000, 544), (450, 3700, 8224), (700, 2500, 800), (500, 4001, 1312), (64, 24577, 512)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gemm_exact_sums_of_medium_tiles(M, N, K, dtype):
+    q, s, xq, xs, xv = exact_case(M, N, K, M + N + K, True)
+    want = xv @ np_mx.dequant(q, s).T
+    assert np.abs(want).max() * 2 ** 9 < 2 ** 24
+    y = nvq.gemm_mxfp4(dev(q), dev(s), dev(xq), dev(xs), out_dtype=dtype)
+    assert bits_equal(f64(y) + 0.0, f64(torch.from_numpy(want).float().to(dtype)) + 0.0)
