@@ -3,8 +3,9 @@
 // (i, kb) = (lane % 16, lane / 16) holding the 16 bytes of codes of one block of row or token i and that block's scale
 // byte.  Sums in fp32.
 //
-// Bound by the matrix units where there is enough to multiply, by the L2's rate into LDS in smaller tiles.  Measured (M x N x K): 4096 x
-// 28672 x 4096 265 us = 3.6 PFLOP/s (the products alone, in a loop: 158), 512 x 4096 x 14336 31 us, 77 x 1003 x 2080 6 us.
+// Bound by the matrix units where there is enough to multiply, by the L2's rate into LDS in smaller tiles.
+// Measured (M x N x K): 4096 x 28672 x 4096 265 us = 3.6 PFLOP/s (the products alone, in a loop: 158), 512 x
+// 4096 x 14336 31 us, 77 x 1003 x 2080 6 us.
 #include "mfma_act.h"
 
 namespace nvq {
@@ -63,9 +64,9 @@ __device__ __forceinline__ GemmTile gemm_tile_of(int block, int tiles, int tiles
     return GemmTile{in / high, first + in % high};
 }
 
-// A wave's results: 16 A tokens at a time through LDS (`out`: 16 A rows of 16 P results and 16 bytes), so that they leave as
-// whole runs of 16 P results, 16 bytes per lane at any alignment (4095 x 28669 x 4096: 281 us, by single results 390).
-// BYTES: of a result.
+// A wave's results: 16 A tokens at a time through LDS (`out`: 16 A rows of 16 P results and 16 bytes), so that
+// they leave as whole runs of 16 P results, 16 bytes per lane at any alignment (4095 x 28669 x 4096: 281 us, by
+// single results 390).  BYTES: of a result.
 template <int P, int T, int A, int BYTES>
 __device__ __forceinline__ void store_tile(unsigned char *out, float4v (&sum)[P][T], int n0, int N, int m0, int M, void *y) {
     constexpr int kRow = 16 * P * BYTES, kPitch = kRow + 16;
@@ -101,17 +102,19 @@ __device__ __forceinline__ void store_tile(unsigned char *out, float4v (&sum)[P]
             }
         } else {
             constexpr int kAtOnce = P == 8 ? 1 : 8;
-            // (one by one, a read of LDS and its store took 2 us more; unrolled in the largest tile, which fills the registers, they
-            // cost its whole rows 4 %)
+            // (one by one, a read of LDS and its store took 2 us more; unrolled in the largest tile, which
+            // fills the registers, they cost its whole rows 4 %)
 #pragma unroll kAtOnce
             for (int c = lane; c < tokens * 16 * P; c += 64) {
                 const int r = c / (16 * P), n = c % (16 * P);
                 if (n0 + n >= N) continue;
                 const int64_t to = (int64_t)(first + r) * N + n0 + n;
                 if (BYTES == 2)
-                    ((__attribute__((address_space(1))) uint16_t *)y)[to] = *reinterpret_cast<const uint16_t *>(out + r * kPitch + n * 2);
+                    ((__attribute__((address_space(1))) uint16_t *)y)[to] =
+                        *reinterpret_cast<const uint16_t *>(out + r * kPitch + n * 2);
                 else
-                    ((__attribute__((address_space(1))) float *)y)[to] = *reinterpret_cast<const float *>(out + r * kPitch + n * 4);
+                    ((__attribute__((address_space(1))) float *)y)[to] =
+                        *reinterpret_cast<const float *>(out + r * kPitch + n * 4);
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -119,8 +122,8 @@ __device__ __forceinline__ void store_tile(unsigned char *out, float4v (&sum)[P]
 }
 
 // A wave of 64 x 64 results: weights are the first operand, so that a lane's four registers of a 16x16 tile are
-// four neighbouring rows (columns of y) of one token.  For short K, where the results are the work: 658 x 9765 x 448 took 20 us
-// with a store from each lane for each result, 12 in whole runs; 4096 x 4096 x 256 40 and 17.
+// four neighbouring rows (columns of y) of one token.  For short K, where the results are the work: 658 x 9765
+// x 448 took 20 us with a store from each lane for each result, 12 in whole runs; 4096 x 4096 x 256 40 and 17.
 __global__ __launch_bounds__(64) void gemm_mxfp4_small_k_kernel(const uint4 *__restrict__ wq,
                                                                const uint8_t *__restrict__ ws, int N, int G,
                                                                const uint4 *__restrict__ xq,
@@ -180,16 +183,17 @@ __device__ __forceinline__ uint4v transpose_bytes(const uint4v &d) {
                   __builtin_amdgcn_perm(hi23, hi01, 0x05040100u), __builtin_amdgcn_perm(hi23, hi01, 0x07060302u)};
 }
 
-// S groups of 2 x 2 waves, each wave 16 P rows by 16 T tokens, W waves per SIMD.  A group takes a slice of K with LDS of its own; group 0
-// adds the slices' results in their order.
+// S groups of 2 x 2 waves, each wave 16 P rows by 16 T tokens, W waves per SIMD.  A group takes a slice of K
+// with LDS of its own; group 0 adds the slices' results in their order.
 //
-// A stage is 256 inputs, 128 bytes of codes, of all the workgroup's rows and tokens: whole lines (with 64 bytes per row the
-// L2 gives half the rate, 69 against 131 bytes per ns and compute unit).  Two stages lie in LDS.  A stage is multiplied in two
-// steps of four blocks.  The second step's operands are read in the first half of the first step; from there on the stage's
-// place is free and the next but one is loaded into it, a few instructions between the products at a time, until the end of the
-// second step, in whose second half the next stage's first operands are read.
-// Piece c (16 bytes) of row r is kept at position c ^ (r / 2 % 8): an LDS read of 16 bytes per lane takes lanes 0-3, 12-15 and
-// 20-27 of a half wave together and then its other sixteen, and either sixteen touch all banks once.
+// A stage is 256 inputs, 128 bytes of codes, of all the workgroup's rows and tokens: whole lines (with 64 bytes
+// per row the L2 gives half the rate, 69 against 131 bytes per ns and compute unit).  Two stages lie in LDS.  A
+// stage is multiplied in two steps of four blocks.  The second step's operands are read in the first half of
+// the first step; from there on the stage's place is free and the next but one is loaded into it, a few
+// instructions between the products at a time, until the end of the second step, in whose second half the next
+// stage's first operands are read.  Piece c (16 bytes) of row r is kept at position c ^ (r / 2 % 8): an LDS read
+// of 16 bytes per lane takes lanes 0-3, 12-15 and 20-27 of a half wave together and then its other sixteen, and
+// either sixteen touch all banks once.
 template <int P, int T, int S, int W>
 __global__ __launch_bounds__(256 * S) __attribute__((amdgpu_waves_per_eu(W, W))) void gemm_mxfp4_kernel(
     const unsigned char *__restrict__ wq, const unsigned char *__restrict__ ws, int N, int G,
@@ -210,11 +214,13 @@ __global__ __launch_bounds__(256 * S) __attribute__((amdgpu_waves_per_eu(W, W)))
     const int wa = wave & 1, wb = wave >> 1;
     const GemmTile tile = gemm_tile_of(blockIdx.x, gridDim.x, tiles_n);
     const int n0 = tile.n * kRows, m0 = tile.m * kTokens;
-    // windows of two stages, sixteen blocks: the group's begin and their number (some groups' last ones may lie past the end)
+    // windows of two stages, sixteen blocks: the group's begin and their number (some groups' last ones may lie
+    // past the end)
     const int windows = S == 1 ? (G + 15) >> 4 : (((G + 15) >> 4) + S - 1) / S, window0 = group * windows;
 
-    // Global memory -> LDS: instruction j of a wave takes 8 rows (then tokens), lane l position l % 8 of row l / 8.  Rows past
-    // the end read the last one, blocks past the end the last one (their scales are zero).
+    // Global memory -> LDS: instruction j of a wave takes 8 rows (then tokens), lane l position l % 8 of row
+    // l / 8.  Rows past the end read the last one, blocks past the end the last one (their scale bytes are zero
+    // on both sides: products of 2^-249 at most, which no fp32 sum holds).
     const unsigned char *const abase = wq + (int64_t)n0 * G * 16, *const bbase = xq + (int64_t)m0 * G * 16;
     uint32_t row_at[kLoads];
 #pragma unroll
@@ -237,8 +243,8 @@ __global__ __launch_bounds__(256 * S) __attribute__((amdgpu_waves_per_eu(W, W)))
                                          (lds_void_ptr)(stage + (own + first) * 128), 16, 0, 0);
     };
 
-    // Scales of a window: thread t takes rows t, t + 256 .. of both, 16 bytes each, transposed so that word kb holds what lane-row
-    // kb needs in the four steps, zero past the end.
+    // Scales of a window: thread t takes rows t, t + 256 .. of both, 16 bytes each, transposed so that word kb
+    // holds what lane-row kb needs in the four steps, zero past the end.
     constexpr int kSc = (kBoth + 255) / 256;
     const unsigned char *scale_row[kSc];
 #pragma unroll
@@ -316,7 +322,8 @@ __global__ __launch_bounds__(256 * S) __attribute__((amdgpu_waves_per_eu(W, W)))
 #define NVQ_LOADS(stage_, slot_)                                                                                    \
     _Pragma("unroll") for (int j = kLoads * (slot_) / kSlots; j < kLoads * ((slot_) + 1) / kSlots; ++j)             \
         load(stage_, j, even_, odd_);
-    // One stage: `cur_` is multiplied (its first operands in a0, b0) and then refilled with stage `ahead_`, `next_` follows.
+    // One stage: `cur_` is multiplied (its first operands in a0, b0) and then refilled with stage `ahead_`,
+    // `next_` follows.
 #define NVQ_STAGE(cur_, next_, k_, ahead_, scales_)                                                                 \
     {                                                                                                               \
         _Pragma("unroll") for (int p = 0; p < kHalf; ++p) {                                                         \
@@ -379,7 +386,8 @@ __global__ __launch_bounds__(256 * S) __attribute__((amdgpu_waves_per_eu(W, W)))
 #pragma unroll
         for (int t = 0; t < T; ++t) asm volatile("s_nop 0" : "+a"(sum[p][t]));  // (the last product was written long ago)
     if constexpr (S > 1) {
-        // slices 1 .. of S hand over their results, a tile of 64 lanes after the other, half of them in either stage's place
+        // slices 1 .. of S hand over their results, a tile of 64 lanes after the other, half of them in either
+        // stage's place
         constexpr int kTiles = P / 2 * T;
         static_assert(4 * kTiles * 1024 <= kBoth * 128, "a slice's results in its part of the stages");
         auto place = [&](int from, int p, int t) -> float4v & {

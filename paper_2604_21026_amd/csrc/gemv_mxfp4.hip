@@ -2,20 +2,23 @@
 // blocks g of 2^(scale - 127) * sum_j code[n][32g + j] * x[m][32g + j], weights and activations unrounded, sums in
 // fp32.
 //
-// Bound by reading the weights once, 17 bytes per 32 of them, which is 4.25 bits; mx_rows.h has the product on the matrix cores.  Five
-// kernels: one or two tokens by dot products; row tiles whose workgroups read the activations with the weights, for few inputs or
-// rows; all activations of a few tokens in LDS; activations shared through LDS step by step; and, for many rows, activations that
-// stay in registers.
+// Bound by reading the weights once, 17 bytes per 32 of them, which is 4.25 bits; mx_rows.h has the product on
+// the matrix cores.  Five kernels: one or two tokens by dot products; row tiles whose workgroups read the
+// activations with the weights, for few inputs or rows; all activations of a few tokens in LDS; activations
+// shared through LDS step by step; and, for many rows, activations that stay in registers.
 //
-// Measured: 4096 x 4096 at one token 3.1 us (an empty launch 2.4), 128256 x 4096 at one token 43 us (6.5 TB/s), at 32 tokens 56 (5.0),
-// 128256 x 14336 at one token 160 (6.1); the choices at the end have more.
+// Measured in captured calls, one after the other, the same weights each time (and weights that no cache
+// holds): 4096 x 4096 at one token 2.9 us (4.4; an empty launch 2.4 from the host), 128256 x 4096 at one token
+// 42 us, 6.6 TB/s (47), at 32 tokens 54, 5.3 TB/s (61), 128256 x 14336 at one token 161, 6.1 TB/s (161); the
+// choices at the end have more.
 #include "mx_rows.h"
 
 namespace nvq {
 
 namespace {
 
-// A workgroup takes R row tiles and T token tiles, its W waves share out K (rows_times_tokens: passes of Q columns, B at a time).
+// A workgroup takes R row tiles and T token tiles, its W waves share out K (rows_times_tokens: passes of Q
+// columns, B at a time).
 template <int R, int T, int W, int B, int Q>
 __global__ __launch_bounds__(64 * W) void gemv_mxfp4_kernel(const uint8_t *__restrict__ q,
                                                             const uint8_t *__restrict__ scales, int N, int G,
@@ -64,13 +67,15 @@ __global__ __launch_bounds__(64 * W) void gemv_mxfp4_kernel(const uint8_t *__res
 }
 
 
-// One or two tokens (M).  KS waves take R rows at a time, a lane of theirs the blocks l, 64 + l, .. (B in all), whose activations it keeps for
-// all its rows, and ask for the next rows meanwhile.  A block's codes become bf16 values, scale and all, eight in four
-// conversions, and go through the dot product of bf16 pairs.  (The matrix cores' way reads the activations for sixteen tokens: four
-// loads for each one of weights, as much of the address path's time.  Of three tokens on the products themselves cost more.)
+// One or two tokens (M).  KS waves take R rows at a time, a lane of theirs the blocks l, 64 + l, .. (B in all),
+// whose activations it keeps for all its rows, and ask for the next rows meanwhile.  A block's codes become
+// bf16 values, scale and all, eight in four conversions, and go through the dot product of bf16 pairs.  (The
+// matrix cores' way reads the activations for sixteen tokens: four loads for each one of weights, as much of
+// the address path's time.  Of three tokens on the products themselves cost more.)
 template <int M, int B, int R, int KS>
-__global__ __launch_bounds__(256) void gemv_mxfp4_dot_kernel(const uint8_t *__restrict__ q, const uint8_t *__restrict__ scales, int N,
-                                                             int G, const uint16_t *__restrict__ x, void *__restrict__ y,
+__global__ __launch_bounds__(256) void gemv_mxfp4_dot_kernel(const uint8_t *__restrict__ q,
+                                                             const uint8_t *__restrict__ scales, int N, int G,
+                                                             const uint16_t *__restrict__ x, void *__restrict__ y,
                                                              int y_dtype) {
     static_assert(KS == 1 || KS == 4, "a wave or the workgroup");
     constexpr int kTeams = 4 / KS;
@@ -104,9 +109,9 @@ __global__ __launch_bounds__(256) void gemv_mxfp4_dot_kernel(const uint8_t *__re
                 xr[m][b][i] = uint4v{0, 0, 0, 0};
                 if (l0 + 64 * b < G) xr[m][b][i] = as_global<uint4v>(x)[((int64_t)m * G + l0 + 64 * b) * 4 + i];
             }
-    // Scales become exponents (the conversions look at nothing else); past the end, where activations are zero, the smallest one, since
-    // values beyond bf16 would make them NaN.  (4096 x 14336 6.4 us for 6.25, others equal; loads or products left out instead cost
-    // up to 10 %.)
+    // Scales become exponents (the conversions look at nothing else); past the end, where activations are zero,
+    // the smallest one, since values beyond bf16 would make them NaN.  (4096 x 14336 6.4 us for 6.25, others
+    // equal; loads or products left out instead cost up to 10 %.)
     int up[B];
 #pragma unroll
     for (int b = 0; b < B; ++b) up[b] = l0 + 64 * b < G ? 23 : 31;
@@ -176,11 +181,12 @@ __global__ __launch_bounds__(256) void gemv_mxfp4_dot_kernel(const uint8_t *__re
     }
 }
 
-// The same for more tokens, whose activations outweigh the weights where every row tile reads them for itself: a workgroup of RG
-// x S waves takes RG * R row tiles, and brings the activations of S passes of C columns into LDS for all of them, a pass ahead
-// (through registers, the loads two passes ahead); wave (g, s) multiplies the row tiles of group g with pass s of each turn.
-// Piece c (16 bytes) of token n lies at position c ^ swapped(n % 16): a read takes lanes 0-3, 12-15 and 20-27 of a half wave
-// together and then its other sixteen, and either sixteen touch every bank once.
+// The same for more tokens, whose activations outweigh the weights where every row tile reads them for itself:
+// a workgroup of RG x S waves takes RG * R row tiles, and brings the activations of S passes of C columns into
+// LDS for all of them, a pass ahead (through registers, the loads two passes ahead); wave (g, s) multiplies the
+// row tiles of group g with pass s of each turn.  Piece c (16 bytes) of token n lies at position c ^ swapped(n %
+// 16): a read takes lanes 0-3, 12-15 and 20-27 of a half wave together and then its other sixteen, and either
+// sixteen touch every bank once.
 __device__ __forceinline__ int swapped(int n) { return (n & 9) | (n & 2) << 1 | (n & 4) >> 1; }
 
 template <int T, int R, int RG, int S, int C>
@@ -265,7 +271,8 @@ __global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const ui
                 for (int t = 0; t < T; ++t)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        a[t][i] = __builtin_bit_cast(bf16x8, xb[(16 * t + n) * kPieces + ((16 * b + 4 * kb + i) ^ swapped(n))]);
+                        a[t][i] = __builtin_bit_cast(bf16x8,
+                                                     xb[(16 * t + n) * kPieces + ((16 * b + 4 * kb + i) ^ swapped(n))]);
                 multiply_column<NVQ_FMT_MXFP4, R, T, C, C>(w[d], b, sc[d], b, a, sum);
             }
         };
@@ -297,7 +304,8 @@ __global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const ui
             for (int r = 0; r < R; ++r)
 #pragma unroll
                 for (int t = 0; t < T; ++t)
-                    *reinterpret_cast<float4v *>(&red[(((g * (S - 1) + s - 1) * (R * T) + r * T + t) * 64 + lane) * 4]) = sum[r][t];
+                    *reinterpret_cast<float4v *>(&red[(((g * (S - 1) + s - 1) * (R * T) + r * T + t) * 64 + lane) * 4]) =
+                        sum[r][t];
         }
         __syncthreads();
         if (s > 0) return;
@@ -307,7 +315,8 @@ __global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const ui
             for (int r = 0; r < R; ++r)
 #pragma unroll
                 for (int t = 0; t < T; ++t)
-                    sum[r][t] += *reinterpret_cast<const float4v *>(&red[(((g * (S - 1) + k) * (R * T) + r * T + t) * 64 + lane) * 4]);
+                    sum[r][t] += *reinterpret_cast<const float4v *>(
+                        &red[(((g * (S - 1) + k) * (R * T) + r * T + t) * 64 + lane) * 4]);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r)
@@ -321,13 +330,13 @@ __global__ __launch_bounds__(64 * RG * S) void gemv_mxfp4_shared_kernel(const ui
 }
 
 
-// The activations stay in registers: wave w of W keeps those of C columns (4 C blocks of 32 inputs), of all tokens, for the whole
-// kernel, and the workgroup streams its row tiles past them, one after the other, D of them requested ahead.  So nothing but weights and
-// their scales is read in the loop (read again for every tile, one token's activations took 25 of 68 us at 128256 x 4096).  The
-// last wave's blocks may begin earlier than its share, where activations and scales are zero.
-// Partial tiles are added through LDS in wave order, by waves that change from tile to tile, and wait there (`out`) until kGroup
-// tiles' results leave as runs of 16 kGroup rows: stored tile by tile, 32 bytes here and there among the loads, 32 tokens' took 64
-// us for 56.
+// The activations stay in registers: wave w of W keeps those of C columns (4 C blocks of 32 inputs), of all
+// tokens, for the whole kernel, and the workgroup streams its row tiles past them, one after the other, D of
+// them requested ahead.  So nothing but weights and their scales is read in the loop (read again for every
+// tile, one token's activations took 25 of 68 us at 128256 x 4096).  The last wave's blocks may begin earlier
+// than its share, where activations and scales are zero.  Partial tiles are added through LDS in wave order, by
+// waves that change from tile to tile, and wait there (`out`) until kGroup tiles' results leave as runs of 16
+// kGroup rows: stored tile by tile, 32 bytes here and there among the loads, 32 tokens' took 64 us for 56.
 template <int T, int W, int C, int D>
 __global__ __launch_bounds__(64 * W) void gemv_mxfp4_resident_kernel(const uint8_t *__restrict__ q,
                                                                      const uint8_t *__restrict__ scales, int N, int G,
@@ -429,9 +438,9 @@ __global__ __launch_bounds__(64 * W) void gemv_mxfp4_resident_kernel(const uint8
     leave(last & 1, last * kGroup, mine - last * kGroup);
 }
 
-// Up to three tokens, whose activations fit in LDS: a workgroup keeps them there for all its row tiles, its W waves share out a
-// tile's columns, four at a time, and four times two are on their way, from tile to tile without a pause.  (Nothing is requested
-// past the last one: that cost a quarter at 4096 x 4096.)
+// Up to three tokens, whose activations fit in LDS: a workgroup keeps them there for all its row tiles, its W
+// waves share out a tile's columns, four at a time, and four times two are on their way, from tile to tile
+// without a pause.  (Nothing is requested past the last one: that cost a quarter at 4096 x 4096.)
 constexpr int kLdsTokens = 3, kLdsBytes = 56 * 1024;  // (two workgroups to a compute unit)
 __device__ __host__ constexpr int lds_pitch(int G) { return ((G + 3) / 4 + 1) * 256 + 16; }
 
@@ -459,7 +468,8 @@ __global__ __launch_bounds__(64 * W, 4) void gemv_mxfp4_lds_kernel(const uint8_t
         typedef uint4v uint4v_any __attribute__((aligned(1)));
         sc[d] = *(const __attribute__((address_space(1))) uint4v_any *)(at.s + (4 * c0 < G - 16 ? 4 * c0 : G - 16));
     };
-    // (the loads' place runs ahead of the products'; a workgroup has two items or more, of two tiles or of one tile's parts)
+    // (the loads' place runs ahead of the products'; a workgroup has two items or more, of two tiles or of one
+    // tile's parts)
     const int items = ((tiles - 1 - (int)blockIdx.x) / (int)gridDim.x + 1) * per;
     int lt = blockIdx.x, lp = 0;
     auto ahead = [&](int d) {
@@ -558,9 +568,9 @@ struct GemvArgs {
     int N, G, M, y_dtype;
 };
 
-// Up to 16 tokens, R row tiles per workgroup.  (Four row tiles, passes of eight columns, two at a time: eight tokens of 14336 x 4096 9.6
-// us, of 128256 x 14336 198; passes of four 10.2 and 209, one column at a time 9.5 and 238.  One row tile, passes of four columns
-// at once: nothing else was better by 1 %.)
+// Up to 16 tokens, R row tiles per workgroup.  (Four row tiles, passes of eight columns, two at a time: eight
+// tokens of 14336 x 4096 9.6 us, of 128256 x 14336 198; passes of four 10.2 and 209, one column at a time 9.5
+// and 238.  One row tile, passes of four columns at once: nothing else was better by 1 %.)
 template <int R>
 int gemv_rows(const GemvArgs &a, hipStream_t st) {
     const dim3 grid((unsigned)(((int64_t)a.N + 16 * R - 1) / (16 * R)));
@@ -572,8 +582,8 @@ int gemv_rows(const GemvArgs &a, hipStream_t st) {
 
 // 17 to 32 tokens, a row tile per workgroup.
 int gemv_two_tiles(const GemvArgs &a, hipStream_t st) {
-    hipLaunchKernelGGL((gemv_mxfp4_kernel<1, 2, 8, 2, 2>), dim3((unsigned)(((int64_t)a.N + 15) / 16)), dim3(512), 0, st, a.q, a.s, a.N,
-                       a.G, a.x, a.M, a.y, a.y_dtype);
+    hipLaunchKernelGGL((gemv_mxfp4_kernel<1, 2, 8, 2, 2>), dim3((unsigned)(((int64_t)a.N + 15) / 16)), dim3(512), 0,
+                       st, a.q, a.s, a.N, a.G, a.x, a.M, a.y, a.y_dtype);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
 }
@@ -589,8 +599,9 @@ int gemv_resident(const GemvArgs &a, int cus, hipStream_t st) {
 template <int M, int B, int R, int KS>
 int gemv_dot(const GemvArgs &a, int cus, hipStream_t st) {
     const int64_t wanted = ((int64_t)a.N * KS + 4 * R - 1) / (4 * R);
-    hipLaunchKernelGGL((gemv_mxfp4_dot_kernel<M, B, R, KS>), dim3((unsigned)(wanted < 2 * cus ? wanted : 2 * cus)), dim3(256), 0, st,
-                       a.q, a.s, a.N, a.G, a.x, a.y, a.y_dtype);
+    const dim3 grid((unsigned)(wanted < 2 * cus ? wanted : 2 * cus));
+    hipLaunchKernelGGL((gemv_mxfp4_dot_kernel<M, B, R, KS>), grid, dim3(256), 0, st, a.q, a.s, a.N, a.G, a.x, a.y,
+                       a.y_dtype);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
 }
@@ -626,49 +637,55 @@ extern "C" int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
     const GemvArgs a = {qweight, scales, x_bf16, y, N, K / 32, M, y_dtype};
     const int cus = device_cu_count();
     const int64_t tiles = ((int64_t)N + 15) / 16;
-    // One token, us against what follows: 4096 x 4096 3.1 (4.0), 14336 x 4096 5.5 (8.3), 1024 x 4096 2.7 (3.9), 4096 x 14336 6.7 (9.2),
-    // 2048 x 8192 3.5 (5.4), 10240 x 8192 9.2 (11.4), 128256 x 4096 43 (45), 14336 x 1024 4.0 (4.9); not 32768 x 512 6.0 (4.3), 4096 x 1024 3.0
-    // (2.5).  Two rows at a time, or four where that is one turn of one workgroup to each compute unit (4096 x 4096 3.2 against 3.5, 14336
-    // x 4096 6.6 against 6.0); from 4096 inputs on the four waves share them, four rows at a time (10240 x 8192 9.5 against 10.6).
+    // One token, us against what follows: 4096 x 4096 2.9 (3.9), 14336 x 4096 5.3 (8.1), 1024 x 4096 2.5 (3.8),
+    // 4096 x 14336 6.5 (8.7), 2048 x 8192 3.4 (5.2), 10240 x 8192 9.3 (11.0), 128256 x 4096 42 (44), 14336 x
+    // 1024 3.9 (4.4); not 32768 x 512 5.9 (4.0), and 4096 x 1024 2.3 (2.3).  Two rows at a time, or four where
+    // that is one turn of one workgroup to each compute unit (4096 x 4096 3.2 against 3.5, 14336 x 4096 6.6
+    // against 6.0); from 4096 inputs on the four waves share them, four rows at a time (10240 x 8192 9.5
+    // against 10.6).
     if (M == 1) {
         if (a.G >= 32 && a.G <= 64 && (int64_t)N * a.G >= 1024 * cus) return gemv_dot<1, 1, 4, 1>(a, cus, st);
-        if (a.G > 64 && a.G <= 128) return N > 8 * cus && N <= 16 * cus ? gemv_dot<1, 2, 4, 1>(a, cus, st) : gemv_dot<1, 2, 2, 1>(a, cus, st);
+        if (a.G > 64 && a.G <= 128)
+            return N > 8 * cus && N <= 16 * cus ? gemv_dot<1, 2, 4, 1>(a, cus, st) : gemv_dot<1, 2, 2, 1>(a, cus, st);
         if (a.G > 128 && a.G <= 256) return gemv_dot<1, 1, 4, 4>(a, cus, st);
         if (a.G > 256 && a.G <= 512) return gemv_dot<1, 2, 4, 4>(a, cus, st);
     }
-    // Two: 4096 x 4096 4.0 (4.3), 14336 x 4096 7.5 (8.5), 1024 x 4096 3.2 (4.1), 4096 x 14336 9.1 (9.8); not 28672 x 4096 13.4 (12.5).
+    // Two: 4096 x 4096 3.8 (4.1), 14336 x 4096 7.3 (8.2), 1024 x 4096 3.1 (4.0), 4096 x 14336 8.8 (9.5, but
+    // with weights that no cache holds 11.9 and 11.2); not 28672 x 4096 12.9 (12.3).
     if (M == 2 && tiles < 4 * cus) {
         if (a.G > 64 && a.G <= 128)
             return N > 8 * cus && N <= 16 * cus ? gemv_dot<2, 2, 4, 1>(a, cus, st) : gemv_dot<2, 2, 2, 1>(a, cus, st);
         if (a.G > 128 && a.G <= 256) return gemv_dot<2, 1, 4, 4>(a, cus, st);
         if (a.G > 256 && a.G <= 512) return gemv_dot<2, 2, 4, 4>(a, cus, st);
     }
-    // Many row tiles, K that eight waves hold: (2, 128256, 4096) 46 us, at 16 tokens 50, at 32 56; below, a tile or two per workgroup,
-    // its start costs more ((1, 14336, 4096) 9.4).
+    // Many row tiles, K that eight waves hold: (2, 128256, 4096) 44 us, at 16 tokens 47, at 32 54; below, a
+    // tile or two per workgroup, its start costs more ((1, 14336, 4096) 9.4).
     if (tiles >= 16 * cus && a.G >= 16 && a.G <= 128) {
         if (a.G <= 64) return M <= 16 ? gemv_resident<1, 2>(a, cus, st) : gemv_resident<2, 2>(a, cus, st);
         return M <= 16 ? gemv_resident<1, 4>(a, cus, st) : gemv_resident<2, 4>(a, cus, st);
     }
-    // Up to three tokens, many row tiles, or several and more K than the waves take at once, or K in whole steps of them (4096 inputs).
-    // us against what follows, of three tokens (18830, 6624) 16.6 and 24.3, (28672, 4096) 13.3 and 14.1, (10240, 8192) 12.4 and
-    // 14.2, (8209, 4224) 7.8 and 9.6, (2048, 8192) 6.1 and 6.6, (33000, 2080) 11.0 and 11.4; of two (28672, 4096) 12.3 and 13.8; of one
-    // (8209, 16672) 19.4 and 27.2, (4096, 24576) 12.4 and 14.4; not of three (4096, 9152) 7.3 and 7.0, of four (14336, 4096) 9.8
-    // and 8.8.
+    // Up to three tokens, many row tiles, or several and more K than the waves take at once, or K in whole
+    // steps of them (4096 inputs).  us against what follows, of three tokens (18830, 6624) 16.6 and 24.3,
+    // (28672, 4096) 13.3 and 14.1, (10240, 8192) 12.4 and 14.2, (8209, 4224) 7.8 and 9.6, (2048, 8192) 6.1 and
+    // 6.6, (33000, 2080) 11.0 and 11.4; of two (28672, 4096) 12.3 and 13.8; of one (8209, 16672) 19.4 and 27.2,
+    // (4096, 24576) 12.4 and 14.4; not of three (4096, 9152) 7.3 and 7.0, of four (14336, 4096) 9.8 and 8.8.
     if (M <= kLdsTokens && a.G > 64 && M * lds_pitch(a.G) <= kLdsBytes &&
         (tiles >= 4 * cus || (a.G > 128 && (tiles > 2 * cus || a.G % 128 == 0))))
         return gemv_lds(a, (int)(tiles < 2 * cus ? tiles : 2 * cus), st);
-    // Up to 16 tokens.  us at (tokens, rows, inputs), R row tiles per workgroup with each wave reading its activations, or activations
-    // shared by the RG groups of S waves; a workgroup to each compute unit where row tiles allow:
+    // Up to 16 tokens.  us at (tokens, rows, inputs), R row tiles per workgroup with each wave reading its
+    // activations, or activations shared by the RG groups of S waves; a workgroup to each compute unit where
+    // row tiles allow:
     //                       rows 1  rows 4  shared 1, 8  shared 2, 4  shared 4, 2
-    //   (1, 4096, 4096)       4.0     7.9        5.9         6.6         8.8
-    //   (16, 4096, 4096)      6.6    10.4        6.1         6.7         8.8
-    //   (8, 4096, 14336)     13.5    24.4       12.4        16.2        23.5
-    //   (4, 4096, 14336)     11.3    22.6       11.7        15.5        23.4
-    //   (2, 8192, 4096)       6.5     8.4       10.2         7.1         9.3
-    //   (8, 8192, 4096)       8.6     9.3       10.6         7.4         9.5
-    //   (8, 14336, 4096)     15.3     9.5       19.7        11.8        10.0
-    //   (16, 14336, 4096)    20.6    10.7       20.6        12.0         9.9
-    // and at (16, 128256, 14336), too many inputs for registers, 16 row tiles 193 against 242 with 4 row tiles of 4.
+    //   (1, 4096, 4096)       3.9     7.7        5.6         6.2         8.3
+    //   (16, 4096, 4096)      6.4    10.2        5.9         6.5         8.5
+    //   (8, 4096, 14336)     13.2    24.5       11.6        16.0        23.0
+    //   (4, 4096, 14336)     11.1    22.3       11.1        15.1        22.9
+    //   (2, 8192, 4096)       6.2     8.2       10.2         6.9         8.8
+    //   (4, 8192, 4096)       7.1     8.6       10.4         7.0         9.0
+    //   (8, 8192, 4096)       8.3     9.2       10.2         7.2         9.1
+    //   (8, 14336, 4096)     15.1     9.2       20.5        11.5         9.2
+    //   (16, 14336, 4096)    20.2    10.5       21.0        11.7         9.2
+    // and at (16, 128256, 14336), too many inputs for registers, 16 row tiles 193 against 238 with 4.
     if (M <= 16) {
         if (tiles <= cus) return M * a.G >= 2048 ? gemv_shared<1, 1, 1, 8, 2>(a, st) : gemv_rows<1>(a, st);
         if (tiles <= 2 * cus) return M > 4 ? gemv_shared<1, 1, 2, 4, 2>(a, st) : gemv_rows<1>(a, st);
@@ -676,14 +693,16 @@ extern "C" int nvq_gemv_mxfp4(const uint8_t *qweight, const uint8_t *scales, int
         return tiles < 16 * cus ? gemv_shared<1, 1, 4, 2, 2>(a, st) : gemv_shared<1, 2, 8, 1, 4>(a, st);
     }
     // us at (32 tokens, rows, inputs)    (4096, 4096) (4096, 14336) (8192, 4096) (14336, 4096) (128256, 4096)
-    //   a row tile, K in eight slices         8.6         21.4         15.8         30.3
-    //   2 row tiles, K in four                9.0         23.9         10.5         18.3          155
-    //   4 row tiles, K in two                10.8         32.1         12.0         12.3           93
-    //   16 row tiles                         26.4         82.8                      27.2           63
-    // (Up to 2 row tiles the activations bound it: every compute unit reads all of them, 0.9 MB at 14336 inputs.  Asked for two turns
-    // ahead, each workgroup beginning at another place of K, or with more weights in flight it took as long.)
-    // and with few inputs, each wave reading its activations: (25, 1236, 1760) 4.4 against 6.9 of two row tiles, (20, 300, 3520) 7.1 against
-    // 9.3, (32, 4096, 1024) 4.1 against 4.5, (32, 2048, 2560) 7.0 against 6.8; not (32, 1024, 4096) 10.2 against 7.7.
+    //   a row tile, K in eight slices         8.0         20.4         15.0         29.7          249
+    //   2 row tiles, K in four                8.4         23.2          9.8         17.8          144
+    //   4 row tiles, K in two                 9.9         30.9         11.1         11.4           87
+    //   16 row tiles                         26.6         83.1         26.7         27.4           65
+    // (Up to 2 row tiles the activations bound it: every compute unit reads all of them, 0.9 MB at 14336
+    // inputs.  Asked for two turns ahead, each workgroup beginning at another place of K, or with more weights
+    // in flight it took as long.)  And with few inputs, each wave reading its activations, against a row tile in
+    // eight slices: (25, 1236, 1760) 4.3 and 5.4, (32, 4096, 1024) 3.9 and 4.2, (20, 300, 3520) 7.0 and 6.9,
+    // (32, 2048, 2560) 6.8 and 5.7 (from about 2000 inputs on slices would do as well or better); not (32,
+    // 1024, 4096) 10.0 and 7.4.
     if (tiles <= cus && a.G < 128) return gemv_two_tiles(a, st);
     if (tiles <= cus && a.G >= 128) return gemv_shared<2, 1, 1, 8, 1>(a, st);
     if (tiles <= 2 * cus) return gemv_shared<2, 1, 2, 4, 2>(a, st);

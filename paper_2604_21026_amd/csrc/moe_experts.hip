@@ -1,17 +1,25 @@
 // nvq_moe_experts: the experts' feed-forward layers of 1 to 32 tokens and the weighted sum of their outputs,
 // y[m] = sum_s w[m][s] * D_e (silu(G_e x[m]) * (U_e x[m])), e = ids[m][s], in two launches.
 //
-// The first one makes h = bf16(silu(g) * u) for every pair of a token and an expert: a workgroup takes gate rows and the up
-// rows beside them of one expert, for all tokens that chose it, so that every weight is read once.  The second one makes y: a
-// workgroup takes 16 or 64 output rows, its waves the experts in turn, or slices of one where there are fewer experts than
-// waves; the sums over experts stay in LDS, one copy per wave, and are added in wave order.  Where a row tile's experts are more
-// than its waves can do with little in flight, up to four workgroups share them: they leave their sums in the workspace, and
-// the last to arrive adds them in their order.  No sum's order depends on timing.  Products: mx_rows.h.  A token or a few that
-// share few experts take another way, by dot products (below).
+// The first one makes h = bf16(silu(g) * u) for every pair of a token and an expert: a workgroup takes gate
+// rows and the up rows beside them of one expert, for all tokens that chose it, so that every weight is read
+// once.  The second one makes y: a workgroup takes 16 or 64 output rows, its waves the experts in turn, or
+// slices of one where there are fewer experts than waves; the sums over experts stay in LDS, one copy per wave,
+// and are added in wave order.  Where a row tile's experts are more than its waves can do with little in
+// flight, up to four workgroups share them: they leave their sums in the workspace, and the last to arrive adds
+// them in their order.  No sum's order depends on timing.  Products: mx_rows.h.  A token or a few that share
+// few experts take another way, by dot products (below).
 //
-// Bound: the chosen experts' weights, each read once.  Microscaled, 32 experts of 4096 x 1792, 32 tokens, four experts each: 373
-// MB in 84.5 us (first launch 53, second 32), 4.4 TB/s; int4 (396 MB) 99.6 us.  One token, eight experts of 2048 x 1024: 28 MB in
-// 11.4 us (int4) and 27 MB in 8.9 (microscaled), two launches (an empty one 2.4), each a chain of ids -> weights -> sums.
+// h is rounded to bf16, the operand type of the second product (as nvq_silu_mul_bf16 rounds it for the layers
+// of single calls): a relative error of up to 2^-8 in each of its values, 0.0016 in y on the average (y in bf16
+// 0.0023 with it, 0.0017 without).  Two bf16 terms would hold it, with twice the reads of h and twice the
+// products of the second launch.
+//
+// Bound: the chosen experts' weights, each read once.  Captured calls, one after the other, the same weights
+// each time (and weights that no cache holds).  Microscaled, 32 experts of 4096 x 1792, 32 tokens, four experts
+// each: 373 MB in 82 us (83; first launch 52, second 33), 4.5 TB/s; int4 (396 MB) 99 us (99).  One token, eight
+// experts of 2048 x 1024: 28 MB in 9.1 us (12.1; int4) and 27 MB in 7.9 (10.2; microscaled), two launches (an
+// empty one 2.4 from the host), each a chain of ids -> weights -> sums.
 #include "mx_rows.h"
 #include "transform.h"
 
@@ -40,8 +48,9 @@ struct MoeArgs {
 
 __device__ __forceinline__ int token_of(const MoeArgs &a, int pair) { return (int)((uint32_t)pair * a.per_token >> 16); }
 
-// The tokens of one expert in ascending order, spread over a wave: lane n of a lane-row has number 16 t + n of them for t =
-// 0, 1 (past the end: the first one's), the pair of its first slot and the sum of its slots' weights.
+// The tokens of one expert in ascending order, spread over a wave: lane n of a lane-row has number 16 t + n of
+// them for t = 0, 1 (past the end: the first one's), the pair of its first slot and the sum of its slots'
+// weights.
 struct ExpertTokens {
     int count, first;  // first: the lowest pair
     int token[2], pair[2];
@@ -77,9 +86,9 @@ __device__ __forceinline__ ExpertTokens tokens_of(const MoeArgs &a, int id, floa
     return et;
 }
 
-// More pairs, id_of(t) and weight_of(t) giving the lane's of chunk t: each that is its token's first with the expert finds its
-// number by counting those below, and sends itself to the lane of that number.  (One after the other, 25 tokens' 200 pairs of
-// twelve experts took a seventh of 29 us.)
+// More pairs, id_of(t) and weight_of(t) giving the lane's of chunk t: each that is its token's first with the
+// expert finds its number by counting those below, and sends itself to the lane of that number.  (One after the
+// other, 25 tokens' 200 pairs of twelve experts took a seventh of 29 us.)
 template <typename IDS, typename WEIGHTS>
 __device__ __forceinline__ ExpertTokens tokens_of(const MoeArgs &a, int e, IDS id_of, WEIGHTS weight_of) {
     int lane = threadIdx.x & 63;
@@ -102,7 +111,8 @@ __device__ __forceinline__ ExpertTokens tokens_of(const MoeArgs &a, int e, IDS i
             const float w = weight_of(t, lane);
             const int to = first ? count + __builtin_popcountll(firsts & lower) : 63;  // (63: none; there are 32 tokens)
             listed |= __builtin_amdgcn_ds_permute(4 * to, p + 1);
-            weight = __uint_as_float(__float_as_uint(weight) | (uint32_t)__builtin_amdgcn_ds_permute(4 * to, (int)__float_as_uint(w)));
+            weight = __uint_as_float(__float_as_uint(weight) |
+                                     (uint32_t)__builtin_amdgcn_ds_permute(4 * to, (int)__float_as_uint(w)));
             for (uint64_t more = here & ~firsts; more; more &= more - 1) {  // (an expert in several slots of a token)
                 const int bit = __builtin_ctzll(more);
                 const float other = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), bit));
@@ -201,9 +211,10 @@ __global__ __launch_bounds__(64 * KS) void moe_gate_up_kernel(MoeArgs a) {
     }
 }
 
-// The same for experts of many rows: wave w of W keeps the activations of C columns of the expert's tokens in registers and
-// the workgroup streams tiles of gate and up rows past them, two turns of both requested ahead; the grid's first axis shares
-// out an expert's tiles.  The waves' sums meet in LDS, one barrier a turn; four waves add them, the other four in the next turn.
+// The same for experts of many rows: wave w of W keeps the activations of C columns of the expert's tokens in
+// registers and the workgroup streams tiles of gate and up rows past them, two turns of both requested ahead;
+// the grid's first axis shares out an expert's tiles.  The waves' sums meet in LDS, one barrier a turn; four
+// waves add them, the other four in the next turn.
 template <int FMT, int W, int C, bool SMALL>
 __global__ __launch_bounds__(64 * W) void moe_gate_up_resident_kernel(MoeArgs a) {
     constexpr int D = 2;
@@ -249,7 +260,8 @@ __global__ __launch_bounds__(64 * W) void moe_gate_up_resident_kernel(MoeArgs a)
             for (int i = 0; i < 4; ++i) {
                 const int block = b0 + 4 * b + (FMT == NVQ_FMT_MXFP4 ? kb : i);
                 raw[i] = uint4v{0, 0, 0, 0};
-                if (block >= share && 16 * t + n < et.count) raw[i] = *as_global<uint4v>(xt + (b0 + 4 * b) * 64 + piece_at<FMT>(i, kb));
+                if (block >= share && 16 * t + n < et.count)
+                    raw[i] = *as_global<uint4v>(xt + (b0 + 4 * b) * 64 + piece_at<FMT>(i, kb));
             }
             to_operands<FMT>(raw, x[b][0]);
         }
@@ -295,9 +307,9 @@ __global__ __launch_bounds__(64 * W) void moe_gate_up_resident_kernel(MoeArgs a)
     }
 }
 
-// A workgroup takes 16 R rows of the outputs; the row tiles' experts, or slices of them, are shared out among the waves of
-// a.parts workgroups.  (R = T = 1: within 128 registers, so that two workgroups run on a compute unit; with 129 one token's eight
-// experts took 17.4 us for 14.6.)
+// A workgroup takes 16 R rows of the outputs; the row tiles' experts, or slices of them, are shared out among
+// the waves of a.parts workgroups.  (R = T = 1: within 128 registers, so that two workgroups run on a compute
+// unit; with 129 one token's eight experts took 17.4 us for 14.6.)
 template <int FMT, int R, int T, int W, int C, bool SMALL>
 __global__ __launch_bounds__(64 * W, R * T == 1 ? 4 : 1) void moe_down_kernel(MoeArgs a) {
     constexpr int kTokens = SMALL ? 16 : NVQ_MAX_M;
@@ -335,8 +347,8 @@ __global__ __launch_bounds__(64 * W, R * T == 1 ? 4 : 1) void moe_down_kernel(Mo
     const int words = (a.E + 31) >> 5;
     int active = 0;
     for (int i = 0; i < words; ++i) active += __builtin_popcount((uint32_t)__builtin_amdgcn_readlane((int)word, i));
-    // The workgroups of all parts share the experts out among their waves; where there are more waves than experts, each in
-    // `split` slices of its inputs.
+    // The workgroups of all parts share the experts out among their waves; where there are more waves than
+    // experts, each in `split` slices of its inputs.
     const int workers = a.parts * W, G = a.F / 32;
     int split = active == 0 || active >= workers ? 1 : (workers + active - 1) / active;
     const int passes = (G + 4 * C - 1) / (4 * C);
@@ -359,7 +371,8 @@ __global__ __launch_bounds__(64 * W, R * T == 1 ? 4 : 1) void moe_down_kernel(Mo
         if constexpr (SMALL)
             et = tokens_of(a, my_id, my_weight, e);
         else
-            et = tokens_of(a, e, [&](int t, int l) { return ids[64 * t + l]; }, [&](int t, int l) { return weights[64 * t + l]; });
+            et = tokens_of(
+                a, e, [&](int t, int l) { return ids[64 * t + l]; }, [&](int t, int l) { return weights[64 * t + l]; });
         RowAt at[R];
 #pragma unroll
         for (int r = 0; r < R; ++r)
@@ -402,8 +415,8 @@ __global__ __launch_bounds__(64 * W, R * T == 1 ? 4 : 1) void moe_down_kernel(Mo
             __hip_atomic_store(mine + i, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     if (a.parts == 1) return;
-    // The parts' sums are added, in their order, by the workgroup that arrives last: they are written through to where all XCDs
-    // see them before it arrives, and read past its caches.
+    // The parts' sums are added, in their order, by the workgroup that arrives last: they are written through
+    // to where all XCDs see them before it arrives, and read past its caches.
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
     __syncthreads();
     if (threadIdx.x == 0)
@@ -427,14 +440,17 @@ __global__ __launch_bounds__(64 * W, R * T == 1 ? 4 : 1) void moe_down_kernel(Mo
 
 // ---- few pairs: by dot products ----
 //
-// With a token or two the matrix cores' way reads activations for sixteen, four loads for each one of weights.  Here a lane keeps the
-// activations of its blocks in registers and takes its blocks of R rows, so that nothing but weights is asked for.  Every pair of a
-// token and a slot is worked off by itself (an expert that two tokens chose is read twice).
+// With a token or two the matrix cores' way reads activations for sixteen, four loads for each one of weights.
+// Here a lane keeps the activations of its blocks in registers and takes its blocks of R rows, so that nothing
+// but weights is asked for.  Every pair of a token and a slot is worked off by itself (an expert that two
+// tokens chose is read twice).
 
-// The dot product of a block's 32 weights with the lane's activations, x[k] inputs 2 k and 2 k + 1, added to `sum`.  int4: a nibble n
-// stands for n - 8 and goes in as bf16 128 + n (exact); `offset`, -136 times the sum of the activations, takes the rest away.
+// The dot product of a block's 32 weights with the lane's activations, x[k] inputs 2 k and 2 k + 1, added to
+// `sum`.  int4: a nibble n stands for n - 8 and goes in as bf16 128 + n (exact); `offset`, -136 times the sum
+// of the activations, takes the rest away.
 template <int FMT>
-__device__ __forceinline__ float block_dot(const uint4v &codes, uint32_t scale, const uint32_t (&x)[16], float offset, float sum) {
+__device__ __forceinline__ float block_dot(const uint4v &codes, uint32_t scale, const uint32_t (&x)[16], float offset,
+                                           float sum) {
     auto dot = [](uint32_t a, uint32_t b, float c) {
         return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(nvq_bf16x2, a), __builtin_bit_cast(nvq_bf16x2, b), c, false);
     };
@@ -487,7 +503,8 @@ __device__ __forceinline__ void load_block(const uint16_t *from, bool there, uin
 }
 // ... and a block's codes and scale, or zeros (which stand for zero, whatever the place holds).
 template <int FMT>
-__device__ __forceinline__ void load_weights(const uint8_t *q, const void *s, int64_t at, bool there, uint4v &codes, uint32_t &scale) {
+__device__ __forceinline__ void load_weights(const uint8_t *q, const void *s, int64_t at, bool there, uint4v &codes,
+                                             uint32_t &scale) {
     codes = uint4v{0, 0, 0, 0};
     scale = 0;
     if (there) {
@@ -533,8 +550,9 @@ __global__ __launch_bounds__(256) void moe_gate_up_dot_kernel(MoeArgs a) {
     if (lane < R) a.h[(int64_t)pair * a.F + f0 + lane] = float_to_bf16_bits(silu_mul_one(g, u));
 }
 
-// y of token blockIdx.y: the token's pairs as one product, whose blocks are those of h of all its slots, 256 B of them, shared out among
-// the lanes of four waves.  Each block's product is weighted with its pair's weight on its way into the row's sum.
+// y of token blockIdx.y: the token's pairs as one product, whose blocks are those of h of all its slots, 256 B
+// of them, shared out among the lanes of four waves.  Each block's product is weighted with its pair's weight
+// on its way into the row's sum.
 template <int FMT, int B, int R>
 __global__ __launch_bounds__(256) void moe_down_dot_kernel(MoeArgs a) {
     __shared__ float red[4][R];
@@ -568,23 +586,25 @@ __global__ __launch_bounds__(256) void moe_down_dot_kernel(MoeArgs a) {
     if (lane < R) red[w][lane] = mine;
     __syncthreads();
     if (w == 0 && lane < R)
-        store_global(a.y, a.y_dtype, (int64_t)m * a.K + row0 + lane, red[0][lane] + red[1][lane] + red[2][lane] + red[3][lane]);
+        store_global(a.y, a.y_dtype, (int64_t)m * a.K + row0 + lane,
+                     red[0][lane] + red[1][lane] + red[2][lane] + red[3][lane]);
 }
 
 constexpr int kColumns = 2;    // of a pass (rows_times_tokens)
 constexpr int kDownWaves = 8;  // of a workgroup of the second launch
 
-// The second launch in tiles of 64 outputs (32 with two token tiles), four row tiles reading a token's h at once, where that leaves a
-// workgroup to each compute unit: 4096 outputs of 32 experts 32 us against 44 microscaled, 38 against 47 int4; 2048 outputs, half
-// the workgroups: 26 against 17.
+// The second launch in tiles of 64 outputs (32 with two token tiles), four row tiles reading a token's h at
+// once, where that leaves a workgroup to each compute unit: 4096 outputs of 32 experts 32 us against 44
+// microscaled, 38 against 47 int4; 2048 outputs, half the workgroups: 26 against 17.
 bool wide_down(const MoeArgs &a, int parts) {
     return a.K / 16 % 4 == 0 && (int64_t)(a.K / 64) * parts >= device_cu_count();
 }
 
-// Workgroups that share a row tile of the second launch: as many as leave each wave a pass (over the experts that the tokens can
-// choose), or two passes where a pass would be more than two workgroups to each compute unit.  Two experts of 4096 outputs, 14
-// passes: 5.1 us with one, 6.2 with two, 7.7 with four; 23 of 28 experts of 992 outputs, 23 passes: both launches 18.2 with one,
-// 13.5 with two; 43 of 64 experts of 2048, 172 passes: 26.5 with one, 18.3 with two, 16.9 with four.
+// Workgroups that share a row tile of the second launch: as many as leave each wave a pass (over the experts
+// that the tokens can choose), or two passes where a pass would be more than two workgroups to each compute
+// unit.  Two experts of 4096 outputs, 14 passes: 5.1 us with one, 6.2 with two, 7.7 with four; 23 of 28 experts
+// of 992 outputs, 23 passes: both launches 18.2 with one, 13.5 with two; 43 of 64 experts of 2048, 172 passes:
+// 26.5 with one, 18.3 with two, 16.9 with four.
 int parts_of(const MoeArgs &a) {
     const int experts = a.E <= a.pairs ? a.E : a.pairs, passes = (a.F + 128 * kColumns - 1) / (128 * kColumns);
     const auto within = [](int v) { return v < 1 ? 1 : v < kMaxParts ? v : kMaxParts; };
@@ -599,10 +619,11 @@ template <int FMT, int T, bool SMALL>
 int launch_experts(const MoeArgs &a, hipStream_t st) {
     const int experts = a.E <= a.pairs ? a.E : a.pairs, tiles = a.F / 16, out_tiles = a.K / 16;
     const int cus = device_cu_count();
-    // Activations in registers: 2048 < K <= 4096, so that each of eight waves has most of its four columns; an expert for most
-    // workgroups that are launched (three choices for each on the average leave one in twenty without); eight tiles for each
-    // compute unit.  32 experts of 4096 x 1792, 32 tokens: 53 us against 68 microscaled, 65 against 73 int4.  Not for fewer
-    // inputs: 64 experts of 2048 x 1024 with half the columns to a wave took 24 us against 20.
+    // Activations in registers: K <= 4096, which is what eight waves of four columns hold, and K > 2048, so
+    // that each has most of them; an expert for most workgroups that are launched (three choices for each on
+    // the average leave one in twenty without); eight tiles for each compute unit.  32 experts of 4096 x 1792,
+    // 32 tokens: 53 us against 68 microscaled, 65 against 73 int4.  Not for fewer inputs: 64 experts of 2048 x
+    // 1024 with half the columns to a wave took 24 us against 20.
     bool resident = false;
     if constexpr (T == 1) {
         resident = a.K > 2048 && a.K <= 4096 && 3 * a.E <= a.pairs && (int64_t)a.E * tiles >= 8 * cus;
@@ -624,11 +645,20 @@ int launch_experts(const MoeArgs &a, hipStream_t st) {
     return NVQ_OK;
 }
 
-// Where dot products are worked off: up to eight tokens, few of whose experts are shared; K and a token's slots (blocks of h) that fit
-// the lanes.  us, by dot products and on the matrix cores: one token, eight of 64 experts of 2048 x 1024, int4 11.0 and 14.5,
-// microscaled 8.9 and 12.8; two tokens 17.5 and 23.5, 12.6 and 18.4; seven tokens, three of 40 experts of 1440 x 992 16.4 and 18.5;
-// eight tokens, eight of 64 experts of 2048 x 1024 microscaled 34.6 and 39.9, int4 54.3 and 47.4; eight tokens, four of 32 of 4096 x 1792
-// 70.6 and 64.5; eight tokens, two of eight 16.1 and 13.1; seven tokens whose slots are four blocks 12.5 and 9.7.
+// Where dot products are worked off: up to eight tokens, few of whose experts are shared; K and a token's slots
+// (blocks of h) that fit the lanes.  us, by dot products and on the matrix cores; tokens, experts of each and
+// in all, inputs, F:
+//                              int4          microscaled                                int4          microscaled
+//   1, 8 of 64, 2048, 1024  10.7  13.8      8.0  12.5      4, 8 of 32, 2048, 1024  29.3  29.9     19.1  23.9
+//   2, 8 of 64, 2048, 1024  18.7  20.8     13.0  17.8      4, 8 of 32, 4096, 1024  53.0  46.1     41.2  41.3
+//   3, 8 of 64, 2048, 1024  24.1  27.5     17.4  23.4      5, 4 of 20, 2048, 1024  21.2  20.7     15.2  17.7
+//   3, 4 of 12, 2048, 1024  12.4  17.0      9.6  12.6      6, 4 of 40, 2048, 1024  25.4  27.3     18.4  23.2
+//   4, 8 of 64, 2048, 1024  30.1  31.0     20.6  29.5      7, 3 of 40, 1440, 992   21.8  26.5     15.5  18.0
+//   4, 4 of 16, 2048, 768   13.4  16.4     10.8  14.1      8, 8 of 64, 2048, 1024  52.6  44.8     32.9  38.7
+//   4, 6 of 24, 1024, 512   10.4  12.2      8.6  11.0      8, 4 of 32, 4096, 1792  77.5  71.4     59.1  55.3
+// So int4 of up to four tokens and 2048 inputs, microscaled of all up to 2048.  (Three tokens of 4096 inputs
+// that choose all of twelve experts lose, int4 39.2 and 32.6; eight tokens, two of eight 16.1 and 13.1: more
+// pairs than experts; seven tokens whose slots are four blocks 12.5 and 9.7: fewer blocks than lanes.)
 template <int FMT>
 bool by_dot_products(const MoeArgs &a) {
     const int blocks = a.top_k * (a.F / 32);
@@ -658,8 +688,8 @@ template <int FMT>
 int launch_experts(const MoeArgs &a, hipStream_t st) {
     if (by_dot_products<FMT>(a)) return launch_experts_dot<FMT>(a, st);
     if (a.pairs <= 64 && a.M <= 16) return launch_experts<FMT, 1, true>(a, st);
-    // Two token tiles at once where most experts have more than 16 tokens: 16 experts of 4096 x 1792 microscaled, 16 tokens each on
-    // the average, 90 us against 101; with twelve 78 against 65.
+    // Two token tiles at once where most experts have more than 16 tokens: 16 experts of 4096 x 1792
+    // microscaled, 16 tokens each on the average, 90 us against 101; with twelve 78 against 65.
     return a.pairs >= 14 * a.E ? launch_experts<FMT, 2, false>(a, st) : launch_experts<FMT, 1, false>(a, st);
 }
 

@@ -6,7 +6,8 @@
 // hundred waves ask for everything at once; each leaves its partial logits in the workspace, and the workgroup that
 // arrives last (a counter that wraps to zero by itself) adds them in the order of the parts and chooses.
 //
-// Measured: one token of 64 experts, 2048 inputs 5.2 us (an empty launch 2.4); 32 tokens of 128 experts, 4096 inputs 7.8 us.
+// Measured: one token of 64 experts, 2048 inputs 5.2 us (an empty launch 2.4); 32 tokens of 128 experts, 4096
+// inputs 7.8 us.
 #include "mfma_act.h"
 
 namespace nvq {
@@ -56,9 +57,9 @@ __device__ __forceinline__ T over_group(T v, OP op) {
     return with_lane_xor<1>(v, op);
 }
 
-// The chosen experts of token m, by L lanes: lane i of them holds the logits of experts i, L + i .., P in all.  Their parts are
-// requested up to eight experts at once (one after the other they were 14 of the 25 us that 32 tokens and 128 experts took).
-// A choice is instructions on one compute unit, not bytes.
+// The chosen experts of token m, by L lanes: lane i of them holds the logits of experts i, L + i .., P in all.
+// Their parts are requested up to eight experts at once (one after the other they were 14 of the 25 us that 32
+// tokens and 128 experts took).  A choice is instructions on one compute unit, not bytes.
 template <int L, int P>
 __device__ __forceinline__ void choose(const RouteArgs &a, int m) {
     const int i = threadIdx.x & (L - 1);
@@ -75,7 +76,8 @@ __device__ __forceinline__ void choose(const RouteArgs &a, int m) {
             const float *const at = own + (int64_t)(in >> 4) * a.parts * a.M * 16 + (in & 15);
 #pragma unroll
             for (int p = 0; p < kRouteMaxParts; ++p)
-                v[j][p] = __hip_atomic_load(at + (int64_t)(p < a.parts ? p : 0) * a.M * 16, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                v[j][p] = __hip_atomic_load(at + (int64_t)(p < a.parts ? p : 0) * a.M * 16, __ATOMIC_RELAXED,
+                                            __HIP_MEMORY_SCOPE_AGENT);
         }
 #pragma unroll
         for (int j = 0; j < kAtOnce; ++j) {
@@ -137,7 +139,8 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(RouteArgs a) {
     const int all_cols = a.K / 32, col0 = part * a.cols;
     const int col1 = col0 + a.cols < all_cols ? col0 + a.cols : all_cols;
 
-    const char *const r = reinterpret_cast<const char *>(a.router) + (int64_t)(e0 + n < a.E ? e0 + n : a.E - 1) * a.K * 2 + kb * 16;
+    const char *const r =
+        reinterpret_cast<const char *>(a.router) + (int64_t)(e0 + n < a.E ? e0 + n : a.E - 1) * a.K * 2 + kb * 16;
     const char *x[T];
     float4v sum[T];
 #pragma unroll
@@ -146,7 +149,8 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(RouteArgs a) {
         x[t] = reinterpret_cast<const char *>(a.x) + (int64_t)(m < a.M ? m : 0) * a.K * 2 + kb * 16;
         sum[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
     }
-    // Two columns at a time, a line of 128 bytes of every row.  (K of an odd number of columns: the last one by itself.)
+    // Two columns at a time, a line of 128 bytes of every row.  (K of an odd number of columns: the last one by
+    // itself.)
     for (int c = col0 + 2 * w; c < col1; c += 2 * kRouteWaves) {
         const bool both = c + 1 < col1;  // (uniform)
         uint4v b[2] = {}, v[2][T] = {};
@@ -184,9 +188,9 @@ __global__ __launch_bounds__(kRouteThreads) void moe_route_kernel(RouteArgs a) {
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this wave's partial logits are written
     __syncthreads();
     if (threadIdx.x == 0) {
-        // The workgroup's partial logits are written through to where all XCDs see them (agent-scope stores, waited for)
-        // before it arrives; the last one's loads are of that scope too and pass its caches by.  So no cache has to be written
-        // back or emptied here, as a fence of that scope would.
+        // The workgroup's partial logits are written through to where all XCDs see them (agent-scope stores,
+        // waited for) before it arrives; the last one's loads are of that scope too and pass its caches by.  So
+        // no cache has to be written back or emptied here, as a fence of that scope would.
         const uint32_t before = __hip_atomic_fetch_add(a.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         last = before == gridDim.x - 1;
         if (last) __hip_atomic_store(a.arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -256,8 +260,9 @@ extern "C" int nvq_moe_route(const uint16_t *x_bf16, const uint16_t *router_bf16
     a.cols = ((cols + parts - 1) / parts + 1) / 2 * 2;  // (whole lines)
     a.parts = (cols + a.cols - 1) / a.cols;
     const hipStream_t st = (hipStream_t)stream;
-    // Lanes per token in the choice: of many tokens four share a wave, sixteen lanes each (32 tokens of 128 experts 7.8 us against 9.4,
-    // of 6 experts 5.5 against 7.7); few tokens have a wave each (one of 256 experts 6.6 against 8.5, of 64 5.2 against 5.9).
+    // Lanes per token in the choice: of many tokens four share a wave, sixteen lanes each (32 tokens of 128
+    // experts 7.8 us against 9.4, of 6 experts 5.5 against 7.7); few tokens have a wave each (one of 256
+    // experts 6.6 against 8.5, of 64 5.2 against 5.9).
     if (M <= 8) return launch_route<1, 64>(a, st);
     return M <= 16 ? launch_route<1, 16>(a, st) : launch_route<2, 16>(a, st);
 }

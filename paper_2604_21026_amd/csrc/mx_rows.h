@@ -1,13 +1,14 @@
 // Products of 16-row tiles of 4-bit weights with bf16 activations of 16-token tiles on the matrix cores, for
 // both weight formats (nvq_gemv_mxfp4, nvq_moe_experts).
 //
-// A wave takes columns of 128 inputs: lane (n, kb) = (lane % 16, lane / 16) loads the 16 bytes of block 4c + kb of row n.
-// Microscaled: MFMA i (16x16x32) takes dword i of every lane's block, eight codes, which become bf16 values, scale
-// and all, in one instruction per two (exact: two bits of significand and a power of two); the four MFMAs add into the
-// same sums.  Which inputs stand at which place of a product is free: the activations follow (lane (m, kb) supplies inputs
-// 32 kb + 8 i .. + 7 of its column), and a lane needs its own block's scale alone.
-// int4: each block's product is scaled on its way to the sum, so an MFMA is one block: a 4x4 transpose across the lane-rows
-// gives the lane dword kb of the blocks 4c .. 4c + 3 (mfma_act.h, as in the small-batch kernels of the int4 layers).
+// A wave takes columns of 128 inputs: lane (n, kb) = (lane % 16, lane / 16) loads the 16 bytes of block 4c + kb
+// of row n.  Microscaled: MFMA i (16x16x32) takes dword i of every lane's block, eight codes, which become bf16
+// values, scale and all, in one instruction per two (exact: two bits of significand and a power of two); the
+// four MFMAs add into the same sums.  Which inputs stand at which place of a product is free: the activations
+// follow (lane (m, kb) supplies inputs 32 kb + 8 i .. + 7 of its column), and a lane needs its own block's
+// scale alone. int4: each block's product is scaled on its way to the sum, so an MFMA is one block: a 4x4
+// transpose across the lane-rows gives the lane dword kb of the blocks 4c .. 4c + 3 (mfma_act.h, as in the
+// small-batch kernels of the int4 layers).
 #pragma once
 
 #include "mfma_act.h"
@@ -16,7 +17,8 @@ namespace nvq {
 
 #if defined(__HIPCC__)
 
-// Codes of C neighbouring columns of a row tile, a lane's 16 bytes of each, and its row's scales of 4 Q blocks, Q columns.
+// Codes of C neighbouring columns of a row tile, a lane's 16 bytes of each, and its row's scales of 4 Q blocks,
+// Q columns.
 template <int C>
 struct Codes {
     uint4v w[C];
@@ -43,14 +45,15 @@ __device__ __forceinline__ RowAt row_at(const uint8_t *q, const void *s, int64_t
                  reinterpret_cast<const char *>(s) + row * G * scale_bytes<FMT>()};
 }
 
-// Columns col .. of that many.  (A row's line of 128 bytes of codes is two columns: asked for together it is fetched once.)
+// Columns col .. of that many.  (A row's line of 128 bytes of codes is two columns: asked for together it is
+// fetched once.)
 template <int C>
 __device__ __forceinline__ void load_codes(Codes<C> &c, const RowAt &at, int col, int kb) {
 #pragma unroll
     for (int b = 0; b < C; ++b) c.w[b] = load_stream(at.q + 4 * (col + b) + kb);
 }
-// (A line of scales serves 32 columns of microscaled rows; asked for a column or two at a time it was fetched again every time, as many
-// bytes as the codes are.)
+// (A line of scales serves 32 columns of microscaled rows; asked for a column or two at a time it was fetched
+// again every time, as many bytes as the codes are.)
 template <int FMT, int Q>
 __device__ __forceinline__ void load_scales(Scales<FMT, Q> &c, const RowAt &at, int col) {
     constexpr int kWords = FMT == NVQ_FMT_MXFP4 ? Q : 2 * Q, kWide = kWords < 4 ? kWords : 4;
@@ -65,7 +68,8 @@ __device__ __forceinline__ void load_scales(Scales<FMT, Q> &c, const RowAt &at, 
     }
 }
 
-// Scales of zero for the first `blocks` blocks (uniform), whose activations are zero: values beyond bf16 would make them NaN.
+// Scales of zero for the first `blocks` blocks (uniform), whose activations are zero: values beyond bf16 would
+// make them NaN.
 template <int FMT, int Q>
 __device__ __forceinline__ void clear_scales(Scales<FMT, Q> &c, int blocks) {
     constexpr int kWords = FMT == NVQ_FMT_MXFP4 ? Q : 2 * Q;
@@ -94,7 +98,8 @@ __device__ __forceinline__ void load_last(Codes<1> &c, Scales<FMT, 1> &sc, const
     }
 }
 
-// 2^(byte - 127) of byte kb of the word, as the conversions take it (they look at the exponent alone, 0 standing for 2^-127).
+// 2^(byte - 127) of byte kb of the word, as the conversions take it (they look at the exponent alone, 0
+// standing for 2^-127).
 __device__ __forceinline__ float mx_scale_of(uint32_t four, int kb) {
     return __uint_as_float(__builtin_amdgcn_ubfe(four, 8 * kb, 8) << 23);
 }
@@ -202,7 +207,8 @@ __device__ __forceinline__ void last_columns(const RowAt (&at)[R], const char *c
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 raw[t][i] = uint4v{0, 0, 0, 0};
-                if ((FMT == NVQ_FMT_MXFP4 ? kb : i) < blocks) raw[t][i] = *as_global<uint4v>(x[t] + (size_t)c * 256 + piece_at<FMT>(i, kb));
+                if ((FMT == NVQ_FMT_MXFP4 ? kb : i) < blocks)
+                    raw[t][i] = *as_global<uint4v>(x[t] + (size_t)c * 256 + piece_at<FMT>(i, kb));
             }
         bf16x8 a[T][4];
 #pragma unroll
@@ -211,9 +217,11 @@ __device__ __forceinline__ void last_columns(const RowAt (&at)[R], const char *c
     }
 }
 
-// A column that counts for nothing: codes of zero, or scales of zero, and activations of zero (an infinite one would make them NaN).
+// A column that counts for nothing: codes of zero, or scales of zero, and activations of zero (an infinite one
+// would make them NaN).
 template <int FMT, int R, int T, int C, int Q>
-__device__ __forceinline__ void clear_column(Codes<C> (&col)[R], uint4v (&raw)[C][T][4], int b, Scales<FMT, Q> (&sc)[R], int qb) {
+__device__ __forceinline__ void clear_column(Codes<C> (&col)[R], uint4v (&raw)[C][T][4], int b,
+                                             Scales<FMT, Q> (&sc)[R], int qb) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         if constexpr (FMT == NVQ_FMT_MXFP4)
@@ -227,12 +235,14 @@ __device__ __forceinline__ void clear_column(Codes<C> (&col)[R], uint4v (&raw)[C
         for (int i = 0; i < 4; ++i) raw[b][t][i] = uint4v{0, 0, 0, 0};
 }
 
-// sum[r][t] += R row tiles times T token tiles over K = 32 G inputs, shared out over `step` waves (this one: number `first`)
-// in passes of Q columns: their scales at once, their codes and activations C columns at a time, requested while the C before are
-// multiplied.  A last pass of fewer columns takes the last Q, and those that it shares with the one before count for nothing: they
-// are left out (kSkip) or cleared.  (Left out in tiles of two steps or two token tiles, the branches cost up to a tenth, 8 tokens of
-// 14336 x 4096 10.0 and 11.0 us; cleared in the others, up to 7 %.)  x[t]: the lane's token of tile t (bf16); a product keeps tokens
-// apart, so a lane without one may take any.  (Loading nothing in such lanes was no faster.)  Every lane of the wave calls it.
+// sum[r][t] += R row tiles times T token tiles over K = 32 G inputs, shared out over `step` waves (this one:
+// number `first`) in passes of Q columns: their scales at once, their codes and activations C columns at a
+// time, requested while the C before are multiplied.  A last pass of fewer columns takes the last Q, and those
+// that it shares with the one before count for nothing: they are left out (kSkip) or cleared.  (Left out in
+// tiles of two steps or two token tiles, the branches cost up to a tenth, 8 tokens of 14336 x 4096 10.0 and
+// 11.0 us; cleared in the others, up to 7 %.)  x[t]: the lane's token of tile t (bf16); a product keeps tokens
+// apart, so a lane without one may take any.  (Loading nothing in such lanes was no faster.)  Every lane of the
+// wave calls it.
 template <int FMT, int R, int T, int C, int Q>
 __device__ __forceinline__ void rows_times_tokens(const RowAt (&at)[R], const char *const (&x)[T], int G, int first,
                                                   int step, float4v (&sum)[R][T]) {

@@ -8,8 +8,8 @@
 // maximum with two or three data-parallel moves; the codes leave as whole words, the scales of four blocks
 // as one.
 //
-// Measured at 14336 x 4096: fp32 to codes 42.7 us (6.2 TB/s; 49.8 with one load in flight per lane, 43.8 with two or eight),
-// codes to bf16 22.4 (6.6 TB/s); 8 x 2048 2.4 us each, an empty launch.
+// Measured at 14336 x 4096: fp32 to codes 42.7 us (6.2 TB/s; 49.8 with one load in flight per lane, 43.8 with
+// two or eight), codes to bf16 22.4 (6.6 TB/s); 8 x 2048 2.4 us each, an empty launch.
 #include "mfma_act.h"
 
 namespace nvq {

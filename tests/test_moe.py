@@ -523,7 +523,8 @@ def positive(fmt, rows, K, rng):
 
 
 NOT_FINITE = [
-    # products of tiles: both launches' last pass meets a column again; in the second one also with several workgroups to a tile, wide tiles
+    # products of tiles: both launches' last pass meets a column again; in the second one also with several
+    # workgroups to a tile, wide tiles
     (5, 2, 2, 416, 416), (20, 4, 2, 416, 672), (32, 16, 8, 4096, 288), (9, 6, 6, 4160, 1056), (20, 60, 2, 416, 416),
     # the first launch with the activations in registers, whose last waves' blocks begin before their share
     (5, 3, 3, 2144, 11008), (22, 4, 1, 2144, 8192),
@@ -598,12 +599,12 @@ def test_experts_with_weights_beyond_the_range(fmt, M, E, k, K, F):
 
 # ---- the general lookup of tokens (more than 16 tokens or 64 pairs) where the first launch's grid is pairs, not experts ----
 @gpu
-@pytest.mark.parametrize("M,E,k,K,F", [(20, 100, 3, 160, 96), (32, 300, 8, 96, 64), (17, 40, 2, 128, 64), (32, 512, 15, 64, 96), (25, 130, 5, 288, 32),
-                                       (9, 160, 16, 96, 32)])
+@pytest.mark.parametrize("M,E,k,K,F", [(20, 100, 3, 160, 96), (32, 300, 8, 96, 64), (17, 40, 2, 128, 64),
+                                       (32, 512, 15, 64, 96), (25, 130, 5, 288, 32), (9, 160, 16, 96, 32)])
 @pytest.mark.parametrize("fmt", ["int4", "mxfp4"])
 def test_many_tokens_of_more_experts_than_pairs(M, E, k, K, F, fmt):
-    """Few experts of many, shared by tokens in different groups of 64 pairs; slots out of range, an expert twice, tokens without any; a
-    workspace of NaN."""
+    """Few experts of many, shared by tokens in different groups of 64 pairs; slots out of range, an expert twice,
+    tokens without any; a workspace of NaN."""
     assert M * k < E and (M > 16 or M * k > 64)
     rng = np.random.default_rng(E)
     ex, values = make(fmt, E, K, F, E)
@@ -624,7 +625,8 @@ def test_many_tokens_of_more_experts_than_pairs(M, E, k, K, F, fmt):
 
 # few tokens of 65 to 128 experts, nine to sixteen of 129 to 256
 @gpu
-@pytest.mark.parametrize("M,E,K,k", [(1, 128, 4096, 8), (3, 100, 320, 7), (8, 65, 96, 16), (9, 256, 288, 8), (16, 140, 2048, 16), (13, 129, 64, 1)])
+@pytest.mark.parametrize("M,E,K,k", [(1, 128, 4096, 8), (3, 100, 320, 7), (8, 65, 96, 16), (9, 256, 288, 8),
+                                     (16, 140, 2048, 16), (13, 129, 64, 1)])
 @pytest.mark.parametrize("renorm", [True, False])
 def test_route_of_exact_logits_with_ties_at_other_sizes(M, E, K, k, renorm):
     test_route_of_exact_logits_with_ties(M, E, K, k, renorm)
