@@ -350,7 +350,7 @@ def _run_plain(st):
         z, index = torch.sort(st["logits"].float(), dim=1, descending=True, stable=True)
         temperature, top_k, top_p, min_p = (None if a is None else a.unsqueeze(1) for a in st["ask"])
         greedy = temperature <= 0
-        w = torch.exp((z - z[:, :1]).double() / torch.where(greedy, 1.0, temperature.double()))
+        w = torch.exp((z.double() - z[:, :1].double()) / torch.where(greedy, 1.0, temperature.double()))
         rank = torch.arange(z.shape[1], device=DEV)
         keep = (rank == 0) | ~greedy
         if top_k is not None:
