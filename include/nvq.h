@@ -625,6 +625,168 @@ int nvq_moe_experts(const nvq_experts *experts, const uint16_t *x_bf16, const in
                     size_t workspace_bytes, void *stream);
 
 /*
+ * What a decode step does between its linear layers: a paged cache of keys and
+ * values, attention over it, adapters beside a layer, the choice of the next token.
+ *
+ * nvq_cache -- keys and values of many sequences in pages of page_size tokens, a
+ * pool that all sequences share.  A table [B][table_width] names the pages of each
+ * sequence in order: position p of sequence b is slot p % page_size of page
+ * table[b][p / page_size].
+ *   k       [pages][heads][page_size][head_dim]
+ *   v       [pages][heads][page_size / 8][head_dim][8]: eight tokens of a channel
+ *           side by side, as the products over tokens take them
+ *   scales  NVQ_E4M3: [pages][heads][2][page_size] bytes (of keys, of values), 8-byte
+ *           aligned; else not looked at
+ *   dtype   NVQ_BF16, or NVQ_E4M3: 8-bit floating point (sign, four bits of exponent,
+ *           three of mantissa, no infinities) times 2^(byte - 127), one byte per token
+ *           and head, the smallest power of two that brings the largest magnitude to
+ *           448 or less, at least byte 1; values ties-to-even.  A token and head that
+ *           holds an infinity or a NaN gets byte 255 and zero codes: all its values
+ *           count as NaN.
+ * page_size is a power of two, 8 to NVQ_MAX_PAGE; head_dim a multiple of 32 up to
+ * NVQ_MAX_HEAD_DIM; k and v are 16-byte aligned.  Of a token whose page number is
+ * outside [0, pages) nothing is stored, and nothing is read.
+ *
+ * nvq_cache_append -- T tokens, token t being position positions[t] of sequence
+ * sequences[t] (NULL: of sequence t), into the cache, their keys and queries turned by
+ * position first: with cos_sin [angles][rot] fp32 (rot / 2 cosines, then the sines of
+ * the same angles) the pair (a, b) of channels j and j + rot / 2 (interleaved = 1: 2 j
+ * and 2 j + 1), j < rot / 2, becomes (a cos_j - b sin_j, b cos_j + a sin_j) of row
+ * positions[t], every product and sum rounded to binary32 and the result to bf16 once;
+ * channels from rot on stay as they are, and all without cos_sin.  An e4m3 cache holds
+ * what these bf16 values become.
+ *   q       [T][H][head_dim] bf16, q_stride elements from token to token, or NULL with
+ *           H = 0; q_out [T][H][head_dim], may be q where q_stride = H * head_dim
+ *   k, v    [T][heads][head_dim], k_stride and v_stride elements from token to token
+ *           (strides: multiples of 8, at least a token's row)
+ * A token whose place is not in the cache (sequence outside [0, B), position below 0 or
+ * outside the table or, with cos_sin, outside its rows, page outside the pool) is
+ * padding: nothing is written for it, its q_out included.  No two tokens of a call may
+ * have the same place.
+ *
+ * nvq_cache_read -- the reverse: k, v [T][heads][head_dim] bf16 of the tokens named as
+ * above; e4m3 values are exact in bf16 down to its smallest.  Zeros for a token whose
+ * place is not in the cache.
+ * T <= 2^24, T * (H + 2 heads) <= 2^26, H <= NVQ_MAX_HEADS; table, sequences, positions 4-byte aligned.
+ */
+enum { NVQ_E4M3 = 2 }; /* nvq_cache.dtype, beside NVQ_BF16 */
+#define NVQ_MAX_PAGE 1024
+#define NVQ_MAX_HEAD_DIM 256
+#define NVQ_MAX_HEADS 1024
+typedef struct nvq_cache {
+    void *k;
+    void *v;
+    uint8_t *scales;
+    int32_t dtype; /* NVQ_BF16 | NVQ_E4M3 */
+    int32_t pages, heads, page_size, head_dim;
+} nvq_cache;
+int nvq_cache_append(const nvq_cache *cache, const int32_t *table, int B, int table_width,
+                     const int32_t *sequences, const int32_t *positions, int T,
+                     const uint16_t *q, int64_t q_stride, int H, uint16_t *q_out,
+                     const uint16_t *k, int64_t k_stride, const uint16_t *v, int64_t v_stride,
+                     const float *cos_sin, int angles, int rot, int interleaved, void *stream);
+int nvq_cache_read(const nvq_cache *cache, const int32_t *table, int B, int table_width,
+                   const int32_t *sequences, const int32_t *positions, int T,
+                   uint16_t *k, uint16_t *v, void *stream);
+
+/*
+ * nvq_attention -- one new token of each of B sequences over the cache.  With n =
+ * lengths[b] tokens in the cache (the new one among them, if it has been appended),
+ * query head h reading key head h / (H / heads), and over the positions t in
+ * [max(0, n - window), n) (window = 0: all) whose page is in the pool:
+ *   s_t = scale * q[b][h] . k[t];  softcap > 0: s_t = softcap * tanh(s_t / softcap)
+ *   out[b][h] = sum_t exp(s_t - max s) v[t] / sum_t exp(s_t - max s)
+ * Scores, maxima, sums in fp32; the weights enter the product with v as two bf16 values
+ * each (16 bits); out is rounded once (out_dtype).  A sequence without such a position
+ * (or with scores of minus infinity alone) gets zeros.  What the cache holds at other
+ * positions does not matter, NaN included.  lengths below 0 count as 0, those past the
+ * table's width as the width.  The same call gives the same bits.
+ *   q       [B][H][head_dim] bf16, q_stride elements from sequence to sequence (a
+ *           multiple of 8)
+ *   out     [B][H][head_dim] f32 or bf16
+ *   lse     NULL, or [B][H] fp32: log(sum_t exp(s_t)), minus infinity without positions
+ *   workspace  nvq_attention_workspace_bytes(cache, B, H) bytes, 256-byte aligned.  Its
+ *              first NVQ_ATTENTION_CLEAR_BYTES must be zero before the first call and are
+ *              zero again after every call: clear it once, then use it for any number of
+ *              calls with caches of this head_dim and of these or fewer heads and
+ *              sequences, one after the other (not by two that overlap).
+ * B <= NVQ_ATTENTION_MAX_B, H a multiple of heads up to NVQ_MAX_HEADS; table_width *
+ * page_size <= 2^30; scale finite, window >= 0, softcap >= 0 and finite.
+ * nvq_attention_workspace_bytes looks at the sizes alone, 0 where they are invalid.
+ */
+#define NVQ_ATTENTION_MAX_B 4096
+#define NVQ_ATTENTION_CLEAR_BYTES 4096
+size_t nvq_attention_workspace_bytes(const nvq_cache *cache, int B, int H);
+int nvq_attention(const nvq_cache *cache, const uint16_t *q, int64_t q_stride, int H,
+                  const int32_t *table, int B, int table_width, const int32_t *lengths, float scale,
+                  int window, float softcap, void *out, int out_dtype, float *lse, void *workspace,
+                  size_t workspace_bytes, void *stream);
+
+/*
+ * nvq_sample -- the next token of each of M rows of logits from one given random number
+ * per row.  The tokens of a row in descending order of their logits, the lowest index
+ * first among equal ones, have the weights w_i = exp((logit_i - max) / temperature);
+ * what is kept is the beginning of that order that satisfies all of
+ *   top_k > 0          the first top_k tokens
+ *   top_p < 1          those before which the weights sum to less than top_p of the sum
+ *                      over the first top_k (over all without top_k)
+ *   min_p > 0          those with w_i >= min_p
+ * and the first token always.  ids[m] = the first token at which the running sum of the
+ * kept weights exceeds u[m] times their sum (u below 0 or NaN counts as 0, from 1 on the
+ * last kept one is taken).  A temperature that is not above 0 takes the first token.
+ * Weights are fixed point with 43 bits after the point, from fp64; sums of them are
+ * exact, so the same call gives the same tokens.  NaN and minus infinity are never
+ * chosen and do not count; plus infinity is chosen before all; a row without a token to
+ * choose gets -1.
+ *   logits  [M][V] f32 or bf16 (dtype), ld >= V elements from row to row; 4-byte
+ *           (bf16: 2-byte) aligned
+ *   u       [M] fp32;  temperature, top_p, min_p [M] fp32, top_k [M] int32, device, each
+ *           may be NULL: 1, 1, 0, 0
+ *   ids     [M] int32, written
+ *   workspace  nvq_sample_workspace_bytes(M, V) bytes, 256-byte aligned.  Its first
+ *              NVQ_SAMPLE_CLEAR_BYTES must be zero before the first call and are zero
+ *              again after every call: clear it once, then use it for any number of calls
+ *              of these or smaller M and V, one after the other (not by two that overlap).
+ * 1 <= M <= NVQ_SAMPLE_MAX_M, 1 <= V <= NVQ_SAMPLE_MAX_V.  nvq_sample_workspace_bytes
+ * returns 0 for sizes out of range.
+ */
+#define NVQ_SAMPLE_MAX_M 1024
+#define NVQ_SAMPLE_MAX_V (1 << 20)
+#define NVQ_SAMPLE_CLEAR_BYTES 4096
+size_t nvq_sample_workspace_bytes(int M, int V);
+int nvq_sample(const void *logits, int dtype, int64_t ld, int M, int V, const float *u,
+               const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+               int32_t *ids, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * nvq_adapters_add -- low-rank adapters beside a layer of N outputs, each token its own:
+ *   out[m] = y[m] + scales[e] * B_e (A_e x[m]),  e = ids[m]
+ * all sums in fp32, A_e x not rounded, out rounded once (dtype).  A token whose id is
+ * outside [0, n) has no adapter: out[m] = y[m].  A token's result does not change by a
+ * value of another token or of an adapter that it does not use.  Any M >= 1; no atomic
+ * additions: the same call gives the same bits.
+ *   adapters  a [n][R][K], b [n][N][R] bf16, scales [n] fp32 or NULL (1)
+ *   x_bf16 [M][K], ids [M]; y, out [M][N] f32 or bf16 (dtype), out may be y itself and
+ *   overlaps nothing else
+ *   workspace  nvq_adapters_workspace_bytes(adapters, M) bytes, 256-byte aligned, scratch
+ *              (whatever it holds), for one call at a time
+ * K % 32 == 0, K <= NVQ_MAX_K, R % 8 == 0, R <= NVQ_MAX_RANK, N <= 2^24, n <= 2^16, M <=
+ * 2^16; a, b, x, y, out 16-byte aligned.  nvq_adapters_workspace_bytes looks at the
+ * sizes alone, 0 where they are invalid.
+ */
+#define NVQ_MAX_RANK 256
+typedef struct nvq_adapters {
+    const uint16_t *a;
+    const uint16_t *b;
+    const float *scales;
+    int32_t n, K, N, R;
+} nvq_adapters;
+size_t nvq_adapters_workspace_bytes(const nvq_adapters *adapters, int M);
+int nvq_adapters_add(const nvq_adapters *adapters, const uint16_t *x_bf16, const int32_t *ids, int M,
+                     const void *y, void *out, int dtype, void *workspace, size_t workspace_bytes,
+                     void *stream);
+
+/*
  * Measurement helpers (not part of the method): a streaming read that sums a
  * buffer into `out` (8 bytes) and a plain copy, used to find the HBM ceiling
  * of the machine and to calibrate profiler byte counters.  bytes % 16 == 0.

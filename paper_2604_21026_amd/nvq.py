@@ -23,6 +23,7 @@ MAX_M = 32
 PLAN_ORDERED = 1
 IN_PLAIN, IN_RMSNORM, IN_SILU_MUL = 0, 1, 2
 FMT_INT4, FMT_MXFP4 = 0, 1
+E4M3 = 2
 
 EXPORTS = (
     "nvq_status_string", "nvq_last_hip_error", "nvq_pack_int4", "nvq_quant_act_i8",
@@ -34,6 +35,8 @@ EXPORTS = (
     "nvq_dequant_bf16", "nvq_gemm_w4a16", "nvq_gemm_describe", "nvq_rms_norm_bf16", "nvq_silu_mul_bf16", "nvq_precision_from_scores", "nvq_token_norms", "nvq_mcap_scores", "nvq_stream_read", "nvq_stream_copy",
     "nvq_quant_mxfp4", "nvq_dequant_mxfp4", "nvq_gemv_mxfp4", "nvq_gemm_mxfp4",
     "nvq_moe_route_workspace_bytes", "nvq_moe_route", "nvq_moe_workspace_bytes", "nvq_moe_experts",
+    "nvq_cache_append", "nvq_cache_read", "nvq_attention_workspace_bytes", "nvq_attention",
+    "nvq_sample_workspace_bytes", "nvq_sample", "nvq_adapters_workspace_bytes", "nvq_adapters_add",
 )
 
 
@@ -58,6 +61,18 @@ class ExpertsStruct(C.Structure):
     _fields_ = [("gate_up", C.c_void_p), ("gate_up_scales", C.c_void_p), ("down", C.c_void_p),
                 ("down_scales", C.c_void_p), ("format", C.c_int32), ("E", C.c_int32), ("K", C.c_int32),
                 ("F", C.c_int32)]
+
+
+class CacheStruct(C.Structure):
+    """Mirror of `nvq_cache`."""
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("scales", C.c_void_p), ("dtype", C.c_int32), ("pages", C.c_int32),
+                ("heads", C.c_int32), ("page_size", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class AdaptersStruct(C.Structure):
+    """Mirror of `nvq_adapters`."""
+    _fields_ = [("a", C.c_void_p), ("b", C.c_void_p), ("scales", C.c_void_p), ("n", C.c_int32), ("K", C.c_int32),
+                ("N", C.c_int32), ("R", C.c_int32)]
 
 
 _lib = None
@@ -136,6 +151,17 @@ def lib() -> C.CDLL:
     L.nvq_moe_workspace_bytes.argtypes = [vp, ci, ci]
     L.nvq_moe_workspace_bytes.restype = sz
     L.nvq_moe_experts.argtypes = [vp, vp, vp, vp, ci, ci, vp, ci, vp, sz, vp]
+    L.nvq_cache_append.argtypes = [vp, vp, ci, ci, vp, vp, ci, vp, i64, ci, vp, vp, i64, vp, i64, vp, ci, ci, ci, vp]
+    L.nvq_cache_read.argtypes = [vp, vp, ci, ci, vp, vp, ci, vp, vp, vp]
+    L.nvq_attention_workspace_bytes.argtypes = [vp, ci, ci]
+    L.nvq_attention_workspace_bytes.restype = sz
+    L.nvq_attention.argtypes = [vp, vp, i64, ci, vp, ci, ci, vp, C.c_float, ci, C.c_float, vp, ci, vp, vp, sz, vp]
+    L.nvq_sample_workspace_bytes.argtypes = [ci, ci]
+    L.nvq_sample_workspace_bytes.restype = sz
+    L.nvq_sample.argtypes = [vp, ci, i64, ci, ci, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.nvq_adapters_workspace_bytes.argtypes = [vp, ci]
+    L.nvq_adapters_workspace_bytes.restype = sz
+    L.nvq_adapters_add.argtypes = [vp, vp, vp, ci, vp, vp, ci, vp, sz, vp]
     for f in ("nvq_pack_int4", "nvq_quant_act_i8", "nvq_gemv_w4a16", "nvq_gemv_w4a8",
               "nvq_quant_mxfp4", "nvq_dequant_mxfp4", "nvq_gemv_mxfp4", "nvq_gemm_mxfp4", "nvq_moe_route",
               "nvq_moe_experts",
@@ -715,6 +741,222 @@ def moe_experts(experts: Experts, x: torch.Tensor, ids: torch.Tensor, weights: t
                                  _y_dtype(y.dtype), _here(workspace, torch.uint8, "workspace"), workspace.numel(),
                                  _stream()), "nvq_moe_experts")
     return y
+
+
+class Cache:
+    """A paged cache of keys and values (`nvq_cache` plus the tensors it points to): k [pages,heads,page_size,head_dim],
+    v [pages,heads,page_size/8,head_dim,8], both bf16, or both u8 (e4m3 codes) with scales u8 [pages,heads,2,page_size]."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, scales: Optional[torch.Tensor] = None):
+        if k.dim() != 4:
+            raise ValueError("shape mismatch")
+        pages, heads, size, D = k.shape
+        if k.dtype not in (torch.bfloat16, torch.uint8):
+            raise ValueError("k must be bfloat16 or uint8 (e4m3 codes), got %s" % k.dtype)
+        if (scales is None) != (k.dtype == torch.bfloat16):
+            raise ValueError("scales belong to uint8 (e4m3 codes), and only to them")
+        if size % 8 or tuple(v.shape) != (pages, heads, size // 8, D, 8) or (
+                scales is not None and tuple(scales.shape) != (pages, heads, 2, size)):
+            raise ValueError("shape mismatch")
+        self.keep = (k, v, scales)
+        if any(t is not None and t.device != k.device for t in self.keep):
+            raise ValueError("tensors on different devices")
+        self.k, self.v, self.scales = k, v, scales
+        self.pages, self.heads, self.page_size, self.head_dim, self.device = pages, heads, size, D, k.device
+        self.struct = CacheStruct(_dev(k, k.dtype, "k"), _dev(v, k.dtype, "v"),
+                                  None if scales is None else _dev(scales, torch.uint8, "scales"),
+                                  BF16 if scales is None else E4M3, pages, heads, size, D)
+        self.address = C.addressof(self.struct)
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, page_size: int, head_dim: int, dtype=torch.bfloat16, device="cuda"):
+        """A cache of new memory; dtype bfloat16, or uint8 for e4m3 codes."""
+        k = torch.empty((pages, heads, page_size, head_dim), dtype=dtype, device=device)
+        v = torch.empty((pages, heads, page_size // 8, head_dim, 8), dtype=dtype, device=device)
+        s = torch.empty((pages, heads, 2, page_size), dtype=torch.uint8, device=device) if dtype == torch.uint8 else None
+        return cls(k, v, s)
+
+    def workspace(self, B: int, H: int) -> torch.Tensor:
+        """The workspace of attention for up to B sequences of H query heads: cleared here, and by every call after
+        its use."""
+        need = lib().nvq_attention_workspace_bytes(self.address, B, H)
+        if need == 0:
+            raise NvqError(2, "nvq_attention_workspace_bytes")
+        return _cleared(need, self.device)
+
+
+def _cleared(nbytes: int, device) -> torch.Tensor:
+    """A workspace whose beginning (4096 bytes, what attention and sample ask for) is zero."""
+    t = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    t[:4096].zero_()
+    return t
+
+
+def _rows(t: torch.Tensor, heads: int, D: int, name: str):
+    """The address of bf16 [T,heads,D] whose tokens may lie apart, and their distance in elements."""
+    if not t.is_cuda or t.dtype != torch.bfloat16:
+        raise ValueError("%s must be a bfloat16 device tensor" % name)
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != D:
+        raise ValueError("%s: shape mismatch" % name)
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != D):
+        raise ValueError("%s: the heads of a token must lie side by side" % name)
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError("%s is on device %d, the current device is %d" % (name, t.get_device(), torch.cuda.current_device()))
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else heads * D
+
+
+def _places(cache: Cache, table, positions, sequences):
+    """Arguments that name the tokens of cache_append and cache_read."""
+    if cache.device.index != torch.cuda.current_device():
+        raise ValueError("the cache is on %s, the current device is %d" % (cache.device, torch.cuda.current_device()))
+    if table.dim() != 2 or positions.dim() != 1 or (sequences is not None and sequences.shape != positions.shape):
+        raise ValueError("shape mismatch")
+    return (cache.address, _here(table, torch.int32, "table"), table.shape[0], table.shape[1],
+            None if sequences is None else _here(sequences, torch.int32, "sequences"),
+            _here(positions, torch.int32, "positions"), positions.shape[0])
+
+
+def cache_append(cache: Cache, table: torch.Tensor, positions: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                 q: Optional[torch.Tensor] = None, cos_sin: Optional[torch.Tensor] = None, interleaved: bool = False,
+                 sequences: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """k, v bf16 [T,heads,head_dim] of tokens positions i32 [T] of sequences i32 [T] (None: token t of sequence t) into
+    the cache through table i32 [B,width]; with cos_sin f32 [angles,rot] (cosines, then sines) k and q bf16
+    [T,H,head_dim] are turned by position first.  Tokens may lie apart (slices of a fused projection).  Returns the
+    queries (`out`: where to, [T,H,head_dim]; may be q), None without q."""
+    where = _places(cache, table, positions, sequences)
+    T, D = where[-1], cache.head_dim
+    if k.shape[0] != T or v.shape[0] != T or (q is not None and q.shape[0] != T):
+        raise ValueError("shape mismatch")
+    ka, ks = _rows(k, cache.heads, D, "k")
+    va, vs = _rows(v, cache.heads, D, "v")
+    qa, qs, H, to = None, 0, 0, None
+    if q is not None:
+        H = q.shape[1]
+        qa, qs = _rows(q, H, D, "q")
+        if out is None:
+            out = torch.empty((T, H, D), dtype=torch.bfloat16, device=q.device)
+        to = _here(out, torch.bfloat16, "out", T * H * D)
+    elif out is not None:
+        raise ValueError("out without q")
+    if cos_sin is not None and cos_sin.dim() != 2:
+        raise ValueError("shape mismatch")
+    _check(lib().nvq_cache_append(*where, qa, qs, H, to, ka, ks, va, vs,
+                                  None if cos_sin is None else _here(cos_sin, torch.float32, "cos_sin"),
+                                  0 if cos_sin is None else cos_sin.shape[0], 0 if cos_sin is None else cos_sin.shape[1],
+                                  int(interleaved), _stream()), "nvq_cache_append")
+    return out
+
+
+def cache_read(cache: Cache, table: torch.Tensor, positions: torch.Tensor, sequences: Optional[torch.Tensor] = None,
+               out=None):
+    """The keys and values, bf16 [T,heads,head_dim] each, of the tokens named as in cache_append (`out`: the two tensors
+    to write into)."""
+    where = _places(cache, table, positions, sequences)
+    T = where[-1]
+    n = T * cache.heads * cache.head_dim
+    if out is None:
+        out = tuple(torch.empty((T, cache.heads, cache.head_dim), dtype=torch.bfloat16, device=cache.device) for _ in range(2))
+    _check(lib().nvq_cache_read(*where, _here(out[0], torch.bfloat16, "k", n), _here(out[1], torch.bfloat16, "v", n),
+                                _stream()), "nvq_cache_read")
+    return out[0], out[1]
+
+
+def attention(cache: Cache, q: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, scale: Optional[float] = None,
+              window: int = 0, softcap: float = 0.0, out_dtype=torch.bfloat16, out: Optional[torch.Tensor] = None,
+              lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """One new token of each sequence, q bf16 [B,H,head_dim] (sequences may lie apart), over the first lengths i32 [B]
+    tokens that table i32 [B,width] names in the cache -> [B,H,head_dim] (scale: None for head_dim ** -0.5; lse f32
+    [B,H]: written if given; `workspace`: from cache.workspace, for calls one after the other)."""
+    if cache.device.index != torch.cuda.current_device():
+        raise ValueError("the cache is on %s, the current device is %d" % (cache.device, torch.cuda.current_device()))
+    B, H, D = q.shape
+    if table.dim() != 2 or table.shape[0] != B or tuple(lengths.shape) != (B,):
+        raise ValueError("shape mismatch")
+    qa, qs = _rows(q, H, cache.head_dim, "q")
+    y = out if out is not None else torch.empty((B, H, D), dtype=out_dtype, device=q.device)
+    if workspace is None:
+        workspace = cache.workspace(B, H)
+    _check(lib().nvq_attention(cache.address, qa, qs, H, _here(table, torch.int32, "table"), B, table.shape[1],
+                               _here(lengths, torch.int32, "lengths"), D ** -0.5 if scale is None else float(scale),
+                               int(window), float(softcap), _here(y, y.dtype, "out", B * H * D), _y_dtype(y.dtype),
+                               None if lse is None else _here(lse, torch.float32, "lse", B * H),
+                               _here(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()), "nvq_attention")
+    return y
+
+
+def sample_workspace(M: int, V: int, device="cuda") -> torch.Tensor:
+    """The workspace of sample for up to M rows of V logits: cleared here, and by every call after its use."""
+    need = lib().nvq_sample_workspace_bytes(M, V)
+    if need == 0:
+        raise NvqError(2, "nvq_sample_workspace_bytes")
+    return _cleared(need, device)
+
+
+def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Tensor] = None,
+           top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None, min_p: Optional[torch.Tensor] = None,
+           out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The next token i32 [M] of logits f32 or bf16 [M,V] (rows may lie apart) from random numbers u f32 [M]; per row
+    temperature f32, top_k i32, top_p f32, min_p f32 [M], or None (`workspace`: from sample_workspace, for calls one
+    after the other)."""
+    if not logits.is_cuda or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        raise ValueError("logits must be a device tensor [M,V], a row's values side by side")
+    if logits.get_device() != torch.cuda.current_device():
+        raise ValueError("logits is on device %d, the current device is %d" % (logits.get_device(), torch.cuda.current_device()))
+    M, V = logits.shape
+    ids = out if out is not None else torch.empty((M,), dtype=torch.int32, device=logits.device)
+    if workspace is None:
+        workspace = sample_workspace(M, V, logits.device)
+    at = [None if t is None else _here(t, d, name, M) for t, d, name in
+          ((u, torch.float32, "u"), (temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"),
+           (top_p, torch.float32, "top_p"), (min_p, torch.float32, "min_p"), (ids, torch.int32, "out"))]
+    _check(lib().nvq_sample(logits.data_ptr(), _y_dtype(logits.dtype), logits.stride(0) if M > 1 else V, M, V, *at,
+                            _here(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()), "nvq_sample")
+    return ids
+
+
+class Adapters:
+    """Low-rank adapters of a layer of N outputs and K inputs (`nvq_adapters` plus the tensors it points to): a bf16
+    [n,R,K], b bf16 [n,N,R], scales f32 [n] (None: 1)."""
+
+    def __init__(self, a: torch.Tensor, b: torch.Tensor, scales: Optional[torch.Tensor] = None):
+        if a.dim() != 3 or b.dim() != 3 or b.shape[0] != a.shape[0] or b.shape[2] != a.shape[1] or (
+                scales is not None and tuple(scales.shape) != (a.shape[0],)):
+            raise ValueError("shape mismatch")
+        self.keep = (a, b, scales)
+        if any(t is not None and t.device != a.device for t in self.keep):
+            raise ValueError("tensors on different devices")
+        self.n, self.R, self.K = a.shape
+        self.N, self.device = b.shape[1], a.device
+        self.struct = AdaptersStruct(_dev(a, torch.bfloat16, "a"), _dev(b, torch.bfloat16, "b"),
+                                     None if scales is None else _dev(scales, torch.float32, "scales"),
+                                     self.n, self.K, self.N, self.R)
+        self.address = C.addressof(self.struct)
+
+    def workspace(self, M: int) -> torch.Tensor:
+        """Scratch memory of adapters_add for up to M tokens."""
+        need = lib().nvq_adapters_workspace_bytes(self.address, M)
+        if need == 0:
+            raise NvqError(2, "nvq_adapters_workspace_bytes")
+        return torch.empty(need, dtype=torch.uint8, device=self.device)
+
+
+def adapters_add(adapters: Adapters, x: torch.Tensor, ids: torch.Tensor, y: torch.Tensor,
+                 out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y f32 or bf16 [M,N] plus what the adapter ids i32 [M] (outside [0,n): none) of each token makes of x bf16 [M,K]
+    (`out`: where to, may be y; `workspace`: from adapters.workspace, for calls one after the other)."""
+    if adapters.device.index != torch.cuda.current_device():
+        raise ValueError("the adapters are on %s, the current device is %d" % (adapters.device, torch.cuda.current_device()))
+    M = x.shape[0]
+    if tuple(x.shape) != (M, adapters.K) or tuple(ids.shape) != (M,) or tuple(y.shape) != (M, adapters.N):
+        raise ValueError("shape mismatch")
+    to = out if out is not None else torch.empty_like(y)
+    if workspace is None:
+        workspace = adapters.workspace(M)
+    _check(lib().nvq_adapters_add(adapters.address, _here(x, torch.bfloat16, "x"), _here(ids, torch.int32, "ids"), M,
+                                  _here(y, y.dtype, "y"), _here(to, y.dtype, "out", M * adapters.N), _y_dtype(y.dtype),
+                                  _here(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()),
+           "nvq_adapters_add")
+    return to
 
 
 def token_norms(a: torch.Tensor, b: Optional[torch.Tensor] = None) -> torch.Tensor:

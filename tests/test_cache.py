@@ -1,0 +1,384 @@
+"""The paged cache of keys and values, and attention over it, against plain forms."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2604_21026_amd import nvq
+from tests import np_decode as ref
+
+DEV = "cuda:0"
+gpu = pytest.mark.gpu
+NO_PAGE = (-1, 1 << 30)
+
+
+def dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a)).to(DEV)
+    return t if dtype is None else t.to(dtype)
+
+
+def f64(t):
+    return t.double().cpu().numpy()
+
+
+# ---- refusals (no device is touched) ----
+def struct(**kw):
+    v = dict(k=0x1000, v=0x1000, scales=0x1000, dtype=1, pages=4, heads=2, page_size=16, head_dim=64)
+    v.update(kw)
+    return nvq.CacheStruct(*v.values())
+
+
+BAD_CACHES = [(dict(k=None), 1), (dict(v=None), 1), (dict(dtype=0), 1), (dict(dtype=3), 1), (dict(dtype=2, scales=None), 1),
+              (dict(pages=0), 2), (dict(heads=0), 2), (dict(heads=1025), 2), (dict(page_size=4), 2), (dict(page_size=24), 2),
+              (dict(page_size=2048), 2), (dict(head_dim=48), 2), (dict(head_dim=0), 2), (dict(head_dim=288), 2),
+              (dict(k=0x1008), 3), (dict(v=0x1002), 3), (dict(dtype=2, scales=0x1004), 3)]
+
+
+def test_append_and_read_refusals_before_any_launch():
+    L, a = nvq.lib(), 0x1000
+
+    def append(cache=None, table=a, B=3, width=5, seq=a, pos=a, T=4, q=a, qs=256, H=4, out=a + 16, k=a, ks=128, v=a, vs=128,
+               cs=a, angles=9, rot=64, inter=0, **kw):
+        s = struct(**kw)
+        return L.nvq_cache_append(C.addressof(s) if cache is None else None, table, B, width, seq, pos, T, q, qs, H, out, k, ks, v, vs,
+                                  cs, angles, rot, inter, None)
+
+    def read(table=a, B=3, width=5, seq=a, pos=a, T=4, k=a, v=a, **kw):
+        s = struct(**kw)
+        return L.nvq_cache_read(C.addressof(s), table, B, width, seq, pos, T, k, v, None)
+
+    assert append(cache=0) == 1
+    for kw, status in BAD_CACHES:
+        assert append(**kw) == status and read(**kw) == status
+    for call in (append, read):
+        assert call(table=None) == 1 and call(pos=None) == 1 and call(k=None) == 1 and call(v=None) == 1
+        assert call(B=0) == 2 and call(width=0) == 2 and call(T=0) == 2 and call(T=(1 << 24) + 1) == 2
+        assert call(table=a + 2) == 3 and call(seq=a + 1) == 3 and call(pos=a + 2) == 3 and call(k=a + 8) == 3 and call(v=a + 8) == 3
+        assert call(T=1 << 24, heads=4, ks=256, vs=256) == 2 if call is append else call(T=1 << 24, heads=4) == 2
+    assert append(q=None) == 1 and append(H=0) == 1 and append(out=None) == 1 and append(inter=2) == 1
+    assert append(H=1025, qs=1 << 20) == 2 and append(H=-1, q=None, out=None) == 2
+    assert append(angles=0) == 2 and append(rot=0) == 2 and append(rot=24) == 2 and append(rot=80) == 2
+    assert append(qs=248) == 2 and append(ks=120) == 2 and append(vs=120) == 2
+    assert append(qs=260) == 3 and append(ks=132) == 3 and append(vs=129) == 3 and append(cs=a + 8) == 3 and append(q=a + 2) == 3
+    assert append(out=a + 4) == 3 and append(out=a, qs=264) == 1  # in place, but the tokens lie apart
+
+
+def test_attention_refusals_before_any_launch():
+    L, a = nvq.lib(), 0x1000
+    s = struct()
+    need = L.nvq_attention_workspace_bytes(C.addressof(s), 3, 4)
+    assert need >= 4096
+    inf, nan = float("inf"), float("nan")
+
+    def call(q=a, qs=256, H=4, table=a, B=3, width=5, lengths=a, scale=0.125, window=0, softcap=0.0, out=a, dt=1, lse=None,
+             ws=a, bytes_=need, **kw):
+        t = struct(**kw)
+        return L.nvq_attention(C.addressof(t), q, qs, H, table, B, width, lengths, scale, window, softcap, out, dt, lse, ws, bytes_, None)
+
+    assert L.nvq_attention(None, a, 256, 4, a, 3, 5, a, 0.1, 0, 0.0, a, 1, None, a, need, None) == 1
+    for kw, status in BAD_CACHES:
+        assert call(**kw) == status
+    assert call(q=None) == 1 and call(table=None) == 1 and call(lengths=None) == 1 and call(out=None) == 1 and call(dt=2) == 1
+    assert call(scale=nan) == 1 and call(scale=inf) == 1 and call(softcap=-1.0) == 1 and call(softcap=nan) == 1 and call(softcap=inf) == 1
+    assert call(H=3) == 2 and call(H=0) == 2 and call(B=0) == 2 and call(B=4097) == 2 and call(width=0) == 2 and call(window=-1) == 2
+    assert call(qs=248) == 2 and call(width=(1 << 26) + 1) == 2 and call(H=1026, qs=1 << 20) == 2
+    assert call(qs=260) == 3 and call(q=a + 8) == 3 and call(table=a + 2) == 3 and call(lengths=a + 1) == 3 and call(out=a + 8) == 3
+    assert call(lse=a + 2) == 3
+    assert call(ws=None) == 6 and call(ws=a + 16) == 6 and call(bytes_=need - 1) == 6
+    assert L.nvq_attention_workspace_bytes(None, 3, 4) == 0 and L.nvq_attention_workspace_bytes(C.addressof(s), 0, 4) == 0
+    assert L.nvq_attention_workspace_bytes(C.addressof(s), 3, 5) == 0 and L.nvq_attention_workspace_bytes(C.addressof(s), 4097, 4) == 0
+
+
+def test_the_binding_refuses_caches_that_do_not_fit():
+    z = lambda *s, dtype=torch.bfloat16: torch.zeros(s, dtype=dtype)
+    u8 = torch.uint8
+    for args in [(z(2, 2, 16, 64), z(2, 2, 2, 64, 8)),  # host tensors
+                 (z(2, 2, 16, 64, dtype=torch.float16), z(2, 2, 2, 64, 8, dtype=torch.float16)),
+                 (z(2, 2, 16, 64), z(2, 2, 16, 64)), (z(2, 2, 12, 64), z(2, 2, 1, 64, 8)), (z(2, 16, 64), z(2, 2, 64, 8)),
+                 (z(2, 2, 16, 64), z(2, 2, 2, 64, 8), z(2, 2, 2, 16, dtype=u8)),
+                 (z(2, 2, 16, 64, dtype=u8), z(2, 2, 2, 64, 8, dtype=u8)),
+                 (z(2, 2, 16, 64, dtype=u8), z(2, 2, 2, 64, 8, dtype=u8), z(2, 2, 16, dtype=u8))]:
+        with pytest.raises(ValueError):
+            nvq.Cache(*args)
+
+
+# ---- a pool, and what it should hold ----
+class Pool:
+    """A cache whose unused places hold what must not matter, and a table with pages in random order."""
+
+    def __init__(self, rng, lengths, heads, D, page, e4m3, room=0):
+        self.heads, self.D, self.page, self.e4m3 = heads, D, page, e4m3
+        need = [-(-(n + room) // page) for n in lengths]
+        self.pages, self.width = sum(need) + 2, max(need) + 2
+        order = rng.permutation(self.pages)
+        # (what the table holds behind a sequence's last page is no page)
+        self.table = rng.choice(NO_PAGE, (len(lengths), self.width)).astype(np.int32)
+        for b, n in enumerate(need):
+            self.table[b, :n] = order[sum(need[:b]):sum(need[:b]) + n]
+        shape = (self.pages, heads, page, D)
+        self.k = np.full(shape, np.nan)
+        self.v = np.full(shape, np.nan)
+        if e4m3:
+            self.kc, self.vc = np.full(shape, 0x7f, np.uint8), np.full(shape, 0xff, np.uint8)
+            self.s = np.full((self.pages, heads, 2, page), 255, np.uint8)
+
+    def put(self, b, t, k, v):
+        """Tokens t of sequence b: k, v [n,heads,D] float64, bf16 values."""
+        at = self.table[b, t // self.page], slice(None), t % self.page
+        if self.e4m3:
+            for i, (x, c) in enumerate(((k, self.kc), (v, self.vc))):
+                c[at], byte = ref.quant_e4m3(x)
+                self.s[at[0], :, i, at[2]] = byte
+                x = ref.E4M3[c[at]] * ref.scale_of(byte)[..., None]
+                (self.v if i else self.k)[at] = x
+        else:
+            self.k[at], self.v[at] = k, v
+
+    def device(self):
+        side = lambda x: x.reshape(self.pages, self.heads, self.page // 8, 8, self.D).swapaxes(-1, -2)
+        if self.e4m3:
+            return nvq.Cache(dev(self.kc), dev(side(self.vc)), dev(self.s))
+        return nvq.Cache(dev(self.k, torch.bfloat16), dev(side(self.v), torch.bfloat16))
+
+    def raw(self, cache):
+        """k, v [pages,heads,page,D] and scales of a device cache, as bits."""
+        bits = lambda t: t.cpu().numpy() if self.e4m3 else t.view(torch.int16).cpu().numpy()
+        return bits(cache.k), bits(cache.v).swapaxes(-1, -2).reshape(cache.k.shape), cache.scales.cpu().numpy() if self.e4m3 else None
+
+
+def bf16(rng, shape, scale=1.0):
+    return ref.to_bf16(rng.standard_normal(shape).astype(np.float32) * np.float32(scale)).astype(np.float64)
+
+
+def same_bits(got, want):
+    """Tensor bf16 against float values that bf16 holds."""
+    return torch.equal(got.cpu().view(torch.int16), torch.from_numpy(np.ascontiguousarray(want, np.float32)).bfloat16().view(torch.int16))
+
+
+# ---- append and read ----
+APPEND = [  # T, B, H, heads, D, rot, page, interleaved
+    (1, 1, 1, 1, 32, 32, 8, False), (1, 1, 32, 8, 64, 64, 16, False), (5, 5, 3, 1, 96, 48, 8, True), (33, 4, 6, 2, 64, 32, 32, False),
+    (70, 2, 8, 4, 128, 128, 16, True), (130, 1, 2, 2, 128, 64, 128, False), (17, 3, 14, 2, 256, 256, 64, False),
+    (9, 9, 5, 5, 224, 112, 1024, True), (40, 1, 7, 1, 160, 16, 8, False), (300, 2, 0, 3, 192, 192, 16, False)]
+
+
+@gpu
+@pytest.mark.parametrize("T,B,H,heads,D,rot,page,inter", APPEND)
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_append_and_read_to_the_bit(T, B, H, heads, D, rot, page, inter, e4m3):
+    rng = np.random.default_rng(T * 7 + D + rot)
+    held = rng.integers(0, 3 * page, B)
+    share = -(-T // B)
+    pool = Pool(rng, held, heads, D, page, e4m3, room=share)
+    for b in range(B):
+        pool.put(b, np.arange(held[b]), bf16(rng, (held[b], heads, D)), bf16(rng, (held[b], heads, D)))
+    cache = pool.device()
+    seq, pos = np.arange(T) // share, held[np.arange(T) // share] + np.arange(T) % share
+    angles = rng.uniform(-7, 7, (pos.max() + 1, rot // 2))
+    cos_sin = np.concatenate((np.cos(angles), np.sin(angles)), 1).astype(np.float32)
+    # rows of very different size, one of zeros; the projections of a token side by side, with room behind them
+    qkv = bf16(rng, (T, H + 2 * heads + 1, D)) * 2.0 ** rng.integers(-30, 30, (T, H + 2 * heads + 1, 1))
+    qkv[0, H] = 0
+    fused = dev(qkv, torch.bfloat16)
+    q, k, v = fused[:, :H], fused[:, H:H + heads], fused[:, H + heads:H + 2 * heads]
+    # some tokens are padding: nothing is written for them
+    pad = np.zeros(T, bool)
+    if T > 4:
+        pad[[1, 2, T - 1]] = True
+    bad_seq, bad_pos = seq.copy(), pos.copy()
+    if T > 4:
+        bad_seq[1], bad_pos[2], bad_pos[T - 1] = B, -1, pos.max() + 1
+    out = dev(np.full((T, H, D), 7.0), torch.bfloat16)
+    got = nvq.cache_append(cache, dev(pool.table), dev(bad_pos.astype(np.int32)), k, v, q if H else None, dev(cos_sin), inter,
+                           dev(bad_seq.astype(np.int32)), out=out if H else None)
+    want = [ref.rotate(qkv[:, :H], cos_sin, pos, inter), ref.rotate(qkv[:, H:H + heads], cos_sin, pos, inter), qkv[:, H + heads:H + 2 * heads]]
+    if H:
+        assert same_bits(got[torch.from_numpy(~pad)], want[0][~pad]) and (f64(got)[pad] == 7).all()
+    for t in np.flatnonzero(~pad):
+        pool.put(seq[t], pos[t:t + 1], want[1][t:t + 1].astype(np.float64), want[2][t:t + 1])
+    for a, b in zip(pool.raw(cache), pool.raw(pool.device())):
+        assert a is None or np.array_equal(a, b)
+    # read back: the new tokens, old ones, and some that are nowhere
+    rs, rp = np.concatenate((seq, [0, 0, -1, B - 1])), np.concatenate((pos, [0, pool.width * page, 0, -3]))
+    k2, v2 = nvq.cache_read(cache, dev(pool.table), dev(rp.astype(np.int32)), dev(rs.astype(np.int32)))
+    live = np.ones(T + 4, bool)
+    live[T + 1:] = False
+    live[:T] = ~pad
+    if held[0] == 0 and share == 0:
+        live[T] = False
+    at = pool.table[rs * live, rp * live // page], slice(None), rp * live % page
+    for x, y in ((k2, pool.k), (v2, pool.v)):
+        known = live & ~np.isnan(y[at]).any((1, 2))
+        assert known[:T][~pad].all()
+        assert same_bits(x[torch.from_numpy(known)], y[at][known]) and (f64(x)[T + 1:] == 0).all()
+
+
+@gpu
+def test_append_without_rotation_in_place_and_by_sequence():
+    """No table of angles: all channels as they are; no sequences: token t is sequence t's; q in place."""
+    rng = np.random.default_rng(5)
+    B, H, heads, D, page = 6, 4, 2, 64, 16
+    held = np.array([0, 15, 16, 31, 7, 40])
+    pool = Pool(rng, held, heads, D, page, False, room=1)
+    cache = pool.device()
+    q, k, v = bf16(rng, (B, H, D)), bf16(rng, (B, heads, D)), bf16(rng, (B, heads, D))
+    qd = dev(q, torch.bfloat16)
+    got = nvq.cache_append(cache, dev(pool.table), dev(held.astype(np.int32)), dev(k, torch.bfloat16), dev(v, torch.bfloat16), qd, out=qd)
+    assert got is qd and same_bits(qd, q)
+    for b in range(B):
+        pool.put(b, held[b:b + 1], k[b:b + 1], v[b:b + 1])
+    assert all(a is None or np.array_equal(a, b) for a, b in zip(pool.raw(cache), pool.raw(pool.device())))
+
+
+@gpu
+def test_append_of_every_bf16_value_and_of_rows_without_a_number():
+    D, page = 256, 256
+    x = torch.arange(65536, dtype=torch.int32).to(torch.int16).view(torch.bfloat16).view(256, 1, D)
+    cache = nvq.Cache.empty(1, 1, page, D, torch.uint8, DEV)
+    table, pos = dev(np.zeros((1, 1), np.int32)), dev(np.arange(256, dtype=np.int32))
+    zero = torch.zeros(256, dtype=torch.int32, device=DEV)
+    nvq.cache_append(cache, table, pos, x.to(DEV), x.to(DEV), sequences=zero)
+    xs = x.double().numpy()[:, 0]
+    finite = np.isfinite(xs).all(1)
+    codes, byte = ref.quant_e4m3(np.where(finite[:, None], xs, 0))
+    codes[~finite], byte[~finite] = 0, 255
+    assert np.array_equal(cache.k.cpu().numpy()[0, 0], codes)
+    assert np.array_equal(cache.v.cpu().numpy()[0, 0].swapaxes(-1, -2).reshape(256, D), codes)
+    assert np.array_equal(cache.scales.cpu().numpy()[0, 0], np.stack((byte, byte)))
+    k, v = nvq.cache_read(cache, table, pos, zero)
+    want = torch.from_numpy(ref.E4M3[codes] * ref.scale_of(byte)[:, None]).bfloat16()
+    for y in (k.cpu()[:, 0], v.cpu()[:, 0]):
+        assert torch.equal(y.isnan(), want.isnan()) and torch.equal(y.nan_to_num(1.0), want.nan_to_num(1.0))
+
+
+# ---- attention ----
+ATTENTION = [  # lengths, H, heads, D, page, window, softcap
+    ([1], 1, 1, 32, 8, 0, 0.0), ([0], 2, 1, 64, 16, 0, 0.0), ([500], 32, 8, 64, 16, 0, 0.0), ([31, 32, 33, 0, 1], 6, 2, 96, 8, 0, 0.0),
+    ([2000, 3, 700], 24, 8, 128, 32, 0, 30.0), ([257, 64, 65, 1023], 8, 8, 128, 128, 100, 0.0), ([90, 40], 7, 1, 160, 16, 33, 5.0),
+    ([333, 0, 8], 32, 2, 256, 64, 0, 0.0), ([120, 1111], 40, 2, 192, 8, 0, 0.0), ([70, 3000], 17, 1, 224, 256, 1, 0.0),
+    ([5000], 16, 1, 128, 1024, 0, 0.0), ([9] * 40, 4, 4, 32, 8, 0, 0.0), ([4097, 1], 48, 1, 64, 16, 4000, 0.0),
+    (list(range(130)), 3, 1, 32, 8, 64, 0.0)]
+
+
+def check_attention(got, lse, pool, q, lengths, window, softcap, scale, out_eps):
+    H, D = q.shape[1:]
+    g = H // pool.heads
+    for b, n in enumerate(lengths):
+        t = np.arange(max(0, n - window) if window else 0, n)
+        if len(t):
+            page = pool.table[b, t // pool.page]
+            t, page = t[(page >= 0) & (page < pool.pages)], page[(page >= 0) & (page < pool.pages)]
+        if len(t) == 0:
+            assert (got[b] == 0).all() and (lse is None or (lse[b] == -np.inf).all())
+            continue
+        for h in range(pool.heads):
+            k, v = pool.k[page, h, t % pool.page], pool.v[page, h, t % pool.page]
+            rows = slice(h * g, (h + 1) * g)
+            y, log, size, spread, mean = ref.attention(q[b, rows], k, v, scale, softcap)
+            # A score: D products and sums and the scale, tanh and its argument to four units of the score.  A weight:
+            # twice that (its own and the maximum's), the rounded argument of exp (its size in units), exp to four.
+            # Two bf16 values of a weight: 2^-17 of it.  Sums over the tokens, numerator and denominator, and the
+            # rescaling at every step of 32.
+            score = (2 * (D + 8) * ref.EPS32 * size + 8 * ref.EPS32 * (softcap if softcap else 0))
+            e = 2 * score + (4 * spread + 16) * ref.EPS32 + 2.0 ** -17 + 2 * (len(t) + 4 * (len(t) // 32 + 600)) * ref.EPS32
+            bound = e[:, None] * (mean + np.abs(y)) + out_eps * np.abs(y) + 1e-30
+            assert (np.abs(got[b, rows] - y) <= bound).all(), (b, h, (np.abs(got[b, rows] - y) / bound).max())
+            if lse is not None:
+                assert (np.abs(lse[b, rows] - log) <= e + 4 * ref.EPS32 * np.abs(log) + 1e-6).all()
+
+
+@gpu
+@pytest.mark.parametrize("lengths,H,heads,D,page,window,softcap", ATTENTION)
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_attention(lengths, H, heads, D, page, window, softcap, e4m3):
+    rng = np.random.default_rng(sum(lengths) + H + D)
+    pool = Pool(rng, lengths, heads, D, page, e4m3)
+    for b, n in enumerate(lengths):
+        grow = 2.0 ** rng.integers(-2, 3, (n, heads, 1))
+        pool.put(b, np.arange(n), bf16(rng, (n, heads, D)) * grow, bf16(rng, (n, heads, D)))
+    q = bf16(rng, (len(lengths), H, D))
+    cache, table, n = pool.device(), dev(pool.table), dev(np.array(lengths, np.int32))
+    apart = dev(np.concatenate((q, q[:, :1]), 1), torch.bfloat16)[:, :H]  # tokens lie apart
+    ws = cache.workspace(len(lengths) + 3, H)
+    lse = torch.empty((len(lengths), H), dtype=torch.float32, device=DEV)
+    for dtype, eps in ((torch.float32, 0.0), (torch.bfloat16, ref.EPS16), (torch.float32, 0.0)):
+        y = nvq.attention(cache, apart, table, n, window=window, softcap=softcap, out_dtype=dtype, lse=lse, workspace=ws)
+        assert int(ws[:4096].sum()) == 0
+        check_attention(f64(y), f64(lse), pool, q, lengths, window, softcap, D ** -0.5, eps)
+    again = nvq.attention(cache, apart, table, n, window=window, softcap=softcap, out_dtype=torch.float32, workspace=ws)
+    assert torch.equal(y, again)
+
+
+@gpu
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_attention_passes_over_pages_that_are_none(e4m3):
+    rng = np.random.default_rng(11)
+    lengths, heads, D, page = [200, 100, 64], 2, 64, 16
+    pool = Pool(rng, lengths, heads, D, page, e4m3)
+    for b, n in enumerate(lengths):
+        pool.put(b, np.arange(n), bf16(rng, (n, heads, D)), bf16(rng, (n, heads, D)))
+    pool.table[0, [0, 3, 4, 12]] = [-1, pool.pages, -2 ** 31, 2 ** 31 - 1]
+    pool.table[1, :] = -5  # nothing left
+    q = bf16(rng, (3, 6, D))
+    lse = torch.empty((3, 6), dtype=torch.float32, device=DEV)
+    y = nvq.attention(pool.device(), dev(q, torch.bfloat16), dev(pool.table), dev(np.array(lengths, np.int32)), scale=-0.3,
+                      out_dtype=torch.float32, lse=lse)
+    check_attention(f64(y), f64(lse), pool, q, lengths, 0, 0.0, np.float64(np.float32(-0.3)), 0.0)
+
+
+@gpu
+def test_attention_of_lengths_that_are_none_and_past_the_table():
+    rng = np.random.default_rng(12)
+    heads, D, page = 1, 32, 8
+    pool = Pool(rng, [48, 48], heads, D, page, False)
+    pool.table = np.ascontiguousarray(pool.table[:, :6])
+    for b in range(2):
+        pool.put(b, np.arange(48), bf16(rng, (48, heads, D)), bf16(rng, (48, heads, D)))
+    q = bf16(rng, (2, 2, D))
+    cache, qd, table = pool.device(), dev(q, torch.bfloat16), dev(pool.table)
+    for given, meant in (([-1, 49], [0, 48]), ([2 ** 31 - 1, -2 ** 31], [48, 0])):
+        y = nvq.attention(cache, qd, table, dev(np.array(given, np.int32)), out_dtype=torch.float32)
+        check_attention(f64(y), None, pool, q, meant, 0, 0.0, D ** -0.5, 0.0)
+
+
+@gpu
+@pytest.mark.parametrize("n", [40, 3000])
+def test_attention_of_values_without_a_number(n):
+    """As the formula has them: an infinite value only where it stands, a NaN key or query in its own head."""
+    rng = np.random.default_rng(13)
+    heads, D, page = 3, 64, 16
+    pool = Pool(rng, [n, n], heads, D, page, False)
+    for b in range(2):
+        pool.put(b, np.arange(n), bf16(rng, (n, heads, D)), bf16(rng, (n, heads, D)))
+    at = lambda t: (pool.table[0, t // page], t % page)
+    p, s = at(7)
+    pool.v[p, 0, s, 5] = np.inf
+    p, s = at(n - 1)
+    pool.k[p, 1, s, 9] = np.nan
+    q = bf16(rng, (2, 6, D))
+    q[0, 5, 3] = np.nan
+    lse = torch.empty((2, 6), dtype=torch.float32, device=DEV)
+    y = f64(nvq.attention(pool.device(), dev(q, torch.bfloat16), dev(pool.table), dev(np.array([n, n], np.int32)), lse=lse, out_dtype=torch.float32))
+    assert np.isposinf(y[0, :2, 5]).all() and np.isfinite(np.delete(y[0, :2], 5, 1)).all()
+    assert np.isnan(y[0, 2:4]).all() and np.isnan(y[0, 5]).all() and np.isfinite(y[0, 4]).all() and np.isfinite(y[1]).all()
+    assert np.isnan(f64(lse)[0, [2, 3, 5]]).all() and np.isfinite(f64(lse)[0, [0, 1, 4]]).all() and np.isfinite(f64(lse)[1]).all()
+
+
+@gpu
+def test_attention_scores_of_infinity():
+    heads, D, page, n = 1, 32, 8, 40
+    rng = np.random.default_rng(14)
+    pool = Pool(rng, [n, n], heads, D, page, False)
+    for b in range(2):
+        pool.put(b, np.arange(n), np.abs(bf16(rng, (n, heads, D))), bf16(rng, (n, heads, D)))
+    pool.k[pool.table[0, 2], 0, 3] = np.inf    # one score of minus infinity: a weight of zero
+    pool.k[pool.table[1, :5], 0, :] = np.inf   # all of them: zeros
+    q = ref.to_bf16((-np.abs(bf16(rng, (2, 1, D))) - 0.5).astype(np.float32)).astype(np.float64)  # (what the kernel gets)
+    y = f64(nvq.attention(pool.device(), dev(q, torch.bfloat16), dev(pool.table), dev(np.array([n, n], np.int32)), out_dtype=torch.float32))
+    keep = np.arange(n) != 19
+    k, v = (np.concatenate([x[p, 0] for p in pool.table[0, :5]])[keep] for x in (pool.k, pool.v))
+    want, _, size, spread, mean = ref.attention(q[0], k, v, D ** -0.5, 0)
+    e = 4 * (D + 8) * ref.EPS32 * size + (4 * spread + 16 + 3000) * ref.EPS32 + 2.0 ** -17
+    assert (np.abs(y[0] - want) <= e[:, None] * (mean + np.abs(want))).all()
+    assert (y[1] == 0).all()
