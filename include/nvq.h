@@ -696,8 +696,7 @@ int nvq_cache_read(const nvq_cache *cache, const int32_t *table, int B, int tabl
  * [max(0, n - window), n) (window = 0: all) whose page is in the pool:
  *   s_t = scale * q[b][h] . k[t];  softcap > 0: s_t = softcap * tanh(s_t / softcap)
  *   out[b][h] = sum_t exp(s_t - max s) v[t] / sum_t exp(s_t - max s)
- * Scores, maxima, sums in fp32; the weights enter the product with v as two bf16 values
- * each (16 bits); out is rounded once (out_dtype).  A sequence without such a position
+ * Scores, weights, maxima and sums in fp32; out is rounded once (out_dtype).  A sequence without such a position
  * (or with scores of minus infinity alone) gets zeros.  What the cache holds at other
  * positions does not matter, NaN included.  lengths below 0 count as 0, those past the
  * table's width as the width.  The same call gives the same bits.
@@ -708,10 +707,10 @@ int nvq_cache_read(const nvq_cache *cache, const int32_t *table, int B, int tabl
  *   workspace  nvq_attention_workspace_bytes(cache, B, H) bytes, 256-byte aligned.  Its
  *              first NVQ_ATTENTION_CLEAR_BYTES must be zero before the first call and are
  *              zero again after every call: clear it once, then use it for any number of
- *              calls with caches of this head_dim and of these or fewer heads and
- *              sequences, one after the other (not by two that overlap).
+ *              calls with caches of this head_dim or a smaller one, one after the other
+ *              (not by two that overlap).
  * B <= NVQ_ATTENTION_MAX_B, H a multiple of heads up to NVQ_MAX_HEADS; table_width *
- * page_size <= 2^30; scale finite, window >= 0, softcap >= 0 and finite.
+ * page_size <= 2^30, B * (table_width * page_size / 32 + 1) <= 2^30; scale finite, window >= 0, softcap >= 0 and finite.
  * nvq_attention_workspace_bytes looks at the sizes alone, 0 where they are invalid.
  */
 #define NVQ_ATTENTION_MAX_B 4096

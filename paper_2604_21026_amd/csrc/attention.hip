@@ -8,10 +8,10 @@
 //                 lane row kb = lane / 16 gets the scores of tokens 8 kb .. 8 kb + 7
 //   O^T = V^T P^T the weights P as they come out of S^T: lane row kb multiplies tokens 8 kb .. 8 kb + 7, which is what
 //                 one 16-byte piece of the value layout holds for a channel
-// P enters as two bf16 values (p - bf16(p) is the second), 16 bits of it: the products are a twentieth of the time that
-// the bytes take, so twice as many of them cost nothing, and results keep the precision of fp32 outputs.  The two
-// products are summed apart and added at the end: what an infinite value makes of the second (zero times infinity,
-// or the other sign) is left out there.
+// P enters as three bf16 values whose sum it is: the products are a twentieth of the time that the bytes take, so more
+// of them cost nothing, and results keep the precision of fp32.  The products with the first and with the rest are
+// summed apart and added at the end: what an infinite value makes of the rest (zero times infinity, or the other sign)
+// is left out there.
 #include "cache.h"
 #include "mfma_act.h"
 
@@ -33,6 +33,8 @@ struct AttentionArgs {
     void *out;
     int out_dtype;
     float *lse;
+    uint32_t *arrived;  // workspace, per workgroup
+    float *partial;     // [workgroup][2][16][D + 2]
 };
 
 struct MaxOp {
@@ -58,7 +60,7 @@ __device__ __forceinline__ Span span_of(const AttentionArgs &a, int b) {
 template <int D>
 struct State {
     float m, l;
-    float4v o[D / 16], rest[D / 16];  // of the weights' first and second values
+    float4v o[D / 16], rest[D / 16];  // of the weights' first values and of the rest
     __device__ void clear() {
         m = -INFINITY;
         l = 0.0f;
@@ -115,13 +117,45 @@ struct Piece<true> {
     }
 };
 
-// Steps `step` .. `step + count - 1` (of the sequence's tokens from 0) into st.
+// Steps `step` .. `step + count - 1` (of the sequence's tokens from 0) into st.  Keys of the next step are asked for
+// as soon as the products have taken this step's, values likewise, and the pages two steps ahead.
 template <int D, bool E4M3>
-__device__ void attend(const AttentionArgs &a, int b, int head, int tile, const Span &sp, int step, int count, State<D> &st) {
+__device__ __forceinline__ void attend(const AttentionArgs &a, int b, int head, int tile, const Span &sp, int step, int count,
+                                       State<D> &st) {
     typedef Piece<E4M3> P;
     constexpr int C = D / 32, T = D / 16;
     const int lane = threadIdx.x & 63, n = lane & 15, kb = lane >> 4;
     const int heads = a.group - kHeadTile * tile < kHeadTile ? a.group - kHeadTile * tile : kHeadTile;
+    const int32_t *const table = a.table + (int64_t)b * a.width;
+    // A lane reads keys of the step's block n / 4 of eight tokens (its tile rows' own) and values of block kb.
+    auto page_of = [&](int s, int block) {
+        const int t = kStep * s + 8 * block;
+        return t < sp.end ? table[t >> a.c.page_shift] : -1;
+    };
+    auto inside = [&](int page) { return (unsigned)page < (unsigned)a.c.pages ? page : 0; };
+    typename P::raw k[2][C], v[T];
+    uint2v key_scales = {}, value_scales = {};
+    auto load_keys = [&](int s, int page, int page_kb) {
+        const int slot = (kStep * s + 8 * (n >> 2) + (n & 3)) & (a.c.page_size - 1);
+        const int64_t at = key_at(a.c, inside(page), head, slot) + 8 * kb;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int c = 0; c < C; ++c) k[t][c] = P::load(a.c.k, at + 4 * t * D + 32 * c);
+        if (E4M3)
+            key_scales = *as_global<uint2v>(a.c.scales + scale_at(a.c, inside(page_kb), head, 0, (kStep * s + 8 * kb) & (a.c.page_size - 1)));
+    };
+    auto load_values = [&](int s, int page) {
+        const int slot = (kStep * s + 8 * kb) & (a.c.page_size - 1);
+        const int64_t at = value_at(a.c, inside(page), head, slot) + 8 * n;
+#pragma unroll
+        for (int d = 0; d < T; ++d) v[d] = P::load(a.c.v, at + 128 * d);
+        if (E4M3) value_scales = *as_global<uint2v>(a.c.scales + scale_at(a.c, inside(page), head, 1, slot));
+    };
+    int key_page = page_of(step, n >> 2), value_page = page_of(step, kb);
+    int next_key_page = page_of(step + 1, n >> 2), next_value_page = page_of(step + 1, kb);
+    load_keys(step, key_page, value_page);
+    load_values(step, value_page);
     bf16x8 q[C];
     {
         const uint16_t *const at = a.q + b * a.q_stride + (int64_t)(head * a.group + kHeadTile * tile + (n < heads ? n : 0)) * D;
@@ -132,35 +166,10 @@ __device__ void attend(const AttentionArgs &a, int b, int head, int tile, const 
             q[c] = __builtin_bit_cast(bf16x8, w);
         }
     }
-    const int32_t *const table = a.table + (int64_t)b * a.width;
-    // A lane reads keys of the step's block n / 4 of eight tokens (its tile rows' own) and values of block kb.
-    auto page_of = [&](int s, int block) {
-        const int t = kStep * s + 8 * block;
-        return t < sp.end ? table[t >> a.c.page_shift] : -1;
-    };
-    int key_page = page_of(step, n >> 2), value_page = page_of(step, kb);
     for (int i = 0; i < count; ++i) {
         const int s = step + i, t0 = kStep * s;
+        const bool more = i + 1 < count;
         const bool value_ok = (unsigned)value_page < (unsigned)a.c.pages;
-        const int kp = (unsigned)key_page < (unsigned)a.c.pages ? key_page : 0, vp = value_ok ? value_page : 0;
-        const int key_slot = (t0 + 8 * (n >> 2) + (n & 3)) & (a.c.page_size - 1);
-        const int value_slot = (t0 + 8 * kb) & (a.c.page_size - 1);
-        const int64_t ka = key_at(a.c, kp, head, key_slot) + 8 * kb, va = value_at(a.c, vp, head, value_slot) + 8 * n;
-        typename P::raw k[2][C], v[T];
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int c = 0; c < C; ++c) k[t][c] = P::load(a.c.k, ka + 4 * t * D + 32 * c);
-#pragma unroll
-        for (int d = 0; d < T; ++d) v[d] = P::load(a.c.v, va + 128 * d);
-        uint2v key_scales = {}, value_scales = {};
-        if (E4M3) {
-            key_scales = *as_global<uint2v>(a.c.scales + scale_at(a.c, vp, head, 0, value_slot));
-            value_scales = *as_global<uint2v>(a.c.scales + scale_at(a.c, vp, head, 1, value_slot));
-        }
-        key_page = page_of(s + 1, n >> 2);
-        value_page = page_of(s + 1, kb);
-
         float4v raw[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
@@ -176,18 +185,21 @@ __device__ void attend(const AttentionArgs &a, int b, int head, int tile, const 
             x[j] = raw[j >> 2][j & 3] * a.scale;
             if (E4M3) x[j] *= scale_value(key_scales[j >> 2] >> 8 * (j & 3) & 255);
         }
+        if (more) load_keys(s + 1, next_key_page, next_value_page);
+        const int coming_key_page = page_of(s + 2, n >> 2), coming_value_page = page_of(s + 2, kb);
         if (a.softcap > 0.0f) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = a.softcap * tanhf(x[j] / a.softcap);
         }
         // Which of the lane's tokens count; of steps in the middle of a sequence all do.
-        uint32_t valid = 0;
+        uint32_t valid = 255u;
+        if (t0 < sp.start || t0 + kStep > sp.end || !__all(value_ok)) {
+            valid = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int t = t0 + 8 * kb + j;
-            valid |= value_ok && t >= sp.start && t < sp.end ? 1u << j : 0u;
-        }
-        if (!__all(valid == 255u)) {
+            for (int j = 0; j < 8; ++j) {
+                const int t = t0 + 8 * kb + j;
+                valid |= value_ok && t >= sp.start && t < sp.end ? 1u << j : 0u;
+            }
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = valid >> j & 1 ? x[j] : -INFINITY;
 #pragma unroll
@@ -199,7 +211,7 @@ __device__ void attend(const AttentionArgs &a, int b, int head, int tile, const 
         top = with_lane_xor<16>(top, MaxOp());
         top = with_lane_xor<32>(top, MaxOp());
         if (__any(top > st.m)) {
-            const float m = fmaxf(st.m, top), f = st.m == m ? 1.0f : exp2f((st.m - m) * kLog2e);
+            const float m = fmaxf(st.m, top), f = st.m == m ? 1.0f : __builtin_amdgcn_exp2f((st.m - m) * kLog2e);
             st.m = m;
             st.l *= f;
 #pragma unroll
@@ -211,67 +223,310 @@ __device__ void attend(const AttentionArgs &a, int b, int head, int tile, const 
                 }
         }
         const float ref = st.m == -INFINITY ? 0.0f : st.m;
-        uint32_t hi[4], lo[4];
+        uint32_t part[3][4];
 #pragma unroll
         for (int j = 0; j < 8; j += 2) {
-            float p[2], rest[2];
+            float p[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                p[e] = exp2f((x[j + e] - ref) * kLog2e);
+                p[e] = __builtin_amdgcn_exp2f((x[j + e] - ref) * kLog2e);
                 st.l += p[e];
                 if (E4M3) {
                     const float f = scale_value(value_scales[(j + e) >> 2] >> 8 * ((j + e) & 3) & 255);
                     p[e] = valid >> (j + e) & 1 ? p[e] * f : 0.0f;
                 }
             }
-            hi[j / 2] = pack_bf16x2(p[0], p[1]);
-            rest[0] = p[0] - __uint_as_float(hi[j / 2] << 16);
-            rest[1] = p[1] - __uint_as_float(hi[j / 2] & 0xffff0000u);
-            lo[j / 2] = pack_bf16x2(rest[0], rest[1]);
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                part[i][j / 2] = pack_bf16x2(p[0], p[1]);
+                p[0] -= __uint_as_float(part[i][j / 2] << 16);
+                p[1] -= __uint_as_float(part[i][j / 2] & 0xffff0000u);
+            }
         }
-        const bf16x8 ph = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-        const bf16x8 pl = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+        bf16x8 w[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) w[i] = __builtin_bit_cast(bf16x8, make_uint4(part[i][0], part[i][1], part[i][2], part[i][3]));
 #pragma unroll
         for (int d = 0; d < T; ++d) {
-            const bf16x8 w = P::operand(v[d]);
-            st.o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, ph, st.o[d], 0, 0, 0);
-            st.rest[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, pl, st.rest[d], 0, 0, 0);
+            const bf16x8 x = P::operand(v[d]);
+            st.o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w[0], st.o[d], 0, 0, 0);
+            st.rest[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w[1], st.rest[d], 0, 0, 0);
+            st.rest[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w[2], st.rest[d], 0, 0, 0);
         }
+        if (more) load_values(s + 1, next_value_page);
+        value_page = next_value_page;
+        next_key_page = coming_key_page;
+        next_value_page = coming_value_page;
 #pragma unroll
         for (int d = 0; d < T; ++d) wait_written(st.o[d], st.rest[d]);
     }
 }
 
-// One wave per sequence and head tile.
+// A piece: steps [begin, end) of the n steps of one sequence and head tile (ht: key head times tiles, tile).
+struct PieceOf {
+    int b, ht, begin, end, n;
+};
+
+// The grid is one flat line of all steps of all sequences and head tiles, cut into as many equal ranges as there are
+// workgroups, and a range into one per wave: however ragged the lengths, every compute unit reads as much.  What a
+// wave has of a sequence and head tile that others share goes to LDS and is joined there, what a workgroup has of one
+// to the workspace, where the workgroup that arrives last joins it.
+template <int D>
+constexpr int waves_of() { return D <= 128 ? 8 : 4; }
+
+__device__ __forceinline__ float factor(float m, float most) { return m == most ? 1.0f : expf(m - most); }
+
+__device__ __forceinline__ void put(float *p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ float get(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
 template <int D, bool E4M3>
-__global__ __launch_bounds__(64) void attention_kernel(AttentionArgs a) {
-    const int per = a.c.heads * a.tiles;
-    const int b = blockIdx.x / per, head = blockIdx.x % per / a.tiles, tile = blockIdx.x % a.tiles;
-    const int lane = threadIdx.x & 63, n = lane & 15, kb = lane >> 4;
-    const int heads = a.group - kHeadTile * tile < kHeadTile ? a.group - kHeadTile * tile : kHeadTile;
-    const Span sp = span_of(a, b);
-    State<D> st;
-    st.clear();
-    attend<D, E4M3>(a, b, head, tile, sp, sp.first, sp.steps, st);
-    float l = with_lane_xor<16>(st.l, AddOp());
-    l = with_lane_xor<32>(l, AddOp());
-    if (n >= heads) return;
-    const int64_t row = (int64_t)b * a.H + head * a.group + kHeadTile * tile + n;
-    const float f = l == 0.0f ? 0.0f : 1.0f / l;
+__global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(AttentionArgs a) {
+    constexpr int kWaves = waves_of<D>(), kThreads = 64 * kWaves, kRow = D + 2;  // (a head's sum, m, l)
+    extern __shared__ __align__(16) char lds[];
+    __shared__ int scan[kWaves + 1];
+    __shared__ PieceOf held[kWaves][2];
+    __shared__ int last[2];
+    int *const upto = reinterpret_cast<int *>(lds);  // [B + 1]: steps before a sequence, of one head tile
+    float *const parts = reinterpret_cast<float *>(lds + (((int64_t)a.B + 1) * 4 + 15) / 16 * 16);  // [waves][2][heads][kRow]
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4;
+    const int per = a.c.heads * a.tiles;                                   // head tiles
+    const int heads_most = a.group < kHeadTile ? a.group : kHeadTile;
+    auto heads_of = [&](int ht) {
+        const int h = a.group - kHeadTile * (ht % a.tiles);
+        return h < kHeadTile ? h : kHeadTile;
+    };
+    auto row_of = [&](int b, int ht) { return (int64_t)b * a.H + ht / a.tiles * a.group + kHeadTile * (ht % a.tiles); };
+
+    int total = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+        const int b = b0 + (int)threadIdx.x;
+        int steps = b < a.B ? span_of(a, b).steps : 0, sum = steps;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(sum, d);
+            if (lane >= d) sum += o;
+        }
+        __syncthreads();
+        if (lane == 63) scan[w] = sum;
+        __syncthreads();
+        int before = total, all = total;
+        for (int i = 0; i < kWaves; ++i) {
+            if (i < w) before += scan[i];
+            all += scan[i];
+        }
+        if (b < a.B) upto[b + 1] = before + sum;
+        total = all;
+    }
+    if (threadIdx.x == 0) upto[0] = 0;
+    if (threadIdx.x < 2 * kWaves) held[threadIdx.x >> 1][threadIdx.x & 1].b = -1;
+    __syncthreads();
+    for (int b = blockIdx.x; b < a.B; b += gridDim.x)
+        if (upto[b + 1] == upto[b]) {  // nothing to attend to
+            for (int i = threadIdx.x; i < a.H * D; i += kThreads) store_global(a.out, a.out_dtype, (int64_t)b * a.H * D + i, 0.0f);
+            if (a.lse)
+                for (int i = threadIdx.x; i < a.H; i += kThreads) a.lse[(int64_t)b * a.H + i] = -INFINITY;
+        }
+    const int64_t T = (int64_t)total * per;
+    if (T == 0) return;
+    // Two steps to a wave at least; and of one sequence whole workgroups to a head tile, so that a short one needs no
+    // joining through memory.
+    int64_t groups = (T + 2 * kWaves - 1) / (2 * kWaves);
+    if (groups >= gridDim.x)
+        groups = gridDim.x;
+    else if (a.B == 1 && groups > per)
+        groups -= groups % per;
+    const int g = blockIdx.x;
+    if (g >= groups) return;
+    const int64_t f0 = T * g / groups, f1 = T * (g + 1) / groups, R = f1 - f0;
+    const int64_t w0 = f0 + R * w / kWaves, w1 = f0 + R * (w + 1) / kWaves;
+
+    auto write = [&](int64_t row, int i, float v) { store_global(a.out, a.out_dtype, row * D + i, v); };
+    for (int64_t f = w0; f < w1;) {
+        const int x = (int)(f / per);
+        int lo = 0, hi = a.B;  // upto[lo] <= x < upto[hi]
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (upto[mid] <= x)
+                lo = mid;
+            else
+                hi = mid;
+        }
+        PieceOf p;
+        p.b = __builtin_amdgcn_readfirstlane(lo);
+        p.n = __builtin_amdgcn_readfirstlane(upto[lo + 1] - upto[lo]);
+        const int64_t r = f - (int64_t)per * upto[lo];
+        p.ht = __builtin_amdgcn_readfirstlane((int)(r / p.n));
+        p.begin = __builtin_amdgcn_readfirstlane((int)(r - (int64_t)p.ht * p.n));
+        p.end = (int64_t)(p.n - p.begin) < w1 - f ? p.n : p.begin + (int)(w1 - f);
+        p.end = __builtin_amdgcn_readfirstlane(p.end);
+        f += p.end - p.begin;
+        Span sp = span_of(a, p.b);
+        State<D> st;
+        st.clear();
+        attend<D, E4M3>(a, p.b, p.ht / a.tiles, p.ht % a.tiles, sp, sp.first + p.begin, p.end - p.begin, st);
+        float l = with_lane_xor<16>(st.l, AddOp());
+        l = with_lane_xor<32>(l, AddOp());
+        const int heads = heads_of(p.ht);
+        if (p.begin == 0 && p.end == p.n) {
+            if (n < heads) {
+                const int64_t row = row_of(p.b, p.ht) + n;
+                const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-    for (int d = 0; d < D / 16; ++d)
+                for (int d = 0; d < D / 16; ++d)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) store_global(a.out, a.out_dtype, row * D + 16 * d + 4 * kb + r, l == 0.0f ? 0.0f : st.sum(d, r) * f);
-    if (a.lse && kb == 0) a.lse[row] = l == 0.0f ? -INFINITY : st.m + logf(l);
+                    for (int i = 0; i < 4; ++i) write(row, 16 * d + 4 * kb + i, l == 0.0f ? 0.0f : st.sum(d, i) * inv);
+                if (a.lse && kb == 0) a.lse[row] = l == 0.0f ? -INFINITY : st.m + logf(l);
+            }
+        } else {
+            const int slot = p.begin > 0 ? 0 : 1;
+            if (n < heads) {
+                float *const to = parts + ((w * 2 + slot) * heads_most + n) * kRow;
+#pragma unroll
+                for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) to[16 * d + 4 * kb + i] = st.sum(d, i);
+                if (kb == 0) {
+                    to[D] = st.m;
+                    to[D + 1] = l;
+                }
+            }
+            if (lane == 0) held[w][slot] = p;
+        }
+    }
+    __syncthreads();
+
+    // The waves' parts: a piece that starts in one wave goes on in the next ones' first slots.
+    PieceOf shared_piece[2];  // what is left for others to join: begun before this workgroup, going on after it
+    shared_piece[0].b = shared_piece[1].b = -1;
+    for (int start = -1; start < kWaves; ++start) {
+        // (-1: what begins before this workgroup, in the first slot of the first wave that has any steps)
+        int first = start < 0 ? 0 : start;
+        const int slot = start < 0 ? 0 : 1;
+        while (start < 0 && R * (first + 1) / kWaves == 0) ++first;
+        PieceOf p = held[first][slot];
+        if (p.b < 0) continue;
+        int until = p.end, lastw = first;
+        while (until < p.n && lastw + 1 < kWaves) {
+            ++lastw;
+            if (held[lastw][0].b >= 0) until = held[lastw][0].end;
+        }
+        const int heads = heads_of(p.ht);
+        const bool whole = p.begin == 0 && until == p.n;
+        const int to_slot = p.begin > 0 ? 0 : 1;
+        if (!whole) {
+            p.end = until;
+            shared_piece[to_slot] = p;
+        }
+        auto part = [&](int i, int h) { return parts + ((i * 2 + (i == first ? slot : 0)) * heads_most + h) * kRow; };
+        auto there = [&](int i) { return held[i][i == first ? slot : 0].b >= 0; };
+        for (int e = threadIdx.x; e < heads * D; e += kThreads) {
+            const int h = e / D, d = e % D;
+            float most = -INFINITY, l = 0.0f, o = 0.0f;
+            for (int i = first; i <= lastw; ++i)
+                if (there(i)) most = fmaxf(most, part(i, h)[D]);
+            for (int i = first; i <= lastw; ++i)
+                if (there(i)) {
+                    const float c = factor(part(i, h)[D], most);
+                    l += c * part(i, h)[D + 1];
+                    o += c * part(i, h)[d];
+                }
+            if (whole) {
+                const int64_t row = row_of(p.b, p.ht) + h;
+                write(row, d, l == 0.0f ? 0.0f : o / l);
+                if (a.lse && d == 0) a.lse[row] = l == 0.0f ? -INFINITY : most + logf(l);
+            } else {
+                float *const to = a.partial + ((int64_t)(g * 2 + to_slot) * kHeadTile + h) * kRow;
+                put(to + d, o);
+                if (d == 0) {
+                    put(to + D, most);
+                    put(to + D + 1, l);
+                }
+            }
+        }
+    }
+    // Parts in the workspace are written through to where all XCDs see them, and waited for, before this workgroup
+    // arrives; the last one's loads pass its caches by.
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    __syncthreads();
+    auto group_of = [&](int64_t f) { return (int)(((f + 1) * groups - 1) / T); };
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            const PieceOf &p = shared_piece[i];
+            last[i] = 0;
+            if (p.b < 0) continue;
+            const int64_t at = (int64_t)per * upto[p.b] + (int64_t)p.ht * p.n;
+            const int from = group_of(at), to = group_of(at + p.n - 1);
+            const uint32_t before = __hip_atomic_fetch_add(a.arrived + from, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            last[i] = before == (uint32_t)(to - from);
+            if (last[i]) __hip_atomic_store(a.arrived + from, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
+    __syncthreads();
+    for (int i = 0; i < 2; ++i) {
+        if (!last[i]) continue;  // (the same for the whole workgroup)
+        const PieceOf p = shared_piece[i];
+        const int64_t at = (int64_t)per * upto[p.b] + (int64_t)p.ht * p.n;
+        const int from = group_of(at), count = group_of(at + p.n - 1) - from + 1, heads = heads_of(p.ht);
+        auto part = [&](int j, int h) { return a.partial + ((int64_t)((from + j) * 2 + (j == 0 ? 1 : 0)) * kHeadTile + h) * kRow; };
+        // The factors of the parts, [count][heads], where the waves' parts were; l and m of a head behind them.
+        float *const scale = parts, *const sums = parts + count * heads;
+        __syncthreads();
+        for (int h = w; h < heads; h += kWaves) {
+            float most = -INFINITY, l = 0.0f;
+            for (int j = lane; j < count; j += 64) {
+                const float m = get(part(j, h) + D);
+                scale[j * heads + h] = m;
+                most = fmaxf(most, m);
+            }
+            for (int d = 32; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+            for (int j = lane; j < count; j += 64) {
+                const float c = factor(scale[j * heads + h], most);
+                scale[j * heads + h] = c;
+                l += c * get(part(j, h) + D + 1);
+            }
+            for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
+            if (lane == 0) {
+                sums[2 * h] = most;
+                sums[2 * h + 1] = l;
+            }
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < heads * D; e += kThreads) {
+            const int h = e / D, d = e % D;
+            float o = 0.0f;
+            constexpr int kAtOnce = 16;
+            for (int j0 = 0; j0 < count; j0 += kAtOnce) {
+                float v[kAtOnce];
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) v[j] = get(part(j0 + j < count ? j0 + j : 0, h) + d);
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j)
+                    if (j0 + j < count) o += scale[(j0 + j) * heads + h] * v[j];
+            }
+            const float most = sums[2 * h], l = sums[2 * h + 1];
+            const int64_t row = row_of(p.b, p.ht) + h;
+            write(row, d, l == 0.0f ? 0.0f : o / l);
+            if (a.lse && d == 0) a.lse[row] = l == 0.0f ? -INFINITY : most + logf(l);
+        }
+    }
 }
+
+constexpr int kMaxGroups = 256;
+constexpr int64_t kMostSteps = 1ll << 30;  // of all sequences, per head tile
 
 template <int D>
 int launch_attention(const AttentionArgs &a, hipStream_t st) {
-    const dim3 grid((unsigned)(a.B * a.c.heads * a.tiles)), block(64);
+    constexpr int kWaves = waves_of<D>();
+    const int cu = device_cu_count(), heads = a.group < kHeadTile ? a.group : kHeadTile;
+    const int64_t steps = (int64_t)a.B * (((int64_t)a.width << a.c.page_shift) / kStep + 1) * a.c.heads * a.tiles;
+    const int64_t want = (steps + 2 * kWaves - 1) / (2 * kWaves), most = cu < kMaxGroups ? cu : kMaxGroups;
+    const dim3 grid((unsigned)(want < most ? want : most)), block(64 * kWaves);
+    // (the parts' room also holds the factors and sums of a join: kMaxGroups + 2 per head)
+    static_assert(2 * kWaves * (D + 2) >= kMaxGroups + 2, "room for a join");
+    const size_t lds = (((size_t)a.B + 1) * 4 + 15) / 16 * 16 + sizeof(float) * 2 * kWaves * heads * (D + 2);
     if (a.c.e4m3)
-        hipLaunchKernelGGL((attention_kernel<D, true>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((attention_kernel<D, true>), grid, block, lds, st, a);
     else
-        hipLaunchKernelGGL((attention_kernel<D, false>), grid, block, 0, st, a);
+        hipLaunchKernelGGL((attention_kernel<D, false>), grid, block, lds, st, a);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
 }
@@ -289,7 +544,7 @@ bool attention_shape(const nvq_cache *c, int B, int H) {
 extern "C" size_t nvq_attention_workspace_bytes(const nvq_cache *cache, int B, int H) {
     using namespace nvq;
     if (!attention_shape(cache, B, H)) return 0;
-    return NVQ_ATTENTION_CLEAR_BYTES;
+    return NVQ_ATTENTION_CLEAR_BYTES + sizeof(float) * kMaxGroups * 2 * kHeadTile * (size_t)(cache->head_dim + 2);
 }
 
 extern "C" int nvq_attention(const nvq_cache *cache, const uint16_t *q, int64_t q_stride, int H, const int32_t *table, int B,
@@ -301,6 +556,7 @@ extern "C" int nvq_attention(const nvq_cache *cache, const uint16_t *q, int64_t 
         !(softcap >= 0.0f && softcap - softcap == 0.0f))
         return NVQ_ERR_INVALID_ARG;
     if (!attention_shape(cache, B, H) || table_width < 1 || (int64_t)table_width * cache->page_size > 1 << 30 || window < 0 ||
+        B * ((int64_t)table_width * cache->page_size / kStep + 1) > kMostSteps ||
         q_stride < (int64_t)H * cache->head_dim)
         return NVQ_ERR_SHAPE;
     if (!aligned(q, 16) || q_stride % 8 || !aligned(table, 4) || !aligned(lengths, 4) ||
@@ -325,6 +581,8 @@ extern "C" int nvq_attention(const nvq_cache *cache, const uint16_t *q, int64_t 
     a.out = out;
     a.out_dtype = out_dtype;
     a.lse = lse;
+    a.arrived = static_cast<uint32_t *>(workspace);
+    a.partial = reinterpret_cast<float *>(static_cast<char *>(workspace) + NVQ_ATTENTION_CLEAR_BYTES);
     const hipStream_t st = (hipStream_t)stream;
     switch (cache->head_dim / 32) {
         case 1: return launch_attention<32>(a, st);
