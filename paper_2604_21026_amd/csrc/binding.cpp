@@ -3,10 +3,10 @@
 // token: 6.4 us a call, of which the launch takes 3.6 and the kernel 2.7).
 //
 // Only the ordinary case is served here: tensors (no subclasses, which may say themselves where their
-// data is) of the expected types on a device (the microscaled products, the router and the experts: on the
-// current one), contiguous, with fitting shapes and room for what is written and read.  For everything else a
-// function returns None and the caller takes its own way, which names what is wrong.  The library's entry
-// points are handed over by address (bind); a call returns their status.
+// data is) of the expected types on a device (all but the int4 layers' calls: on the current one), contiguous
+// (queries, keys, values and logits: or with tokens apart), with fitting shapes and room for what is written
+// and read.  For everything else a function returns None and the caller takes its own way, which names what
+// is wrong.  The library's entry points are handed over by address (bind); a call returns their status.
 #include <Python.h>
 
 #include <c10/hip/HIPFunctions.h>
@@ -28,6 +28,11 @@ decltype(&nvq_gemv_mxfp4) g_gemv_mxfp4;
 decltype(&nvq_gemm_mxfp4) g_gemm_mxfp4;
 decltype(&nvq_moe_route) g_moe_route;
 decltype(&nvq_moe_experts) g_moe_experts;
+decltype(&nvq_cache_append) g_cache_append;
+decltype(&nvq_cache_read) g_cache_read;
+decltype(&nvq_attention) g_attention;
+decltype(&nvq_sample) g_sample;
+decltype(&nvq_adapters_add) g_adapters_add;
 
 constexpr int kAny = -1, kNone = -2;  // for a device's number: any, one that no tensor is on
 
@@ -322,14 +327,217 @@ PyObject *moe_experts(PyObject *, PyObject *const *a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// The handle of a call: the address of the struct that the library takes and the number of its device.  The device's
+// number if that is the current one, else kNone.
+template <typename T>
+int handle_of(PyObject *address, PyObject *device, const T **h) {
+    int d;
+    if (!PyLong_CheckExact(address) || !small_int(device, &d)) return kNone;
+    *h = static_cast<const T *>(PyLong_AsVoidPtr(address));
+    if (!*h) {
+        PyErr_Clear();
+        return kNone;
+    }
+    return d == c10::hip::current_device() ? d : kNone;
+}
+
+// bf16 [T][heads][D] whose tokens may lie apart, on that device.
+struct Rows {
+    const uint16_t *p;
+    int64_t T, heads, stride;
+};
+bool rows_of(PyObject *o, int64_t D, int device, Rows *r) {
+    if (!THPVariable_CheckExact(o)) return false;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.defined() || !t.is_cuda() || t.scalar_type() != at::kBFloat16 || t.get_device() != device || t.dim() != 3) return false;
+    r->T = t.size(0);
+    r->heads = t.size(1);
+    if (t.size(2) != D || t.stride(2) != 1 || (r->heads > 1 && t.stride(1) != D) || r->T > INT32_MAX || r->heads > INT32_MAX)
+        return false;
+    r->stride = r->T > 1 ? t.stride(0) : r->heads * D;
+    r->p = static_cast<const uint16_t *>(t.data_ptr());
+    return true;
+}
+
+// The address of a tensor as above, or null for None.
+template <typename T>
+bool room_or_none(PyObject *o, at::ScalarType type, int64_t n, int device, T **p) {
+    *p = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor *const t = device_room(o, type, n, device);
+    if (t) *p = static_cast<T *>(t->data_ptr());
+    return t != nullptr;
+}
+
+// The tokens of cache_append and cache_read.
+struct Tokens {
+    const int32_t *table, *positions, *sequences;
+    int B, width, T;
+};
+bool tokens_of(PyObject *table, PyObject *positions, PyObject *sequences, int here, Tokens *k) {
+    const at::Tensor *const t = device_tensor(table, at::kInt, 2, here), *const p = device_tensor(positions, at::kInt, 1, here);
+    if (!t || !p || t->size(0) > INT32_MAX || t->size(1) > INT32_MAX || p->size(0) > INT32_MAX) return false;
+    k->sequences = nullptr;
+    if (sequences != Py_None) {
+        const at::Tensor *const s = device_tensor(sequences, at::kInt, 1, here);
+        if (!s || s->size(0) != p->size(0)) return false;
+        k->sequences = static_cast<const int32_t *>(s->data_ptr());
+    }
+    k->table = static_cast<const int32_t *>(t->data_ptr());
+    k->positions = static_cast<const int32_t *>(p->data_ptr());
+    k->B = (int)t->size(0);
+    k->width = (int)t->size(1);
+    k->T = (int)p->size(0);
+    return true;
+}
+
+// (address of an nvq_cache, its device, table, positions, k, v, q, cos_sin, interleaved, sequences, out); q, cos_sin,
+// sequences, out: or None
+PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const nvq_cache *c;
+    if (n != 11) return none();
+    const int here = handle_of(a[0], a[1], &c);
+    Tokens at;
+    Rows k, v, q = {nullptr, 0, 0, 0};
+    int interleaved;
+    if (here == kNone || !tokens_of(a[2], a[3], a[9], here, &at) || !rows_of(a[4], c->head_dim, here, &k) ||
+        !rows_of(a[5], c->head_dim, here, &v) || !small_int(a[8], &interleaved))
+        return none();
+    if (k.T != at.T || v.T != at.T || k.heads != c->heads || v.heads != c->heads) return none();
+    uint16_t *out = nullptr;
+    if (a[6] != Py_None) {
+        if (!rows_of(a[6], c->head_dim, here, &q) || q.T != at.T) return none();
+        const at::Tensor *const o = device_room(a[10], at::kBFloat16, q.T * q.heads * c->head_dim, here);
+        if (!o) return none();
+        out = static_cast<uint16_t *>(o->data_ptr());
+    } else if (a[10] != Py_None) {
+        return none();
+    }
+    const float *cos_sin = nullptr;
+    int angles = 0, rot = 0;
+    if (a[7] != Py_None) {
+        const at::Tensor *const t = device_tensor(a[7], at::kFloat, 2, here);
+        if (!t || t->size(0) > INT32_MAX || t->size(1) > INT32_MAX) return none();
+        cos_sin = static_cast<const float *>(t->data_ptr());
+        angles = (int)t->size(0);
+        rot = (int)t->size(1);
+    }
+    void *const st = current_stream();
+    return status_of([&] {
+        return g_cache_append(c, at.table, at.B, at.width, at.sequences, at.positions, at.T, q.p, q.stride, (int)q.heads, out, k.p,
+                              k.stride, v.p, v.stride, cos_sin, angles, rot, interleaved, st);
+    });
+    END_HANDLE_TH_ERRORS
+}
+
+// (address of an nvq_cache, its device, table, positions, sequences or None, k, v)
+PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const nvq_cache *c;
+    if (n != 7) return none();
+    const int here = handle_of(a[0], a[1], &c);
+    Tokens at;
+    if (here == kNone || !tokens_of(a[2], a[3], a[4], here, &at)) return none();
+    const int64_t values = (int64_t)at.T * c->heads * c->head_dim;
+    const at::Tensor *const k = device_room(a[5], at::kBFloat16, values, here), *const v = device_room(a[6], at::kBFloat16, values, here);
+    if (!k || !v) return none();
+    uint16_t *const kp = static_cast<uint16_t *>(k->data_ptr()), *const vp = static_cast<uint16_t *>(v->data_ptr());
+    void *const st = current_stream();
+    return status_of([&] { return g_cache_read(c, at.table, at.B, at.width, at.sequences, at.positions, at.T, kp, vp, st); });
+    END_HANDLE_TH_ERRORS
+}
+
+// (address of an nvq_cache, its device, q, table, lengths, scale, window, softcap, out, lse or None, workspace)
+PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const nvq_cache *c;
+    if (n != 11) return none();
+    const int here = handle_of(a[0], a[1], &c);
+    Rows q;
+    int window, out_dtype;
+    if (here == kNone || !rows_of(a[2], c->head_dim, here, &q) || !PyFloat_CheckExact(a[5]) || !small_int(a[6], &window) ||
+        !PyFloat_CheckExact(a[7]))
+        return none();
+    const float scale = (float)PyFloat_AS_DOUBLE(a[5]), softcap = (float)PyFloat_AS_DOUBLE(a[7]);
+    const at::Tensor *const table = device_tensor(a[3], at::kInt, 2, here), *const lengths = device_tensor(a[4], at::kInt, 1, here),
+                     *const out = output_tensor(a[8], q.T * q.heads * c->head_dim, &out_dtype, here),
+                     *const ws = device_tensor(a[10], at::kByte, -1, here);
+    float *lse;
+    if (!table || !lengths || !out || !ws || table->size(0) != q.T || lengths->size(0) != q.T || table->size(1) > INT32_MAX ||
+        !room_or_none(a[9], at::kFloat, q.T * q.heads, here, &lse))
+        return none();
+    const int32_t *const tp = static_cast<const int32_t *>(table->data_ptr()), *const lp = static_cast<const int32_t *>(lengths->data_ptr());
+    const int width = (int)table->size(1);
+    void *const yp = out->data_ptr(), *const sp = ws->data_ptr(), *const st = current_stream();
+    const size_t bytes = (size_t)ws->numel();
+    return status_of([&] {
+        return g_attention(c, q.p, q.stride, (int)q.heads, tp, (int)q.T, width, lp, scale, window, softcap, yp, out_dtype, lse, sp,
+                           bytes, st);
+    });
+    END_HANDLE_TH_ERRORS
+}
+
+// (logits, u, temperature, top_k, top_p, min_p, out, workspace); the four in the middle: or None
+PyObject *sample(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 8) return none();
+    const int here = device_of(a[0]);
+    if (here == kNone) return none();
+    const at::Tensor &l = THPVariable_Unpack(a[0]);
+    if (l.dim() != 2 || (l.scalar_type() != at::kFloat && l.scalar_type() != at::kBFloat16) || (l.size(1) > 1 && l.stride(1) != 1) ||
+        l.size(0) > INT32_MAX || l.size(1) > INT32_MAX)
+        return none();
+    const int M = (int)l.size(0), V = (int)l.size(1), dtype = l.scalar_type() == at::kFloat ? NVQ_F32 : NVQ_BF16;
+    const int64_t ld = M > 1 ? l.stride(0) : V;
+    const at::Tensor *const u = device_room(a[1], at::kFloat, M, here), *const ids = device_room(a[6], at::kInt, M, here),
+                     *const ws = device_tensor(a[7], at::kByte, -1, here);
+    float *temperature, *top_p, *min_p;
+    int32_t *top_k;
+    if (!u || !ids || !ws || !room_or_none(a[2], at::kFloat, M, here, &temperature) || !room_or_none(a[3], at::kInt, M, here, &top_k) ||
+        !room_or_none(a[4], at::kFloat, M, here, &top_p) || !room_or_none(a[5], at::kFloat, M, here, &min_p))
+        return none();
+    const void *const lp = l.data_ptr();
+    const float *const up = static_cast<const float *>(u->data_ptr());
+    int32_t *const ip = static_cast<int32_t *>(ids->data_ptr());
+    void *const sp = ws->data_ptr(), *const st = current_stream();
+    const size_t bytes = (size_t)ws->numel();
+    return status_of([&] { return g_sample(lp, dtype, ld, M, V, up, temperature, top_k, top_p, min_p, ip, sp, bytes, st); });
+    END_HANDLE_TH_ERRORS
+}
+
+// (address of an nvq_adapters, its device, x, ids, y, out, workspace)
+PyObject *adapters_add(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    const nvq_adapters *g;
+    if (n != 7) return none();
+    const int here = handle_of(a[0], a[1], &g);
+    if (here == kNone) return none();
+    const at::Tensor *const x = device_tensor(a[2], at::kBFloat16, 2, here), *const ids = device_tensor(a[3], at::kInt, 1, here),
+                     *const ws = device_tensor(a[6], at::kByte, -1, here);
+    if (!x || !ids || !ws || x->size(1) != g->K || x->size(0) != ids->size(0) || x->size(0) > INT32_MAX) return none();
+    const int M = (int)x->size(0);
+    int dtype, out_dtype;
+    const at::Tensor *const y = output_tensor(a[4], (int64_t)M * g->N, &dtype, here),
+                     *const out = output_tensor(a[5], (int64_t)M * g->N, &out_dtype, here);
+    if (!y || !out || dtype != out_dtype || y->dim() != 2 || y->size(0) != M || y->size(1) != g->N) return none();
+    const uint16_t *const xp = static_cast<const uint16_t *>(x->data_ptr());
+    const int32_t *const ip = static_cast<const int32_t *>(ids->data_ptr());
+    const void *const yp = y->data_ptr();
+    void *const op = out->data_ptr(), *const sp = ws->data_ptr(), *const st = current_stream();
+    const size_t bytes = (size_t)ws->numel();
+    return status_of([&] { return g_adapters_add(g, xp, ip, M, yp, op, dtype, sp, bytes, st); });
+    END_HANDLE_TH_ERRORS
+}
+
 // The addresses of gemv_w4a16, gemv_w4a8, quant_act_i8, gemm_w4a16, quant_mxfp4, dequant_mxfp4, gemv_mxfp4, gemm_mxfp4,
-// moe_route, moe_experts in the library.
+// moe_route, moe_experts, cache_append, cache_read, attention, sample, adapters_add in the library.
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    constexpr int kCalls = 10;
+    constexpr int kCalls = 15;
     void *p[kCalls];
     if (n != kCalls) {
-        PyErr_SetString(PyExc_TypeError, "ten addresses");
+        PyErr_SetString(PyExc_TypeError, "fifteen addresses");
         return nullptr;
     }
     for (int i = 0; i < kCalls; ++i) {
@@ -349,6 +557,11 @@ PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n) {
     g_gemm_mxfp4 = reinterpret_cast<decltype(g_gemm_mxfp4)>(p[7]);
     g_moe_route = reinterpret_cast<decltype(g_moe_route)>(p[8]);
     g_moe_experts = reinterpret_cast<decltype(g_moe_experts)>(p[9]);
+    g_cache_append = reinterpret_cast<decltype(g_cache_append)>(p[10]);
+    g_cache_read = reinterpret_cast<decltype(g_cache_read)>(p[11]);
+    g_attention = reinterpret_cast<decltype(g_attention)>(p[12]);
+    g_sample = reinterpret_cast<decltype(g_sample)>(p[13]);
+    g_adapters_add = reinterpret_cast<decltype(g_adapters_add)>(p[14]);
     return none();
     END_HANDLE_TH_ERRORS
 }
@@ -372,6 +585,11 @@ PyMethodDef methods[] = {{"bind", NVQ_FAST(bind)},
                          {"gemm_mxfp4", NVQ_FAST(gemm_mxfp4)},
                          {"moe_route", NVQ_FAST(moe_route)},
                          {"moe_experts", NVQ_FAST(moe_experts)},
+                         {"cache_append", NVQ_FAST(cache_append)},
+                         {"cache_read", NVQ_FAST(cache_read)},
+                         {"attention", NVQ_FAST(attention)},
+                         {"sample", NVQ_FAST(sample)},
+                         {"adapters_add", NVQ_FAST(adapters_add)},
                          {"stream_handle", stream_handle, METH_NOARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

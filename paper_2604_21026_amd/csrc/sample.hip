@@ -1,10 +1,16 @@
 // nvq_sample: the next token of each row of logits.
 //
 // Every question is one of the descending order of a row's tokens: which token brings the count to top_k, the sum of
-// the weights to top_p, to u times the kept sum.  It is answered without sorting: the logits are words whose unsigned
-// order is theirs, a histogram over eight bits of them (counts, or sums of weights) says in which bin the answer
-// lies, and the next eight bits are looked at inside that bin alone.  Weights are 64-bit fixed point, so that sums do
-// not depend on their order and all passes agree to the last bit.
+// the weights to top_p, to u times the kept sum.  It is answered without sorting the row, in two launches:
+//   1. Workgroups share a row's logits, a part each: the part's largest, and relative to it a histogram of counts and
+//      weights over bins of min(temperature, 1) / 32 in the logit.  The one that arrives last adds the parts' bins up
+//      and sees in which bins the answers can lie: the weight of a bin that a border falls into is known, which of its
+//      tokens are in is not, so the later borders are ranges of a bin or a few.
+//   2. The tokens of those bins are collected (a few hundred of 128256), and the workgroup that arrives last sorts
+//      them by logit and index and answers every question to the token.
+// Weights are 64-bit fixed point relative to the largest, so that sums do not depend on their order.  A row whose bins
+// hold too many tokens (nearly equal logits), or whose logits are out of the bins' range, is looked at by one workgroup
+// alone, eight bits of the sort words after the other (choose_slowly).
 #include "mfma_act.h"
 
 namespace nvq {
@@ -23,6 +29,11 @@ struct SampleArgs {
     const float *u, *temperature, *top_p, *min_p;
     const int32_t *top_k;
     int32_t *ids;
+    int parts, part;  // workgroups to a row, logits of each
+    uint32_t *arrived;  // workspace
+    struct RowState *rows;
+    struct PartHead *heads;
+    struct PartBins *bins;
 };
 
 // Words in the order of the logits; minus infinity and NaN: 0, both zeros alike.
@@ -38,17 +49,40 @@ __device__ __forceinline__ float of_sort_word(uint32_t w) {
 struct Row {
     const void *at;
     int dtype, V;
-    __device__ uint32_t word(int i) const {
-        return sort_word(dtype == NVQ_F32 ? static_cast<const float *>(at)[i]
-                                          : bf16_bits_to_float(static_cast<const uint16_t *>(at)[i]));
+    __device__ float logit(int i) const {
+        return dtype == NVQ_F32 ? *as_global<float>(static_cast<const float *>(at) + i)
+                                : bf16_bits_to_float(*as_global<uint16_t>(static_cast<const uint16_t *>(at) + i));
     }
+    __device__ uint32_t word(int i) const { return sort_word(logit(i)); }
 };
 
+// exp(x) as fixed point, x = (logit - top) / temperature <= 0: 2^k times the exponential series of the rest, |rest| <=
+// ln 2 / 2, to 13 terms (the next is 2e-16 of the sum).  One half unit of the last place, 2^-44, as rounding.
 struct Weights {
-    double top, temperature;
-    __device__ uint64_t of(uint32_t word) const {
-        return (uint64_t)(exp(((double)of_sort_word(word) - top) / temperature) * kOne + 0.5);
+    double top, rate;  // log2(e) / temperature
+    __device__ Weights(float most, float temperature) : top(most), rate(1.4426950408889634074 / (double)temperature) {}
+    __device__ uint64_t of(float logit) const {
+        double t = ((double)logit - top) * rate;
+        t = t > -64.0 ? t : -64.0;  // (nothing is left of the weight long before)
+        const double k = rint(t), x = (t - k) * 0.69314718055994530942;
+        double e = 1.0 / 479001600;
+        e = fma(e, x, 1.0 / 39916800);
+        e = fma(e, x, 1.0 / 3628800);
+        e = fma(e, x, 1.0 / 362880);
+        e = fma(e, x, 1.0 / 40320);
+        e = fma(e, x, 1.0 / 5040);
+        e = fma(e, x, 1.0 / 720);
+        e = fma(e, x, 1.0 / 120);
+        e = fma(e, x, 1.0 / 24);
+        e = fma(e, x, 1.0 / 6);
+        e = fma(e, x, 0.5);
+        e = fma(e, x, 1.0);
+        e = fma(e, x, 1.0);
+        // e times 2^(k + kPoint), below 2^44; beside 2^52 its whole part is the low bits
+        const double scaled = __longlong_as_double(__double_as_longlong(e) + ((int64_t)((int)k + kPoint) << 52));
+        return (uint64_t)__double_as_longlong(scaled + 4503599627370496.0) & 0xfffffffffffffull;
     }
+    __device__ uint64_t of_word(uint32_t word) const { return of(of_sort_word(word)); }
 };
 
 struct Shared {
@@ -93,7 +127,7 @@ __device__ void find(Shared &s, const Row &row, const Weights &w, uint64_t x, ui
             const uint32_t v = row.word(i);
             if (v == 0 || (shift < 24 && v >> (shift + 8) != prefix)) continue;
             if (MASS)
-                atomicAdd(&s.mass[v >> shift & 255], (unsigned long long)w.of(v));
+                atomicAdd(&s.mass[v >> shift & 255], (unsigned long long)w.of_word(v));
             else
                 atomicAdd(&s.count[v >> shift & 255], 1u);
         }
@@ -147,74 +181,514 @@ __device__ int nth_of_word(Shared &s, const Row &row, uint32_t word, uint64_t n)
     return (int)s.bin;
 }
 
-__global__ __launch_bounds__(kSampleThreads) void sample_kernel(SampleArgs a) {
-    __shared__ Shared s;
-    const int m = blockIdx.x;
-    Row row;
-    row.at = a.dtype == NVQ_F32 ? (const void *)(static_cast<const float *>(a.logits) + m * a.ld)
-                                : (const void *)(static_cast<const uint16_t *>(a.logits) + m * a.ld);
-    row.dtype = a.dtype;
-    row.V = a.V;
-    uint64_t best = 0, n = 0;
-    for (int i = threadIdx.x; i < a.V; i += kSampleThreads) {
-        const uint32_t v = row.word(i);
-        const uint64_t k = (uint64_t)v << 32 | (uint32_t)~i;
-        best = k > best ? k : best;
-        n += v != 0;
-    }
-    best = over_block(s, best, Most64());
-    n = over_block(s, n, Add64());
-    const uint32_t top = (uint32_t)(best >> 32);
-    const float temperature = a.temperature ? a.temperature[m] : 1.0f, most = of_sort_word(top);
-    if (top == 0 || !(temperature > 0.0f) || most == INFINITY) {  // (the same for the whole row)
-        if (threadIdx.x == 0) a.ids[m] = top == 0 ? -1 : (int)~(uint32_t)best;
-        return;
-    }
-    const Weights w{(double)most, (double)temperature};
-    const int top_k = a.top_k ? a.top_k[m] : 0;
-    const float top_p = a.top_p ? a.top_p[m] : 1.0f, min_p = a.min_p ? a.min_p[m] : 0.0f;
+// What a row asks for.
+struct Ask {
+    float temperature, top_p, min_p, u;
+    int top_k;
+};
+__device__ __forceinline__ Ask ask_of(const SampleArgs &a, int m) {
+    Ask k;
+    k.temperature = a.temperature ? a.temperature[m] : 1.0f;
+    k.top_k = a.top_k ? a.top_k[m] : 0;
+    k.top_p = a.top_p ? a.top_p[m] : 1.0f;
+    k.min_p = a.min_p ? a.min_p[m] : 0.0f;
+    k.u = a.u[m];
+    return k;
+}
+__device__ __forceinline__ Row row_of(const SampleArgs &a, int m) {
+    Row r;
+    r.at = a.dtype == NVQ_F32 ? (const void *)(static_cast<const float *>(a.logits) + m * a.ld)
+                              : (const void *)(static_cast<const uint16_t *>(a.logits) + m * a.ld);
+    r.dtype = a.dtype;
+    r.V = a.V;
+    return r;
+}
+// Where in a kept sum the random number points.
+__device__ __forceinline__ uint64_t point_of(float u, uint64_t kept) {
+    const uint64_t x = !(u > 0.0f) ? 0 : u >= 1.0f ? kept - 1 : (uint64_t)((double)u * (double)kept);
+    return x < kept ? x : kept - 1;
+}
+// The sum that top_p asks for, at least 1 and at most all.
+__device__ __forceinline__ uint64_t reach_of(float top_p, uint64_t all) {
+    const double share = top_p > 0.0f ? ceil((double)top_p * (double)all) : 0.0;
+    return share < 1.0 ? 1 : share < (double)all ? (uint64_t)share : all;
+}
+
+// The answer for a row of n tokens to choose from, by one workgroup and any logits.
+__device__ int choose_slowly(Shared &s, const Row &row, const Ask &k, float most, uint64_t n) {
+    const Weights w(most, k.temperature);
     uint32_t word;
     uint64_t before, kept;
-    if (top_k > 0 && (uint64_t)top_k < n) {
-        find<false>(s, row, w, (uint64_t)top_k - 1, &word, &before);
+    if (k.top_k > 0 && (uint64_t)k.top_k < n) {
+        find<false>(s, row, w, (uint64_t)k.top_k - 1, &word, &before);
         uint64_t above = 0;
-        for (int i = threadIdx.x; i < a.V; i += kSampleThreads) {
+        for (int i = threadIdx.x; i < row.V; i += kSampleThreads) {
             const uint32_t v = row.word(i);
-            above += v > word ? w.of(v) : 0;
+            above += v > word ? w.of_word(v) : 0;
         }
-        kept = over_block(s, above, Add64()) + ((uint64_t)top_k - before) * w.of(word);
+        kept = over_block(s, above, Add64()) + ((uint64_t)k.top_k - before) * w.of_word(word);
     } else {
         uint64_t all = 0;
-        for (int i = threadIdx.x; i < a.V; i += kSampleThreads) {
+        for (int i = threadIdx.x; i < row.V; i += kSampleThreads) {
             const uint32_t v = row.word(i);
-            all += v ? w.of(v) : 0;
+            all += v ? w.of_word(v) : 0;
         }
         kept = over_block(s, all, Add64());
     }
-    if (!(top_p >= 1.0f)) {
-        const double share = top_p > 0.0f ? ceil((double)top_p * (double)kept) : 0.0;
-        const uint64_t reach = share < 1.0 ? 1 : share < (double)kept ? (uint64_t)share : kept;
+    if (!(k.top_p >= 1.0f)) {
+        const uint64_t reach = reach_of(k.top_p, kept);
         find<true>(s, row, w, reach - 1, &word, &before);
-        const uint64_t each = w.of(word);
+        const uint64_t each = w.of_word(word);
         kept = before + (reach - before + each - 1) / each * each;
     }
-    if (min_p > 0.0f) {
+    if (k.min_p > 0.0f) {
         uint64_t enough = 0;
-        for (int i = threadIdx.x; i < a.V; i += kSampleThreads) {
+        for (int i = threadIdx.x; i < row.V; i += kSampleThreads) {
             const uint32_t v = row.word(i);
-            const uint64_t x = v ? w.of(v) : 0;
-            enough += (double)x >= (double)min_p * kOne ? x : 0;
+            const uint64_t x = v ? w.of_word(v) : 0;
+            enough += (double)x >= (double)k.min_p * kOne ? x : 0;
         }
         enough = over_block(s, enough, Add64());
         kept = enough < kept ? enough : kept;
     }
     kept = kept < 1ull << kPoint ? 1ull << kPoint : kept;  // (the first token's weight is 1)
-    const float u = a.u[m];
-    const uint64_t x = !(u > 0.0f) ? 0 : u >= 1.0f ? kept - 1 : (uint64_t)((double)u * (double)kept);
-    find<true>(s, row, w, x < kept ? x : kept - 1, &word, &before);
-    const uint64_t at = x < kept ? x : kept - 1;
-    const int id = nth_of_word(s, row, word, (at - before) / w.of(word));
-    if (threadIdx.x == 0) a.ids[m] = id;
+    const uint64_t x = point_of(k.u, kept);
+    find<true>(s, row, w, x, &word, &before);
+    return nth_of_word(s, row, word, (x - before) / w.of_word(word));
+}
+
+// ---- bins
+constexpr int kBins = kSampleThreads;   // the last one: everything below the others
+constexpr int kBlock = 8 * kSampleThreads;  // logits that a workgroup has in flight together
+constexpr int kList = 4096;             // tokens that can be collected
+constexpr int kMostParts = 32;
+constexpr float kFar = 16777216.0f;     // bin numbers are whole floats up to here
+static_assert(NVQ_SAMPLE_CLEAR_BYTES >= 4 * NVQ_SAMPLE_MAX_M, "a counter per row");
+
+// Bins of a row: number floor(logit * steps), and from the largest one down the place among kBins.
+struct Grid {
+    float steps, top;  // top: the largest logit's number
+    __device__ static float steps_of(float temperature) { return 32.0f / (temperature < 1.0f ? temperature : 1.0f); }
+    __device__ static float number(float logit, float steps) { return fmaxf(floorf(logit * steps), -kFar); }
+    __device__ int bin(float logit) const { return (int)fminf(fmaxf(top - number(logit, steps), 0.0f), (float)(kBins - 1)); }
+};
+
+struct PartHead {
+    unsigned long long best;  // sort word and complement of the index of the part's first token; 0: none
+};
+struct PartBins {
+    unsigned long long mass[kBins];  // relative to the part's largest
+    uint32_t count[kBins];
+};
+// What the second launch has to know of a row.
+struct RowState {
+    uint32_t gather;   // 0: the row has its answer
+    uint32_t listed, arrived;
+    float steps, top, most;
+    int lo[4], hi[4];  // bins whose tokens are collected
+    unsigned long long all;  // of the weights
+    uint32_t count;
+    int cut;           // min_p: bins before have the weight, those from cut + 3 on have not
+    unsigned long long before[kBins];  // weights of the bins before
+    uint32_t ranked[kBins];            // tokens of the bins before
+    uint32_t first[kBins];             // collected tokens of the bins before
+    unsigned long long list[kList];
+};
+
+__device__ __forceinline__ void put64(unsigned long long *p, uint64_t v) {
+    __hip_atomic_store(p, (unsigned long long)v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ uint64_t get64(const unsigned long long *p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ void put32(uint32_t *p, uint32_t v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ uint32_t get32(const uint32_t *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Sum over the threads before this one; *all: over all.
+template <typename T>
+__device__ T scan_block(T *wave, T v, T *all) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    T sum = v;
+    for (int d = 1; d < 64; d <<= 1) {
+        const T o = __shfl_up(sum, d);
+        if (lane >= d) sum += o;
+    }
+    __syncthreads();
+    if (lane == 63) wave[w] = sum;
+    __syncthreads();
+    T before = 0, total = 0;
+    for (int i = 0; i < kSampleWaves; ++i) {
+        const T x = wave[i];
+        before += i < w ? x : 0;
+        total += x;
+    }
+    *all = total;
+    return before + sum - v;
+}
+// The lowest thread for which `is` holds, kSampleThreads if none.
+__device__ __forceinline__ int first_thread(uint32_t *wave, bool is) {
+    const uint64_t b = __ballot(is);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = b ? (uint32_t)(threadIdx.x + __builtin_ctzll(b)) : (uint32_t)kSampleThreads;
+    __syncthreads();
+    uint32_t f = kSampleThreads;
+    for (int i = 0; i < kSampleWaves; ++i) f = wave[i] < f ? wave[i] : f;
+    return (int)f;
+}
+
+// A workgroup's part of a row: logits [*i0, *i1).
+__device__ __forceinline__ void part_of(const SampleArgs &a, int part, int *i0, int *i1) {
+    *i0 = part * a.part < a.V ? part * a.part : a.V;
+    *i1 = *i0 + a.part < a.V ? *i0 + a.part : a.V;
+}
+
+__global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(SampleArgs a) {
+    __shared__ Shared s;
+    __shared__ unsigned long long mass[kBins], wave64[kSampleWaves];
+    __shared__ uint32_t count[kBins], wave32[kSampleWaves];
+    __shared__ unsigned long long heads[kMostParts];
+    __shared__ unsigned long long edge[2];
+    __shared__ uint32_t last;
+    const int m = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x;
+    const Row row = row_of(a, m);
+    const Ask k = ask_of(a, m);
+    RowState &state = a.rows[m];
+    int i0, i1;
+    part_of(a, part, &i0, &i1);
+
+    uint64_t best = 0;
+    for (int b = i0; b < i1; b += kBlock) {
+        float l[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = b + j * kSampleThreads + tid;
+            l[j] = i < i1 ? row.logit(i) : -INFINITY;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t v = sort_word(l[j]);
+            const uint64_t key = v ? (uint64_t)v << 32 | (uint32_t)~(b + j * kSampleThreads + tid) : 0;
+            best = key > best ? key : best;
+        }
+    }
+    mass[tid] = 0;
+    count[tid] = 0;
+    best = over_block(s, best, Most64());
+    const uint32_t top_word = (uint32_t)(best >> 32);
+    const bool ordinary = k.temperature > 0.0f;  // (else the first token is the answer)
+    const float steps = Grid::steps_of(k.temperature);
+    if (ordinary && top_word) {
+        const float most = of_sort_word(top_word);
+        const Weights w(most, k.temperature);
+        const Grid grid = {steps, Grid::number(most, steps)};
+        for (int b = i0; b < i1; b += kBlock) {
+            float l[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int i = b + j * kSampleThreads + tid;
+                l[j] = i < i1 ? row.logit(i) : -INFINITY;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (!(l[j] > -INFINITY)) continue;
+                const int bin = grid.bin(l[j]);
+                atomicAdd(&count[bin], 1u);
+                atomicAdd(&mass[bin], (unsigned long long)w.of(l[j]));
+            }
+        }
+    }
+    __syncthreads();
+    if (a.parts > 1) {
+        PartBins &to = a.bins[(int64_t)m * a.parts + part];
+        put64(&to.mass[tid], mass[tid]);
+        put32(&to.count[tid], count[tid]);
+        if (tid == 0) put64(&a.heads[(int64_t)m * a.parts + part].best, best);
+        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): written through to where all XCDs see it
+        __syncthreads();
+        if (tid == 0) {
+            const uint32_t before = __hip_atomic_fetch_add(a.arrived + m, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            last = before == (uint32_t)a.parts - 1;
+            if (last) put32(a.arrived + m, 0);
+        }
+        __syncthreads();
+        if (!last) return;
+        if (tid < a.parts) heads[tid] = get64(&a.heads[(int64_t)m * a.parts + tid].best);
+        __syncthreads();
+        best = 0;
+        for (int p = 0; p < a.parts; ++p) best = heads[p] > best ? heads[p] : best;
+    }
+    const uint32_t first = (uint32_t)(best >> 32);
+    const float most = of_sort_word(first);
+    if (first == 0 || !ordinary || most == INFINITY) {  // (the same for the whole row)
+        if (tid == 0) {
+            a.ids[m] = first == 0 ? -1 : (int)~(uint32_t)best;
+            state.gather = 0;
+        }
+        return;
+    }
+    const Grid grid = {steps, Grid::number(most, steps)};
+    if (a.parts > 1) {
+        mass[tid] = 0;
+        count[tid] = 0;
+        __syncthreads();
+        for (int p0 = 0; p0 < a.parts; p0 += 8) {
+            uint64_t ms[8];
+            uint32_t cs[8];
+#pragma unroll
+            for (int p = 0; p < 8; ++p) {
+                const PartBins &from = a.bins[(int64_t)m * a.parts + (p0 + p < a.parts ? p0 + p : 0)];
+                ms[p] = get64(&from.mass[tid]);
+                cs[p] = get32(&from.count[tid]);
+            }
+#pragma unroll
+            for (int p = 0; p < 8; ++p) {
+                if (p0 + p >= a.parts || cs[p] == 0) continue;
+                const float top = of_sort_word((uint32_t)(heads[p0 + p] >> 32));
+                const float shift = grid.top - Grid::number(top, steps);
+                const int bin = (int)fminf(shift + (float)tid, (float)(kBins - 1));
+                // its weights, relative to the row's largest
+                const double f = exp(((double)top - (double)most) / (double)k.temperature);
+                atomicAdd(&count[bin], cs[p]);
+                atomicAdd(&mass[bin], (unsigned long long)(f * (double)ms[p]));
+            }
+        }
+        __syncthreads();
+    }
+    // Where the answers can lie.  Bounds of the sums are a little wide: a bin's weight has been rounded otherwise than
+    // the sum of its tokens'.
+    const uint64_t mine = mass[tid];
+    const uint32_t here = count[tid];
+    unsigned long long all;
+    uint32_t n;
+    const uint64_t before = scan_block(wave64, (unsigned long long)mine, &all);
+    const uint32_t ranked = scan_block(wave32, here, &n);
+    const uint64_t upto = before + mine;
+    const double wide = 1.0 + 0x1p-30;
+    auto bin_reaching = [&](double x) {  // the first bin with which the sum reaches x
+        const int b = first_thread(wave32, here && (double)upto >= x);
+        return b < kBins ? b : kBins - 1;
+    };
+    auto bounds = [&](int lo, int hi, double *least, double *most_) {  // of a sum that ends in these bins
+        __syncthreads();
+        if (tid == lo) edge[0] = before;
+        if (tid == hi) edge[1] = upto;
+        __syncthreads();
+        *least = (double)edge[0];
+        *most_ = (double)edge[1];
+    };
+    int lo[4] = {kBins, kBins, kBins, kBins}, hi[4] = {-1, -1, -1, -1}, cut = 0;
+    double least = (double)all, greatest = (double)all;
+    if (k.top_k > 0 && (uint32_t)k.top_k < n) {
+        lo[0] = hi[0] = first_thread(wave32, ranked + here >= (uint32_t)k.top_k);
+        bounds(lo[0], hi[0], &least, &greatest);
+    }
+    if (!(k.top_p >= 1.0f)) {
+        const double p = k.top_p > 0.0f ? (double)k.top_p : 0.0;
+        lo[1] = bin_reaching(fmax(p * least / wide, 1.0));
+        hi[1] = bin_reaching(fmin(fmax(p * greatest * wide + 2.0, 1.0), (double)all));
+        hi[1] = hi[1] > lo[1] ? hi[1] : lo[1];
+        double l, g;
+        bounds(lo[1], hi[1], &l, &g);
+        least = fmin(least, l);
+        greatest = fmin(greatest, g);
+    }
+    if (k.min_p > 0.0f) {
+        const double at = (double)most + (double)k.temperature * log((double)k.min_p);
+        cut = grid.bin((float)at);  // (its rounding moves it to a neighbouring bin at most)
+        cut = cut > 0 ? cut - 1 : 0;
+        lo[2] = cut;
+        hi[2] = cut + 2 < kBins - 1 ? cut + 2 : kBins - 1;
+        double l, g;
+        bounds(lo[2], hi[2], &l, &g);
+        least = fmin(least, l);
+        greatest = fmin(greatest, g);
+    }
+    least = fmax(least, kOne);
+    greatest = fmax(greatest, kOne);
+    const double u = k.u > 0.0f ? (k.u < 1.0f ? (double)k.u : 1.0) : 0.0;
+    lo[3] = bin_reaching(fmax(u * least / wide - 2.0, 0.0));
+    hi[3] = bin_reaching(fmin(u * greatest * wide + 2.0, (double)all));
+    hi[3] = hi[3] > lo[3] ? hi[3] : lo[3];
+    bool wanted = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) wanted |= tid >= lo[i] && tid <= hi[i];
+    uint32_t listed;
+    const uint32_t at = scan_block(wave32, wanted ? here : 0u, &listed);
+    if (listed > (uint32_t)kList || !(fabsf(grid.top) < kFar)) {  // (the same for the whole row)
+        __syncthreads();
+        const int id = choose_slowly(s, row, k, most, n);
+        if (tid == 0) {
+            a.ids[m] = id;
+            state.gather = 0;
+        }
+        return;
+    }
+    state.before[tid] = before;
+    state.ranked[tid] = ranked;
+    state.first[tid] = at;
+    if (tid == 0) {
+        state.gather = 1;
+        state.listed = 0;
+        state.arrived = 0;
+        state.steps = steps;
+        state.top = grid.top;
+        state.most = most;
+        for (int i = 0; i < 4; ++i) {
+            state.lo[i] = lo[i];
+            state.hi[i] = hi[i];
+        }
+        state.all = all;
+        state.count = n;
+        state.cut = cut;
+    }
+}
+
+__global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs a) {
+    __shared__ unsigned long long key[kList], sum[kList + 1], wave64[kSampleWaves];
+    __shared__ uint32_t wave32[kSampleWaves], shared_at, last;
+    __shared__ unsigned long long found[3];
+    const int m = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x;
+    RowState &state = a.rows[m];
+    if (!state.gather) return;
+    const Row row = row_of(a, m);
+    const Grid grid = {state.steps, state.top};
+    int lo[4], hi[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        lo[i] = state.lo[i];
+        hi[i] = state.hi[i];
+    }
+    int i0, i1;
+    part_of(a, part, &i0, &i1);
+    for (int b = i0; b < i1; b += kBlock) {
+        float l[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = b + j * kSampleThreads + tid;
+            l[j] = i < i1 ? row.logit(i) : -INFINITY;
+        }
+        uint32_t hits = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int bin = l[j] > -INFINITY ? grid.bin(l[j]) : kBins;
+            bool is = false;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) is |= bin >= lo[i] && bin <= hi[i];
+            hits |= is && bin < kBins ? 1u << j : 0u;
+        }
+        uint32_t all;
+        uint32_t at = scan_block(wave32, (uint32_t)__builtin_popcount(hits), &all);
+        if (tid == 0 && all) shared_at = __hip_atomic_fetch_add(&state.listed, all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        at += shared_at;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if ((hits >> j & 1) && at < (uint32_t)kList)
+                put64(&state.list[at++], (uint64_t)sort_word(l[j]) << 32 | (uint32_t)~(b + j * kSampleThreads + tid));
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): written through to where all XCDs see it
+    __syncthreads();
+    if (tid == 0) last = __hip_atomic_fetch_add(&state.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.parts - 1;
+    __syncthreads();
+    if (!last) return;
+
+    const Ask k = ask_of(a, m);
+    const int n = (int)get32(&state.listed) < kList ? (int)get32(&state.listed) : kList;
+    int size = 64;
+    while (size < n) size *= 2;
+    for (int i = tid; i < size; i += kSampleThreads) key[i] = i < n ? get64(&state.list[i]) : 0;
+    __syncthreads();
+    // descending, in pairs of sorted runs
+    for (int run = 2; run <= size; run *= 2)
+        for (int d = run / 2; d; d /= 2) {
+            for (int i = tid; i < size / 2; i += kSampleThreads) {
+                const int x = i / d * 2 * d + i % d, y = x + d;
+                const bool down = (x & run) == 0;
+                const uint64_t p = key[x], q = key[y];
+                if (down ? p < q : p > q) {
+                    key[x] = q;
+                    key[y] = p;
+                }
+            }
+            __syncthreads();
+        }
+    const Weights w(state.most, k.temperature);
+    uint64_t carry = 0;
+    for (int b = 0; b < n; b += kSampleThreads) {
+        const int i = b + tid;
+        const uint64_t v = i < n ? w.of_word((uint32_t)(key[i] >> 32)) : 0;
+        unsigned long long all;
+        const uint64_t at = scan_block(wave64, (unsigned long long)v, &all);
+        if (i < n) sum[i] = carry + at;
+        carry += all;
+    }
+    if (tid == 0) sum[n] = carry;
+    if (tid < 3) found[tid] = ~0ull;
+    __syncthreads();
+    // A listed token's place in the row: the sum of the weights up to it (itself included), and before it its rank.
+    struct At {
+        uint64_t upto;
+        uint32_t rank;
+        int bin;
+    };
+    auto place = [&](int i) {
+        At p;
+        p.bin = grid.bin(of_sort_word((uint32_t)(key[i] >> 32)));
+        const uint32_t first = state.first[p.bin];
+        p.upto = state.before[p.bin] + (sum[i + 1] - sum[first]);
+        p.rank = state.ranked[p.bin] + ((uint32_t)i - first);
+        return p;
+    };
+    uint64_t kept = state.all;
+    if (k.top_k > 0 && (uint32_t)k.top_k < state.count) {
+        for (int i = tid; i < n; i += kSampleThreads) {
+            const At p = place(i);
+            if (p.rank == (uint32_t)k.top_k - 1) found[0] = p.upto;
+        }
+        __syncthreads();
+        kept = found[0] < kept ? found[0] : kept;
+    }
+    if (!(k.top_p >= 1.0f)) {
+        const uint64_t reach = reach_of(k.top_p, kept);
+        for (int i = tid; i < n; i += kSampleThreads) {
+            const At p = place(i);
+            if (p.upto >= reach) atomicMin(&found[1], (unsigned long long)p.upto);
+        }
+        __syncthreads();
+        kept = found[1] < kept ? found[1] : kept;
+    }
+    if (k.min_p > 0.0f) {
+        __syncthreads();
+        if (tid == 0) found[2] = state.before[state.cut];
+        __syncthreads();
+        for (int i = tid; i < n; i += kSampleThreads) {
+            const At p = place(i);
+            if (p.bin >= state.cut && (double)(sum[i + 1] - sum[i]) >= (double)k.min_p * kOne) atomicMax(&found[2], (unsigned long long)p.upto);
+        }
+        __syncthreads();
+        kept = found[2] < kept ? found[2] : kept;
+    }
+    kept = kept < 1ull << kPoint ? 1ull << kPoint : kept;  // (the first token's weight is 1)
+    const uint64_t x = point_of(k.u, kept);
+    if (tid == 0) last = ~0u;
+    __syncthreads();
+    for (int i = tid; i < n; i += kSampleThreads)
+        if (place(i).upto > x) atomicMin(&last, (uint32_t)i);
+    __syncthreads();
+    if (tid == 0) a.ids[m] = (int)~(uint32_t)key[last < (uint32_t)n ? last : (uint32_t)n - 1];
+}
+
+// Parts of a row: blocks of kBlock logits, as many workgroups in all as fill the device a few times over.
+int parts_of(int M, int V) {
+    const int blocks = (V + kBlock - 1) / kBlock, share = (1024 + M - 1) / M;
+    const int p = blocks < share ? blocks : share;
+    return p < kMostParts ? p : kMostParts;
+}
+// Parts that calls of up to M rows of up to V logits have in all.
+size_t most_parts(int M, int V) {
+    const size_t blocks = (size_t)((V + kBlock - 1) / kBlock), per = blocks < kMostParts ? blocks : kMostParts;
+    const size_t rows = (size_t)M * per, share = 1024 + (size_t)M;
+    return rows < share ? rows : share;
 }
 
 bool sample_shape(int M, int V) { return M >= 1 && M <= NVQ_SAMPLE_MAX_M && V >= 1 && V <= NVQ_SAMPLE_MAX_V; }
@@ -225,7 +699,8 @@ bool sample_shape(int M, int V) { return M >= 1 && M <= NVQ_SAMPLE_MAX_M && V >=
 
 extern "C" size_t nvq_sample_workspace_bytes(int M, int V) {
     using namespace nvq;
-    return sample_shape(M, V) ? NVQ_SAMPLE_CLEAR_BYTES : 0;
+    if (!sample_shape(M, V)) return 0;
+    return NVQ_SAMPLE_CLEAR_BYTES + sizeof(RowState) * (size_t)M + (sizeof(PartHead) + sizeof(PartBins)) * most_parts(M, V);
 }
 
 extern "C" int nvq_sample(const void *logits, int dtype, int64_t ld, int M, int V, const float *u, const float *temperature,
@@ -250,7 +725,18 @@ extern "C" int nvq_sample(const void *logits, int dtype, int64_t ld, int M, int 
     a.top_p = top_p;
     a.min_p = min_p;
     a.ids = ids;
-    hipLaunchKernelGGL(sample_kernel, dim3((unsigned)M), dim3(kSampleThreads), 0, (hipStream_t)stream, a);
+    a.parts = parts_of(M, V);
+    a.part = ((V + a.parts - 1) / a.parts + kBlock - 1) / kBlock * kBlock;
+    char *const ws = static_cast<char *>(workspace);
+    a.arrived = reinterpret_cast<uint32_t *>(ws);
+    a.rows = reinterpret_cast<RowState *>(ws + NVQ_SAMPLE_CLEAR_BYTES);
+    a.bins = reinterpret_cast<PartBins *>(a.rows + M);
+    a.heads = reinterpret_cast<PartHead *>(a.bins + (size_t)M * a.parts);
+    const dim3 grid((unsigned)(M * a.parts)), block(kSampleThreads);
+    const hipStream_t st = (hipStream_t)stream;
+    hipLaunchKernelGGL(sample_bins_kernel, grid, block, 0, st, a);
+    NVQ_HIP_TRY(hipGetLastError());
+    hipLaunchKernelGGL(sample_list_kernel, grid, block, 0, st, a);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
 }

@@ -92,7 +92,8 @@ def _load_calls(L):
         return None
     calls.bind(*(C.cast(f, C.c_void_p).value for f in
                  (L.nvq_gemv_w4a16, L.nvq_gemv_w4a8, L.nvq_quant_act_i8, L.nvq_gemm_w4a16, L.nvq_quant_mxfp4,
-                  L.nvq_dequant_mxfp4, L.nvq_gemv_mxfp4, L.nvq_gemm_mxfp4, L.nvq_moe_route, L.nvq_moe_experts)))
+                  L.nvq_dequant_mxfp4, L.nvq_gemv_mxfp4, L.nvq_gemm_mxfp4, L.nvq_moe_route, L.nvq_moe_experts,
+                  L.nvq_cache_append, L.nvq_cache_read, L.nvq_attention, L.nvq_sample, L.nvq_adapters_add)))
     return calls
 
 
@@ -763,6 +764,7 @@ class Cache:
             raise ValueError("tensors on different devices")
         self.k, self.v, self.scales = k, v, scales
         self.pages, self.heads, self.page_size, self.head_dim, self.device = pages, heads, size, D, k.device
+        self.index = k.device.index
         self.struct = CacheStruct(_dev(k, k.dtype, "k"), _dev(v, k.dtype, "v"),
                                   None if scales is None else _dev(scales, torch.uint8, "scales"),
                                   BF16 if scales is None else E4M3, pages, heads, size, D)
@@ -823,6 +825,13 @@ def cache_append(cache: Cache, table: torch.Tensor, positions: torch.Tensor, k: 
     the cache through table i32 [B,width]; with cos_sin f32 [angles,rot] (cosines, then sines) k and q bf16
     [T,H,head_dim] are turned by position first.  Tokens may lie apart (slices of a fused projection).  Returns the
     queries (`out`: where to, [T,H,head_dim]; may be q), None without q."""
+    if (q is None) == (out is None) and _calls is not None:
+        status = _calls.cache_append(cache.address, cache.index, table, positions, k, v, q, cos_sin, int(interleaved),
+                                     sequences, out)
+        if status is not None:  # (None: not the ordinary case)
+            if status:
+                _check(status, "nvq_cache_append")
+            return out
     where = _places(cache, table, positions, sequences)
     T, D = where[-1], cache.head_dim
     if k.shape[0] != T or v.shape[0] != T or (q is not None and q.shape[0] != T):
@@ -851,6 +860,12 @@ def cache_read(cache: Cache, table: torch.Tensor, positions: torch.Tensor, seque
                out=None):
     """The keys and values, bf16 [T,heads,head_dim] each, of the tokens named as in cache_append (`out`: the two tensors
     to write into)."""
+    if out is not None and _calls is not None:
+        status = _calls.cache_read(cache.address, cache.index, table, positions, sequences, out[0], out[1])
+        if status is not None:  # (None: not the ordinary case)
+            if status:
+                _check(status, "nvq_cache_read")
+            return out[0], out[1]
     where = _places(cache, table, positions, sequences)
     T = where[-1]
     n = T * cache.heads * cache.head_dim
@@ -867,6 +882,13 @@ def attention(cache: Cache, q: torch.Tensor, table: torch.Tensor, lengths: torch
     """One new token of each sequence, q bf16 [B,H,head_dim] (sequences may lie apart), over the first lengths i32 [B]
     tokens that table i32 [B,width] names in the cache -> [B,H,head_dim] (scale: None for head_dim ** -0.5; lse f32
     [B,H]: written if given; `workspace`: from cache.workspace, for calls one after the other)."""
+    if out is not None and workspace is not None and _calls is not None:
+        status = _calls.attention(cache.address, cache.index, q, table, lengths,
+                                  cache.head_dim ** -0.5 if scale is None else float(scale), window, float(softcap), out, lse, workspace)
+        if status is not None:  # (None: not the ordinary case)
+            if status:
+                _check(status, "nvq_attention")
+            return out
     if cache.device.index != torch.cuda.current_device():
         raise ValueError("the cache is on %s, the current device is %d" % (cache.device, torch.cuda.current_device()))
     B, H, D = q.shape
@@ -898,6 +920,12 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Te
     """The next token i32 [M] of logits f32 or bf16 [M,V] (rows may lie apart) from random numbers u f32 [M]; per row
     temperature f32, top_k i32, top_p f32, min_p f32 [M], or None (`workspace`: from sample_workspace, for calls one
     after the other)."""
+    if out is not None and workspace is not None and _calls is not None:
+        status = _calls.sample(logits, u, temperature, top_k, top_p, min_p, out, workspace)
+        if status is not None:  # (None: not the ordinary case)
+            if status:
+                _check(status, "nvq_sample")
+            return out
     if not logits.is_cuda or logits.dim() != 2 or (logits.shape[1] > 1 and logits.stride(1) != 1):
         raise ValueError("logits must be a device tensor [M,V], a row's values side by side")
     if logits.get_device() != torch.cuda.current_device():
@@ -926,7 +954,7 @@ class Adapters:
         if any(t is not None and t.device != a.device for t in self.keep):
             raise ValueError("tensors on different devices")
         self.n, self.R, self.K = a.shape
-        self.N, self.device = b.shape[1], a.device
+        self.N, self.device, self.index = b.shape[1], a.device, a.device.index
         self.struct = AdaptersStruct(_dev(a, torch.bfloat16, "a"), _dev(b, torch.bfloat16, "b"),
                                      None if scales is None else _dev(scales, torch.float32, "scales"),
                                      self.n, self.K, self.N, self.R)
@@ -944,6 +972,12 @@ def adapters_add(adapters: Adapters, x: torch.Tensor, ids: torch.Tensor, y: torc
                  out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """y f32 or bf16 [M,N] plus what the adapter ids i32 [M] (outside [0,n): none) of each token makes of x bf16 [M,K]
     (`out`: where to, may be y; `workspace`: from adapters.workspace, for calls one after the other)."""
+    if out is not None and workspace is not None and _calls is not None:
+        status = _calls.adapters_add(adapters.address, adapters.index, x, ids, y, out, workspace)
+        if status is not None:  # (None: not the ordinary case)
+            if status:
+                _check(status, "nvq_adapters_add")
+            return out
     if adapters.device.index != torch.cuda.current_device():
         raise ValueError("the adapters are on %s, the current device is %d" % (adapters.device, torch.cuda.current_device()))
     M = x.shape[0]
