@@ -1,17 +1,19 @@
 // nvq_adapters_add: low-rank adapters beside a layer, each token its own.
 //
-// Two launches, h = A x and y + scale * B h, both on the matrix cores in tiles of sixteen tokens.  A tile goes through
-// the distinct adapters of its tokens one after the other and keeps of each product the rows of that adapter's own
-// tokens: an adapter's weights are read once per tile however many of its tokens use it, and sixteen tokens with
-// sixteen adapters read what they have to.  h stays fp32 between the launches; it enters the second product as three
-// bf16 values whose sum it is, so nothing of it is lost.
+// Two launches, h = A x and y + scale * B h, both on the matrix cores in tiles of sixteen tokens.  A tile goes by the
+// distinct adapters of its tokens, a workgroup to one of them (or to several in turn, of long batches), and keeps of a
+// product the tokens of that adapter: an adapter's weights are read once per tile however many of its tokens use it,
+// and sixteen tokens with sixteen adapters read what they have to.  h stays fp32 between the launches, in as many
+// partial sums as K is cut into; it enters the second product as three bf16 values whose sum it is, so nothing of it
+// is lost.
 #include "mfma_act.h"
 
 namespace nvq {
 
 namespace {
 
-constexpr int kTile = 16, kDownWaves = 4, kUpWaves = 4;
+constexpr int kTile = 16, kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kMostSlices = 16;
 
 struct AdaptersArgs {
     const uint16_t *a, *b, *x;
@@ -21,7 +23,10 @@ struct AdaptersArgs {
     void *out;
     int dtype;
     int n, K, N, R, M;
-    float *h;  // workspace, [M][R]
+    float *h;             // workspace, [slices][M][R]
+    int slices, columns;  // of K, 32 inputs each
+    int shares;           // workgroups that share a tile's adapters
+    int blocks;           // of ranks (first launch), of outputs (second)
 };
 
 // The adapter of a lane's token (lane & 15 of a tile), -1: none.
@@ -40,37 +45,70 @@ __device__ __forceinline__ uint32_t turn(int mine, uint32_t *left, int *e) {
     return with;
 }
 
-// h[m0 ..][r0 ..]: K split over the waves.
-__global__ __launch_bounds__(64 * kDownWaves) void adapters_down_kernel(AdaptersArgs g) {
-    __shared__ float red[kDownWaves][4][64];
+// h of a tile's tokens: RT tiles of sixteen ranks, a slice of K, its columns in turn over the waves.
+template <int RT>
+__global__ __launch_bounds__(kThreads) void adapters_down_kernel(AdaptersArgs g) {
+    __shared__ float red[kWaves][RT * 4][64];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4;
-    const int m0 = blockIdx.y * kTile, r0 = blockIdx.x * 16;
+    int i = blockIdx.x;
+    const int slice = i % g.slices;
+    i /= g.slices;
+    const int r0 = i % g.blocks * 16 * RT;
+    i /= g.blocks;
+    const int share = i % g.shares, m0 = i / g.shares * kTile;
+    const int c0 = slice * g.columns, c1 = c0 + g.columns < g.K / 32 ? c0 + g.columns : g.K / 32;
     const int mine = adapter_of(g, m0);
     uint32_t left = (uint32_t)__ballot(mine >= 0) & 0xffffu;
     const uint16_t *const x = g.x + (int64_t)(m0 + n < g.M ? m0 + n : m0) * g.K + 8 * kb;
-    const int r = r0 + n < g.R ? r0 + n : g.R - 1;
-    while (left) {
+    for (int at = 0; left; ++at) {
         int e;
         const uint32_t with = turn(mine, &left, &e);
-        const uint16_t *const a = g.a + ((int64_t)e * g.R + r) * g.K + 8 * kb;
-        float4v sum = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int c = w; c < g.K / 32; c += kDownWaves)
-            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, *as_global<uint4v>(x + 32 * c)),
-                                                         __builtin_bit_cast(bf16x8, *as_global<uint4v>(a + 32 * c)), sum, 0, 0, 0);
-        wait_written(sum);
-        __syncthreads();
+        if (at % g.shares != share) continue;
+        const uint16_t *a[RT];
+        float4v sum[RT];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) red[w][j][lane] = sum[j];
-        __syncthreads();
-        if (w == 0) {
+        for (int t = 0; t < RT; ++t) {
+            const int r = r0 + 16 * t + n < g.R ? r0 + 16 * t + n : g.R - 1;
+            a[t] = g.a + ((int64_t)e * g.R + r) * g.K + 8 * kb;
+            sum[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        constexpr int kAtOnce = RT == 4 ? 2 : 4;  // columns whose loads are in flight together
+        for (int c = c0 + w; c < c1; c += kAtOnce * kWaves) {
+            uint4v xv[kAtOnce], av[kAtOnce][RT];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int row = 4 * kb + j;
-                float v = red[0][j][lane];
+            for (int k = 0; k < kAtOnce; ++k) {
+                const int cc = c + k * kWaves < c1 ? c + k * kWaves : c;
+                xv[k] = *as_global<uint4v>(x + 32 * cc);
 #pragma unroll
-                for (int k = 1; k < kDownWaves; ++k) v += red[k][j][lane];
-                if ((with >> row & 1) && r0 + n < g.R) g.h[(int64_t)(m0 + row) * g.R + r0 + n] = v;
+                for (int t = 0; t < RT; ++t) av[k][t] = *as_global<uint4v>(a[t] + 32 * cc);
             }
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) {
+                const bool in = c + k * kWaves < c1;
+                if (!in) xv[k] = uint4v{0, 0, 0, 0};
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    if (!in) av[k][t] = uint4v{0, 0, 0, 0};
+                    sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xv[k]), __builtin_bit_cast(bf16x8, av[k][t]),
+                                                                    sum[t], 0, 0, 0);
+                }
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < RT; ++t) wait_written(sum[t]);
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < RT; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) red[w][4 * t + j][lane] = sum[t][j];
+        __syncthreads();
+        for (int o = threadIdx.x; o < RT * 256; o += kThreads) {
+            const int reg = o >> 6, l = o & 63;
+            const int row = 4 * (l >> 4) + (reg & 3), r = r0 + 16 * (reg >> 2) + (l & 15);
+            float v = red[0][reg][l];
+#pragma unroll
+            for (int k = 1; k < kWaves; ++k) v += red[k][reg][l];
+            if ((with >> row & 1) && r < g.R) g.h[((int64_t)slice * g.M + m0 + row) * g.R + r] = v;
         }
     }
 }
@@ -85,69 +123,179 @@ __device__ __forceinline__ void split(float v, uint32_t *hi, uint32_t *mid, uint
     *lo = __float_as_uint(rest - __uint_as_float(c)) >> 16;
 }
 
-// out[m0 ..][n0 ..], a wave per sixteen outputs.
-__global__ __launch_bounds__(64 * kUpWaves) void adapters_up_kernel(AdaptersArgs g) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4;
-    const int m0 = blockIdx.y * kTile, n0 = (blockIdx.x * kUpWaves + w) * 16;
-    const int mine = adapter_of(g, m0);
-    uint32_t left = (uint32_t)__ballot(mine >= 0) & 0xffffu;
-    const int o = n0 + n < g.N ? n0 + n : g.N - 1;
-    const float *const h = g.h + (int64_t)(m0 + n < g.M ? m0 + n : m0) * g.R + 8 * kb;
-    float add[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    while (left) {
-        int e;
-        const uint32_t with = turn(mine, &left, &e);
-        const uint16_t *const b = g.b + ((int64_t)e * g.N + o) * g.R + 8 * kb;
-        float4v sum = {0.0f, 0.0f, 0.0f, 0.0f};
-        for (int c = 0; c < g.R; c += 32) {
-            uint4v hw[3] = {}, bw = {};
-            if (c + 8 * kb < g.R) {
-                bw = *as_global<uint4v>(b + c);
-                if (with >> n & 1) {  // (what h holds of other tokens may be anything)
+// Results side by side as one access, at the alignment of a single one.
+typedef uint4v uint4_apart __attribute__((aligned(2)));
+typedef uint2v uint2_apart __attribute__((aligned(2)));
+template <int COUNT>  // 4 or 16
+__device__ __forceinline__ void load_results(const void *p, int dtype, int64_t at, float (&v)[COUNT]) {
+    if (dtype == NVQ_F32) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        uint32_t lo[3], hi[3];
-                        split(h[c + 2 * j], &lo[0], &lo[1], &lo[2]);
-                        split(h[c + 2 * j + 1], &hi[0], &hi[1], &hi[2]);
+        for (int i = 0; i < COUNT; i += 4) {
+            const uint4v w = *reinterpret_cast<const uint4_apart *>(static_cast<const float *>(p) + at + i);
 #pragma unroll
-                        for (int k = 0; k < 3; ++k) hw[k][j] = lo[k] | hi[k] << 16;
-                    }
-                }
-            }
-#pragma unroll
-            for (int k = 0; k < 3; ++k)
-                sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, hw[k]), __builtin_bit_cast(bf16x8, bw), sum,
-                                                             0, 0, 0);
+            for (int j = 0; j < 4; ++j) v[i + j] = __uint_as_float(w[j]);
         }
-        wait_written(sum);
-        const float scale = g.scales ? g.scales[e] : 1.0f;
+    } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (with >> (4 * kb + j) & 1) add[j] = sum[j] * scale;
+        for (int i = 0; i < COUNT; i += 4) {
+            const uint2v w = *reinterpret_cast<const uint2_apart *>(static_cast<const uint16_t *>(p) + at + i);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i + j] = __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+        }
     }
-    const uint32_t has = (uint32_t)__ballot(mine >= 0) & 0xffffu;
-    if (n0 + n >= g.N) return;
+}
+template <int COUNT>
+__device__ __forceinline__ void store_results(void *p, int dtype, int64_t at, const float (&v)[COUNT]) {
+    if (dtype == NVQ_F32) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int m = m0 + 4 * kb + j;
-        if (m >= g.M) continue;
-        const int64_t at = (int64_t)m * g.N + n0 + n;
-        if (has >> (4 * kb + j) & 1) {
-            const float y = g.dtype == NVQ_F32 ? static_cast<const float *>(g.y)[at]
-                                               : bf16_bits_to_float(static_cast<const uint16_t *>(g.y)[at]);
-            store_global(g.out, g.dtype, at, y + add[j]);
-        } else if (g.out != g.y) {  // (as it is)
-            if (g.dtype == NVQ_F32)
-                static_cast<uint32_t *>(g.out)[at] = static_cast<const uint32_t *>(g.y)[at];
-            else
-                static_cast<uint16_t *>(g.out)[at] = static_cast<const uint16_t *>(g.y)[at];
+        for (int i = 0; i < COUNT; i += 4) {
+            const uint4v w = {__float_as_uint(v[i]), __float_as_uint(v[i + 1]), __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3])};
+            *reinterpret_cast<uint4_apart *>(static_cast<float *>(p) + at + i) = w;
+        }
+    } else if constexpr (COUNT == 4) {
+        const uint2v w = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+        *reinterpret_cast<uint2_apart *>(static_cast<uint16_t *>(p) + at) = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < COUNT; i += 8) {
+            const uint4v w = {pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]), pack_bf16x2(v[i + 4], v[i + 5]),
+                              pack_bf16x2(v[i + 6], v[i + 7])};
+            *reinterpret_cast<uint4_apart *>(static_cast<uint16_t *>(p) + at + i) = w;
         }
     }
 }
 
+// Results of a tile's tokens, NT tiles of sixteen outputs per wave, outputs the rows of a product and tokens its
+// columns.  Row 4 q + j of tile t is output 4 NT q + 4 t + j, so that a lane has 4 NT outputs side by side.
+template <int NT>
+__global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
+    constexpr int kPitch = NVQ_MAX_RANK + 8;  // (16 bytes more than a row, against bank conflicts)
+    __shared__ __align__(16) uint16_t hs[3][kTile][kPitch];
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4;
+    const int n0 = ((int)(blockIdx.x % g.blocks) * kWaves + w) * 16 * NT;  // (past the last output: nothing is stored)
+    const int i = blockIdx.x / g.blocks;
+    const int share = i % g.shares, m0 = i / g.shares * kTile, m = m0 + n;
+    const int mine = adapter_of(g, m0);
+    uint32_t left = (uint32_t)__ballot(mine >= 0) & 0xffffu;
+    const int o0 = n0 + 4 * NT * kb;  // the lane's outputs
+    const int64_t at_y = (int64_t)m * g.N + o0;
+    const int64_t h_slice = (int64_t)g.M * g.R;
+    const bool whole = o0 + 4 * NT <= g.N;
+    if (share == 0 && g.out != g.y && m < g.M && mine < 0) {  // no adapter: as it is
+        for (int j = 0; j < 4 * NT && o0 + j < g.N; ++j) {
+            if (g.dtype == NVQ_F32)
+                static_cast<uint32_t *>(g.out)[at_y + j] = static_cast<const uint32_t *>(g.y)[at_y + j];
+            else
+                static_cast<uint16_t *>(g.out)[at_y + j] = static_cast<const uint16_t *>(g.y)[at_y + j];
+        }
+    }
+    for (int at = 0; left; ++at) {
+        int e;
+        const uint32_t with = turn(mine, &left, &e);
+        if (at % g.shares != share) continue;
+        const bool my = with >> n & 1;
+        const uint16_t *b[NT];
+        float4v sum[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int o = n0 + 4 * NT * (n >> 2) + 4 * t + (n & 3);
+            b[t] = g.b + ((int64_t)e * g.N + (o < g.N ? o : g.N - 1)) * g.R + 8 * kb;
+            sum[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        // The weights of two columns of 32 ranks at a time, those of the first two and y asked for before h is there.
+        uint4v bw[2][NT];
+        auto load = [&](int c) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    bw[k][t] = uint4v{0, 0, 0, 0};
+                    if (c + 32 * k + 8 * kb < g.R) bw[k][t] = *as_global<uint4v>(b[t] + c + 32 * k);
+                }
+        };
+        load(0);
+        float y[4 * NT];
+        if (my && whole) load_results<4 * NT>(g.y, g.dtype, at_y, y);
+        __syncthreads();
+        for (int u = threadIdx.x; u < kTile * g.R; u += kThreads) {
+            const int token = u / g.R, r = u - token * g.R;
+            float v = 0.0f;
+            if (with >> token & 1) {  // (what the workspace holds of other tokens may be anything)
+                const float *const h = g.h + (int64_t)(m0 + token) * g.R + r;
+                for (int s0 = 0; s0 < g.slices; s0 += 8) {
+                    float part[8];
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) part[s] = h[(s0 + s < g.slices ? s0 + s : 0) * h_slice];
+#pragma unroll
+                    for (int s = 0; s < 8; ++s) v += s0 + s < g.slices ? part[s] : 0.0f;
+                }
+            }
+            uint32_t hi, mid, lo;
+            split(v, &hi, &mid, &lo);
+            hs[0][token][r] = (uint16_t)hi;
+            hs[1][token][r] = (uint16_t)mid;
+            hs[2][token][r] = (uint16_t)lo;
+        }
+        __syncthreads();
+        for (int c = 0; c < g.R; c += 64) {
+            if (c > 0) load(c);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const int r = c + 32 * k + 8 * kb;
+#pragma unroll
+                for (int q = 0; q < 3; ++q) {
+                    uint4v hw = {0, 0, 0, 0};
+                    if (r < g.R) hw = *reinterpret_cast<const uint4v *>(&hs[q][n][r]);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+                        sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bw[k][t]), __builtin_bit_cast(bf16x8, hw),
+                                                                        sum[t], 0, 0, 0);
+                }
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) wait_written(sum[t]);
+        if (!my) continue;
+        const float scale = g.scales ? g.scales[e] : 1.0f;
+        if (whole) {
+#pragma unroll
+            for (int j = 0; j < 4 * NT; ++j) y[j] += sum[j >> 2][j & 3] * scale;
+            store_results<4 * NT>(g.out, g.dtype, at_y, y);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4 * NT; ++j)
+                if (o0 + j < g.N) {
+                    const float v = g.dtype == NVQ_F32 ? static_cast<const float *>(g.y)[at_y + j]
+                                                       : bf16_bits_to_float(static_cast<const uint16_t *>(g.y)[at_y + j]);
+                    store_global(g.out, g.dtype, at_y + j, v + sum[j >> 2][j & 3] * scale);
+                }
+        }
+    }
+}
+
+// Tiles of a batch, and workgroups that share a tile's adapters: one each where there are few tiles.
+int tiles_of(int M) { return (M + kTile - 1) / kTile; }
+int shares_of(int M, int n) {
+    const int most = n < kTile ? n : kTile;
+    return tiles_of(M) <= 4 ? (M < most ? M : most) : 1;
+}
+// Blocks of 64, 32 or 16 ranks.
+int rank_tiles(int R) { return R > 32 ? 4 : R > 16 ? 2 : 1; }
+int rank_blocks(int R) { return (R + 16 * rank_tiles(R) - 1) / (16 * rank_tiles(R)); }
+// Slices of K: as many as bring a thousand workgroups, of four columns (one per wave) or more.
+int slices_of(const nvq_adapters &s, int M) {
+    const int64_t others = (int64_t)tiles_of(M) * shares_of(M, s.n) * rank_blocks(s.R);
+    int64_t want = 1024 / others;
+    const int64_t most = (s.K / 32 + kWaves - 1) / kWaves;
+    want = want < most ? want : most;
+    want = want < kMostSlices ? want : kMostSlices;
+    return want > 1 ? (int)want : 1;
+}
+
 bool adapters_shape(const nvq_adapters *s, int M) {
     return s && s->n >= 1 && s->n <= 1 << 16 && s->K >= 32 && s->K % 32 == 0 && s->K <= NVQ_MAX_K && s->N >= 1 && s->N <= 1 << 24 &&
-           s->R >= 8 && s->R % 8 == 0 && s->R <= NVQ_MAX_RANK && M >= 1 && M <= 1 << 16;
+           s->R >= 8 && s->R % 8 == 0 && s->R <= NVQ_MAX_RANK && M >= 1 && M <= 1 << 16 &&
+           (int64_t)M * s->N <= 1ll << 35;  // (the launches stay below 2^32 threads)
 }
 
 }  // namespace
@@ -156,7 +304,10 @@ bool adapters_shape(const nvq_adapters *s, int M) {
 
 extern "C" size_t nvq_adapters_workspace_bytes(const nvq_adapters *adapters, int M) {
     using namespace nvq;
-    return adapters_shape(adapters, M) ? (size_t)M * adapters->R * sizeof(float) : 0;
+    if (!adapters_shape(adapters, M)) return 0;
+    // (fewer tokens may take more slices: of no more than kMostSlices tiles in all, or of all M in one)
+    const size_t rows = (size_t)M < 1024 ? (size_t)M * kMostSlices : (size_t)M + 1024 * kMostSlices;
+    return rows * adapters->R * sizeof(float);
 }
 
 extern "C" int nvq_adapters_add(const nvq_adapters *adapters, const uint16_t *x_bf16, const int32_t *ids, int M, const void *y,
@@ -185,12 +336,29 @@ extern "C" int nvq_adapters_add(const nvq_adapters *adapters, const uint16_t *x_
     g.R = adapters->R;
     g.M = M;
     g.h = static_cast<float *>(workspace);
+    g.slices = slices_of(*adapters, M);
+    g.columns = (g.K / 32 + g.slices - 1) / g.slices;
+    g.slices = (g.K / 32 + g.columns - 1) / g.columns;
+    g.shares = shares_of(M, g.n);
+    g.blocks = rank_blocks(g.R);
     const hipStream_t st = (hipStream_t)stream;
-    const unsigned tiles = (unsigned)((M + kTile - 1) / kTile);
-    hipLaunchKernelGGL(adapters_down_kernel, dim3((unsigned)((g.R + 15) / 16), tiles), dim3(64 * kDownWaves), 0, st, g);
+    const int64_t groups = (int64_t)tiles_of(M) * g.shares;
+    const dim3 block(kThreads), down((unsigned)(groups * g.blocks * g.slices));
+    if (rank_tiles(g.R) == 1)
+        hipLaunchKernelGGL(adapters_down_kernel<1>, down, block, 0, st, g);
+    else if (rank_tiles(g.R) == 2)
+        hipLaunchKernelGGL(adapters_down_kernel<2>, down, block, 0, st, g);
+    else
+        hipLaunchKernelGGL(adapters_down_kernel<4>, down, block, 0, st, g);
     NVQ_HIP_TRY(hipGetLastError());
-    hipLaunchKernelGGL(adapters_up_kernel, dim3((unsigned)((g.N + 16 * kUpWaves - 1) / (16 * kUpWaves)), tiles), dim3(64 * kUpWaves), 0, st,
-                       g);
+    const bool wide = groups * g.N >= 1024 * 64;  // a wave to 64 outputs where that leaves four a compute unit
+    const int per = (wide ? 64 : 16) * kWaves;
+    g.blocks = (g.N + per - 1) / per;
+    const dim3 up((unsigned)(groups * g.blocks));
+    if (wide)
+        hipLaunchKernelGGL(adapters_up_kernel<4>, up, block, 0, st, g);
+    else
+        hipLaunchKernelGGL(adapters_up_kernel<1>, up, block, 0, st, g);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
 }
