@@ -1,18 +1,17 @@
 // nvq_adapters_add: low-rank adapters beside a layer, each token its own.
 //
-// Two launches, h = A x and y + scale * B h, both on the matrix cores in tiles of sixteen tokens.  A tile goes by the
-// distinct adapters of its tokens, a workgroup to one of them (or to several in turn, of long batches), and keeps of a
-// product the tokens of that adapter: an adapter's weights are read once per tile however many of its tokens use it,
-// and sixteen tokens with sixteen adapters read what they have to.  h stays fp32 between the launches, in as many
-// partial sums as K is cut into; it enters the second product as three bf16 values whose sum it is, so nothing of it
-// is lost.
+// Two launches, h = A x and y + scale * B h, both on the matrix cores.  Tokens go in groups of 64, a group by the
+// distinct adapters of its tokens, and the tokens of one adapter, wherever they stand in the group, are sixteen to a
+// product: an adapter's weights are read once per group however its tokens lie, and 64 tokens of 64 adapters read what
+// they have to.  h stays fp32 between the launches, in as many partial sums as K is cut into; it enters the second
+// product as three bf16 values whose sum it is, so nothing of it is lost.
 #include "mfma_act.h"
 
 namespace nvq {
 
 namespace {
 
-constexpr int kTile = 16, kWaves = 4, kThreads = 64 * kWaves;
+constexpr int kGroup = 64, kTile = 16, kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kMostSlices = 16;
 
 struct AdaptersArgs {
@@ -25,27 +24,40 @@ struct AdaptersArgs {
     int n, K, N, R, M;
     float *h;             // workspace, [slices][M][R]
     int slices, columns;  // of K, 32 inputs each
-    int shares;           // workgroups that share a tile's adapters
+    int shares, tiles;    // workgroups that share a group's adapters, and the tiles of tokens of each
     int blocks;           // of ranks (first launch), of outputs (second)
 };
 
-// The adapter of a lane's token (lane & 15 of a tile), -1: none.
+// The adapter of a lane's token, -1: none.
 __device__ __forceinline__ int adapter_of(const AdaptersArgs &g, int m0) {
-    const int m = m0 + (threadIdx.x & 15);
+    const int m = m0 + (threadIdx.x & 63);
     const int e = m < g.M ? g.ids[m] : -1;
     return (unsigned)e < (unsigned)g.n ? e : -1;
 }
 
-// The distinct adapters of a tile one after the other: `left` has a bit per token that has not had its turn.
-__device__ __forceinline__ uint32_t turn(int mine, uint32_t *left, int *e) {
-    const int first = __builtin_ctz(*left);
-    *e = __builtin_amdgcn_readlane(mine, first);
-    const uint32_t with = (uint32_t)__ballot(mine == *e) & 0xffffu;
+// The distinct adapters of a group one after the other: `left` has a bit per token that has not had its turn.
+__device__ __forceinline__ uint64_t turn(int mine, uint64_t *left, int *e) {
+    *e = __builtin_amdgcn_readlane(mine, __builtin_ctzll(*left));
+    const uint64_t with = __ballot(mine == *e);
     *left &= ~with;
     return with;
 }
 
-// h of a tile's tokens: RT tiles of sixteen ranks, a slice of K, its columns in turn over the waves.
+// The place of the k-th bit that is set (k from 0, below their number).
+__device__ __forceinline__ int nth_bit(uint64_t bits, int k) {
+    int at = 0;
+#pragma unroll
+    for (int step = 32; step; step >>= 1) {
+        const int c = __builtin_popcountll(bits >> at & ((1ull << step) - 1));
+        if (k >= c) {
+            k -= c;
+            at += step;
+        }
+    }
+    return at;
+}
+
+// h of a group's tokens: RT tiles of sixteen ranks, a slice of K, its columns in turn over the waves.
 template <int RT>
 __global__ __launch_bounds__(kThreads) void adapters_down_kernel(AdaptersArgs g) {
     __shared__ float red[kWaves][RT * 4][64];
@@ -55,60 +67,67 @@ __global__ __launch_bounds__(kThreads) void adapters_down_kernel(AdaptersArgs g)
     i /= g.slices;
     const int r0 = i % g.blocks * 16 * RT;
     i /= g.blocks;
-    const int share = i % g.shares, m0 = i / g.shares * kTile;
+    const int tile = i % g.tiles;
+    i /= g.tiles;
+    const int share = i % g.shares, m0 = i / g.shares * kGroup;
     const int c0 = slice * g.columns, c1 = c0 + g.columns < g.K / 32 ? c0 + g.columns : g.K / 32;
     const int mine = adapter_of(g, m0);
-    uint32_t left = (uint32_t)__ballot(mine >= 0) & 0xffffu;
-    const uint16_t *const x = g.x + (int64_t)(m0 + n < g.M ? m0 + n : m0) * g.K + 8 * kb;
+    uint64_t left = __ballot(mine >= 0);
     for (int at = 0; left; ++at) {
         int e;
-        const uint32_t with = turn(mine, &left, &e);
+        const uint64_t with = turn(mine, &left, &e);
         if (at % g.shares != share) continue;
+        const int tokens = __builtin_popcountll(with);
         const uint16_t *a[RT];
-        float4v sum[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             const int r = r0 + 16 * t + n < g.R ? r0 + 16 * t + n : g.R - 1;
             a[t] = g.a + ((int64_t)e * g.R + r) * g.K + 8 * kb;
-            sum[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
         }
-        constexpr int kAtOnce = RT == 4 ? 2 : 4;  // columns whose loads are in flight together
-        for (int c = c0 + w; c < c1; c += kAtOnce * kWaves) {
-            uint4v xv[kAtOnce], av[kAtOnce][RT];
+        for (int k0 = tile * kTile; k0 < tokens; k0 += kTile * g.tiles) {
+            const int m = m0 + nth_bit(with, k0 + n < tokens ? k0 + n : k0);
+            const uint16_t *const x = g.x + (int64_t)m * g.K + 8 * kb;
+            float4v sum[RT];
 #pragma unroll
-            for (int k = 0; k < kAtOnce; ++k) {
-                const int cc = c + k * kWaves < c1 ? c + k * kWaves : c;
-                xv[k] = *as_global<uint4v>(x + 32 * cc);
+            for (int t = 0; t < RT; ++t) sum[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+            constexpr int kAtOnce = RT == 4 ? 2 : 4;  // columns whose loads are in flight together
+            for (int c = c0 + w; c < c1; c += kAtOnce * kWaves) {
+                uint4v xv[kAtOnce], av[kAtOnce][RT];
 #pragma unroll
-                for (int t = 0; t < RT; ++t) av[k][t] = *as_global<uint4v>(a[t] + 32 * cc);
-            }
+                for (int k = 0; k < kAtOnce; ++k) {
+                    const int cc = c + k * kWaves < c1 ? c + k * kWaves : c;
+                    xv[k] = *as_global<uint4v>(x + 32 * cc);
 #pragma unroll
-            for (int k = 0; k < kAtOnce; ++k) {
-                const bool in = c + k * kWaves < c1;
-                if (!in) xv[k] = uint4v{0, 0, 0, 0};
+                    for (int t = 0; t < RT; ++t) av[k][t] = *as_global<uint4v>(a[t] + 32 * cc);
+                }
 #pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    if (!in) av[k][t] = uint4v{0, 0, 0, 0};
-                    sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xv[k]), __builtin_bit_cast(bf16x8, av[k][t]),
-                                                                    sum[t], 0, 0, 0);
+                for (int k = 0; k < kAtOnce; ++k) {
+                    const bool in = c + k * kWaves < c1;
+                    if (!in) xv[k] = uint4v{0, 0, 0, 0};
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) {
+                        if (!in) av[k][t] = uint4v{0, 0, 0, 0};
+                        sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xv[k]),
+                                                                        __builtin_bit_cast(bf16x8, av[k][t]), sum[t], 0, 0, 0);
+                    }
                 }
             }
-        }
 #pragma unroll
-        for (int t = 0; t < RT; ++t) wait_written(sum[t]);
-        __syncthreads();
+            for (int t = 0; t < RT; ++t) wait_written(sum[t]);
+            __syncthreads();
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
+            for (int t = 0; t < RT; ++t)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) red[w][4 * t + j][lane] = sum[t][j];
-        __syncthreads();
-        for (int o = threadIdx.x; o < RT * 256; o += kThreads) {
-            const int reg = o >> 6, l = o & 63;
-            const int row = 4 * (l >> 4) + (reg & 3), r = r0 + 16 * (reg >> 2) + (l & 15);
-            float v = red[0][reg][l];
+                for (int j = 0; j < 4; ++j) red[w][4 * t + j][lane] = sum[t][j];
+            __syncthreads();
+            for (int o = threadIdx.x; o < RT * 256; o += kThreads) {
+                const int reg = o >> 6, l = o & 63;
+                const int k = k0 + 4 * (l >> 4) + (reg & 3), r = r0 + 16 * (reg >> 2) + (l & 15);
+                float v = red[0][reg][l];
 #pragma unroll
-            for (int k = 1; k < kWaves; ++k) v += red[k][reg][l];
-            if ((with >> row & 1) && r < g.R) g.h[((int64_t)slice * g.M + m0 + row) * g.R + r] = v;
+                for (int q = 1; q < kWaves; ++q) v += red[q][reg][l];
+                if (k < tokens && r < g.R) g.h[((int64_t)slice * g.M + m0 + nth_bit(with, k)) * g.R + r] = v;
+            }
         }
     }
 }
@@ -165,42 +184,49 @@ __device__ __forceinline__ void store_results(void *p, int dtype, int64_t at, co
     }
 }
 
-// Results of a tile's tokens, NT tiles of sixteen outputs per wave, outputs the rows of a product and tokens its
+// Results of a group's tokens, NT tiles of sixteen outputs per wave, outputs the rows of a product and tokens its
 // columns.  Row 4 q + j of tile t is output 4 NT q + 4 t + j, so that a lane has 4 NT outputs side by side.
 template <int NT>
 __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
     constexpr int kPitch = NVQ_MAX_RANK + 8;  // (16 bytes more than a row, against bank conflicts)
     __shared__ __align__(16) uint16_t hs[3][kTile][kPitch];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4;
-    const int n0 = ((int)(blockIdx.x % g.blocks) * kWaves + w) * 16 * NT;  // (past the last output: nothing is stored)
-    const int i = blockIdx.x / g.blocks;
-    const int share = i % g.shares, m0 = i / g.shares * kTile, m = m0 + n;
+    const int block0 = (int)(blockIdx.x % g.blocks) * kWaves * 16 * NT;
+    const int n0 = block0 + w * 16 * NT;  // (past the last output: nothing is stored)
+    int i = blockIdx.x / g.blocks;
+    const int tile = i % g.tiles;
+    i /= g.tiles;
+    const int share = i % g.shares, m0 = i / g.shares * kGroup;
     const int mine = adapter_of(g, m0);
-    uint32_t left = (uint32_t)__ballot(mine >= 0) & 0xffffu;
+    uint64_t left = __ballot(mine >= 0);
     const int o0 = n0 + 4 * NT * kb;  // the lane's outputs
-    const int64_t at_y = (int64_t)m * g.N + o0;
     const int64_t h_slice = (int64_t)g.M * g.R;
     const bool whole = o0 + 4 * NT <= g.N;
-    if (share == 0 && g.out != g.y && m < g.M && mine < 0) {  // no adapter: as it is
-        for (int j = 0; j < 4 * NT && o0 + j < g.N; ++j) {
-            if (g.dtype == NVQ_F32)
-                static_cast<uint32_t *>(g.out)[at_y + j] = static_cast<const uint32_t *>(g.y)[at_y + j];
-            else
-                static_cast<uint16_t *>(g.out)[at_y + j] = static_cast<const uint16_t *>(g.y)[at_y + j];
+    if (share == 0 && g.out != g.y) {  // tokens without an adapter: as they are
+        uint64_t none = ~left;
+        if (g.M - m0 < kGroup) none &= (1ull << (g.M - m0)) - 1;
+        for (int k = 0; none; ++k, none &= none - 1) {
+            if (k % g.tiles != tile) continue;
+            const int64_t row = (int64_t)(m0 + __builtin_ctzll(none)) * g.N;
+            for (int o = block0 + (int)threadIdx.x; o < block0 + kWaves * 16 * NT && o < g.N; o += kThreads) {
+                if (g.dtype == NVQ_F32)
+                    static_cast<uint32_t *>(g.out)[row + o] = static_cast<const uint32_t *>(g.y)[row + o];
+                else
+                    static_cast<uint16_t *>(g.out)[row + o] = static_cast<const uint16_t *>(g.y)[row + o];
+            }
         }
     }
     for (int at = 0; left; ++at) {
         int e;
-        const uint32_t with = turn(mine, &left, &e);
+        const uint64_t with = turn(mine, &left, &e);
         if (at % g.shares != share) continue;
-        const bool my = with >> n & 1;
+        const int tokens = __builtin_popcountll(with);
+        if (tile * kTile >= tokens) continue;
         const uint16_t *b[NT];
-        float4v sum[NT];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const int o = n0 + 4 * NT * (n >> 2) + 4 * t + (n & 3);
             b[t] = g.b + ((int64_t)e * g.N + (o < g.N ? o : g.N - 1)) * g.R + 8 * kb;
-            sum[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
         }
         // The weights of two columns of 32 ranks at a time, those of the first two and y asked for before h is there.
         uint4v bw[2][NT];
@@ -214,14 +240,21 @@ __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
                 }
         };
         load(0);
-        float y[4 * NT];
-        if (my && whole) load_results<4 * NT>(g.y, g.dtype, at_y, y);
-        __syncthreads();
-        for (int u = threadIdx.x; u < kTile * g.R; u += kThreads) {
-            const int token = u / g.R, r = u - token * g.R;
-            float v = 0.0f;
-            if (with >> token & 1) {  // (what the workspace holds of other tokens may be anything)
-                const float *const h = g.h + (int64_t)(m0 + token) * g.R + r;
+        const float scale = g.scales ? g.scales[e] : 1.0f;
+        for (int k0 = tile * kTile; k0 < tokens; k0 += kTile * g.tiles) {
+            const bool my = k0 + n < tokens;
+            const int64_t at_y = (int64_t)(m0 + nth_bit(with, my ? k0 + n : k0)) * g.N + o0;
+            float y[4 * NT];
+            float4v sum[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) sum[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+            if (my && whole) load_results<4 * NT>(g.y, g.dtype, at_y, y);
+            __syncthreads();
+            for (int u = threadIdx.x; u < kTile * g.R; u += kThreads) {
+                const int k = u / g.R, r = u - k * g.R;
+                if (k0 + k >= tokens) break;  // (the columns of no token are not looked at)
+                const float *const h = g.h + (int64_t)(m0 + nth_bit(with, k0 + k)) * g.R + r;
+                float v = 0.0f;
                 for (int s0 = 0; s0 < g.slices; s0 += 8) {
                     float part[8];
 #pragma unroll
@@ -229,62 +262,63 @@ __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
 #pragma unroll
                     for (int s = 0; s < 8; ++s) v += s0 + s < g.slices ? part[s] : 0.0f;
                 }
+                uint32_t hi, mid, lo;
+                split(v, &hi, &mid, &lo);
+                hs[0][k][r] = (uint16_t)hi;
+                hs[1][k][r] = (uint16_t)mid;
+                hs[2][k][r] = (uint16_t)lo;
             }
-            uint32_t hi, mid, lo;
-            split(v, &hi, &mid, &lo);
-            hs[0][token][r] = (uint16_t)hi;
-            hs[1][token][r] = (uint16_t)mid;
-            hs[2][token][r] = (uint16_t)lo;
-        }
-        __syncthreads();
-        for (int c = 0; c < g.R; c += 64) {
-            if (c > 0) load(c);
+            __syncthreads();
+            for (int c = 0; c < g.R; c += 64) {
+                if (c > 0 || (k0 >= kTile * g.tiles && g.R > 64)) load(c);  // (others are there)
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int r = c + 32 * k + 8 * kb;
+                for (int k = 0; k < 2; ++k) {
+                    const int r = c + 32 * k + 8 * kb;
 #pragma unroll
-                for (int q = 0; q < 3; ++q) {
-                    uint4v hw = {0, 0, 0, 0};
-                    if (r < g.R) hw = *reinterpret_cast<const uint4v *>(&hs[q][n][r]);
+                    for (int q = 0; q < 3; ++q) {
+                        uint4v hw = {0, 0, 0, 0};
+                        if (r < g.R) hw = *reinterpret_cast<const uint4v *>(&hs[q][n][r]);
 #pragma unroll
-                    for (int t = 0; t < NT; ++t)
-                        sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bw[k][t]), __builtin_bit_cast(bf16x8, hw),
-                                                                        sum[t], 0, 0, 0);
+                        for (int t = 0; t < NT; ++t)
+                            sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bw[k][t]),
+                                                                            __builtin_bit_cast(bf16x8, hw), sum[t], 0, 0, 0);
+                    }
                 }
             }
-        }
 #pragma unroll
-        for (int t = 0; t < NT; ++t) wait_written(sum[t]);
-        if (!my) continue;
-        const float scale = g.scales ? g.scales[e] : 1.0f;
-        if (whole) {
+            for (int t = 0; t < NT; ++t) wait_written(sum[t]);
+            if (my && whole) {
 #pragma unroll
-            for (int j = 0; j < 4 * NT; ++j) y[j] += sum[j >> 2][j & 3] * scale;
-            store_results<4 * NT>(g.out, g.dtype, at_y, y);
-        } else {
+                for (int j = 0; j < 4 * NT; ++j) y[j] += sum[j >> 2][j & 3] * scale;
+                store_results<4 * NT>(g.out, g.dtype, at_y, y);
+            } else if (my) {
 #pragma unroll
-            for (int j = 0; j < 4 * NT; ++j)
-                if (o0 + j < g.N) {
-                    const float v = g.dtype == NVQ_F32 ? static_cast<const float *>(g.y)[at_y + j]
-                                                       : bf16_bits_to_float(static_cast<const uint16_t *>(g.y)[at_y + j]);
-                    store_global(g.out, g.dtype, at_y + j, v + sum[j >> 2][j & 3] * scale);
-                }
+                for (int j = 0; j < 4 * NT; ++j)
+                    if (o0 + j < g.N) {
+                        const float v = g.dtype == NVQ_F32 ? static_cast<const float *>(g.y)[at_y + j]
+                                                           : bf16_bits_to_float(static_cast<const uint16_t *>(g.y)[at_y + j]);
+                        store_global(g.out, g.dtype, at_y + j, v + sum[j >> 2][j & 3] * scale);
+                    }
+            }
         }
     }
 }
 
-// Tiles of a batch, and workgroups that share a tile's adapters: one each where there are few tiles.
-int tiles_of(int M) { return (M + kTile - 1) / kTile; }
+// Groups of a batch, and the workgroups to one of them: each distinct adapter its own where there are few groups, each
+// tile of an adapter's tokens its own in any case.
+int groups_of(int M) { return (M + kGroup - 1) / kGroup; }
 int shares_of(int M, int n) {
-    const int most = n < kTile ? n : kTile;
-    return tiles_of(M) <= 4 ? (M < most ? M : most) : 1;
+    const int most = n < kGroup ? n : kGroup;
+    return groups_of(M) <= 4 ? (M < most ? M : most) : 1;
 }
+int tiles_of(int M) { return M < kGroup ? (M + kTile - 1) / kTile : kGroup / kTile; }
 // Blocks of 64, 32 or 16 ranks.
 int rank_tiles(int R) { return R > 32 ? 4 : R > 16 ? 2 : 1; }
 int rank_blocks(int R) { return (R + 16 * rank_tiles(R) - 1) / (16 * rank_tiles(R)); }
-// Slices of K: as many as bring a thousand workgroups, of four columns (one per wave) or more.
+// Slices of K: as many as bring a thousand workgroups with work, of four columns (one per wave) or more.
 int slices_of(const nvq_adapters &s, int M) {
-    const int64_t others = (int64_t)tiles_of(M) * shares_of(M, s.n) * rank_blocks(s.R);
+    const int64_t others = (int64_t)((M + kTile - 1) / kTile > shares_of(M, s.n) ? (M + kTile - 1) / kTile : shares_of(M, s.n)) *
+                           rank_blocks(s.R);
     int64_t want = 1024 / others;
     const int64_t most = (s.K / 32 + kWaves - 1) / kWaves;
     want = want < most ? want : most;
@@ -342,7 +376,8 @@ extern "C" int nvq_adapters_add(const nvq_adapters *adapters, const uint16_t *x_
     g.shares = shares_of(M, g.n);
     g.blocks = rank_blocks(g.R);
     const hipStream_t st = (hipStream_t)stream;
-    const int64_t groups = (int64_t)tiles_of(M) * g.shares;
+    g.tiles = tiles_of(M);
+    const int64_t groups = (int64_t)groups_of(M) * g.shares * g.tiles;
     const dim3 block(kThreads), down((unsigned)(groups * g.blocks * g.slices));
     if (rank_tiles(g.R) == 1)
         hipLaunchKernelGGL(adapters_down_kernel<1>, down, block, 0, st, g);
@@ -351,7 +386,7 @@ extern "C" int nvq_adapters_add(const nvq_adapters *adapters, const uint16_t *x_
     else
         hipLaunchKernelGGL(adapters_down_kernel<4>, down, block, 0, st, g);
     NVQ_HIP_TRY(hipGetLastError());
-    const bool wide = groups * g.N >= 1024 * 64;  // a wave to 64 outputs where that leaves four a compute unit
+    const bool wide = (int64_t)(M < g.shares ? M : g.shares) * g.N >= 1024 * 64 || (int64_t)groups_of(M) * g.tiles * g.N >= 1024 * 64;  // a wave to 64 outputs where that leaves four a compute unit
     const int per = (wide ? 64 : 16) * kWaves;
     g.blocks = (g.N + per - 1) / per;
     const dim3 up((unsigned)(groups * g.blocks));
