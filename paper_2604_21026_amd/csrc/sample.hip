@@ -325,15 +325,133 @@ __device__ T scan_block(T *wave, T v, T *all) {
     *all = total;
     return before + sum - v;
 }
-// The lowest thread for which `is` holds, kSampleThreads if none.
-__device__ __forceinline__ int first_thread(uint32_t *wave, bool is) {
-    const uint64_t b = __ballot(is);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = b ? (uint32_t)(threadIdx.x + __builtin_ctzll(b)) : (uint32_t)kSampleThreads;
-    __syncthreads();
-    uint32_t f = kSampleThreads;
-    for (int i = 0; i < kSampleWaves; ++i) f = wave[i] < f ? wave[i] : f;
-    return (int)f;
+
+// The bins of a row in LDS: sixteen of a lane's lie side by side, and a gap behind them against bank conflicts.
+constexpr int kLaneBins = kBins / 64, kRoom = kBins + 64 + 1;
+__device__ __forceinline__ int at_bin(int b) { return b + b / kLaneBins; }
+
+// Where a row's answers can lie, by one wave (scans and searches within it need no barrier; by the whole workgroup they
+// took 7 of 24 us).
+struct Search {
+    int lo[4], hi[4], cut;  // bins
+    uint64_t all;           // of the weights
+    uint32_t n, listed;     // tokens in all, in those bins
+};
+__device__ Search search(const Ask &k, const Grid &grid, float most, const unsigned long long *mass, const uint32_t *count,
+                         unsigned long long *before, uint32_t *ranked, uint32_t *first) {
+    const int lane = threadIdx.x & 63, b0 = kLaneBins * lane;
+    uint64_t m[kLaneBins], sum = 0;
+    uint32_t c[kLaneBins], n = 0;
+#pragma unroll
+    for (int i = 0; i < kLaneBins; ++i) {
+        m[i] = mass[at_bin(b0 + i)];
+        c[i] = count[at_bin(b0 + i)];
+        sum += m[i];
+        n += c[i];
+    }
+    uint64_t to = sum;
+    uint32_t nto = n;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint64_t o = __shfl_up((unsigned long long)to, d);
+        const uint32_t p = __shfl_up(nto, d);
+        if (lane >= d) {
+            to += o;
+            nto += p;
+        }
+    }
+    Search r;
+    r.all = __shfl((unsigned long long)to, 63);
+    r.n = __shfl(nto, 63);
+    to -= sum;
+    nto -= n;
+#pragma unroll
+    for (int i = 0; i < kLaneBins; ++i) {  // m, c become sums up to the bin, itself included
+        before[at_bin(b0 + i)] = to;
+        ranked[at_bin(b0 + i)] = nto;
+        to += m[i];
+        nto += c[i];
+        m[i] = to;
+        c[i] = nto;
+    }
+    // (upto of a bin: before of the next; a wave's LDS accesses stay in order)
+    if (lane == 63) before[at_bin(kBins)] = to;
+    // The first bin with which the sum reaches x, the last one if none does.  (Its own weight is not zero then, or x is
+    // not above the sum before, and the first bin holds the first token.)
+    auto reaching = [&](double x) {
+        int b = kBins;
+#pragma unroll
+        for (int i = kLaneBins - 1; i >= 0; --i) b = (double)m[i] >= x ? b0 + i : b;
+        const uint64_t any = __ballot(b < kBins);
+        return any ? __shfl(b, __builtin_ctzll(any)) : kBins - 1;
+    };
+    auto counting = [&](uint32_t x) {
+        int b = kBins;
+#pragma unroll
+        for (int i = kLaneBins - 1; i >= 0; --i) b = c[i] >= x ? b0 + i : b;
+        const uint64_t any = __ballot(b < kBins);
+        return any ? __shfl(b, __builtin_ctzll(any)) : kBins - 1;
+    };
+    // Bounds of the sums are a little wide: a bin's weight has been rounded otherwise than the sum of its tokens'.
+    const double wide = 1.0 + 0x1p-30, all = (double)r.all;
+    double least = all, greatest = all;
+    auto bounds = [&](int i) {  // of a kept sum that ends in these bins
+        least = fmin(least, (double)before[at_bin(r.lo[i])]);
+        greatest = fmin(greatest, (double)before[at_bin(r.hi[i] + 1)]);
+    };
+    for (int i = 0; i < 4; ++i) {
+        r.lo[i] = kBins;
+        r.hi[i] = -1;
+    }
+    r.cut = 0;
+    if (k.top_k > 0 && (uint32_t)k.top_k < r.n) {
+        r.lo[0] = r.hi[0] = counting((uint32_t)k.top_k);
+        bounds(0);
+    }
+    if (!(k.top_p >= 1.0f)) {
+        const double p = k.top_p > 0.0f ? (double)k.top_p : 0.0;
+        r.lo[1] = reaching(fmax(p * least / wide, 1.0));
+        r.hi[1] = reaching(fmin(fmax(p * greatest * wide + 2.0, 1.0), all));
+        r.hi[1] = r.hi[1] > r.lo[1] ? r.hi[1] : r.lo[1];
+        bounds(1);
+    }
+    if (k.min_p > 0.0f) {
+        const double at = (double)most + (double)k.temperature * log((double)k.min_p);
+        const int cut = grid.bin((float)at);  // (its rounding moves it to a neighbouring bin at most)
+        r.cut = r.lo[2] = cut > 0 ? cut - 1 : 0;
+        r.hi[2] = r.cut + 2 < kBins - 1 ? r.cut + 2 : kBins - 1;
+        bounds(2);
+    }
+    least = fmax(least, kOne);
+    greatest = fmax(greatest, kOne);
+    const double u = k.u > 0.0f ? (k.u < 1.0f ? (double)k.u : 1.0) : 0.0;
+    r.lo[3] = reaching(fmax(u * least / wide - 2.0, 1.0));
+    r.hi[3] = reaching(fmin(u * greatest * wide + 2.0, all));
+    r.hi[3] = r.hi[3] > r.lo[3] ? r.hi[3] : r.lo[3];
+    uint32_t own[kLaneBins], wanted = 0;
+#pragma unroll
+    for (int i = 0; i < kLaneBins; ++i) {
+        const int b = b0 + i;
+        bool is = false;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) is |= b >= r.lo[j] && b <= r.hi[j];
+        own[i] = is ? c[i] - ranked[at_bin(b)] : 0u;
+        wanted += own[i];
+    }
+    uint32_t at = wanted;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const uint32_t o = __shfl_up(at, d);
+        if (lane >= d) at += o;
+    }
+    r.listed = __shfl(at, 63);
+    at -= wanted;
+#pragma unroll
+    for (int i = 0; i < kLaneBins; ++i) {
+        first[at_bin(b0 + i)] = at;
+        at += own[i];
+    }
+    return r;
 }
 
 // A workgroup's part of a row: logits [*i0, *i1).
@@ -344,11 +462,12 @@ __device__ __forceinline__ void part_of(const SampleArgs &a, int part, int *i0, 
 
 __global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(SampleArgs a) {
     __shared__ Shared s;
-    __shared__ unsigned long long mass[kBins], wave64[kSampleWaves];
-    __shared__ uint32_t count[kBins], wave32[kSampleWaves];
+    __shared__ unsigned long long mass[kRoom], before[kRoom + 1];
+    __shared__ uint32_t count[kRoom], ranked[kRoom], first_of[kRoom];
     __shared__ unsigned long long heads[kMostParts];
-    __shared__ unsigned long long edge[2];
+    __shared__ double factors[kMostParts];
     __shared__ uint32_t last;
+    __shared__ Search found;
     const int m = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x;
     const Row row = row_of(a, m);
     const Ask k = ask_of(a, m);
@@ -371,8 +490,9 @@ __global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(SampleArgs 
             best = key > best ? key : best;
         }
     }
-    mass[tid] = 0;
-    count[tid] = 0;
+    const int my = at_bin(tid);
+    mass[my] = 0;
+    count[my] = 0;
     best = over_block(s, best, Most64());
     const uint32_t top_word = (uint32_t)(best >> 32);
     const bool ordinary = k.temperature > 0.0f;  // (else the first token is the answer)
@@ -391,7 +511,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(SampleArgs 
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 if (!(l[j] > -INFINITY)) continue;
-                const int bin = grid.bin(l[j]);
+                const int bin = at_bin(grid.bin(l[j]));
                 atomicAdd(&count[bin], 1u);
                 atomicAdd(&mass[bin], (unsigned long long)w.of(l[j]));
             }
@@ -400,8 +520,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(SampleArgs 
     __syncthreads();
     if (a.parts > 1) {
         PartBins &to = a.bins[(int64_t)m * a.parts + part];
-        put64(&to.mass[tid], mass[tid]);
-        put32(&to.count[tid], count[tid]);
+        put64(&to.mass[tid], mass[my]);
+        put32(&to.count[tid], count[my]);
         if (tid == 0) put64(&a.heads[(int64_t)m * a.parts + part].best, best);
         __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): written through to where all XCDs see it
         __syncthreads();
@@ -428,8 +548,10 @@ __global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(SampleArgs 
     }
     const Grid grid = {steps, Grid::number(most, steps)};
     if (a.parts > 1) {
-        mass[tid] = 0;
-        count[tid] = 0;
+        mass[my] = 0;
+        count[my] = 0;
+        // a part's weights, relative to the row's largest
+        if (tid < a.parts) factors[tid] = exp(((double)of_sort_word((uint32_t)(heads[tid] >> 32)) - (double)most) / (double)k.temperature);
         __syncthreads();
         for (int p0 = 0; p0 < a.parts; p0 += 8) {
             uint64_t ms[8];
@@ -445,87 +567,29 @@ __global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(SampleArgs 
                 if (p0 + p >= a.parts || cs[p] == 0) continue;
                 const float top = of_sort_word((uint32_t)(heads[p0 + p] >> 32));
                 const float shift = grid.top - Grid::number(top, steps);
-                const int bin = (int)fminf(shift + (float)tid, (float)(kBins - 1));
-                // its weights, relative to the row's largest
-                const double f = exp(((double)top - (double)most) / (double)k.temperature);
+                const int bin = at_bin((int)fminf(shift + (float)tid, (float)(kBins - 1)));
                 atomicAdd(&count[bin], cs[p]);
-                atomicAdd(&mass[bin], (unsigned long long)(f * (double)ms[p]));
+                atomicAdd(&mass[bin], (unsigned long long)(factors[p0 + p] * (double)ms[p]));
             }
         }
         __syncthreads();
     }
-    // Where the answers can lie.  Bounds of the sums are a little wide: a bin's weight has been rounded otherwise than
-    // the sum of its tokens'.
-    const uint64_t mine = mass[tid];
-    const uint32_t here = count[tid];
-    unsigned long long all;
-    uint32_t n;
-    const uint64_t before = scan_block(wave64, (unsigned long long)mine, &all);
-    const uint32_t ranked = scan_block(wave32, here, &n);
-    const uint64_t upto = before + mine;
-    const double wide = 1.0 + 0x1p-30;
-    auto bin_reaching = [&](double x) {  // the first bin with which the sum reaches x
-        const int b = first_thread(wave32, here && (double)upto >= x);
-        return b < kBins ? b : kBins - 1;
-    };
-    auto bounds = [&](int lo, int hi, double *least, double *most_) {  // of a sum that ends in these bins
-        __syncthreads();
-        if (tid == lo) edge[0] = before;
-        if (tid == hi) edge[1] = upto;
-        __syncthreads();
-        *least = (double)edge[0];
-        *most_ = (double)edge[1];
-    };
-    int lo[4] = {kBins, kBins, kBins, kBins}, hi[4] = {-1, -1, -1, -1}, cut = 0;
-    double least = (double)all, greatest = (double)all;
-    if (k.top_k > 0 && (uint32_t)k.top_k < n) {
-        lo[0] = hi[0] = first_thread(wave32, ranked + here >= (uint32_t)k.top_k);
-        bounds(lo[0], hi[0], &least, &greatest);
+    if (tid < 64) {
+        const Search r = search(k, grid, most, mass, count, before, ranked, first_of);
+        if (tid == 0) found = r;
     }
-    if (!(k.top_p >= 1.0f)) {
-        const double p = k.top_p > 0.0f ? (double)k.top_p : 0.0;
-        lo[1] = bin_reaching(fmax(p * least / wide, 1.0));
-        hi[1] = bin_reaching(fmin(fmax(p * greatest * wide + 2.0, 1.0), (double)all));
-        hi[1] = hi[1] > lo[1] ? hi[1] : lo[1];
-        double l, g;
-        bounds(lo[1], hi[1], &l, &g);
-        least = fmin(least, l);
-        greatest = fmin(greatest, g);
-    }
-    if (k.min_p > 0.0f) {
-        const double at = (double)most + (double)k.temperature * log((double)k.min_p);
-        cut = grid.bin((float)at);  // (its rounding moves it to a neighbouring bin at most)
-        cut = cut > 0 ? cut - 1 : 0;
-        lo[2] = cut;
-        hi[2] = cut + 2 < kBins - 1 ? cut + 2 : kBins - 1;
-        double l, g;
-        bounds(lo[2], hi[2], &l, &g);
-        least = fmin(least, l);
-        greatest = fmin(greatest, g);
-    }
-    least = fmax(least, kOne);
-    greatest = fmax(greatest, kOne);
-    const double u = k.u > 0.0f ? (k.u < 1.0f ? (double)k.u : 1.0) : 0.0;
-    lo[3] = bin_reaching(fmax(u * least / wide - 2.0, 0.0));
-    hi[3] = bin_reaching(fmin(u * greatest * wide + 2.0, (double)all));
-    hi[3] = hi[3] > lo[3] ? hi[3] : lo[3];
-    bool wanted = false;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) wanted |= tid >= lo[i] && tid <= hi[i];
-    uint32_t listed;
-    const uint32_t at = scan_block(wave32, wanted ? here : 0u, &listed);
-    if (listed > (uint32_t)kList || !(fabsf(grid.top) < kFar)) {  // (the same for the whole row)
-        __syncthreads();
-        const int id = choose_slowly(s, row, k, most, n);
+    __syncthreads();
+    if (found.listed > (uint32_t)kList || !(fabsf(grid.top) < kFar)) {  // (the same for the whole row)
+        const int id = choose_slowly(s, row, k, most, found.n);
         if (tid == 0) {
             a.ids[m] = id;
             state.gather = 0;
         }
         return;
     }
-    state.before[tid] = before;
-    state.ranked[tid] = ranked;
-    state.first[tid] = at;
+    state.before[tid] = before[my];
+    state.ranked[tid] = ranked[my];
+    state.first[tid] = first_of[my];
     if (tid == 0) {
         state.gather = 1;
         state.listed = 0;
@@ -534,18 +598,19 @@ __global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(SampleArgs 
         state.top = grid.top;
         state.most = most;
         for (int i = 0; i < 4; ++i) {
-            state.lo[i] = lo[i];
-            state.hi[i] = hi[i];
+            state.lo[i] = found.lo[i];
+            state.hi[i] = found.hi[i];
         }
-        state.all = all;
-        state.count = n;
-        state.cut = cut;
+        state.all = found.all;
+        state.count = found.n;
+        state.cut = found.cut;
     }
 }
 
 __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs a) {
-    __shared__ unsigned long long key[kList], sum[kList + 1], wave64[kSampleWaves];
+    __shared__ unsigned long long key[kList], sum[kList], wave64[kSampleWaves];
     __shared__ uint32_t wave32[kSampleWaves], shared_at, last;
+    uint32_t *const place = reinterpret_cast<uint32_t *>(sum);  // (before the sums are there)
     __shared__ unsigned long long found[3];
     const int m = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x;
     RowState &state = a.rows[m];
@@ -594,86 +659,107 @@ __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs 
 
     const Ask k = ask_of(a, m);
     const int n = (int)get32(&state.listed) < kList ? (int)get32(&state.listed) : kList;
+    // A token's place in the descending order is the number of larger keys (they are all different): counted by as
+    // many threads per token as there are, each over a share of the keys.
     int size = 64;
-    while (size < n) size *= 2;
-    for (int i = tid; i < size; i += kSampleThreads) key[i] = i < n ? get64(&state.list[i]) : 0;
-    __syncthreads();
-    // descending, in pairs of sorted runs
-    for (int run = 2; run <= size; run *= 2)
-        for (int d = run / 2; d; d /= 2) {
-            for (int i = tid; i < size / 2; i += kSampleThreads) {
-                const int x = i / d * 2 * d + i % d, y = x + d;
-                const bool down = (x & run) == 0;
-                const uint64_t p = key[x], q = key[y];
-                if (down ? p < q : p > q) {
-                    key[x] = q;
-                    key[y] = p;
-                }
-            }
-            __syncthreads();
+    while (size < n && size < kSampleThreads) size *= 2;
+    const int shares = kSampleThreads / size, share = tid / size, per = (n + shares - 1) / shares;
+    uint64_t mine[kList / kSampleThreads];
+#pragma unroll
+    for (int q = 0; q < kList / kSampleThreads; ++q) {
+        const int i = q * kSampleThreads + tid;
+        mine[q] = i < n ? get64(&state.list[i]) : 0;
+        if (i < n) {
+            key[i] = mine[q];
+            place[i] = 0;
         }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kList / kSampleThreads; ++q) {
+        const int i = q * kSampleThreads + tid % size;
+        if (q * kSampleThreads >= n || i >= n) continue;
+        const uint64_t x = shares == 1 ? mine[q] : (uint64_t)key[i];
+        const int j1 = (share + 1) * per < n ? (share + 1) * per : n;
+        uint32_t larger = 0;
+        for (int j = share * per; j < j1; ++j) larger += key[j] > x;
+        if (shares == 1)
+            place[i] = larger;
+        else
+            atomicAdd(&place[i], larger);
+    }
+    __syncthreads();
+    uint32_t to[kList / kSampleThreads];
+#pragma unroll
+    for (int q = 0; q < kList / kSampleThreads; ++q) to[q] = q * kSampleThreads + tid < n ? place[q * kSampleThreads + tid] : 0;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kList / kSampleThreads; ++q)
+        if (q * kSampleThreads + tid < n) key[to[q]] = mine[q];
+    __syncthreads();
+    // Per token: its weight, the sum of the weights up to it (itself included) in the row, and its rank there.
     const Weights w(state.most, k.temperature);
-    uint64_t carry = 0;
-    for (int b = 0; b < n; b += kSampleThreads) {
-        const int i = b + tid;
-        const uint64_t v = i < n ? w.of_word((uint32_t)(key[i] >> 32)) : 0;
+    uint64_t weight[kList / kSampleThreads], upto[kList / kSampleThreads], carry = 0;
+    uint32_t rank[kList / kSampleThreads];
+    int bin[kList / kSampleThreads];
+#pragma unroll
+    for (int q = 0; q < kList / kSampleThreads; ++q) {
+        weight[q] = 0;
+        if (q * kSampleThreads >= n) continue;
+        const int i = q * kSampleThreads + tid;
+        if (i < n) weight[q] = w.of_word((uint32_t)(key[i] >> 32));
         unsigned long long all;
-        const uint64_t at = scan_block(wave64, (unsigned long long)v, &all);
+        const uint64_t at = scan_block(wave64, (unsigned long long)weight[q], &all);
         if (i < n) sum[i] = carry + at;
         carry += all;
     }
-    if (tid == 0) sum[n] = carry;
     if (tid < 3) found[tid] = ~0ull;
+    if (tid == 0) last = ~0u;
     __syncthreads();
-    // A listed token's place in the row: the sum of the weights up to it (itself included), and before it its rank.
-    struct At {
-        uint64_t upto;
-        uint32_t rank;
-        int bin;
-    };
-    auto place = [&](int i) {
-        At p;
-        p.bin = grid.bin(of_sort_word((uint32_t)(key[i] >> 32)));
-        const uint32_t first = state.first[p.bin];
-        p.upto = state.before[p.bin] + (sum[i + 1] - sum[first]);
-        p.rank = state.ranked[p.bin] + ((uint32_t)i - first);
-        return p;
+#pragma unroll
+    for (int q = 0; q < kList / kSampleThreads; ++q) {
+        const int i = q * kSampleThreads + tid;
+        if (i >= n) continue;
+        bin[q] = grid.bin(of_sort_word((uint32_t)(key[i] >> 32)));
+        const uint32_t first = state.first[bin[q]];
+        upto[q] = state.before[bin[q]] + (sum[i] + weight[q] - sum[first]);
+        rank[q] = state.ranked[bin[q]] + ((uint32_t)i - first);
+    }
+    auto each = [&](auto f) {
+#pragma unroll
+        for (int q = 0; q < kList / kSampleThreads; ++q)
+            if (q * kSampleThreads + tid < n) f(q);
     };
     uint64_t kept = state.all;
     if (k.top_k > 0 && (uint32_t)k.top_k < state.count) {
-        for (int i = tid; i < n; i += kSampleThreads) {
-            const At p = place(i);
-            if (p.rank == (uint32_t)k.top_k - 1) found[0] = p.upto;
-        }
+        each([&](int q) {
+            if (rank[q] == (uint32_t)k.top_k - 1) found[0] = upto[q];
+        });
         __syncthreads();
         kept = found[0] < kept ? found[0] : kept;
     }
     if (!(k.top_p >= 1.0f)) {
         const uint64_t reach = reach_of(k.top_p, kept);
-        for (int i = tid; i < n; i += kSampleThreads) {
-            const At p = place(i);
-            if (p.upto >= reach) atomicMin(&found[1], (unsigned long long)p.upto);
-        }
+        each([&](int q) {
+            if (upto[q] >= reach) atomicMin(&found[1], (unsigned long long)upto[q]);
+        });
         __syncthreads();
         kept = found[1] < kept ? found[1] : kept;
     }
     if (k.min_p > 0.0f) {
-        __syncthreads();
         if (tid == 0) found[2] = state.before[state.cut];
         __syncthreads();
-        for (int i = tid; i < n; i += kSampleThreads) {
-            const At p = place(i);
-            if (p.bin >= state.cut && (double)(sum[i + 1] - sum[i]) >= (double)k.min_p * kOne) atomicMax(&found[2], (unsigned long long)p.upto);
-        }
+        each([&](int q) {
+            if (bin[q] >= state.cut && (double)weight[q] >= (double)k.min_p * kOne) atomicMax(&found[2], (unsigned long long)upto[q]);
+        });
         __syncthreads();
         kept = found[2] < kept ? found[2] : kept;
     }
     kept = kept < 1ull << kPoint ? 1ull << kPoint : kept;  // (the first token's weight is 1)
     const uint64_t x = point_of(k.u, kept);
-    if (tid == 0) last = ~0u;
-    __syncthreads();
-    for (int i = tid; i < n; i += kSampleThreads)
-        if (place(i).upto > x) atomicMin(&last, (uint32_t)i);
+    each([&](int q) {
+        if (upto[q] > x) atomicMin(&last, (uint32_t)(q * kSampleThreads + tid));
+    });
     __syncthreads();
     if (tid == 0) a.ids[m] = (int)~(uint32_t)key[last < (uint32_t)n ? last : (uint32_t)n - 1];
 }
