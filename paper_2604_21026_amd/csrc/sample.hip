@@ -610,7 +610,8 @@ __global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(SampleArgs 
 __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs a) {
     __shared__ unsigned long long key[kList], sum[kList], wave64[kSampleWaves];
     __shared__ uint32_t wave32[kSampleWaves], shared_at, last;
-    uint32_t *const place = reinterpret_cast<uint32_t *>(sum);  // (before the sums are there)
+    // Before the keys are in order: tokens per slot, and of the slots before.  Before the sums: keys by slot.
+    uint32_t *const count = reinterpret_cast<uint32_t *>(key), *const begin = count + kList;
     __shared__ unsigned long long found[3];
     const int m = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x;
     RowState &state = a.rows[m];
@@ -659,51 +660,69 @@ __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs 
 
     const Ask k = ask_of(a, m);
     const int n = (int)get32(&state.listed) < kList ? (int)get32(&state.listed) : kList;
-    // A token's place in the descending order is the number of larger keys (they are all different): counted by as
-    // many threads per token as there are, each over a share of the keys.
-    int size = 64;
-    while (size < n && size < kSampleThreads) size *= 2;
-    const int shares = kSampleThreads / size, share = tid / size, per = (n + shares - 1) / shares;
-    uint64_t mine[kList / kSampleThreads];
+    // Sorted by interpolation: a bin's tokens have as many slots as they are, a logit's slot goes by its place within the
+    // bin, and the few that share one (equal logits among them) are ranked by counting.
+    constexpr int kEach = kList / kSampleThreads;
+    uint64_t mine[kEach];
+    uint32_t slot[kEach], nth[kEach];
 #pragma unroll
-    for (int q = 0; q < kList / kSampleThreads; ++q) {
+    for (int q = 0; q < kEach; ++q) {
         const int i = q * kSampleThreads + tid;
         mine[q] = i < n ? get64(&state.list[i]) : 0;
-        if (i < n) {
-            key[i] = mine[q];
-            place[i] = 0;
+        count[i] = 0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+        if (q * kSampleThreads + tid >= n) continue;
+        const float l = of_sort_word((uint32_t)(mine[q] >> 32));
+        const int b = grid.bin(l);
+        const uint32_t from = state.first[b], room = (b + 1 < kBins ? state.first[b + 1] : (uint32_t)n) - from;
+        const float v = l * grid.steps, down = b + 1 < kBins ? floorf(v) + 1.0f - v : 0.0f;  // (0, 1]; the last bin: one slot
+        const uint32_t in = (uint32_t)(down * (float)room);
+        slot[q] = from + (in < room ? in : room - 1);
+        nth[q] = atomicAdd(&count[slot[q]], 1u);
+    }
+    __syncthreads();
+    {
+        uint32_t c[kEach], sum4 = 0, all;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            c[q] = count[kEach * tid + q];
+            sum4 += c[q];
+        }
+        uint32_t at = scan_block(wave32, sum4, &all);
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            begin[kEach * tid + q] = at;
+            at += c[q];
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int q = 0; q < kList / kSampleThreads; ++q) {
-        const int i = q * kSampleThreads + tid % size;
-        if (q * kSampleThreads >= n || i >= n) continue;
-        const uint64_t x = shares == 1 ? mine[q] : (uint64_t)key[i];
-        const int j1 = (share + 1) * per < n ? (share + 1) * per : n;
-        uint32_t larger = 0;
-        for (int j = share * per; j < j1; ++j) larger += key[j] > x;
-        if (shares == 1)
-            place[i] = larger;
-        else
-            atomicAdd(&place[i], larger);
+    for (int q = 0; q < kEach; ++q)
+        if (q * kSampleThreads + tid < n) sum[begin[slot[q]] + nth[q]] = mine[q];
+    __syncthreads();
+    uint32_t to[kEach];
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+        if (q * kSampleThreads + tid >= n) continue;
+        const uint32_t j0 = begin[slot[q]], j1 = j0 + count[slot[q]];
+        to[q] = j0;
+        for (uint32_t j = j0; j < j1; ++j) to[q] += sum[j] > mine[q];
     }
     __syncthreads();
-    uint32_t to[kList / kSampleThreads];
 #pragma unroll
-    for (int q = 0; q < kList / kSampleThreads; ++q) to[q] = q * kSampleThreads + tid < n ? place[q * kSampleThreads + tid] : 0;
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < kList / kSampleThreads; ++q)
+    for (int q = 0; q < kEach; ++q)
         if (q * kSampleThreads + tid < n) key[to[q]] = mine[q];
     __syncthreads();
     // Per token: its weight, the sum of the weights up to it (itself included) in the row, and its rank there.
     const Weights w(state.most, k.temperature);
-    uint64_t weight[kList / kSampleThreads], upto[kList / kSampleThreads], carry = 0;
-    uint32_t rank[kList / kSampleThreads];
-    int bin[kList / kSampleThreads];
+    uint64_t weight[kEach], upto[kEach], carry = 0;
+    uint32_t rank[kEach];
+    int bin[kEach];
 #pragma unroll
-    for (int q = 0; q < kList / kSampleThreads; ++q) {
+    for (int q = 0; q < kEach; ++q) {
         weight[q] = 0;
         if (q * kSampleThreads >= n) continue;
         const int i = q * kSampleThreads + tid;
@@ -717,7 +736,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs 
     if (tid == 0) last = ~0u;
     __syncthreads();
 #pragma unroll
-    for (int q = 0; q < kList / kSampleThreads; ++q) {
+    for (int q = 0; q < kEach; ++q) {
         const int i = q * kSampleThreads + tid;
         if (i >= n) continue;
         bin[q] = grid.bin(of_sort_word((uint32_t)(key[i] >> 32)));
@@ -727,7 +746,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs 
     }
     auto each = [&](auto f) {
 #pragma unroll
-        for (int q = 0; q < kList / kSampleThreads; ++q)
+        for (int q = 0; q < kEach; ++q)
             if (q * kSampleThreads + tid < n) f(q);
     };
     uint64_t kept = state.all;
