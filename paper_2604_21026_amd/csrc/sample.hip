@@ -10,7 +10,7 @@
 //      them by logit and index and answers every question to the token.
 // Weights are 64-bit fixed point relative to the largest, so that sums do not depend on their order.  A row whose bins
 // hold too many tokens (nearly equal logits), or whose logits are out of the bins' range, is looked at by one workgroup
-// alone, eight bits of the sort words after the other (choose_slowly).
+// alone, eight bits of the sort words after the other (choose_slowly, in the second launch).
 #include "mfma_act.h"
 
 namespace nvq {
@@ -56,30 +56,40 @@ struct Row {
     __device__ uint32_t word(int i) const { return sort_word(logit(i)); }
 };
 
-// exp(x) as fixed point, x = (logit - top) / temperature <= 0: 2^k times the exponential series of the rest, |rest| <=
-// ln 2 / 2, to 13 terms (the next is 2e-16 of the sum).  One half unit of the last place, 2^-44, as rounding.
+// exp(x) as fixed point, x = (logit - top) / temperature <= 0: 2^(k / 64), its fraction from a table, times the
+// exponential series of the rest, |rest| <= ln 2 / 128, to six terms (the next is 4e-17 of the sum; without the table it
+// takes thirteen, and the weights of a row of 128256 in sixteen parts 4.4 us instead of XX).
+constexpr int kRoots = 64;
+__constant__ const double kRoot[kRoots] = {
+    1.0, 1.0108892860517005, 1.0218971486541166, 1.0330248790212284, 1.0442737824274138, 1.0556451783605572,
+    1.0671404006768237, 1.0787607977571199, 1.0905077326652577, 1.102382583307841, 1.1143867425958924, 1.1265216186082418,
+    1.1387886347566916, 1.1511892299529827, 1.1637248587775775, 1.1763969916502812, 1.189207115002721, 1.202156731452703,
+    1.215247359980469, 1.22848053610687, 1.241857812073484, 1.255380757024691, 1.2690509571917332, 1.2828700160787783,
+    1.2968395546510096, 1.3109612115247644, 1.3252366431597413, 1.339667524053303, 1.3542555469368927, 1.3690024229745905,
+    1.383909881963832, 1.3989796725383112, 1.4142135623730951, 1.42961333839197, 1.4451808069770467, 1.460917794180647,
+    1.4768261459394993, 1.4929077282912648, 1.5091644275934228, 1.5255981507445384, 1.5422108254079407, 1.559004400237837,
+    1.5759808451078865, 1.593142151342267, 1.6104903319492543, 1.6280274218573478, 1.645755478153965, 1.6636765803267364,
+    1.681792830507429, 1.7001063537185235, 1.718619298122478, 1.7373338352737062, 1.7562521603732995, 1.7753764925265212,
+    1.7947090750031072, 1.8142521755003989, 1.8340080864093424, 1.8539791250833855, 1.8741676341103, 1.8945759815869656,
+    1.9152065613971474, 1.9360617934922943, 1.9571441241754002, 1.978456026387951};
 struct Weights {
-    double top, rate;  // log2(e) / temperature
-    __device__ Weights(float most, float temperature) : top(most), rate(1.4426950408889634074 / (double)temperature) {}
+    double top, rate;  // 64 log2(e) / temperature
+    const double *root;  // kRoot, or a copy in LDS
+    __device__ Weights(float most, float temperature, const double *roots)
+        : top(most), rate(kRoots * 1.4426950408889634074 / (double)temperature), root(roots) {}
     __device__ uint64_t of(float logit) const {
         double t = ((double)logit - top) * rate;
-        t = t > -64.0 ? t : -64.0;  // (nothing is left of the weight long before)
-        const double k = rint(t), x = (t - k) * 0.69314718055994530942;
-        double e = 1.0 / 479001600;
-        e = fma(e, x, 1.0 / 39916800);
-        e = fma(e, x, 1.0 / 3628800);
-        e = fma(e, x, 1.0 / 362880);
-        e = fma(e, x, 1.0 / 40320);
-        e = fma(e, x, 1.0 / 5040);
-        e = fma(e, x, 1.0 / 720);
-        e = fma(e, x, 1.0 / 120);
+        t = t > -64.0 * kRoots ? t : -64.0 * kRoots;  // (nothing is left of the weight long before)
+        const double k = rint(t), x = (t - k) * (0.69314718055994530942 / kRoots);
+        const int i = (int)k;
+        double e = 1.0 / 120;
         e = fma(e, x, 1.0 / 24);
         e = fma(e, x, 1.0 / 6);
         e = fma(e, x, 0.5);
         e = fma(e, x, 1.0);
-        e = fma(e, x, 1.0);
-        // e times 2^(k + kPoint), below 2^44; beside 2^52 its whole part is the low bits
-        const double scaled = __longlong_as_double(__double_as_longlong(e) + ((int64_t)((int)k + kPoint) << 52));
+        e = fma(e, x, 1.0) * root[i & (kRoots - 1)];
+        // e times 2^(k / 64 + kPoint), below 2^44; beside 2^52 its whole part is the low bits
+        const double scaled = __longlong_as_double(__double_as_longlong(e) + ((int64_t)((i >> 6) + kPoint) << 52));
         return (uint64_t)__double_as_longlong(scaled + 4503599627370496.0) & 0xfffffffffffffull;
     }
     __device__ uint64_t of_word(uint32_t word) const { return of(of_sort_word(word)); }
@@ -94,13 +104,14 @@ struct Shared {
 };
 
 template <typename OP>
-__device__ uint64_t over_block(Shared &s, uint64_t v, OP op) {
+__device__ uint64_t over_block(unsigned long long *wave, uint64_t v, OP op) {
     for (int d = 32; d; d >>= 1) v = op(v, (uint64_t)__shfl_xor((unsigned long long)v, d));
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) s.wave[threadIdx.x >> 6] = v;
+    if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = s.wave[0];
-    for (int i = 1; i < kSampleWaves; ++i) v = op(v, (uint64_t)s.wave[i]);
+    v = wave[0];
+#pragma unroll
+    for (int i = 1; i < kSampleWaves; ++i) v = op(v, (uint64_t)wave[i]);
     return v;
 }
 struct Most64 {
@@ -216,7 +227,7 @@ __device__ __forceinline__ uint64_t reach_of(float top_p, uint64_t all) {
 
 // The answer for a row of n tokens to choose from, by one workgroup and any logits.
 __device__ int choose_slowly(Shared &s, const Row &row, const Ask &k, float most, uint64_t n) {
-    const Weights w(most, k.temperature);
+    const Weights w(most, k.temperature, kRoot);
     uint32_t word;
     uint64_t before, kept;
     if (k.top_k > 0 && (uint64_t)k.top_k < n) {
@@ -226,14 +237,14 @@ __device__ int choose_slowly(Shared &s, const Row &row, const Ask &k, float most
             const uint32_t v = row.word(i);
             above += v > word ? w.of_word(v) : 0;
         }
-        kept = over_block(s, above, Add64()) + ((uint64_t)k.top_k - before) * w.of_word(word);
+        kept = over_block(s.wave, above, Add64()) + ((uint64_t)k.top_k - before) * w.of_word(word);
     } else {
         uint64_t all = 0;
         for (int i = threadIdx.x; i < row.V; i += kSampleThreads) {
             const uint32_t v = row.word(i);
             all += v ? w.of_word(v) : 0;
         }
-        kept = over_block(s, all, Add64());
+        kept = over_block(s.wave, all, Add64());
     }
     if (!(k.top_p >= 1.0f)) {
         const uint64_t reach = reach_of(k.top_p, kept);
@@ -248,7 +259,7 @@ __device__ int choose_slowly(Shared &s, const Row &row, const Ask &k, float most
             const uint64_t x = v ? w.of_word(v) : 0;
             enough += (double)x >= (double)k.min_p * kOne ? x : 0;
         }
-        enough = over_block(s, enough, Add64());
+        enough = over_block(s.wave, enough, Add64());
         kept = enough < kept ? enough : kept;
     }
     kept = kept < 1ull << kPoint ? 1ull << kPoint : kept;  // (the first token's weight is 1)
@@ -277,21 +288,20 @@ struct PartHead {
     unsigned long long best;  // sort word and complement of the index of the part's first token; 0: none
 };
 struct PartBins {
-    unsigned long long mass[kBins];  // relative to the part's largest
+    double mass[kBins];  // relative to the part's largest
     uint32_t count[kBins];
 };
 // What the second launch has to know of a row.
 struct RowState {
-    uint32_t gather;   // 0: the row has its answer
+    uint32_t gather;   // 0: the row has its answer, 1: in these bins, 2: they do not serve
     uint32_t listed, arrived;
     float steps, top, most;
-    int lo[4], hi[4];  // bins whose tokens are collected
+    int lo[4], hi[4];  // bins whose tokens are collected: ranges in ascending order that share no bin
     unsigned long long all;  // of the weights
     uint32_t count;
     int cut;           // min_p: bins before have the weight, those from cut + 3 on have not
     unsigned long long before[kBins];  // weights of the bins before
-    uint32_t ranked[kBins];            // tokens of the bins before
-    uint32_t first[kBins];             // collected tokens of the bins before
+    uint32_t ranked[kBins + 1];        // tokens of the bins before
     unsigned long long list[kList];
 };
 
@@ -305,7 +315,7 @@ __device__ __forceinline__ void put32(uint32_t *p, uint32_t v) { __hip_atomic_st
 __device__ __forceinline__ uint32_t get32(const uint32_t *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // Sum over the threads before this one; *all: over all.
-template <typename T>
+template <int W, typename T>
 __device__ T scan_block(T *wave, T v, T *all) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     T sum = v;
@@ -317,7 +327,8 @@ __device__ T scan_block(T *wave, T v, T *all) {
     if (lane == 63) wave[w] = sum;
     __syncthreads();
     T before = 0, total = 0;
-    for (int i = 0; i < kSampleWaves; ++i) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
         const T x = wave[i];
         before += i < w ? x : 0;
         total += x;
@@ -326,86 +337,84 @@ __device__ T scan_block(T *wave, T v, T *all) {
     return before + sum - v;
 }
 
-// The bins of a row in LDS: sixteen of a lane's lie side by side, and a gap behind them against bank conflicts.
-constexpr int kLaneBins = kBins / 64, kRoom = kBins + 64 + 1;
-__device__ __forceinline__ int at_bin(int b) { return b + b / kLaneBins; }
-
-// Where a row's answers can lie, by one wave (scans and searches within it need no barrier; by the whole workgroup they
-// took 7 of 24 us).
-struct Search {
-    int lo[4], hi[4], cut;  // bins
-    uint64_t all;           // of the weights
-    uint32_t n, listed;     // tokens in all, in those bins
-};
-__device__ Search search(const Ask &k, const Grid &grid, float most, const unsigned long long *mass, const uint32_t *count,
-                         unsigned long long *before, uint32_t *ranked, uint32_t *first) {
-    const int lane = threadIdx.x & 63, b0 = kLaneBins * lane;
-    uint64_t m[kLaneBins], sum = 0;
-    uint32_t c[kLaneBins], n = 0;
-#pragma unroll
-    for (int i = 0; i < kLaneBins; ++i) {
-        m[i] = mass[at_bin(b0 + i)];
-        c[i] = count[at_bin(b0 + i)];
-        sum += m[i];
-        n += c[i];
-    }
-    uint64_t to = sum;
-    uint32_t nto = n;
+// Both at once, one value per thread.
+__device__ void scan_pair(unsigned long long *wave64, uint32_t *wave32, uint64_t v, uint32_t c, uint64_t *before, uint32_t *ranked,
+                          uint64_t *all, uint32_t *n) {
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    uint64_t sum = v;
+    uint32_t num = c;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t o = __shfl_up((unsigned long long)to, d);
-        const uint32_t p = __shfl_up(nto, d);
+        const uint64_t o = __shfl_up((unsigned long long)sum, d);
+        const uint32_t p = __shfl_up(num, d);
         if (lane >= d) {
-            to += o;
-            nto += p;
+            sum += o;
+            num += p;
         }
     }
-    Search r;
-    r.all = __shfl((unsigned long long)to, 63);
-    r.n = __shfl(nto, 63);
-    to -= sum;
-    nto -= n;
-#pragma unroll
-    for (int i = 0; i < kLaneBins; ++i) {  // m, c become sums up to the bin, itself included
-        before[at_bin(b0 + i)] = to;
-        ranked[at_bin(b0 + i)] = nto;
-        to += m[i];
-        nto += c[i];
-        m[i] = to;
-        c[i] = nto;
+    __syncthreads();
+    if (lane == 63) {
+        wave64[w] = sum;
+        wave32[w] = num;
     }
-    // (upto of a bin: before of the next; a wave's LDS accesses stay in order)
-    if (lane == 63) before[at_bin(kBins)] = to;
-    // The first bin with which the sum reaches x, the last one if none does.  (Its own weight is not zero then, or x is
-    // not above the sum before, and the first bin holds the first token.)
-    auto reaching = [&](double x) {
-        int b = kBins;
+    __syncthreads();
+    uint64_t b = 0, t = 0;
+    uint32_t r = 0, u = 0;
 #pragma unroll
-        for (int i = kLaneBins - 1; i >= 0; --i) b = (double)m[i] >= x ? b0 + i : b;
-        const uint64_t any = __ballot(b < kBins);
-        return any ? __shfl(b, __builtin_ctzll(any)) : kBins - 1;
-    };
-    auto counting = [&](uint32_t x) {
-        int b = kBins;
+    for (int i = 0; i < kSampleWaves; ++i) {
+        b += i < w ? wave64[i] : 0;
+        r += i < w ? wave32[i] : 0;
+        t += wave64[i];
+        u += wave32[i];
+    }
+    *before = b + sum - v;
+    *ranked = r + num - c;
+    *all = t;
+    *n = u;
+}
+
+// Tokens in ranges of bins, of the bins before b; lo and hi: ranges in ascending order that share no bin.
+__device__ __forceinline__ uint32_t listed_before(const int *lo, const int *hi, const uint32_t *ranked, int b) {
+    uint32_t n = 0;
 #pragma unroll
-        for (int i = kLaneBins - 1; i >= 0; --i) b = c[i] >= x ? b0 + i : b;
-        const uint64_t any = __ballot(b < kBins);
-        return any ? __shfl(b, __builtin_ctzll(any)) : kBins - 1;
+    for (int i = 0; i < 4; ++i) {
+        const int end = hi[i] + 1 < b ? hi[i] + 1 : b;
+        if (end > lo[i]) n += ranked[end] - ranked[lo[i]];
+    }
+    return n;
+}
+
+// Where a row's answers can lie, from the sums before its bins (before[kBins], ranked[kBins]: all), by one wave.
+struct Search {
+    int lo[4], hi[4], cut;  // bins
+};
+__device__ Search search(const Ask &k, const Grid &grid, float most, const unsigned long long *before, const uint32_t *ranked) {
+    const int lane = threadIdx.x & 63;
+    constexpr int kSkip = kBins / 64;
+    // The first bin for which `is` holds, as it does for all that follow; the last one if there is none.
+    auto first_bin = [&](auto is) {
+        const uint64_t some = __ballot(is(kSkip * lane + kSkip - 1));
+        const int b0 = some ? kSkip * __builtin_ctzll(some) : kBins - kSkip;
+        const uint64_t any = __ballot(lane < kSkip && is(b0 + (lane < kSkip ? lane : 0)));
+        return any ? b0 + __builtin_ctzll(any) : kBins - 1;
     };
+    // The first bin with which the sum reaches x.
+    auto reaching = [&](double x) { return first_bin([&](int b) { return (double)before[b + 1] >= x; }); };
     // Bounds of the sums are a little wide: a bin's weight has been rounded otherwise than the sum of its tokens'.
-    const double wide = 1.0 + 0x1p-30, all = (double)r.all;
+    const double wide = 1.0 + 0x1p-30, all = (double)before[kBins];
     double least = all, greatest = all;
+    Search r;
     auto bounds = [&](int i) {  // of a kept sum that ends in these bins
-        least = fmin(least, (double)before[at_bin(r.lo[i])]);
-        greatest = fmin(greatest, (double)before[at_bin(r.hi[i] + 1)]);
+        least = fmin(least, (double)before[r.lo[i]]);
+        greatest = fmin(greatest, (double)before[r.hi[i] + 1]);
     };
     for (int i = 0; i < 4; ++i) {
         r.lo[i] = kBins;
         r.hi[i] = -1;
     }
     r.cut = 0;
-    if (k.top_k > 0 && (uint32_t)k.top_k < r.n) {
-        r.lo[0] = r.hi[0] = counting((uint32_t)k.top_k);
+    if (k.top_k > 0 && (uint32_t)k.top_k < ranked[kBins]) {
+        r.lo[0] = r.hi[0] = first_bin([&](int b) { return ranked[b + 1] >= (uint32_t)k.top_k; });
         bounds(0);
     }
     if (!(k.top_p >= 1.0f)) {
@@ -428,29 +437,25 @@ __device__ Search search(const Ask &k, const Grid &grid, float most, const unsig
     r.lo[3] = reaching(fmax(u * least / wide - 2.0, 1.0));
     r.hi[3] = reaching(fmin(u * greatest * wide + 2.0, all));
     r.hi[3] = r.hi[3] > r.lo[3] ? r.hi[3] : r.lo[3];
-    uint32_t own[kLaneBins], wanted = 0;
+    // in ascending order, ranges that meet as one (the other empty, behind the last bin)
 #pragma unroll
-    for (int i = 0; i < kLaneBins; ++i) {
-        const int b = b0 + i;
-        bool is = false;
+    for (int pass = 0; pass < 3; ++pass)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) is |= b >= r.lo[j] && b <= r.hi[j];
-        own[i] = is ? c[i] - ranked[at_bin(b)] : 0u;
-        wanted += own[i];
-    }
-    uint32_t at = wanted;
+        for (int i = 0; i < 3; ++i) {
+            if (r.lo[i] <= r.lo[i + 1]) continue;
+            const int l = r.lo[i], h = r.hi[i];
+            r.lo[i] = r.lo[i + 1];
+            r.hi[i] = r.hi[i + 1];
+            r.lo[i + 1] = l;
+            r.hi[i + 1] = h;
+        }
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint32_t o = __shfl_up(at, d);
-        if (lane >= d) at += o;
-    }
-    r.listed = __shfl(at, 63);
-    at -= wanted;
-#pragma unroll
-    for (int i = 0; i < kLaneBins; ++i) {
-        first[at_bin(b0 + i)] = at;
-        at += own[i];
-    }
+    for (int i = 0; i < 3; ++i)
+        if (r.lo[i + 1] <= r.hi[i]) {  // the second becomes both, the first empty where it stands
+            r.hi[i + 1] = r.hi[i] > r.hi[i + 1] ? r.hi[i] : r.hi[i + 1];
+            r.lo[i + 1] = r.lo[i];
+            r.hi[i] = r.lo[i] - 1;
+        }
     return r;
 }
 
@@ -460,12 +465,13 @@ __device__ __forceinline__ void part_of(const SampleArgs &a, int part, int *i0, 
     *i1 = *i0 + a.part < a.V ? *i0 + a.part : a.V;
 }
 
-__global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(SampleArgs a) {
-    __shared__ Shared s;
-    __shared__ unsigned long long mass[kRoom], before[kRoom + 1];
-    __shared__ uint32_t count[kRoom], ranked[kRoom], first_of[kRoom];
+__global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleArgs a) {
+    __shared__ unsigned long long mass[kBins], before[kBins + 1], wave64[kSampleWaves];
+    __shared__ uint32_t count[kBins], ranked[kBins + 1], wave32[kSampleWaves];
     __shared__ unsigned long long heads[kMostParts];
     __shared__ double factors[kMostParts];
+    __shared__ int shifts[kMostParts];
+    __shared__ double roots[kRoots];
     __shared__ uint32_t last;
     __shared__ Search found;
     const int m = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x;
@@ -475,53 +481,63 @@ __global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(SampleArgs 
     int i0, i1;
     part_of(a, part, &i0, &i1);
 
-    uint64_t best = 0;
-    for (int b = i0; b < i1; b += kBlock) {
-        float l[8];
+    // The first block of logits stays in registers from here to the bins, others (of parts that have more) are read
+    // twice.
+    float l[8];
+    auto load = [&](int b, float (&to)[8]) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int i = b + j * kSampleThreads + tid;
-            l[j] = i < i1 ? row.logit(i) : -INFINITY;
+            to[j] = i < i1 ? row.logit(i) : -INFINITY;
         }
+    };
+    uint64_t best = 0;
+    auto look = [&](int b, const float (&at)[8]) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const uint32_t v = sort_word(l[j]);
+            const uint32_t v = sort_word(at[j]);
             const uint64_t key = v ? (uint64_t)v << 32 | (uint32_t)~(b + j * kSampleThreads + tid) : 0;
             best = key > best ? key : best;
         }
+    };
+    load(i0, l);
+    for (int b = i0 + kBlock; b < i1; b += kBlock) {
+        float more[8];
+        load(b, more);
+        look(b, more);
     }
-    const int my = at_bin(tid);
-    mass[my] = 0;
-    count[my] = 0;
-    best = over_block(s, best, Most64());
+    look(i0, l);
+    mass[tid] = 0;
+    count[tid] = 0;
+    if (tid < kRoots) roots[tid] = kRoot[tid];
+    best = over_block(wave64, best, Most64());
     const uint32_t top_word = (uint32_t)(best >> 32);
     const bool ordinary = k.temperature > 0.0f;  // (else the first token is the answer)
     const float steps = Grid::steps_of(k.temperature);
     if (ordinary && top_word) {
         const float most = of_sort_word(top_word);
-        const Weights w(most, k.temperature);
+        const Weights w(most, k.temperature, roots);
         const Grid grid = {steps, Grid::number(most, steps)};
-        for (int b = i0; b < i1; b += kBlock) {
-            float l[8];
+        auto add = [&](const float (&at)[8]) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int i = b + j * kSampleThreads + tid;
-                l[j] = i < i1 ? row.logit(i) : -INFINITY;
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (!(l[j] > -INFINITY)) continue;
-                const int bin = at_bin(grid.bin(l[j]));
+                if (!(at[j] > -INFINITY)) continue;
+                const int bin = grid.bin(at[j]);
                 atomicAdd(&count[bin], 1u);
-                atomicAdd(&mass[bin], (unsigned long long)w.of(l[j]));
+                atomicAdd(&mass[bin], (unsigned long long)w.of(at[j]));
             }
+        };
+        add(l);
+        for (int b = i0 + kBlock; b < i1; b += kBlock) {
+            load(b, l);
+            add(l);
         }
     }
     __syncthreads();
     if (a.parts > 1) {
         PartBins &to = a.bins[(int64_t)m * a.parts + part];
-        put64(&to.mass[tid], mass[my]);
-        put32(&to.count[tid], count[my]);
+        put64(reinterpret_cast<unsigned long long *>(&to.mass[tid]), (uint64_t)__double_as_longlong((double)mass[tid]));
+        put32(&to.count[tid], count[tid]);
         if (tid == 0) put64(&a.heads[(int64_t)m * a.parts + part].best, best);
         __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): written through to where all XCDs see it
         __syncthreads();
@@ -548,50 +564,82 @@ __global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(SampleArgs 
     }
     const Grid grid = {steps, Grid::number(most, steps)};
     if (a.parts > 1) {
-        mass[my] = 0;
-        count[my] = 0;
-        // a part's weights, relative to the row's largest
-        if (tid < a.parts) factors[tid] = exp(((double)of_sort_word((uint32_t)(heads[tid] >> 32)) - (double)most) / (double)k.temperature);
+        // A part's weights, relative to the row's largest; its bins, so many places further down.
+        if (tid < a.parts) {
+            const uint32_t top = (uint32_t)(heads[tid] >> 32);
+            factors[tid] = top ? exp(((double)of_sort_word(top) - (double)most) / (double)k.temperature) : 0.0;
+            shifts[tid] = top ? (int)fminf(grid.top - Grid::number(of_sort_word(top), steps), (float)kBins) : kBins;
+        }
         __syncthreads();
+        double sum = 0.0;
+        uint32_t num = 0, rest = 0;
         for (int p0 = 0; p0 < a.parts; p0 += 8) {
-            uint64_t ms[8];
+            double ms[8];
             uint32_t cs[8];
 #pragma unroll
             for (int p = 0; p < 8; ++p) {
-                const PartBins &from = a.bins[(int64_t)m * a.parts + (p0 + p < a.parts ? p0 + p : 0)];
-                ms[p] = get64(&from.mass[tid]);
+                const int part = p0 + p < a.parts ? p0 + p : 0, b = tid - shifts[part];
+                const PartBins &from = a.bins[(int64_t)m * a.parts + part];
+                ms[p] = __longlong_as_double((long long)get64(reinterpret_cast<const unsigned long long *>(&from.mass[b > 0 ? b : 0])));
+                cs[p] = get32(&from.count[b > 0 ? b : 0]);
+            }
+#pragma unroll
+            for (int p = 0; p < 8; ++p) {
+                if (p0 + p >= a.parts || tid < shifts[p0 + p]) continue;
+                sum += factors[p0 + p] * ms[p];
+                num += cs[p];
+            }
+        }
+        mass[tid] = (unsigned long long)sum;
+        count[tid] = num;
+        __syncthreads();
+        // What a shift has moved past the last bin belongs to it.
+        sum = 0.0;
+        for (int p0 = 0; p0 < a.parts; p0 += 8) {
+            double ms[8];
+            uint32_t cs[8];
+#pragma unroll
+            for (int p = 0; p < 8; ++p) {
+                cs[p] = 0;
+                ms[p] = 0.0;
+                if (p0 + p >= a.parts || shifts[p0 + p] == 0 || tid + shifts[p0 + p] < kBins) continue;
+                const PartBins &from = a.bins[(int64_t)m * a.parts + p0 + p];
+                ms[p] = __longlong_as_double((long long)get64(reinterpret_cast<const unsigned long long *>(&from.mass[tid])));
                 cs[p] = get32(&from.count[tid]);
             }
 #pragma unroll
             for (int p = 0; p < 8; ++p) {
-                if (p0 + p >= a.parts || cs[p] == 0) continue;
-                const float top = of_sort_word((uint32_t)(heads[p0 + p] >> 32));
-                const float shift = grid.top - Grid::number(top, steps);
-                const int bin = at_bin((int)fminf(shift + (float)tid, (float)(kBins - 1)));
-                atomicAdd(&count[bin], cs[p]);
-                atomicAdd(&mass[bin], (unsigned long long)(factors[p0 + p] * (double)ms[p]));
+                rest += cs[p];
+                if (cs[p]) sum += factors[p0 + p] * ms[p];
             }
+        }
+        if (rest) {
+            atomicAdd(&count[kBins - 1], rest);
+            atomicAdd(&mass[kBins - 1], (unsigned long long)sum);
         }
         __syncthreads();
     }
+    uint64_t own_before, all;
+    uint32_t own_ranked, n;
+    scan_pair(wave64, wave32, mass[tid], count[tid], &own_before, &own_ranked, &all, &n);
+    before[tid] = own_before;
+    ranked[tid] = own_ranked;
+    if (tid == 0) {
+        before[kBins] = all;
+        ranked[kBins] = n;
+    }
+    __syncthreads();
     if (tid < 64) {
-        const Search r = search(k, grid, most, mass, count, before, ranked, first_of);
+        const Search r = search(k, grid, most, before, ranked);
         if (tid == 0) found = r;
     }
     __syncthreads();
-    if (found.listed > (uint32_t)kList || !(fabsf(grid.top) < kFar)) {  // (the same for the whole row)
-        const int id = choose_slowly(s, row, k, most, found.n);
-        if (tid == 0) {
-            a.ids[m] = id;
-            state.gather = 0;
-        }
-        return;
-    }
-    state.before[tid] = before[my];
-    state.ranked[tid] = ranked[my];
-    state.first[tid] = first_of[my];
+    const uint32_t listed = listed_before(found.lo, found.hi, ranked, kBins);
+    state.before[tid] = own_before;
+    state.ranked[tid] = own_ranked;
     if (tid == 0) {
-        state.gather = 1;
+        state.ranked[kBins] = n;
+        state.gather = listed > (uint32_t)kList || !(fabsf(grid.top) < kFar) ? 2 : 1;
         state.listed = 0;
         state.arrived = 0;
         state.steps = steps;
@@ -601,22 +649,161 @@ __global__ __launch_bounds__(kSampleThreads) void sample_bins_kernel(SampleArgs 
             state.lo[i] = found.lo[i];
             state.hi[i] = found.hi[i];
         }
-        state.all = found.all;
-        state.count = found.n;
+        state.all = all;
+        state.count = n;
         state.cut = found.cut;
     }
+}
+
+// The answer from the n listed tokens, by the first W waves, which are all that is left of the workgroup (kEach tokens to
+// a thread).  key, sum: room for kList each.
+template <int W, int kEach>
+__device__ int finish(const RowState &state, const Ask &k, const Grid &grid, const int (&lo)[4], const int (&hi)[4], int n,
+                      unsigned long long *key, unsigned long long *sum, unsigned long long *wave64, uint32_t *wave32, uint32_t *found,
+                      unsigned long long *kept_at) {
+    constexpr int kThreads = 64 * W, kSlots = kThreads * kEach;
+    const int tid = threadIdx.x;
+    // Before the keys are in order: tokens per slot, and of the slots before.  Before the sums: keys by slot.
+    uint32_t *const count = reinterpret_cast<uint32_t *>(key), *const begin = count + kSlots;
+    // Sorted by interpolation: a bin's tokens have as many slots as they are, a logit's slot goes by its place within the
+    // bin, and the few that share one (equal logits among them) are ranked by counting.
+    uint64_t mine[kEach];
+    uint32_t slot[kEach], nth[kEach];
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+        const int i = q * kThreads + tid;
+        mine[q] = i < n ? get64(&state.list[i]) : 0;
+        count[i] = 0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+        if (q * kThreads + tid >= n) continue;
+        const float l = of_sort_word((uint32_t)(mine[q] >> 32));
+        const int b = grid.bin(l);
+        const uint32_t from = listed_before(lo, hi, state.ranked, b), room = state.ranked[b + 1] - state.ranked[b];
+        const float v = l * grid.steps, down = b + 1 < kBins ? floorf(v) + 1.0f - v : 0.0f;  // (0, 1]; the last bin: one slot
+        const uint32_t in = (uint32_t)(down * (float)room);
+        slot[q] = from + (in < room ? in : room - 1);
+        nth[q] = atomicAdd(&count[slot[q]], 1u);
+    }
+    __syncthreads();
+    {
+        uint32_t c[kEach], sum4 = 0, all;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            c[q] = count[kEach * tid + q];
+            sum4 += c[q];
+        }
+        uint32_t at = scan_block<W>(wave32, sum4, &all);
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            begin[kEach * tid + q] = at;
+            at += c[q];
+        }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kEach; ++q)
+        if (q * kThreads + tid < n) sum[begin[slot[q]] + nth[q]] = mine[q];
+    __syncthreads();
+    uint32_t to[kEach];
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+        if (q * kThreads + tid >= n) continue;
+        const uint32_t j0 = begin[slot[q]], j1 = j0 + count[slot[q]];
+        to[q] = j0;
+        for (uint32_t j = j0; j < j1; ++j) to[q] += sum[j] > mine[q];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kEach; ++q)
+        if (q * kThreads + tid < n) key[to[q]] = mine[q];
+    __syncthreads();
+    // Per token: its weight, the sum of the weights up to it (itself included) in the row, and its rank there.
+    const Weights w(state.most, k.temperature, kRoot);
+    uint64_t weight[kEach], upto[kEach], carry = 0;
+    uint32_t rank[kEach];
+    int bin[kEach];
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+        weight[q] = 0;
+        if (q * kThreads >= n) continue;
+        const int i = q * kThreads + tid;
+        if (i < n) weight[q] = w.of_word((uint32_t)(key[i] >> 32));
+        unsigned long long all;
+        const uint64_t at = scan_block<W>(wave64, (unsigned long long)weight[q], &all);
+        if (i < n) sum[i] = carry + at;
+        carry += all;
+    }
+    if (tid < 3) found[tid] = ~0u;
+    if (tid == 0) *kept_at = state.all;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < kEach; ++q) {
+        const int i = q * kThreads + tid;
+        if (i >= n) continue;
+        bin[q] = grid.bin(of_sort_word((uint32_t)(key[i] >> 32)));
+        const uint32_t first = listed_before(lo, hi, state.ranked, bin[q]);
+        upto[q] = state.before[bin[q]] + (sum[i] + weight[q] - sum[first]);
+        rank[q] = state.ranked[bin[q]] + ((uint32_t)i - first);
+    }
+    // The first token for which `is` holds, as it does for all behind it; n if there is none.  `at`: a word of LDS.
+    auto first_token = [&](uint32_t *at, auto is) {
+#pragma unroll
+        for (int q = 0; q < kEach; ++q) {
+            const uint64_t any = __ballot(q * kThreads + tid < n && is(q));
+            if (any && (tid & 63) == 0) atomicMin(at, (uint32_t)(q * kThreads + tid + __builtin_ctzll(any)));
+        }
+        __syncthreads();
+        return *at < (uint32_t)n ? (int)*at : n;
+    };
+    // The sum of the weights with which a token is reached: by the thread that has it.
+    auto keep = [&](uint64_t v) { if (v < *kept_at) *kept_at = v; };
+    if (k.top_k > 0 && (uint32_t)k.top_k < state.count) {
+#pragma unroll
+        for (int q = 0; q < kEach; ++q)
+            if (q * kThreads + tid < n && rank[q] == (uint32_t)k.top_k - 1) keep(upto[q]);
+        __syncthreads();
+    }
+    if (!(k.top_p >= 1.0f)) {
+        const uint64_t reach = reach_of(k.top_p, *kept_at);
+        const int i = first_token(&found[0], [&](int q) { return upto[q] >= reach; });
+#pragma unroll
+        for (int q = 0; q < kEach; ++q)
+            if (q * kThreads + tid == i) keep(upto[q]);
+        __syncthreads();
+    }
+    if (k.min_p > 0.0f) {
+        // (of the bins from `cut` on; before them all have the weight)
+        const int i = first_token(&found[1], [&](int q) { return bin[q] >= state.cut && !((double)weight[q] >= (double)k.min_p * kOne); });
+        if (i == 0 && tid == 0) keep(state.before[state.cut]);
+#pragma unroll
+        for (int q = 0; q < kEach; ++q)
+            if (q * kThreads + tid == i - 1) keep(bin[q] >= state.cut ? upto[q] : state.before[state.cut]);
+        __syncthreads();
+    }
+    const uint64_t kept = *kept_at < 1ull << kPoint ? 1ull << kPoint : *kept_at;  // (the first token's weight is 1)
+    const uint64_t x = point_of(k.u, kept);
+    const int i = first_token(&found[2], [&](int q) { return upto[q] > x; });
+    return (int)~(uint32_t)key[i < n ? i : n - 1];
 }
 
 __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs a) {
     __shared__ unsigned long long key[kList], sum[kList], wave64[kSampleWaves];
     __shared__ uint32_t wave32[kSampleWaves], shared_at, last;
-    // Before the keys are in order: tokens per slot, and of the slots before.  Before the sums: keys by slot.
-    uint32_t *const count = reinterpret_cast<uint32_t *>(key), *const begin = count + kList;
-    __shared__ unsigned long long found[3];
+    __shared__ unsigned long long kept;
+    __shared__ uint32_t found[3];
     const int m = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x;
     RowState &state = a.rows[m];
-    if (!state.gather) return;
+    const uint32_t gather = state.gather;
+    if (gather == 0 || (gather == 2 && part > 0)) return;
     const Row row = row_of(a, m);
+    if (gather == 2) {  // (the second launch has the registers: in the first they would halve its workgroups)
+        const int id = choose_slowly(*reinterpret_cast<Shared *>(key), row, ask_of(a, m), state.most, state.count);
+        if (tid == 0) a.ids[m] = id;
+        return;
+    }
     const Grid grid = {state.steps, state.top};
     int lo[4], hi[4];
 #pragma unroll
@@ -643,7 +830,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs 
             hits |= is && bin < kBins ? 1u << j : 0u;
         }
         uint32_t all;
-        uint32_t at = scan_block(wave32, (uint32_t)__builtin_popcount(hits), &all);
+        uint32_t at = scan_block<kSampleWaves>(wave32, (uint32_t)__builtin_popcount(hits), &all);
         if (tid == 0 && all) shared_at = __hip_atomic_fetch_add(&state.listed, all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
         at += shared_at;
@@ -658,129 +845,18 @@ __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs 
     __syncthreads();
     if (!last) return;
 
-    const Ask k = ask_of(a, m);
     const int n = (int)get32(&state.listed) < kList ? (int)get32(&state.listed) : kList;
-    // Sorted by interpolation: a bin's tokens have as many slots as they are, a logit's slot goes by its place within the
-    // bin, and the few that share one (equal logits among them) are ranked by counting.
-    constexpr int kEach = kList / kSampleThreads;
-    uint64_t mine[kEach];
-    uint32_t slot[kEach], nth[kEach];
-#pragma unroll
-    for (int q = 0; q < kEach; ++q) {
-        const int i = q * kSampleThreads + tid;
-        mine[q] = i < n ? get64(&state.list[i]) : 0;
-        count[i] = 0;
+    // By as few waves as hold the tokens: the others have ended, so that barriers wait for few.
+    int id = 0;
+    const Ask k = ask_of(a, m);
+    if (n <= 64) {
+        if (tid < 64) id = finish<1, 1>(state, k, grid, lo, hi, n, key, sum, wave64, wave32, found, &kept);
+    } else if (n <= 256) {
+        if (tid < 256) id = finish<4, 1>(state, k, grid, lo, hi, n, key, sum, wave64, wave32, found, &kept);
+    } else {
+        id = finish<kSampleWaves, kList / kSampleThreads>(state, k, grid, lo, hi, n, key, sum, wave64, wave32, found, &kept);
     }
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < kEach; ++q) {
-        if (q * kSampleThreads + tid >= n) continue;
-        const float l = of_sort_word((uint32_t)(mine[q] >> 32));
-        const int b = grid.bin(l);
-        const uint32_t from = state.first[b], room = (b + 1 < kBins ? state.first[b + 1] : (uint32_t)n) - from;
-        const float v = l * grid.steps, down = b + 1 < kBins ? floorf(v) + 1.0f - v : 0.0f;  // (0, 1]; the last bin: one slot
-        const uint32_t in = (uint32_t)(down * (float)room);
-        slot[q] = from + (in < room ? in : room - 1);
-        nth[q] = atomicAdd(&count[slot[q]], 1u);
-    }
-    __syncthreads();
-    {
-        uint32_t c[kEach], sum4 = 0, all;
-#pragma unroll
-        for (int q = 0; q < kEach; ++q) {
-            c[q] = count[kEach * tid + q];
-            sum4 += c[q];
-        }
-        uint32_t at = scan_block(wave32, sum4, &all);
-#pragma unroll
-        for (int q = 0; q < kEach; ++q) {
-            begin[kEach * tid + q] = at;
-            at += c[q];
-        }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < kEach; ++q)
-        if (q * kSampleThreads + tid < n) sum[begin[slot[q]] + nth[q]] = mine[q];
-    __syncthreads();
-    uint32_t to[kEach];
-#pragma unroll
-    for (int q = 0; q < kEach; ++q) {
-        if (q * kSampleThreads + tid >= n) continue;
-        const uint32_t j0 = begin[slot[q]], j1 = j0 + count[slot[q]];
-        to[q] = j0;
-        for (uint32_t j = j0; j < j1; ++j) to[q] += sum[j] > mine[q];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < kEach; ++q)
-        if (q * kSampleThreads + tid < n) key[to[q]] = mine[q];
-    __syncthreads();
-    // Per token: its weight, the sum of the weights up to it (itself included) in the row, and its rank there.
-    const Weights w(state.most, k.temperature);
-    uint64_t weight[kEach], upto[kEach], carry = 0;
-    uint32_t rank[kEach];
-    int bin[kEach];
-#pragma unroll
-    for (int q = 0; q < kEach; ++q) {
-        weight[q] = 0;
-        if (q * kSampleThreads >= n) continue;
-        const int i = q * kSampleThreads + tid;
-        if (i < n) weight[q] = w.of_word((uint32_t)(key[i] >> 32));
-        unsigned long long all;
-        const uint64_t at = scan_block(wave64, (unsigned long long)weight[q], &all);
-        if (i < n) sum[i] = carry + at;
-        carry += all;
-    }
-    if (tid < 3) found[tid] = ~0ull;
-    if (tid == 0) last = ~0u;
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < kEach; ++q) {
-        const int i = q * kSampleThreads + tid;
-        if (i >= n) continue;
-        bin[q] = grid.bin(of_sort_word((uint32_t)(key[i] >> 32)));
-        const uint32_t first = state.first[bin[q]];
-        upto[q] = state.before[bin[q]] + (sum[i] + weight[q] - sum[first]);
-        rank[q] = state.ranked[bin[q]] + ((uint32_t)i - first);
-    }
-    auto each = [&](auto f) {
-#pragma unroll
-        for (int q = 0; q < kEach; ++q)
-            if (q * kSampleThreads + tid < n) f(q);
-    };
-    uint64_t kept = state.all;
-    if (k.top_k > 0 && (uint32_t)k.top_k < state.count) {
-        each([&](int q) {
-            if (rank[q] == (uint32_t)k.top_k - 1) found[0] = upto[q];
-        });
-        __syncthreads();
-        kept = found[0] < kept ? found[0] : kept;
-    }
-    if (!(k.top_p >= 1.0f)) {
-        const uint64_t reach = reach_of(k.top_p, kept);
-        each([&](int q) {
-            if (upto[q] >= reach) atomicMin(&found[1], (unsigned long long)upto[q]);
-        });
-        __syncthreads();
-        kept = found[1] < kept ? found[1] : kept;
-    }
-    if (k.min_p > 0.0f) {
-        if (tid == 0) found[2] = state.before[state.cut];
-        __syncthreads();
-        each([&](int q) {
-            if (bin[q] >= state.cut && (double)weight[q] >= (double)k.min_p * kOne) atomicMax(&found[2], (unsigned long long)upto[q]);
-        });
-        __syncthreads();
-        kept = found[2] < kept ? found[2] : kept;
-    }
-    kept = kept < 1ull << kPoint ? 1ull << kPoint : kept;  // (the first token's weight is 1)
-    const uint64_t x = point_of(k.u, kept);
-    each([&](int q) {
-        if (upto[q] > x) atomicMin(&last, (uint32_t)(q * kSampleThreads + tid));
-    });
-    __syncthreads();
-    if (tid == 0) a.ids[m] = (int)~(uint32_t)key[last < (uint32_t)n ? last : (uint32_t)n - 1];
+    if (tid == 0) a.ids[m] = id;
 }
 
 // Parts of a row: blocks of kBlock logits, as many workgroups in all as fill the device a few times over.
