@@ -571,51 +571,44 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleAr
             shifts[tid] = top ? (int)fminf(grid.top - Grid::number(of_sort_word(top), steps), (float)kBins) : kBins;
         }
         __syncthreads();
-        double sum = 0.0;
+        // A part's bin that comes to stand at this thread's, and this thread's bin of the part where the shift moves it past
+        // the last one, to which it belongs.
+        double sum = 0.0, past = 0.0;
         uint32_t num = 0, rest = 0;
         for (int p0 = 0; p0 < a.parts; p0 += 8) {
-            double ms[8];
-            uint32_t cs[8];
+            double ms[8], mp[8];
+            uint32_t cs[8], cp[8];
 #pragma unroll
             for (int p = 0; p < 8; ++p) {
-                const int part = p0 + p < a.parts ? p0 + p : 0, b = tid - shifts[part];
+                const bool in = p0 + p < a.parts;
+                const int part = in ? p0 + p : 0, shift = shifts[part];
                 const PartBins &from = a.bins[(int64_t)m * a.parts + part];
-                ms[p] = __longlong_as_double((long long)get64(reinterpret_cast<const unsigned long long *>(&from.mass[b > 0 ? b : 0])));
-                cs[p] = get32(&from.count[b > 0 ? b : 0]);
+                ms[p] = mp[p] = 0.0;
+                cs[p] = cp[p] = 0;
+                if (in && tid >= shift) {
+                    ms[p] = __longlong_as_double((long long)get64(reinterpret_cast<const unsigned long long *>(&from.mass[tid - shift])));
+                    cs[p] = get32(&from.count[tid - shift]);
+                }
+                if (in && shift > 0 && tid + shift >= kBins) {
+                    mp[p] = __longlong_as_double((long long)get64(reinterpret_cast<const unsigned long long *>(&from.mass[tid])));
+                    cp[p] = get32(&from.count[tid]);
+                }
             }
 #pragma unroll
             for (int p = 0; p < 8; ++p) {
-                if (p0 + p >= a.parts || tid < shifts[p0 + p]) continue;
-                sum += factors[p0 + p] * ms[p];
+                const double f = factors[p0 + p < a.parts ? p0 + p : 0];
+                sum += f * ms[p];
                 num += cs[p];
+                past += f * mp[p];
+                rest += cp[p];
             }
         }
         mass[tid] = (unsigned long long)sum;
         count[tid] = num;
         __syncthreads();
-        // What a shift has moved past the last bin belongs to it.
-        sum = 0.0;
-        for (int p0 = 0; p0 < a.parts; p0 += 8) {
-            double ms[8];
-            uint32_t cs[8];
-#pragma unroll
-            for (int p = 0; p < 8; ++p) {
-                cs[p] = 0;
-                ms[p] = 0.0;
-                if (p0 + p >= a.parts || shifts[p0 + p] == 0 || tid + shifts[p0 + p] < kBins) continue;
-                const PartBins &from = a.bins[(int64_t)m * a.parts + p0 + p];
-                ms[p] = __longlong_as_double((long long)get64(reinterpret_cast<const unsigned long long *>(&from.mass[tid])));
-                cs[p] = get32(&from.count[tid]);
-            }
-#pragma unroll
-            for (int p = 0; p < 8; ++p) {
-                rest += cs[p];
-                if (cs[p]) sum += factors[p0 + p] * ms[p];
-            }
-        }
         if (rest) {
             atomicAdd(&count[kBins - 1], rest);
-            atomicAdd(&mass[kBins - 1], (unsigned long long)sum);
+            atomicAdd(&mass[kBins - 1], (unsigned long long)past);
         }
         __syncthreads();
     }
@@ -660,7 +653,7 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleAr
 template <int W, int kEach>
 __device__ int finish(const RowState &state, const Ask &k, const Grid &grid, const int (&lo)[4], const int (&hi)[4], int n,
                       unsigned long long *key, unsigned long long *sum, unsigned long long *wave64, uint32_t *wave32, uint32_t *found,
-                      unsigned long long *kept_at) {
+                      unsigned long long *kept_at, const unsigned long long *before, const uint32_t *ranked, const double *roots) {
     constexpr int kThreads = 64 * W, kSlots = kThreads * kEach;
     const int tid = threadIdx.x;
     // Before the keys are in order: tokens per slot, and of the slots before.  Before the sums: keys by slot.
@@ -681,7 +674,7 @@ __device__ int finish(const RowState &state, const Ask &k, const Grid &grid, con
         if (q * kThreads + tid >= n) continue;
         const float l = of_sort_word((uint32_t)(mine[q] >> 32));
         const int b = grid.bin(l);
-        const uint32_t from = listed_before(lo, hi, state.ranked, b), room = state.ranked[b + 1] - state.ranked[b];
+        const uint32_t from = listed_before(lo, hi, ranked, b), room = ranked[b + 1] - ranked[b];
         const float v = l * grid.steps, down = b + 1 < kBins ? floorf(v) + 1.0f - v : 0.0f;  // (0, 1]; the last bin: one slot
         const uint32_t in = (uint32_t)(down * (float)room);
         slot[q] = from + (in < room ? in : room - 1);
@@ -721,7 +714,7 @@ __device__ int finish(const RowState &state, const Ask &k, const Grid &grid, con
         if (q * kThreads + tid < n) key[to[q]] = mine[q];
     __syncthreads();
     // Per token: its weight, the sum of the weights up to it (itself included) in the row, and its rank there.
-    const Weights w(state.most, k.temperature, kRoot);
+    const Weights w(state.most, k.temperature, roots);
     uint64_t weight[kEach], upto[kEach], carry = 0;
     uint32_t rank[kEach];
     int bin[kEach];
@@ -744,9 +737,9 @@ __device__ int finish(const RowState &state, const Ask &k, const Grid &grid, con
         const int i = q * kThreads + tid;
         if (i >= n) continue;
         bin[q] = grid.bin(of_sort_word((uint32_t)(key[i] >> 32)));
-        const uint32_t first = listed_before(lo, hi, state.ranked, bin[q]);
-        upto[q] = state.before[bin[q]] + (sum[i] + weight[q] - sum[first]);
-        rank[q] = state.ranked[bin[q]] + ((uint32_t)i - first);
+        const uint32_t first = listed_before(lo, hi, ranked, bin[q]);
+        upto[q] = before[bin[q]] + (sum[i] + weight[q] - sum[first]);
+        rank[q] = ranked[bin[q]] + ((uint32_t)i - first);
     }
     // The first token for which `is` holds, as it does for all behind it; n if there is none.  `at`: a word of LDS.
     auto first_token = [&](uint32_t *at, auto is) {
@@ -777,10 +770,10 @@ __device__ int finish(const RowState &state, const Ask &k, const Grid &grid, con
     if (k.min_p > 0.0f) {
         // (of the bins from `cut` on; before them all have the weight)
         const int i = first_token(&found[1], [&](int q) { return bin[q] >= state.cut && !((double)weight[q] >= (double)k.min_p * kOne); });
-        if (i == 0 && tid == 0) keep(state.before[state.cut]);
+        if (i == 0 && tid == 0) keep(before[state.cut]);
 #pragma unroll
         for (int q = 0; q < kEach; ++q)
-            if (q * kThreads + tid == i - 1) keep(bin[q] >= state.cut ? upto[q] : state.before[state.cut]);
+            if (q * kThreads + tid == i - 1) keep(bin[q] >= state.cut ? upto[q] : before[state.cut]);
         __syncthreads();
     }
     const uint64_t kept = *kept_at < 1ull << kPoint ? 1ull << kPoint : *kept_at;  // (the first token's weight is 1)
@@ -792,15 +785,17 @@ __device__ int finish(const RowState &state, const Ask &k, const Grid &grid, con
 __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs a) {
     __shared__ unsigned long long key[kList], sum[kList], wave64[kSampleWaves];
     __shared__ uint32_t wave32[kSampleWaves], shared_at, last;
-    __shared__ unsigned long long kept;
-    __shared__ uint32_t found[3];
+    __shared__ unsigned long long kept, before[kBins];
+    __shared__ uint32_t found[3], ranked[kBins + 1];
+    __shared__ double roots[kRoots];
     const int m = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x;
     RowState &state = a.rows[m];
     const uint32_t gather = state.gather;
     if (gather == 0 || (gather == 2 && part > 0)) return;
     const Row row = row_of(a, m);
+    const Ask k = ask_of(a, m);
     if (gather == 2) {  // (the second launch has the registers: in the first they would halve its workgroups)
-        const int id = choose_slowly(*reinterpret_cast<Shared *>(key), row, ask_of(a, m), state.most, state.count);
+        const int id = choose_slowly(*reinterpret_cast<Shared *>(key), row, k, state.most, state.count);
         if (tid == 0) a.ids[m] = id;
         return;
     }
@@ -811,6 +806,11 @@ __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs 
         lo[i] = state.lo[i];
         hi[i] = state.hi[i];
     }
+    // (what the last workgroup looks up: asked for by all, beside their logits)
+    before[tid] = state.before[tid];
+    ranked[tid] = state.ranked[tid];
+    if (tid == 0) ranked[kBins] = state.ranked[kBins];
+    if (tid < kRoots) roots[tid] = kRoot[tid];
     int i0, i1;
     part_of(a, part, &i0, &i1);
     for (int b = i0; b < i1; b += kBlock) {
@@ -848,13 +848,12 @@ __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs 
     const int n = (int)get32(&state.listed) < kList ? (int)get32(&state.listed) : kList;
     // By as few waves as hold the tokens: the others have ended, so that barriers wait for few.
     int id = 0;
-    const Ask k = ask_of(a, m);
     if (n <= 64) {
-        if (tid < 64) id = finish<1, 1>(state, k, grid, lo, hi, n, key, sum, wave64, wave32, found, &kept);
+        if (tid < 64) id = finish<1, 1>(state, k, grid, lo, hi, n, key, sum, wave64, wave32, found, &kept, before, ranked, roots);
     } else if (n <= 256) {
-        if (tid < 256) id = finish<4, 1>(state, k, grid, lo, hi, n, key, sum, wave64, wave32, found, &kept);
+        if (tid < 256) id = finish<4, 1>(state, k, grid, lo, hi, n, key, sum, wave64, wave32, found, &kept, before, ranked, roots);
     } else {
-        id = finish<kSampleWaves, kList / kSampleThreads>(state, k, grid, lo, hi, n, key, sum, wave64, wave32, found, &kept);
+        id = finish<kSampleWaves, kList / kSampleThreads>(state, k, grid, lo, hi, n, key, sum, wave64, wave32, found, &kept, before, ranked, roots);
     }
     if (tid == 0) a.ids[m] = id;
 }
