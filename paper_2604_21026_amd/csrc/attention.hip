@@ -8,9 +8,9 @@
 //                 lane row kb = lane / 16 gets the scores of tokens 8 kb .. 8 kb + 7
 //   O^T = V^T P^T the weights P as they come out of S^T: lane row kb multiplies tokens 8 kb .. 8 kb + 7, which is what
 //                 one 16-byte piece of the value layout holds for a channel
-// P enters as three bf16 values whose sum it is: the products are a twentieth of the time that the bytes take, so more
-// of them cost nothing, and results keep the precision of fp32.  The products with the first and with the rest are
-// summed apart and added at the end: what an infinite value makes of the rest (zero times infinity, or the other sign)
+// P enters as bf16 values whose sum it is: three of them (all 24 bits) where results leave as fp32, two (2^-17 of a weight is
+// left out) where they are rounded to bf16, 2^-9, themselves.  The products with the first and with the rest are summed
+// apart and added at the end: what an infinite value makes of the rest (zero times infinity, or the other sign)
 // is left out there.
 #include "cache.h"
 #include "mfma_act.h"
@@ -21,6 +21,7 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kStep = 32, kHeadTile = 16;
+constexpr int kMaxGroups = 256;
 
 struct AttentionArgs {
     CacheView c;
@@ -57,18 +58,24 @@ __device__ __forceinline__ Span span_of(const AttentionArgs &a, int b) {
 
 // What a wave holds of one sequence and head tile: m and l per lane (l of the lane's own tokens), O^T in tiles of 16
 // channels.
-template <int D>
+template <int D, bool E4M3>
 struct State {
+    static constexpr bool kApart = !E4M3;  // (the 8-bit format has no infinities)
     float m, l;
-    float4v o[D / 16], rest[D / 16];  // of the weights' first values and of the rest
+    float4v o[D / 16], rest[kApart ? D / 16 : 1];  // of the weights' first values and of the rest
     __device__ void clear() {
         m = -INFINITY;
         l = 0.0f;
 #pragma unroll
-        for (int i = 0; i < D / 16; ++i) o[i] = rest[i] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+        for (int i = 0; i < D / 16; ++i) {
+            o[i] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+            if (kApart) rest[i] = o[i];
+        }
     }
+    // Where the products with the rest of the weights are summed.
+    __device__ float4v &small(int i) { return kApart ? rest[kApart ? i : 0] : o[i]; }
     __device__ float sum(int tile, int r) const {
-        return __builtin_isfinite(o[tile][r]) ? o[tile][r] + rest[tile][r] : o[tile][r];
+        return kApart && __builtin_isfinite(o[tile][r]) ? o[tile][r] + rest[kApart ? tile : 0][r] : o[tile][r];
     }
 };
 
@@ -117,45 +124,60 @@ struct Piece<true> {
     }
 };
 
-// Steps `step` .. `step + count - 1` (of the sequence's tokens from 0) into st.  Keys of the next step are asked for
-// as soon as the products have taken this step's, values likewise, and the pages two steps ahead.
+// Loads stay on their side of this.  (The compiler moved the values' up to the keys', into registers of their own that it
+// waited for and copied at the loop's end.)
+__device__ __forceinline__ void keep_order() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Keys and values of a step on their way to a wave.
+template <int D, bool E4M3>
+struct Fetch {
+    typename Piece<E4M3>::raw k[2][D / 32], v[D / 16];
+    uint2v key_scales, value_scales;
+    bool value_ok;  // the lane's block of eight tokens has a page
+};
+
+// Steps `step` .. `step + count - 1` (of the sequence's tokens from 0; at least one) into st.  Keys of the next step are
+// asked for as soon as the products have taken this step's, values likewise, and pages a step before that.
 template <int D, bool E4M3>
 __device__ __forceinline__ void attend(const AttentionArgs &a, int b, int head, int tile, const Span &sp, int step, int count,
-                                       State<D> &st) {
+                                       State<D, E4M3> &st) {
     typedef Piece<E4M3> P;
     constexpr int C = D / 32, T = D / 16;
     const int lane = threadIdx.x & 63, n = lane & 15, kb = lane >> 4;
     const int heads = a.group - kHeadTile * tile < kHeadTile ? a.group - kHeadTile * tile : kHeadTile;
     const int32_t *const table = a.table + (int64_t)b * a.width;
-    // A lane reads keys of the step's block n / 4 of eight tokens (its tile rows' own) and values of block kb.
+    // A lane reads keys of the step's block n / 4 of eight tokens (its tile rows' own) and values of block kb.  No load
+    // stands behind a branch: where one does, the compiler waits for all of them at the loop's end, and a step takes the
+    // memory's latency (27 of 104 us at 131072 tokens).  So a number is looked up for every block, past the last one the
+    // last one's, and what it is worth is decided where it is used; past the last step the last one is read again.
     auto page_of = [&](int s, int block) {
         const int t = kStep * s + 8 * block;
-        return t < sp.end ? table[t >> a.c.page_shift] : -1;
+        return *as_global<int32_t>(table + ((t < sp.end ? t : sp.end - 1) >> a.c.page_shift));
     };
-    auto inside = [&](int page) { return (unsigned)page < (unsigned)a.c.pages ? page : 0; };
-    typename P::raw k[2][C], v[T];
-    uint2v key_scales = {}, value_scales = {};
-    auto load_keys = [&](int s, int page, int page_kb) {
+    auto there = [&](int s, int block, int page) { return kStep * s + 8 * block < sp.end && (unsigned)page < (unsigned)a.c.pages; };
+    auto load_keys = [&](Fetch<D, E4M3> &f, int s, int page, int page_kb) {
         const int slot = (kStep * s + 8 * (n >> 2) + (n & 3)) & (a.c.page_size - 1);
-        const int64_t at = key_at(a.c, inside(page), head, slot) + 8 * kb;
+        const int64_t at = key_at(a.c, there(s, n >> 2, page) ? page : 0, head, slot) + 8 * kb;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int c = 0; c < C; ++c) k[t][c] = P::load(a.c.k, at + 4 * t * D + 32 * c);
+            for (int c = 0; c < C; ++c) f.k[t][c] = P::load(a.c.k, at + 4 * t * D + 32 * c);
         if (E4M3)
-            key_scales = *as_global<uint2v>(a.c.scales + scale_at(a.c, inside(page_kb), head, 0, (kStep * s + 8 * kb) & (a.c.page_size - 1)));
+            f.key_scales = *as_global<uint2v>(
+                a.c.scales + scale_at(a.c, there(s, kb, page_kb) ? page_kb : 0, head, 0, (kStep * s + 8 * kb) & (a.c.page_size - 1)));
     };
-    auto load_values = [&](int s, int page) {
+    auto load_values = [&](Fetch<D, E4M3> &f, int s, int page) {
         const int slot = (kStep * s + 8 * kb) & (a.c.page_size - 1);
-        const int64_t at = value_at(a.c, inside(page), head, slot) + 8 * n;
+        f.value_ok = there(s, kb, page);
+        const int64_t at = value_at(a.c, f.value_ok ? page : 0, head, slot) + 8 * n;
 #pragma unroll
-        for (int d = 0; d < T; ++d) v[d] = P::load(a.c.v, at + 128 * d);
-        if (E4M3) value_scales = *as_global<uint2v>(a.c.scales + scale_at(a.c, inside(page), head, 1, slot));
+        for (int d = 0; d < T; ++d) f.v[d] = P::load(a.c.v, at + 128 * d);
+        if (E4M3) f.value_scales = *as_global<uint2v>(a.c.scales + scale_at(a.c, f.value_ok ? page : 0, head, 1, slot));
     };
-    int key_page = page_of(step, n >> 2), value_page = page_of(step, kb);
-    int next_key_page = page_of(step + 1, n >> 2), next_value_page = page_of(step + 1, kb);
-    load_keys(step, key_page, value_page);
-    load_values(step, value_page);
+    const int key_page = page_of(step, n >> 2), first_value_page = page_of(step, kb);
     bf16x8 q[C];
     {
         const uint16_t *const at = a.q + b * a.q_stride + (int64_t)(head * a.group + kHeadTile * tile + (n < heads ? n : 0)) * D;
@@ -166,27 +188,41 @@ __device__ __forceinline__ void attend(const AttentionArgs &a, int b, int head, 
             q[c] = __builtin_bit_cast(bf16x8, w);
         }
     }
+    // (in the order of the loop, whose waits count what is under way)
+    Fetch<D, E4M3> fetch;
+    keep_order();
+    load_keys(fetch, step, key_page, first_value_page);
+    keep_order();
+    int next_key_page = page_of(count > 1 ? step + 1 : step, n >> 2), next_value_page = page_of(count > 1 ? step + 1 : step, kb);
+    keep_order();
+    load_values(fetch, step, first_value_page);
+    keep_order();
+    const bool fine = a.out_dtype == NVQ_F32;
     for (int i = 0; i < count; ++i) {
-        const int s = step + i, t0 = kStep * s;
-        const bool more = i + 1 < count;
-        const bool value_ok = (unsigned)value_page < (unsigned)a.c.pages;
+        Fetch<D, E4M3> &f = fetch;
+        const int s = step + i, t0 = kStep * s, next = i + 1 < count ? s + 1 : s;
+        const bool value_ok = f.value_ok;
         float4v raw[2];
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
             raw[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int c = 0; c < C; ++c)
-                raw[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P::operand(k[t][c]), q[c], raw[t], 0, 0, 0);
+                raw[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P::operand(f.k[t][c]), q[c], raw[t], 0, 0, 0);
         }
         wait_written(raw[0], raw[1]);
         float x[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             x[j] = raw[j >> 2][j & 3] * a.scale;
-            if (E4M3) x[j] *= scale_value(key_scales[j >> 2] >> 8 * (j & 3) & 255);
+            if (E4M3) x[j] *= scale_value(f.key_scales[j >> 2] >> 8 * (j & 3) & 255);
         }
-        if (more) load_keys(s + 1, next_key_page, next_value_page);
-        const int coming_key_page = page_of(s + 2, n >> 2), coming_value_page = page_of(s + 2, kb);
+        keep_order();
+        load_keys(f, next, next_key_page, next_value_page);
+        const int value_page = next_value_page;
+        next_key_page = page_of(i + 2 < count ? s + 2 : step + count - 1, n >> 2);
+        next_value_page = page_of(i + 2 < count ? s + 2 : step + count - 1, kb);
+        keep_order();
         if (a.softcap > 0.0f) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = a.softcap * tanhf(x[j] / a.softcap);
@@ -203,7 +239,7 @@ __device__ __forceinline__ void attend(const AttentionArgs &a, int b, int head, 
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = valid >> j & 1 ? x[j] : -INFINITY;
 #pragma unroll
-            for (int d = 0; d < T; ++d) v[d] = P::only(v[d], valid);
+            for (int d = 0; d < T; ++d) f.v[d] = P::only(f.v[d], valid);
         }
         float top = x[0];
 #pragma unroll
@@ -211,54 +247,58 @@ __device__ __forceinline__ void attend(const AttentionArgs &a, int b, int head, 
         top = with_lane_xor<16>(top, MaxOp());
         top = with_lane_xor<32>(top, MaxOp());
         if (__any(top > st.m)) {
-            const float m = fmaxf(st.m, top), f = st.m == m ? 1.0f : __builtin_amdgcn_exp2f((st.m - m) * kLog2e);
+            const float m = fmaxf(st.m, top), c = st.m == m ? 1.0f : __builtin_amdgcn_exp2f((st.m - m) * kLog2e);
             st.m = m;
-            st.l *= f;
+            st.l *= c;
 #pragma unroll
             for (int d = 0; d < T; ++d)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    st.o[d][r] *= f;
-                    st.rest[d][r] *= f;
+                    st.o[d][r] *= c;
+                    if (State<D, E4M3>::kApart) st.small(d)[r] *= c;
                 }
         }
         const float ref = st.m == -INFINITY ? 0.0f : st.m;
-        uint32_t part[3][4];
+        float p[8];
 #pragma unroll
-        for (int j = 0; j < 8; j += 2) {
-            float p[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                p[e] = __builtin_amdgcn_exp2f((x[j + e] - ref) * kLog2e);
-                st.l += p[e];
-                if (E4M3) {
-                    const float f = scale_value(value_scales[(j + e) >> 2] >> 8 * ((j + e) & 3) & 255);
-                    p[e] = valid >> (j + e) & 1 ? p[e] * f : 0.0f;
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 3; ++i) {
-                part[i][j / 2] = pack_bf16x2(p[0], p[1]);
-                p[0] -= __uint_as_float(part[i][j / 2] << 16);
-                p[1] -= __uint_as_float(part[i][j / 2] & 0xffff0000u);
+        for (int j = 0; j < 8; ++j) {
+            p[j] = __builtin_amdgcn_exp2f((x[j] - ref) * kLog2e);
+            st.l += p[j];
+            if (E4M3) {
+                const float c = scale_value(f.value_scales[j >> 2] >> 8 * (j & 3) & 255);
+                p[j] = valid >> j & 1 ? p[j] * c : 0.0f;
             }
         }
-        bf16x8 w[3];
+        auto part = [&]() {  // the next eight bits of the weights
+            uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 3; ++i) w[i] = __builtin_bit_cast(bf16x8, make_uint4(part[i][0], part[i][1], part[i][2], part[i][3]));
+            for (int j = 0; j < 4; ++j) {
+                w[j] = pack_bf16x2(p[2 * j], p[2 * j + 1]);
+                p[2 * j] -= __uint_as_float(w[j] << 16);
+                p[2 * j + 1] -= __uint_as_float(w[j] & 0xffff0000u);
+            }
+            return __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+        };
+        const bf16x8 w0 = part(), w1 = part();
 #pragma unroll
         for (int d = 0; d < T; ++d) {
-            const bf16x8 x = P::operand(v[d]);
-            st.o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w[0], st.o[d], 0, 0, 0);
-            st.rest[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w[1], st.rest[d], 0, 0, 0);
-            st.rest[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w[2], st.rest[d], 0, 0, 0);
+            const bf16x8 y = P::operand(f.v[d]);
+            st.o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, w0, st.o[d], 0, 0, 0);
+            st.small(d) = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, w1, st.small(d), 0, 0, 0);
         }
-        if (more) load_values(s + 1, next_value_page);
-        value_page = next_value_page;
-        next_key_page = coming_key_page;
-        next_value_page = coming_value_page;
 #pragma unroll
-        for (int d = 0; d < T; ++d) wait_written(st.o[d], st.rest[d]);
+        for (int d = 0; d < T; ++d) wait_written(st.o[d], st.small(d));
+        if (fine) {
+            const bf16x8 w2 = part();
+#pragma unroll
+            for (int d = 0; d < T; ++d)
+                st.small(d) = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P::operand(f.v[d]), w2, st.small(d), 0, 0, 0);
+#pragma unroll
+            for (int d = 0; d < T; ++d) wait_written(st.small(d));
+        }
+        keep_order();
+        load_values(f, next, value_page);
+        keep_order();
     }
 }
 
@@ -274,7 +314,17 @@ struct PieceOf {
 template <int D>
 constexpr int waves_of() { return D <= 128 ? 8 : 4; }
 
-__device__ __forceinline__ float factor(float m, float most) { return m == most ? 1.0f : expf(m - most); }
+__device__ __forceinline__ float factor(float m, float most) {
+    return m == most ? 1.0f : __builtin_amdgcn_exp2f((m - most) * kLog2e);
+}
+__device__ __forceinline__ float wave_max(float v) {
+    v = with_lane_xor<32>(v, MaxOp());
+    v = with_lane_xor<16>(v, MaxOp());
+    v = with_lane_xor<8>(v, MaxOp());
+    v = with_lane_xor<4>(v, MaxOp());
+    v = with_lane_xor<2>(v, MaxOp());
+    return with_lane_xor<1>(v, MaxOp());
+}
 
 __device__ __forceinline__ void put(float *p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ float get(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
@@ -360,7 +410,7 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
         p.end = __builtin_amdgcn_readfirstlane(p.end);
         f += p.end - p.begin;
         Span sp = span_of(a, p.b);
-        State<D> st;
+        State<D, E4M3> st;
         st.clear();
         attend<D, E4M3>(a, p.b, p.ht / a.tiles, p.ht % a.tiles, sp, sp.first + p.begin, p.end - p.begin, st);
         float l = with_lane_xor<16>(st.l, AddOp());
@@ -394,51 +444,77 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     }
     __syncthreads();
 
-    // The waves' parts: a piece that starts in one wave goes on in the next ones' first slots.
+    // The waves' parts: a piece that starts in one wave goes on in the next ones' first slots.  (What all have is looked at
+    // at once; with loops over the waves, one value after the other, this took 4 us.)
     PieceOf shared_piece[2];  // what is left for others to join: begun before this workgroup, going on after it
     shared_piece[0].b = shared_piece[1].b = -1;
+    int ends[kWaves];  // of the first slots; -1: empty
+    uint32_t starts = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) {
+        ends[i] = held[i][0].b >= 0 ? held[i][0].end : -1;
+        starts |= held[i][1].b >= 0 ? 1u << i : 0u;
+    }
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) ends[i] = __builtin_amdgcn_readfirstlane(ends[i]);
+    starts = __builtin_amdgcn_readfirstlane(starts);
+    // (start -1: what begins before this workgroup, in the first slot of the first wave that has any steps)
+    int front = 0;
+    while (R * (front + 1) / kWaves == 0) ++front;
     for (int start = -1; start < kWaves; ++start) {
-        // (-1: what begins before this workgroup, in the first slot of the first wave that has any steps)
-        int first = start < 0 ? 0 : start;
-        const int slot = start < 0 ? 0 : 1;
-        while (start < 0 && R * (first + 1) / kWaves == 0) ++first;
+        if (start >= 0 && !(starts >> start & 1)) continue;
+        const int slot = start < 0 ? 0 : 1, first = start < 0 ? front : start;
         PieceOf p = held[first][slot];
         if (p.b < 0) continue;
-        int until = p.end, lastw = first;
-        while (until < p.n && lastw + 1 < kWaves) {
-            ++lastw;
-            if (held[lastw][0].b >= 0) until = held[lastw][0].end;
-        }
+        uint32_t members = 1u << first;
+        int until = p.end;
+#pragma unroll
+        for (int i = 1; i < kWaves; ++i)
+            if (i > first && until < p.n && ends[i] >= 0) {
+                members |= 1u << i;
+                until = ends[i];
+            }
+        members = __builtin_amdgcn_readfirstlane(members);
         const int heads = heads_of(p.ht);
         const bool whole = p.begin == 0 && until == p.n;
         const int to_slot = p.begin > 0 ? 0 : 1;
         if (!whole) {
             p.end = until;
-            shared_piece[to_slot] = p;
+            if (to_slot)
+                shared_piece[1] = p;
+            else
+                shared_piece[0] = p;
         }
-        auto part = [&](int i, int h) { return parts + ((i * 2 + (i == first ? slot : 0)) * heads_most + h) * kRow; };
-        auto there = [&](int i) { return held[i][i == first ? slot : 0].b >= 0; };
         for (int e = threadIdx.x; e < heads * D; e += kThreads) {
             const int h = e / D, d = e % D;
-            float most = -INFINITY, l = 0.0f, o = 0.0f;
-            for (int i = first; i <= lastw; ++i)
-                if (there(i)) most = fmaxf(most, part(i, h)[D]);
-            for (int i = first; i <= lastw; ++i)
-                if (there(i)) {
-                    const float c = factor(part(i, h)[D], most);
-                    l += c * part(i, h)[D + 1];
-                    o += c * part(i, h)[d];
-                }
+            float m[kWaves], l[kWaves], o[kWaves], most = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) {
+                const float *const part = parts + ((i * 2 + (i == first ? slot : 0)) * heads_most + h) * kRow;
+                const bool there = members >> i & 1;
+                m[i] = there ? part[D] : -INFINITY;
+                l[i] = there ? part[D + 1] : 0.0f;
+                o[i] = there ? part[d] : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) most = fmaxf(most, m[i]);
+            float sum = 0.0f, out = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kWaves; ++i) {
+                const float c = members >> i & 1 ? factor(m[i], most) : 0.0f;
+                sum += c * l[i];
+                out += c * o[i];
+            }
             if (whole) {
                 const int64_t row = row_of(p.b, p.ht) + h;
-                write(row, d, l == 0.0f ? 0.0f : o / l);
-                if (a.lse && d == 0) a.lse[row] = l == 0.0f ? -INFINITY : most + logf(l);
+                write(row, d, sum == 0.0f ? 0.0f : out / sum);
+                if (a.lse && d == 0) a.lse[row] = sum == 0.0f ? -INFINITY : most + logf(sum);
             } else {
                 float *const to = a.partial + ((int64_t)(g * 2 + to_slot) * kHeadTile + h) * kRow;
-                put(to + d, o);
+                put(to + d, out);
                 if (d == 0) {
                     put(to + D, most);
-                    put(to + D + 1, l);
+                    put(to + D + 1, sum);
                 }
             }
         }
@@ -450,7 +526,7 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     auto group_of = [&](int64_t f) { return (int)(((f + 1) * groups - 1) / T); };
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
-            const PieceOf &p = shared_piece[i];
+            const PieceOf &p = i ? shared_piece[1] : shared_piece[0];
             last[i] = 0;
             if (p.b < 0) continue;
             const int64_t at = (int64_t)per * upto[p.b] + (int64_t)p.ht * p.n;
@@ -463,27 +539,42 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     __syncthreads();
     for (int i = 0; i < 2; ++i) {
         if (!last[i]) continue;  // (the same for the whole workgroup)
-        const PieceOf p = shared_piece[i];
+        const PieceOf p = i ? shared_piece[1] : shared_piece[0];
         const int64_t at = (int64_t)per * upto[p.b] + (int64_t)p.ht * p.n;
         const int from = group_of(at), count = group_of(at + p.n - 1) - from + 1, heads = heads_of(p.ht);
         auto part = [&](int j, int h) { return a.partial + ((int64_t)((from + j) * 2 + (j == 0 ? 1 : 0)) * kHeadTile + h) * kRow; };
-        // The factors of the parts, [count][heads], where the waves' parts were; l and m of a head behind them.
+        // The factors of the parts, [count][heads], where the waves' parts were; m and l of a head behind them.  The first
+        // parts' sums are asked for together with what the factors are made of.
         float *const scale = parts, *const sums = parts + count * heads;
+        constexpr int kAtOnce = 16;
+        float v[kAtOnce];
+        auto ask = [&](int e, int j0) {
+            const int h = e / D, d = e % D;
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) v[j] = get(part(j0 + j < count ? j0 + j : 0, h) + d);
+        };
+        if ((int)threadIdx.x < heads * D) ask(threadIdx.x, 0);
         __syncthreads();
         for (int h = w; h < heads; h += kWaves) {
-            float most = -INFINITY, l = 0.0f;
-            for (int j = lane; j < count; j += 64) {
-                const float m = get(part(j, h) + D);
-                scale[j * heads + h] = m;
-                most = fmaxf(most, m);
+            float m[kMaxGroups / 64], s[kMaxGroups / 64], most = -INFINITY, l = 0.0f;
+#pragma unroll
+            for (int k = 0; k < kMaxGroups / 64; ++k) {
+                const int j = 64 * k + lane;
+                m[k] = j < count ? get(part(j, h) + D) : -INFINITY;
+                s[k] = j < count ? get(part(j, h) + D + 1) : 0.0f;
             }
-            for (int d = 32; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
-            for (int j = lane; j < count; j += 64) {
-                const float c = factor(scale[j * heads + h], most);
+#pragma unroll
+            for (int k = 0; k < kMaxGroups / 64; ++k) most = fmaxf(most, m[k]);
+            most = wave_max(most);
+#pragma unroll
+            for (int k = 0; k < kMaxGroups / 64; ++k) {
+                const int j = 64 * k + lane;
+                if (j >= count) continue;
+                const float c = factor(m[k], most);
                 scale[j * heads + h] = c;
-                l += c * get(part(j, h) + D + 1);
+                l += c * s[k];
             }
-            for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
+            l = group_sum<64>(l);
             if (lane == 0) {
                 sums[2 * h] = most;
                 sums[2 * h + 1] = l;
@@ -493,24 +584,20 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
         for (int e = threadIdx.x; e < heads * D; e += kThreads) {
             const int h = e / D, d = e % D;
             float o = 0.0f;
-            constexpr int kAtOnce = 16;
             for (int j0 = 0; j0 < count; j0 += kAtOnce) {
-                float v[kAtOnce];
+                if (j0 > 0 || e >= kThreads) ask(e, j0);
 #pragma unroll
-                for (int j = 0; j < kAtOnce; ++j) v[j] = get(part(j0 + j < count ? j0 + j : 0, h) + d);
-#pragma unroll
-                for (int j = 0; j < kAtOnce; ++j)
-                    if (j0 + j < count) o += scale[(j0 + j) * heads + h] * v[j];
+                for (int j = 0; j < kAtOnce; ++j) o += j0 + j < count ? scale[(j0 + j) * heads + h] * v[j] : 0.0f;
             }
             const float most = sums[2 * h], l = sums[2 * h + 1];
             const int64_t row = row_of(p.b, p.ht) + h;
             write(row, d, l == 0.0f ? 0.0f : o / l);
             if (a.lse && d == 0) a.lse[row] = l == 0.0f ? -INFINITY : most + logf(l);
         }
+        __syncthreads();  // (the room may be needed for the other piece)
     }
 }
 
-constexpr int kMaxGroups = 256;
 constexpr int64_t kMostSteps = 1ll << 30;  // of all sequences, per head tile
 
 template <int D>
