@@ -314,6 +314,10 @@ struct PieceOf {
 template <int D>
 constexpr int waves_of() { return D <= 128 ? 8 : 4; }
 
+// a / b for 0 <= a < 2^49, 0 < b < 2^41 and quotients whose product with b is below 2^49: in fp64 (a quotient that is no
+// whole number is further from one than its rounding), which takes a tenth of an integer division of 64 bits.
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) { return (int64_t)((double)a / (double)b); }
+
 __device__ __forceinline__ float factor(float m, float most) {
     return m == most ? 1.0f : __builtin_amdgcn_exp2f((m - most) * kLog2e);
 }
@@ -379,19 +383,17 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     if (T == 0) return;
     // Two steps to a wave at least; and of one sequence whole workgroups to a head tile, so that a short one needs no
     // joining through memory.
-    int64_t groups = (T + 2 * kWaves - 1) / (2 * kWaves);
-    if (groups >= gridDim.x)
-        groups = gridDim.x;
-    else if (a.B == 1 && groups > per)
-        groups -= groups % per;
+    const int64_t want = (T + 2 * kWaves - 1) / (2 * kWaves);
+    int groups = want < (int64_t)gridDim.x ? (int)want : (int)gridDim.x;
+    if (a.B == 1 && groups < (int)gridDim.x && groups > per) groups -= groups % per;
     const int g = blockIdx.x;
     if (g >= groups) return;
-    const int64_t f0 = T * g / groups, f1 = T * (g + 1) / groups, R = f1 - f0;
+    const int64_t f0 = quotient(T * g, groups), f1 = quotient(T * (g + 1), groups), R = f1 - f0;
     const int64_t w0 = f0 + R * w / kWaves, w1 = f0 + R * (w + 1) / kWaves;
 
     auto write = [&](int64_t row, int i, float v) { store_global(a.out, a.out_dtype, row * D + i, v); };
     for (int64_t f = w0; f < w1;) {
-        const int x = (int)(f / per);
+        const int x = (int)quotient(f, per);
         int lo = 0, hi = a.B;  // upto[lo] <= x < upto[hi]
         while (hi - lo > 1) {
             const int mid = (lo + hi) / 2;
@@ -404,7 +406,7 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
         p.b = __builtin_amdgcn_readfirstlane(lo);
         p.n = __builtin_amdgcn_readfirstlane(upto[lo + 1] - upto[lo]);
         const int64_t r = f - (int64_t)per * upto[lo];
-        p.ht = __builtin_amdgcn_readfirstlane((int)(r / p.n));
+        p.ht = __builtin_amdgcn_readfirstlane((int)quotient(r, p.n));
         p.begin = __builtin_amdgcn_readfirstlane((int)(r - (int64_t)p.ht * p.n));
         p.end = (int64_t)(p.n - p.begin) < w1 - f ? p.n : p.begin + (int)(w1 - f);
         p.end = __builtin_amdgcn_readfirstlane(p.end);
@@ -461,7 +463,9 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     // (start -1: what begins before this workgroup, in the first slot of the first wave that has any steps)
     int front = 0;
     while (R * (front + 1) / kWaves == 0) ++front;
-    for (int start = -1; start < kWaves; ++start) {
+    // (of short sequences many begin and end in a workgroup, a wave to each then)
+    const bool many = __builtin_popcount(starts) > 2;
+    for (int start = -1, turn = 0; start < kWaves; ++start) {
         if (start >= 0 && !(starts >> start & 1)) continue;
         const int slot = start < 0 ? 0 : 1, first = start < 0 ? front : start;
         PieceOf p = held[first][slot];
@@ -485,25 +489,28 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
             else
                 shared_piece[0] = p;
         }
-        for (int e = threadIdx.x; e < heads * D; e += kThreads) {
+        if (many && turn++ % kWaves != w) continue;
+        for (int e = many ? lane : (int)threadIdx.x; e < heads * D; e += many ? 64 : kThreads) {
             const int h = e / D, d = e % D;
             float m[kWaves], l[kWaves], o[kWaves], most = -INFINITY;
 #pragma unroll
             for (int i = 0; i < kWaves; ++i) {
                 const float *const part = parts + ((i * 2 + (i == first ? slot : 0)) * heads_most + h) * kRow;
                 const bool there = members >> i & 1;
-                m[i] = there ? part[D] : -INFINITY;
-                l[i] = there ? part[D + 1] : 0.0f;
-                o[i] = there ? part[d] : 0.0f;
+                m[i] = part[D];  // (without a branch; what is not there may be anything)
+                l[i] = part[D + 1];
+                o[i] = part[d];
+                m[i] = there ? m[i] : -INFINITY;
             }
 #pragma unroll
             for (int i = 0; i < kWaves; ++i) most = fmaxf(most, m[i]);
             float sum = 0.0f, out = 0.0f;
 #pragma unroll
             for (int i = 0; i < kWaves; ++i) {
-                const float c = members >> i & 1 ? factor(m[i], most) : 0.0f;
-                sum += c * l[i];
-                out += c * o[i];
+                const bool there = members >> i & 1;
+                const float c = factor(m[i], most);
+                sum += there ? c * l[i] : 0.0f;
+                out += there ? c * o[i] : 0.0f;
             }
             if (whole) {
                 const int64_t row = row_of(p.b, p.ht) + h;
@@ -523,7 +530,7 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     // arrives; the last one's loads pass its caches by.
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
     __syncthreads();
-    auto group_of = [&](int64_t f) { return (int)(((f + 1) * groups - 1) / T); };
+    auto group_of = [&](int64_t f) { return (int)quotient((f + 1) * groups - 1, T); };
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
             const PieceOf &p = i ? shared_piece[1] : shared_piece[0];
@@ -541,40 +548,34 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
         if (!last[i]) continue;  // (the same for the whole workgroup)
         const PieceOf p = i ? shared_piece[1] : shared_piece[0];
         const int64_t at = (int64_t)per * upto[p.b] + (int64_t)p.ht * p.n;
-        const int from = group_of(at), count = group_of(at + p.n - 1) - from + 1, heads = heads_of(p.ht);
-        auto part = [&](int j, int h) { return a.partial + ((int64_t)((from + j) * 2 + (j == 0 ? 1 : 0)) * kHeadTile + h) * kRow; };
+        const int from = __builtin_amdgcn_readfirstlane(group_of(at));
+        const int count = __builtin_amdgcn_readfirstlane(group_of(at + p.n - 1)) - from + 1, heads = heads_of(p.ht);
+        // What workgroup from + j has of it: behind the beginning in the first slot.
+        auto part = [&](int j) { return a.partial + (int64_t)((from + j) * 2 + (j == 0 ? 1 : 0)) * kHeadTile * kRow; };
         // The factors of the parts, [count][heads], where the waves' parts were; m and l of a head behind them.  The first
-        // parts' sums are asked for together with what the factors are made of.
+        // parts' sums are asked for together with what the factors are made of, all loads without branches between them.
         float *const scale = parts, *const sums = parts + count * heads;
-        constexpr int kAtOnce = 16;
+        constexpr int kAtOnce = 32;
         float v[kAtOnce];
-        auto ask = [&](int e, int j0) {
-            const int h = e / D, d = e % D;
+        auto ask = [&](int off, int j0) {
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) v[j] = get(part(j0 + j < count ? j0 + j : 0, h) + d);
+            for (int j = 0; j < kAtOnce; ++j) v[j] = get(part(j0 + j < count ? j0 + j : count - 1) + off);
         };
-        if ((int)threadIdx.x < heads * D) ask(threadIdx.x, 0);
+        const int e0 = (int)threadIdx.x < heads * D ? (int)threadIdx.x : 0;
+        ask(e0 / D * kRow + e0 % D, 0);
         __syncthreads();
         for (int h = w; h < heads; h += kWaves) {
-            float m[kMaxGroups / 64], s[kMaxGroups / 64], most = -INFINITY, l = 0.0f;
-#pragma unroll
-            for (int k = 0; k < kMaxGroups / 64; ++k) {
-                const int j = 64 * k + lane;
-                m[k] = j < count ? get(part(j, h) + D) : -INFINITY;
-                s[k] = j < count ? get(part(j, h) + D + 1) : 0.0f;
-            }
-#pragma unroll
-            for (int k = 0; k < kMaxGroups / 64; ++k) most = fmaxf(most, m[k]);
-            most = wave_max(most);
-#pragma unroll
-            for (int k = 0; k < kMaxGroups / 64; ++k) {
-                const int j = 64 * k + lane;
-                if (j >= count) continue;
-                const float c = factor(m[k], most);
-                scale[j * heads + h] = c;
-                l += c * s[k];
+            float most = -INFINITY, l = 0.0f;
+            for (int j0 = 0; j0 < count; j0 += 64) {
+                const int j = j0 + lane < count ? j0 + lane : count - 1;
+                const float m = get(part(j) + h * kRow + D), s = get(part(j) + h * kRow + D + 1);
+                if (j0 + lane < count) scale[j * heads + h] = m;
+                const float top = fmaxf(most, wave_max(m));
+                l = l * factor(most, top) + (j0 + lane < count ? s * factor(m, top) : 0.0f);  // (of a lane)
+                most = top;
             }
             l = group_sum<64>(l);
+            for (int j = lane; j < count; j += 64) scale[j * heads + h] = factor(scale[j * heads + h], most);
             if (lane == 0) {
                 sums[2 * h] = most;
                 sums[2 * h + 1] = l;
@@ -585,7 +586,7 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
             const int h = e / D, d = e % D;
             float o = 0.0f;
             for (int j0 = 0; j0 < count; j0 += kAtOnce) {
-                if (j0 > 0 || e >= kThreads) ask(e, j0);
+                if (j0 > 0 || e >= kThreads) ask(h * kRow + d, j0);
 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j) o += j0 + j < count ? scale[(j0 + j) * heads + h] * v[j] : 0.0f;
             }
