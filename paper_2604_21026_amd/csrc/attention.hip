@@ -12,6 +12,8 @@
 // left out) where they are rounded to bf16, 2^-9, themselves.  The products with the first and with the rest are summed
 // apart and added at the end: what an infinite value makes of the rest (zero times infinity, or the other sign)
 // is left out there.
+#include <type_traits>
+
 #include "cache.h"
 #include "mfma_act.h"
 
@@ -553,48 +555,58 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
         // What workgroup from + j has of it: behind the beginning in the first slot.
         auto part = [&](int j) { return a.partial + (int64_t)((from + j) * 2 + (j == 0 ? 1 : 0)) * kHeadTile * kRow; };
         // The factors of the parts, [count][heads], where the waves' parts were; m and l of a head behind them.  The first
-        // parts' sums are asked for together with what the factors are made of, all loads without branches between them.
+        // parts' sums are asked for together with what the factors are made of, as many as there are likely to be and
+        // without branches between the loads.
         float *const scale = parts, *const sums = parts + count * heads;
-        constexpr int kAtOnce = 32;
-        float v[kAtOnce];
-        auto ask = [&](int off, int j0) {
+        auto join = [&](auto at_once) {
+            constexpr int kAtOnce = decltype(at_once)::value;
+            float v[kAtOnce];
+            auto ask = [&](int off, int j0) {
 #pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) v[j] = get(part(j0 + j < count ? j0 + j : count - 1) + off);
+                for (int j = 0; j < kAtOnce; ++j) v[j] = get(part(j0 + j < count ? j0 + j : count - 1) + off);
+            };
+            const int e0 = (int)threadIdx.x < heads * D ? (int)threadIdx.x : 0;
+            ask(e0 / D * kRow + e0 % D, 0);
+            __syncthreads();
+            for (int h = w; h < heads; h += kWaves) {
+                float most = -INFINITY, l = 0.0f;
+                for (int j0 = 0; j0 < count; j0 += 64) {
+                    const int j = j0 + lane < count ? j0 + lane : count - 1;
+                    const float m = get(part(j) + h * kRow + D), s = get(part(j) + h * kRow + D + 1);
+                    if (j0 + lane < count) scale[j * heads + h] = m;
+                    const float top = fmaxf(most, wave_max(m));
+                    l = l * factor(most, top) + (j0 + lane < count ? s * factor(m, top) : 0.0f);  // (of a lane)
+                    most = top;
+                }
+                l = group_sum<64>(l);
+                for (int j = lane; j < count; j += 64) scale[j * heads + h] = factor(scale[j * heads + h], most);
+                if (lane == 0) {
+                    sums[2 * h] = most;
+                    sums[2 * h + 1] = l;
+                }
+            }
+            __syncthreads();
+            for (int e = threadIdx.x; e < heads * D; e += kThreads) {
+                const int h = e / D, d = e % D;
+                float o = 0.0f;
+                for (int j0 = 0; j0 < count; j0 += kAtOnce) {
+                    if (j0 > 0 || e >= kThreads) ask(h * kRow + d, j0);
+                    float c[kAtOnce];
+#pragma unroll
+                    for (int j = 0; j < kAtOnce; ++j) c[j] = scale[(j0 + j < count ? j0 + j : count - 1) * heads + h];
+#pragma unroll
+                    for (int j = 0; j < kAtOnce; ++j) o += j0 + j < count ? c[j] * v[j] : 0.0f;
+                }
+                const float most = sums[2 * h], l = sums[2 * h + 1];
+                const int64_t row = row_of(p.b, p.ht) + h;
+                write(row, d, l == 0.0f ? 0.0f : o / l);
+                if (a.lse && d == 0) a.lse[row] = l == 0.0f ? -INFINITY : most + logf(l);
+            }
         };
-        const int e0 = (int)threadIdx.x < heads * D ? (int)threadIdx.x : 0;
-        ask(e0 / D * kRow + e0 % D, 0);
-        __syncthreads();
-        for (int h = w; h < heads; h += kWaves) {
-            float most = -INFINITY, l = 0.0f;
-            for (int j0 = 0; j0 < count; j0 += 64) {
-                const int j = j0 + lane < count ? j0 + lane : count - 1;
-                const float m = get(part(j) + h * kRow + D), s = get(part(j) + h * kRow + D + 1);
-                if (j0 + lane < count) scale[j * heads + h] = m;
-                const float top = fmaxf(most, wave_max(m));
-                l = l * factor(most, top) + (j0 + lane < count ? s * factor(m, top) : 0.0f);  // (of a lane)
-                most = top;
-            }
-            l = group_sum<64>(l);
-            for (int j = lane; j < count; j += 64) scale[j * heads + h] = factor(scale[j * heads + h], most);
-            if (lane == 0) {
-                sums[2 * h] = most;
-                sums[2 * h + 1] = l;
-            }
-        }
-        __syncthreads();
-        for (int e = threadIdx.x; e < heads * D; e += kThreads) {
-            const int h = e / D, d = e % D;
-            float o = 0.0f;
-            for (int j0 = 0; j0 < count; j0 += kAtOnce) {
-                if (j0 > 0 || e >= kThreads) ask(h * kRow + d, j0);
-#pragma unroll
-                for (int j = 0; j < kAtOnce; ++j) o += j0 + j < count ? scale[(j0 + j) * heads + h] * v[j] : 0.0f;
-            }
-            const float most = sums[2 * h], l = sums[2 * h + 1];
-            const int64_t row = row_of(p.b, p.ht) + h;
-            write(row, d, l == 0.0f ? 0.0f : o / l);
-            if (a.lse && d == 0) a.lse[row] = l == 0.0f ? -INFINITY : most + logf(l);
-        }
+        if (count <= 4)
+            join(std::integral_constant<int, 4>());
+        else
+            join(std::integral_constant<int, 16>());
         __syncthreads();  // (the room may be needed for the other piece)
     }
 }
