@@ -24,6 +24,9 @@ namespace {
 constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kStep = 32, kHeadTile = 16;
 constexpr int kMaxGroups = 256;
+// Steps that a sequence and head tile counts for beyond its own: its numbers, first loads and last sums take a wave about
+// as long, and workgroups of many short ones would end last.
+constexpr int kPieceCost = 1;
 
 struct AttentionArgs {
     CacheView c;
@@ -342,7 +345,7 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     __shared__ int scan[kWaves + 1];
     __shared__ PieceOf held[kWaves][2];
     __shared__ int last[2];
-    int *const upto = reinterpret_cast<int *>(lds);  // [B + 1]: steps before a sequence, of one head tile
+    int *const upto = reinterpret_cast<int *>(lds);  // [B + 1]: steps before a sequence, of one head tile, kPieceCost included
     float *const parts = reinterpret_cast<float *>(lds + (((int64_t)a.B + 1) * 4 + 15) / 16 * 16);  // [waves][2][heads][kRow]
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4;
     const int per = a.c.heads * a.tiles;                                   // head tiles
@@ -356,7 +359,8 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     int total = 0;
     for (int b0 = 0; b0 < a.B; b0 += kThreads) {
         const int b = b0 + (int)threadIdx.x;
-        int steps = b < a.B ? span_of(a, b).steps : 0, sum = steps;
+        const int steps = b < a.B ? span_of(a, b).steps : 0;
+        int sum = steps > 0 ? steps + kPieceCost : 0;
         for (int d = 1; d < 64; d <<= 1) {
             const int o = __shfl_up(sum, d);
             if (lane >= d) sum += o;
@@ -416,7 +420,8 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
         Span sp = span_of(a, p.b);
         State<D, E4M3> st;
         st.clear();
-        attend<D, E4M3>(a, p.b, p.ht / a.tiles, p.ht % a.tiles, sp, sp.first + p.begin, p.end - p.begin, st);
+        const int count = (p.end < sp.steps ? p.end : sp.steps) - p.begin;
+        if (count > 0) attend<D, E4M3>(a, p.b, p.ht / a.tiles, p.ht % a.tiles, sp, sp.first + p.begin, count, st);
         float l = with_lane_xor<16>(st.l, AddOp());
         l = with_lane_xor<32>(l, AddOp());
         const int heads = heads_of(p.ht);
@@ -491,8 +496,40 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
             else
                 shared_piece[0] = p;
         }
-        if (many && turn++ % kWaves != w) continue;
-        for (int e = many ? lane : (int)threadIdx.x; e < heads * D; e += many ? 64 : kThreads) {
+        auto finish = [&](int h, int d, float most, float sum, float out) {
+            if (whole) {
+                const int64_t row = row_of(p.b, p.ht) + h;
+                write(row, d, sum == 0.0f ? 0.0f : out / sum);
+                if (a.lse && d == 0) a.lse[row] = sum == 0.0f ? -INFINITY : most + logf(sum);
+            } else {
+                float *const to = a.partial + ((int64_t)(g * 2 + to_slot) * kHeadTile + h) * kRow;
+                put(to + d, out);
+                if (d == 0) {
+                    put(to + D, most);
+                    put(to + D + 1, sum);
+                }
+            }
+        };
+        if (many) {
+            if (turn++ % kWaves != w) continue;
+            for (int h = 0; h < heads; ++h) {  // (of few waves each)
+                float most = -INFINITY, sum = 0.0f, out[(D + 63) / 64] = {};
+                for (uint32_t left = members; left; left &= left - 1) {
+                    const int i = __builtin_ctz(left);
+                    const float *const part = parts + ((i * 2 + (i == first ? slot : 0)) * heads_most + h) * kRow;
+                    const float m = part[D], next = fmaxf(most, m), old = factor(most, next), c = factor(m, next);
+                    sum = sum * old + c * part[D + 1];
+#pragma unroll
+                    for (int k = 0; k < (D + 63) / 64; ++k) out[k] = out[k] * old + c * part[64 * k + lane < D ? 64 * k + lane : 0];
+                    most = next;
+                }
+#pragma unroll
+                for (int k = 0; k < (D + 63) / 64; ++k)
+                    if (64 * k + lane < D) finish(h, 64 * k + lane, most, sum, out[k]);
+            }
+            continue;
+        }
+        for (int e = threadIdx.x; e < heads * D; e += kThreads) {
             const int h = e / D, d = e % D;
             float m[kWaves], l[kWaves], o[kWaves], most = -INFINITY;
 #pragma unroll
@@ -514,18 +551,7 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
                 sum += there ? c * l[i] : 0.0f;
                 out += there ? c * o[i] : 0.0f;
             }
-            if (whole) {
-                const int64_t row = row_of(p.b, p.ht) + h;
-                write(row, d, sum == 0.0f ? 0.0f : out / sum);
-                if (a.lse && d == 0) a.lse[row] = sum == 0.0f ? -INFINITY : most + logf(sum);
-            } else {
-                float *const to = a.partial + ((int64_t)(g * 2 + to_slot) * kHeadTile + h) * kRow;
-                put(to + d, out);
-                if (d == 0) {
-                    put(to + D, most);
-                    put(to + D + 1, sum);
-                }
-            }
+            finish(h, d, most, sum, out);
         }
     }
     // Parts in the workspace are written through to where all XCDs see them, and waited for, before this workgroup
@@ -617,7 +643,7 @@ template <int D>
 int launch_attention(const AttentionArgs &a, hipStream_t st) {
     constexpr int kWaves = waves_of<D>();
     const int cu = device_cu_count(), heads = a.group < kHeadTile ? a.group : kHeadTile;
-    const int64_t steps = (int64_t)a.B * (((int64_t)a.width << a.c.page_shift) / kStep + 1) * a.c.heads * a.tiles;
+    const int64_t steps = (int64_t)a.B * (((int64_t)a.width << a.c.page_shift) / kStep + 1 + kPieceCost) * a.c.heads * a.tiles;
     const int64_t want = (steps + 2 * kWaves - 1) / (2 * kWaves), most = cu < kMaxGroups ? cu : kMaxGroups;
     const dim3 grid((unsigned)(want < most ? want : most)), block(64 * kWaves);
     // (the parts' room also holds the factors and sums of a join: kMaxGroups + 2 per head)
