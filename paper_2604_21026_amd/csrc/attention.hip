@@ -25,8 +25,9 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr int kStep = 32, kHeadTile = 16;
 constexpr int kMaxGroups = 256;
 // Steps that a sequence and head tile counts for beyond its own: its numbers, first loads and last sums take a wave about
-// as long, and workgroups of many short ones would end last.
-constexpr int kPieceCost = 1;
+// as long, and workgroups of many short ones would end last.  (0, 1, 2, 3: 68, 64.5, 63, 62 us for 32 ragged sequences of
+// up to 16384 tokens in 8 bits, 24, 22.4, 21.7, 21.5 for 40 of 150 to 300.)
+constexpr int kPieceCost = 2;
 
 struct AttentionArgs {
     CacheView c;
@@ -35,6 +36,7 @@ struct AttentionArgs {
     const int32_t *table, *lengths;
     int B, H, width, group, tiles;  // query heads per key head; head tiles of them
     int window;
+    int most_groups;  // workgroups that the device holds at once
     float scale, softcap;
     void *out;
     int out_dtype;
@@ -391,7 +393,7 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     // joining through memory.
     const int64_t want = (T + 2 * kWaves - 1) / (2 * kWaves);
     int groups = want < (int64_t)gridDim.x ? (int)want : (int)gridDim.x;
-    if (a.B == 1 && groups < (int)gridDim.x && groups > per) groups -= groups % per;
+    if (a.B == 1 && want < a.most_groups && groups > per) groups -= groups % per;
     const int g = blockIdx.x;
     if (g >= groups) return;
     const int64_t f0 = quotient(T * g, groups), f1 = quotient(T * (g + 1), groups), R = f1 - f0;
@@ -640,11 +642,12 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
 constexpr int64_t kMostSteps = 1ll << 30;  // of all sequences, per head tile
 
 template <int D>
-int launch_attention(const AttentionArgs &a, hipStream_t st) {
+int launch_attention(AttentionArgs a, hipStream_t st) {
     constexpr int kWaves = waves_of<D>();
     const int cu = device_cu_count(), heads = a.group < kHeadTile ? a.group : kHeadTile;
     const int64_t steps = (int64_t)a.B * (((int64_t)a.width << a.c.page_shift) / kStep + 1 + kPieceCost) * a.c.heads * a.tiles;
     const int64_t want = (steps + 2 * kWaves - 1) / (2 * kWaves), most = cu < kMaxGroups ? cu : kMaxGroups;
+    a.most_groups = (int)most;
     const dim3 grid((unsigned)(want < most ? want : most)), block(64 * kWaves);
     // (the parts' room also holds the factors and sums of a join: kMaxGroups + 2 per head)
     static_assert(2 * kWaves * (D + 2) >= kMaxGroups + 2, "room for a join");
