@@ -25,7 +25,8 @@ struct AdaptersArgs {
     float *h;             // workspace, [slices][M][R]
     int slices, columns;  // of K, 32 inputs each
     int shares, tiles;    // workgroups that share a group's adapters, and the tiles of tokens of each
-    int blocks;           // of ranks (first launch), of outputs (second)
+    int blocks;           // of ranks (first launch)
+    int turns;            // workgroups that share the outputs (second)
 };
 
 // The adapter of a lane's token, -1: none.
@@ -184,134 +185,171 @@ __device__ __forceinline__ void store_results(void *p, int dtype, int64_t at, co
     }
 }
 
-// Results of a group's tokens, NT tiles of sixteen outputs per wave, outputs the rows of a product and tokens its
-// columns.  Row 4 q + j of tile t is output 4 NT q + 4 t + j, so that a lane has 4 NT outputs side by side.
+// Results of a group's tokens, NT tiles of sixteen outputs per wave and turn, outputs the rows of a product and tokens its
+// columns.  Row 4 q + j of tile t is output 4 NT q + 4 t + j, so that a lane has 4 NT outputs side by side.  A workgroup
+// takes blocks of outputs in turn with the h that it has split once, the next block's weights asked for before this
+// one's results are stored.
 template <int NT>
 __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
     constexpr int kPitch = NVQ_MAX_RANK + 8;  // (16 bytes more than a row, against bank conflicts)
+    constexpr int kBlock = kWaves * 16 * NT;
     __shared__ __align__(16) uint16_t hs[3][kTile][kPitch];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4;
-    const int block0 = (int)(blockIdx.x % g.blocks) * kWaves * 16 * NT;
-    const int n0 = block0 + w * 16 * NT;  // (past the last output: nothing is stored)
-    int i = blockIdx.x / g.blocks;
+    const int first = (int)(blockIdx.x % g.turns) * kBlock, stride = g.turns * kBlock;
+    int i = blockIdx.x / g.turns;
     const int tile = i % g.tiles;
     i /= g.tiles;
-    const int share = i % g.shares, m0 = i / g.shares * kGroup;
+    const int all = g.shares + (g.out != g.y);  // (the last: tokens without an adapter, which stay as they are)
+    const int share = i % all, m0 = i / all * kGroup;
     const int mine = adapter_of(g, m0);
     uint64_t left = __ballot(mine >= 0);
-    const int o0 = n0 + 4 * NT * kb;  // the lane's outputs
-    const int64_t h_slice = (int64_t)g.M * g.R;
-    const bool whole = o0 + 4 * NT <= g.N;
-    if (share == 0 && g.out != g.y) {  // tokens without an adapter: as they are
+    if (share == g.shares) {
         uint64_t none = ~left;
         if (g.M - m0 < kGroup) none &= (1ull << (g.M - m0)) - 1;
-        for (int k = 0; none; ++k, none &= none - 1) {
-            if (k % g.tiles != tile) continue;
-            const int64_t row = (int64_t)(m0 + __builtin_ctzll(none)) * g.N;
-            for (int o = block0 + (int)threadIdx.x; o < block0 + kWaves * 16 * NT && o < g.N; o += kThreads) {
-                if (g.dtype == NVQ_F32)
-                    static_cast<uint32_t *>(g.out)[row + o] = static_cast<const uint32_t *>(g.y)[row + o];
-                else
-                    static_cast<uint16_t *>(g.out)[row + o] = static_cast<const uint16_t *>(g.y)[row + o];
+        const int count = __builtin_popcountll(none);
+        for (int k0 = tile; k0 < count; k0 += 8 * g.tiles) {
+            int64_t row[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int at = k0 + k * g.tiles;
+                row[k] = at < count ? (int64_t)(m0 + nth_bit(none, at)) * g.N : -1;
             }
+            for (int block = first; block < g.N; block += stride)
+                for (int o = block + (int)threadIdx.x; o < block + kBlock && o < g.N; o += kThreads) {
+                    uint32_t v[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if (row[k] < 0) continue;
+                        v[k] = g.dtype == NVQ_F32 ? static_cast<const uint32_t *>(g.y)[row[k] + o] : static_cast<const uint16_t *>(g.y)[row[k] + o];
+                    }
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if (row[k] < 0) continue;
+                        if (g.dtype == NVQ_F32)
+                            static_cast<uint32_t *>(g.out)[row[k] + o] = v[k];
+                        else
+                            static_cast<uint16_t *>(g.out)[row[k] + o] = (uint16_t)v[k];
+                    }
+                }
         }
+        return;
     }
+    const int64_t h_slice = (int64_t)g.M * g.R;
     for (int at = 0; left; ++at) {
         int e;
         const uint64_t with = turn(mine, &left, &e);
         if (at % g.shares != share) continue;
         const int tokens = __builtin_popcountll(with);
         if (tile * kTile >= tokens) continue;
-        const uint16_t *b[NT];
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const int o = n0 + 4 * NT * (n >> 2) + 4 * t + (n & 3);
-            b[t] = g.b + ((int64_t)e * g.N + (o < g.N ? o : g.N - 1)) * g.R + 8 * kb;
-        }
-        // The weights of two columns of 32 ranks at a time, those of the first two and y asked for before h is there.
+        // The weights of two columns of 32 ranks at a time.
         uint4v bw[2][NT];
-        auto load = [&](int c) {
+        auto load = [&](int block, int c) {
+            const int n0 = block + w * 16 * NT + 4 * NT * (n >> 2) + (n & 3);
+            const uint16_t *const b = g.b + (int64_t)e * g.N * g.R;
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+            for (int t = 0; t < NT; ++t) {
+                const int o = n0 + 4 * t < g.N ? n0 + 4 * t : g.N - 1;
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    bw[k][t] = uint4v{0, 0, 0, 0};
-                    if (c + 32 * k + 8 * kb < g.R) bw[k][t] = *as_global<uint4v>(b[t] + c + 32 * k);
+                for (int k = 0; k < 2; ++k) {
+                    const int r = c + 32 * k + 8 * kb;  // (past the last rank h is zero: any weight of the row will do that is there)
+                    bw[k][t] = *as_global<uint4v>(b + (int64_t)o * g.R + (r < g.R ? r : 0));
+                    if (r >= g.R) bw[k][t] = uint4v{0, 0, 0, 0};
                 }
+            }
         };
-        load(0);
+        load(first, 0);
         const float scale = g.scales ? g.scales[e] : 1.0f;
         for (int k0 = tile * kTile; k0 < tokens; k0 += kTile * g.tiles) {
             const bool my = k0 + n < tokens;
-            const int64_t at_y = (int64_t)(m0 + nth_bit(with, my ? k0 + n : k0)) * g.N + o0;
+            const int64_t row = (int64_t)(m0 + nth_bit(with, my ? k0 + n : k0)) * g.N;
             float y[4 * NT];
-            float4v sum[NT];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) sum[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-            if (my && whole) load_results<4 * NT>(g.y, g.dtype, at_y, y);
+            auto load_y = [&](int block) {
+                const int o0 = block + w * 16 * NT + 4 * NT * kb;
+                if (my && o0 + 4 * NT <= g.N) load_results<4 * NT>(g.y, g.dtype, row + o0, y);
+            };
+            load_y(first);
             __syncthreads();
-            for (int u = threadIdx.x; u < kTile * g.R; u += kThreads) {
-                const int k = u / g.R, r = u - k * g.R;
+            // four ranks of a token per thread
+            const int fours = g.R / 4;
+            for (int u = threadIdx.x; u < kTile * fours; u += kThreads) {
+                const int k = u / fours, r = 4 * (u - k * fours);
                 if (k0 + k >= tokens) break;  // (the columns of no token are not looked at)
                 const float *const h = g.h + (int64_t)(m0 + nth_bit(with, k0 + k)) * g.R + r;
-                float v = 0.0f;
-                for (int s0 = 0; s0 < g.slices; s0 += 8) {
-                    float part[8];
+                float4v v = {0.0f, 0.0f, 0.0f, 0.0f};
+                constexpr int kAtOnce = 8;  // (sixteen take registers that a third workgroup needs: 20 us for 15 of 32 tokens)
+                for (int s0 = 0; s0 < g.slices; s0 += kAtOnce) {
+                    float4v part[kAtOnce];
 #pragma unroll
-                    for (int s = 0; s < 8; ++s) part[s] = h[(s0 + s < g.slices ? s0 + s : 0) * h_slice];
+                    for (int s = 0; s < kAtOnce; ++s) part[s] = *as_global<float4v>(h + (s0 + s < g.slices ? s0 + s : 0) * h_slice);
 #pragma unroll
-                    for (int s = 0; s < 8; ++s) v += s0 + s < g.slices ? part[s] : 0.0f;
+                    for (int s = 0; s < kAtOnce; ++s)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[j] += s0 + s < g.slices ? part[s][j] : 0.0f;
                 }
-                uint32_t hi, mid, lo;
-                split(v, &hi, &mid, &lo);
-                hs[0][k][r] = (uint16_t)hi;
-                hs[1][k][r] = (uint16_t)mid;
-                hs[2][k][r] = (uint16_t)lo;
+                uint32_t p[4][3];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) split(v[j], &p[j][0], &p[j][1], &p[j][2]);
+#pragma unroll
+                for (int q = 0; q < 3; ++q)
+                    *reinterpret_cast<uint2v *>(&hs[q][k][r]) = uint2v{p[0][q] | p[1][q] << 16, p[2][q] | p[3][q] << 16};
             }
             __syncthreads();
-            for (int c = 0; c < g.R; c += 64) {
-                if (c > 0 || (k0 >= kTile * g.tiles && g.R > 64)) load(c);  // (others are there)
+            if (k0 >= kTile * g.tiles) load(first, 0);  // (of the first tile it is there)
+            for (int block = first; block < g.N; block += stride) {
+                const int o0 = block + w * 16 * NT + 4 * NT * kb;  // the lane's outputs
+                const bool whole = o0 + 4 * NT <= g.N;
+                const int64_t at_y = row + o0;
+                float4v sum[NT];
 #pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int r = c + 32 * k + 8 * kb;
+                for (int t = 0; t < NT; ++t) sum[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+                for (int c = 0; c < g.R; c += 64) {
+                    if (c > 0) load(block, c);
 #pragma unroll
-                    for (int q = 0; q < 3; ++q) {
-                        uint4v hw = {0, 0, 0, 0};
-                        if (r < g.R) hw = *reinterpret_cast<const uint4v *>(&hs[q][n][r]);
+                    for (int k = 0; k < 2; ++k) {
+                        const int r = c + 32 * k + 8 * kb;
 #pragma unroll
-                        for (int t = 0; t < NT; ++t)
-                            sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bw[k][t]),
-                                                                            __builtin_bit_cast(bf16x8, hw), sum[t], 0, 0, 0);
+                        for (int q = 0; q < 3; ++q) {
+                            uint4v hw = {0, 0, 0, 0};
+                            if (r < g.R) hw = *reinterpret_cast<const uint4v *>(&hs[q][n][r]);
+#pragma unroll
+                            for (int t = 0; t < NT; ++t)
+                                sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bw[k][t]),
+                                                                                __builtin_bit_cast(bf16x8, hw), sum[t], 0, 0, 0);
+                        }
                     }
                 }
-            }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) wait_written(sum[t]);
-            if (my && whole) {
+                for (int t = 0; t < NT; ++t) wait_written(sum[t]);
+                const int next = block + stride;
+                if (next < g.N) load(next, 0);
+                if (my && whole) {
+                    float v[4 * NT];
 #pragma unroll
-                for (int j = 0; j < 4 * NT; ++j) y[j] += sum[j >> 2][j & 3] * scale;
-                store_results<4 * NT>(g.out, g.dtype, at_y, y);
-            } else if (my) {
+                    for (int j = 0; j < 4 * NT; ++j) v[j] = y[j] + sum[j >> 2][j & 3] * scale;
+                    if (next < g.N) load_y(next);
+                    store_results<4 * NT>(g.out, g.dtype, at_y, v);
+                } else if (my) {
 #pragma unroll
-                for (int j = 0; j < 4 * NT; ++j)
-                    if (o0 + j < g.N) {
-                        const float v = g.dtype == NVQ_F32 ? static_cast<const float *>(g.y)[at_y + j]
-                                                           : bf16_bits_to_float(static_cast<const uint16_t *>(g.y)[at_y + j]);
-                        store_global(g.out, g.dtype, at_y + j, v + sum[j >> 2][j & 3] * scale);
-                    }
+                    for (int j = 0; j < 4 * NT; ++j)
+                        if (o0 + j < g.N) {
+                            const float v = g.dtype == NVQ_F32 ? static_cast<const float *>(g.y)[at_y + j]
+                                                               : bf16_bits_to_float(static_cast<const uint16_t *>(g.y)[at_y + j]);
+                            store_global(g.out, g.dtype, at_y + j, v + sum[j >> 2][j & 3] * scale);
+                        }
+                }
             }
         }
     }
 }
 
-// Groups of a batch, and the workgroups to one of them: each distinct adapter its own where there are few groups, each
-// tile of an adapter's tokens its own in any case.
+// Groups of a batch, and the workgroups to one of them: each distinct adapter its own where there are few groups; where
+// there are several, each tile of an adapter's tokens its own (in one group the weights are read once for all tiles).
 int groups_of(int M) { return (M + kGroup - 1) / kGroup; }
 int shares_of(int M, int n) {
     const int most = n < kGroup ? n : kGroup;
     return groups_of(M) <= 4 ? (M < most ? M : most) : 1;
 }
-int tiles_of(int M) { return M < kGroup ? (M + kTile - 1) / kTile : kGroup / kTile; }
+int tiles_of(int M) { return M <= kGroup ? 1 : kGroup / kTile; }
 // Blocks of 64, 32 or 16 ranks.
 int rank_tiles(int R) { return R > 32 ? 4 : R > 16 ? 2 : 1; }
 int rank_blocks(int R) { return (R + 16 * rank_tiles(R) - 1) / (16 * rank_tiles(R)); }
@@ -387,9 +425,13 @@ extern "C" int nvq_adapters_add(const nvq_adapters *adapters, const uint16_t *x_
         hipLaunchKernelGGL(adapters_down_kernel<4>, down, block, 0, st, g);
     NVQ_HIP_TRY(hipGetLastError());
     const bool wide = (int64_t)(M < g.shares ? M : g.shares) * g.N >= 1024 * 64 || (int64_t)groups_of(M) * g.tiles * g.N >= 1024 * 64;  // a wave to 64 outputs where that leaves four a compute unit
-    const int per = (wide ? 64 : 16) * kWaves;
-    g.blocks = (g.N + per - 1) / per;
-    const dim3 up((unsigned)(groups * g.blocks));
+    const int per = (wide ? 64 : 16) * kWaves, blocks = (g.N + per - 1) / per;
+    // As many as the device holds at once (three a compute unit) between those with work: each adapter or tile of tokens.
+    const int busy = (M + kTile - 1) / kTile > g.shares ? (M + kTile - 1) / kTile : g.shares, resident = 3 * device_cu_count() / busy;
+    const int copies = out != y ? groups_of(M) * g.tiles : 0;
+    const int each = resident < 1 ? blocks : (blocks + resident - 1) / resident;
+    g.turns = (blocks + each - 1) / each;
+    const dim3 up((unsigned)((groups + copies) * g.turns));
     if (wide)
         hipLaunchKernelGGL(adapters_up_kernel<4>, up, block, 0, st, g);
     else
