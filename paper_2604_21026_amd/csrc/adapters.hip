@@ -4,7 +4,8 @@
 // distinct adapters of its tokens, and the tokens of one adapter, wherever they stand in the group, are sixteen to a
 // product: an adapter's weights are read once per group however its tokens lie, and 64 tokens of 64 adapters read what
 // they have to.  h stays fp32 between the launches, in as many partial sums as K is cut into; it enters the second
-// product as three bf16 values whose sum it is, so nothing of it is lost.
+// product as three bf16 values whose sum it is, so nothing of it is lost; the products with the first and with the rest are
+// summed apart and added at the end, where what an infinite weight makes of a rest of zero is left out.
 #include "mfma_act.h"
 
 namespace nvq {
@@ -299,9 +300,9 @@ __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
                 const int o0 = block + w * 16 * NT + 4 * NT * kb;  // the lane's outputs
                 const bool whole = o0 + 4 * NT <= g.N;
                 const int64_t at_y = row + o0;
-                float4v sum[NT];
+                float4v sum[NT], rest[NT];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) sum[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+                for (int t = 0; t < NT; ++t) sum[t] = rest[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
                 for (int c = 0; c < g.R; c += 64) {
                     if (c > 0) load(block, c);
 #pragma unroll
@@ -312,14 +313,20 @@ __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
                             uint4v hw = {0, 0, 0, 0};
                             if (r < g.R) hw = *reinterpret_cast<const uint4v *>(&hs[q][n][r]);
 #pragma unroll
-                            for (int t = 0; t < NT; ++t)
-                                sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bw[k][t]),
-                                                                                __builtin_bit_cast(bf16x8, hw), sum[t], 0, 0, 0);
+                            for (int t = 0; t < NT; ++t) {
+                                float4v &to = q ? rest[t] : sum[t];
+                                to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bw[k][t]),
+                                                                             __builtin_bit_cast(bf16x8, hw), to, 0, 0, 0);
+                            }
                         }
                     }
                 }
 #pragma unroll
-                for (int t = 0; t < NT; ++t) wait_written(sum[t]);
+                for (int t = 0; t < NT; ++t) wait_written(sum[t], rest[t]);
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) sum[t][j] += __builtin_isfinite(sum[t][j]) ? rest[t][j] : 0.0f;
                 const int next = block + stride;
                 if (next < g.N) load(next, 0);
                 if (my && whole) {

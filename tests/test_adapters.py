@@ -119,3 +119,24 @@ def test_adapters_of_tokens_without_a_number():
             assert np.isposinf(got[m]).all()
         else:
             assert np.isfinite(got[m]).all()
+
+
+@gpu
+@pytest.mark.parametrize("M,N", [(3, 50), (20, 5000)])
+def test_adapters_of_infinite_weights(M, N):
+    """An infinite weight makes its output infinite, whatever the bits of what it meets; a zero that it meets makes it NaN."""
+    n, K, R = 2, 64, 16
+    a, b, x = (torch.ones(s, dtype=torch.bfloat16) for s in ((n, R, K), (n, N, R), (M, K)))
+    a[:, 1] = 0
+    a[:, 2] = 1 / 3  # (sums that take more than eight bits)
+    b[0, 5, 0], b[0, 6, 2], b[0, 7, 1], b[1, N - 1, 3] = float("inf"), -float("inf"), float("inf"), -float("inf")
+    ids = torch.arange(M, dtype=torch.int32) % n
+    for dtype in (torch.float32, torch.bfloat16):
+        got = f64(nvq.adapters_add(nvq.Adapters(a.to(DEV), b.to(DEV)), x.to(DEV), ids.to(DEV), torch.ones((M, N), dtype=dtype, device=DEV)))
+        for m in range(M):
+            at = [5, 6, 7] if m % n == 0 else [N - 1]
+            assert np.isfinite(np.delete(got[m], at)).all()
+            if m % n == 0:
+                assert np.isposinf(got[m, 5]) and np.isneginf(got[m, 6]) and np.isnan(got[m, 7])
+            else:
+                assert np.isneginf(got[m, N - 1])
