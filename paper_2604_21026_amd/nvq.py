@@ -218,6 +218,13 @@ def _here(t: torch.Tensor, dtype, name: str, n: int = 0) -> int:
     return at
 
 
+def _int(n, name: str) -> int:
+    """A number as the library takes it (ctypes would drop its upper bits)."""
+    if not -1 << 31 <= int(n) < 1 << 31:
+        raise ValueError("%s is out of range" % name)
+    return int(n)
+
+
 def _space(t: torch.Tensor, nbytes: int, name: str) -> int:
     """The address of a contiguous device tensor of any type with room for that many bytes."""
     return _dev(t, t.dtype, name, -(-nbytes // t.element_size()))
@@ -852,7 +859,7 @@ def cache_append(cache: Cache, table: torch.Tensor, positions: torch.Tensor, k: 
     _check(lib().nvq_cache_append(*where, qa, qs, H, to, ka, ks, va, vs,
                                   None if cos_sin is None else _here(cos_sin, torch.float32, "cos_sin"),
                                   0 if cos_sin is None else cos_sin.shape[0], 0 if cos_sin is None else cos_sin.shape[1],
-                                  int(interleaved), _stream()), "nvq_cache_append")
+                                  _int(interleaved, "interleaved"), _stream()), "nvq_cache_append")
     return out
 
 
@@ -900,7 +907,7 @@ def attention(cache: Cache, q: torch.Tensor, table: torch.Tensor, lengths: torch
         workspace = cache.workspace(B, H)
     _check(lib().nvq_attention(cache.address, qa, qs, H, _here(table, torch.int32, "table"), B, table.shape[1],
                                _here(lengths, torch.int32, "lengths"), D ** -0.5 if scale is None else float(scale),
-                               int(window), float(softcap), _here(y, y.dtype, "out", B * H * D), _y_dtype(y.dtype),
+                               _int(window, "window"), float(softcap), _here(y, y.dtype, "out", B * H * D), _y_dtype(y.dtype),
                                None if lse is None else _here(lse, torch.float32, "lse", B * H),
                                _here(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()), "nvq_attention")
     return y
@@ -930,7 +937,7 @@ def sample(logits: torch.Tensor, u: torch.Tensor, temperature: Optional[torch.Te
         raise ValueError("logits must be a device tensor [M,V], a row's values side by side")
     if logits.get_device() != torch.cuda.current_device():
         raise ValueError("logits is on device %d, the current device is %d" % (logits.get_device(), torch.cuda.current_device()))
-    M, V = logits.shape
+    M, V = logits.shape[0], _int(logits.shape[1], "logits")
     ids = out if out is not None else torch.empty((M,), dtype=torch.int32, device=logits.device)
     if workspace is None:
         workspace = sample_workspace(M, V, logits.device)
@@ -954,7 +961,7 @@ class Adapters:
         if any(t is not None and t.device != a.device for t in self.keep):
             raise ValueError("tensors on different devices")
         self.n, self.R, self.K = a.shape
-        self.N, self.device, self.index = b.shape[1], a.device, a.device.index
+        self.N, self.device, self.index = _int(b.shape[1], "b"), a.device, a.device.index
         self.struct = AdaptersStruct(_dev(a, torch.bfloat16, "a"), _dev(b, torch.bfloat16, "b"),
                                      None if scales is None else _dev(scales, torch.float32, "scales"),
                                      self.n, self.K, self.N, self.R)
