@@ -11,6 +11,8 @@
 // Weights are 64-bit fixed point relative to the largest, so that sums do not depend on their order.  A row whose bins
 // hold too many tokens (nearly equal logits), or whose logits are out of the bins' range, is looked at by one workgroup
 // alone, eight bits of the sort words after the other (choose_slowly, in the second launch).
+#include <type_traits>
+
 #include "mfma_act.h"
 
 namespace nvq {
@@ -23,7 +25,6 @@ constexpr double kOne = (double)(1ull << kPoint);
 
 struct SampleArgs {
     const void *logits;
-    int dtype;
     int64_t ld;
     int M, V;
     const float *u, *temperature, *top_p, *min_p;
@@ -46,19 +47,36 @@ __device__ __forceinline__ float of_sort_word(uint32_t w) {
     return __uint_as_float(w & 0x80000000u ? w & 0x7fffffffu : ~w);
 }
 
+// (The type is a template's: a branch on it at every load made the compiler wait for each before the next.)
+template <bool BF16>
 struct Row {
-    const void *at;
-    int dtype, V;
+    typedef std::conditional_t<BF16, uint16_t, float> Value;
+    const Value *at;
+    int V;
+    __device__ Row(const SampleArgs &a, int m) : at(static_cast<const Value *>(a.logits) + m * a.ld), V(a.V) {}
     __device__ float logit(int i) const {
-        return dtype == NVQ_F32 ? *as_global<float>(static_cast<const float *>(at) + i)
-                                : bf16_bits_to_float(*as_global<uint16_t>(static_cast<const uint16_t *>(at) + i));
+        const Value v = *as_global<Value>(at + i);
+        if constexpr (BF16)
+            return bf16_bits_to_float(v);
+        else
+            return v;
     }
     __device__ uint32_t word(int i) const { return sort_word(logit(i)); }
+    // Logits b + tid + 1024 j, those past `end` minus infinity (the first is loaded there: no load behind a branch).
+    __device__ void load(int b, int end, float (&to)[8]) const {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = b + j * 1024 + (int)threadIdx.x;
+            to[j] = logit(i < end ? i : 0);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) to[j] = b + j * 1024 + (int)threadIdx.x < end ? to[j] : -INFINITY;
+    }
 };
 
 // exp(x) as fixed point, x = (logit - top) / temperature <= 0: 2^(k / 64), its fraction from a table, times the
 // exponential series of the rest, |rest| <= ln 2 / 128, to six terms (the next is 4e-17 of the sum; without the table it
-// takes thirteen, and the weights of a row of 128256 in sixteen parts 4.4 us instead of XX).
+// takes thirteen, and the weights of a row of 128256 in sixteen parts 4.4 us instead of 3.1).
 constexpr int kRoots = 64;
 __constant__ const double kRoot[kRoots] = {
     1.0, 1.0108892860517005, 1.0218971486541166, 1.0330248790212284, 1.0442737824274138, 1.0556451783605572,
@@ -103,28 +121,89 @@ struct Shared {
     uint32_t bin;
 };
 
-template <typename OP>
-__device__ uint64_t over_block(unsigned long long *wave, uint64_t v, OP op) {
-    for (int d = 32; d; d >>= 1) v = op(v, (uint64_t)__shfl_xor((unsigned long long)v, d));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) wave[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = wave[0];
-#pragma unroll
-    for (int i = 1; i < kSampleWaves; ++i) v = op(v, (uint64_t)wave[i]);
-    return v;
+// ---- over a wave and over the workgroup, by moves between lanes (shuffles go through LDS: 16 waves of six 64-bit steps
+// and sixteen reads each took about 1.2 us where these take 0.5)
+struct MaxU32 {
+    __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return a > b ? a : b; }
+};
+struct MinU32 {
+    __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return a < b ? a : b; }
+};
+template <int LANES, typename OP>  // 16 or 64
+__device__ __forceinline__ uint32_t over_lanes(uint32_t v, OP op) {
+    if constexpr (LANES == 64) {
+        v = with_lane_xor<32>(v, op);
+        v = with_lane_xor<16>(v, op);
+    }
+    v = with_lane_xor<8>(v, op);
+    v = with_lane_xor<4>(v, op);
+    v = with_lane_xor<2>(v, op);
+    return with_lane_xor<1>(v, op);
 }
-struct Most64 {
-    __device__ uint64_t operator()(uint64_t a, uint64_t b) const { return a > b ? a : b; }
+// The lane's value N lanes before it in its row of sixteen, 0 for the first N.
+template <int N, typename T>
+__device__ __forceinline__ T row_up(T v) {
+    if constexpr (sizeof(T) == 8) {
+        const uint32_t lo = row_up<N>((uint32_t)v), hi = row_up<N>((uint32_t)((uint64_t)v >> 32));
+        return (T)((uint64_t)hi << 32 | lo);
+    } else {
+        return (T)__builtin_amdgcn_update_dpp(0, (int)v, 0x110 | N, 0xf, 0xf, true);
+    }
+}
+template <typename T>
+__device__ __forceinline__ T of_lane(T v, int lane) {  // (a lane that all have in common)
+    if constexpr (sizeof(T) == 8)
+        return (T)((uint64_t)of_lane((uint32_t)((uint64_t)v >> 32), lane) << 32 | of_lane((uint32_t)v, lane));
+    else
+        return (T)__builtin_amdgcn_readlane((int)v, lane);
+}
+// Sum up to and with each lane, in its row of sixteen and in the wave.
+template <typename T>
+__device__ __forceinline__ T scan_row(T v) {
+    v += row_up<1>(v);
+    v += row_up<2>(v);
+    v += row_up<4>(v);
+    return v + row_up<8>(v);
+}
+template <typename T>
+__device__ __forceinline__ T scan_wave(T v) {
+    v = scan_row(v);
+    const T r0 = of_lane(v, 15), r1 = of_lane(v, 31), r2 = of_lane(v, 47);
+    const int lane = threadIdx.x & 63;
+    return v + (lane >= 16 ? r0 : 0) + (lane >= 32 ? r1 : 0) + (lane >= 48 ? r2 : 0);
+}
+// Sum over the threads before this one; *all: over all.  By the first W waves.
+template <int W, typename T>
+__device__ __forceinline__ T scan_block(T *wave, T v, T *all) {
+    const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const T sum = scan_wave(v);
+    __syncthreads();
+    if (lane == 63) wave[w] = sum;
+    __syncthreads();
+    const T waves = scan_row(wave[(lane & 15) < W ? lane & 15 : W - 1]);
+    *all = of_lane(waves, W - 1);
+    return (w ? of_lane(waves, w ? w - 1 : 0) : 0) + sum - v;
+}
+__device__ uint64_t sum_block(unsigned long long *wave, uint64_t v) {
+    unsigned long long all;
+    scan_block<kSampleWaves>(wave, (unsigned long long)v, &all);
+    return all;
+}
+
+// The first token of a row or a part of it: sort word and index.  Of a wave, or of sixteen lanes that lie side by side.
+struct First {
+    uint32_t word, index;
 };
-struct Add64 {
-    __device__ uint64_t operator()(uint64_t a, uint64_t b) const { return a + b; }
-};
+template <int LANES>
+__device__ __forceinline__ First first_of(First f) {
+    const uint32_t top = over_lanes<LANES>(f.word, MaxU32());
+    return First{top, over_lanes<LANES>(f.word == top ? f.index : ~0u, MinU32())};
+}
 
 // The token at which the running count (or sum of weights) of the descending order first exceeds x: its word, and the
 // count (sum) before all tokens of that word.  x is below the row's whole count (sum).
-template <bool MASS>
-__device__ void find(Shared &s, const Row &row, const Weights &w, uint64_t x, uint32_t *word, uint64_t *before) {
+template <bool MASS, typename ROW>
+__device__ void find(Shared &s, const ROW &row, const Weights &w, uint64_t x, uint32_t *word, uint64_t *before) {
     uint32_t prefix = 0;
     uint64_t base = 0;
     for (int shift = 24; shift >= 0; shift -= 8) {
@@ -163,7 +242,8 @@ __device__ void find(Shared &s, const Row &row, const Weights &w, uint64_t x, ui
 }
 
 // The n-th token (from 0, by index) of a word; -1 if there are fewer.
-__device__ int nth_of_word(Shared &s, const Row &row, uint32_t word, uint64_t n) {
+template <typename ROW>
+__device__ int nth_of_word(Shared &s, const ROW &row, uint32_t word, uint64_t n) {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int part = (row.V + kSampleThreads - 1) / kSampleThreads * 64;  // of a wave, in one piece
     const int i0 = w * part, i1 = i0 + part < row.V ? i0 + part : row.V;
@@ -197,22 +277,11 @@ struct Ask {
     float temperature, top_p, min_p, u;
     int top_k;
 };
+// (What is not given is read from u instead, so that no load stands behind a branch.)
 __device__ __forceinline__ Ask ask_of(const SampleArgs &a, int m) {
-    Ask k;
-    k.temperature = a.temperature ? a.temperature[m] : 1.0f;
-    k.top_k = a.top_k ? a.top_k[m] : 0;
-    k.top_p = a.top_p ? a.top_p[m] : 1.0f;
-    k.min_p = a.min_p ? a.min_p[m] : 0.0f;
-    k.u = a.u[m];
-    return k;
-}
-__device__ __forceinline__ Row row_of(const SampleArgs &a, int m) {
-    Row r;
-    r.at = a.dtype == NVQ_F32 ? (const void *)(static_cast<const float *>(a.logits) + m * a.ld)
-                              : (const void *)(static_cast<const uint16_t *>(a.logits) + m * a.ld);
-    r.dtype = a.dtype;
-    r.V = a.V;
-    return r;
+    const float t = (a.temperature ? a.temperature : a.u)[m], p = (a.top_p ? a.top_p : a.u)[m], q = (a.min_p ? a.min_p : a.u)[m];
+    const int k = (a.top_k ? a.top_k : reinterpret_cast<const int32_t *>(a.u))[m];
+    return Ask{a.temperature ? t : 1.0f, a.top_p ? p : 1.0f, a.min_p ? q : 0.0f, a.u[m], a.top_k ? k : 0};
 }
 // Where in a kept sum the random number points.
 __device__ __forceinline__ uint64_t point_of(float u, uint64_t kept) {
@@ -226,7 +295,8 @@ __device__ __forceinline__ uint64_t reach_of(float top_p, uint64_t all) {
 }
 
 // The answer for a row of n tokens to choose from, by one workgroup and any logits.
-__device__ int choose_slowly(Shared &s, const Row &row, const Ask &k, float most, uint64_t n) {
+template <typename ROW>
+__device__ int choose_slowly(Shared &s, const ROW &row, const Ask &k, float most, uint64_t n) {
     const Weights w(most, k.temperature, kRoot);
     uint32_t word;
     uint64_t before, kept;
@@ -237,14 +307,14 @@ __device__ int choose_slowly(Shared &s, const Row &row, const Ask &k, float most
             const uint32_t v = row.word(i);
             above += v > word ? w.of_word(v) : 0;
         }
-        kept = over_block(s.wave, above, Add64()) + ((uint64_t)k.top_k - before) * w.of_word(word);
+        kept = sum_block(s.wave, above) + ((uint64_t)k.top_k - before) * w.of_word(word);
     } else {
         uint64_t all = 0;
         for (int i = threadIdx.x; i < row.V; i += kSampleThreads) {
             const uint32_t v = row.word(i);
             all += v ? w.of_word(v) : 0;
         }
-        kept = over_block(s.wave, all, Add64());
+        kept = sum_block(s.wave, all);
     }
     if (!(k.top_p >= 1.0f)) {
         const uint64_t reach = reach_of(k.top_p, kept);
@@ -259,7 +329,7 @@ __device__ int choose_slowly(Shared &s, const Row &row, const Ask &k, float most
             const uint64_t x = v ? w.of_word(v) : 0;
             enough += (double)x >= (double)k.min_p * kOne ? x : 0;
         }
-        enough = over_block(s.wave, enough, Add64());
+        enough = sum_block(s.wave, enough);
         kept = enough < kept ? enough : kept;
     }
     kept = kept < 1ull << kPoint ? 1ull << kPoint : kept;  // (the first token's weight is 1)
@@ -280,12 +350,13 @@ static_assert(NVQ_SAMPLE_CLEAR_BYTES >= 4 * NVQ_SAMPLE_MAX_M, "a counter per row
 struct Grid {
     float steps, top;  // top: the largest logit's number
     __device__ static float steps_of(float temperature) { return 32.0f / (temperature < 1.0f ? temperature : 1.0f); }
-    __device__ static float number(float logit, float steps) { return fmaxf(floorf(logit * steps), -kFar); }
+    __device__ static float number(float logit, float steps) { return fminf(fmaxf(floorf(logit * steps), -kFar), kFar); }
     __device__ int bin(float logit) const { return (int)fminf(fmaxf(top - number(logit, steps), 0.0f), (float)(kBins - 1)); }
 };
 
+// Of a part: its first token, and its bins, each at its number modulo kBins, which is the same place for every part.
 struct PartHead {
-    unsigned long long best;  // sort word and complement of the index of the part's first token; 0: none
+    unsigned long long first;  // sort word (0: none) and index
 };
 struct PartBins {
     double mass[kBins];  // relative to the part's largest
@@ -314,65 +385,6 @@ __device__ __forceinline__ uint64_t get64(const unsigned long long *p) {
 __device__ __forceinline__ void put32(uint32_t *p, uint32_t v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ uint32_t get32(const uint32_t *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-// Sum over the threads before this one; *all: over all.
-template <int W, typename T>
-__device__ T scan_block(T *wave, T v, T *all) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    T sum = v;
-    for (int d = 1; d < 64; d <<= 1) {
-        const T o = __shfl_up(sum, d);
-        if (lane >= d) sum += o;
-    }
-    __syncthreads();
-    if (lane == 63) wave[w] = sum;
-    __syncthreads();
-    T before = 0, total = 0;
-#pragma unroll
-    for (int i = 0; i < W; ++i) {
-        const T x = wave[i];
-        before += i < w ? x : 0;
-        total += x;
-    }
-    *all = total;
-    return before + sum - v;
-}
-
-// Both at once, one value per thread.
-__device__ void scan_pair(unsigned long long *wave64, uint32_t *wave32, uint64_t v, uint32_t c, uint64_t *before, uint32_t *ranked,
-                          uint64_t *all, uint32_t *n) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-    uint64_t sum = v;
-    uint32_t num = c;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t o = __shfl_up((unsigned long long)sum, d);
-        const uint32_t p = __shfl_up(num, d);
-        if (lane >= d) {
-            sum += o;
-            num += p;
-        }
-    }
-    __syncthreads();
-    if (lane == 63) {
-        wave64[w] = sum;
-        wave32[w] = num;
-    }
-    __syncthreads();
-    uint64_t b = 0, t = 0;
-    uint32_t r = 0, u = 0;
-#pragma unroll
-    for (int i = 0; i < kSampleWaves; ++i) {
-        b += i < w ? wave64[i] : 0;
-        r += i < w ? wave32[i] : 0;
-        t += wave64[i];
-        u += wave32[i];
-    }
-    *before = b + sum - v;
-    *ranked = r + num - c;
-    *all = t;
-    *n = u;
-}
-
 // Tokens in ranges of bins, of the bins before b; lo and hi: ranges in ascending order that share no bin.
 __device__ __forceinline__ uint32_t listed_before(const int *lo, const int *hi, const uint32_t *ranked, int b) {
     uint32_t n = 0;
@@ -391,15 +403,16 @@ struct Search {
 __device__ Search search(const Ask &k, const Grid &grid, float most, const unsigned long long *before, const uint32_t *ranked) {
     const int lane = threadIdx.x & 63;
     constexpr int kSkip = kBins / 64;
-    // The first bin for which `is` holds, as it does for all that follow; the last one if there is none.
-    auto first_bin = [&](auto is) {
-        const uint64_t some = __ballot(is(kSkip * lane + kSkip - 1));
+    // The first bin with which what is counted reaches x, or the last one: the lane's sixteen bins, then the bin of those.
+    auto reached = [&](auto x, auto upto, const auto *counted) {
+        const uint64_t some = __ballot(upto >= x);
         const int b0 = some ? kSkip * __builtin_ctzll(some) : kBins - kSkip;
-        const uint64_t any = __ballot(lane < kSkip && is(b0 + (lane < kSkip ? lane : 0)));
+        const uint64_t any = __ballot(lane < kSkip && (decltype(upto))counted[b0 + 1 + (lane & (kSkip - 1))] >= x);
         return any ? b0 + __builtin_ctzll(any) : kBins - 1;
     };
-    // The first bin with which the sum reaches x.
-    auto reaching = [&](double x) { return first_bin([&](int b) { return (double)before[b + 1] >= x; }); };
+    const double upto = (double)before[kSkip * lane + kSkip];
+    const uint32_t ranks = ranked[kSkip * lane + kSkip];
+    auto reaching = [&](double x) { return reached(x, upto, before); };
     // Bounds of the sums are a little wide: a bin's weight has been rounded otherwise than the sum of its tokens'.
     const double wide = 1.0 + 0x1p-30, all = (double)before[kBins];
     double least = all, greatest = all;
@@ -414,7 +427,7 @@ __device__ Search search(const Ask &k, const Grid &grid, float most, const unsig
     }
     r.cut = 0;
     if (k.top_k > 0 && (uint32_t)k.top_k < ranked[kBins]) {
-        r.lo[0] = r.hi[0] = first_bin([&](int b) { return ranked[b + 1] >= (uint32_t)k.top_k; });
+        r.lo[0] = r.hi[0] = reached((uint32_t)k.top_k, ranks, ranked);
         bounds(0);
     }
     if (!(k.top_p >= 1.0f)) {
@@ -465,17 +478,15 @@ __device__ __forceinline__ void part_of(const SampleArgs &a, int part, int *i0, 
     *i1 = *i0 + a.part < a.V ? *i0 + a.part : a.V;
 }
 
+template <bool BF16>
 __global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleArgs a) {
     __shared__ unsigned long long mass[kBins], before[kBins + 1], wave64[kSampleWaves];
     __shared__ uint32_t count[kBins], ranked[kBins + 1], wave32[kSampleWaves];
-    __shared__ unsigned long long heads[kMostParts];
-    __shared__ double factors[kMostParts];
-    __shared__ int shifts[kMostParts];
+    __shared__ First firsts[kSampleWaves];
     __shared__ double roots[kRoots];
     __shared__ uint32_t last;
-    __shared__ Search found;
-    const int m = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x;
-    const Row row = row_of(a, m);
+    const int m = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x, lane = tid & 63;
+    const Row<BF16> row(a, m);
     const Ask k = ask_of(a, m);
     RowState &state = a.rows[m];
     int i0, i1;
@@ -484,127 +495,116 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleAr
     // The first block of logits stays in registers from here to the bins, others (of parts that have more) are read
     // twice.
     float l[8];
-    auto load = [&](int b, float (&to)[8]) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int i = b + j * kSampleThreads + tid;
-            to[j] = i < i1 ? row.logit(i) : -INFINITY;
-        }
-    };
-    uint64_t best = 0;
+    First best = {0, ~0u};
     auto look = [&](int b, const float (&at)[8]) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const uint32_t v = sort_word(at[j]);
-            const uint64_t key = v ? (uint64_t)v << 32 | (uint32_t)~(b + j * kSampleThreads + tid) : 0;
-            best = key > best ? key : best;
+            const int i = b + j * kSampleThreads + tid;
+            if (v > best.word || (v == best.word && (uint32_t)i < best.index)) best = First{v, (uint32_t)i};
         }
     };
-    load(i0, l);
+    row.load(i0, i1, l);
     for (int b = i0 + kBlock; b < i1; b += kBlock) {
         float more[8];
-        load(b, more);
+        row.load(b, i1, more);
         look(b, more);
     }
     look(i0, l);
     mass[tid] = 0;
     count[tid] = 0;
     if (tid < kRoots) roots[tid] = kRoot[tid];
-    best = over_block(wave64, best, Most64());
-    const uint32_t top_word = (uint32_t)(best >> 32);
+    best = first_of<64>(best);
+    if (lane == 0) firsts[tid >> 6] = best;
+    __syncthreads();
+    best = first_of<16>(firsts[lane & 15]);
     const bool ordinary = k.temperature > 0.0f;  // (else the first token is the answer)
     const float steps = Grid::steps_of(k.temperature);
-    if (ordinary && top_word) {
-        const float most = of_sort_word(top_word);
+    if (ordinary && best.word) {
+        const float most = of_sort_word(best.word);
         const Weights w(most, k.temperature, roots);
         const Grid grid = {steps, Grid::number(most, steps)};
         auto add = [&](const float (&at)[8]) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (!(at[j] > -INFINITY)) continue;
-                const int bin = grid.bin(at[j]);
-                atomicAdd(&count[bin], 1u);
-                atomicAdd(&mass[bin], (unsigned long long)w.of(at[j]));
+            for (int j0 = 0; j0 < 8; j0 += 4) {
+                uint64_t weight[4];
+                int bin[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    bin[j] = grid.bin(at[j0 + j]);
+                    weight[j] = w.of(at[j0 + j]);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (!(at[j0 + j] > -INFINITY)) continue;
+                    atomicAdd(&count[bin[j]], 1u);
+                    atomicAdd(&mass[bin[j]], (unsigned long long)weight[j]);
+                }
             }
         };
         add(l);
         for (int b = i0 + kBlock; b < i1; b += kBlock) {
-            load(b, l);
+            row.load(b, i1, l);
             add(l);
         }
     }
     __syncthreads();
+    float most = of_sort_word(best.word);
     if (a.parts > 1) {
         PartBins &to = a.bins[(int64_t)m * a.parts + part];
-        put64(reinterpret_cast<unsigned long long *>(&to.mass[tid]), (uint64_t)__double_as_longlong((double)mass[tid]));
-        put32(&to.count[tid], count[tid]);
-        if (tid == 0) put64(&a.heads[(int64_t)m * a.parts + part].best, best);
+        const int place = ((int)Grid::number(most, steps) - tid) & (kBins - 1);
+        put64(reinterpret_cast<unsigned long long *>(&to.mass[place]), (uint64_t)__double_as_longlong((double)mass[tid]));
+        put32(&to.count[place], count[tid]);
+        if (tid == 0) put64(&a.heads[(int64_t)m * a.parts + part].first, (uint64_t)best.word << 32 | best.index);
         __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): written through to where all XCDs see it
         __syncthreads();
         if (tid == 0) {
-            const uint32_t before = __hip_atomic_fetch_add(a.arrived + m, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            last = before == (uint32_t)a.parts - 1;
+            const uint32_t arrived = __hip_atomic_fetch_add(a.arrived + m, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            last = arrived == (uint32_t)a.parts - 1;
             if (last) put32(a.arrived + m, 0);
         }
         __syncthreads();
         if (!last) return;
-        if (tid < a.parts) heads[tid] = get64(&a.heads[(int64_t)m * a.parts + tid].best);
-        __syncthreads();
-        best = 0;
-        for (int p = 0; p < a.parts; ++p) best = heads[p] > best ? heads[p] : best;
-    }
-    const uint32_t first = (uint32_t)(best >> 32);
-    const float most = of_sort_word(first);
-    if (first == 0 || !ordinary || most == INFINITY) {  // (the same for the whole row)
-        if (tid == 0) {
-            a.ids[m] = first == 0 ? -1 : (int)~(uint32_t)best;
-            state.gather = 0;
-        }
-        return;
-    }
-    const Grid grid = {steps, Grid::number(most, steps)};
-    if (a.parts > 1) {
+        // Every part's bin at this place, and by a lane each the parts' first tokens; without branches between the loads.
+        constexpr int kAtOnce = 8;
+        double ms[kAtOnce];
+        uint32_t cs[kAtOnce];
+        auto ask = [&](int p0) {
+#pragma unroll
+            for (int p = 0; p < kAtOnce; ++p) {
+                const PartBins &from = a.bins[(int64_t)m * a.parts + (p0 + p < a.parts ? p0 + p : 0)];
+                ms[p] = __longlong_as_double((long long)get64(reinterpret_cast<const unsigned long long *>(&from.mass[tid])));
+                cs[p] = get32(&from.count[tid]);
+            }
+        };
+        const uint64_t head = get64(&a.heads[(int64_t)m * a.parts + (lane < a.parts ? lane : 0)].first);
+        ask(0);
+        First mine = {(uint32_t)(head >> 32), (uint32_t)head};
+        if (lane >= a.parts) mine = First{0, ~0u};
+        best = first_of<64>(mine);
+        most = of_sort_word(best.word);
         // A part's weights, relative to the row's largest; its bins, so many places further down.
-        if (tid < a.parts) {
-            const uint32_t top = (uint32_t)(heads[tid] >> 32);
-            factors[tid] = top ? exp(((double)of_sort_word(top) - (double)most) / (double)k.temperature) : 0.0;
-            shifts[tid] = top ? (int)fminf(grid.top - Grid::number(of_sort_word(top), steps), (float)kBins) : kBins;
-        }
-        __syncthreads();
-        // A part's bin that comes to stand at this thread's, and this thread's bin of the part where the shift moves it past
-        // the last one, to which it belongs.
+        const float own = of_sort_word(mine.word), top = Grid::number(most, steps);
+        const double factor = mine.word ? exp(((double)own - (double)most) / (double)k.temperature) : 0.0;
+        const int shift = (int)fminf(top - Grid::number(own, steps), (float)kBins), bin = ((int)top - tid) & (kBins - 1);
+        // What a part has at this place is in the row's bin, or was moved past the last one, to which it belongs.
         double sum = 0.0, past = 0.0;
         uint32_t num = 0, rest = 0;
-        for (int p0 = 0; p0 < a.parts; p0 += 8) {
-            double ms[8], mp[8];
-            uint32_t cs[8], cp[8];
+        for (int p0 = 0; p0 < a.parts; p0 += kAtOnce) {
+            if (p0 > 0) ask(p0);
 #pragma unroll
-            for (int p = 0; p < 8; ++p) {
-                const bool in = p0 + p < a.parts;
-                const int part = in ? p0 + p : 0, shift = shifts[part];
-                const PartBins &from = a.bins[(int64_t)m * a.parts + part];
-                ms[p] = mp[p] = 0.0;
-                cs[p] = cp[p] = 0;
-                if (in && tid >= shift) {
-                    ms[p] = __longlong_as_double((long long)get64(reinterpret_cast<const unsigned long long *>(&from.mass[tid - shift])));
-                    cs[p] = get32(&from.count[tid - shift]);
-                }
-                if (in && shift > 0 && tid + shift >= kBins) {
-                    mp[p] = __longlong_as_double((long long)get64(reinterpret_cast<const unsigned long long *>(&from.mass[tid])));
-                    cp[p] = get32(&from.count[tid]);
-                }
-            }
-#pragma unroll
-            for (int p = 0; p < 8; ++p) {
-                const double f = factors[p0 + p < a.parts ? p0 + p : 0];
-                sum += f * ms[p];
-                num += cs[p];
-                past += f * mp[p];
-                rest += cp[p];
+            for (int p = 0; p < kAtOnce; ++p) {
+                if (p0 + p >= a.parts) break;
+                const double v = __longlong_as_double((long long)of_lane((uint64_t)__double_as_longlong(factor), p0 + p)) * ms[p];
+                const bool in = bin >= of_lane(shift, p0 + p);
+                sum += in ? v : 0.0;
+                past += in ? 0.0 : v;
+                num += in ? cs[p] : 0;
+                rest += in ? 0 : cs[p];
             }
         }
-        mass[tid] = (unsigned long long)sum;
-        count[tid] = num;
+        mass[bin] = (unsigned long long)sum;
+        count[bin] = num;
         __syncthreads();
         if (rest) {
             atomicAdd(&count[kBins - 1], rest);
@@ -612,24 +612,45 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleAr
         }
         __syncthreads();
     }
-    uint64_t own_before, all;
-    uint32_t own_ranked, n;
-    scan_pair(wave64, wave32, mass[tid], count[tid], &own_before, &own_ranked, &all, &n);
-    before[tid] = own_before;
-    ranked[tid] = own_ranked;
+    if (best.word == 0 || !ordinary || most == INFINITY) {  // (the same for the whole row)
+        if (tid == 0) {
+            a.ids[m] = best.word == 0 ? -1 : (int)best.index;
+            state.gather = 0;
+        }
+        return;
+    }
+    const Grid grid = {steps, Grid::number(most, steps)};
+    const unsigned long long own_mass = mass[tid];
+    const uint32_t own_count = count[tid];
+    unsigned long long all;
+    uint32_t n;
+    {
+        // scan_block of both at once
+        const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const unsigned long long sum = scan_wave(own_mass);
+        const uint32_t num = scan_wave(own_count);
+        if (lane == 63) {
+            wave64[w] = sum;
+            wave32[w] = num;
+        }
+        __syncthreads();
+        const unsigned long long sums = scan_row(wave64[lane & 15]);
+        const uint32_t nums = scan_row(wave32[lane & 15]);
+        all = of_lane(sums, 15);
+        n = of_lane(nums, 15);
+        const unsigned long long own_before = (w ? of_lane(sums, w ? w - 1 : 0) : 0) + sum - own_mass;
+        const uint32_t own_ranked = (w ? of_lane(nums, w ? w - 1 : 0) : 0) + num - own_count;
+        state.before[tid] = before[tid] = own_before;
+        state.ranked[tid] = ranked[tid] = own_ranked;
+    }
     if (tid == 0) {
         before[kBins] = all;
         ranked[kBins] = n;
     }
     __syncthreads();
-    if (tid < 64) {
-        const Search r = search(k, grid, most, before, ranked);
-        if (tid == 0) found = r;
-    }
-    __syncthreads();
+    if (tid >= 64) return;
+    const Search found = search(k, grid, most, before, ranked);
     const uint32_t listed = listed_before(found.lo, found.hi, ranked, kBins);
-    state.before[tid] = own_before;
-    state.ranked[tid] = own_ranked;
     if (tid == 0) {
         state.ranked[kBins] = n;
         state.gather = listed > (uint32_t)kList || !(fabsf(grid.top) < kFar) ? 2 : 1;
@@ -782,23 +803,65 @@ __device__ int finish(const RowState &state, const Ask &k, const Grid &grid, con
     return (int)~(uint32_t)key[i < n ? i : n - 1];
 }
 
+// The same from up to 64 tokens by one wave, a token to a lane, which takes no LDS but for what it looks up.
+__device__ int finish_few(const RowState &state, const Ask &k, const Grid &grid, const int (&lo)[4], const int (&hi)[4], int n,
+                          const unsigned long long *before, const uint32_t *ranked, const double *roots) {
+    const int lane = threadIdx.x & 63;
+    const uint64_t mine = lane < n ? get64(&state.list[lane]) : 0;
+    const uint64_t all = state.all;
+    const uint32_t row_count = state.count;
+    const float most = state.most;
+    const int row_cut = state.cut;
+    int to = lane < n ? 0 : lane;
+    for (int j = 0; j < n; ++j) to += of_lane(mine, j) > mine && lane < n;
+    const uint32_t word = (uint32_t)__builtin_amdgcn_ds_permute(4 * to, (int)(mine >> 32));
+    const uint32_t index = ~(uint32_t)__builtin_amdgcn_ds_permute(4 * to, (int)(uint32_t)mine);
+    const Weights w(most, k.temperature, roots);
+    const uint64_t weight = lane < n ? w.of_word(word) : 0, sum = scan_wave(weight) - weight;
+    const int bin = lane < n ? grid.bin(of_sort_word(word)) : kBins - 1;
+    const uint32_t first = listed_before(lo, hi, ranked, bin) & 63;  // (the first listed token of the bin; of no token: any lane)
+    const uint64_t upto = before[bin] + (sum + weight - (uint64_t)__shfl((unsigned long long)sum, (int)first));
+    const uint32_t rank = ranked[bin] + ((uint32_t)lane - first);
+    const uint64_t live = n < 64 ? (1ull << n) - 1 : ~0ull;
+    uint64_t kept = all;
+    auto keep = [&](uint64_t v) { kept = v < kept ? v : kept; };
+    if (k.top_k > 0 && (uint32_t)k.top_k < row_count) {
+        const uint64_t at = __ballot(rank == (uint32_t)k.top_k - 1) & live;
+        if (at) keep(of_lane(upto, __builtin_ctzll(at)));
+    }
+    if (!(k.top_p >= 1.0f)) {
+        const uint64_t reach = reach_of(k.top_p, kept), at = __ballot(upto >= reach) & live;
+        if (at) keep(of_lane(upto, __builtin_ctzll(at)));
+    }
+    if (k.min_p > 0.0f) {
+        // (of the bins from `cut` on; before them all have the weight)
+        const uint64_t below = __ballot(bin >= row_cut && !((double)weight >= (double)k.min_p * kOne)) & live;
+        const int i = below ? __builtin_ctzll(below) : n;
+        if (i == 0 || of_lane(bin, i ? i - 1 : 0) < row_cut)
+            keep(before[row_cut]);
+        else
+            keep(of_lane(upto, i - 1));
+    }
+    kept = kept < 1ull << kPoint ? 1ull << kPoint : kept;  // (the first token's weight is 1)
+    const uint64_t x = point_of(k.u, kept), at = __ballot(upto > x) & live;
+    return (int)of_lane(index, at ? __builtin_ctzll(at) : n - 1);
+}
+
+template <bool BF16>
 __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs a) {
     __shared__ unsigned long long key[kList], sum[kList], wave64[kSampleWaves];
-    __shared__ uint32_t wave32[kSampleWaves], shared_at, last;
+    __shared__ uint32_t wave32[kSampleWaves], last;
     __shared__ unsigned long long kept, before[kBins];
     __shared__ uint32_t found[3], ranked[kBins + 1];
     __shared__ double roots[kRoots];
-    const int m = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x;
+    const int m = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x, lane = tid & 63;
     RowState &state = a.rows[m];
+    const Row<BF16> row(a, m);
+    int i0, i1;
+    part_of(a, part, &i0, &i1);
+    // (asked for together: what the row's answer is made of, its first logits, and what the last workgroup looks up)
     const uint32_t gather = state.gather;
-    if (gather == 0 || (gather == 2 && part > 0)) return;
-    const Row row = row_of(a, m);
     const Ask k = ask_of(a, m);
-    if (gather == 2) {  // (the second launch has the registers: in the first they would halve its workgroups)
-        const int id = choose_slowly(*reinterpret_cast<Shared *>(key), row, k, state.most, state.count);
-        if (tid == 0) a.ids[m] = id;
-        return;
-    }
     const Grid grid = {state.steps, state.top};
     int lo[4], hi[4];
 #pragma unroll
@@ -806,39 +869,46 @@ __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs 
         lo[i] = state.lo[i];
         hi[i] = state.hi[i];
     }
-    // (what the last workgroup looks up: asked for by all, beside their logits)
-    before[tid] = state.before[tid];
-    ranked[tid] = state.ranked[tid];
-    if (tid == 0) ranked[kBins] = state.ranked[kBins];
-    if (tid < kRoots) roots[tid] = kRoot[tid];
-    int i0, i1;
-    part_of(a, part, &i0, &i1);
+    float l[8];
+    row.load(i0, i1, l);
+    const unsigned long long own_before = state.before[tid];
+    const uint32_t own_ranked = state.ranked[tid], all_ranked = state.ranked[kBins];
+    const double own_root = kRoot[lane];
+    if (gather == 0 || (gather == 2 && part > 0)) return;
+    if (gather == 2) {  // (the second launch has the registers: in the first they would halve its workgroups)
+        const int id = choose_slowly(*reinterpret_cast<Shared *>(key), row, k, state.most, state.count);
+        if (tid == 0) a.ids[m] = id;
+        return;
+    }
     for (int b = i0; b < i1; b += kBlock) {
-        float l[8];
+        if (b > i0) row.load(b, i1, l);
+        uint64_t hits[8];
+        uint32_t all = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int i = b + j * kSampleThreads + tid;
-            l[j] = i < i1 ? row.logit(i) : -INFINITY;
-        }
-        uint32_t hits = 0;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int bin = l[j] > -INFINITY ? grid.bin(l[j]) : kBins;
+            const int bin = grid.bin(l[j]);
             bool is = false;
 #pragma unroll
             for (int i = 0; i < 4; ++i) is |= bin >= lo[i] && bin <= hi[i];
-            hits |= is && bin < kBins ? 1u << j : 0u;
+            hits[j] = __ballot(is && l[j] > -INFINITY);
+            all += (uint32_t)__builtin_popcountll(hits[j]);
         }
-        uint32_t all;
-        uint32_t at = scan_block<kSampleWaves>(wave32, (uint32_t)__builtin_popcount(hits), &all);
-        if (tid == 0 && all) shared_at = __hip_atomic_fetch_add(&state.listed, all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        __syncthreads();
-        at += shared_at;
+        if (all == 0) continue;  // (the wave's: most have none)
+        uint32_t at = 0;
+        if (lane == 0) at = __hip_atomic_fetch_add(&state.listed, all, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        at = __builtin_amdgcn_readfirstlane(at);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if ((hits >> j & 1) && at < (uint32_t)kList)
-                put64(&state.list[at++], (uint64_t)sort_word(l[j]) << 32 | (uint32_t)~(b + j * kSampleThreads + tid));
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t to = at + (uint32_t)__builtin_popcountll(hits[j] & ((1ull << lane) - 1));
+            if ((hits[j] >> lane & 1) && to < (uint32_t)kList)
+                put64(&state.list[to], (uint64_t)sort_word(l[j]) << 32 | (uint32_t)~(b + j * kSampleThreads + tid));
+            at += (uint32_t)__builtin_popcountll(hits[j]);
+        }
     }
+    before[tid] = own_before;
+    ranked[tid] = own_ranked;
+    if (tid == 0) ranked[kBins] = all_ranked;
+    if (tid < kRoots) roots[tid] = own_root;
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): written through to where all XCDs see it
     __syncthreads();
     if (tid == 0) last = __hip_atomic_fetch_add(&state.arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)a.parts - 1;
@@ -849,7 +919,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs 
     // By as few waves as hold the tokens: the others have ended, so that barriers wait for few.
     int id = 0;
     if (n <= 64) {
-        if (tid < 64) id = finish<1, 1>(state, k, grid, lo, hi, n, key, sum, wave64, wave32, found, &kept, before, ranked, roots);
+        if (tid < 64) id = finish_few(state, k, grid, lo, hi, n, before, ranked, roots);
     } else if (n <= 256) {
         if (tid < 256) id = finish<4, 1>(state, k, grid, lo, hi, n, key, sum, wave64, wave32, found, &kept, before, ranked, roots);
     } else {
@@ -895,7 +965,6 @@ extern "C" int nvq_sample(const void *logits, int dtype, int64_t ld, int M, int 
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < nvq_sample_workspace_bytes(M, V)) return NVQ_ERR_WORKSPACE;
     SampleArgs a;
     a.logits = logits;
-    a.dtype = dtype;
     a.ld = ld;
     a.M = M;
     a.V = V;
@@ -914,9 +983,15 @@ extern "C" int nvq_sample(const void *logits, int dtype, int64_t ld, int M, int 
     a.heads = reinterpret_cast<PartHead *>(a.bins + (size_t)M * a.parts);
     const dim3 grid((unsigned)(M * a.parts)), block(kSampleThreads);
     const hipStream_t st = (hipStream_t)stream;
-    hipLaunchKernelGGL(sample_bins_kernel, grid, block, 0, st, a);
+    if (dtype == NVQ_BF16)
+        hipLaunchKernelGGL(sample_bins_kernel<true>, grid, block, 0, st, a);
+    else
+        hipLaunchKernelGGL(sample_bins_kernel<false>, grid, block, 0, st, a);
     NVQ_HIP_TRY(hipGetLastError());
-    hipLaunchKernelGGL(sample_list_kernel, grid, block, 0, st, a);
+    if (dtype == NVQ_BF16)
+        hipLaunchKernelGGL(sample_list_kernel<true>, grid, block, 0, st, a);
+    else
+        hipLaunchKernelGGL(sample_list_kernel<false>, grid, block, 0, st, a);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
 }
