@@ -59,6 +59,15 @@ __device__ __forceinline__ int nth_bit(uint64_t bits, int k) {
     return at;
 }
 
+// The first tile of an adapter's tokens that is this workgroup's, of g.tiles that take them in turn; where they share all of
+// a group's adapters, they go on where the one before ended (*base: tiles before), so that many with few tokens each
+// keep all four at work: 500 tokens of 8 adapters in no order, 14336 outputs and 64 ranks: 109 us without, 51 with.
+__device__ __forceinline__ int first_tile(const AdaptersArgs &g, int tile, int tokens, int *base) {
+    const int first = (tile - *base) & (g.tiles - 1);
+    if (g.shares == 1) *base += (tokens + kTile - 1) / kTile;
+    return first;
+}
+
 // h of a group's tokens: RT tiles of sixteen ranks, a slice of K, its columns in turn over the waves.
 template <int RT>
 __global__ __launch_bounds__(kThreads) void adapters_down_kernel(AdaptersArgs g) {
@@ -75,18 +84,19 @@ __global__ __launch_bounds__(kThreads) void adapters_down_kernel(AdaptersArgs g)
     const int c0 = slice * g.columns, c1 = c0 + g.columns < g.K / 32 ? c0 + g.columns : g.K / 32;
     const int mine = adapter_of(g, m0);
     uint64_t left = __ballot(mine >= 0);
-    for (int at = 0; left; ++at) {
+    for (int at = 0, base = 0; left; ++at) {
         int e;
         const uint64_t with = turn(mine, &left, &e);
         if (at % g.shares != share) continue;
-        const int tokens = __builtin_popcountll(with);
+        const int tokens = __builtin_popcountll(with), begin = first_tile(g, tile, tokens, &base) * kTile;
+        if (begin >= tokens) continue;
         const uint16_t *a[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             const int r = r0 + 16 * t + n < g.R ? r0 + 16 * t + n : g.R - 1;
             a[t] = g.a + ((int64_t)e * g.R + r) * g.K + 8 * kb;
         }
-        for (int k0 = tile * kTile; k0 < tokens; k0 += kTile * g.tiles) {
+        for (int k0 = begin; k0 < tokens; k0 += kTile * g.tiles) {
             const int m = m0 + nth_bit(with, k0 + n < tokens ? k0 + n : k0);
             const uint16_t *const x = g.x + (int64_t)m * g.K + 8 * kb;
             float4v sum[RT];
@@ -200,11 +210,13 @@ __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
     int i = blockIdx.x / g.turns;
     const int tile = i % g.tiles;
     i /= g.tiles;
-    const int all = g.shares + (g.out != g.y);  // (the last: tokens without an adapter, which stay as they are)
+    // Tokens without an adapter stay as they are: by the last share, or, of a single one, by every tile's workgroup some.
+    const bool copies = g.out != g.y;
+    const int all = g.shares + (copies && g.shares > 1);
     const int share = i % all, m0 = i / all * kGroup;
     const int mine = adapter_of(g, m0);
     uint64_t left = __ballot(mine >= 0);
-    if (share == g.shares) {
+    if (copies && (g.shares == 1 || share == g.shares)) {
         uint64_t none = ~left;
         if (g.M - m0 < kGroup) none &= (1ull << (g.M - m0)) - 1;
         const int count = __builtin_popcountll(none);
@@ -233,15 +245,15 @@ __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
                     }
                 }
         }
-        return;
+        if (g.shares > 1) return;
     }
     const int64_t h_slice = (int64_t)g.M * g.R;
-    for (int at = 0; left; ++at) {
+    for (int at = 0, base = 0; left; ++at) {
         int e;
         const uint64_t with = turn(mine, &left, &e);
         if (at % g.shares != share) continue;
-        const int tokens = __builtin_popcountll(with);
-        if (tile * kTile >= tokens) continue;
+        const int tokens = __builtin_popcountll(with), begin = first_tile(g, tile, tokens, &base) * kTile;
+        if (begin >= tokens) continue;
         // The weights of two columns of 32 ranks at a time.
         uint4v bw[2][NT];
         auto load = [&](int block, int c) {
@@ -260,7 +272,7 @@ __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
         };
         load(first, 0);
         const float scale = g.scales ? g.scales[e] : 1.0f;
-        for (int k0 = tile * kTile; k0 < tokens; k0 += kTile * g.tiles) {
+        for (int k0 = begin; k0 < tokens; k0 += kTile * g.tiles) {
             const bool my = k0 + n < tokens;
             const int64_t row = (int64_t)(m0 + nth_bit(with, my ? k0 + n : k0)) * g.N;
             float y[4 * NT];
@@ -295,7 +307,7 @@ __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
                     *reinterpret_cast<uint2v *>(&hs[q][k][r]) = uint2v{p[0][q] | p[1][q] << 16, p[2][q] | p[3][q] << 16};
             }
             __syncthreads();
-            if (k0 >= kTile * g.tiles) load(first, 0);  // (of the first tile it is there)
+            if (k0 > begin) load(first, 0);  // (of the first tile it is there)
             for (int block = first; block < g.N; block += stride) {
                 const int o0 = block + w * 16 * NT + 4 * NT * kb;  // the lane's outputs
                 const bool whole = o0 + 4 * NT <= g.N;
@@ -360,14 +372,17 @@ int tiles_of(int M) { return M <= kGroup ? 1 : kGroup / kTile; }
 // Blocks of 64, 32 or 16 ranks.
 int rank_tiles(int R) { return R > 32 ? 4 : R > 16 ? 2 : 1; }
 int rank_blocks(int R) { return (R + 16 * rank_tiles(R) - 1) / (16 * rank_tiles(R)); }
-// Slices of K: as many as bring a thousand workgroups with work, of four columns (one per wave) or more.
+// Slices of K: as many as bring a thousand workgroups with work, of four columns (one per wave) or more.  Every workgroup of
+// the second launch adds them up, so that more than eight pay where it has many outputs then (8 instead of 16: one token
+// of 2048 outputs 7.3 -> 6.8 us, 500 of 4099 19.4 -> 17.3; 32 of 28672 21.2 -> 22.0).
 int slices_of(const nvq_adapters &s, int M) {
     const int64_t others = (int64_t)((M + kTile - 1) / kTile > shares_of(M, s.n) ? (M + kTile - 1) / kTile : shares_of(M, s.n)) *
                            rank_blocks(s.R);
     int64_t want = 1024 / others;
     const int64_t most = (s.K / 32 + kWaves - 1) / kWaves;
     want = want < most ? want : most;
-    want = want < kMostSlices ? want : kMostSlices;
+    const int64_t pay = s.N >= 16384 ? kMostSlices : kMostSlices / 2;
+    want = want < pay ? want : pay;
     return want > 1 ? (int)want : 1;
 }
 
@@ -435,7 +450,7 @@ extern "C" int nvq_adapters_add(const nvq_adapters *adapters, const uint16_t *x_
     const int per = (wide ? 64 : 16) * kWaves, blocks = (g.N + per - 1) / per;
     // As many as the device holds at once (three a compute unit) between those with work: each adapter or tile of tokens.
     const int busy = (M + kTile - 1) / kTile > g.shares ? (M + kTile - 1) / kTile : g.shares, resident = 3 * device_cu_count() / busy;
-    const int copies = out != y ? groups_of(M) * g.tiles : 0;
+    const int copies = out != y && g.shares > 1 ? groups_of(M) * g.tiles : 0;
     const int each = resident < 1 ? blocks : (blocks + resident - 1) / resident;
     g.turns = (blocks + each - 1) / each;
     const dim3 up((unsigned)((groups + copies) * g.turns));
