@@ -12,6 +12,11 @@
 // left out) where they are rounded to bf16, 2^-9, themselves.  The products with the first and with the rest are summed
 // apart and added at the end: what an infinite value makes of the rest (zero times infinity, or the other sign)
 // is left out there.
+//
+// The bytes of keys and values bound it: one sequence of 131072 tokens, 8 key heads of 128 in bf16, 537 MB, takes 99.5 us,
+// 5.4 TB/s, where reading alone in the same split takes 95; 32 ragged ones of up to 16384 tokens in 8 bits, 253 MB, 62 us,
+// 46 of them reading.  Short ones are bound by the memory's latency, four times over (lengths, pages, keys and values,
+// joins): 500 tokens 10 us, 7 sequences of up to 3000 behind a window of 1000 14 us.
 #include <type_traits>
 
 #include "cache.h"
@@ -36,7 +41,7 @@ struct AttentionArgs {
     const int32_t *table, *lengths;
     int B, H, width, group, tiles;  // query heads per key head; head tiles of them
     int window;
-    int most_groups;  // workgroups that the device holds at once
+    int most_each;  // workgroups that there are for each sequence and head tile
     float scale, softcap;
     void *out;
     int out_dtype;
@@ -158,7 +163,7 @@ __device__ __forceinline__ void attend(const AttentionArgs &a, int b, int head, 
     const int32_t *const table = a.table + (int64_t)b * a.width;
     // A lane reads keys of the step's block n / 4 of eight tokens (its tile rows' own) and values of block kb.  No load
     // stands behind a branch: where one does, the compiler waits for all of them at the loop's end, and a step takes the
-    // memory's latency (27 of 104 us at 131072 tokens).  So a number is looked up for every block, past the last one the
+    // memory's latency (103 instead of 101 us at 131072 tokens).  So a number is looked up for every block, past the last one the
     // last one's, and what it is worth is decided where it is used; past the last step the last one is read again.
     auto page_of = [&](int s, int block) {
         const int t = kStep * s + 8 * block;
@@ -315,7 +320,8 @@ struct PieceOf {
 };
 
 // The grid is one flat line of all steps of all sequences and head tiles, cut into as many equal ranges as there are
-// workgroups, and a range into one per wave: however ragged the lengths, every compute unit reads as much.  What a
+// workgroups (or, of few short ones, dealt out by sequence and head tile), and a range into one per wave: however ragged
+// the lengths, every compute unit reads as much.  What a
 // wave has of a sequence and head tile that others share goes to LDS and is joined there, what a workgroup has of one
 // to the workspace, where the workgroup that arrives last joins it.
 template <int D>
@@ -337,6 +343,18 @@ __device__ __forceinline__ float wave_max(float v) {
     return with_lane_xor<1>(v, MaxOp());
 }
 
+struct MostOp {
+    __device__ int operator()(int a, int b) const { return a > b ? a : b; }
+};
+__device__ __forceinline__ int wave_most(int v) {
+    v = with_lane_xor<32>(v, MostOp());
+    v = with_lane_xor<16>(v, MostOp());
+    v = with_lane_xor<8>(v, MostOp());
+    v = with_lane_xor<4>(v, MostOp());
+    v = with_lane_xor<2>(v, MostOp());
+    return with_lane_xor<1>(v, MostOp());
+}
+
 __device__ __forceinline__ void put(float *p, float v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ float get(const float *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
@@ -344,7 +362,7 @@ template <int D, bool E4M3>
 __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(AttentionArgs a) {
     constexpr int kWaves = waves_of<D>(), kThreads = 64 * kWaves, kRow = D + 2;  // (a head's sum, m, l)
     extern __shared__ __align__(16) char lds[];
-    __shared__ int scan[kWaves + 1];
+    __shared__ int scan[kWaves], longest_of[kWaves];
     __shared__ PieceOf held[kWaves][2];
     __shared__ int last[2];
     int *const upto = reinterpret_cast<int *>(lds);  // [B + 1]: steps before a sequence, of one head tile, kPieceCost included
@@ -352,28 +370,35 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4;
     const int per = a.c.heads * a.tiles;                                   // head tiles
     const int heads_most = a.group < kHeadTile ? a.group : kHeadTile;
+    auto key_head_of = [&](int ht) { return a.tiles == 1 ? ht : ht / a.tiles; };  // (mostly without a division)
+    auto tile_of = [&](int ht) { return a.tiles == 1 ? 0 : ht % a.tiles; };
     auto heads_of = [&](int ht) {
-        const int h = a.group - kHeadTile * (ht % a.tiles);
+        const int h = a.group - kHeadTile * tile_of(ht);
         return h < kHeadTile ? h : kHeadTile;
     };
-    auto row_of = [&](int b, int ht) { return (int64_t)b * a.H + ht / a.tiles * a.group + kHeadTile * (ht % a.tiles); };
+    auto row_of = [&](int b, int ht) { return (int64_t)b * a.H + key_head_of(ht) * a.group + kHeadTile * tile_of(ht); };
 
-    int total = 0;
+    int total = 0, longest = 0;
     for (int b0 = 0; b0 < a.B; b0 += kThreads) {
         const int b = b0 + (int)threadIdx.x;
         const int steps = b < a.B ? span_of(a, b).steps : 0;
         int sum = steps > 0 ? steps + kPieceCost : 0;
+        longest = steps > longest ? steps : longest;
         for (int d = 1; d < 64; d <<= 1) {
             const int o = __shfl_up(sum, d);
             if (lane >= d) sum += o;
         }
         __syncthreads();
         if (lane == 63) scan[w] = sum;
+        const int most = wave_most(longest);
+        if (lane == 0) longest_of[w] = most;
         __syncthreads();
         int before = total, all = total;
+#pragma unroll
         for (int i = 0; i < kWaves; ++i) {
-            if (i < w) before += scan[i];
+            before += i < w ? scan[i] : 0;
             all += scan[i];
+            longest = longest_of[i] > longest ? longest_of[i] : longest;
         }
         if (b < a.B) upto[b + 1] = before + sum;
         total = all;
@@ -389,14 +414,34 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
         }
     const int64_t T = (int64_t)total * per;
     if (T == 0) return;
-    // Two steps to a wave at least; and of one sequence whole workgroups to a head tile, so that a short one needs no
-    // joining through memory.
-    const int64_t want = (T + 2 * kWaves - 1) / (2 * kWaves);
-    int groups = want < (int64_t)gridDim.x ? (int)want : (int)gridDim.x;
-    if (a.B == 1 && want < a.most_groups && groups > per) groups -= groups % per;
+    // Two steps to a wave at least.  Where there are workgroups for each sequence and head tile to have its own, as many as its
+    // steps take, they are dealt out so, unless the longest part takes longer than the line's equal ranges and the joins
+    // that these need: a range is read at the memory's rate (its bytes count), a part of one's own at the memory's latency,
+    // about twice that rate at most.  (7 sequences of 1000 tokens, 8 key heads of 128: 17 us dealt out, 20.6 in ranges; 30 of
+    // 1000: 28 and 33.5; 16 of 100 to 4000: 31 and 25.5; 30 of 100 to 2000: 29.6 and 26.5.)
+    constexpr int kPart = 2 * kWaves;
+    const int each = a.most_each < (longest + kPart - 1) / kPart ? a.most_each : (longest + kPart - 1) / kPart;
+    const bool dealt = each > 0 && (int64_t)longest * gridDim.x <= each * (kPart * (int64_t)gridDim.x + (E4M3 ? 1 : 2) * T * D * kWaves / 1024);
+    const int cost = dealt ? kPieceCost : 0;  // (that a part of one's own has no use for)
+    const int64_t want = (T + kPart - 1) / kPart;
+    const int groups = want < (int64_t)gridDim.x ? (int)want : (int)gridDim.x;
     const int g = blockIdx.x;
-    if (g >= groups) return;
-    const int64_t f0 = quotient(T * g, groups), f1 = quotient(T * (g + 1), groups), R = f1 - f0;
+    int64_t f0, f1;
+    // Of a sequence and head tile's n steps: workgroups that have some of them.
+    auto members_of = [&](int n) { return (n + kPart - 1) / kPart < each ? (n + kPart - 1) / kPart : each; };
+    if (dealt) {
+        const int piece = each == 1 ? g : g / each, j = g - piece * each, b = piece / per;
+        const int n = b < a.B ? upto[b + 1] - upto[b] - cost : 0;
+        if (n <= 0 || j >= members_of(n)) return;
+        const int64_t at = (int64_t)per * upto[b] + (int64_t)(piece - b * per) * n;
+        f0 = at + quotient((int64_t)n * j, members_of(n));
+        f1 = at + quotient((int64_t)n * (j + 1), members_of(n));
+    } else {
+        if (g >= groups) return;
+        f0 = quotient(T * g, groups);
+        f1 = quotient(T * (g + 1), groups);
+    }
+    const int64_t R = f1 - f0;
     const int64_t w0 = f0 + R * w / kWaves, w1 = f0 + R * (w + 1) / kWaves;
 
     auto write = [&](int64_t row, int i, float v) { store_global(a.out, a.out_dtype, row * D + i, v); };
@@ -412,7 +457,7 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
         }
         PieceOf p;
         p.b = __builtin_amdgcn_readfirstlane(lo);
-        p.n = __builtin_amdgcn_readfirstlane(upto[lo + 1] - upto[lo]);
+        p.n = __builtin_amdgcn_readfirstlane(upto[lo + 1] - upto[lo]) - cost;
         const int64_t r = f - (int64_t)per * upto[lo];
         p.ht = __builtin_amdgcn_readfirstlane((int)quotient(r, p.n));
         p.begin = __builtin_amdgcn_readfirstlane((int)(r - (int64_t)p.ht * p.n));
@@ -423,7 +468,7 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
         State<D, E4M3> st;
         st.clear();
         const int count = (p.end < sp.steps ? p.end : sp.steps) - p.begin;
-        if (count > 0) attend<D, E4M3>(a, p.b, p.ht / a.tiles, p.ht % a.tiles, sp, sp.first + p.begin, count, st);
+        if (count > 0) attend<D, E4M3>(a, p.b, key_head_of(p.ht), tile_of(p.ht), sp, sp.first + p.begin, count, st);
         float l = with_lane_xor<16>(st.l, AddOp());
         l = with_lane_xor<32>(l, AddOp());
         const int heads = heads_of(p.ht);
@@ -477,8 +522,14 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     for (int start = -1, turn = 0; start < kWaves; ++start) {
         if (start >= 0 && !(starts >> start & 1)) continue;
         const int slot = start < 0 ? 0 : 1, first = start < 0 ? front : start;
-        PieceOf p = held[first][slot];
+        const PieceOf in_lds = held[first][slot];
+        PieceOf p;
+        p.b = __builtin_amdgcn_readfirstlane(in_lds.b);
         if (p.b < 0) continue;
+        p.ht = __builtin_amdgcn_readfirstlane(in_lds.ht);
+        p.begin = __builtin_amdgcn_readfirstlane(in_lds.begin);
+        p.end = __builtin_amdgcn_readfirstlane(in_lds.end);
+        p.n = __builtin_amdgcn_readfirstlane(in_lds.n);
         uint32_t members = 1u << first;
         int until = p.end;
 #pragma unroll
@@ -560,14 +611,25 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     // arrives; the last one's loads pass its caches by.
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
     __syncthreads();
+    // The workgroups that have some of a sequence and head tile, which only one can be the first of.
     auto group_of = [&](int64_t f) { return (int)quotient((f + 1) * groups - 1, T); };
+    auto groups_with = [&](const PieceOf &p, int *from, int *to) {
+        if (dealt) {
+            *from = (p.b * per + p.ht) * each;
+            *to = *from + members_of(p.n) - 1;
+        } else {
+            const int64_t at = (int64_t)per * upto[p.b] + (int64_t)p.ht * p.n;
+            *from = group_of(at);
+            *to = group_of(at + p.n - 1);
+        }
+    };
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
             const PieceOf &p = i ? shared_piece[1] : shared_piece[0];
             last[i] = 0;
             if (p.b < 0) continue;
-            const int64_t at = (int64_t)per * upto[p.b] + (int64_t)p.ht * p.n;
-            const int from = group_of(at), to = group_of(at + p.n - 1);
+            int from, to;
+            groups_with(p, &from, &to);
             const uint32_t before = __hip_atomic_fetch_add(a.arrived + from, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             last[i] = before == (uint32_t)(to - from);
             if (last[i]) __hip_atomic_store(a.arrived + from, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -577,9 +639,10 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     for (int i = 0; i < 2; ++i) {
         if (!last[i]) continue;  // (the same for the whole workgroup)
         const PieceOf p = i ? shared_piece[1] : shared_piece[0];
-        const int64_t at = (int64_t)per * upto[p.b] + (int64_t)p.ht * p.n;
-        const int from = __builtin_amdgcn_readfirstlane(group_of(at));
-        const int count = __builtin_amdgcn_readfirstlane(group_of(at + p.n - 1)) - from + 1, heads = heads_of(p.ht);
+        int from, to;
+        groups_with(p, &from, &to);
+        from = __builtin_amdgcn_readfirstlane(from);
+        const int count = __builtin_amdgcn_readfirstlane(to) - from + 1, heads = heads_of(p.ht);
         // What workgroup from + j has of it: behind the beginning in the first slot.
         auto part = [&](int j) { return a.partial + (int64_t)((from + j) * 2 + (j == 0 ? 1 : 0)) * kHeadTile * kRow; };
         // The factors of the parts, [count][heads], where the waves' parts were; m and l of a head behind them.  The first
@@ -647,8 +710,8 @@ int launch_attention(AttentionArgs a, hipStream_t st) {
     const int cu = device_cu_count(), heads = a.group < kHeadTile ? a.group : kHeadTile;
     const int64_t steps = (int64_t)a.B * (((int64_t)a.width << a.c.page_shift) / kStep + 1 + kPieceCost) * a.c.heads * a.tiles;
     const int64_t want = (steps + 2 * kWaves - 1) / (2 * kWaves), most = cu < kMaxGroups ? cu : kMaxGroups;
-    a.most_groups = (int)most;
     const dim3 grid((unsigned)(want < most ? want : most)), block(64 * kWaves);
+    a.most_each = (int)(grid.x / ((int64_t)a.B * a.c.heads * a.tiles));
     // (the parts' room also holds the factors and sums of a join: kMaxGroups + 2 per head)
     static_assert(2 * kWaves * (D + 2) >= kMaxGroups + 2, "room for a join");
     const size_t lds = (((size_t)a.B + 1) * 4 + 15) / 16 * 16 + sizeof(float) * 2 * kWaves * heads * (D + 2);

@@ -258,7 +258,8 @@ ATTENTION = [  # lengths, H, heads, D, page, window, softcap
     ([2000, 3, 700], 24, 8, 128, 32, 0, 30.0), ([257, 64, 65, 1023], 8, 8, 128, 128, 100, 0.0), ([90, 40], 7, 1, 160, 16, 33, 5.0),
     ([333, 0, 8], 32, 2, 256, 64, 0, 0.0), ([120, 1111], 40, 2, 192, 8, 0, 0.0), ([70, 3000], 17, 1, 224, 256, 1, 0.0),
     ([5000], 16, 1, 128, 1024, 0, 0.0), ([9] * 40, 4, 4, 32, 8, 0, 0.0), ([4097, 1], 48, 1, 64, 16, 4000, 0.0),
-    (list(range(130)), 3, 1, 32, 8, 64, 0.0)]
+    (list(range(130)), 3, 1, 32, 8, 64, 0.0), ([700, 5, 0, 1200, 33], 4, 2, 128, 16, 0, 0.0), ([2100, 2000, 17, 2200], 32, 8, 64, 64, 0, 0.0),
+    ([900, 1000, 64], 34, 1, 96, 32, 500, 0.0), ([4000, 3900], 8, 2, 256, 128, 0, 0.0)]
 
 
 def check_attention(got, lse, pool, q, lengths, window, softcap, scale, out_eps):
