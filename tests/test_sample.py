@@ -148,3 +148,35 @@ def test_sample_of_rows_that_lie_apart_at_any_alignment(dtype):
         flat = torch.from_numpy(rng.standard_normal(M * ld + 8).astype(np.float32) * 4).to(dtype)
         view = lambda t: t[first:first + M * ld].view(M, ld)[:, :V]
         check(view(flat).contiguous(), rng.random(M).astype(np.float32), given=view(flat.to(DEV)), **asks(rng, M))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_sample_of_rows_that_are_mostly_masked(dtype):
+    """All but a few tokens at the type's lowest value, or far below: filters that reach into them."""
+    rng = np.random.default_rng(21)
+    M, V = 8, 60000
+    x = np.full((M, V), torch.finfo(dtype).min, np.float64)
+    x[4:] = -80.0
+    for m in range(M):
+        x[m, rng.choice(V, 3 + 5 * m, False)] = rng.standard_normal(3 + 5 * m) * 3
+    logits, u = torch.from_numpy(x).to(dtype), rng.random(M).astype(np.float32)
+    f = lambda v, t=np.float32: np.full(M, v, t)
+    for kw in ({}, dict(top_k=f(50, np.int32)), dict(top_p=f(0.9999)), dict(min_p=f(1e-30)), dict(top_k=f(50, np.int32), top_p=f(0.95), min_p=f(1e-25)),
+               dict(temperature=f(0.2), top_k=f(1000, np.int32)), dict(temperature=f(3.0), top_k=f(20, np.int32), min_p=f(0.01))):
+        check(logits, u, **kw)
+
+
+@gpu
+@pytest.mark.parametrize("spread", [0.02, 2.5, 40.0])
+def test_sample_of_low_and_high_temperatures(spread):
+    """Filters that end in every part of the bins, behind them, and rows that no bins serve."""
+    rng = np.random.default_rng(22)
+    M, V = 10, 40000
+    logits = torch.from_numpy((rng.standard_normal((M, V)) * spread).astype(np.float32))
+    for t in (0.01, 0.1, 0.3, 2.0, 30.0):
+        u = rng.random(M).astype(np.float32)
+        kw = dict(temperature=np.full(M, t, np.float32))
+        check(logits, u, **kw)
+        check(logits, u, top_k=np.geomspace(1, V - 1, M).astype(np.int32), **kw)
+        check(logits, u, top_k=np.full(M, 50, np.int32), top_p=np.linspace(0.1, 0.99, M).astype(np.float32), min_p=np.full(M, 0.02, np.float32), **kw)
