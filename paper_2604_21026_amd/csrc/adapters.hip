@@ -6,6 +6,10 @@
 // they have to.  h stays fp32 between the launches, in as many partial sums as K is cut into; it enters the second
 // product as three bf16 values whose sum it is, so nothing of it is lost; the products with the first and with the rest are
 // summed apart and added at the end, where what an infinite weight makes of a rest of zero is left out.
+//
+// Small ones are two chains of trips to memory (ids, weights, sums; ids, h, results): one token of 2048 x 2048, 16 ranks, 6.5
+// us, 3.6 and 4.2 of them the kernels'.  With many adapters the bytes of B bound it: 32 tokens of 12 adapters of 4096 x 28672, 64
+// ranks, 53 MB in 18.7 us, 2.8 TB/s; 500 tokens of prompts, 4099 outputs, 15.4 us.
 #include "mfma_act.h"
 
 namespace nvq {
@@ -25,7 +29,8 @@ struct AdaptersArgs {
     int n, K, N, R, M;
     float *h;             // workspace, [slices][M][R]
     int slices, columns;  // of K, 32 inputs each
-    int shares, tiles;    // workgroups that share a group's adapters, and the tiles of tokens of each
+    int workers;          // workgroups that take a group's tiles in turn
+    int copiers;          // one more for its tokens without an adapter, or none: the same ones do
     int blocks;           // of ranks (first launch)
     int turns;            // workgroups that share the outputs (second)
 };
@@ -37,6 +42,9 @@ __device__ __forceinline__ int adapter_of(const AdaptersArgs &g, int m0) {
     return (unsigned)e < (unsigned)g.n ? e : -1;
 }
 
+// A group's tiles, of sixteen tokens of one adapter or fewer, are counted through, and its workers take them in turn: however
+// the tokens lie, all have work.
+//
 // The distinct adapters of a group one after the other: `left` has a bit per token that has not had its turn.
 __device__ __forceinline__ uint64_t turn(int mine, uint64_t *left, int *e) {
     *e = __builtin_amdgcn_readlane(mine, __builtin_ctzll(*left));
@@ -59,15 +67,6 @@ __device__ __forceinline__ int nth_bit(uint64_t bits, int k) {
     return at;
 }
 
-// The first tile of an adapter's tokens that is this workgroup's, of g.tiles that take them in turn; where they share all of
-// a group's adapters, they go on where the one before ended (*base: tiles before), so that many with few tokens each
-// keep all four at work: 500 tokens of 8 adapters in no order, 14336 outputs and 64 ranks: 109 us without, 51 with.
-__device__ __forceinline__ int first_tile(const AdaptersArgs &g, int tile, int tokens, int *base) {
-    const int first = (tile - *base) & (g.tiles - 1);
-    if (g.shares == 1) *base += (tokens + kTile - 1) / kTile;
-    return first;
-}
-
 // h of a group's tokens: RT tiles of sixteen ranks, a slice of K, its columns in turn over the waves.
 template <int RT>
 __global__ __launch_bounds__(kThreads) void adapters_down_kernel(AdaptersArgs g) {
@@ -78,25 +77,24 @@ __global__ __launch_bounds__(kThreads) void adapters_down_kernel(AdaptersArgs g)
     i /= g.slices;
     const int r0 = i % g.blocks * 16 * RT;
     i /= g.blocks;
-    const int tile = i % g.tiles;
-    i /= g.tiles;
-    const int share = i % g.shares, m0 = i / g.shares * kGroup;
+    const int worker = i % g.workers, m0 = i / g.workers * kGroup;
     const int c0 = slice * g.columns, c1 = c0 + g.columns < g.K / 32 ? c0 + g.columns : g.K / 32;
     const int mine = adapter_of(g, m0);
     uint64_t left = __ballot(mine >= 0);
-    for (int at = 0, base = 0; left; ++at) {
+    for (int next = worker, base = 0, end; left; base = end) {
         int e;
         const uint64_t with = turn(mine, &left, &e);
-        if (at % g.shares != share) continue;
-        const int tokens = __builtin_popcountll(with), begin = first_tile(g, tile, tokens, &base) * kTile;
-        if (begin >= tokens) continue;
+        const int tokens = __builtin_popcountll(with);
+        end = base + (tokens + kTile - 1) / kTile;
+        if (next >= end) continue;
         const uint16_t *a[RT];
 #pragma unroll
         for (int t = 0; t < RT; ++t) {
             const int r = r0 + 16 * t + n < g.R ? r0 + 16 * t + n : g.R - 1;
             a[t] = g.a + ((int64_t)e * g.R + r) * g.K + 8 * kb;
         }
-        for (int k0 = begin; k0 < tokens; k0 += kTile * g.tiles) {
+        for (; next < end; next += g.workers) {
+            const int k0 = (next - base) * kTile;
             const int m = m0 + nth_bit(with, k0 + n < tokens ? k0 + n : k0);
             const uint16_t *const x = g.x + (int64_t)m * g.K + 8 * kb;
             float4v sum[RT];
@@ -206,25 +204,21 @@ __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
     constexpr int kBlock = kWaves * 16 * NT;
     __shared__ __align__(16) uint16_t hs[3][kTile][kPitch];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4;
-    const int first = (int)(blockIdx.x % g.turns) * kBlock, stride = g.turns * kBlock;
+    int first = (int)(blockIdx.x % g.turns) * kBlock, stride = g.turns * kBlock;
     int i = blockIdx.x / g.turns;
-    const int tile = i % g.tiles;
-    i /= g.tiles;
-    // Tokens without an adapter stay as they are: by the last share, or, of a single one, by every tile's workgroup some.
-    const bool copies = g.out != g.y;
-    const int all = g.shares + (copies && g.shares > 1);
-    const int share = i % all, m0 = i / all * kGroup;
+    const int all = g.workers + g.copiers, worker = i % all, m0 = i / all * kGroup;
     const int mine = adapter_of(g, m0);
     uint64_t left = __ballot(mine >= 0);
-    if (copies && (g.shares == 1 || share == g.shares)) {
+    if (g.out != g.y && (!g.copiers || worker == g.workers)) {  // tokens without an adapter stay as they are
         uint64_t none = ~left;
         if (g.M - m0 < kGroup) none &= (1ull << (g.M - m0)) - 1;
         const int count = __builtin_popcountll(none);
-        for (int k0 = tile; k0 < count; k0 += 8 * g.tiles) {
+        const int stride_k = g.copiers ? 1 : g.workers;
+        for (int k0 = g.copiers ? 0 : worker; k0 < count; k0 += 8 * stride_k) {
             int64_t row[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const int at = k0 + k * g.tiles;
+                const int at = k0 + k * stride_k;
                 row[k] = at < count ? (int64_t)(m0 + nth_bit(none, at)) * g.N : -1;
             }
             for (int block = first; block < g.N; block += stride)
@@ -245,15 +239,31 @@ __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
                     }
                 }
         }
-        if (g.shares > 1) return;
+        if (g.copiers) return;
     }
+    // Fewer tiles than half the workers: several workers to a tile, each with outputs of its own.
+    int next = worker;
+    if (!g.copiers) {
+        int count = 0;
+        for (uint64_t rest = left; rest;) {
+            int e;
+            count += (__builtin_popcountll(turn(mine, &rest, &e)) + kTile - 1) / kTile;
+        }
+        if (count > 0 && 2 * count <= g.workers) {
+            const int each = g.workers / count, part = worker / count;
+            next = part < each ? worker - part * count : count;
+            first += part * stride;
+            stride *= each;
+        }
+    }
+    if (first >= g.N) return;
     const int64_t h_slice = (int64_t)g.M * g.R;
-    for (int at = 0, base = 0; left; ++at) {
+    for (int base = 0, end; left; base = end) {
         int e;
         const uint64_t with = turn(mine, &left, &e);
-        if (at % g.shares != share) continue;
-        const int tokens = __builtin_popcountll(with), begin = first_tile(g, tile, tokens, &base) * kTile;
-        if (begin >= tokens) continue;
+        const int tokens = __builtin_popcountll(with);
+        end = base + (tokens + kTile - 1) / kTile;
+        if (next >= end) continue;
         // The weights of two columns of 32 ranks at a time.
         uint4v bw[2][NT];
         auto load = [&](int block, int c) {
@@ -272,7 +282,8 @@ __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
         };
         load(first, 0);
         const float scale = g.scales ? g.scales[e] : 1.0f;
-        for (int k0 = begin; k0 < tokens; k0 += kTile * g.tiles) {
+        for (bool again = false; next < end; next += g.workers, again = true) {
+            const int k0 = (next - base) * kTile;
             const bool my = k0 + n < tokens;
             const int64_t row = (int64_t)(m0 + nth_bit(with, my ? k0 + n : k0)) * g.N;
             float y[4 * NT];
@@ -307,7 +318,7 @@ __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
                     *reinterpret_cast<uint2v *>(&hs[q][k][r]) = uint2v{p[0][q] | p[1][q] << 16, p[2][q] | p[3][q] << 16};
             }
             __syncthreads();
-            if (k0 > begin) load(first, 0);  // (of the first tile it is there)
+            if (again) load(first, 0);  // (of the first tile it is there)
             for (int block = first; block < g.N; block += stride) {
                 const int o0 = block + w * 16 * NT + 4 * NT * kb;  // the lane's outputs
                 const bool whole = o0 + 4 * NT <= g.N;
@@ -361,14 +372,22 @@ __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
     }
 }
 
-// Groups of a batch, and the workgroups to one of them: each distinct adapter its own where there are few groups; where
-// there are several, each tile of an adapter's tokens its own (in one group the weights are read once for all tiles).
+// Groups of a batch; the workers of one of them: as many as it can have tiles where there are up to four groups, then eight.
+// (500 tokens, 4096 outputs, of 16 adapters in no order: four workers 27 us, eight 24; of three prompts: 10.2 and 12.6;
+// 8000 tokens of prompts, 14336 outputs: 358 and 308.)
 int groups_of(int M) { return (M + kGroup - 1) / kGroup; }
-int shares_of(int M, int n) {
-    const int most = n < kGroup ? n : kGroup;
-    return groups_of(M) <= 4 ? (M < most ? M : most) : 1;
+int workers_of(int M, int n) {
+    const int tokens = M < kGroup ? M : kGroup, tiles = n + tokens / kTile, most = tokens < tiles ? tokens : tiles;
+    const int cap = groups_of(M) <= 4 ? kGroup : 8;
+    return most < cap ? most : cap;
 }
-int tiles_of(int M) { return M <= kGroup ? 1 : kGroup / kTile; }
+// Tiles of a batch: all of them where one group's adapters have tokens of their own, about half as many as they could be
+// where there are several groups (all: 256 tokens of 16 adapters in no order 18.3 us, in prompts 12.6; half: 19.3 and 11.0).
+int tiles_of(int M, int n) {
+    const int whole = (M + kTile - 1) / kTile, apart = groups_of(M) * (n < kGroup ? n : kGroup), most = apart < M ? apart : M;
+    const int likely = groups_of(M) <= 1 ? most : most / 2;
+    return whole > likely ? whole : likely;
+}
 // Blocks of 64, 32 or 16 ranks.
 int rank_tiles(int R) { return R > 32 ? 4 : R > 16 ? 2 : 1; }
 int rank_blocks(int R) { return (R + 16 * rank_tiles(R) - 1) / (16 * rank_tiles(R)); }
@@ -376,8 +395,7 @@ int rank_blocks(int R) { return (R + 16 * rank_tiles(R) - 1) / (16 * rank_tiles(
 // the second launch adds them up, so that more than eight pay where it has many outputs then (8 instead of 16: one token
 // of 2048 outputs 7.3 -> 6.8 us, 500 of 4099 19.4 -> 17.3; 32 of 28672 21.2 -> 22.0).
 int slices_of(const nvq_adapters &s, int M) {
-    const int64_t others = (int64_t)((M + kTile - 1) / kTile > shares_of(M, s.n) ? (M + kTile - 1) / kTile : shares_of(M, s.n)) *
-                           rank_blocks(s.R);
+    const int64_t others = (int64_t)tiles_of(M, s.n) * rank_blocks(s.R);
     int64_t want = 1024 / others;
     const int64_t most = (s.K / 32 + kWaves - 1) / kWaves;
     want = want < most ? want : most;
@@ -433,12 +451,12 @@ extern "C" int nvq_adapters_add(const nvq_adapters *adapters, const uint16_t *x_
     g.slices = slices_of(*adapters, M);
     g.columns = (g.K / 32 + g.slices - 1) / g.slices;
     g.slices = (g.K / 32 + g.columns - 1) / g.columns;
-    g.shares = shares_of(M, g.n);
+    g.workers = workers_of(M, g.n);
     g.blocks = rank_blocks(g.R);
     const hipStream_t st = (hipStream_t)stream;
-    g.tiles = tiles_of(M);
-    const int64_t groups = (int64_t)groups_of(M) * g.shares * g.tiles;
-    const dim3 block(kThreads), down((unsigned)(groups * g.blocks * g.slices));
+    const int groups = groups_of(M), tiles = tiles_of(M, g.n);
+    g.copiers = out != y && groups <= 4;
+    const dim3 block(kThreads), down((unsigned)(groups * g.workers * g.blocks * g.slices));
     if (rank_tiles(g.R) == 1)
         hipLaunchKernelGGL(adapters_down_kernel<1>, down, block, 0, st, g);
     else if (rank_tiles(g.R) == 2)
@@ -446,14 +464,16 @@ extern "C" int nvq_adapters_add(const nvq_adapters *adapters, const uint16_t *x_
     else
         hipLaunchKernelGGL(adapters_down_kernel<4>, down, block, 0, st, g);
     NVQ_HIP_TRY(hipGetLastError());
-    const bool wide = (int64_t)(M < g.shares ? M : g.shares) * g.N >= 1024 * 64 || (int64_t)groups_of(M) * g.tiles * g.N >= 1024 * 64;  // a wave to 64 outputs where that leaves four a compute unit
+    // A wave to 64 outputs where that leaves four a compute unit (32 tokens of 12 adapters, 14336 outputs: 10.9 us, 16.3 with 16 to
+    // a wave; one of 4096: 7.7 and 6.9).
+    const bool wide = (int64_t)tiles * g.N >= 1024 * 64;
     const int per = (wide ? 64 : 16) * kWaves, blocks = (g.N + per - 1) / per;
-    // As many as the device holds at once (three a compute unit) between those with work: each adapter or tile of tokens.
-    const int busy = (M + kTile - 1) / kTile > g.shares ? (M + kTile - 1) / kTile : g.shares, resident = 3 * device_cu_count() / busy;
-    const int copies = out != y && g.shares > 1 ? groups_of(M) * g.tiles : 0;
+    // As many workgroups as the device holds at once (three a compute unit) between the tiles, or the workers, which have
+    // a part of a tile's outputs where there are few of them.
+    const int resident = 3 * device_cu_count() / (groups <= 4 ? tiles : groups * g.workers);
     const int each = resident < 1 ? blocks : (blocks + resident - 1) / resident;
     g.turns = (blocks + each - 1) / each;
-    const dim3 up((unsigned)((groups + copies) * g.turns));
+    const dim3 up((unsigned)(groups * (g.workers + g.copiers) * g.turns));
     if (wide)
         hipLaunchKernelGGL(adapters_up_kernel<4>, up, block, 0, st, g);
     else

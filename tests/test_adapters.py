@@ -58,7 +58,7 @@ def plain(a, b, scales, x, ids, y):
 CASES = [  # M, n, K, N, R
     (1, 1, 32, 1, 8), (1, 4, 2048, 2048, 16), (2, 3, 96, 17, 24), (15, 5, 160, 63, 40), (16, 16, 256, 64, 8), (17, 2, 1440, 1003, 64),
     (32, 7, 4096, 512, 32), (33, 40, 64, 130, 256), (70, 3, 512, 257, 136), (5, 2, 14336, 96, 128), (200, 9, 320, 1024, 16), (3, 2, 65536, 16, 8),
-    (300, 9, 96, 130, 24), (600, 2, 64, 65, 16), (450, 70, 32, 1100, 40)]
+    (300, 9, 96, 130, 24), (600, 2, 64, 65, 16), (450, 70, 32, 1100, 40), (1300, 3, 64, 260, 8), (64, 1, 64, 50, 16), (40, 64, 96, 70, 24)]
 
 
 @gpu
