@@ -263,7 +263,8 @@ def test_attention_of_as_many_sequences_as_it_takes():
 
 
 @gpu
-def test_a_token_read_twice_and_pages_that_sequences_share():
+@pytest.mark.parametrize("times", [8, 60])
+def test_a_token_read_twice_and_pages_that_sequences_share(times):
     rng = np.random.default_rng(3)
     n, heads, D, page = 40, 2, 64, 16
     pool = Pool(rng, [n, n], heads, D, page, False)
@@ -272,7 +273,7 @@ def test_a_token_read_twice_and_pages_that_sequences_share():
     pool.put(0, np.arange(n), k, v)
     pool.put(1, np.arange(32, n), ref.to_bf16((k[32:] + 1.0).astype(np.float32)).astype(np.float64), v[32:])
     cache, table = pool.device(), dev(pool.table)
-    at, of = np.array([5, 5, 6, 7, 6, 0, 39, 38, 39, 31, 32, 33] * 8, np.int32), np.array([0, 1, 1, 1, 0, 0, 0, 0, 0, 1, 1, 1] * 8, np.int32)
+    at, of = np.array([5, 5, 6, 7, 6, 0, 39, 38, 39, 31, 32, 33] * times, np.int32), np.array([0, 1, 1, 1, 0, 0, 0, 0, 0, 1, 1, 1] * times, np.int32)
     got = nvq.cache_read(cache, table, dev(at), dev(of))
     page_of = pool.table[of, at // page]
     assert same_bits(got[0], pool.k[page_of, :, at % page]) and same_bits(got[1], pool.v[page_of, :, at % page])
