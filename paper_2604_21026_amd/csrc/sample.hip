@@ -11,6 +11,10 @@
 // Weights are 64-bit fixed point relative to the largest, so that sums do not depend on their order.  A row whose bins
 // hold too many tokens (nearly equal logits), or whose logits are out of the bins' range, is looked at by one workgroup
 // alone, eleven bits of the sort words after the other (choose_slowly, in the second launch).
+//
+// Neither bytes nor operations bound a few rows but the chain of trips to memory and through LDS: one row of 128256 in 20.5 us (14
+// and 6.5 in the kernels: logits 1.5, bins 2.6, the parts' arrival 1, their bins 3.5 (196 KB through one compute unit), sums
+// 0.9, search 1.4; logits and list 3.5, the choice 1.5), five of 32003 in 16 bits 19.8, 32 of 128256 29.7 (16.4 MB).
 #include <type_traits>
 
 #include "mfma_act.h"
