@@ -732,9 +732,11 @@ int nvq_attention(const nvq_cache *cache, const uint16_t *q, int64_t q_stride, i
  *   min_p > 0          those with w_i >= min_p
  * and the first token always.  ids[m] = the first token at which the running sum of the
  * kept weights exceeds u[m] times their sum (u below 0 or NaN counts as 0, from 1 on the
- * last kept one is taken).  A temperature that is not above 0 takes the first token.
- * Weights are fixed point with 43 bits after the point, from fp64; sums of them are
- * exact, so the same call gives the same tokens.  NaN and minus infinity are never
+ * last kept one with a weight is taken).  A temperature that is not above 0 takes the
+ * first token, and so does a top_p that is not.
+ * Weights are fixed point with 43 bits after the point, from fp64 (those below half of
+ * that count for nothing); their sums are off by less than 2^-30 of the row's and do not
+ * depend on an order, so the same call gives the same tokens.  NaN and minus infinity are never
  * chosen and do not count; plus infinity is chosen before all; a row without a token to
  * choose gets -1.
  *   logits  [M][V] f32 or bf16 (dtype), ld >= V elements from row to row; 4-byte

@@ -14,8 +14,8 @@
 // is left out there.
 //
 // The bytes of keys and values bound it: one sequence of 131072 tokens, 8 key heads of 128 in bf16, 537 MB, takes 99.5 us,
-// 5.4 TB/s, where reading alone in the same split takes 95; 32 ragged ones of up to 16384 tokens in 8 bits, 253 MB, 62 us,
-// 46 of them reading.  Short ones are bound by the memory's latency, four times over (lengths, pages, keys and values,
+// 5.4 TB/s, where reading alone in the same split takes 95; 32 ragged ones of up to 16384 tokens in 8 bits, 261 MB, 62 us,
+// 47 of them reading.  Short ones are bound by the memory's latency, four times over (lengths, pages, keys and values,
 // joins): 500 tokens 10 us, 7 sequences of up to 3000 behind a window of 1000 14 us.
 #include <type_traits>
 

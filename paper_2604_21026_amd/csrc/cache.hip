@@ -5,7 +5,7 @@
 // such block are taken together, turned over in registers (8 channels by 8 tokens a thread) and stored as whole pieces;
 // a token whose neighbours are elsewhere, as each one of a decode step, goes element by element.
 //
-// 4096 tokens of 32 + 8 heads of 128 into an 8-bit cache: 94 MB in 26.6 us, 3.5 TB/s (a copy of that size 4.8); read back 33 MB in
+// 4096 tokens of 32 + 8 heads of 128 into an 8-bit cache: 94 MB in 26.6 us, 3.5 TB/s (a copy of that size 4.8); read back 25 MB in
 // 9.8.  One token: 3.7 and 2.2 us, a launch and two trips to memory (places, then rows).
 #include "cache.h"
 
