@@ -13,8 +13,8 @@
 // apart and added at the end: what an infinite value makes of the rest (zero times infinity, or the other sign)
 // is left out there.
 //
-// The bytes of keys and values bound it: one sequence of 131072 tokens, 8 key heads of 128 in bf16, 537 MB, takes 99.5 us,
-// 5.4 TB/s, where reading alone in the same split takes 95; 32 ragged ones of up to 16384 tokens in 8 bits, 261 MB, 62 us,
+// The bytes of keys and values bound it: one sequence of 131072 tokens, 8 key heads of 128 in bf16, 537 MB, takes 92 us,
+// 5.8 TB/s, where a plain reading of as much takes 83; 32 ragged ones of up to 16384 tokens in 8 bits, 261 MB, 61 us,
 // 47 of them reading.  Short ones are bound by the memory's latency, four times over (lengths, pages, keys and values,
 // joins): 500 tokens 10 us, 7 sequences of up to 3000 behind a window of 1000 14 us.
 #include <type_traits>
@@ -91,7 +91,9 @@ struct State {
     }
 };
 
-// Pieces of eight values as they lie in the cache, and as an operand.
+// Pieces of eight values as they lie in the cache, and as an operand.  load_once: for what one load takes whole lines of and no
+// other reads (the values: 131072 tokens 99.3 -> 91.9 us, 30 sequences of 2000 48.7 -> 45.8; keys, of whose lines a load takes
+// a half or a quarter, would come twice, 61 -> 72 us in 8 bits.  16000 tokens, which a cache may hold, 21.8 -> 22.9).
 template <bool E4M3>
 struct Piece;
 template <>
@@ -99,6 +101,9 @@ struct Piece<false> {
     typedef uint4v raw;
     __device__ static raw load(const void *base, int64_t at) {
         return *as_global<uint4v>(static_cast<const uint16_t *>(base) + at);
+    }
+    __device__ static raw load_once(const void *base, int64_t at) {
+        return __builtin_nontemporal_load(as_global<uint4v>(static_cast<const uint16_t *>(base) + at));
     }
     __device__ static bf16x8 operand(raw r) { return __builtin_bit_cast(bf16x8, r); }
     // Zeros where the token of a value does not count (bit j: token j does).
@@ -114,6 +119,9 @@ struct Piece<true> {
     typedef uint2v raw;
     __device__ static raw load(const void *base, int64_t at) {
         return *as_global<uint2v>(static_cast<const uint8_t *>(base) + at);
+    }
+    __device__ static raw load_once(const void *base, int64_t at) {
+        return __builtin_nontemporal_load(as_global<uint2v>(static_cast<const uint8_t *>(base) + at));
     }
     __device__ static bf16x8 operand(raw r) {
         const uint32_t lo = r.x, hi = r.y;
@@ -186,7 +194,7 @@ __device__ __forceinline__ void attend(const AttentionArgs &a, int b, int head, 
         f.value_ok = there(s, kb, page);
         const int64_t at = value_at(a.c, f.value_ok ? page : 0, head, slot) + 8 * n;
 #pragma unroll
-        for (int d = 0; d < T; ++d) f.v[d] = P::load(a.c.v, at + 128 * d);
+        for (int d = 0; d < T; ++d) f.v[d] = P::load_once(a.c.v, at + 128 * d);
         if (E4M3) f.value_scales = *as_global<uint2v>(a.c.scales + scale_at(a.c, f.value_ok ? page : 0, head, 1, slot));
     };
     const int key_page = page_of(step, n >> 2), first_value_page = page_of(step, kb);
