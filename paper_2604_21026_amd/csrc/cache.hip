@@ -5,8 +5,10 @@
 // such block are taken together, turned over in registers (8 channels by 8 tokens a thread) and stored as whole pieces;
 // a token whose neighbours are elsewhere, as each one of a decode step, goes element by element.
 //
-// 4096 tokens of 32 + 8 heads of 128 into an 8-bit cache: 94 MB in 26.6 us, 3.5 TB/s (a copy of that size 4.8); read back 25 MB in
-// 9.8.  One token: 3.7 and 2.2 us, a launch and two trips to memory (places, then rows).
+// 4096 tokens of 32 + 8 heads of 128 into an 8-bit cache: 94 MB in 21 us, 4.5 TB/s (a copy of that size 4.8); read back 25 MB in
+// 9.1.  One token: 3.7 and 2.2 us, a launch and two trips to memory (places, then rows).
+#include <type_traits>
+
 #include "cache.h"
 
 namespace nvq {
@@ -76,6 +78,7 @@ struct AppendArgs {
     int H, angles, rot, interleaved;
     int row_blocks;  // workgroups of queries and keys
     int step;        // tokens of a workgroup's threads, one after the other: 8, or 1 of a few tokens
+    bool once;       // queries and keys past the caches
 };
 
 struct MaxBits {
@@ -181,6 +184,26 @@ __device__ __forceinline__ uint32_t both(uint32_t a, uint32_t b, int i) {
 }
 
 constexpr int kRowsEach = 4;
+
+// 16 bytes of a row; ONCE: past the caches, for calls whose rows are more than these keep anyway (once_of).
+template <bool ONCE>
+__device__ __forceinline__ uint4 load_row(const uint16_t *p) {
+    typedef uint32_t vec __attribute__((ext_vector_type(4)));
+    if constexpr (!ONCE) return *reinterpret_cast<const uint4 *>(p);
+    const vec v = __builtin_nontemporal_load(reinterpret_cast<const vec *>(p));
+    return make_uint4(v.x, v.y, v.z, v.w);
+}
+template <typename T>
+__device__ __forceinline__ void store_row(uint16_t *p, const T &w, bool once) {
+    typedef uint32_t vec __attribute__((ext_vector_type(sizeof(T) / 4)));
+    if (once) {
+        asm volatile("" ::: "memory");  // (around it, or the two stores become one plain one)
+        __builtin_nontemporal_store(__builtin_bit_cast(vec, w), reinterpret_cast<vec *>(p));
+        asm volatile("" ::: "memory");
+    } else {
+        *reinterpret_cast<T *>(p) = w;
+    }
+}
 
 // The values of `a.step` tokens from t0 on, E channels of head h per thread, L threads to a head: what lies side by side
 // is read row by row, turned over and stored as whole pieces of eight tokens.
@@ -296,15 +319,21 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(AppendArgs a) {
     const int o1 = halves ? o0 + a.rot / 2 : o0 + 8;
     uint4 w[kRowsEach][2];
     float c[8], s[8];
+    auto read_rows = [&](auto once) {
 #pragma unroll
-    for (int r = 0; r < kRowsEach; ++r) {
-        w[r][0] = w[r][1] = make_uint4(0, 0, 0, 0);
-        const int h = h0 + r;
-        if (!in || h >= all) continue;  // (rows are read before it is known whether they have a place)
-        const uint16_t *const row = h < a.H ? a.q + t * a.q_stride + h * D : a.k + t * a.k_stride + (h - a.H) * D;
-        w[r][0] = *reinterpret_cast<const uint4 *>(row + o0);
-        w[r][1] = *reinterpret_cast<const uint4 *>(row + o1);
-    }
+        for (int r = 0; r < kRowsEach; ++r) {
+            w[r][0] = w[r][1] = make_uint4(0, 0, 0, 0);
+            const int h = h0 + r;
+            if (!in || h >= all) continue;  // (rows are read before it is known whether they have a place)
+            const uint16_t *const row = h < a.H ? a.q + t * a.q_stride + h * D : a.k + t * a.k_stride + (h - a.H) * D;
+            w[r][0] = load_row<decltype(once)::value>(row + o0);
+            w[r][1] = load_row<decltype(once)::value>(row + o1);
+        }
+    };
+    if (a.once)
+        read_rows(std::true_type());
+    else
+        read_rows(std::false_type());
     if (on && turn) {
         const float *const cs = a.cos_sin + (int64_t)at.position * a.rot + 8 * i;
 #pragma unroll
@@ -342,8 +371,8 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(AppendArgs a) {
         }
         if (on && h < a.H) {
             uint16_t *const out = a.q_out + ((int64_t)t * a.H + h) * D;
-            *reinterpret_cast<uint4 *>(out + o0) = w[r][0];
-            *reinterpret_cast<uint4 *>(out + o1) = w[r][1];
+            store_row(out + o0, w[r][0], a.once);
+            store_row(out + o1, w[r][1], a.once);
         }
         const bool key = on && h >= a.H && h < all;
         if (!__any(key)) continue;
@@ -374,6 +403,7 @@ struct ReadArgs {
     uint16_t *k, *v;
     int row_blocks;  // workgroups of keys
     int step;        // as in AppendArgs
+    bool once;       // results past the caches
 };
 
 typedef float float2v __attribute__((ext_vector_type(2)));
@@ -451,7 +481,7 @@ __device__ void read_values(const ReadArgs &a, int unit_block) {
         }
 #pragma unroll
         for (int k = 0; k < 8; ++k)
-            if (k >= first && k < first + n) *reinterpret_cast<word *>(out + (int64_t)(k - first) * a.c.heads * D) = row[k];
+            if (k >= first && k < first + n) store_row(out + (int64_t)(k - first) * a.c.heads * D, row[k], a.once);
     }
 }
 
@@ -476,7 +506,7 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(ReadArgs a) {
         else
             w = *reinterpret_cast<const uint4 *>(static_cast<const uint16_t *>(a.c.k) + from);
     }
-    *reinterpret_cast<uint4 *>(a.k + (t * a.c.heads + h) * D + 8 * i) = w;
+    store_row(a.k + (t * a.c.heads + h) * D + 8 * i, w, a.once);
 }
 
 // Threads to a head: L of sixteen channels of keys; and of the values 8 L of two, or 64 of four.
@@ -487,6 +517,9 @@ int value_lanes(int D) { return D <= 128 ? 8 * key_lanes(D) : 64; }
 // tokens 4.0 + 3.0 and 3.7 + 3.7 us, of 512 5.1 + 3.7 and 4.4 + 3.9, of 1024 8.3 + 5.4 and 6.3 + 4.3, in 8 bits 11.4 + 6.3 and 7.3 +
 // 4.5; 512 tokens of as many sequences 6.8 + 3.3 and 9.5 + 7.2.)
 int step_of(const Places &p) { return p.sequences && p.T >= 512 ? 8 : 1; }
+// Rows past the caches from 8 MiB on, twice a cache's size: queries and keys of 4096 tokens of 40 heads of 128 21 instead of 26 us, of
+// 2048 13.5 and 16.8 (12.7 and 13.9 where caches hold what comes in), of 1000 8.2 and 10.1 (8.4 and 8.4); read back, 4096 9.1 and 9.8.
+bool once_of(int64_t values) { return 2 * values >= 8 << 20; }
 int64_t value_blocks(const Places &p, int heads, int D) {
     const int step = step_of(p);
     return ((int64_t)((p.T + step - 1) / step) * heads * value_lanes(D) + kThreads - 1) / kThreads;
@@ -533,6 +566,7 @@ extern "C" int nvq_cache_append(const nvq_cache *cache, const int32_t *table, in
     const int64_t rows = (int64_t)T * ((H + cache->heads + kRowsEach - 1) / kRowsEach);
     a.row_blocks = (int)((rows * L + kThreads - 1) / kThreads);
     a.step = step_of(a.p);
+    a.once = once_of(T * ((int64_t)H + cache->heads) * D);
     const dim3 grid((unsigned)(a.row_blocks + value_blocks(a.p, cache->heads, (int)D))), block(kThreads);
     const hipStream_t st = (hipStream_t)stream;
     if (L == 2)
@@ -564,6 +598,7 @@ extern "C" int nvq_cache_read(const nvq_cache *cache, const int32_t *table, int 
     const int L = key_lanes(cache->head_dim);
     a.row_blocks = (int)(((int64_t)T * cache->heads * 2 * L + kThreads - 1) / kThreads);
     a.step = step_of(a.p);
+    a.once = once_of((int64_t)T * 2 * cache->heads * cache->head_dim);
     const dim3 grid((unsigned)(a.row_blocks + value_blocks(a.p, cache->heads, cache->head_dim))), block(kThreads);
     const hipStream_t st = (hipStream_t)stream;
     if (L == 2)

@@ -163,7 +163,9 @@ APPEND = [  # T, B, H, heads, D, rot, page, interleaved
     (9, 9, 5, 5, 224, 112, 1024, True), (40, 1, 7, 1, 160, 16, 8, False), (300, 2, 0, 3, 192, 192, 16, False),
     # (values in runs of up to eight tokens from 512 tokens on)
     (600, 2, 8, 4, 128, 128, 16, True), (515, 50, 0, 3, 192, 96, 8, False), (777, 3, 2, 2, 64, 32, 1024, False), (1030, 1, 7, 1, 160, 16, 8, False),
-    (520, 4, 2, 2, 256, 256, 64, True), (512, 512, 1, 1, 32, 32, 16, False), (900, 7, 3, 1, 96, 48, 32, False)]
+    (520, 4, 2, 2, 256, 256, 64, True), (512, 512, 1, 1, 32, 32, 16, False), (900, 7, 3, 1, 96, 48, 32, False),
+    # (rows past the caches)
+    (2200, 3, 9, 8, 128, 128, 32, False)]
 
 
 @gpu
