@@ -180,3 +180,20 @@ def test_sample_of_low_and_high_temperatures(spread):
         check(logits, u, **kw)
         check(logits, u, top_k=np.geomspace(1, V - 1, M).astype(np.int32), **kw)
         check(logits, u, top_k=np.full(M, 50, np.int32), top_p=np.linspace(0.1, 0.99, M).astype(np.float32), min_p=np.full(M, 0.02, np.float32), **kw)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_sample_of_many_equal_logits_among_others(dtype):
+    """bf16 values of both signs around powers of two, where their distance changes, many of each: lists of hundreds of equal ones."""
+    rng = np.random.default_rng(23)
+    M, V = 12, 30000
+    for centre, spread in ((0.0, 1.0), (4.0, 0.3), (-4.0, 0.3), (-8.0, 0.5), (16.0, 1.0), (-0.25, 0.02), (-1.0, 0.05)):
+        logits = torch.from_numpy((centre + rng.standard_normal((M, V)) * spread).astype(np.float32)).bfloat16().to(dtype)
+        u = rng.random(M).astype(np.float32)
+        check(logits, u, temperature=np.full(M, 1.5, np.float32))
+        check(logits, u, top_k=np.geomspace(2, V - 1, M).astype(np.int32), top_p=np.full(M, 0.9, np.float32))
+        # (one value among them that bf16 does not hold)
+        if dtype == torch.float32:
+            logits[:, 7] += 2.0 ** -12
+            check(logits, u, temperature=np.full(M, 1.5, np.float32), top_p=np.full(M, 0.97, np.float32))
