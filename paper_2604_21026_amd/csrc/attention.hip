@@ -387,15 +387,17 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     auto row_of = [&](int b, int ht) { return (int64_t)b * a.H + key_head_of(ht) * a.group + kHeadTile * tile_of(ht); };
 
     int total = 0, longest = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kThreads) {
+    if (a.B <= 64) {  // every wave all of them, without waiting for the others
+        const int steps = lane < a.B ? span_of(a, lane).steps : 0, sum = scan_wave(steps > 0 ? steps + kPieceCost : 0);
+        longest = wave_most(steps);
+        total = of_lane(sum, 63);
+        if (lane < a.B) upto[lane + 1] = sum;  // (the same by all)
+    }
+    for (int b0 = 0; a.B > 64 && b0 < a.B; b0 += kThreads) {
         const int b = b0 + (int)threadIdx.x;
         const int steps = b < a.B ? span_of(a, b).steps : 0;
-        int sum = steps > 0 ? steps + kPieceCost : 0;
+        const int sum = scan_wave(steps > 0 ? steps + kPieceCost : 0);
         longest = steps > longest ? steps : longest;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int o = __shfl_up(sum, d);
-            if (lane >= d) sum += o;
-        }
         __syncthreads();
         if (lane == 63) scan[w] = sum;
         const int most = wave_most(longest);
@@ -411,9 +413,9 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
         if (b < a.B) upto[b + 1] = before + sum;
         total = all;
     }
-    if (threadIdx.x == 0) upto[0] = 0;
-    if (threadIdx.x < 2 * kWaves) held[threadIdx.x >> 1][threadIdx.x & 1].b = -1;
-    __syncthreads();
+    if (lane == 0) upto[0] = 0;
+    if (lane < 2) held[w][lane].b = -1;
+    if (a.B > 64) __syncthreads();
     for (int b = blockIdx.x; b < a.B; b += gridDim.x)
         if (upto[b + 1] == upto[b]) {  // nothing to attend to
             for (int i = threadIdx.x; i < a.H * D; i += kThreads) store_global(a.out, a.out_dtype, (int64_t)b * a.H * D + i, 0.0f);
@@ -717,9 +719,10 @@ int launch_attention(AttentionArgs a, hipStream_t st) {
     constexpr int kWaves = waves_of<D>();
     const int cu = device_cu_count(), heads = a.group < kHeadTile ? a.group : kHeadTile;
     const int64_t steps = (int64_t)a.B * (((int64_t)a.width << a.c.page_shift) / kStep + 1 + kPieceCost) * a.c.heads * a.tiles;
-    const int64_t want = (steps + 2 * kWaves - 1) / (2 * kWaves), most = cu < kMaxGroups ? cu : kMaxGroups;
+    const int64_t pieces = (int64_t)a.B * a.c.heads * a.tiles, ranges = (steps + 2 * kWaves - 1) / (2 * kWaves),
+                  want = ranges > pieces ? ranges : pieces, most = cu < kMaxGroups ? cu : kMaxGroups;
     const dim3 grid((unsigned)(want < most ? want : most)), block(64 * kWaves);
-    a.most_each = (int)(grid.x / ((int64_t)a.B * a.c.heads * a.tiles));
+    a.most_each = (int)(grid.x / pieces);
     // (the parts' room also holds the factors and sums of a join: kMaxGroups + 2 per head)
     static_assert(2 * kWaves * (D + 2) >= kMaxGroups + 2, "room for a join");
     const size_t lds = (((size_t)a.B + 1) * 4 + 15) / 16 * 16 + sizeof(float) * 2 * kWaves * heads * (D + 2);

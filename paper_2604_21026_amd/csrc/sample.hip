@@ -146,38 +146,6 @@ __device__ __forceinline__ uint32_t over_lanes(uint32_t v, OP op) {
     v = with_lane_xor<2>(v, op);
     return with_lane_xor<1>(v, op);
 }
-// The lane's value N lanes before it in its row of sixteen, 0 for the first N.
-template <int N, typename T>
-__device__ __forceinline__ T row_up(T v) {
-    if constexpr (sizeof(T) == 8) {
-        const uint32_t lo = row_up<N>((uint32_t)v), hi = row_up<N>((uint32_t)((uint64_t)v >> 32));
-        return (T)((uint64_t)hi << 32 | lo);
-    } else {
-        return (T)__builtin_amdgcn_update_dpp(0, (int)v, 0x110 | N, 0xf, 0xf, true);
-    }
-}
-template <typename T>
-__device__ __forceinline__ T of_lane(T v, int lane) {  // (a lane that all have in common)
-    if constexpr (sizeof(T) == 8)
-        return (T)((uint64_t)of_lane((uint32_t)((uint64_t)v >> 32), lane) << 32 | of_lane((uint32_t)v, lane));
-    else
-        return (T)__builtin_amdgcn_readlane((int)v, lane);
-}
-// Sum up to and with each lane, in its row of sixteen and in the wave.
-template <typename T>
-__device__ __forceinline__ T scan_row(T v) {
-    v += row_up<1>(v);
-    v += row_up<2>(v);
-    v += row_up<4>(v);
-    return v + row_up<8>(v);
-}
-template <typename T>
-__device__ __forceinline__ T scan_wave(T v) {
-    v = scan_row(v);
-    const T r0 = of_lane(v, 15), r1 = of_lane(v, 31), r2 = of_lane(v, 47);
-    const int lane = threadIdx.x & 63;
-    return v + (lane >= 16 ? r0 : 0) + (lane >= 32 ? r1 : 0) + (lane >= 48 ? r2 : 0);
-}
 // Sum over the threads before this one; *all: over all.  By the first W waves.
 template <int W, typename T>
 __device__ __forceinline__ T scan_block(T *wave, T v, T *all) {
