@@ -13,10 +13,10 @@
 // apart and added at the end: what an infinite value makes of the rest (zero times infinity, or the other sign)
 // is left out there.
 //
-// The bytes of keys and values bound it: one sequence of 131072 tokens, 8 key heads of 128 in bf16, 537 MB, takes 92 us,
-// 5.8 TB/s, where a plain reading of as much takes 83; 32 ragged ones of up to 16384 tokens in 8 bits, 261 MB, 61 us,
+// The bytes of keys and values bound it: one sequence of 131072 tokens, 8 key heads of 128 in bf16, 537 MB, takes 90 us,
+// 6.0 TB/s, where a plain reading of as much takes 83; 32 ragged ones of up to 16384 tokens in 8 bits, 261 MB, 60 us,
 // 47 of them reading.  Short ones are bound by the memory's latency, four times over (lengths, pages, keys and values,
-// joins): 500 tokens 10 us, 7 sequences of up to 3000 behind a window of 1000 14 us.
+// joins): 500 tokens 9 us, 7 sequences of up to 3000 behind a window of 1000 13.8 us.
 #include <type_traits>
 
 #include "cache.h"
@@ -437,15 +437,23 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     const int groups = want < (int64_t)gridDim.x ? (int)want : (int)gridDim.x;
     const int g = blockIdx.x;
     int64_t f0, f1;
+    PieceOf own;      // the sequence and head tile of one's own, if dealt out; `begin`: none
+    int64_t own_at;   // its place on the line
     // Of a sequence and head tile's n steps: workgroups that have some of them.
     auto members_of = [&](int n) { return (n + kPart - 1) / kPart < each ? (n + kPart - 1) / kPart : each; };
     if (dealt) {
-        const int piece = each == 1 ? g : g / each, j = g - piece * each, b = piece / per;
-        const int n = b < a.B ? upto[b + 1] - upto[b] - cost : 0;
-        if (n <= 0 || j >= members_of(n)) return;
-        const int64_t at = (int64_t)per * upto[b] + (int64_t)(piece - b * per) * n;
-        f0 = at + quotient((int64_t)n * j, members_of(n));
-        f1 = at + quotient((int64_t)n * (j + 1), members_of(n));
+        const int piece = each == 1 ? g : g / each, j = g - piece * each;
+        own.b = piece / per;
+        own.ht = piece - own.b * per;
+        own.n = own.b < a.B ? upto[own.b + 1] - upto[own.b] - cost : 0;
+        const int members = members_of(own.n);
+        if (own.n <= 0 || j >= members) return;
+        f0 = own_at = (int64_t)per * upto[own.b] + (int64_t)own.ht * own.n;
+        f1 = f0 + own.n;
+        if (members > 1) {
+            f1 = f0 + quotient((int64_t)own.n * (j + 1), members);
+            f0 += quotient((int64_t)own.n * j, members);
+        }
     } else {
         if (g >= groups) return;
         f0 = quotient(T * g, groups);
@@ -456,21 +464,27 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
 
     auto write = [&](int64_t row, int i, float v) { store_global(a.out, a.out_dtype, row * D + i, v); };
     for (int64_t f = w0; f < w1;) {
-        const int x = (int)quotient(f, per);
-        int lo = 0, hi = a.B;  // upto[lo] <= x < upto[hi]
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (upto[mid] <= x)
-                lo = mid;
-            else
-                hi = mid;
-        }
         PieceOf p;
-        p.b = __builtin_amdgcn_readfirstlane(lo);
-        p.n = __builtin_amdgcn_readfirstlane(upto[lo + 1] - upto[lo]) - cost;
-        const int64_t r = f - (int64_t)per * upto[lo];
-        p.ht = __builtin_amdgcn_readfirstlane((int)quotient(r, p.n));
-        p.begin = __builtin_amdgcn_readfirstlane((int)(r - (int64_t)p.ht * p.n));
+        if (dealt) {
+            p = own;
+            p.begin = __builtin_amdgcn_readfirstlane((int)(f - own_at));
+        } else {
+            const int x = (int)quotient(f, per);
+            int lo = 0, hi = a.B;  // upto[lo] <= x < upto[hi]
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) / 2;
+                if (upto[mid] <= x)
+                    lo = mid;
+                else
+                    hi = mid;
+            }
+            p.b = __builtin_amdgcn_readfirstlane(lo);
+            p.n = upto[lo + 1] - upto[lo];
+            const int64_t r = f - (int64_t)per * upto[lo];
+            p.ht = __builtin_amdgcn_readfirstlane((int)quotient(r, p.n));
+            p.begin = __builtin_amdgcn_readfirstlane((int)(r - (int64_t)p.ht * p.n));
+        }
+        p.n = __builtin_amdgcn_readfirstlane(p.n);
         p.end = (int64_t)(p.n - p.begin) < w1 - f ? p.n : p.begin + (int)(w1 - f);
         p.end = __builtin_amdgcn_readfirstlane(p.end);
         f += p.end - p.begin;
@@ -514,16 +528,12 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     // at once; with loops over the waves, one value after the other, this took 4 us.)
     PieceOf shared_piece[2];  // what is left for others to join: begun before this workgroup, going on after it
     shared_piece[0].b = shared_piece[1].b = -1;
-    int ends[kWaves];  // of the first slots; -1: empty
-    uint32_t starts = 0;
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) {
-        ends[i] = held[i][0].b >= 0 ? held[i][0].end : -1;
-        starts |= held[i][1].b >= 0 ? 1u << i : 0u;
-    }
-#pragma unroll
-    for (int i = 0; i < kWaves; ++i) ends[i] = __builtin_amdgcn_readfirstlane(ends[i]);
-    starts = __builtin_amdgcn_readfirstlane(starts);
+    // Of the first slots, by a lane each: where their pieces end, which there are, and which end in them; which second ones there are.
+    const PieceOf first_slot = held[lane & (kWaves - 1)][0];
+    const int end_of = first_slot.end;
+    const uint32_t goes = (uint32_t)__ballot(lane < kWaves && first_slot.b >= 0);
+    const uint32_t ended = goes & (uint32_t)__ballot(first_slot.end == first_slot.n);
+    const uint32_t starts = (uint32_t)__ballot(lane < kWaves && held[lane & (kWaves - 1)][1].b >= 0);
     // (start -1: what begins before this workgroup, in the first slot of the first wave that has any steps)
     int front = 0;
     while (R * (front + 1) / kWaves == 0) ++front;
@@ -542,13 +552,12 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
         p.n = __builtin_amdgcn_readfirstlane(in_lds.n);
         uint32_t members = 1u << first;
         int until = p.end;
-#pragma unroll
-        for (int i = 1; i < kWaves; ++i)
-            if (i > first && until < p.n && ends[i] >= 0) {
-                members |= 1u << i;
-                until = ends[i];
-            }
-        members = __builtin_amdgcn_readfirstlane(members);
+        if (until < p.n) {
+            const uint32_t after = ~((2u << first) - 1), stop = ended & after;
+            members |= goes & after & (stop ? stop ^ (stop - 1) : ~0u);
+            const int top = 31 - __builtin_clz(members);
+            if (top > first) until = __builtin_amdgcn_readlane(end_of, top);
+        }
         const int heads = heads_of(p.ht);
         const bool whole = p.begin == 0 && until == p.n;
         const int to_slot = p.begin > 0 ? 0 : 1;
