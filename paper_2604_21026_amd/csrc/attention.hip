@@ -628,6 +628,7 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     }
     // Parts in the workspace are written through to where all XCDs see them, and waited for, before this workgroup
     // arrives; the last one's loads pass its caches by.
+    if (shared_piece[0].b < 0 && shared_piece[1].b < 0) return;  // (the same for the whole workgroup)
     __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
     __syncthreads();
     // The workgroups that have some of a sequence and head tile, which only one can be the first of.
@@ -642,17 +643,17 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
             *to = group_of(at + p.n - 1);
         }
     };
-    if (threadIdx.x == 0) {
-        for (int i = 0; i < 2; ++i) {
-            const PieceOf &p = i ? shared_piece[1] : shared_piece[0];
-            last[i] = 0;
-            if (p.b < 0) continue;
+    if (w < 2) {  // (a wave each, side by side)
+        const PieceOf p = w ? shared_piece[1] : shared_piece[0];
+        bool done = false;
+        if (p.b >= 0 && lane == 0) {
             int from, to;
             groups_with(p, &from, &to);
             const uint32_t before = __hip_atomic_fetch_add(a.arrived + from, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            last[i] = before == (uint32_t)(to - from);
-            if (last[i]) __hip_atomic_store(a.arrived + from, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            done = before == (uint32_t)(to - from);
+            if (done) __hip_atomic_store(a.arrived + from, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
+        if (lane == 0) last[w] = done;
     }
     __syncthreads();
     for (int i = 0; i < 2; ++i) {
@@ -677,7 +678,6 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
             };
             const int e0 = (int)threadIdx.x < heads * D ? (int)threadIdx.x : 0;
             ask(e0 / D * kRow + e0 % D, 0);
-            __syncthreads();
             for (int h = w; h < heads; h += kWaves) {
                 float most = -INFINITY, l = 0.0f;
                 for (int j0 = 0; j0 < count; j0 += 64) {
