@@ -672,6 +672,8 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleAr
     }
 }
 
+constexpr int kFound = 5;  // words of LDS that finish looks for tokens with
+
 // The answer from the n listed tokens, by the first W waves, which are all that is left of the workgroup (kEach tokens to
 // a thread).  key, sum: room for kList each.
 template <int W, int kEach>
@@ -767,7 +769,7 @@ __device__ int finish(const RowState &state, const Ask &k, const Grid &grid, con
         if (i < n) sum[i] = carry + at;
         carry += all;
     }
-    if (tid < 3) found[tid] = ~0u;
+    if (tid < kFound) found[tid] = ~0u;
     if (tid == 0) *kept_at = state.all;
     __syncthreads();
 #pragma unroll
@@ -794,15 +796,20 @@ __device__ int finish(const RowState &state, const Ask &k, const Grid &grid, con
     if (k.top_k > 0 && (uint32_t)k.top_k < state.count) {
 #pragma unroll
         for (int q = 0; q < kEach; ++q)
-            if (q * kThreads + tid < n && rank[q] == (uint32_t)k.top_k - 1) keep(upto[q]);
+            if (q * kThreads + tid < n && rank[q] == (uint32_t)k.top_k - 1) {
+                keep(upto[q]);
+                found[3] = (uint32_t)(q * kThreads + tid + 1);
+            }
         __syncthreads();
     }
+    int end = n;  // the listed tokens before it are those that top_p and min_p keep, those before found[3] top_k
     if (!(k.top_p >= 1.0f)) {
         const uint64_t reach = reach_of(k.top_p, *kept_at);
         const int i = first_token(&found[0], [&](int q) { return upto[q] >= reach; });
 #pragma unroll
         for (int q = 0; q < kEach; ++q)
             if (q * kThreads + tid == i) keep(upto[q]);
+        end = i < n ? i + 1 : n;
         __syncthreads();
     }
     if (k.min_p > 0.0f) {
@@ -812,12 +819,18 @@ __device__ int finish(const RowState &state, const Ask &k, const Grid &grid, con
 #pragma unroll
         for (int q = 0; q < kEach; ++q)
             if (q * kThreads + tid == i - 1) keep(bin[q] >= state.cut ? upto[q] : before[state.cut]);
+        end = i < end ? i : end;
         __syncthreads();
     }
     const uint64_t kept = *kept_at < 1ull << kPoint ? 1ull << kPoint : *kept_at;  // (the first token's weight is 1)
     const uint64_t x = point_of(k.u, kept);
-    const int i = first_token(&found[2], [&](int q) { return upto[q] > x; });
-    return (int)~(uint32_t)key[i < n ? i : n - 1];
+    int i = first_token(&found[2], [&](int q) { return weight[q] && upto[q] > x; });
+    end = found[3] < (uint32_t)end ? (int)found[3] : end;
+    if (i >= end) {  // (a bin's sum and its tokens' have been rounded apart: the last token that is kept and has a weight)
+        i = first_token(&found[4], [&](int q) { return weight[q] == 0; });
+        i = (i < end ? i : end) - 1;
+    }
+    return (int)~(uint32_t)key[i > 0 ? i : 0];
 }
 
 // The same from up to 64 tokens by one wave, a token to a lane, which takes no LDS but for what it looks up.
@@ -841,14 +854,22 @@ __device__ int finish_few(const RowState &state, const Ask &k, const Grid &grid,
     const uint32_t rank = ranked[bin] + ((uint32_t)lane - first);
     const uint64_t live = n < 64 ? (1ull << n) - 1 : ~0ull;
     uint64_t kept = all;
+    int end = n;  // the tokens before it are those that are kept
     auto keep = [&](uint64_t v) { kept = v < kept ? v : kept; };
     if (k.top_k > 0 && (uint32_t)k.top_k < row_count) {
         const uint64_t at = __ballot(rank == (uint32_t)k.top_k - 1) & live;
-        if (at) keep(of_lane(upto, __builtin_ctzll(at)));
+        if (at) {
+            end = __builtin_ctzll(at) + 1;
+            keep(of_lane(upto, end - 1));
+        }
     }
     if (!(k.top_p >= 1.0f)) {
         const uint64_t reach = reach_of(k.top_p, kept), at = __ballot(upto >= reach) & live;
-        if (at) keep(of_lane(upto, __builtin_ctzll(at)));
+        if (at) {
+            const int i = __builtin_ctzll(at);
+            end = i + 1 < end ? i + 1 : end;
+            keep(of_lane(upto, i));
+        }
     }
     if (k.min_p > 0.0f) {
         // (of the bins from `cut` on; before them all have the weight)
@@ -858,10 +879,16 @@ __device__ int finish_few(const RowState &state, const Ask &k, const Grid &grid,
             keep(before[row_cut]);
         else
             keep(of_lane(upto, i - 1));
+        end = i < end ? i : end;
     }
     kept = kept < 1ull << kPoint ? 1ull << kPoint : kept;  // (the first token's weight is 1)
-    const uint64_t x = point_of(k.u, kept), at = __ballot(upto > x) & live;
-    return (int)of_lane(index, at ? __builtin_ctzll(at) : n - 1);
+    const uint64_t x = point_of(k.u, kept), weighty = __ballot(weight != 0) & live, at = __ballot(upto > x) & weighty;
+    int i = at ? __builtin_ctzll(at) : n;
+    if (i >= end) {  // (as in finish; those with a weight are the first)
+        i = __builtin_popcountll(weighty);
+        i = (i < end ? i : end) - 1;
+    }
+    return (int)of_lane(index, i > 0 ? i : 0);
 }
 
 template <bool BF16>
@@ -869,7 +896,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs 
     __shared__ unsigned long long key[kList], sum[kList], wave64[kSampleWaves];
     __shared__ uint32_t wave32[kSampleWaves], last;
     __shared__ unsigned long long kept, before[kBins];
-    __shared__ uint32_t found[3], ranked[kBins + 1];
+    __shared__ uint32_t found[kFound], ranked[kBins + 1];
     __shared__ double roots[kRoots];
     const int m = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x, lane = tid & 63;
     RowState &state = a.rows[m];

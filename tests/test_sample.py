@@ -197,3 +197,40 @@ def test_sample_of_many_equal_logits_among_others(dtype):
         if dtype == torch.float32:
             logits[:, 7] += 2.0 ** -12
             check(logits, u, temperature=np.full(M, 1.5, np.float32), top_p=np.full(M, 0.97, np.float32))
+
+
+@gpu
+@pytest.mark.parametrize("V", [700, 40000, 128256])
+def test_sample_at_the_end_of_what_is_kept(V):
+    """u = 1: the last kept token, whichever filter ends there, however the sums of its bin and of its tokens were rounded."""
+    rng = np.random.default_rng(V)
+    M = 24
+    x = rng.standard_normal((M, V)) * 2.0
+    x[:, rng.choice(V, 60, False)] += np.linspace(14, 2, 60)
+    logits, one = torch.from_numpy(x.astype(np.float32)), np.ones(M, np.float32)
+    f = lambda a: a.astype(np.float32)
+    for kw in (dict(min_p=f(np.geomspace(1e-7, 0.5, M))), dict(top_k=np.geomspace(1, 0.9 * V, M).astype(np.int32)),
+               dict(top_p=f(np.linspace(0.05, 0.999, M))), dict(min_p=f(np.full(M, 1e-3)), top_k=np.full(M, 40, np.int32)),
+               dict(min_p=f(np.full(M, 1e-3)), top_p=f(np.full(M, 0.99)), temperature=f(np.full(M, 1.3))), {}):
+        check(logits, one, **kw)
+        check(logits, one * 3, **kw)
+
+
+@gpu
+def test_sample_at_the_end_passes_over_tokens_without_a_weight():
+    """Below half of 2^-43 a weight counts for nothing: 30.6 below the largest 0.45 of it, as bins of a part's own largest have it."""
+    V, few = 128256, 3000
+    x = torch.full((4, V), -100.0)
+    x[:, 5] = 0.0
+    x[0, -few:] = -30.6
+    x[1, -few:] = -30.6
+    x[1, 40000] = -29.0
+    x[2, -50:] = -30.6
+    x[3, 100:100 + few] = -30.6
+    u = torch.ones(4, device=DEV)
+    want = [5, 40000, 5, 5]
+    for dtype in (torch.float32, torch.bfloat16):  # (in 16 bits -30.625)
+        logits = x.to(dtype).to(DEV)
+        assert nvq.sample(logits, u).tolist() == want
+        assert nvq.sample(logits, u, top_k=torch.full((4,), 30, dtype=torch.int32, device=DEV)).tolist() == want
+        assert nvq.sample(logits, u, min_p=torch.full((4,), 1e-30, device=DEV)).tolist() == want
