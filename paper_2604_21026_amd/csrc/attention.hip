@@ -424,13 +424,17 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
         }
     const int64_t T = (int64_t)total * per;
     if (T == 0) return;
-    // Two steps to a wave at least.  Where there are workgroups for each sequence and head tile to have its own, as many as its
-    // steps take, they are dealt out so, unless the longest part takes longer than the line's equal ranges and the joins
+    // Two steps to a wave at least, in ranges.  Where there are workgroups for each sequence and head tile to have its own, as many
+    // as its steps take, they are dealt out so, unless the longest part takes longer than the line's equal ranges and the joins
     // that these need: a range is read at the memory's rate (its bytes count), a part of one's own at the memory's latency,
     // about twice that rate at most.  (7 sequences of 1000 tokens, 8 key heads of 128: 17 us dealt out, 20.6 in ranges; 30 of
     // 1000: 28 and 33.5; 16 of 100 to 4000: 31 and 25.5; 30 of 100 to 2000: 29.6 and 26.5.)
     constexpr int kPart = 2 * kWaves;
-    const int each = a.most_each < (longest + kPart - 1) / kPart ? a.most_each : (longest + kPart - 1) / kPart;
+    // One workgroup takes up to two steps a wave, which cost what a join through memory does; of more, every step a wave of its
+    // own, where there are as many.  (Two steps to a wave, and one: a sequence of 1000 tokens, 8 key heads of 128, 14.9 and 12.6 us, of
+    // 4000 16.9 and 14.4, 7 of 1000 17.2 and 14.9; 500 tokens of heads of 64 8.7 and, in two workgroups, 10.1.)
+    auto parts_for = [&](int n) { return n <= kPart ? 1 : (n + kWaves - 1) / kWaves; };
+    const int each = a.most_each < parts_for(longest) ? a.most_each : parts_for(longest);
     const bool dealt = each > 0 && (int64_t)longest * gridDim.x <= each * (kPart * (int64_t)gridDim.x + (E4M3 ? 1 : 2) * T * D * kWaves / 1024);
     const int cost = dealt ? kPieceCost : 0;  // (that a part of one's own has no use for)
     const int64_t want = (T + kPart - 1) / kPart;
@@ -440,7 +444,7 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     PieceOf own;      // the sequence and head tile of one's own, if dealt out; `begin`: none
     int64_t own_at;   // its place on the line
     // Of a sequence and head tile's n steps: workgroups that have some of them.
-    auto members_of = [&](int n) { return (n + kPart - 1) / kPart < each ? (n + kPart - 1) / kPart : each; };
+    auto members_of = [&](int n) { return parts_for(n) < each ? parts_for(n) : each; };
     if (dealt) {
         const int piece = each == 1 ? g : g / each, j = g - piece * each;
         own.b = piece / per;
@@ -728,7 +732,7 @@ int launch_attention(AttentionArgs a, hipStream_t st) {
     constexpr int kWaves = waves_of<D>();
     const int cu = device_cu_count(), heads = a.group < kHeadTile ? a.group : kHeadTile;
     const int64_t steps = (int64_t)a.B * (((int64_t)a.width << a.c.page_shift) / kStep + 1 + kPieceCost) * a.c.heads * a.tiles;
-    const int64_t pieces = (int64_t)a.B * a.c.heads * a.tiles, ranges = (steps + 2 * kWaves - 1) / (2 * kWaves),
+    const int64_t pieces = (int64_t)a.B * a.c.heads * a.tiles, ranges = (steps + kWaves - 1) / kWaves,
                   want = ranges > pieces ? ranges : pieces, most = cu < kMaxGroups ? cu : kMaxGroups;
     const dim3 grid((unsigned)(want < most ? want : most)), block(64 * kWaves);
     a.most_each = (int)(grid.x / pieces);
