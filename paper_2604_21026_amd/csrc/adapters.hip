@@ -1,14 +1,14 @@
 // nvq_adapters_add: low-rank adapters beside a layer, each token its own.
 //
-// Two launches, h = A x and y + scale * B h, both on the matrix cores.  Tokens go in groups of 64, a group by the
+// Two launches, h = A x and y + scale * B h, both on the matrix cores (or one, where a workgroup's own h costs less: one_launch).  Tokens go in groups of 64, a group by the
 // distinct adapters of its tokens, and the tokens of one adapter, wherever they stand in the group, are sixteen to a
 // product: an adapter's weights are read once per group however its tokens lie, and 64 tokens of 64 adapters read what
 // they have to.  h stays fp32 between the launches, in as many partial sums as K is cut into; it enters the second
 // product as three bf16 values whose sum it is, so nothing of it is lost; the products with the first and with the rest are
 // summed apart and added at the end, where what an infinite weight makes of a rest of zero is left out.
 //
-// Small ones are two chains of trips to memory (ids, weights, sums; ids, h, results): one token of 2048 x 2048, 16 ranks, 6.5
-// us, 3.6 and 4.2 of them the kernels'.  With many adapters the bytes of B bound it: 32 tokens of 12 adapters of 4096 x 28672, 64
+// Small ones are chains of trips to memory (ids, weights, sums; ids, h, results): one token of 2048 x 2048, 16 ranks, 5.8 us in one
+// launch, of 4096 x 4096 6.8 in two.  With many adapters the bytes of B bound it: 32 tokens of 12 adapters of 4096 x 28672, 64
 // ranks, 53 MB in 18.7 us, 2.8 TB/s; 500 tokens of prompts, 4099 outputs, 15.4 us.
 #include "mfma_act.h"
 
@@ -67,6 +67,37 @@ __device__ __forceinline__ int nth_bit(uint64_t bits, int k) {
     return at;
 }
 
+// A wave's share of h of one tile: columns c0 + w, c0 + w + W, .. before c1 of 32 inputs each, x of the lane's token and a of its
+// ranks; AT_ONCE columns whose loads are in flight together.
+template <int RT, int W, int AT_ONCE>
+__device__ __forceinline__ void down_products(const uint16_t *x, const uint16_t *const (&a)[RT], int c0, int c1, float4v (&sum)[RT]) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) sum[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int c = c0 + (int)(threadIdx.x >> 6); c < c1; c += AT_ONCE * W) {
+        uint4v xv[AT_ONCE], av[AT_ONCE][RT];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int cc = c + k * W < c1 ? c + k * W : c;
+            xv[k] = *as_global<uint4v>(x + 32 * cc);
+#pragma unroll
+            for (int t = 0; t < RT; ++t) av[k][t] = *as_global<uint4v>(a[t] + 32 * cc);
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const bool in = c + k * W < c1;
+            if (!in) xv[k] = uint4v{0, 0, 0, 0};
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                if (!in) av[k][t] = uint4v{0, 0, 0, 0};
+                sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xv[k]),
+                                                                __builtin_bit_cast(bf16x8, av[k][t]), sum[t], 0, 0, 0);
+            }
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < RT; ++t) wait_written(sum[t]);
+}
+
 // h of a group's tokens: RT tiles of sixteen ranks, a slice of K, its columns in turn over the waves.
 template <int RT>
 __global__ __launch_bounds__(kThreads) void adapters_down_kernel(AdaptersArgs g) {
@@ -98,32 +129,7 @@ __global__ __launch_bounds__(kThreads) void adapters_down_kernel(AdaptersArgs g)
             const int m = m0 + nth_bit(with, k0 + n < tokens ? k0 + n : k0);
             const uint16_t *const x = g.x + (int64_t)m * g.K + 8 * kb;
             float4v sum[RT];
-#pragma unroll
-            for (int t = 0; t < RT; ++t) sum[t] = float4v{0.0f, 0.0f, 0.0f, 0.0f};
-            constexpr int kAtOnce = RT == 4 ? 2 : 4;  // columns whose loads are in flight together
-            for (int c = c0 + w; c < c1; c += kAtOnce * kWaves) {
-                uint4v xv[kAtOnce], av[kAtOnce][RT];
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) {
-                    const int cc = c + k * kWaves < c1 ? c + k * kWaves : c;
-                    xv[k] = *as_global<uint4v>(x + 32 * cc);
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) av[k][t] = *as_global<uint4v>(a[t] + 32 * cc);
-                }
-#pragma unroll
-                for (int k = 0; k < kAtOnce; ++k) {
-                    const bool in = c + k * kWaves < c1;
-                    if (!in) xv[k] = uint4v{0, 0, 0, 0};
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) {
-                        if (!in) av[k][t] = uint4v{0, 0, 0, 0};
-                        sum[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xv[k]),
-                                                                        __builtin_bit_cast(bf16x8, av[k][t]), sum[t], 0, 0, 0);
-                    }
-                }
-            }
-#pragma unroll
-            for (int t = 0; t < RT; ++t) wait_written(sum[t]);
+            down_products<RT, kWaves, RT == 4 ? 2 : 4>(x, a, c0, c1, sum);
             __syncthreads();
 #pragma unroll
             for (int t = 0; t < RT; ++t)
@@ -198,10 +204,14 @@ __device__ __forceinline__ void store_results(void *p, int dtype, int64_t at, co
 // columns.  Row 4 q + j of tile t is output 4 NT q + 4 t + j, so that a lane has 4 NT outputs side by side.  A workgroup
 // takes blocks of outputs in turn with the h that it has split once, the next block's weights asked for before this
 // one's results are stored.
-template <int NT>
-__global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
-    constexpr int kPitch = NVQ_MAX_RANK + 8;  // (16 bytes more than a row, against bank conflicts)
-    constexpr int kBlock = kWaves * 16 * NT;
+//
+// RT > 0: h, of RT tiles of sixteen ranks, is not there; every workgroup makes it for its tile, from all of A.
+template <int NT, int RT, int W>
+__global__ __launch_bounds__(64 * W) void adapters_up_kernel(AdaptersArgs g) {
+    constexpr int kThreads = 64 * W;
+    constexpr int kPitch = (RT ? 16 * RT : NVQ_MAX_RANK) + 8;  // (16 bytes more than a row, against bank conflicts)
+    constexpr int kBlock = W * 16 * NT;
+    __shared__ float red[RT ? W : 1][RT ? RT * 4 : 1][64];
     __shared__ __align__(16) uint16_t hs[3][kTile][kPitch];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = lane & 15, kb = lane >> 4;
     int first = (int)(blockIdx.x % g.turns) * kBlock, stride = g.turns * kBlock;
@@ -292,16 +302,34 @@ __global__ __launch_bounds__(kThreads) void adapters_up_kernel(AdaptersArgs g) {
                 if (my && o0 + 4 * NT <= g.N) load_results<4 * NT>(g.y, g.dtype, row + o0, y);
             };
             load_y(first);
+            if constexpr (RT > 0) {
+                const uint16_t *a[RT];
+#pragma unroll
+                for (int t = 0; t < RT; ++t) a[t] = g.a + ((int64_t)e * g.R + (16 * t + n < g.R ? 16 * t + n : g.R - 1)) * g.K + 8 * kb;
+                float4v part[RT];
+                down_products<RT, W, RT == 1 ? 8 : 4>(g.x + (int64_t)(m0 + nth_bit(with, my ? k0 + n : k0)) * g.K + 8 * kb, a, 0, g.K / 32, part);
+                __syncthreads();
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) red[w][4 * t + j][lane] = part[t][j];
+            }
             __syncthreads();
             // four ranks of a token per thread
             const int fours = g.R / 4;
             for (int u = threadIdx.x; u < kTile * fours; u += kThreads) {
                 const int k = u / fours, r = 4 * (u - k * fours);
                 if (k0 + k >= tokens) break;  // (the columns of no token are not looked at)
-                const float *const h = g.h + (int64_t)(m0 + nth_bit(with, k0 + k)) * g.R + r;
                 float4v v = {0.0f, 0.0f, 0.0f, 0.0f};
+                if constexpr (RT > 0) {
+#pragma unroll
+                    for (int q = 0; q < W; ++q)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) v[j] += red[q][4 * (r >> 4) + (k & 3)][16 * (k >> 2) + (r & 15) + j];
+                }
+                const float *const h = g.h + (int64_t)(m0 + nth_bit(with, k0 + k)) * g.R + r;
                 constexpr int kAtOnce = 8;  // (sixteen take registers that a third workgroup needs: 20 us for 15 of 32 tokens)
-                for (int s0 = 0; s0 < g.slices; s0 += kAtOnce) {
+                for (int s0 = 0; RT == 0 && s0 < g.slices; s0 += kAtOnce) {
                     float4v part[kAtOnce];
 #pragma unroll
                     for (int s = 0; s < kAtOnce; ++s) part[s] = *as_global<float4v>(h + (s0 + s < g.slices ? s0 + s : 0) * h_slice);
@@ -404,6 +432,16 @@ int slices_of(const nvq_adapters &s, int M) {
     return want > 1 ? (int)want : 1;
 }
 
+// Whether a batch takes one launch: a group of tokens, adapters whose A a workgroup of eight waves asks for in one trip, and a tile
+// with 128 outputs to a compute unit at most.  (Outputs of one token of 2048 inputs, 16 ranks: 2048 6.8 -> 5.8 us, 28672 7.6 -> 6.3;
+// 32 tokens of 12 adapters 2048 8.4 -> 7.0, but 4096, 384 workgroups, 9.1 and 9.3, 8192 9.1 and 15.2.  One token of 4096 inputs, two
+// trips, 6.8 and 8.1.)
+constexpr int kOneWaves = 8, kOneInputs = 32768;
+bool one_launch(const nvq_adapters &s, int M) {
+    const int64_t blocks = (s.N + 16 * kOneWaves - 1) / (16 * kOneWaves);
+    return groups_of(M) == 1 && s.R <= 32 && (int64_t)s.R * s.K <= kOneInputs && tiles_of(M, s.n) * blocks <= device_cu_count();
+}
+
 bool adapters_shape(const nvq_adapters *s, int M) {
     return s && s->n >= 1 && s->n <= 1 << 16 && s->K >= 32 && s->K % 32 == 0 && s->K <= NVQ_MAX_K && s->N >= 1 && s->N <= 1 << 24 &&
            s->R >= 8 && s->R % 8 == 0 && s->R <= NVQ_MAX_RANK && M >= 1 && M <= 1 << 16 &&
@@ -456,6 +494,16 @@ extern "C" int nvq_adapters_add(const nvq_adapters *adapters, const uint16_t *x_
     const hipStream_t st = (hipStream_t)stream;
     const int groups = groups_of(M), tiles = tiles_of(M, g.n);
     g.copiers = out != y && groups <= 4;
+    if (one_launch(*adapters, M)) {
+        g.turns = (g.N + 16 * kOneWaves - 1) / (16 * kOneWaves);
+        const dim3 grid((unsigned)((g.workers + g.copiers) * g.turns)), threads(64 * kOneWaves);
+        if (rank_tiles(g.R) == 1)
+            hipLaunchKernelGGL((adapters_up_kernel<1, 1, kOneWaves>), grid, threads, 0, st, g);
+        else
+            hipLaunchKernelGGL((adapters_up_kernel<1, 2, kOneWaves>), grid, threads, 0, st, g);
+        NVQ_HIP_TRY(hipGetLastError());
+        return NVQ_OK;
+    }
     const dim3 block(kThreads), down((unsigned)(groups * g.workers * g.blocks * g.slices));
     if (rank_tiles(g.R) == 1)
         hipLaunchKernelGGL(adapters_down_kernel<1>, down, block, 0, st, g);
@@ -475,9 +523,9 @@ extern "C" int nvq_adapters_add(const nvq_adapters *adapters, const uint16_t *x_
     g.turns = (blocks + each - 1) / each;
     const dim3 up((unsigned)(groups * (g.workers + g.copiers) * g.turns));
     if (wide)
-        hipLaunchKernelGGL(adapters_up_kernel<4>, up, block, 0, st, g);
+        hipLaunchKernelGGL((adapters_up_kernel<4, 0, kWaves>), up, block, 0, st, g);
     else
-        hipLaunchKernelGGL(adapters_up_kernel<1>, up, block, 0, st, g);
+        hipLaunchKernelGGL((adapters_up_kernel<1, 0, kWaves>), up, block, 0, st, g);
     NVQ_HIP_TRY(hipGetLastError());
     return NVQ_OK;
 }

@@ -141,3 +141,28 @@ def test_adapters_of_infinite_weights(M, N):
                 assert np.isposinf(got[m, 5]) and np.isneginf(got[m, 6]) and np.isnan(got[m, 7])
             else:
                 assert np.isneginf(got[m, N - 1])
+
+
+@gpu
+@pytest.mark.parametrize("M,n,K,N,R", [(64, 64, 96, 500, 32), (64, 64, 96, 513, 32), (1, 3, 1024, 28672, 32), (1, 3, 1056, 300, 32), (16, 9, 2048, 1029, 16),
+                                       (31, 2, 1984, 129, 16), (64, 5, 4096, 640, 8), (64, 5, 4128, 640, 8), (65, 5, 96, 130, 24), (9, 20, 32, 127, 24)])
+def test_adapters_around_the_sizes_of_one_launch(M, n, K, N, R):
+    """With weights that nothing may read: adapters that no token has hold no numbers, and x neither where a token has no adapter."""
+    g = torch.Generator().manual_seed(M * K + N)
+    nan = float("nan")
+    a, b = (torch.randn((n, R, K), generator=g) * K ** -0.5).bfloat16(), (torch.randn((n, N, R), generator=g) * R ** -0.5).bfloat16()
+    x, y = torch.randn((M, K), generator=g).bfloat16(), torch.randn((M, N), generator=g)
+    scales = torch.rand((n,), generator=g) + 0.5
+    ids = torch.randint(0, max(1, n - 1), (M,), generator=g, dtype=torch.int32)
+    ids[torch.rand((M,), generator=g) < 0.2] = n
+    none = ids == n
+    want, size = plain(f64(a), f64(b), f64(scales), f64(x), ids.tolist(), f64(y))
+    unused = [e for e in range(n) if e not in ids.tolist()]
+    a[unused], b[unused], x[none] = nan, nan, nan
+    handle = nvq.Adapters(a.to(DEV), b.to(DEV), scales.to(DEV))
+    got = nvq.adapters_add(handle, x.to(DEV), ids.to(DEV), y.to(DEV))
+    # fp32 sums of K products, then of R, each rounding and its like inside the matrix instructions
+    bound = 2 * (K + R + 16) * EPS32 * size + EPS32 * np.abs(want)
+    assert (np.abs(f64(got) - want) <= bound).all() and torch.equal(got.cpu()[none], y[none])
+    here = y.to(DEV)
+    assert torch.equal(nvq.adapters_add(handle, x.to(DEV), ids.to(DEV), here, out=here), got)
