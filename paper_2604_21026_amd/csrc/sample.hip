@@ -1,7 +1,8 @@
 // nvq_sample: the next token of each row of logits.
 //
 // Every question is one of the descending order of a row's tokens: which token brings the count to top_k, the sum of
-// the weights to top_p, to u times the kept sum.  It is answered without sorting the row, in two launches:
+// the weights to top_p, to u times the kept sum.  It is answered without sorting the row, in two launches (or in one, rows that a
+// workgroup takes alone):
 //   1. Workgroups share a row's logits, a part each: the part's largest, and relative to it a histogram of counts and
 //      weights over bins of 1 / 32 in the logit.  The one that arrives last adds the parts' bins up
 //      and sees in which bins the answers can lie: the weight of a bin that a border falls into is known, which of its
@@ -10,7 +11,7 @@
 //      them by logit and index and answers every question to the token.
 // Weights are 64-bit fixed point relative to the largest, so that sums do not depend on their order.  A row whose bins
 // hold too many tokens (nearly equal logits), or whose logits are out of the bins' range, is looked at by one workgroup
-// alone, eleven bits of the sort words after the other (choose_slowly, in the second launch).
+// alone, eleven bits of the sort words after the other (choose_slowly, in the last launch).
 //
 // Neither bytes nor operations bound a few rows but the chain of trips to memory and through LDS: one row of 128256 in 20.5 us (14
 // and 6.5 in the kernels: logits 1.5, bins 2.6, the parts' arrival 1, their bins 3.5 (196 KB through one compute unit), sums
@@ -381,6 +382,13 @@ __device__ __forceinline__ uint32_t listed_before(const int *lo, const int *hi, 
     return n;
 }
 
+__device__ __forceinline__ bool listed_bin(const int (&lo)[4], const int (&hi)[4], int bin) {
+    bool is = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) is |= bin >= lo[i] && bin <= hi[i];
+    return is;
+}
+
 // Where a row's answers can lie, from the sums before its bins (before[kBins], ranked[kBins]: all), by one wave.
 struct Search {
     int lo[4], hi[4], cut;  // bins
@@ -468,23 +476,25 @@ __device__ __forceinline__ void part_of(const SampleArgs &a, int part, int *i0, 
     *i1 = *i0 + a.part < a.V ? *i0 + a.part : a.V;
 }
 
-template <bool BF16>
-__global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleArgs a) {
-    __shared__ unsigned long long mass[kBins], before[kBins + 1], wave64[kSampleWaves];
-    __shared__ uint32_t count[kBins], ranked[kBins + 1], wave32[kSampleWaves];
-    __shared__ First firsts[kSampleWaves];
-    __shared__ double roots[kRoots];
-    __shared__ uint32_t last;
-    const int m = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x, lane = tid & 63;
-    const Row<BF16> row(a, m);
-    const Ask k = ask_of(a, m);
-    RowState &state = a.rows[m];
-    int i0, i1;
-    part_of(a, part, &i0, &i1);
+// Into the last bin, a wave's together.  (Hundreds of additions to one place take microseconds.)
+__device__ __forceinline__ void add_last(unsigned long long *mass, uint32_t *count, uint32_t c, unsigned long long w) {
+    if (!__any(c != 0)) return;
+    const uint32_t wave_count = scan_wave(c);
+    const unsigned long long wave_mass = scan_wave(w);
+    if ((threadIdx.x & 63) == 63) {
+        atomicAdd(&count[kBins - 1], wave_count);
+        atomicAdd(&mass[kBins - 1], wave_mass);
+    }
+}
 
+// Of logits [i0, i1) of a row the first token, and relative to it the bins, for a temperature above 0; l: the first block of
+// them (of the last one, if there are more).  The workgroup's, who has to meet before the bins are read.
+template <bool BF16>
+__device__ __forceinline__ First fill_bins(const Row<BF16> &row, const Ask &k, int i0, int i1, float (&l)[8], unsigned long long *mass,
+                                           uint32_t *count, double *roots, First *firsts) {
+    const int tid = threadIdx.x, lane = tid & 63;
     // The first block of logits stays in registers from here to the bins, others (of parts that have more) are read
     // twice.
-    float l[8];
     First best = {0, ~0u};
     auto look = [&](int b, const float (&at)[8]) {
 #pragma unroll
@@ -508,18 +518,7 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleAr
     if (lane == 0) firsts[tid >> 6] = best;
     __syncthreads();
     best = first_of<16>(firsts[lane & 15]);
-    // Into the last bin, a wave's together.  (Hundreds of additions to one place take microseconds.)
-    auto add_last = [&](uint32_t c, unsigned long long w) {
-        if (!__any(c != 0)) return;
-        const uint32_t wave_count = scan_wave(c);
-        const unsigned long long wave_mass = scan_wave(w);
-        if (lane == 63) {
-            atomicAdd(&count[kBins - 1], wave_count);
-            atomicAdd(&mass[kBins - 1], wave_mass);
-        }
-    };
-    const bool ordinary = k.temperature > 0.0f;  // (else the first token is the answer)
-    if (ordinary && best.word) {
+    if (k.temperature > 0.0f && best.word) {
         const float most = of_sort_word(best.word);
         const Weights w(most, k.temperature, roots);
         const Grid grid = {Grid::number(most)};
@@ -553,11 +552,52 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleAr
             row.load(b, i1, l);
             add(l);
         }
-        add_last(far, far_mass);
+        add_last(mass, count, far, far_mass);
+    }
+    return best;
+}
+
+// The sums of the weights and tokens of the bins before a thread's own; *all, *n: of all bins.
+__device__ __forceinline__ void scan_bins(unsigned long long own_mass, uint32_t own_count, unsigned long long *wave64, uint32_t *wave32,
+                                          unsigned long long *own_before, uint32_t *own_ranked, unsigned long long *all, uint32_t *n) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    // scan_block of both at once
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const unsigned long long sum = scan_wave(own_mass);
+    const uint32_t num = scan_wave(own_count);
+    if (lane == 63) {
+        wave64[w] = sum;
+        wave32[w] = num;
     }
     __syncthreads();
+    const unsigned long long sums = scan_row(wave64[lane & 15]);
+    const uint32_t nums = scan_row(wave32[lane & 15]);
+    *all = of_lane(sums, 15);
+    *n = of_lane(nums, 15);
+    *own_before = (w ? of_lane(sums, w ? w - 1 : 0) : 0) + sum - own_mass;
+    *own_ranked = (w ? of_lane(nums, w ? w - 1 : 0) : 0) + num - own_count;
+}
+
+template <bool BF16>
+__global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleArgs a) {
+    __shared__ unsigned long long mass[kBins], before[kBins + 1], wave64[kSampleWaves];
+    __shared__ uint32_t count[kBins], ranked[kBins + 1], wave32[kSampleWaves];
+    __shared__ First firsts[kSampleWaves];
+    __shared__ double roots[kRoots];
+    __shared__ uint32_t last;
+    const int m = blockIdx.x / a.parts, part = blockIdx.x % a.parts, tid = threadIdx.x, lane = tid & 63;
+    const Row<BF16> row(a, m);
+    const Ask k = ask_of(a, m);
+    RowState &state = a.rows[m];
+    int i0, i1;
+    part_of(a, part, &i0, &i1);
+
+    float l[8];
+    First best = fill_bins(row, k, i0, i1, l, mass, count, roots, firsts);
+    const bool ordinary = k.temperature > 0.0f;  // (else the first token is the answer)
+    __syncthreads();
     float most = of_sort_word(best.word);
-    if (a.parts > 1) {
+    {  // the parts' bins, joined
         PartBins &to = a.bins[(int64_t)m * a.parts + part];
         const int place = ((int)Grid::number(most) - tid) & (kBins - 1);
         put64(reinterpret_cast<unsigned long long *>(&to.mass[place]), (uint64_t)__double_as_longlong((double)mass[tid]));
@@ -613,7 +653,7 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleAr
         mass[bin] = (unsigned long long)sum;
         count[bin] = num;
         __syncthreads();
-        add_last(rest, (unsigned long long)past);
+        add_last(mass, count, rest, (unsigned long long)past);
         __syncthreads();
     }
     if (best.word == 0 || !ordinary || most == INFINITY) {  // (the same for the whole row)
@@ -624,29 +664,11 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleAr
         return;
     }
     const Grid grid = {Grid::number(most)};
-    const unsigned long long own_mass = mass[tid];
-    const uint32_t own_count = count[tid];
-    unsigned long long all;
-    uint32_t n;
-    {
-        // scan_block of both at once
-        const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-        const unsigned long long sum = scan_wave(own_mass);
-        const uint32_t num = scan_wave(own_count);
-        if (lane == 63) {
-            wave64[w] = sum;
-            wave32[w] = num;
-        }
-        __syncthreads();
-        const unsigned long long sums = scan_row(wave64[lane & 15]);
-        const uint32_t nums = scan_row(wave32[lane & 15]);
-        all = of_lane(sums, 15);
-        n = of_lane(nums, 15);
-        const unsigned long long own_before = (w ? of_lane(sums, w ? w - 1 : 0) : 0) + sum - own_mass;
-        const uint32_t own_ranked = (w ? of_lane(nums, w ? w - 1 : 0) : 0) + num - own_count;
-        state.before[tid] = before[tid] = own_before;
-        state.ranked[tid] = ranked[tid] = own_ranked;
-    }
+    unsigned long long all, own_before;
+    uint32_t n, own_ranked;
+    scan_bins(mass[tid], count[tid], wave64, wave32, &own_before, &own_ranked, &all, &n);
+    state.before[tid] = before[tid] = own_before;
+    state.ranked[tid] = ranked[tid] = own_ranked;
     if (tid == 0) {
         before[kBins] = all;
         ranked[kBins] = n;
@@ -674,10 +696,18 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleAr
 
 constexpr int kFound = 5;  // words of LDS that finish looks for tokens with
 
+// What is known of a row whose tokens have been listed.
+struct Listed {
+    float most;
+    int cut;
+    uint32_t count;
+    unsigned long long all;
+};
+
 // The answer from the n listed tokens, by the first W waves, which are all that is left of the workgroup (kEach tokens to
-// a thread).  key, sum: room for kList each.
-template <int W, int kEach>
-__device__ int finish(const RowState &state, const Ask &k, const Grid &grid, const int (&lo)[4], const int (&hi)[4], int n,
+// a thread).  list(i): token i of them; key, sum: room for kList each, sum also where they may come from.
+template <int W, int kEach, typename LIST>
+__device__ int finish(const Listed &state, LIST list, const Ask &k, const Grid &grid, const int (&lo)[4], const int (&hi)[4], int n,
                       unsigned long long *key, unsigned long long *sum, unsigned long long *wave64, uint32_t *wave32, uint32_t *found,
                       unsigned long long *kept_at, const unsigned long long *before, const uint32_t *ranked, const double *roots,
                       float per_index) {
@@ -695,7 +725,7 @@ __device__ int finish(const RowState &state, const Ask &k, const Grid &grid, con
 #pragma unroll
     for (int q = 0; q < kEach; ++q) {
         const int i = q * kThreads + tid;
-        mine[q] = i < n ? get64(&state.list[i]) : 0;
+        mine[q] = i < n ? list(i) : 0;
         count[i] = 0;
         fine |= i < n && (__float_as_uint(of_sort_word((uint32_t)(mine[q] >> 32))) & 0xffffu);
     }
@@ -834,10 +864,11 @@ __device__ int finish(const RowState &state, const Ask &k, const Grid &grid, con
 }
 
 // The same from up to 64 tokens by one wave, a token to a lane, which takes no LDS but for what it looks up.
-__device__ int finish_few(const RowState &state, const Ask &k, const Grid &grid, const int (&lo)[4], const int (&hi)[4], int n,
+template <typename LIST>
+__device__ int finish_few(const Listed &state, LIST list, const Ask &k, const Grid &grid, const int (&lo)[4], const int (&hi)[4], int n,
                           const unsigned long long *before, const uint32_t *ranked, const double *roots) {
     const int lane = threadIdx.x & 63;
-    const uint64_t mine = lane < n ? get64(&state.list[lane]) : 0;
+    const uint64_t mine = lane < n ? list(lane) : 0;
     const uint64_t all = state.all;
     const uint32_t row_count = state.count;
     const float most = state.most;
@@ -891,6 +922,29 @@ __device__ int finish_few(const RowState &state, const Ask &k, const Grid &grid,
     return (int)of_lane(index, i > 0 ? i : 0);
 }
 
+// The same by whoever is needed, the answer in the first thread.
+template <typename LIST>
+__device__ __forceinline__ int choose(const Listed &row, LIST list, const Ask &k, const Grid &grid, const int (&lo)[4], const int (&hi)[4], int n, int V,
+                                      unsigned long long *key, unsigned long long *sum, unsigned long long *wave64, uint32_t *wave32,
+                                      uint32_t *found, unsigned long long *kept, const unsigned long long *before, const uint32_t *ranked,
+                                      const double *roots) {
+    const int tid = threadIdx.x;
+    // By as few waves as hold the tokens, at first one to a thread: the others have ended, so that barriers wait for few.
+    // (Four to a thread where one would do: 33.4 instead of 32.6 us for 32 rows of 128256.)
+    const float per_index = 1.0f / (float)V;
+    int id = 0;
+    if (n <= 64) {
+        if (tid < 64) id = finish_few(row, list, k, grid, lo, hi, n, before, ranked, roots);
+    } else if (n <= 256) {
+        if (tid < 256) id = finish<4, 1>(row, list, k, grid, lo, hi, n, key, sum, wave64, wave32, found, kept, before, ranked, roots, per_index);
+    } else if (n <= 1024) {
+        if (tid < 1024) id = finish<16, 1>(row, list, k, grid, lo, hi, n, key, sum, wave64, wave32, found, kept, before, ranked, roots, per_index);
+    } else {
+        id = finish<kSampleWaves, kList / kSampleThreads>(row, list, k, grid, lo, hi, n, key, sum, wave64, wave32, found, kept, before, ranked, roots, per_index);
+    }
+    return id;
+}
+
 template <bool BF16>
 __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs a) {
     __shared__ unsigned long long key[kList], sum[kList], wave64[kSampleWaves];
@@ -932,10 +986,7 @@ __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs 
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int bin = grid.bin(l[j]);
-            bool is = false;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) is |= bin >= lo[i] && bin <= hi[i];
-            hits[j] = __ballot(is && l[j] > -INFINITY);
+            hits[j] = __ballot(listed_bin(lo, hi, bin) && l[j] > -INFINITY);
             all += (uint32_t)__builtin_popcountll(hits[j]);
         }
         if (all == 0) continue;  // (the wave's: most have none)
@@ -961,27 +1012,103 @@ __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs 
     if (!last) return;
 
     const int n = (int)get32(&state.listed) < kList ? (int)get32(&state.listed) : kList;
-    // By as few waves as hold the tokens, at first one to a thread: the others have ended, so that barriers wait for few.
-    // (Four to a thread where one would do: 33.4 instead of 32.6 us for 32 rows of 128256.)
-    const float per_index = 1.0f / (float)a.V;
-    int id = 0;
-    if (n <= 64) {
-        if (tid < 64) id = finish_few(state, k, grid, lo, hi, n, before, ranked, roots);
-    } else if (n <= 256) {
-        if (tid < 256) id = finish<4, 1>(state, k, grid, lo, hi, n, key, sum, wave64, wave32, found, &kept, before, ranked, roots, per_index);
-    } else if (n <= 1024) {
-        if (tid < 1024) id = finish<16, 1>(state, k, grid, lo, hi, n, key, sum, wave64, wave32, found, &kept, before, ranked, roots, per_index);
-    } else {
-        id = finish<kSampleWaves, kList / kSampleThreads>(state, k, grid, lo, hi, n, key, sum, wave64, wave32, found, &kept, before, ranked, roots, per_index);
+    const int id = choose(Listed{state.most, state.cut, state.count, state.all}, [&](int i) { return get64(&state.list[i]); }, k, grid, lo, hi, n, a.V,
+                          key, sum, wave64, wave32, found, &kept, before, ranked, roots);
+    if (tid == 0) a.ids[m] = id;
+}
+
+// Both in one launch, a workgroup to a row of one part; of one block the logits stay in registers.  (A row of 1000 10.4 us instead
+// of 12.9, 64 of 8000 14.6 instead of 17.6, 256 of 32000 34.7 instead of 39.)  Two workgroups to a compute unit, which is worth more
+// than the registers that one could have: 1024 rows of 8000 35 us, with one 42.5.
+template <bool BF16>
+__global__ __launch_bounds__(kSampleThreads, 8) void sample_row_kernel(SampleArgs a) {
+    __shared__ unsigned long long key[kList], sum[kList], wave64[kSampleWaves];
+    __shared__ unsigned long long kept, before[kBins + 1];
+    __shared__ uint32_t wave32[kSampleWaves], found[kFound], ranked[kBins + 1], listed;
+    __shared__ First firsts[kSampleWaves];
+    __shared__ double roots[kRoots];
+    __shared__ Search where;
+    __shared__ bool serve;
+    // (until they are summed)
+    unsigned long long *const mass = key;
+    uint32_t *const count = reinterpret_cast<uint32_t *>(key + kBins);
+    const int m = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
+    const Row<BF16> row(a, m);
+    const Ask k = ask_of(a, m);
+    float l[8];
+    const First best = fill_bins(row, k, 0, a.V, l, mass, count, roots, firsts);
+    const float most = of_sort_word(best.word);
+    if (best.word == 0 || !(k.temperature > 0.0f) || most == INFINITY) {  // (the same for the whole row)
+        if (tid == 0) a.ids[m] = best.word == 0 ? -1 : (int)best.index;
+        return;
     }
+    __syncthreads();
+    const Grid grid = {Grid::number(most)};
+    unsigned long long all, own_before;
+    uint32_t tokens, own_ranked;
+    scan_bins(mass[tid], count[tid], wave64, wave32, &own_before, &own_ranked, &all, &tokens);
+    before[tid] = own_before;
+    ranked[tid] = own_ranked;
+    if (tid == 0) {
+        before[kBins] = all;
+        ranked[kBins] = tokens;
+        listed = 0;
+    }
+    __syncthreads();
+    if (tid < 64) {
+        const Search at = search(k, grid, most, before, ranked);
+        const bool can = listed_before(at.lo, at.hi, ranked, kBins) <= (uint32_t)kList && fabsf(grid.top) < kFar;
+        if (tid == 0) {
+            where = at;
+            serve = can;
+        }
+    }
+    __syncthreads();
+    if (!serve) {
+        const int id = choose_slowly(*reinterpret_cast<Shared *>(key), row, k, most, tokens);
+        if (tid == 0) a.ids[m] = id;
+        return;
+    }
+    int lo[4], hi[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        lo[i] = where.lo[i];
+        hi[i] = where.hi[i];
+    }
+    for (int b = 0; b < a.V; b += kBlock) {
+        if (a.V > kBlock) row.load(b, a.V, l);
+        uint64_t hits[8];
+        uint32_t mine = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            hits[j] = __ballot(listed_bin(lo, hi, grid.bin(l[j])) && l[j] > -INFINITY);
+            mine += (uint32_t)__builtin_popcountll(hits[j]);
+        }
+        if (mine == 0) continue;  // (the wave's)
+        uint32_t at = 0;
+        if (lane == 0) at = atomicAdd(&listed, mine);
+        at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t to = at + (uint32_t)__builtin_popcountll(hits[j] & ((1ull << lane) - 1));
+            if ((hits[j] >> lane & 1) && to < (uint32_t)kList)
+                sum[to] = (uint64_t)sort_word(l[j]) << 32 | (uint32_t)~(b + j * kSampleThreads + tid);
+            at += (uint32_t)__builtin_popcountll(hits[j]);
+        }
+    }
+    __syncthreads();
+    const int n = (int)listed < kList ? (int)listed : kList;
+    const int id = choose(Listed{most, where.cut, tokens, all}, [&](int i) { return (uint64_t)sum[i]; }, k, grid, lo, hi, n, a.V, key, sum, wave64,
+                          wave32, found, &kept, before, ranked, roots);
     if (tid == 0) a.ids[m] = id;
 }
 
 // Parts of a row: blocks of kBlock logits, as many workgroups in all as there are compute units where that is enough (64 rows
 // of 128256 in four parts each 48 us, in sixteen 56; in the last workgroup of a row the parts' bins cost as much as a part's).
+// Two blocks are one part, in one launch: a row of 10000 16.1 us instead of 17.6, of 16000 17.8 and 18.0, 200 of these 20.7 and 28.
 int parts_of(int M, int V) {
     const int blocks = (V + kBlock - 1) / kBlock, share = (256 + M - 1) / M;
-    const int p = blocks < share ? blocks : share;
+    const int p = blocks <= 2 ? 1 : blocks < share ? blocks : share;
     return p < kMostParts ? p : kMostParts;
 }
 // Parts that calls of up to M rows of up to V logits have in all.
@@ -1033,6 +1160,14 @@ extern "C" int nvq_sample(const void *logits, int dtype, int64_t ld, int M, int 
     a.heads = reinterpret_cast<PartHead *>(a.bins + (size_t)M * a.parts);
     const dim3 grid((unsigned)(M * a.parts)), block(kSampleThreads);
     const hipStream_t st = (hipStream_t)stream;
+    if (a.parts == 1) {
+        if (dtype == NVQ_BF16)
+            hipLaunchKernelGGL(sample_row_kernel<true>, grid, block, 0, st, a);
+        else
+            hipLaunchKernelGGL(sample_row_kernel<false>, grid, block, 0, st, a);
+        NVQ_HIP_TRY(hipGetLastError());
+        return NVQ_OK;
+    }
     if (dtype == NVQ_BF16)
         hipLaunchKernelGGL(sample_bins_kernel<true>, grid, block, 0, st, a);
     else

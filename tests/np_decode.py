@@ -77,4 +77,5 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     if min_p > 0:
         n = min(n, max(1, int((w >= min_p).sum())))
     u = u if u > 0 else 0.0
-    return order[min(n - 1, int((upto[:n] <= u * upto[n - 1]).sum()))]
+    last = max(1, int((w[:n] >= 2.0 ** -44).sum())) - 1  # (smaller weights count for nothing: such a token is never chosen)
+    return order[min(last, int((upto[:n] <= u * upto[n - 1]).sum()))]

@@ -234,3 +234,23 @@ def test_sample_at_the_end_passes_over_tokens_without_a_weight():
         assert nvq.sample(logits, u).tolist() == want
         assert nvq.sample(logits, u, top_k=torch.full((4,), 30, dtype=torch.int32, device=DEV)).tolist() == want
         assert nvq.sample(logits, u, min_p=torch.full((4,), 1e-30, device=DEV)).tolist() == want
+
+
+@gpu
+@pytest.mark.parametrize("M,V", [(3, 8192), (3, 8193), (5, 10001), (2, 16384), (3, 16385), (257, 9001), (300, 1000), (270, 20001), (1024, 700)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_sample_of_rows_that_one_workgroup_takes(M, V, dtype):
+    """Around one and two blocks of 8192 logits, and of batches with a row to every compute unit; rows that no bins serve among them."""
+    rng = np.random.default_rng(M + V)
+    ws = nvq.sample_workspace(M, V, DEV)
+    for spread in (0.02, 2.5):
+        x = rng.standard_normal((M, V)) * spread
+        x[0] = 700000.0 + rng.standard_normal(V) * 1000
+        x[1, rng.choice(V, V // 2, False)] = -np.inf
+        x[2 % M, 1:] = np.nan
+        logits = torch.from_numpy(x.astype(np.float32)).to(dtype)
+        u = rng.random(M).astype(np.float32)
+        check(logits, u, workspace=ws)
+        check(logits, u, workspace=ws, **asks(rng, M))
+        check(logits, np.ones(M, np.float32), workspace=ws, top_k=rng.integers(1, 60, M).astype(np.int32))
+        assert int(ws[:4096].sum()) == 0
