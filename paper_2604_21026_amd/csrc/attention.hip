@@ -16,7 +16,7 @@
 // The bytes of keys and values bound it: one sequence of 131072 tokens, 8 key heads of 128 in bf16, 537 MB, takes 90 us,
 // 6.0 TB/s, where a plain reading of as much takes 83; 32 ragged ones of up to 16384 tokens in 8 bits, 261 MB, 60 us,
 // 47 of them reading.  Short ones are bound by the memory's latency, four times over (lengths, pages, keys and values,
-// joins): 500 tokens 9 us, 7 sequences of up to 3000 behind a window of 1000 13.8 us.
+// joins): 500 tokens 8.8 us, 7 sequences of up to 3000 behind a window of 1000 11.7 us.
 #include <type_traits>
 
 #include "cache.h"
@@ -427,8 +427,8 @@ __global__ __launch_bounds__(64 * waves_of<D>()) void attention_kernel(Attention
     // Two steps to a wave at least, in ranges.  Where there are workgroups for each sequence and head tile to have its own, as many
     // as its steps take, they are dealt out so, unless the longest part takes longer than the line's equal ranges and the joins
     // that these need: a range is read at the memory's rate (its bytes count), a part of one's own at the memory's latency,
-    // about twice that rate at most.  (7 sequences of 1000 tokens, 8 key heads of 128: 17 us dealt out, 20.6 in ranges; 30 of
-    // 1000: 28 and 33.5; 16 of 100 to 4000: 31 and 25.5; 30 of 100 to 2000: 29.6 and 26.5.)
+    // about twice that rate at most.  (Two steps a wave throughout, 7 sequences of 1000 tokens, 8 key heads of 128: 17 us dealt out,
+    // 20.6 in ranges; 30 of 1000: 28 and 33.5; 16 of 100 to 4000: 31 and 25.5; 30 of 100 to 2000: 29.6 and 26.5.)
     constexpr int kPart = 2 * kWaves;
     // One workgroup takes up to two steps a wave, which cost what a join through memory does; of more, every step a wave of its
     // own, where there are as many.  (Two steps to a wave, and one: a sequence of 1000 tokens, 8 key heads of 128, 14.9 and 12.6 us, of
