@@ -487,13 +487,13 @@ __device__ __forceinline__ void add_last(unsigned long long *mass, uint32_t *cou
     }
 }
 
-// Of logits [i0, i1) of a row the first token, and relative to it the bins, for a temperature above 0; l: the first block of
-// them (of the last one, if there are more).  The workgroup's, who has to meet before the bins are read.
-template <bool BF16>
-__device__ __forceinline__ First fill_bins(const Row<BF16> &row, const Ask &k, int i0, int i1, float (&l)[8], unsigned long long *mass,
+// Of logits [i0, i1) of a row the first token, and relative to it the bins, for a temperature above 0; l: the first N
+// blocks of them (the first of these: the last one of all, if there are more).  The workgroup's, who has to meet before the bins are read.
+template <int N, bool BF16>
+__device__ __forceinline__ First fill_bins(const Row<BF16> &row, const Ask &k, int i0, int i1, float (&l)[N][8], unsigned long long *mass,
                                            uint32_t *count, double *roots, First *firsts) {
     const int tid = threadIdx.x, lane = tid & 63;
-    // The first block of logits stays in registers from here to the bins, others (of parts that have more) are read
+    // The first N blocks of logits stay in registers from here to the bins, others (of parts that have more) are read
     // twice.
     First best = {0, ~0u};
     auto look = [&](int b, const float (&at)[8]) {
@@ -504,13 +504,15 @@ __device__ __forceinline__ First fill_bins(const Row<BF16> &row, const Ask &k, i
             if (v > best.word || (v == best.word && (uint32_t)i < best.index)) best = First{v, (uint32_t)i};
         }
     };
-    row.load(i0, i1, l);
-    for (int b = i0 + kBlock; b < i1; b += kBlock) {
+#pragma unroll
+    for (int q = 0; q < N; ++q) row.load(i0 + q * kBlock, i1, l[q]);
+    for (int b = i0 + N * kBlock; b < i1; b += kBlock) {
         float more[8];
         row.load(b, i1, more);
         look(b, more);
     }
-    look(i0, l);
+#pragma unroll
+    for (int q = 0; q < N; ++q) look(i0 + q * kBlock, l[q]);
     mass[tid] = 0;
     count[tid] = 0;
     if (tid < kRoots) roots[tid] = kRoot[tid];
@@ -547,10 +549,11 @@ __device__ __forceinline__ First fill_bins(const Row<BF16> &row, const Ask &k, i
                 }
             }
         };
-        add(l);
-        for (int b = i0 + kBlock; b < i1; b += kBlock) {
-            row.load(b, i1, l);
-            add(l);
+#pragma unroll
+        for (int q = 0; q < N; ++q) add(l[q]);
+        for (int b = i0 + N * kBlock; b < i1; b += kBlock) {
+            row.load(b, i1, l[0]);
+            add(l[0]);
         }
         add_last(mass, count, far, far_mass);
     }
@@ -592,7 +595,7 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleAr
     int i0, i1;
     part_of(a, part, &i0, &i1);
 
-    float l[8];
+    float l[1][8];
     First best = fill_bins(row, k, i0, i1, l, mass, count, roots, firsts);
     const bool ordinary = k.temperature > 0.0f;  // (else the first token is the answer)
     __syncthreads();
@@ -1017,11 +1020,11 @@ __global__ __launch_bounds__(kSampleThreads) void sample_list_kernel(SampleArgs 
     if (tid == 0) a.ids[m] = id;
 }
 
-// Both in one launch, a workgroup to a row of one part; of one block the logits stay in registers.  (A row of 1000 10.4 us instead
-// of 12.9, 64 of 8000 14.6 instead of 17.6, 256 of 32000 34.7 instead of 39.)  Two workgroups to a compute unit, which is worth more
-// than the registers that one could have: 1024 rows of 8000 35 us, with one 42.5.
-template <bool BF16>
-__global__ __launch_bounds__(kSampleThreads, 8) void sample_row_kernel(SampleArgs a) {
+// Both in one launch, a workgroup to a row of one part.  N > 1: of up to N blocks, which stay in registers; 1: of any number.  (A
+// row of 1000 10.4 us instead of 12.9, 64 of 8000 14.6 instead of 17.6; one of 16000 16.5, read again 17.7.)  More rows than compute
+// units go two workgroups to one, which is worth more than the registers that one could have: 1024 rows of 8000 35 us, with one 42.5.
+template <bool BF16, int N>
+__global__ __launch_bounds__(kSampleThreads, N == 1 ? 8 : 4) void sample_row_kernel(SampleArgs a) {
     __shared__ unsigned long long key[kList], sum[kList], wave64[kSampleWaves];
     __shared__ unsigned long long kept, before[kBins + 1];
     __shared__ uint32_t wave32[kSampleWaves], found[kFound], ranked[kBins + 1], listed;
@@ -1035,7 +1038,7 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_row_kernel(SampleArg
     const int m = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const Row<BF16> row(a, m);
     const Ask k = ask_of(a, m);
-    float l[8];
+    float l[N][8];
     const First best = fill_bins(row, k, 0, a.V, l, mass, count, roots, firsts);
     const float most = of_sort_word(best.word);
     if (best.word == 0 || !(k.temperature > 0.0f) || most == INFINITY) {  // (the same for the whole row)
@@ -1075,16 +1078,15 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_row_kernel(SampleArg
         lo[i] = where.lo[i];
         hi[i] = where.hi[i];
     }
-    for (int b = 0; b < a.V; b += kBlock) {
-        if (a.V > kBlock) row.load(b, a.V, l);
+    auto collect = [&](int b, const float (&from)[8]) {
         uint64_t hits[8];
         uint32_t mine = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            hits[j] = __ballot(listed_bin(lo, hi, grid.bin(l[j])) && l[j] > -INFINITY);
+            hits[j] = __ballot(listed_bin(lo, hi, grid.bin(from[j])) && from[j] > -INFINITY);
             mine += (uint32_t)__builtin_popcountll(hits[j]);
         }
-        if (mine == 0) continue;  // (the wave's)
+        if (mine == 0) return;  // (the wave's)
         uint32_t at = 0;
         if (lane == 0) at = atomicAdd(&listed, mine);
         at = __builtin_amdgcn_readfirstlane(at);
@@ -1092,8 +1094,17 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_row_kernel(SampleArg
         for (int j = 0; j < 8; ++j) {
             const uint32_t to = at + (uint32_t)__builtin_popcountll(hits[j] & ((1ull << lane) - 1));
             if ((hits[j] >> lane & 1) && to < (uint32_t)kList)
-                sum[to] = (uint64_t)sort_word(l[j]) << 32 | (uint32_t)~(b + j * kSampleThreads + tid);
+                sum[to] = (uint64_t)sort_word(from[j]) << 32 | (uint32_t)~(b + j * kSampleThreads + tid);
             at += (uint32_t)__builtin_popcountll(hits[j]);
+        }
+    };
+    if constexpr (N > 1) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) collect(q * kBlock, l[q]);
+    } else {
+        for (int b = 0; b < a.V; b += kBlock) {
+            if (a.V > kBlock) row.load(b, a.V, l[0]);
+            collect(b, l[0]);
         }
     }
     __syncthreads();
@@ -1105,10 +1116,12 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_row_kernel(SampleArg
 
 // Parts of a row: blocks of kBlock logits, as many workgroups in all as there are compute units where that is enough (64 rows
 // of 128256 in four parts each 48 us, in sixteen 56; in the last workgroup of a row the parts' bins cost as much as a part's).
-// Two blocks are one part, in one launch: a row of 10000 16.1 us instead of 17.6, of 16000 17.8 and 18.0, 200 of these 20.7 and 28.
+// Two blocks are one part, in one launch: a row of 10000 14.7 us instead of 17.6, of 16000 16.6 and 18.0, 200 of these 19.7 and 28;
+// and so are three and four, of rows that would have fewer workgroups: 100 of 32000 30.1 and 37.3, 200 of 24000 27.5 and 39.7 (but
+// with one to a block, one of 20000 22.4 and 18.1, 50 of 30000 28.8 and 21.5, 86 of 20000 25.9 and 23.3).
 int parts_of(int M, int V) {
     const int blocks = (V + kBlock - 1) / kBlock, share = (256 + M - 1) / M;
-    const int p = blocks <= 2 ? 1 : blocks < share ? blocks : share;
+    const int p = blocks <= 2 || (blocks <= 4 && share < blocks) ? 1 : blocks < share ? blocks : share;
     return p < kMostParts ? p : kMostParts;
 }
 // Parts that calls of up to M rows of up to V logits have in all.
@@ -1161,10 +1174,20 @@ extern "C" int nvq_sample(const void *logits, int dtype, int64_t ld, int M, int 
     const dim3 grid((unsigned)(M * a.parts)), block(kSampleThreads);
     const hipStream_t st = (hipStream_t)stream;
     if (a.parts == 1) {
+        const int held = M > device_cu_count() || V <= kBlock || V > 4 * kBlock ? 1 : V <= 2 * kBlock ? 2 : 4;
+        auto launch = [&](auto bf16) {
+            constexpr bool kBf16 = decltype(bf16)::value;
+            if (held == 1)
+                hipLaunchKernelGGL((sample_row_kernel<kBf16, 1>), grid, block, 0, st, a);
+            else if (held == 2)
+                hipLaunchKernelGGL((sample_row_kernel<kBf16, 2>), grid, block, 0, st, a);
+            else
+                hipLaunchKernelGGL((sample_row_kernel<kBf16, 4>), grid, block, 0, st, a);
+        };
         if (dtype == NVQ_BF16)
-            hipLaunchKernelGGL(sample_row_kernel<true>, grid, block, 0, st, a);
+            launch(std::true_type());
         else
-            hipLaunchKernelGGL(sample_row_kernel<false>, grid, block, 0, st, a);
+            launch(std::false_type());
         NVQ_HIP_TRY(hipGetLastError());
         return NVQ_OK;
     }

@@ -254,3 +254,14 @@ def test_sample_of_rows_that_one_workgroup_takes(M, V, dtype):
         check(logits, u, workspace=ws, **asks(rng, M))
         check(logits, np.ones(M, np.float32), workspace=ws, top_k=rng.integers(1, 60, M).astype(np.int32))
         assert int(ws[:4096].sum()) == 0
+
+
+@gpu
+@pytest.mark.parametrize("M,V", [(86, 32768), (86, 32769), (85, 24577), (256, 30011), (257, 30011), (256, 40011), (255, 40011)])
+def test_sample_around_the_rows_of_four_blocks_that_one_workgroup_takes(M, V):
+    rng = np.random.default_rng(M + V)
+    ws = nvq.sample_workspace(M, V, DEV)
+    logits, u = torch.from_numpy((rng.standard_normal((M, V)) * 2.5).astype(np.float32)).bfloat16(), rng.random(M).astype(np.float32)
+    check(logits, u, workspace=ws)
+    check(logits, u, workspace=ws, **asks(rng, M))
+    assert int(ws[:4096].sum()) == 0
