@@ -1114,15 +1114,19 @@ __global__ __launch_bounds__(kSampleThreads, N == 1 ? 8 : 4) void sample_row_ker
     if (tid == 0) a.ids[m] = id;
 }
 
-// Parts of a row: blocks of kBlock logits, as many workgroups in all as there are compute units where that is enough (64 rows
-// of 128256 in four parts each 48 us, in sixteen 56; in the last workgroup of a row the parts' bins cost as much as a part's).
+// Parts of a row, of whole blocks of kBlock logits and as many each: as many workgroups in all as there are compute units, or twice
+// as many where they would have more than two blocks each.  (In the last workgroup of a row the parts' bins cost as much as a part's:
+// 32 rows of 128256, 256 and 512 workgroups, 31 and 34 us; 64 45 and 43, 100 79 and 63, 150 98 and 79, 200 107 and 101, 255 115 and
+// 121.  28 rows in ten parts, two of them empty, 38.4, in eight 30.3.)
 // Two blocks are one part, in one launch: a row of 10000 14.7 us instead of 17.6, of 16000 16.6 and 18.0, 200 of these 19.7 and 28;
 // and so are three and four, of rows that would have fewer workgroups: 100 of 32000 30.1 and 37.3, 200 of 24000 27.5 and 39.7 (but
 // with one to a block, one of 20000 22.4 and 18.1, 50 of 30000 28.8 and 21.5, 86 of 20000 25.9 and 23.3).
 int parts_of(int M, int V) {
     const int blocks = (V + kBlock - 1) / kBlock, share = (256 + M - 1) / M;
-    const int p = blocks <= 2 || (blocks <= 4 && share < blocks) ? 1 : blocks < share ? blocks : share;
-    return p < kMostParts ? p : kMostParts;
+    const int more = share > 1 && blocks > 2 * share ? (512 + M - 1) / M : share, most = more < kMostParts ? more : kMostParts;
+    if (blocks <= 2 || (blocks <= 4 && share < blocks)) return 1;
+    const int each = (blocks + most - 1) / most;  // (no part without a block)
+    return (blocks + each - 1) / each;
 }
 // Parts that calls of up to M rows of up to V logits have in all.
 size_t most_parts(int M, int V) {

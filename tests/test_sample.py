@@ -265,3 +265,14 @@ def test_sample_around_the_rows_of_four_blocks_that_one_workgroup_takes(M, V):
     check(logits, u, workspace=ws)
     check(logits, u, workspace=ws, **asks(rng, M))
     assert int(ws[:4096].sum()) == 0
+
+
+@gpu
+@pytest.mark.parametrize("M,V", [(28, 128256), (48, 50000), (100, 50001), (3, 270000), (130, 41000)])
+def test_sample_of_parts_of_several_blocks(M, V):
+    rng = np.random.default_rng(M + V)
+    ws = nvq.sample_workspace(M, V, DEV)
+    logits, u = torch.from_numpy((rng.standard_normal((M, V)) * 3.0).astype(np.float32)), rng.random(M).astype(np.float32)
+    check(logits, u, workspace=ws)
+    check(logits, u, workspace=ws, **asks(rng, M))
+    assert int(ws[:4096].sum()) == 0
