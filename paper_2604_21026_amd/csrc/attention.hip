@@ -8,10 +8,10 @@
 //                 lane row kb = lane / 16 gets the scores of tokens 8 kb .. 8 kb + 7
 //   O^T = V^T P^T the weights P as they come out of S^T: lane row kb multiplies tokens 8 kb .. 8 kb + 7, which is what
 //                 one 16-byte piece of the value layout holds for a channel
-// P enters as bf16 values whose sum it is: three of them (all 24 bits) where results leave as fp32, two (2^-17 of a weight is
-// left out) where they are rounded to bf16, 2^-9, themselves.  The products with the first and with the rest are summed
-// apart and added at the end: what an infinite value makes of the rest (zero times infinity, or the other sign)
-// is left out there.
+// P enters as three bf16 values whose sum it is, all 24 bits.  (With two, 2^-18 of a weight left out, large values that cancel show
+// it, also in results of bf16; 32 ragged sequences in 8 bits 59.6 us instead of 60.3, 131072 tokens the same.)  The products with
+// the first and with the rest are summed apart and added at the end: what an infinite value makes of the rest (zero times
+// infinity, or the other sign) is left out there.
 //
 // The bytes of keys and values bound it: one sequence of 131072 tokens, 8 key heads of 128 in bf16, 537 MB, takes 90 us,
 // 6.0 TB/s, where a plain reading of as much takes 83; 32 ragged ones of up to 16384 tokens in 8 bits, 261 MB, 60 us,
@@ -217,7 +217,6 @@ __device__ __forceinline__ void attend(const AttentionArgs &a, int b, int head, 
     keep_order();
     load_values(fetch, step, first_value_page);
     keep_order();
-    const bool fine = a.out_dtype == NVQ_F32;
     for (int i = 0; i < count; ++i) {
         Fetch<D, E4M3> &f = fetch;
         const int s = step + i, t0 = kStep * s, next = i + 1 < count ? s + 1 : s;
@@ -299,23 +298,16 @@ __device__ __forceinline__ void attend(const AttentionArgs &a, int b, int head, 
             }
             return __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
         };
-        const bf16x8 w0 = part(), w1 = part();
+        const bf16x8 w0 = part(), w1 = part(), w2 = part();
 #pragma unroll
         for (int d = 0; d < T; ++d) {
             const bf16x8 y = P::operand(f.v[d]);
             st.o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, w0, st.o[d], 0, 0, 0);
             st.small(d) = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, w1, st.small(d), 0, 0, 0);
+            st.small(d) = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, w2, st.small(d), 0, 0, 0);
         }
 #pragma unroll
         for (int d = 0; d < T; ++d) wait_written(st.o[d], st.small(d));
-        if (fine) {
-            const bf16x8 w2 = part();
-#pragma unroll
-            for (int d = 0; d < T; ++d)
-                st.small(d) = __builtin_amdgcn_mfma_f32_16x16x32_bf16(P::operand(f.v[d]), w2, st.small(d), 0, 0, 0);
-#pragma unroll
-            for (int d = 0; d < T; ++d) wait_written(st.small(d));
-        }
         keep_order();
         load_values(f, next, value_page);
         keep_order();
