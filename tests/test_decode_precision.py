@@ -59,3 +59,40 @@ def test_attention_weighs_values_with_weights_of_fp32(n, e4m3, dtype, eps):
         assert (np.abs(want) < 2.0 ** -14 * mean).all()
         off = np.abs(y[b] - want) / (halves * ref.EPS32 * (mean + np.abs(want)) + eps * np.abs(want))
         assert off.max() <= 1, (b, off.max())
+
+
+@gpu
+@pytest.mark.parametrize("M,K,N,R", [(1, 2048, 50, 16), (5, 1024, 130, 32), (20, 992, 40, 24), (64, 512, 33, 64), (3, 4096, 700, 128), (70, 320, 2051, 40), (300, 96, 257, 256)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_adapters_take_h_with_all_its_bits(M, K, N, R, dtype):
+    """h of 24 bits, whole numbers, and weights of one and minus one under which all but their last bits cancel: every sum is
+    exact, and so is the result but for its one rounding."""
+    rng = np.random.default_rng(M + N)
+    n = 3
+    # x: three numbers that make h's three parts, in columns of their own; ones and zeros of a say which h has them
+    x, a = np.zeros((M, K)), np.zeros((n, R, K))
+    col = rng.permutation(K)[:3]
+    x[:, col[0]] = rng.integers(128, 256, M) * 2.0 ** 15
+    x[:, col[1]] = (2 * rng.integers(64, 128, M) + 1) * 2.0 ** 7
+    x[:, col[2]] = 2 * rng.integers(0, 64, M) + 1
+    a[:, :, col[0]] = 1
+    a[:, :, col[1:]] = rng.integers(0, 2, (n, R, 2))
+    # b: as many of one as of minus one
+    sign = np.repeat([1.0, -1.0], R // 2)
+    b = np.stack([[rng.permutation(sign) for _ in range(N)] for _ in range(n)])
+    y = rng.integers(-9, 10, (M, N)).astype(np.float64)
+    ids = rng.integers(-1, n, M).astype(np.int32)
+    want = y.copy()
+    for m, e in enumerate(ids):
+        if e >= 0:
+            h = a[e] @ x[m]
+            assert h.max() < 2 ** 24 and (h % 2 ** 7).any()
+            want[m] += b[e] @ h
+    assert np.abs(want).max() < 2 ** 24 and (M < 5 or (want % 2 ** 7).any())
+    as_bf16 = lambda t: dev(t, torch.bfloat16)
+    for t in (x, a, b):
+        assert np.array_equal(f64(as_bf16(t)), t)
+    got = nvq.adapters_add(nvq.Adapters(as_bf16(a), as_bf16(b)), as_bf16(x), dev(ids), dev(y, dtype))
+    if dtype == torch.bfloat16:
+        want = ref.to_bf16(want.astype(np.float32)).astype(np.float64)
+    assert np.array_equal(f64(got), want)
