@@ -697,7 +697,10 @@ __global__ __launch_bounds__(kSampleThreads, 8) void sample_bins_kernel(SampleAr
     }
 }
 
-constexpr int kFound = 5;  // words of LDS that finish looks for tokens with
+constexpr int kFound = 6;  // words of LDS that finish looks for tokens with; the last one: whether a slot is crowded
+// Tokens of a slot that are too many to be ranked by counting.  (Each counts for 0.036 us in a list of up to 1024 tokens, 0.13 in a
+// longer one; sorting these by exchanges takes 14 and 38 us.)
+constexpr uint32_t kCrowd = 320;
 
 // What is known of a row whose tokens have been listed.
 struct Listed {
@@ -725,6 +728,7 @@ __device__ int finish(const Listed &state, LIST list, const Ask &k, const Grid &
     uint64_t mine[kEach];
     uint32_t slot[kEach], nth[kEach];
     bool fine = false;
+    if (tid == 0) found[kFound - 1] = 0;
 #pragma unroll
     for (int q = 0; q < kEach; ++q) {
         const int i = q * kThreads + tid;
@@ -752,40 +756,65 @@ __device__ int finish(const Listed &state, LIST list, const Ask &k, const Grid &
         const uint32_t in = (uint32_t)(down * (float)room);
         slot[q] = from + (in < room ? in : room - 1);
         nth[q] = atomicAdd(&count[slot[q]], 1u);
+        if (nth[q] >= kCrowd) found[kFound - 1] = 1;
     }
     __syncthreads();
-    {
-        uint32_t c[kEach], sum4 = 0, all;
+    if (__builtin_amdgcn_readfirstlane(found[kFound - 1])) {
+        // Equal logits beside one that bf16 does not hold, nearly equal ones, and those of the last bin share a slot, where every
+        // token would read all the others.  Exchanges at halving distances take the same time whatever the tokens are (4000 times
+        // 0.1: 57 us instead of 540).
+        int slots = 64;
+        while (slots < n) slots *= 2;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q)
+            if (q * kThreads + tid < slots) key[q * kThreads + tid] = mine[q];
+        __syncthreads();
+        for (int size = 2; size <= slots; size *= 2)
+            for (int far = size / 2; far; far /= 2) {
+                for (int p = tid; p < slots / 2; p += kThreads) {
+                    const int i = 2 * p - (p & (far - 1)), j = i + far;
+                    const uint64_t a = key[i], b = key[j];
+                    if ((a < b) == !(i & size)) {
+                        key[i] = b;
+                        key[j] = a;
+                    }
+                }
+                __syncthreads();
+            }
+    } else {
+        {
+            uint32_t c[kEach], sum4 = 0, all;
+#pragma unroll
+            for (int q = 0; q < kEach; ++q) {
+                c[q] = count[kEach * tid + q];
+                sum4 += c[q];
+            }
+            uint32_t at = scan_block<W>(wave32, sum4, &all);
+#pragma unroll
+            for (int q = 0; q < kEach; ++q) {
+                begin[kEach * tid + q] = at;
+                at += c[q];
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < kEach; ++q)
+            if (q * kThreads + tid < n) sum[begin[slot[q]] + nth[q]] = mine[q];
+        __syncthreads();
+        uint32_t to[kEach];
 #pragma unroll
         for (int q = 0; q < kEach; ++q) {
-            c[q] = count[kEach * tid + q];
-            sum4 += c[q];
+            if (q * kThreads + tid >= n) continue;
+            const uint32_t j0 = begin[slot[q]], j1 = j0 + count[slot[q]];
+            to[q] = j0;
+            for (uint32_t j = j0; j < j1; ++j) to[q] += sum[j] > mine[q];
         }
-        uint32_t at = scan_block<W>(wave32, sum4, &all);
+        __syncthreads();
 #pragma unroll
-        for (int q = 0; q < kEach; ++q) {
-            begin[kEach * tid + q] = at;
-            at += c[q];
-        }
+        for (int q = 0; q < kEach; ++q)
+            if (q * kThreads + tid < n) key[to[q]] = mine[q];
+        __syncthreads();
     }
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < kEach; ++q)
-        if (q * kThreads + tid < n) sum[begin[slot[q]] + nth[q]] = mine[q];
-    __syncthreads();
-    uint32_t to[kEach];
-#pragma unroll
-    for (int q = 0; q < kEach; ++q) {
-        if (q * kThreads + tid >= n) continue;
-        const uint32_t j0 = begin[slot[q]], j1 = j0 + count[slot[q]];
-        to[q] = j0;
-        for (uint32_t j = j0; j < j1; ++j) to[q] += sum[j] > mine[q];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int q = 0; q < kEach; ++q)
-        if (q * kThreads + tid < n) key[to[q]] = mine[q];
-    __syncthreads();
     // Per token: its weight, the sum of the weights up to it (itself included) in the row, and its rank there.
     const Weights w(state.most, k.temperature, roots);
     uint64_t weight[kEach], upto[kEach], carry = 0;

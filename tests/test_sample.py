@@ -276,3 +276,47 @@ def test_sample_of_parts_of_several_blocks(M, V):
     check(logits, u, workspace=ws)
     check(logits, u, workspace=ws, **asks(rng, M))
     assert int(ws[:4096].sum()) == 0
+
+
+@gpu
+@pytest.mark.parametrize("V", [900, 4000, 4096, 128256])
+def test_sample_of_many_equal_logits_that_bf16_does_not_hold(V):
+    """Lists of up to thousands of equal tokens, alone, in crowds, beside others: by index, whatever their bits."""
+    rng = np.random.default_rng(V)
+    M = 6
+    few = min(V, 4000)
+    x = np.full((M, V), -50.0, np.float32)
+    x[0, :few] = 0.1
+    x[1, rng.choice(V, few, False)] = np.float32(0.1) + np.float32(2.0 ** -20) * rng.integers(0, 3, few).astype(np.float32)
+    x[2, :few] = rng.standard_normal(few).astype(np.float16) * np.float16(0.01)
+    x[3, rng.choice(V, few, False)] = np.where(rng.random(few) < 0.5, np.float32(0.7), rng.random(few).astype(np.float32))
+    x[4, :few] = 0.125  # (one that bf16 holds, and one among them that it does not)
+    x[4, 7] = 0.1250001
+    x[5, :few] = (4 + rng.standard_normal(few) * 0.02).astype(np.float32)
+    logits = torch.from_numpy(x)
+    for _ in range(3):
+        u = rng.random(M).astype(np.float32)
+        check(logits, u)
+        check(logits, u, top_k=rng.integers(1, few, M).astype(np.int32), top_p=np.full(M, 0.9, np.float32))
+    check(logits, np.ones(M, np.float32))
+
+
+@gpu
+def test_sample_of_many_equal_logits_takes_no_time_out_of_proportion():
+    """4000 equal logits, and 4000 different ones: a slot with all of them was ranked in thirty times the time, token by token."""
+    def time_of(x):
+        out, ws, u = torch.empty(1, dtype=torch.int32, device=DEV), nvq.sample_workspace(1, 4000, DEV), torch.full((1,), 0.5, device=DEV)
+        x = x.to(DEV)
+        least = float("inf")
+        for _ in range(10):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            for _ in range(50):
+                nvq.sample(x, u, out=out, workspace=ws)
+            end.record()
+            torch.cuda.synchronize()
+            least = min(least, start.elapsed_time(end))
+        return least
+
+    g = torch.Generator().manual_seed(1)
+    assert time_of(torch.full((1, 4000), 0.1)) < 10 * time_of(torch.randn((1, 4000), generator=g) * 0.02)
