@@ -734,10 +734,11 @@ int nvq_attention(const nvq_cache *cache, const uint16_t *q, int64_t q_stride, i
  * kept weights exceeds u[m] times their sum (u below 0 or NaN counts as 0, from 1 on the
  * last kept one with a weight is taken).  A temperature that is not above 0 takes the
  * first token, and so does a top_p that is not.
- * Weights are fixed point with 43 bits after the point, from fp64 (those below half of
- * that count for nothing and are never chosen); their sums are off by less than 2^-30 of
- * the row's, where those may still count, and do not depend on an order, so the same call
- * gives the same tokens.  NaN and minus infinity are never
+ * Weights are fixed point with 43 bits after the point, from fp64, and those below half of
+ * that are never chosen.  Where several workgroups share a row (how many goes by M and V),
+ * its sums are of weights that each rounds relative to the largest of its own logits: a sum
+ * is off by less than 2^-42 of the largest weight for every token in it.  Sums do not depend
+ * on an order, so the same call gives the same tokens.  NaN and minus infinity are never
  * chosen and do not count; plus infinity is chosen before all; a row without a token to
  * choose gets -1.
  *   logits  [M][V] f32 or bf16 (dtype), ld >= V elements from row to row; 4-byte

@@ -406,7 +406,9 @@ __device__ Search search(const Ask &k, const Grid &grid, float most, const unsig
     const double upto = (double)before[kSkip * lane + kSkip];
     const uint32_t ranks = ranked[kSkip * lane + kSkip];
     auto reaching = [&](double x) { return reached(x, upto, before); };
-    // Bounds of the sums are a little wide: a bin's weight has been rounded otherwise than the sum of its tokens'.
+    // Bounds of the sums are a little wide: a bin's weight has been rounded otherwise than its tokens' (by less than two units
+    // a token, so by 2^13 for the kList that can be listed), and a sum that does not end in the first token is of 2^kPoint or more.
+    static_assert(2 * kList <= 1 << (kPoint - 30), "room for their rounding");
     const double wide = 1.0 + 0x1p-30, all = (double)before[kBins];
     double least = all, greatest = all;
     Search r;
