@@ -774,7 +774,7 @@ int nvq_sample(const void *logits, int dtype, int64_t ld, int M, int V, const fl
  *   workspace  nvq_adapters_workspace_bytes(adapters, M) bytes, 256-byte aligned, scratch
  *              (whatever it holds), for one call at a time
  * K % 32 == 0, K <= NVQ_MAX_K, R % 8 == 0, R <= NVQ_MAX_RANK, N <= 2^24, n <= 2^16, M <=
- * 2^16, M * N <= 2^35; a, b, x, y, out 16-byte aligned.  nvq_adapters_workspace_bytes looks at the
+ * 2^16; a, b, x, y, out 16-byte aligned.  nvq_adapters_workspace_bytes looks at the
  * sizes alone, 0 where they are invalid.
  */
 #define NVQ_MAX_RANK 256

@@ -444,8 +444,7 @@ bool one_launch(const nvq_adapters &s, int M) {
 
 bool adapters_shape(const nvq_adapters *s, int M) {
     return s && s->n >= 1 && s->n <= 1 << 16 && s->K >= 32 && s->K % 32 == 0 && s->K <= NVQ_MAX_K && s->N >= 1 && s->N <= 1 << 24 &&
-           s->R >= 8 && s->R % 8 == 0 && s->R <= NVQ_MAX_RANK && M >= 1 && M <= 1 << 16 &&
-           (int64_t)M * s->N <= 1ll << 35;  // (the launches stay below 2^32 threads)
+           s->R >= 8 && s->R % 8 == 0 && s->R <= NVQ_MAX_RANK && M >= 1 && M <= 1 << 16;
 }
 
 }  // namespace
