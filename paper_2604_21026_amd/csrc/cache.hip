@@ -47,7 +47,10 @@ CacheView view_of(const nvq_cache &c) {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int64_t kMaxRows = 1 << 26;  // of a call: at most 32 threads each, fewer than 2^32 in all
+// Rows of a call (queries, keys, values).  A launch has fewer than 2^32 threads: a key and a value row read together take up to 32
+// and 64 of them, written 16 (of four rows) and 64.
+constexpr int64_t kMaxRows = 1 << 26;
+static_assert(kMaxRows / 2 * (32 + 64) < 1ll << 32, "threads of a launch");
 
 struct Place {
     int page, slot, position;
@@ -130,7 +133,7 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
 // Eight values -> codes under that scale byte (255: zeros).
 __device__ __forceinline__ uint2 codes_of(const float (&x)[8], uint32_t byte) {
     if (byte == 255) return make_uint2(0, 0);
-    const float up = __uint_as_float((254u - byte) << 23);  // (byte 1 to 246: a normal number)
+    const float up = __uint_as_float((254u - byte) << 23);  // (byte 1 to 247: a normal number)
     uint32_t w[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {

@@ -40,3 +40,31 @@ def test_adapters_of_more_than_2_35_results():
     assert not any(bool(part.any()) for part in y.split(300))
     del y
     torch.cuda.empty_cache()
+
+
+@gpu
+@pytest.mark.parametrize("heads,D", [(2, 32), (2, 160), (1, 160)])
+def test_cache_calls_of_the_most_rows(heads, D):
+    """As many tokens as rows are allowed, or 2^24: appended, and read back by twice the rows' threads."""
+    T, page = 1 << 24, 1024
+    assert T * 2 * heads <= 1 << 26
+    cache = nvq.Cache.empty(T // page, heads, page, D, torch.uint8, DEV)
+    table = torch.arange(T // page, dtype=torch.int32, device=DEV).flip(0).contiguous().view(1, -1)
+    zero, at = torch.zeros(T, dtype=torch.int32, device=DEV), torch.arange(T, dtype=torch.int32, device=DEV)
+    # a token's keys are the low digits of its number, its values the high ones: four bits each, which 8 bits hold exactly
+    digit = lambda t, s: (t >> s & 15).bfloat16()
+    k = torch.empty((T, heads, D), dtype=torch.bfloat16, device=DEV)
+    v = torch.empty((T, heads, D), dtype=torch.bfloat16, device=DEV)
+    for x, shifts in ((k, (0, 4, 8)), (v, (12, 16, 20))):
+        for part in range(0, T, 1 << 20):
+            here = at[part:part + (1 << 20)]
+            x[part:part + (1 << 20)] = digit(here, shifts[0])[:, None, None]
+            x[part:part + (1 << 20), :, 1] = digit(here, shifts[1])[:, None]
+            x[part:part + (1 << 20), heads - 1, D - 1] = digit(here, shifts[2])
+    nvq.cache_append(cache, table, at, k, v, sequences=zero)
+    back = (torch.full_like(k, -1), torch.full_like(v, -1))
+    nvq.cache_read(cache, table, at, zero, out=back)
+    for got, want in zip(back, (k, v)):
+        assert all(torch.equal(g, w) for g, w in zip(got.split(1 << 20), want.split(1 << 20)))
+    del k, v, back, cache
+    torch.cuda.empty_cache()
