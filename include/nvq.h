@@ -653,20 +653,21 @@ int nvq_moe_experts(const nvq_experts *experts, const uint16_t *x_bf16, const in
  * the same angles) the pair (a, b) of channels j and j + rot / 2 (interleaved = 1: 2 j
  * and 2 j + 1), j < rot / 2, becomes (a cos_j - b sin_j, b cos_j + a sin_j) of row
  * positions[t], every product and sum rounded to binary32 and the result to bf16 once;
- * channels from rot on stay as they are, and all without cos_sin.  An e4m3 cache holds
- * what these bf16 values become.
+ * channels from rot on stay as they are, and all without cos_sin.  rot is a multiple of 16
+ * up to head_dim, angles at least 1.  An e4m3 cache holds what these bf16 values become.
  *   q       [T][H][head_dim] bf16, q_stride elements from token to token, or NULL with
  *           H = 0; q_out [T][H][head_dim], may be q where q_stride = H * head_dim
  *   k, v    [T][heads][head_dim], k_stride and v_stride elements from token to token
  *           (strides: multiples of 8, at least a token's row)
+ *   q, q_out, k, v and cos_sin are 16-byte aligned
  * A token whose place is not in the cache (sequence outside [0, B), position below 0 or
  * outside the table or, with cos_sin, outside its rows, page outside the pool) is
  * padding: nothing is written for it, its q_out included.  No two tokens of a call may
  * have the same place.
  *
  * nvq_cache_read -- the reverse: k, v [T][heads][head_dim] bf16 of the tokens named as
- * above; e4m3 values are exact in bf16 down to its smallest.  Zeros for a token whose
- * place is not in the cache.
+ * above, 16-byte aligned; e4m3 values are exact in bf16 down to its smallest.  Zeros for a
+ * token whose place is not in the cache.
  * T <= 2^24, T * (H + 2 heads) <= 2^26, H <= NVQ_MAX_HEADS; table, sequences, positions 4-byte aligned.
  */
 enum { NVQ_E4M3 = 2 }; /* nvq_cache.dtype, beside NVQ_BF16 */
@@ -702,7 +703,7 @@ int nvq_cache_read(const nvq_cache *cache, const int32_t *table, int B, int tabl
  * table's width as the width.  The same call gives the same bits.
  *   q       [B][H][head_dim] bf16, q_stride elements from sequence to sequence (a
  *           multiple of 8)
- *   out     [B][H][head_dim] f32 or bf16
+ *   out     [B][H][head_dim] f32 or bf16, 16-byte aligned, as q is
  *   lse     NULL, or [B][H] fp32: log(sum_t exp(s_t)), minus infinity without positions
  *   workspace  nvq_attention_workspace_bytes(cache, B, H) bytes, 256-byte aligned.  Its
  *              first NVQ_ATTENTION_CLEAR_BYTES must be zero before the first call and are

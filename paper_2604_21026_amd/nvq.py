@@ -829,8 +829,8 @@ def cache_append(cache: Cache, table: torch.Tensor, positions: torch.Tensor, k: 
                  q: Optional[torch.Tensor] = None, cos_sin: Optional[torch.Tensor] = None, interleaved: bool = False,
                  sequences: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
     """k, v bf16 [T,heads,head_dim] of tokens positions i32 [T] of sequences i32 [T] (None: token t of sequence t) into
-    the cache through table i32 [B,width]; with cos_sin f32 [angles,rot] (cosines, then sines) k and q bf16
-    [T,H,head_dim] are turned by position first.  Tokens may lie apart (slices of a fused projection).  Returns the
+    the cache through table i32 [B,width]; with cos_sin f32 [angles,rot] (cosines, then sines; rot a multiple of 16) k and
+    q bf16 [T,H,head_dim] are turned by position first.  Tokens may lie apart (slices of a fused projection).  Returns the
     queries (`out`: where to, [T,H,head_dim]; may be q), None without q."""
     if (q is None) == (out is None) and _calls is not None:
         status = _calls.cache_append(cache.address, cache.index, table, positions, k, v, q, cos_sin, int(interleaved),
