@@ -1152,17 +1152,19 @@ __global__ __launch_bounds__(kSampleThreads, N == 1 ? 8 : 4) void sample_row_ker
 // Two blocks are one part, in one launch: a row of 10000 14.7 us instead of 17.6, of 16000 16.6 and 18.0, 200 of these 19.7 and 28;
 // and so are three and four, of rows that would have fewer workgroups: 100 of 32000 30.1 and 37.3, 200 of 24000 27.5 and 39.7 (but
 // with one to a block, one of 20000 22.4 and 18.1, 50 of 30000 28.8 and 21.5, 86 of 20000 25.9 and 23.3).
+constexpr int kMostUnits = 256;
 int parts_of(int M, int V) {
-    const int blocks = (V + kBlock - 1) / kBlock, share = (256 + M - 1) / M;
-    const int more = share > 1 && blocks > 2 * share ? (512 + M - 1) / M : share, most = more < kMostParts ? more : kMostParts;
+    const int units = device_cu_count() < kMostUnits ? device_cu_count() : kMostUnits;
+    const int blocks = (V + kBlock - 1) / kBlock, share = (units + M - 1) / M;
+    const int more = share > 1 && blocks > 2 * share ? (2 * units + M - 1) / M : share, most = more < kMostParts ? more : kMostParts;
     if (blocks <= 2 || (blocks <= 4 && share < blocks)) return 1;
     const int each = (blocks + most - 1) / most;  // (no part without a block)
     return (blocks + each - 1) / each;
 }
-// Parts that calls of up to M rows of up to V logits have in all.
+// Parts that calls of up to M rows of up to V logits have in all, on a device of any size.
 size_t most_parts(int M, int V) {
     const size_t blocks = (size_t)((V + kBlock - 1) / kBlock), per = blocks < kMostParts ? blocks : kMostParts;
-    const size_t rows = (size_t)M * per, share = 1024 + (size_t)M;
+    const size_t rows = (size_t)M * per, share = 4 * kMostUnits + (size_t)M;
     return rows < share ? rows : share;
 }
 
