@@ -91,9 +91,11 @@ struct State {
     }
 };
 
-// Pieces of eight values as they lie in the cache, and as an operand.  load_once: for what one load takes whole lines of and no
-// other reads (the values: 131072 tokens 99.3 -> 91.9 us, 30 sequences of 2000 48.7 -> 45.8; keys, of whose lines a load takes
-// a half or a quarter, would come twice, 61 -> 72 us in 8 bits.  16000 tokens, which a cache may hold, 21.8 -> 22.9).
+// Pieces of eight values as they lie in the cache, and as an operand.  load_once: for what one load takes whole lines of (the
+// values: 131072 tokens 98.1 -> 90.9 us, 30 sequences of 2000 47.8 -> 45.1; keys, of whose lines a load takes a half or a quarter,
+// would come twice, 61 -> 72 us in 8 bits).  It costs where a cache may hold the values, 16000 tokens 20.0 -> 21.1, and where groups
+// of more than sixteen query heads read them once for each tile: of 32, 16000 tokens of 4 key heads 25.0 -> 26.1, 131072 of 8 115.7 -> 123.3,
+// 8 sequences of 8000 49.1 -> 50.2, but 40 of 4000 58.7 -> 57.7.
 template <bool E4M3>
 struct Piece;
 template <>

@@ -520,8 +520,10 @@ int value_lanes(int D) { return D <= 128 ? 8 * key_lanes(D) : 64; }
 // tokens 4.0 + 3.0 and 3.7 + 3.7 us, of 512 5.1 + 3.7 and 4.4 + 3.9, of 1024 8.3 + 5.4 and 6.3 + 4.3, in 8 bits 11.4 + 6.3 and 7.3 +
 // 4.5; 512 tokens of as many sequences 6.8 + 3.3 and 9.5 + 7.2.)
 int step_of(const Places &p) { return p.sequences && p.T >= 512 ? 8 : 1; }
-// Rows past the caches from 8 MiB on, twice a cache's size: queries and keys of 4096 tokens of 40 heads of 128 21 instead of 26 us, of
-// 2048 13.5 and 16.8 (12.7 and 13.9 where caches hold what comes in), of 1000 8.2 and 10.1 (8.4 and 8.4); read back, 4096 9.1 and 9.8.
+// Rows past the caches from 8 MiB on, twice a cache's size.  Queries and keys of 40 heads of 128, past the caches and through them: 1024
+// tokens 8.6 and 9.6 us, 2048 13.7 and 14.0, 4096 21.4 and 22.8, 8192 37.9 and 44.5; read back, 2048 5.4 and 6.0, 4096 8.5 and 9.9, 8192 13.9
+// and 15.0.  With a kernel behind that reads all results: 13.4 and 13.5, 21.1 and 19.7, 33.3 and 36.6, 65.7 and 66.3; 12.4 and 12.6, 17.7
+// and 17.7, 28.4 and 27.1.
 bool once_of(int64_t values) { return 2 * values >= 8 << 20; }
 int64_t value_blocks(const Places &p, int heads, int D) {
     const int step = step_of(p);

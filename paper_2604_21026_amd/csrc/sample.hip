@@ -761,7 +761,7 @@ __device__ int finish(const Listed &state, LIST list, const Ask &k, const Grid &
         if (nth[q] >= kCrowd) found[kFound - 1] = 1;
     }
     __syncthreads();
-    if (__builtin_amdgcn_readfirstlane(found[kFound - 1])) {
+    if (kSlots > (int)kCrowd && __builtin_amdgcn_readfirstlane(found[kFound - 1])) {
         // Equal logits beside one that bf16 does not hold, nearly equal ones, and those of the last bin share a slot, where every
         // token would read all the others.  Exchanges at halving distances take the same time whatever the tokens are (4000 times
         // 0.1: 57 us instead of 540).
