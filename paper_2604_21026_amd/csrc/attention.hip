@@ -14,9 +14,9 @@
 // infinity, or the other sign) is left out there.
 //
 // The bytes of keys and values bound it: one sequence of 131072 tokens, 8 key heads of 128 in bf16, 537 MB, takes 90 us,
-// 6.0 TB/s, where a plain reading of as much takes 83; 32 ragged ones of up to 16384 tokens in 8 bits, 261 MB, 60 us,
+// 6.0 TB/s, where a plain reading of as much takes 83; 32 ragged ones of up to 16384 tokens in 8 bits, 261 MB, 60.3 us,
 // 47 of them reading.  Short ones are bound by the memory's latency, four times over (lengths, pages, keys and values,
-// joins): 500 tokens 8.8 us, 7 sequences of up to 3000 behind a window of 1000 11.7 us.
+// joins): 500 tokens 8.9 us, 7 sequences of up to 3000 behind a window of 1000 11.4 us.
 #include <type_traits>
 
 #include "cache.h"
