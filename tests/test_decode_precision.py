@@ -38,17 +38,17 @@ def cancelling(rng, B, n, D, e4m3):
 
 
 @gpu
-@pytest.mark.parametrize("n", [3, 5, 40, 70, 1003, 5000])
+@pytest.mark.parametrize("n,D", [(3, 64), (5, 64), (40, 64), (70, 64), (1003, 64), (5000, 64), (40, 32), (40, 96), (1003, 128), (40, 160), (1003, 256)])
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("dtype,eps", [(torch.float32, 0.0), (torch.bfloat16, ref.EPS16)])
-def test_attention_weighs_values_with_weights_of_fp32(n, e4m3, dtype, eps):
+def test_attention_weighs_values_with_weights_of_fp32(n, D, e4m3, dtype, eps):
     """Counted in halves of a unit of fp32 (2^-24) of the sum of the sizes.  The weight: the power of two that it is, up to
-    1.62, is rounded as a product, its factor log2 e by half as much, 1.5 * 1.62 * ln 2, and the exponential is off by a unit, 2.  The sums: many + 1 products, each
-    addition off by up to a unit, 2 each; the sums of the weights' parts, and of waves and workgroups (of which all but one
-    weigh nothing), 4."""
+    1.62, is rounded as a product, its factor log2 e by half as much, 1.5 * 1.62 * ln 2, and the exponential is off by a
+    unit, 2.  The sums: many + 1 products, each addition off by up to a unit, 2 each; the sums of the weights' parts, and of
+    waves and workgroups (of which all but one weigh nothing), 4."""
     rng = np.random.default_rng(n)
     n = n + 2 if e4m3 else n
-    B, D = 24, 64
+    B = 24
     pool, q, many = cancelling(rng, B, n, D, e4m3)
     y = f64(nvq.attention(pool.device(), dev(q, torch.bfloat16), dev(pool.table), dev(np.full(B, n, np.int32)), scale=1.0, out_dtype=dtype))
     halves = 1.7 + 2 + 2 * (many + 1) + 4

@@ -1,12 +1,13 @@
 """The operators of a decode step at the largest sizes that they take."""
 import ctypes as C
 
+import numpy as np
 import pytest
 import torch
 
 from paper_2604_21026_amd import nvq
+from tests.test_cache import DEV, Pool, bf16, check_attention, dev, f64, same_bits
 
-DEV = "cuda:0"
 gpu = pytest.mark.gpu
 
 
@@ -68,3 +69,45 @@ def test_cache_calls_of_the_most_rows(heads, D):
         assert all(torch.equal(g, w) for g, w in zip(got.split(1 << 20), want.split(1 << 20)))
     del k, v, back, cache
     torch.cuda.empty_cache()
+
+
+@gpu
+@pytest.mark.parametrize("H,heads,lengths", [(1024, 1, [70, 0, 1]), (1024, 1024, [70, 33]), (1024, 8, [300] * 3), (1000, 8, [40] * 70), (1024, 64, [2000])])
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_a_step_of_the_most_heads(H, heads, lengths, e4m3):
+    rng = np.random.default_rng(H + heads)
+    D, page, B = 32, 16, len(lengths)
+    pool = Pool(rng, lengths, heads, D, page, e4m3, room=1)
+    for b, n in enumerate(lengths):
+        pool.put(b, np.arange(n), bf16(rng, (n, heads, D)), bf16(rng, (n, heads, D)))
+    cache, q, k, v = pool.device(), bf16(rng, (B, H, D)), bf16(rng, (B, heads, D)), bf16(rng, (B, heads, D))
+    as_bf16 = lambda x: dev(x, torch.bfloat16)
+    table, at = dev(pool.table), dev(np.array(lengths, np.int32))
+    out = torch.empty((B, H, D), dtype=torch.bfloat16, device=DEV)
+    nvq.cache_append(cache, table, at, as_bf16(k), as_bf16(v), as_bf16(q), out=out)
+    assert same_bits(out, q)
+    for b, n in enumerate(lengths):
+        pool.put(b, np.array([n]), k[b:b + 1], v[b:b + 1])
+    lse = torch.empty((B, H), dtype=torch.float32, device=DEV)
+    y = nvq.attention(cache, out, table, at + 1, out_dtype=torch.float32, lse=lse)
+    check_attention(f64(y), f64(lse), pool, q, [n + 1 for n in lengths], 0, 0.0, D ** -0.5, 0.0)
+
+
+@gpu
+@pytest.mark.parametrize("M,n,K,N,R", [(1 << 16, 3, 32, 70, 8), (40, 1 << 16, 32, 33, 8), (1000, 1 << 16, 64, 260, 16)])
+def test_adapters_of_the_most_tokens_and_of_the_most_adapters(M, n, K, N, R):
+    """Small whole numbers: every sum exact."""
+    g = torch.Generator().manual_seed(M)
+    a, b = (torch.randint(-2, 3, s, generator=g, dtype=torch.int8).to(DEV).bfloat16() for s in ((n, R, K), (n, N, R)))
+    x, y = torch.randint(-2, 3, (M, K), generator=g).to(DEV).bfloat16(), torch.randint(-9, 10, (M, N), generator=g).to(DEV).float()
+    ids = torch.randint(-1, n, (M,), generator=g, dtype=torch.int32).to(DEV)
+    ids[0], ids[M - 1] = n - 1, n
+    got = nvq.adapters_add(nvq.Adapters(a, b), x, ids, y)
+    want = y.double()
+    for part in range(0, M, 1024):
+        e = ids[part:part + 1024].long()
+        live = (e >= 0) & (e < n)
+        e = e[live]
+        h = (a[e].double() * x[part:part + 1024][live].double().unsqueeze(1)).sum(-1)
+        want[part:part + 1024][live] += (b[e].double() * h.unsqueeze(1)).sum(-1)
+    assert torch.equal(got.double(), want)
